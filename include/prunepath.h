@@ -268,6 +268,156 @@ pp_status pp_moefy_permute(const pp_desc *desc, const int32_t *perm, const void 
                            const void *W_down, void *W_gate_out, void *W_up_out, void *W_down_out, void *ws,
                            size_t ws_bytes, void *stream);
 
+/* ------------------------------------------------------------------------
+ * The attention side of a decode step: rotary positions, a paged key/value
+ * cache, and attention of new tokens over it.  A step appends its new tokens
+ * (pp_kv_append), attends (pp_tree_attention) and, when the new tokens were a
+ * tree of drafts, keeps the accepted path (pp_kv_commit).  The paper leaves
+ * attention unchanged; these calls supply the rest of the layer around the
+ * sparse FFN.
+ *
+ * Shapes: heads of head_dim = D elements, n_heads query heads in groups of
+ * n_heads / n_kv_heads that share one key head (query head h reads key head
+ * h / (n_heads / n_kv_heads)).  D is a multiple of 8 (bf16) or 4 (fp32), at
+ * most 256.  Token tensors q, k, v, out are [n_tokens][heads][D] with the
+ * heads of a token contiguous and a caller-given stride between tokens (in
+ * elements, a multiple of 16 bytes), so that the parts of one fused
+ * projection [n_tokens][(n_heads + 2 n_kv_heads) D] can be passed as they are.
+ * ------------------------------------------------------------------------ */
+
+/* A layer's key and value pages: entry j of a sequence lies in page
+   pages[b][j / page_size] at offset j % page_size, head h at
+     base + page * page_stride + offset * token_stride + h * head_stride
+   (strides in elements, multiples of 16 bytes; the same for k and v).  The
+   strides give both usual orders of a page, [page_size][n_kv_heads][D] and
+   [n_kv_heads][page_size][D].  What pages hold past a sequence's length may
+   be anything, NaN included. */
+typedef struct pp_cache {
+    int dtype;        /* pp_dtype of the pages and of q, k, v, out */
+    int n_heads;      /* query heads, a multiple of n_kv_heads     */
+    int n_kv_heads;
+    int head_dim;     /* D                                         */
+    int page_size;    /* tokens per page, >= 1                     */
+    int n_pages;      /* pages behind k and v                      */
+    int64_t page_stride, token_stride, head_stride;
+    void *k, *v;      /* device                                    */
+} pp_cache;
+
+/* The step's sequences.  Sequence b brings the new tokens
+   [q_start[b], q_start[b + 1]) of the token tensors, which follow ctx_len[b]
+   cached ones; new token i is cache entry ctx_len[b] + i.  Tokens from
+   q_start[n_seqs] on are padding: no call reads or writes anything for them.
+   A sequence may bring no token and may have no cached one.  Found on the
+   device: q_start not ascending or past n_tokens, a negative ctx_len, more
+   entries than max_pages pages hold (the sequence is skipped) and a page
+   number outside [0, n_pages) (its entries are not written and read as
+   zeros) record PP_ERR_INVALID_ARG in the workspace status. */
+typedef struct pp_batch {
+    int n_seqs;
+    int n_tokens;           /* rows of the token tensors           */
+    int max_pages;          /* row length of pages                 */
+    const int32_t *q_start; /* [n_seqs + 1] device                 */
+    const int32_t *ctx_len; /* [n_seqs] device                     */
+    const int32_t *pages;   /* [n_seqs][max_pages] device          */
+} pp_batch;
+
+/* Which elements of a head form pair i of the rot_dim / 2 rotated pairs:
+   HALF (i, i + rot_dim / 2), INTERLEAVED (2 i, 2 i + 1). */
+typedef enum pp_rope_layout { PP_ROPE_HALF = 0, PP_ROPE_INTERLEAVED = 1 } pp_rope_layout;
+
+/* Rotation of the first rot_dim elements of a head (the others are copied):
+   pair (a, b) at position s becomes
+     scale * (a cos(s f_i) - b sin(s f_i),  b cos(s f_i) + a sin(s f_i)).
+   The angle is reduced to one turn before it is rounded, so its error does
+   not grow with the position. */
+typedef struct pp_rotation {
+    int rot_dim;           /* a multiple of 4, 4 <= rot_dim <= head_dim      */
+    int layout;            /* pp_rope_layout                                 */
+    float scale;           /* 1, or the attention factor of YaRN             */
+    const float *inv_freq; /* f [rot_dim / 2], radians per position, device  */
+} pp_rotation;
+
+/* How the frequencies f_i = base^(-2 i / rot_dim) are stretched for contexts
+   longer than the trained one.
+   NONE; LINEAR: f_i / factor; NTK: base * factor^(rot_dim / (rot_dim - 2)) in
+   place of base; BANDED: f_i where the wavelength 2 pi / f_i is below
+   trained_len / high, f_i / factor where it is above trained_len / low, and
+   the mean of both weighted by (trained_len f_i / 2 pi - low) / (high - low)
+   between; YARN: f_i (1 - r_i) + f_i / factor r_i with r_i rising linearly
+   from 0 to 1 between the pairs that turn `high` and `low` times over
+   trained_len positions (rounded outwards to whole pairs), and the rotation
+   scaled by 0.1 ln(factor) + 1. */
+typedef enum pp_rope_scaling {
+    PP_ROPE_NONE = 0, PP_ROPE_LINEAR = 1, PP_ROPE_NTK = 2, PP_ROPE_BANDED = 3, PP_ROPE_YARN = 4
+} pp_rope_scaling;
+
+/* HOST routine, run once per model: writes f (inv_freq [rot_dim / 2], host
+   memory, computed in fp64 and rounded once) and *scale for a pp_rotation.
+   low, high and trained_len are read for BANDED and YARN only.  Errors:
+   PP_ERR_INVALID_ARG (NULL output, unknown kind, base or factor not positive
+   and finite, high <= low, low <= 0, trained_len < 1), PP_ERR_SHAPE (rot_dim). */
+pp_status pp_rope_frequencies(int scaling, int rot_dim, double base, double factor, double low, double high,
+                              int trained_len, float *inv_freq, float *scale);
+
+/* y = x rotated by its tokens' positions: x, y [n_tokens][n_heads][head_dim]
+   in dtype, rows x_stride and y_stride elements apart, positions [n_tokens]
+   int32 (any value).  inverse != 0 rotates back (sin replaced by -sin), which
+   is also the backward pass: the gradient of x is the gradient of y rotated
+   back.  y may be x itself with the same stride; other overlaps are
+   PP_ERR_INVALID_ARG.  Arithmetic in fp32, rounded once. */
+pp_status pp_rope(int dtype, const pp_rotation *rot, const int32_t *positions, int n_tokens, int n_heads,
+                  int head_dim, const void *x, int64_t x_stride, void *y, int64_t y_stride, int inverse,
+                  void *stream);
+
+/* Workspace bytes of pp_kv_append, pp_tree_attention and pp_kv_commit for
+   this cache, whatever the batch (0 for an unsupported one).  Initialise it
+   with pp_workspace_init; errors found on the device are read with
+   pp_get_device_status. */
+size_t pp_attn_workspace_size(const pp_cache *cache);
+
+/* Append the new tokens' keys and values to the cache and rotate on the way:
+   k is rotated and written to its page, v copied to its page, q rotated into
+   q_out (q and q_out may both be NULL; q_out may be q itself).  rot NULL: no
+   rotation.  positions [n_tokens] int32, or NULL for ctx_len[b] + i (the
+   nodes of a drafted tree sit at ctx_len[b] + depth instead).  One launch. */
+pp_status pp_kv_append(const pp_cache *cache, const pp_batch *batch, const pp_rotation *rot,
+                       const int32_t *positions, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                       const void *v, int64_t v_stride, void *q_out, int64_t q_out_stride, void *ws,
+                       size_t ws_bytes, void *stream);
+
+/* Attention of the new tokens over the cache, their own entries (appended
+   before) included:
+     out_t = sum_j p_tj v_j,  p_t = softmax over the visible j of scale q_t . k_j
+   for every query head.  Every new token sees all ctx_len[b] cached tokens of
+   its sequence; of the sequence's new tokens it sees
+     mask NULL:  those up to and including itself (a prompt, a single token);
+     otherwise:  token j if bit j % 32 of word j / 32 of its mask row is set;
+                 mask [n_tokens][mask_words] uint32, tokens past 32 mask_words
+                 are not seen, bits past the sequence's tokens are not read
+                 as tokens (a drafted tree: the node's ancestors and itself).
+   A token that sees nothing gets zeros.  Entries that a token does not see
+   do not reach its output, whatever they hold.  Scores, maxima, sums and
+   outputs are fp32; the bf16 path rounds the softmax weights to bf16 for the
+   product with v (and divides by the sum of the rounded weights), out is
+   rounded once.  The same call gives the same bits every time.  out must not
+   overlap q.  scale: positive and finite. */
+pp_status pp_tree_attention(const pp_cache *cache, const pp_batch *batch, const void *q, int64_t q_stride,
+                            const uint32_t *mask, int mask_words, float scale, void *out, int64_t out_stride,
+                            void *ws, size_t ws_bytes, void *stream);
+
+/* Keep the accepted path of a drafted tree: for sequence b the entries of its
+   new tokens path[b][0] < path[b][1] < ... (n_accept[b] of them, numbered
+   within the sequence's new tokens) move to the entries ctx_len[b],
+   ctx_len[b] + 1, ..., and new_len[b] = ctx_len[b] + n_accept[b] (new_len may
+   be NULL; it must not overlap the inputs).  cache gives the first layer's
+   pages; layer l's lie l * layer_stride elements further; n_layers >= 1.  A
+   path that is not ascending or leaves the sequence's new tokens, or
+   n_accept outside [0, max_path], records PP_ERR_INVALID_ARG and leaves the
+   sequence as it was (new_len[b] = ctx_len[b]).  One launch for all layers. */
+pp_status pp_kv_commit(const pp_cache *cache, const pp_batch *batch, int n_layers, int64_t layer_stride,
+                       const int32_t *path, int max_path, const int32_t *n_accept, int32_t *new_len, void *ws,
+                       size_t ws_bytes, void *stream);
+
 /* Synchronise `stream` and return the sticky device status of `ws`. */
 pp_status pp_get_device_status(void *ws, void *stream);
 

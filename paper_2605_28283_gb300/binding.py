@@ -24,6 +24,11 @@ ACTS = {"relu": PP_ACT_RELU, "gelu_tanh": PP_ACT_GELU_TANH, "gelu": PP_ACT_GELU_
 GATES = {"sigmoid": PP_GATE_SIGMOID, "none": PP_GATE_NONE}
 RULES = {"min_prefix": PP_SEL_MIN_PREFIX, "paper": PP_SEL_PAPER, "topk": PP_SEL_TOPK, "lte": PP_SEL_LTE}
 DTYPES = {"f32": PP_F32, "bf16": PP_BF16}
+PP_ROPE_HALF, PP_ROPE_INTERLEAVED = 0, 1
+PP_ROPE_NONE, PP_ROPE_LINEAR, PP_ROPE_NTK, PP_ROPE_BANDED, PP_ROPE_YARN = 0, 1, 2, 3, 4
+ROPE_LAYOUTS = {"half": PP_ROPE_HALF, "interleaved": PP_ROPE_INTERLEAVED}
+ROPE_SCALINGS = {"none": PP_ROPE_NONE, "linear": PP_ROPE_LINEAR, "ntk": PP_ROPE_NTK, "banded": PP_ROPE_BANDED,
+                 "yarn": PP_ROPE_YARN}
 
 
 class pp_desc(ctypes.Structure):
@@ -37,6 +42,23 @@ class pp_selection(ctypes.Structure):
                 ("logits", ctypes.c_void_p)]
 
 
+class pp_cache(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("n_heads", ctypes.c_int), ("n_kv_heads", ctypes.c_int),
+                ("head_dim", ctypes.c_int), ("page_size", ctypes.c_int), ("n_pages", ctypes.c_int),
+                ("page_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p)]
+
+
+class pp_batch(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int), ("n_tokens", ctypes.c_int), ("max_pages", ctypes.c_int),
+                ("q_start", ctypes.c_void_p), ("ctx_len", ctypes.c_void_p), ("pages", ctypes.c_void_p)]
+
+
+class pp_rotation(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int), ("layout", ctypes.c_int), ("scale", ctypes.c_float),
+                ("inv_freq", ctypes.c_void_p)]
+
+
 class PPError(RuntimeError):
     def __init__(self, status, what):
         super().__init__("%s failed: %s" % (what, status_name(status)))
@@ -47,6 +69,8 @@ _lib = None
 _P, _I, _F, _Z, _LL = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_size_t, ctypes.c_longlong
 _PD = ctypes.POINTER(pp_desc)
 _PS = ctypes.POINTER(pp_selection)
+_D = ctypes.c_double
+_PC, _PB, _PR = ctypes.POINTER(pp_cache), ctypes.POINTER(pp_batch), ctypes.POINTER(pp_rotation)
 
 EXPORTS = {
     "pp_workspace_size": (_Z, [_PD, _I]),
@@ -61,6 +85,12 @@ EXPORTS = {
     "pp_router_stats": (_I, [_PD, _P, _I, _F, _P, _P, _Z, _P]),
     "pp_moefy_cluster": (_I, [_PD, _P, _P, _P, _I, _P, _P, _P, _P]),
     "pp_moefy_permute": (_I, [_PD, _P, _P, _P, _P, _P, _P, _P, _P, _Z, _P]),
+    "pp_rope_frequencies": (_I, [_I, _I, _D, _D, _D, _D, _I, _P, _P]),
+    "pp_rope": (_I, [_I, _PR, _P, _I, _I, _I, _P, _LL, _P, _LL, _I, _P]),
+    "pp_attn_workspace_size": (_Z, [_PC]),
+    "pp_kv_append": (_I, [_PC, _PB, _PR, _P, _P, _LL, _P, _LL, _P, _LL, _P, _LL, _P, _Z, _P]),
+    "pp_tree_attention": (_I, [_PC, _PB, _P, _LL, _P, _I, _F, _P, _LL, _P, _Z, _P]),
+    "pp_kv_commit": (_I, [_PC, _PB, _I, _LL, _P, _I, _P, _P, _P, _Z, _P]),
     "pp_get_device_status": (_I, [_P, _P]),
     "pp_debug_wait_timeout": (_I, [_P, _Z, _LL, _P]),
     "pp_debug_decode_timeline": (_I, [_PD, _P, _P, _P, _P, _P, _F, _P, _P, _Z, _P, _Z, _P]),
@@ -246,6 +276,168 @@ def pp_moefy_permute(desc, perm, W_gate, W_up, W_down, W_gate_out, W_up_out, W_d
     _check(load().pp_moefy_permute(ctypes.byref(desc), _ptr(perm), _ptr(W_gate), _ptr(W_up), _ptr(W_down),
                                    _ptr(W_gate_out), _ptr(W_up_out), _ptr(W_down_out), *_wsargs(ws),
                                    _stream(stream)), "pp_moefy_permute")
+
+
+def _torch_dtype(t) -> int:
+    """pp_dtype of a tensor (PP_ERR_DTYPE for any other)."""
+    import torch
+    if t.dtype == torch.bfloat16:
+        return PP_BF16
+    if t.dtype == torch.float32:
+        return PP_F32
+    raise PPError(PP_ERR_DTYPE, "dtype %s" % t.dtype)
+
+
+def _rows(t, n_tokens, n_heads, head_dim, dtype, what):
+    """Pointer and token stride of a token tensor [n_tokens, heads, head_dim] (or [n_tokens, heads * head_dim])
+    whose tokens are each contiguous."""
+    if t.dtype != dtype:
+        raise PPError(PP_ERR_DTYPE, what)
+    if t.numel() != n_tokens * n_heads * head_dim or (t.dim() == 3 and t.shape[1] != n_heads) or \
+            t.dim() not in (2, 3) or t.shape[0] != n_tokens:
+        raise PPError(PP_ERR_SHAPE, what)
+    if t.stride(-1) != 1 or (t.dim() == 3 and n_heads > 1 and t.stride(1) != head_dim):
+        raise PPError(PP_ERR_INVALID_ARG, what + ": the heads of a token must be contiguous")
+    return t.data_ptr(), (t.stride(0) if n_tokens > 1 else n_heads * head_dim)
+
+
+def _int32(t, what):
+    import torch
+    if t.dtype != torch.int32:
+        raise PPError(PP_ERR_DTYPE, what + " must be int32")
+    if not t.is_contiguous():
+        raise PPError(PP_ERR_INVALID_ARG, what + " must be contiguous")
+    return t.data_ptr()
+
+
+class Rotation:
+    """Rotary positions: inv_freq (device, float32, one entry a rotated pair), layout, attention factor."""
+
+    def __init__(self, inv_freq, layout="half", scale=1.0):
+        import torch
+        if inv_freq.dtype != torch.float32 or not inv_freq.is_contiguous():
+            raise PPError(PP_ERR_DTYPE, "inv_freq must be contiguous float32")
+        self.inv_freq = inv_freq
+        self.c = pp_rotation(2 * inv_freq.numel(), ROPE_LAYOUTS.get(layout, layout), float(scale),
+                             inv_freq.data_ptr())
+
+    @classmethod
+    def make(cls, rot_dim, base=10000.0, layout="half", scaling="none", factor=1.0, low=1.0, high=32.0,
+             trained_len=0, device="cuda"):
+        """Frequencies from pp_rope_frequencies, on the device, with the scaling's attention factor."""
+        import torch
+        freq, scale = pp_rope_frequencies(scaling, rot_dim, base, factor, low, high, trained_len)
+        return cls(torch.from_numpy(freq).to(device), layout, scale)
+
+
+class KVCache:
+    """A layer's key and value pages: k, v [n_pages, page_size, n_kv_heads, head_dim] of any strides (the same for
+    both) with contiguous head_dim.  Pages stored head by head are passed as their transposed view."""
+
+    def __init__(self, k, v, n_heads):
+        if k.dim() != 4 or k.shape != v.shape:
+            raise PPError(PP_ERR_SHAPE, "KVCache")
+        if k.dtype != v.dtype:
+            raise PPError(PP_ERR_DTYPE, "KVCache")
+        if k.stride() != v.stride() or k.stride(3) != 1:
+            raise PPError(PP_ERR_INVALID_ARG, "KVCache: strides")
+        self.k, self.v = k, v
+        self.c = pp_cache(_torch_dtype(k), int(n_heads), k.shape[2], k.shape[3], k.shape[1], k.shape[0], k.stride(0),
+                          k.stride(1), k.stride(2), k.data_ptr(), v.data_ptr())
+
+
+class Batch:
+    """The sequences of a step: q_start [n_seqs + 1], ctx_len [n_seqs], pages [n_seqs, max_pages] (device, int32)."""
+
+    def __init__(self, q_start, ctx_len, pages, n_tokens):
+        n = ctx_len.numel()
+        if q_start.numel() != n + 1 or pages.dim() != 2 or pages.shape[0] != n:
+            raise PPError(PP_ERR_SHAPE, "Batch")
+        self.q_start, self.ctx_len, self.pages = q_start, ctx_len, pages
+        self.c = pp_batch(n, int(n_tokens), pages.shape[1], _int32(q_start, "q_start"), _int32(ctx_len, "ctx_len"),
+                          _int32(pages, "pages"))
+
+
+def pp_rope_frequencies(scaling, rot_dim, base=10000.0, factor=1.0, low=1.0, high=32.0, trained_len=0):
+    """(inv_freq, a numpy float32 array of rot_dim / 2; attention factor)."""
+    import numpy as np
+    freq = np.empty(max(0, int(rot_dim)) // 2, np.float32)
+    scale = ctypes.c_float(0.0)
+    _check(load().pp_rope_frequencies(ROPE_SCALINGS.get(scaling, scaling), int(rot_dim), float(base), float(factor),
+                                      float(low), float(high), int(trained_len), _host(freq), ctypes.byref(scale)),
+           "pp_rope_frequencies")
+    return freq, scale.value
+
+
+def pp_rope(rot, positions, x, y, inverse=False, stream=None):
+    """y = x [T, heads, head_dim] rotated by positions [T] (back, with inverse: the gradient); y may be x."""
+    if x.dim() != 3:
+        raise PPError(PP_ERR_SHAPE, "pp_rope: x")
+    T, H, D = x.shape
+    if positions.numel() != T:
+        raise PPError(PP_ERR_SHAPE, "pp_rope: positions")
+    px, sx = _rows(x, T, H, D, x.dtype, "pp_rope: x")
+    py, sy = _rows(y, T, H, D, x.dtype, "pp_rope: y")
+    _check(load().pp_rope(_torch_dtype(x), ctypes.byref(rot.c), _int32(positions, "positions"), T, H, D, px, sx, py,
+                          sy, 1 if inverse else 0, _stream(stream)), "pp_rope")
+
+
+def pp_attn_workspace_size(cache) -> int:
+    return int(load().pp_attn_workspace_size(ctypes.byref(cache.c)))
+
+
+def alloc_attn_workspace(cache, device=None, stream=None):
+    """A zero-initialised workspace tensor for the calls on caches of this shape."""
+    import torch
+    ws = torch.empty(max(256, pp_attn_workspace_size(cache)), dtype=torch.uint8, device=device or cache.k.device)
+    pp_workspace_init(ws, stream)
+    return ws
+
+
+def pp_kv_append(cache, batch, rot, positions, q, k, v, q_out, ws, stream=None):
+    """Append k, v [T, n_kv_heads, head_dim] to their pages, keys rotated; q_out = q rotated (both may be None)."""
+    c, T = cache.c, batch.c.n_tokens
+    dt = cache.k.dtype
+    pq, sq, po, so = None, 0, None, 0
+    if q is not None:
+        pq, sq = _rows(q, T, c.n_heads, c.head_dim, dt, "pp_kv_append: q")
+    if q_out is not None:
+        po, so = _rows(q_out, T, c.n_heads, c.head_dim, dt, "pp_kv_append: q_out")
+    pk, sk = _rows(k, T, c.n_kv_heads, c.head_dim, dt, "pp_kv_append: k")
+    pv, sv = _rows(v, T, c.n_kv_heads, c.head_dim, dt, "pp_kv_append: v")
+    pos = None
+    if positions is not None:
+        if positions.numel() != T:
+            raise PPError(PP_ERR_SHAPE, "pp_kv_append: positions")
+        pos = _int32(positions, "positions")
+    _check(load().pp_kv_append(ctypes.byref(c), ctypes.byref(batch.c), None if rot is None else ctypes.byref(rot.c),
+                               pos, pq, sq, pk, sk, pv, sv, po, so, *_wsargs(ws), _stream(stream)), "pp_kv_append")
+
+
+def pp_tree_attention(cache, batch, q, mask, scale, out, ws, stream=None):
+    """out = attention of q [T, n_heads, head_dim] over the cache; mask [T, words] int32 bits, or None (chains)."""
+    c, T = cache.c, batch.c.n_tokens
+    pq, sq = _rows(q, T, c.n_heads, c.head_dim, cache.k.dtype, "pp_tree_attention: q")
+    po, so = _rows(out, T, c.n_heads, c.head_dim, cache.k.dtype, "pp_tree_attention: out")
+    pm, words = None, 0
+    if mask is not None:
+        if mask.dim() != 2 or mask.shape[0] != T:
+            raise PPError(PP_ERR_SHAPE, "pp_tree_attention: mask")
+        pm, words = _int32(mask, "mask"), mask.shape[1]
+    _check(load().pp_tree_attention(ctypes.byref(c), ctypes.byref(batch.c), pq, sq, pm, words, float(scale), po, so,
+                                    *_wsargs(ws), _stream(stream)), "pp_tree_attention")
+
+
+def pp_kv_commit(cache, batch, path, n_accept, ws, new_len=None, n_layers=1, layer_stride=0, stream=None):
+    """Move the accepted path [n_seqs, max_path] of each tree behind its context, in every layer's cache."""
+    n = batch.c.n_seqs
+    if path.dim() != 2 or path.shape[0] != n or n_accept.numel() != n or \
+            (new_len is not None and new_len.numel() != n):
+        raise PPError(PP_ERR_SHAPE, "pp_kv_commit")
+    _check(load().pp_kv_commit(ctypes.byref(cache.c), ctypes.byref(batch.c), int(n_layers), int(layer_stride),
+                               _int32(path, "path"), path.shape[1], _int32(n_accept, "n_accept"),
+                               None if new_len is None else _int32(new_len, "new_len"), *_wsargs(ws),
+                               _stream(stream)), "pp_kv_commit")
 
 
 def pp_get_device_status(ws, stream=None) -> int:

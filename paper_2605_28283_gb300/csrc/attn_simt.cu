@@ -1,0 +1,280 @@
+// Attention over the paged cache on the CUDA cores, fp32 arithmetic: the fp32
+// path.  One CTA streams its stretch of the key line (pp_attn_sched.cuh) tile
+// by tile: TOK keys and values into shared memory, scores, the running
+// maximum and weight sum of each row, weighted values into registers.
+//
+// Register tiles are 4 rows x 1 key (scores, the head dimension split over
+// the threads that a small row tile leaves free) and 4 rows x 4 elements
+// (values, the keys split likewise); the splits are joined through shared
+// memory.  Several CTAs per SM overlap the loads of one with the arithmetic
+// of the others.
+#include "pp_attn_sched.cuh"
+#include "pp_launch.cuh"
+
+namespace pp {
+namespace {
+
+constexpr int kThreads = 256;
+
+// Rows of a tile, keys of a tile, padded head dimension.
+template <typename T, int ROWS, int TOK, int DP>
+struct Simt {
+    static constexpr int kRG = ROWS / 4;                        // groups of 4 rows
+    static constexpr int kScoreCols = TOK * kRG;                 // (row group, key) pairs
+    static constexpr int kDSplit = kThreads / kScoreCols;        // head-dimension split of the scores
+    static constexpr int kD4 = DP / 4;
+    static constexpr int kTSplit = kThreads / (kD4 * kRG);       // key split of the values
+    static constexpr int kKStride = DP + 4;
+    static_assert(kDSplit >= 1 && kTSplit >= 1 && kRG >= 1, "thread layout");
+    static constexpr int kQ = 0;
+    static constexpr int kK = kQ + ROWS * DP;
+    static constexpr int kV = kK + TOK * kKStride;
+    static constexpr int kS = kV + TOK * DP;                     // partial scores [kDSplit][ROWS][TOK]
+    static constexpr int kP = kS + kDSplit * ROWS * TOK;         // weights [TOK][ROWS]
+    static constexpr int kStat = kP + TOK * ROWS;                // max, sum, factor [ROWS] each
+    static constexpr int kFloats = kStat + 3 * ROWS;
+    static_assert((kTSplit - 1) * ROWS * DP <= TOK * (kKStride + DP), "joining area");
+};
+
+template <typename T, int ROWS, int TOK, int DP>
+__global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_constant__ AttnArgs a) {
+    using L = Simt<T, ROWS, TOK, DP>;
+    constexpr int kVec = Elem<T>::kPer16B;
+    extern __shared__ __align__(16) float sm[];
+    __shared__ long long scratch[36];
+    __shared__ unsigned last_s;
+    float *Qs = sm + L::kQ, *Ks = sm + L::kK, *Vs = sm + L::kV, *Ss = sm + L::kS, *Ps = sm + L::kP;
+    float *Mx = sm + L::kStat, *Sum = Mx + ROWS, *Fac = Sum + ROWS;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    pdl_launch_dependents();
+    pdl_wait();
+    Walk<ROWS, TOK> walk = start_walk<ROWS, TOK>(&a, scratch);
+    const int D = a.head_dim;
+    // score threads: key, row group, part of the head dimension
+    const int s_key = tid % TOK, s_rg = tid / TOK % L::kRG, s_ds = tid / L::kScoreCols;
+    // value threads: 4 elements, row group, part of the keys
+    const int v_d = tid % L::kD4 * 4, v_rg = tid / L::kD4 % L::kRG, v_ts = tid / (L::kD4 * L::kRG);
+    Part p;
+    while (walk.next(p)) {
+        const int rows = min(ROWS, p.seq.n * a.group - p.j * ROWS);
+        __syncthreads();  // the last part's readers are done
+        for (int e = tid; e < ROWS * (DP / kVec); e += kThreads) {
+            const int r = e / (DP / kVec), d = e % (DP / kVec) * kVec;
+            float f[kVec] = {};
+            if (r < rows && d < D)
+                Elem<T>::unpack(*reinterpret_cast<const uint4*>(
+                                    a.q + row_offset(a, p, p.j * ROWS + r, a.q_stride, (int)sizeof(T)) + d * sizeof(T)),
+                                f);
+#pragma unroll
+            for (int i = 0; i < kVec; i++) Qs[r * DP + d + i] = f[i] * a.scale_log2;
+        }
+        if (tid < ROWS) {
+            Mx[tid] = -INFINITY;
+            Sum[tid] = 0.f;
+        }
+        float o[4][4] = {};
+        for (int t = p.t0; t < p.t1; t++) {
+            const int k0 = t * TOK;
+            __syncthreads();  // the last tile's readers are done (first tile: rows are in place)
+            for (int e = tid; e < TOK * (DP / kVec); e += kThreads) {
+                const int r = e / (DP / kVec), d = e % (DP / kVec) * kVec, j = k0 + r;
+                float fk[kVec] = {}, fv[kVec] = {};
+                if (j < p.key_end && d < D) {
+                    const int page = entry_page(a.batch, p.b, j);
+                    if (page >= 0) {
+                        const long long at = entry_offset(a.batch, a.cache, page, j) + (long long)p.h * a.cache.head_stride +
+                                             d * (long long)sizeof(T);
+                        Elem<T>::unpack(*reinterpret_cast<const uint4*>(a.cache.k + at), fk);
+                        Elem<T>::unpack(*reinterpret_cast<const uint4*>(a.cache.v + at), fv);
+                    } else {
+                        record_status(a.status, PP_ERR_INVALID_ARG);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < kVec; i += 4) {
+                    *reinterpret_cast<float4*>(Ks + r * L::kKStride + d + i) = make_float4(fk[i], fk[i + 1], fk[i + 2], fk[i + 3]);
+                    *reinterpret_cast<float4*>(Vs + r * DP + d + i) = make_float4(fv[i], fv[i + 1], fv[i + 2], fv[i + 3]);
+                }
+            }
+            __syncthreads();
+            if (s_ds < L::kDSplit) {
+                float acc[4] = {};
+                constexpr int kPart = DP / L::kDSplit;
+                const float* kr = Ks + s_key * L::kKStride + s_ds * kPart;
+                const float* qr = Qs + s_rg * 4 * DP + s_ds * kPart;
+#pragma unroll 8
+                for (int d = 0; d < kPart; d += 4) {
+                    const float4 kv = *reinterpret_cast<const float4*>(kr + d);
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        const float4 qv = *reinterpret_cast<const float4*>(qr + i * DP + d);
+                        acc[i] = fmaf(qv.x, kv.x, fmaf(qv.y, kv.y, fmaf(qv.z, kv.z, fmaf(qv.w, kv.w, acc[i]))));
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; i++) Ss[(s_ds * ROWS + s_rg * 4 + i) * TOK + s_key] = acc[i];
+            }
+            __syncthreads();
+            // running maximum and weights, one warp a row
+            for (int r = warp; r < ROWS; r += kThreads / 32) {
+                const int row = p.j * ROWS + r, tok = row / a.group;
+                float s[TOK / 32];
+                float mx = -INFINITY;
+#pragma unroll
+                for (int i = 0; i < TOK / 32; i++) {
+                    const int c = i * 32 + lane, j = k0 + c - p.seq.ctx;  // new token's number when >= 0
+                    bool see = r < rows && k0 + c < p.key_end;
+                    if (see && j >= 0)
+                        see = a.mask ? j < 32 * a.mask_words &&
+                                           (a.mask[(size_t)(p.seq.q0 + tok) * a.mask_words + (j >> 5)] >> (j & 31) & 1u)
+                                     : j <= tok;
+                    s[i] = 0.f;
+#pragma unroll
+                    for (int x = 0; x < L::kDSplit; x++) s[i] += Ss[(x * ROWS + r) * TOK + c];
+                    if (!see) s[i] = -INFINITY;
+                    mx = fmaxf(mx, s[i]);
+                }
+                const float m_old = Mx[r], m_new = fmaxf(m_old, warp_max(mx));
+                const float m = m_new == -INFINITY ? 0.f : m_new;
+                float sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < TOK / 32; i++) {
+                    const float w = exp2f(s[i] - m);
+                    Ps[(i * 32 + lane) * ROWS + r] = w;
+                    sum += w;
+                }
+                sum = warp_sum(sum);
+                if (lane == 0) {
+                    const float f = exp2f(m_old - m);
+                    Mx[r] = m_new;
+                    Fac[r] = f;
+                    Sum[r] = Sum[r] * f + sum;
+                }
+                __syncwarp();
+            }
+            __syncthreads();
+            if (v_ts < L::kTSplit) {
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const float f = Fac[v_rg * 4 + i];
+#pragma unroll
+                    for (int x = 0; x < 4; x++) o[i][x] *= f;
+                }
+                // past the cached tokens a weight of zero may stand for an unseen
+                // entry, whose values (NaN, say) must not reach the sum
+                const bool strict = k0 + TOK > p.seq.ctx;
+#pragma unroll 4
+                for (int c = v_ts; c < TOK; c += L::kTSplit) {
+                    const float4 v = *reinterpret_cast<const float4*>(Vs + c * DP + v_d);
+                    const float4 w4 = *reinterpret_cast<const float4*>(Ps + c * ROWS + v_rg * 4);
+                    const float w[4] = {w4.x, w4.y, w4.z, w4.w};
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        if (strict && w[i] == 0.f) continue;
+                        o[i][0] = fmaf(w[i], v.x, o[i][0]);
+                        o[i][1] = fmaf(w[i], v.y, o[i][1]);
+                        o[i][2] = fmaf(w[i], v.z, o[i][2]);
+                        o[i][3] = fmaf(w[i], v.w, o[i][3]);
+                    }
+                }
+            }
+        }
+        // join the key splits in the key and value area
+        if (L::kTSplit > 1) {
+            __syncthreads();
+            float* J = Ks;
+            if (v_ts > 0 && v_ts < L::kTSplit) {
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+                    *reinterpret_cast<float4*>(J + ((v_ts - 1) * ROWS + v_rg * 4 + i) * DP + v_d) =
+                        make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
+            }
+            __syncthreads();
+            if (v_ts == 0) {
+#pragma unroll
+                for (int x = 0; x < L::kTSplit - 1; x++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        const float4 v = *reinterpret_cast<const float4*>(J + (x * ROWS + v_rg * 4 + i) * DP + v_d);
+                        o[i][0] += v.x;
+                        o[i][1] += v.y;
+                        o[i][2] += v.z;
+                        o[i][3] += v.w;
+                    }
+            }
+        }
+        if (p.whole()) {
+            if (v_ts == 0 && v_d < D) {
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const int r = v_rg * 4 + i;
+                    if (r >= rows) break;
+                    const float l = Sum[r], inv = l == 0.f ? 0.f : 1.f / l;
+                    char* dst = a.out + row_offset(a, p, p.j * ROWS + r, a.out_stride, (int)sizeof(T)) + v_d * (int)sizeof(T);
+                    if (sizeof(T) == 4)
+                        *reinterpret_cast<float4*>(dst) = make_float4(o[i][0] * inv, o[i][1] * inv, o[i][2] * inv, o[i][3] * inv);
+                    else
+                        *reinterpret_cast<uint2*>(dst) = make_uint2(Elem<__nv_bfloat16>::pair(o[i][0] * inv, o[i][1] * inv),
+                                                                    Elem<__nv_bfloat16>::pair(o[i][2] * inv, o[i][3] * inv));
+                }
+            }
+            continue;
+        }
+        const Split<ROWS, TOK> sp(walk.sched, p);
+        float* pl = sp.place(a, blockIdx.x);
+        if (v_ts == 0 && v_d < D) {
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                *reinterpret_cast<float4*>(pl + (size_t)(v_rg * 4 + i) * D + v_d) = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
+        }
+        if (tid < ROWS) {
+            pl[(size_t)ROWS * D + tid] = Mx[tid];
+            pl[(size_t)ROWS * (D + 1) + tid] = Sum[tid];
+        }
+        __threadfence();
+        __syncthreads();
+        if (tid == 0) {
+            last_s = atomicAdd(a.counters + sp.c0, 1u) == (unsigned)(sp.c1 - sp.c0);
+            if (last_s) a.counters[sp.c0] = 0;
+            __threadfence();
+        }
+        __syncthreads();
+        if (last_s) merge_parts<T, ROWS, TOK>(a, p, sp, tid, kThreads);
+    }
+}
+
+template <typename T, int ROWS, int TOK, int DP>
+cudaError_t go(const AttnArgs& a, int sms, cudaStream_t st) {
+    using L = Simt<T, ROWS, TOK, DP>;
+    auto* kern = attn_simt_kernel<T, ROWS, TOK, DP>;
+    constexpr int kBytes = L::kFloats * 4;
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+    if (e != cudaSuccess) return e;
+    const int per_sm = 227 * 1024 / (kBytes + 2048);
+    int grid = sms * (per_sm < 1 ? 1 : per_sm > 4 ? 4 : per_sm);
+    if (grid > kAttnMaxGrid) grid = kAttnMaxGrid;
+    return launch_overlapped(kern, dim3((unsigned)grid), dim3(kThreads), kBytes, st, a);
+}
+
+template <typename T>
+cudaError_t go_dim(const AttnArgs& a, int sms, cudaStream_t st) {
+    // rows a sequence brings to a key head on average: small tiles spread
+    // their threads over keys and elements instead of rows that do not exist
+    const long long rows = ((long long)a.batch.n_tokens * a.group + a.batch.n_seqs - 1) / a.batch.n_seqs;
+    const bool few = rows <= 4;
+    if (a.head_dim <= 64) return few ? go<T, 4, 64, 64>(a, sms, st) : go<T, 16, 64, 64>(a, sms, st);
+    if (a.head_dim <= 128) return few ? go<T, 4, 64, 128>(a, sms, st) : go<T, 16, 64, 128>(a, sms, st);
+    return few ? go<T, 4, 64, 256>(a, sms, st) : go<T, 16, 64, 256>(a, sms, st);
+}
+
+}  // namespace
+
+size_t attn_part_floats(int head_dim) {
+    return (size_t)2 * kAttnMaxGrid * kAttnSimtRows * (head_dim + 2);
+}
+
+cudaError_t attn_simt_launch(const AttnArgs& a, int dtype, int sms, cudaStream_t st) {
+    return dtype == PP_BF16 ? go_dim<__nv_bfloat16>(a, sms, st) : go_dim<float>(a, sms, st);
+}
+
+}  // namespace pp

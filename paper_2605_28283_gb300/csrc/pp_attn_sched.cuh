@@ -1,0 +1,248 @@
+// Division of an attention call over the CTAs of one launch.
+//
+// An item is a tile of up to ROWS query rows of one (sequence, key head): the
+// rows are the (new token, query head of the group) pairs, token-major.  Its
+// work is the key tiles of TOK tokens that any of its rows may see.  All
+// items' tiles form one line, ordered by sequence, key head and row tile, and
+// CTA c of C takes the c-th of C equal stretches of it, so that every SM
+// streams the same number of keys however ragged the batch is, without the
+// host knowing a length.  A stretch covers whole items and at most one part
+// of an item at each end.  A part that is not its whole item leaves its
+// unnormalised sum, maximum and weight sum in the workspace; the CTA that
+// arrives last adds an item's parts up in stretch order (so the result does
+// not depend on who that is).
+#pragma once
+
+#include "pp_batch.cuh"
+
+namespace pp {
+
+// Tiles of the key line: the schedule is recomputed by whoever walks it, from
+// the lengths alone.
+template <int ROWS, int TOK>
+struct Sched {
+    const AttnArgs* a;
+    long long total;  // key tiles of the call
+    int ctas;         // CTAs with work: min(grid, total)
+
+    PP_DEVINL int row_tiles(const Seq& s) const { return (int)(((unsigned)s.n * (unsigned)a->group + ROWS - 1) / ROWS); }
+
+    // Entries that row tile j's rows may see (all of a masked tree's).
+    PP_DEVINL int key_end(const Seq& s, int j) const {
+        if (a->mask) return s.ctx + s.n;
+        const unsigned last = ((unsigned)(j + 1) * ROWS - 1u) / (unsigned)a->group;  // rows stay below 2^31
+        return s.ctx + min(s.n, (int)last + 1);
+    }
+    PP_DEVINL int key_tiles(const Seq& s, int j) const { return max(1, (key_end(s, j) + TOK - 1) / TOK); }
+
+    // Key tiles of one key head of a sequence.
+    PP_DEVINL long long head_tiles(const Seq& s) const {
+        const int m = row_tiles(s);
+        if (a->mask || m <= 1) return m ? (long long)m * key_tiles(s, m - 1) : 0;
+        long long sum = 0;
+        for (int j = 0; j < m; j++) sum += key_tiles(s, j);
+        return sum;
+    }
+
+    PP_DEVINL long long begin_of(int c) const { return total * c / ctas; }
+    // CTA whose stretch holds tile u
+    PP_DEVINL int cta_of(long long u) const {
+        int c = (int)(u * ctas / total);
+        while (c + 1 < ctas && begin_of(c + 1) <= u) c++;
+        while (begin_of(c) > u) c--;
+        return c;
+    }
+};
+
+// One CTA's share of an item.
+struct Part {
+    int b, h, j;       // sequence, key head, row tile
+    Seq seq;
+    int key_end;       // entries any row of the tile may see
+    int t0, t1;        // key tiles of the part
+    int tiles;         // key tiles of the item
+    long long first;   // the item's first tile on the line
+    PP_DEVINL bool whole() const { return t0 == 0 && t1 == tiles; }
+};
+
+// Walks the parts of one CTA's stretch.
+template <int ROWS, int TOK>
+struct Walk {
+    Sched<ROWS, TOK> sched;
+    long long at, end;  // the rest of the stretch
+    long long base;     // line position of sequence b
+    int b, h, j;
+    long long head_base;  // line position of the current item
+    Seq seq;
+    int m;
+
+    PP_DEVINL void enter(int b_, long long base_) {
+        b = b_;
+        base = base_;
+        seq = load_seq(sched.a->batch, b);
+        m = sched.row_tiles(seq);
+        h = 0;
+        j = 0;
+        head_base = base;
+        const long long per = sched.head_tiles(seq);
+        if (per > 0) {
+            h = (int)((at - base) / per);
+            head_base = base + (long long)h * per;
+        }
+        while (m > 0 && j + 1 < m && head_base + sched.key_tiles(seq, j) <= at) {
+            head_base += sched.key_tiles(seq, j);
+            j++;
+        }
+    }
+
+    // The next part; false at the end of the stretch.
+    PP_DEVINL bool next(Part& p) {
+        if (at >= end) return false;
+        while (m == 0 || h >= sched.a->n_kv_heads) enter(b + 1, m == 0 ? base : head_base);
+        p.b = b;
+        p.h = h;
+        p.j = j;
+        p.seq = seq;
+        p.key_end = sched.key_end(seq, j);
+        p.tiles = sched.key_tiles(seq, j);
+        p.first = head_base;
+        p.t0 = (int)(at - head_base);
+        p.t1 = (int)min((long long)p.tiles, end - head_base);
+        at = head_base + p.t1;
+        if (p.t1 == p.tiles) {
+            head_base += p.tiles;
+            if (++j == m) {
+                j = 0;
+                h++;
+            }
+        }
+        return true;
+    }
+};
+
+// The line's length and this CTA's first sequence, by all threads of the CTA.
+// scratch: 3 * 32 + 4 words of shared memory (8-byte aligned).
+template <int ROWS, int TOK>
+PP_DEVINL Walk<ROWS, TOK> start_walk(const AttnArgs* a, long long* scratch) {
+    Walk<ROWS, TOK> w;
+    w.sched.a = a;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nwarps = (int)blockDim.x / 32;
+    const int B = a->batch.n_seqs;
+    long long* sums = scratch;       // [32]
+    long long* found = scratch + 32;  // sequence, its line position
+    // pass 0: the total; pass 1: the sequence that holds this CTA's first tile
+    long long lo = 0, total = 0, mine = 0;
+    for (int pass = 0; pass < 2; pass++) {
+        long long before = 0;
+        for (int b0 = 0; b0 < B; b0 += (int)blockDim.x) {
+            if (pass == 0 || B > (int)blockDim.x) {
+                mine = 0;
+                if (b0 + tid < B) {
+                    const Seq s = load_seq(a->batch, b0 + tid);
+                    if (pass == 0 && s.bad && blockIdx.x == 0) record_status(a->status, PP_ERR_INVALID_ARG);
+                    mine = w.sched.head_tiles(s) * a->n_kv_heads;
+                }
+            }
+            long long inc = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long v = __shfl_up_sync(kFull, inc, o);
+                if (lane >= o) inc += v;
+            }
+            if (lane == 31) sums[warp] = inc;
+            __syncthreads();
+            long long pre = before, chunk = 0;
+            for (int i = 0; i < nwarps; i++) {
+                if (i < warp) pre += sums[i];
+                chunk += sums[i];
+            }
+            if (pass == 1) {
+                const long long e = pre + inc, s = e - mine;
+                if (s <= lo && lo < e) {
+                    found[0] = b0 + tid;
+                    found[1] = s;
+                }
+            }
+            before += chunk;
+            __syncthreads();
+        }
+        if (pass == 0) {
+            total = before;
+            w.sched.total = total;
+            w.sched.ctas = (int)min((long long)gridDim.x, total);
+            if ((int)blockIdx.x >= w.sched.ctas) break;  // uniform over the CTA
+            lo = w.sched.begin_of(blockIdx.x);
+        }
+    }
+    w.at = w.end = 0;
+    w.m = 0;
+    if ((int)blockIdx.x < w.sched.ctas) {
+        w.at = lo;
+        w.end = w.sched.begin_of((int)blockIdx.x + 1);
+        w.enter((int)found[0], found[1]);
+    }
+    return w;
+}
+
+// ------------------------------------------------------------ split items
+// Partial results: CTA c has two places, for the item its stretch begins in
+// (2 c) and for the one it ends in (2 c + 1); a place holds the sums
+// [ROWS][D], then the maxima and the weight sums [ROWS] each.
+template <int ROWS>
+PP_DEVINL float* part_place(const AttnArgs& a, int c, bool tail) {
+    return a.part + (size_t)(2 * c + (tail ? 1 : 0)) * ROWS * (a.head_dim + 2);
+}
+
+// Range of CTAs that hold a split item's parts.
+template <int ROWS, int TOK>
+struct Split {
+    int c0, c1;
+    bool c0_tail;  // the first part lies in c0's second place
+    PP_DEVINL Split(const Sched<ROWS, TOK>& s, const Part& p) {
+        c0 = s.cta_of(p.first);
+        c1 = s.cta_of(p.first + p.tiles - 1);
+        c0_tail = s.begin_of(c0) != p.first;
+    }
+    PP_DEVINL float* place(const AttnArgs& a, int c) const { return part_place<ROWS>(a, c, c == c0 && c0_tail); }
+};
+
+// Address of row r of an item in out (or q, with its own stride).
+PP_DEVINL long long row_offset(const AttnArgs& a, const Part& p, int row, long long stride, int esz) {
+    const int tok = row / a.group, g = row - tok * a.group;
+    return (long long)(p.seq.q0 + tok) * stride + ((long long)p.h * a.group + g) * a.head_dim * esz;
+}
+
+// Adds up the parts of an item and writes its rows, by `nthr` threads (tid of
+// them).  The caller has made the parts visible (arrival counter).
+template <typename T, int ROWS, int TOK>
+PP_DEVINL void merge_parts(const AttnArgs& a, const Part& p, const Split<ROWS, TOK>& sp, int tid, int nthr) {
+    const int rows = min(ROWS, p.seq.n * a.group - p.j * ROWS);
+    const int d4s = a.head_dim / 4, D = a.head_dim;
+    for (int e = tid; e < rows * d4s; e += nthr) {
+        const int r = e / d4s, d = (e - r * d4s) * 4;
+        float m = -INFINITY;
+        for (int c = sp.c0; c <= sp.c1; c++) m = fmaxf(m, __ldcg(sp.place(a, c) + (size_t)ROWS * D + r));
+        if (m == -INFINITY) m = 0.f;  // nothing seen (or NaN scores only, whose sums stay NaN)
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        float l = 0.f;
+        for (int c = sp.c0; c <= sp.c1; c++) {
+            const float* pl = sp.place(a, c);
+            const float w = exp2f(__ldcg(pl + (size_t)ROWS * D + r) - m);
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(pl + (size_t)r * D + d));
+            l += w * __ldcg(pl + (size_t)ROWS * (D + 1) + r);
+            o.x += w * v.x;
+            o.y += w * v.y;
+            o.z += w * v.z;
+            o.w += w * v.w;
+        }
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        char* dst = a.out + row_offset(a, p, p.j * ROWS + r, a.out_stride, (int)sizeof(T)) + d * (int)sizeof(T);
+        if (sizeof(T) == 4)
+            *reinterpret_cast<float4*>(dst) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+        else
+            *reinterpret_cast<uint2*>(dst) = make_uint2(Elem<__nv_bfloat16>::pair(o.x * inv, o.y * inv),
+                                                        Elem<__nv_bfloat16>::pair(o.z * inv, o.w * inv));
+    }
+}
+
+}  // namespace pp

@@ -1,0 +1,28 @@
+// Host helper: kernel launch with programmatic dependent launch allowed (the
+// kernel may be scheduled while its predecessor on the stream finishes, and
+// waits for it in griddepcontrol.wait before it touches global memory).
+#pragma once
+
+#include <cuda_runtime.h>
+
+#include <utility>
+
+namespace pp {
+
+template <typename... KArgs, typename... Args>
+cudaError_t launch_overlapped(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st,
+                              Args&&... args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kern, std::forward<Args>(args)...);
+}
+
+}  // namespace pp
