@@ -307,7 +307,8 @@ pp_status pp_tree_attention(const pp_cache* cache, const pp_batch* batch, const 
     a.counters = reinterpret_cast<unsigned*>(static_cast<char*>(ws) + L.counters);
     a.status = status_of(ws);
     a.timeout_ns = kWaitLimitNs;
-    return cuda_status(attn_simt_launch(a, cache->dtype, sms, static_cast<cudaStream_t>(stream)));
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return cuda_status(cache->dtype == PP_BF16 ? attn_tc_launch(a, sms, st) : attn_simt_launch(a, sms, st));
 }
 
 pp_status pp_kv_commit(const pp_cache* cache, const pp_batch* batch, int n_layers, int64_t layer_stride,

@@ -270,11 +270,10 @@ cudaError_t go_dim(const AttnArgs& a, int sms, cudaStream_t st) {
 }  // namespace
 
 size_t attn_part_floats(int head_dim) {
-    return (size_t)2 * kAttnMaxGrid * kAttnSimtRows * (head_dim + 2);
+    const size_t simt = (size_t)kAttnMaxGrid * kAttnSimtRows, tc = (size_t)kAttnTcGrid * kAttnTcRows;
+    return 2 * (simt > tc ? simt : tc) * (head_dim + 2);
 }
 
-cudaError_t attn_simt_launch(const AttnArgs& a, int dtype, int sms, cudaStream_t st) {
-    return dtype == PP_BF16 ? go_dim<__nv_bfloat16>(a, sms, st) : go_dim<float>(a, sms, st);
-}
+cudaError_t attn_simt_launch(const AttnArgs& a, int sms, cudaStream_t st) { return go_dim<float>(a, sms, st); }
 
 }  // namespace pp

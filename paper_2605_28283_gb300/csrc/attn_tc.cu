@@ -1,0 +1,629 @@
+// Attention over the paged cache on the tensor cores (bf16).
+//
+// One persistent CTA per SM walks its stretch of the key line
+// (pp_attn_sched.cuh).  For a tile of BN keys: S = Q K^T (tcgen05, 128 rows x
+// BN, accumulator in TMEM), softmax weights by one thread a row with a running
+// maximum, P (bf16) written back over S in TMEM, O += P V (P from TMEM, V from
+// shared memory as it lies in the cache, O in TMEM).  The maximum is lazy: O
+// and the weight sum are rescaled only when a row's maximum has grown by more
+// than 2^8, so the rescaling round trip through registers almost never runs.
+//
+// Warps: 4 per row tile for the softmax, one that issues the products, one
+// that loads the rows of q, and one producer for each slot of the key/value
+// ring.  A producer fills its slot with 16-byte cp.async into the 128-byte
+// swizzled layout (any page size, stride and head dimension; entries past the
+// sequence are filled with zeros), waits for its own copies and hands the slot
+// over, so that all slots can be in flight at once.
+//
+// Few rows (a single token has as many as heads share a key head): 128-row
+// products cost the tensor cores less than the keys cost HBM (8 of 23 cycles a
+// key at D = 128), but one warp would hold all rows.  For up to 32 rows the
+// rows are therefore repeated in every warp's lanes, each warp weighs its own
+// 32 keys of the tile (P is zero elsewhere) with its own maximum and sum, and
+// the copies are added up at the end of the part.
+#include "pp_attn_sched.cuh"
+#include "pp_launch.cuh"
+#include "pp_tc_attn.cuh"
+
+namespace pp {
+namespace {
+
+constexpr float kLazy = 8.0f;  // growth of a row's maximum (log2) that O and the sum absorb unscaled
+
+template <int DP, int MT>
+struct Tc {
+    static constexpr int BN = DP == 256 ? 64 : 128;  // keys of a tile
+    static constexpr int NG = DP / 64;               // 64-element groups of the head dimension
+    static constexpr int kRows = 128 * MT;
+    static constexpr int kSlot = BN * DP * 2;
+    static constexpr int kSlots = DP == 64 ? 6 : 4;  // even: a producer sees keys only or values only
+    static constexpr int kQTile = 128 * DP * 2;
+    static constexpr int kQBufs = MT == 2 ? 2 : DP == 256 ? 1 : 2;  // MT 2: one for each row tile
+    static constexpr int kParts = BN / 32;           // copies of the rows when there are few
+    static constexpr int kStage = MT == 1 ? 4 * 32 * 33 * 4 : 0;
+    static constexpr int kSmem = kSlots * kSlot + kQBufs * kQTile + kStage + 1024;
+    static constexpr int kSoftWarps = 4 * MT;
+    static constexpr int kWarps = kSoftWarps + 2 + kSlots;
+    static constexpr uint32_t kTmemO = 2 * BN;       // S / P slots first
+    static constexpr uint32_t kTmemCols = 512;
+    static_assert(kTmemO + MT * DP <= 512, "TMEM columns");
+};
+
+// First entry that some row of the tile does not see (entries below it need
+// no mask, and their values no check).
+template <int ROWS>
+PP_DEVINL int all_see(const AttnArgs& a, const Part& p) {
+    return a.mask ? p.seq.ctx : p.seq.ctx + (int)((unsigned)p.j * ROWS / (unsigned)a.group) + 1;
+}
+
+// Bits of the 32 entries from k0 on that new token `tok` sees.
+PP_DEVINL uint32_t seen_bits(const AttnArgs& a, const Part& p, int tok, int k0) {
+    const int j = k0 - p.seq.ctx;  // new token's number of bit 0
+    int end;
+    uint32_t bits = 0xffffffffu;
+    if (a.mask) {
+        end = p.seq.n - j;
+        if (j > -32) {
+            const uint32_t* w = a.mask + (size_t)(p.seq.q0 + tok) * a.mask_words;
+            if (j < 0) {  // the first -j bits are cached tokens
+                bits = (w[0] << -j) | (0xffffffffu >> (32 + j));
+            } else {
+                const int i = j >> 5;
+                const uint32_t lo = i < a.mask_words ? w[i] : 0u, hi = i + 1 < a.mask_words ? w[i + 1] : 0u;
+                bits = __funnelshift_r(lo, hi, j & 31);
+            }
+        }
+    } else {
+        end = tok + 1 - j;
+    }
+    return end >= 32 ? bits : end <= 0 ? 0u : bits & ((1u << end) - 1u);
+}
+
+PP_DEVINL bool sees(const AttnArgs& a, const Part& p, int tok, int j) {  // new token j
+    if (!a.mask) return j <= tok;
+    return j < 32 * a.mask_words && (a.mask[(size_t)(p.seq.q0 + tok) * a.mask_words + (j >> 5)] >> (j & 31) & 1u);
+}
+
+// Position in a CTA's stretch: tile t of part p.
+template <int ROWS, int TOK>
+struct Cursor {
+    Walk<ROWS, TOK> w;
+    Part p;
+    int t;
+    PP_DEVINL explicit Cursor(const Walk<ROWS, TOK>& walk) : w(walk) {
+        w.next(p);
+        t = p.t0;
+    }
+    // k tiles further; the caller stays inside the stretch.  True if a new part began.
+    PP_DEVINL bool advance(int k) {
+        t += k;
+        bool moved = false;
+        while (t >= p.t1) {
+            const int over = t - p.t1;
+            if (!w.next(p)) break;
+            t = p.t0 + over;
+            moved = true;
+        }
+        return moved;
+    }
+};
+
+// One warp copies `rows` rows (a multiple of 32) of DP elements into the
+// swizzled tile at dst: 64-element groups of rows * 128 bytes each.  off[x] is
+// the byte offset from base of row 32 x + lane, negative: zeros.
+template <int DP, int XR>
+PP_DEVINL void copy_rows(unsigned char* dst, const char* base, const long long (&off)[XR], int D, int lane) {
+    constexpr int rows = XR * 32;
+    const int sub = lane >> 3, c = lane & 7;
+#pragma unroll
+    for (int x = 0; x < XR; x++) {
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const int r = 4 * i + sub;
+            const long long o = __shfl_sync(kFull, off[x], r);
+#pragma unroll
+            for (int g = 0; g < DP / 64; g++) {
+                const bool in = o >= 0 && (g * 8 + c) * 8 < D;
+                cp_async_16(dst + g * rows * 128 + (32 * x + r) * 128 + ((c ^ (r & 7)) << 4),
+                            in ? base + o + (g * 8 + c) * 16 : base, in ? 16u : 0u);
+            }
+        }
+    }
+}
+
+// Non-finite values of entries that not every row sees would reach all rows
+// of the product (0 * NaN): they are taken out of the tile here and added to
+// the rows that do see them at the end (add_nonfinite).  Rows [r0, r1) of a
+// value tile in shared memory; true if there were any.
+template <int DP, int BN>
+PP_DEVINL bool drop_nonfinite(unsigned char* tile, int r0, int r1, int lane) {
+    bool any = false;
+    for (int e = r0 * 8 + lane; e < r1 * 8; e += 32) {
+#pragma unroll
+        for (int g = 0; g < DP / 64; g++) {
+            uint4* at = reinterpret_cast<uint4*>(tile + g * BN * 128 + e * 16);
+            uint4 v = *at;
+            uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+            const uint32_t m = __vmaxu2(__vmaxu2(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu),
+                                        __vmaxu2(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu));
+            if ((m & 0xffffu) >= 0x7f80u || (m >> 16) >= 0x7f80u) {
+                any = true;
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    if ((w[i] & 0x7f80u) == 0x7f80u) w[i] &= 0xffff0000u;
+                    if ((w[i] & 0x7f800000u) == 0x7f800000u) w[i] &= 0x0000ffffu;
+                }
+                *at = v;
+            }
+        }
+    }
+    return __any_sync(kFull, any);
+}
+
+// o[0..7] += the non-finite values at elements d..d+7 of the part's new
+// tokens that row's token sees (their weights are positive).
+__device__ __noinline__ void add_nonfinite_slow(const AttnArgs& a, const Part& p, int row, int d, int bn, float* o) {
+    const int tok = row / a.group;
+    const int k1 = min(p.key_end, p.t1 * bn);
+    for (int k = max(p.seq.ctx, p.t0 * bn); k < k1; k++) {
+        if (!sees(a, p, tok, k - p.seq.ctx)) continue;
+        const int page = entry_page(a.batch, p.b, k);
+        if (page < 0) continue;
+        float v[8];
+        Elem<__nv_bfloat16>::unpack(*reinterpret_cast<const uint4*>(a.cache.v + entry_offset(a.batch, a.cache, page, k) +
+                                                                    (long long)p.h * a.cache.head_stride + d * 2),
+                                    v);
+        for (int i = 0; i < 8; i++)
+            if ((__float_as_uint(v[i]) & 0x7f800000u) == 0x7f800000u) o[i] += v[i];
+    }
+}
+
+PP_DEVINL void add_nonfinite(const AttnArgs& a, const Part& p, int row, int d, int bn, float (&o)[8]) {
+    float t[8];  // in memory only when there is something to add
+    for (int i = 0; i < 8; i++) t[i] = o[i];
+    add_nonfinite_slow(a, p, row, d, bn, t);
+    for (int i = 0; i < 8; i++) o[i] = t[i];
+}
+
+template <int DP, int MT>
+__global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1) attn_tc_kernel(const __grid_constant__ AttnArgs a) {
+    using C = Tc<DP, MT>;
+    constexpr int BN = C::BN, NG = C::NG, ROWS = C::kRows, NS = C::kSlots;
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    unsigned char* ring = smem;
+    unsigned char* qs = smem + NS * C::kSlot;
+    float* stage = reinterpret_cast<float*>(qs + C::kQBufs * C::kQTile);
+    __shared__ long long scratch[36];
+    __shared__ uint64_t full[NS], empty[NS], qfull[2], qempty[2], sfull[2], pfull[2], odone[2];
+    __shared__ uint32_t taddr_s;
+    __shared__ float stat_m[4][32], stat_l[4][32];
+    __shared__ unsigned last_s;
+    __shared__ volatile unsigned bad_s;  // a value was taken out of a tile
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint64_t lim = a.timeout_ns;
+    pdl_launch_dependents();
+    if (tid == 0) {
+        for (int i = 0; i < NS; i++) {
+            mbar_init(&full[i], 1);
+            mbar_init(&empty[i], 1);
+        }
+        for (int i = 0; i < 2; i++) {
+            mbar_init(&qfull[i], 1);
+            mbar_init(&qempty[i], 1);
+            mbar_init(&sfull[i], 1);
+            mbar_init(&pfull[i], 4);
+            mbar_init(&odone[i], 1);
+        }
+        fence_mbar_init();
+        bad_s = 0;
+    }
+    if (warp == C::kSoftWarps) {
+        tmem_alloc(&taddr_s, C::kTmemCols);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = taddr_s;
+    pdl_wait();
+    const Walk<ROWS, BN> walk = start_walk<ROWS, BN>(&a, scratch);
+    const int tiles = (int)(walk.end - walk.at);  // of this CTA
+
+    if (tiles <= 0) {
+        // nothing for this CTA
+    } else if (warp >= C::kSoftWarps + 2) {
+        // ------------------------------------------------- producer of one slot
+        const int slot = warp - (C::kSoftWarps + 2);
+        unsigned char* dst = ring + slot * C::kSlot;
+        Cursor<ROWS, BN> cur(walk);
+        int at = 0, uses = 0;
+        for (int pos = slot;; pos += NS, uses++) {
+            // order of the loads: K0 K1 V0 K2 V1 K3 ... (MT 1: scores run two
+            // tiles ahead), K0 V0 K1 V1 ... (MT 2)
+            const bool key = MT == 1 ? pos == 0 || (pos & 1) : !(pos & 1);
+            const int g = MT == 1 ? (pos == 0 ? 0 : key ? (pos + 1) / 2 : (pos - 2) / 2) : pos / 2;
+            if (g >= tiles) break;
+            cur.advance(g - at);
+            at = g;
+            const Part& p = cur.p;
+            const int k0 = cur.t * BN;
+            long long off[BN / 32];
+#pragma unroll
+            for (int x = 0; x < BN / 32; x++) {
+                const int j = k0 + 32 * x + lane;
+                off[x] = -1;
+                if (j < p.key_end) {
+                    const int page = entry_page(a.batch, p.b, j);
+                    if (page >= 0)
+                        off[x] = entry_offset(a.batch, a.cache, page, j) + (long long)p.h * a.cache.head_stride;
+                    else
+                        record_status(a.status, PP_ERR_INVALID_ARG);
+                }
+            }
+            if (uses > 0) mbar_wait(&empty[slot], (uint32_t)(uses - 1) & 1u, a.status, lim);
+            __syncwarp();
+            copy_rows<DP, BN / 32>(dst, key ? a.cache.k : a.cache.v, off, a.head_dim, lane);
+            cp_async_commit();
+            cp_async_wait<0>();
+            if (!key) {
+                const int r0 = max(all_see<ROWS>(a, p) - k0, 0), r1 = min(p.key_end - k0, BN);
+                if (r0 < r1) {
+                    __syncwarp();
+                    if (drop_nonfinite<DP, BN>(dst, r0, r1, lane) && lane == 0) bad_s = 1;
+                }
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&full[slot]);
+        }
+    } else if (warp == C::kSoftWarps + 1) {
+        // --------------------------------------------------------- rows of q
+        Walk<ROWS, BN> w = walk;
+        Part p;
+        for (int n = 0; w.next(p); n++) {
+            const int rows = p.seq.n * a.group - p.j * ROWS;
+#pragma unroll 1
+            for (int m = 0; m < MT; m++) {
+                const int buf = MT == 2 ? m : n % C::kQBufs, use = MT == 2 ? n : n / C::kQBufs;
+                const bool few = MT == 1 && rows <= 32;
+                long long off[4];
+#pragma unroll
+                for (int x = 0; x < 4; x++) {
+                    const int r = few ? (x < C::kParts ? lane : ROWS) : 128 * m + 32 * x + lane;
+                    off[x] = r < rows && r < ROWS ? row_offset(a, p, p.j * ROWS + r, a.q_stride, 2) : -1;
+                }
+                if (use > 0) mbar_wait(&qempty[buf], (uint32_t)(use - 1) & 1u, a.status, lim);
+                __syncwarp();
+                copy_rows<DP, 4>(qs + buf * C::kQTile, a.q, off, a.head_dim, lane);
+                cp_async_commit();
+                cp_async_wait<0>();
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&qfull[buf]);
+            }
+        }
+    } else if (warp == C::kSoftWarps) {
+        // ---------------------------------------------------------- products
+        if (lane == 0) {
+            constexpr uint32_t id_s = idesc_bf16_m128(BN), id_o = idesc_bf16_m128_bn(DP);
+            Cursor<ROWS, BN> cs(walk), co(walk);  // scores, values
+            int part_s = 0;
+            // scores of tile g for row tile m
+            auto scores = [&](int g, int m) {
+                const int buf = MT == 2 ? m : part_s % C::kQBufs, use = MT == 2 ? part_s : part_s / C::kQBufs;
+                const int pos = MT == 1 ? (g == 0 ? 0 : 2 * g - 1) : 2 * g;
+                const int sl = MT == 1 ? g & 1 : m;
+                if (cs.t == cs.p.t0) mbar_wait(&qfull[buf], (uint32_t)use & 1u, a.status, lim);
+                mbar_wait(&full[pos % NS], (uint32_t)(pos / NS) & 1u, a.status, lim);
+                tc_fence_after();
+                const unsigned char* kt = ring + (pos % NS) * C::kSlot;
+                const unsigned char* qt = qs + buf * C::kQTile;
+#pragma unroll
+                for (int d = 0; d < NG; d++)
+                    umma_k64(tmem + (uint32_t)(sl * BN), qt + d * 128 * 128, kt + d * BN * 128, id_s, d > 0);
+                umma_commit(&sfull[sl]);
+                if (cs.t + 1 == cs.p.t1) umma_commit(&qempty[buf]);
+                if (m == MT - 1) umma_commit(&empty[pos % NS]);
+            };
+            auto values = [&](int g, int m) {
+                const int pos = MT == 1 ? 2 * g + 2 : 2 * g + 1;
+                const int sl = MT == 1 ? g & 1 : m;
+                const uint32_t par = (uint32_t)(MT == 1 ? g >> 1 : g) & 1u;
+                mbar_wait(&full[pos % NS], (uint32_t)(pos / NS) & 1u, a.status, lim);
+                mbar_wait(&pfull[sl], par, a.status, lim);
+                tc_fence_after();
+                const uint64_t vd = sdesc_sw128_n(ring + (pos % NS) * C::kSlot, BN * 128);
+#pragma unroll
+                for (int k = 0; k < BN / 16; k++)
+                    umma_bf16_ta(tmem + C::kTmemO + (uint32_t)(m * DP), tmem + (uint32_t)(sl * BN + 8 * k),
+                                 vd + (uint64_t)(k * 128), id_o, (co.t > co.p.t0 || k > 0) ? 1u : 0u);
+                umma_commit(&odone[sl]);
+                if (m == MT - 1) umma_commit(&empty[pos % NS]);
+            };
+            auto step = [&]() {
+                if (cs.advance(1)) part_s++;
+            };
+            if (MT == 1) {
+                scores(0, 0);
+                step();
+                if (tiles > 1) {
+                    scores(1, 0);
+                    step();
+                }
+                for (int g = 0; g < tiles; g++) {
+                    values(g, 0);
+                    co.advance(1);
+                    if (g + 2 < tiles) {
+                        scores(g + 2, 0);
+                        step();
+                    }
+                }
+            } else {
+                for (int m = 0; m < MT; m++) scores(0, m);
+                step();
+                for (int g = 0; g < tiles; g++) {
+                    for (int m = 0; m < MT; m++) {
+                        values(g, m);
+                        if (g + 1 < tiles) scores(g + 1, m);
+                    }
+                    co.advance(1);
+                    step();
+                }
+            }
+        }
+        __syncwarp();
+    } else {
+        // ----------------------------------------------------------- softmax
+        const int m = warp >> 2, wq = warp & 3;  // row tile, quarter of its lanes
+        const uint32_t lanes = (uint32_t)(32 * wq) << 16;
+        const uint32_t t_o = tmem + C::kTmemO + (uint32_t)(m * DP) + lanes;
+        Walk<ROWS, BN> w = walk;
+        Part p;
+        int g = 0;  // tile of the stretch
+        // O holds the products up to tile x (the last or last but one whose
+        // scores this warp has seen, so a parity names its phase)
+        auto products_done = [&](int x) {
+            mbar_wait(&odone[MT == 1 ? x & 1 : m], (uint32_t)(MT == 1 ? x >> 1 : x) & 1u, a.status, lim);
+            tc_fence_after();
+        };
+        while (w.next(p)) {
+            const int rows = min(ROWS, p.seq.n * a.group - p.j * ROWS);
+            const bool few = MT == 1 && rows <= 32;
+            const int r = few ? lane : tid;  // row of the item
+            const bool active = few ? wq < C::kParts : 32 * warp < rows;
+            const int tok = min((p.j * ROWS + r) / a.group, p.seq.n - 1);
+            const int open = all_see<ROWS>(a, p);
+            float mx = -INFINITY, sum = 0.f;
+            for (int t = p.t0; t < p.t1; t++, g++) {
+                const int sl = MT == 1 ? g & 1 : m;
+                const uint32_t par = (uint32_t)(MT == 1 ? g >> 1 : g) & 1u;
+                const uint32_t t_s = tmem + (uint32_t)(sl * BN) + lanes;
+                const int k0 = t * BN;
+                const bool masked = k0 + BN > open;
+                uint32_t see[BN / 32];
+#pragma unroll
+                for (int c = 0; c < BN / 32; c++)
+                    see[c] = !masked ? 0xffffffffu : active && (!few || c == wq) ? seen_bits(a, p, tok, k0 + 32 * c) : 0u;
+                mbar_wait(&sfull[sl], par, a.status, lim);
+                tc_fence_after();
+                if (active) {
+                    // the tile's maximum
+                    float tm = -INFINITY;
+#pragma unroll
+                    for (int c = 0; c < BN / 32; c++) {
+                        if (few && c != wq) continue;
+                        uint32_t s[32];
+                        tmem_ld32(t_s + 32 * c, s);
+                        tmem_ld_wait();
+                        if (masked) {
+#pragma unroll
+                            for (int i = 0; i < 32; i++)
+                                if (see[c] >> i & 1u) tm = fmaxf(tm, __uint_as_float(s[i]));
+                        } else {
+                            float tn = -INFINITY;
+#pragma unroll
+                            for (int i = 0; i < 32; i += 2) {
+                                tm = fmaxf(tm, __uint_as_float(s[i]));
+                                tn = fmaxf(tn, __uint_as_float(s[i + 1]));
+                            }
+                            tm = fmaxf(tm, tn);
+                        }
+                    }
+                    tm *= a.scale_log2;
+                    const bool grow = tm > mx + kLazy || (mx == -INFINITY && tm > mx);
+                    if (t == p.t0) {
+                        mx = tm;
+                    } else if (__any_sync(kFull, grow)) {
+                        // every product before this tile's is done; this tile's waits for us
+                        products_done(g - 1);
+                        const float top = grow ? tm : mx;
+                        const float f = grow ? ex2(mx - top) : 1.f;  // 0 from -inf
+                        mx = top;
+                        sum *= f;
+#pragma unroll 1
+                        for (int c = 0; c < DP; c += 32) {
+                            uint32_t o[32];
+                            tmem_ld32(t_o + c, o);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int i = 0; i < 32; i++) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                            tmem_st32(t_o + c, o);
+                        }
+                    }
+                    const float base = mx == -INFINITY ? 0.f : mx;
+                    // weights over the scores: chunk c of P lies in columns that chunk c of S has left
+                    float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+                    for (int c = 0; c < BN / 32; c++) {
+                        uint32_t pw[16];
+                        if (few && c != wq) {
+#pragma unroll
+                            for (int i = 0; i < 16; i++) pw[i] = 0u;
+                        } else {
+                            uint32_t s[32];
+                            tmem_ld32(t_s + 32 * c, s);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int i = 0; i < 16; i++) {
+                                float x0 = ex2(fmaf(__uint_as_float(s[2 * i]), a.scale_log2, -base));
+                                float x1 = ex2(fmaf(__uint_as_float(s[2 * i + 1]), a.scale_log2, -base));
+                                if (masked) {
+                                    if (!(see[c] >> (2 * i) & 1u)) x0 = 0.f;
+                                    if (!(see[c] >> (2 * i + 1) & 1u)) x1 = 0.f;
+                                }
+                                pw[i] = pack_bf16x2(x0, x1);
+                                s0 += bf16lo(pw[i]);  // the sum of the weights as the product sees them
+                                s1 += bf16hi(pw[i]);
+                            }
+                        }
+                        if (few && c < wq) continue;  // would overwrite scores not read yet
+                        tmem_st16(t_s + 16 * c, pw);
+                    }
+                    if (few) {
+                        uint32_t z[16] = {};
+#pragma unroll
+                        for (int c = 0; c < BN / 32; c++)
+                            if (c < wq) tmem_st16(t_s + 16 * c, z);
+                    }
+                    sum += s0 + s1;
+                    tmem_st_wait();
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&pfull[sl]);
+            }
+            // ------------------------------------------------ end of the part
+            products_done(g - 1);
+            const bool whole = p.whole(), bad = bad_s != 0;
+            const Split<ROWS, BN> sp(w.sched, p);
+            float* place = sp.place(a, blockIdx.x);
+            const int D = a.head_dim;
+            if (few) {
+                // add up the warps' copies, 32 elements at a time
+                stat_m[wq][lane] = active ? mx : -INFINITY;
+                stat_l[wq][lane] = active ? sum : 0.f;
+                named_bar_sync(1, 128);
+                float top = -INFINITY;
+#pragma unroll
+                for (int i = 0; i < C::kParts; i++) top = fmaxf(top, stat_m[i][lane]);
+                if (top == -INFINITY) top = 0.f;
+                const float f = ex2(mx - top);
+                const int er = tid >> 2, ed = (tid & 3) * 8;
+                float etop = -INFINITY, l = 0.f;
+#pragma unroll
+                for (int i = 0; i < C::kParts; i++) etop = fmaxf(etop, stat_m[i][er]);
+                const float ebase = etop == -INFINITY ? 0.f : etop;
+#pragma unroll
+                for (int i = 0; i < C::kParts; i++) l += stat_l[i][er] * ex2(stat_m[i][er] - ebase);
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll 1
+                for (int c = 0; c < D; c += 32) {
+                    if (active) {
+                        uint32_t o[32];
+                        tmem_ld32(t_o + c, o);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 32; i++) stage[(wq * 32 + lane) * 33 + i] = __uint_as_float(o[i]) * f;
+                    }
+                    named_bar_sync(1, 128);
+                    if (er < rows && c + ed < D) {
+                        float o[8] = {};
+#pragma unroll
+                        for (int x = 0; x < C::kParts; x++)
+#pragma unroll
+                            for (int i = 0; i < 8; i++) o[i] += stage[(x * 32 + er) * 33 + ed + i];
+                        if (bad) add_nonfinite(a, p, p.j * ROWS + er, c + ed, BN, o);
+                        if (whole) {
+#pragma unroll
+                            for (int i = 0; i < 8; i++) o[i] *= inv;
+                            *reinterpret_cast<uint4*>(a.out + row_offset(a, p, p.j * ROWS + er, a.out_stride, 2) + (c + ed) * 2) =
+                                Elem<__nv_bfloat16>::pack(o);
+                        } else {
+                            float4* dst = reinterpret_cast<float4*>(place + (size_t)er * D + c + ed);
+                            dst[0] = make_float4(o[0], o[1], o[2], o[3]);
+                            dst[1] = make_float4(o[4], o[5], o[6], o[7]);
+                        }
+                    }
+                    named_bar_sync(1, 128);
+                }
+                if (!whole && (tid & 3) == 0) {
+                    place[(size_t)ROWS * D + er] = etop;
+                    place[(size_t)ROWS * (D + 1) + er] = l;
+                }
+            } else if (active) {
+                const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                char* dst = a.out + row_offset(a, p, p.j * ROWS + min(r, rows - 1), a.out_stride, 2);
+#pragma unroll 1
+                for (int c = 0; c < D; c += 32) {
+                    uint32_t u[32];
+                    tmem_ld32(t_o + c, u);
+                    tmem_ld_wait();
+                    if (r >= rows) continue;
+                    for (int i = 0; i < 32; i += 8) {
+                        if (c + i >= D) break;
+                        float o[8];
+#pragma unroll
+                        for (int x = 0; x < 8; x++) o[x] = __uint_as_float(u[i + x]);
+                        if (bad) add_nonfinite(a, p, p.j * ROWS + r, c + i, BN, o);
+                        if (whole) {
+#pragma unroll
+                            for (int x = 0; x < 8; x++) o[x] *= inv;
+                            *reinterpret_cast<uint4*>(dst + (c + i) * 2) = Elem<__nv_bfloat16>::pack(o);
+                        } else {
+                            float4* out = reinterpret_cast<float4*>(place + (size_t)r * D + c + i);
+                            out[0] = make_float4(o[0], o[1], o[2], o[3]);
+                            out[1] = make_float4(o[4], o[5], o[6], o[7]);
+                        }
+                    }
+                }
+                if (!whole && r < rows) {
+                    place[(size_t)ROWS * D + r] = mx;
+                    place[(size_t)ROWS * (D + 1) + r] = sum;
+                }
+            }
+            tc_fence_before();
+            if (!whole) {
+                __threadfence();
+                named_bar_sync(1, 32 * C::kSoftWarps);
+                if (tid == 0) {
+                    last_s = atomicAdd(a.counters + sp.c0, 1u) == (unsigned)(sp.c1 - sp.c0);
+                    if (last_s) a.counters[sp.c0] = 0;
+                    __threadfence();
+                }
+                named_bar_sync(1, 32 * C::kSoftWarps);
+                if (last_s) merge_parts<__nv_bfloat16, ROWS, BN>(a, p, sp, tid, 32 * C::kSoftWarps);
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == C::kSoftWarps) {
+        tc_fence_after();
+        tmem_dealloc(tmem, C::kTmemCols);
+    }
+}
+
+template <int DP, int MT>
+cudaError_t go(const AttnArgs& a, int sms, cudaStream_t st) {
+    using C = Tc<DP, MT>;
+    auto* kern = attn_tc_kernel<DP, MT>;
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
+    if (e != cudaSuccess) return e;
+    return launch_overlapped(kern, dim3((unsigned)(sms < kAttnTcGrid ? sms : kAttnTcGrid)), dim3(C::kWarps * 32),
+                             C::kSmem, st, a);
+}
+
+}  // namespace
+
+cudaError_t attn_tc_launch(const AttnArgs& a, int sms, cudaStream_t st) {
+    // rows a sequence brings to a key head on average: two row tiles share
+    // each key tile where one does not hold them
+    const long long rows = ((long long)a.batch.n_tokens * a.group + a.batch.n_seqs - 1) / a.batch.n_seqs;
+    const bool two = rows > 128;
+    if (a.head_dim <= 64) return two ? go<64, 2>(a, sms, st) : go<64, 1>(a, sms, st);
+    if (a.head_dim <= 128) return two ? go<128, 2>(a, sms, st) : go<128, 1>(a, sms, st);
+    return go<256, 1>(a, sms, st);
+}
+
+}  // namespace pp

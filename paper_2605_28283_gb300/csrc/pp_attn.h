@@ -13,6 +13,8 @@ namespace pp {
 // counters in their workspace.
 constexpr int kAttnMaxGrid = 608;      // CUDA-core kernel: up to 4 CTAs on each of 152 SMs
 constexpr int kAttnSimtRows = 16;      // rows (token, head of the group) of its largest tile
+constexpr int kAttnTcGrid = 152;       // tensor-core kernel: one CTA per SM ...
+constexpr int kAttnTcRows = 256;       // ... and two tiles of 128 rows
 
 struct BatchArgs {
     const int32_t* q_start;
@@ -75,6 +77,7 @@ cudaError_t append_launch(const AppendArgs& a, int dtype, int layout, cudaStream
 cudaError_t commit_launch(const CommitArgs& a, cudaStream_t st);
 
 size_t attn_part_floats(int head_dim);  // floats behind AttnArgs.part
-cudaError_t attn_simt_launch(const AttnArgs& a, int dtype, int sms, cudaStream_t st);
+cudaError_t attn_simt_launch(const AttnArgs& a, int sms, cudaStream_t st);  // fp32
+cudaError_t attn_tc_launch(const AttnArgs& a, int sms, cudaStream_t st);    // bf16
 
 }  // namespace pp

@@ -1,0 +1,64 @@
+// tcgen05 helpers of the attention kernel beyond pp_tc.cuh: an A operand in
+// TMEM, a B operand whose N runs along the contiguous dimension (values as
+// they lie in the cache: [token][element]), and TMEM stores.
+#pragma once
+
+#include "pp_tc.cuh"
+
+namespace pp {
+
+// Instruction descriptor with B "N-major" (bit 16).
+PP_DEVINL constexpr uint32_t idesc_bf16_m128_bn(int n) { return idesc_bf16_m128(n) | (1u << 16); }
+
+// Shared-memory descriptor of an N-major operand with the 128-byte swizzle:
+// atoms of 64 elements of N (128 B) x 8 of K (128 B apart); the next 8 of K
+// lie 1024 B further, the next 64 of N `group_bytes` further.
+PP_DEVINL uint64_t sdesc_sw128_n(const void* p, uint32_t group_bytes) {
+    const uint32_t a = smem_u32(p);
+    uint64_t d = (uint64_t)((a & 0x3ffffu) >> 4);
+    d |= (uint64_t)(group_bytes >> 4) << 16;  // leading byte offset: next 64 of N
+    d |= (uint64_t)(1024u >> 4) << 32;        // stride byte offset: next 8 of K
+    d |= (uint64_t)1u << 46;                  // descriptor version
+    d |= (uint64_t)2u << 61;                  // 128-byte swizzle
+    return d;
+}
+
+// D[128 x N] (+)= A[128 x 16] * B, A in TMEM: lane = row, two bf16 a column.
+PP_DEVINL void umma_bf16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
+// Warp-collective: lane i writes 16 consecutive columns of row (lane base + i).
+PP_DEVINL void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
+        "%15, %16};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+PP_DEVINL void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
+        "%15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
+        "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
+        "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+PP_DEVINL void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// 2^x, flushing subnormals (softmax weights below 2^-126 count as zero).
+PP_DEVINL float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+}  // namespace pp
