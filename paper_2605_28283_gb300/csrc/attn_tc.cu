@@ -22,6 +22,7 @@
 // 32 keys of the tile (P is zero elsewhere) with its own maximum and sum, and
 // the copies are added up at the end of the part.
 #include "pp_attn_sched.cuh"
+#include "pp_kernels.h"
 #include "pp_launch.cuh"
 #include "pp_tc_attn.cuh"
 
@@ -108,27 +109,38 @@ struct Cursor {
     }
 };
 
-// One warp copies `rows` rows (a multiple of 32) of DP elements into the
-// swizzled tile at dst: 64-element groups of rows * 128 bytes each.  off[x] is
-// the byte offset from base of row 32 x + lane, negative: zeros.
-template <int DP, int XR>
-PP_DEVINL void copy_rows(unsigned char* dst, const char* base, const long long (&off)[XR], int D, int lane) {
-    constexpr int rows = XR * 32;
+// One warp copies 32 rows of DP elements with 16-byte cp.async into a
+// swizzled tile of 64-element groups, `group` bytes each; dst is the first
+// row's place.  off is the byte offset from base of row `lane`, negative:
+// zeros.  Rolled up: the code is run a few times a tile by one warp, and
+// fetching it straight-line cost more than running it.
+template <int DP>
+PP_DEVINL void copy_rows32(unsigned char* dst, int group, const char* base, long long off, int D, int lane) {
     const int sub = lane >> 3, c = lane & 7;
+#pragma unroll 1
+    for (int i = 0; i < 8; i += 2) {
 #pragma unroll
-    for (int x = 0; x < XR; x++) {
-#pragma unroll
-        for (int i = 0; i < 8; i++) {
-            const int r = 4 * i + sub;
-            const long long o = __shfl_sync(kFull, off[x], r);
+        for (int k = 0; k < 2; k++) {
+            const int r = 4 * (i + k) + sub;
+            const long long o = __shfl_sync(kFull, off, r);
 #pragma unroll
             for (int g = 0; g < DP / 64; g++) {
                 const bool in = o >= 0 && (g * 8 + c) * 8 < D;
-                cp_async_16(dst + g * rows * 128 + (32 * x + r) * 128 + ((c ^ (r & 7)) << 4),
-                            in ? base + o + (g * 8 + c) * 16 : base, in ? 16u : 0u);
+                cp_async_16(dst + g * group + r * 128 + ((c ^ (r & 7)) << 4), in ? base + o + (g * 8 + c) * 16 : base,
+                            in ? 16u : 0u);
             }
         }
     }
+}
+
+// Rows [r0, r1) of a value tile set to zero.
+template <int DP, int BN>
+PP_DEVINL void zero_rows(unsigned char* tile, int r0, int r1, int lane) {
+#pragma unroll 1
+    for (int e = r0 * 8 + lane; e < r1 * 8; e += 32)
+#pragma unroll
+        for (int g = 0; g < DP / 64; g++)
+            *reinterpret_cast<uint4*>(tile + g * BN * 128 + e * 16) = make_uint4(0u, 0u, 0u, 0u);
 }
 
 // Non-finite values of entries that not every row sees would reach all rows
@@ -138,6 +150,7 @@ PP_DEVINL void copy_rows(unsigned char* dst, const char* base, const long long (
 template <int DP, int BN>
 PP_DEVINL bool drop_nonfinite(unsigned char* tile, int r0, int r1, int lane) {
     bool any = false;
+#pragma unroll 1
     for (int e = r0 * 8 + lane; e < r1 * 8; e += 32) {
 #pragma unroll
         for (int g = 0; g < DP / 64; g++) {
@@ -186,7 +199,9 @@ PP_DEVINL void add_nonfinite(const AttnArgs& a, const Part& p, int row, int d, i
 }
 
 template <int DP, int MT>
-__global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1) attn_tc_kernel(const __grid_constant__ AttnArgs a) {
+__global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
+    attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensorMap map_k,
+                   const __grid_constant__ CUtensorMap map_v) {
     using C = Tc<DP, MT>;
     constexpr int BN = C::BN, NG = C::NG, ROWS = C::kRows, NS = C::kSlots;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
@@ -195,7 +210,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1) attn_tc_kernel(con
     unsigned char* qs = smem + NS * C::kSlot;
     float* stage = reinterpret_cast<float*>(qs + C::kQBufs * C::kQTile);
     __shared__ long long scratch[36];
-    __shared__ uint64_t full[NS], empty[NS], qfull[2], qempty[2], sfull[2], pfull[2], odone[2];
+    __shared__ uint64_t full[NS], empty[NS], landed[NS], qfull[2], qempty[2], sfull[2], pfull[2], odone[2];
     __shared__ uint32_t taddr_s;
     __shared__ float stat_m[4][32], stat_l[4][32];
     __shared__ unsigned last_s;
@@ -207,6 +222,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1) attn_tc_kernel(con
         for (int i = 0; i < NS; i++) {
             mbar_init(&full[i], 1);
             mbar_init(&empty[i], 1);
+            mbar_init(&landed[i], 1);
         }
         for (int i = 0; i < 2; i++) {
             mbar_init(&qfull[i], 1);
@@ -237,7 +253,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1) attn_tc_kernel(con
         const int slot = warp - (C::kSoftWarps + 2);
         unsigned char* dst = ring + slot * C::kSlot;
         Cursor<ROWS, BN> cur(walk);
-        int at = 0, uses = 0;
+        int at = 0, uses = 0, fixes = 0;
         for (int pos = slot;; pos += NS, uses++) {
             // order of the loads: K0 K1 V0 K2 V1 K3 ... (MT 1: scores run two
             // tiles ahead), K0 V0 K1 V1 ... (MT 2)
@@ -248,34 +264,61 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1) attn_tc_kernel(con
             at = g;
             const Part& p = cur.p;
             const int k0 = cur.t * BN;
-            long long off[BN / 32];
-#pragma unroll
-            for (int x = 0; x < BN / 32; x++) {
-                const int j = k0 + 32 * x + lane;
-                off[x] = -1;
-                if (j < p.key_end) {
-                    const int page = entry_page(a.batch, p.b, j);
-                    if (page >= 0)
-                        off[x] = entry_offset(a.batch, a.cache, page, j) + (long long)p.h * a.cache.head_stride;
-                    else
-                        record_status(a.status, PP_ERR_INVALID_ARG);
+            const int end = min(p.key_end - k0, BN);  // rows of the tile that exist
+            // values: rows that some row of queries does not see are looked through, rows past the end set to zero
+            const int open = key ? BN : max(all_see<ROWS>(a, p) - k0, 0);
+            if (a.box > 0) {
+                // boxes of 64 elements x min(page, BN) tokens, one for a lane at a time
+                const int boxes = (end + a.box - 1) / a.box * NG;
+                const bool fix = !key && (end < BN || open < end);
+                uint64_t* bar = fix ? &landed[slot] : &full[slot];
+                int page = 0, b = lane;
+                if (b < boxes) page = entry_page(a.batch, p.b, k0 + b / NG * a.box);
+                if (uses > 0) mbar_wait(&empty[slot], (uint32_t)(uses - 1) & 1u, a.status, lim);
+                if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(boxes * a.box * 128));
+                __syncwarp();
+                while (b < boxes) {
+                    const int row = b / NG * a.box, grp = b % NG;
+                    if (page < 0) record_status(a.status, PP_ERR_INVALID_ARG);
+                    // a page that does not exist lies past the last one: zeros
+                    tma_load_4d(dst + grp * BN * 128 + row * 128, key ? &map_k : &map_v, grp * 64, p.h,
+                                (int)((unsigned)(k0 + row) % (unsigned)a.batch.page_size),
+                                page < 0 ? a.batch.n_pages : page, bar);
+                    b += 32;
+                    if (b < boxes) page = entry_page(a.batch, p.b, k0 + b / NG * a.box);
                 }
-            }
-            if (uses > 0) mbar_wait(&empty[slot], (uint32_t)(uses - 1) & 1u, a.status, lim);
-            __syncwarp();
-            copy_rows<DP, BN / 32>(dst, key ? a.cache.k : a.cache.v, off, a.head_dim, lane);
-            cp_async_commit();
-            cp_async_wait<0>();
-            if (!key) {
-                const int r0 = max(all_see<ROWS>(a, p) - k0, 0), r1 = min(p.key_end - k0, BN);
-                if (r0 < r1) {
+                if (fix) {
+                    mbar_wait(bar, (uint32_t)fixes++ & 1u, a.status, lim);
+                    if (open < end && drop_nonfinite<DP, BN>(dst, open, end, lane) && lane == 0) bad_s = 1;
+                    zero_rows<DP, BN>(dst, end, BN, lane);
+                    fence_proxy_async_smem();
                     __syncwarp();
-                    if (drop_nonfinite<DP, BN>(dst, r0, r1, lane) && lane == 0) bad_s = 1;
+                    if (lane == 0) mbar_arrive(&full[slot]);
                 }
+            } else {
+                if (uses > 0) mbar_wait(&empty[slot], (uint32_t)(uses - 1) & 1u, a.status, lim);
+                __syncwarp();
+#pragma unroll 1
+                for (int x = 0; x < BN; x += 32) {
+                    const int j = k0 + x + lane;
+                    long long off = -1;
+                    if (x + lane < end) {
+                        const int page = entry_page(a.batch, p.b, j);
+                        if (page >= 0)
+                            off = entry_offset(a.batch, a.cache, page, j) + (long long)p.h * a.cache.head_stride;
+                        else
+                            record_status(a.status, PP_ERR_INVALID_ARG);
+                    }
+                    copy_rows32<DP>(dst + x * 128, BN * 128, key ? a.cache.k : a.cache.v, off, a.head_dim, lane);
+                }
+                cp_async_commit();
+                cp_async_wait<0>();
+                __syncwarp();
+                if (open < end && drop_nonfinite<DP, BN>(dst, open, end, lane) && lane == 0) bad_s = 1;
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&full[slot]);
             }
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&full[slot]);
         }
     } else if (warp == C::kSoftWarps + 1) {
         // --------------------------------------------------------- rows of q
@@ -287,15 +330,14 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1) attn_tc_kernel(con
             for (int m = 0; m < MT; m++) {
                 const int buf = MT == 2 ? m : n % C::kQBufs, use = MT == 2 ? n : n / C::kQBufs;
                 const bool few = MT == 1 && rows <= 32;
-                long long off[4];
-#pragma unroll
-                for (int x = 0; x < 4; x++) {
-                    const int r = few ? (x < C::kParts ? lane : ROWS) : 128 * m + 32 * x + lane;
-                    off[x] = r < rows && r < ROWS ? row_offset(a, p, p.j * ROWS + r, a.q_stride, 2) : -1;
-                }
                 if (use > 0) mbar_wait(&qempty[buf], (uint32_t)(use - 1) & 1u, a.status, lim);
                 __syncwarp();
-                copy_rows<DP, 4>(qs + buf * C::kQTile, a.q, off, a.head_dim, lane);
+#pragma unroll 1
+                for (int x = 0; x < 4; x++) {
+                    const int r = few ? (x < C::kParts ? lane : ROWS) : 128 * m + 32 * x + lane;
+                    const long long off = r < rows && r < ROWS ? row_offset(a, p, p.j * ROWS + r, a.q_stride, 2) : -1;
+                    copy_rows32<DP>(qs + buf * C::kQTile + x * 32 * 128, 128 * 128, a.q, off, a.head_dim, lane);
+                }
                 cp_async_commit();
                 cp_async_wait<0>();
                 fence_proxy_async_smem();
@@ -401,34 +443,30 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1) attn_tc_kernel(con
                 const uint32_t t_s = tmem + (uint32_t)(sl * BN) + lanes;
                 const int k0 = t * BN;
                 const bool masked = k0 + BN > open;
-                uint32_t see[BN / 32];
-#pragma unroll
-                for (int c = 0; c < BN / 32; c++)
-                    see[c] = !masked ? 0xffffffffu : active && (!few || c == wq) ? seen_bits(a, p, tok, k0 + 32 * c) : 0u;
                 mbar_wait(&sfull[sl], par, a.status, lim);
                 tc_fence_after();
                 if (active) {
-                    // the tile's maximum
+                    // the tile's maximum (chunks of 32 keys; few rows: this warp's only)
+                    const int c0 = few ? wq : 0, c1 = few ? wq + 1 : BN / 32;
                     float tm = -INFINITY;
-#pragma unroll
-                    for (int c = 0; c < BN / 32; c++) {
-                        if (few && c != wq) continue;
+#pragma unroll 1
+                    for (int c = c0; c < c1; c++) {
                         uint32_t s[32];
                         tmem_ld32(t_s + 32 * c, s);
+                        const uint32_t see = masked ? seen_bits(a, p, tok, k0 + 32 * c) : 0xffffffffu;
                         tmem_ld_wait();
                         if (masked) {
 #pragma unroll
                             for (int i = 0; i < 32; i++)
-                                if (see[c] >> i & 1u) tm = fmaxf(tm, __uint_as_float(s[i]));
-                        } else {
-                            float tn = -INFINITY;
-#pragma unroll
-                            for (int i = 0; i < 32; i += 2) {
-                                tm = fmaxf(tm, __uint_as_float(s[i]));
-                                tn = fmaxf(tn, __uint_as_float(s[i + 1]));
-                            }
-                            tm = fmaxf(tm, tn);
+                                if (!(see >> i & 1u)) s[i] = __float_as_uint(-INFINITY);
                         }
+                        float tn = -INFINITY;
+#pragma unroll
+                        for (int i = 0; i < 32; i += 2) {
+                            tm = fmaxf(tm, __uint_as_float(s[i]));
+                            tn = fmaxf(tn, __uint_as_float(s[i + 1]));
+                        }
+                        tm = fmaxf(tm, tn);
                     }
                     tm *= a.scale_log2;
                     const bool grow = tm > mx + kLazy || (mx == -INFINITY && tm > mx);
@@ -454,37 +492,32 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1) attn_tc_kernel(con
                     const float base = mx == -INFINITY ? 0.f : mx;
                     // weights over the scores: chunk c of P lies in columns that chunk c of S has left
                     float s0 = 0.f, s1 = 0.f;
+#pragma unroll 1
+                    for (int c = c0; c < c1; c++) {
+                        uint32_t s[32], pw[16];
+                        tmem_ld32(t_s + 32 * c, s);
+                        const uint32_t see = masked ? seen_bits(a, p, tok, k0 + 32 * c) : 0xffffffffu;
+                        tmem_ld_wait();
+                        if (masked) {
 #pragma unroll
-                    for (int c = 0; c < BN / 32; c++) {
-                        uint32_t pw[16];
-                        if (few && c != wq) {
-#pragma unroll
-                            for (int i = 0; i < 16; i++) pw[i] = 0u;
-                        } else {
-                            uint32_t s[32];
-                            tmem_ld32(t_s + 32 * c, s);
-                            tmem_ld_wait();
-#pragma unroll
-                            for (int i = 0; i < 16; i++) {
-                                float x0 = ex2(fmaf(__uint_as_float(s[2 * i]), a.scale_log2, -base));
-                                float x1 = ex2(fmaf(__uint_as_float(s[2 * i + 1]), a.scale_log2, -base));
-                                if (masked) {
-                                    if (!(see[c] >> (2 * i) & 1u)) x0 = 0.f;
-                                    if (!(see[c] >> (2 * i + 1) & 1u)) x1 = 0.f;
-                                }
-                                pw[i] = pack_bf16x2(x0, x1);
-                                s0 += bf16lo(pw[i]);  // the sum of the weights as the product sees them
-                                s1 += bf16hi(pw[i]);
-                            }
+                            for (int i = 0; i < 32; i++)
+                                if (!(see >> i & 1u)) s[i] = __float_as_uint(-INFINITY);
                         }
-                        if (few && c < wq) continue;  // would overwrite scores not read yet
+#pragma unroll
+                        for (int i = 0; i < 16; i++) {
+                            const float x0 = ex2(fmaf(__uint_as_float(s[2 * i]), a.scale_log2, -base));
+                            const float x1 = ex2(fmaf(__uint_as_float(s[2 * i + 1]), a.scale_log2, -base));
+                            pw[i] = pack_bf16x2(x0, x1);
+                            s0 += bf16lo(pw[i]);  // the sum of the weights as the product sees them
+                            s1 += bf16hi(pw[i]);
+                        }
                         tmem_st16(t_s + 16 * c, pw);
                     }
-                    if (few) {
-                        uint32_t z[16] = {};
-#pragma unroll
+                    if (few) {  // the other warps' keys
+                        const uint32_t z[16] = {};
+#pragma unroll 1
                         for (int c = 0; c < BN / 32; c++)
-                            if (c < wq) tmem_st16(t_s + 16 * c, z);
+                            if (c != wq) tmem_st16(t_s + 16 * c, z);
                     }
                     sum += s0 + s1;
                     tmem_st_wait();
@@ -496,8 +529,8 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1) attn_tc_kernel(con
             // ------------------------------------------------ end of the part
             products_done(g - 1);
             const bool whole = p.whole(), bad = bad_s != 0;
-            const Split<ROWS, BN> sp(w.sched, p);
-            float* place = sp.place(a, blockIdx.x);
+            const Split<ROWS, BN> sp = whole ? Split<ROWS, BN>() : Split<ROWS, BN>(w.sched, p);
+            float* place = whole ? nullptr : sp.place(a, blockIdx.x);
             const int D = a.head_dim;
             if (few) {
                 // add up the warps' copies, 32 elements at a time
@@ -604,14 +637,38 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1) attn_tc_kernel(con
     }
 }
 
+// Keys or values as a 4-D tensor (element, head, offset in the page, page),
+// boxes of 64 elements x `box` tokens of one head and page.
+bool cache_map(CUtensorMap* map, const AttnArgs& a, const char* base) {
+    auto enc = tensor_map_encoder();
+    if (!enc) return false;
+    const cuuint64_t dims[4] = {(cuuint64_t)a.head_dim, (cuuint64_t)a.n_kv_heads, (cuuint64_t)a.batch.page_size,
+                                (cuuint64_t)a.batch.n_pages};
+    // a dimension of one entry may carry any stride, 0 too; it is never stepped over
+    const long long steps[3] = {a.cache.head_stride, a.cache.token_stride, a.cache.page_stride};
+    cuuint64_t strides[3];
+    for (int i = 0; i < 3; i++) strides[i] = dims[i + 1] == 1 && steps[i] < 16 ? 16 : (cuuint64_t)steps[i];
+    const cuuint32_t box[4] = {64, 1, (cuuint32_t)a.box, 1};
+    const cuuint32_t estr[4] = {1, 1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<char*>(base), dims, strides, box, estr,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int DP, int MT>
-cudaError_t go(const AttnArgs& a, int sms, cudaStream_t st) {
+cudaError_t go(AttnArgs a, int sms, cudaStream_t st) {
     using C = Tc<DP, MT>;
     auto* kern = attn_tc_kernel<DP, MT>;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
     if (e != cudaSuccess) return e;
+    // TMA boxes where pages and key tiles divide one another and a box fills
+    // whole 8-row swizzle atoms; else 16-byte cp.async, for any page
+    const int ps = a.batch.page_size;
+    a.box = ps >= 8 && (C::BN % ps == 0 || ps % C::BN == 0) ? (ps < C::BN ? ps : C::BN) : 0;
+    CUtensorMap mk{}, mv{};
+    if (a.box && (!cache_map(&mk, a, a.cache.k) || !cache_map(&mv, a, a.cache.v))) a.box = 0;
     return launch_overlapped(kern, dim3((unsigned)(sms < kAttnTcGrid ? sms : kAttnTcGrid)), dim3(C::kWarps * 32),
-                             C::kSmem, st, a);
+                             C::kSmem, st, a, mk, mv);
 }
 
 }  // namespace

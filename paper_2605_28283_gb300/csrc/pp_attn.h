@@ -66,6 +66,7 @@ struct AttnArgs {
     const uint32_t* mask;
     int mask_words;
     int n_kv_heads, group, head_dim;
+    int box;             // tokens of a TMA box, 0: copied row by row
     float scale_log2;    // scale * log2(e): softmax in powers of two
     float* part;         // partial results of split items
     unsigned* counters;  // arrivals per split item, zero at rest

@@ -17,6 +17,13 @@
 
 namespace pp {
 
+// Quotient of two non-negative numbers, in 32 bits where they fit (a 64-bit
+// division is a call of a hundred instructions).
+PP_DEVINL long long quotient(long long a, long long b) {
+    if ((unsigned long long)(a | b) >> 32 == 0) return (long long)((unsigned)a / (unsigned)b);
+    return a / b;
+}
+
 // Tiles of the key line: the schedule is recomputed by whoever walks it, from
 // the lengths alone.
 template <int ROWS, int TOK>
@@ -44,13 +51,21 @@ struct Sched {
         return sum;
     }
 
-    PP_DEVINL long long begin_of(int c) const { return total * c / ctas; }
+    // Stretches: the first `longer` ones of `each` + 1 tiles, the others of `each`.
+    long long each;
+    int longer;
+    PP_DEVINL void deal(long long total_, int grid) {
+        total = total_;
+        ctas = (int)min((long long)grid, total);
+        if (ctas == 0) return;
+        each = quotient(total, ctas);
+        longer = (int)(total - each * ctas);
+    }
+    PP_DEVINL long long begin_of(int c) const { return each * c + min(c, longer); }
     // CTA whose stretch holds tile u
     PP_DEVINL int cta_of(long long u) const {
-        int c = (int)(u * ctas / total);
-        while (c + 1 < ctas && begin_of(c + 1) <= u) c++;
-        while (begin_of(c) > u) c--;
-        return c;
+        const long long head = (each + 1) * longer;
+        return u < head ? (int)quotient(u, each + 1) : longer + (int)quotient(u - head, each);
     }
 };
 
@@ -86,7 +101,7 @@ struct Walk {
         head_base = base;
         const long long per = sched.head_tiles(seq);
         if (per > 0) {
-            h = (int)((at - base) / per);
+            h = (int)quotient(at - base, per);
             head_base = base + (long long)h * per;
         }
         while (m > 0 && j + 1 < m && head_base + sched.key_tiles(seq, j) <= at) {
@@ -131,7 +146,7 @@ PP_DEVINL Walk<ROWS, TOK> start_walk(const AttnArgs* a, long long* scratch) {
     long long* sums = scratch;       // [32]
     long long* found = scratch + 32;  // sequence, its line position
     // pass 0: the total; pass 1: the sequence that holds this CTA's first tile
-    long long lo = 0, total = 0, mine = 0;
+    long long lo = 0, mine = 0;
     for (int pass = 0; pass < 2; pass++) {
         long long before = 0;
         for (int b0 = 0; b0 < B; b0 += (int)blockDim.x) {
@@ -167,9 +182,7 @@ PP_DEVINL Walk<ROWS, TOK> start_walk(const AttnArgs* a, long long* scratch) {
             __syncthreads();
         }
         if (pass == 0) {
-            total = before;
-            w.sched.total = total;
-            w.sched.ctas = (int)min((long long)gridDim.x, total);
+            w.sched.deal(before, (int)gridDim.x);
             if ((int)blockIdx.x >= w.sched.ctas) break;  // uniform over the CTA
             lo = w.sched.begin_of(blockIdx.x);
         }
@@ -198,6 +211,7 @@ template <int ROWS, int TOK>
 struct Split {
     int c0, c1;
     bool c0_tail;  // the first part lies in c0's second place
+    PP_DEVINL Split() : c0(0), c1(0), c0_tail(false) {}
     PP_DEVINL Split(const Sched<ROWS, TOK>& s, const Part& p) {
         c0 = s.cta_of(p.first);
         c1 = s.cta_of(p.first + p.tiles - 1);

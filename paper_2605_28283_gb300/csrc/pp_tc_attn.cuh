@@ -54,6 +54,15 @@ PP_DEVINL void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
 }
 PP_DEVINL void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// 4-D tiled tensor copy global -> shared; boxes past an extent read zeros.
+PP_DEVINL void tma_load_4d(void* dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, "
+        "{%2, %3, %4, %5}], [%6];" ::"r"(smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(smem_u32(bar))
+        : "memory");
+}
+
 // 2^x, flushing subnormals (softmax weights below 2^-126 count as zero).
 PP_DEVINL float ex2(float x) {
     float y;
