@@ -54,6 +54,7 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_consta
     const int s_key = tid % TOK, s_rg = tid / TOK % L::kRG, s_ds = tid / L::kScoreCols;
     // value threads: 4 elements, row group, part of the keys
     const int v_d = tid % L::kD4 * 4, v_rg = tid / L::kD4 % L::kRG, v_ts = tid / (L::kD4 * L::kRG);
+    if (walk.at < walk.end) walk.begin();
     Part p;
     while (walk.next(p)) {
         const int rows = min(ROWS, p.seq.n * a.group - p.j * ROWS);
@@ -231,13 +232,8 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_consta
             pl[(size_t)ROWS * D + tid] = Mx[tid];
             pl[(size_t)ROWS * (D + 1) + tid] = Sum[tid];
         }
-        __threadfence();
         __syncthreads();
-        if (tid == 0) {
-            last_s = atomicAdd(a.counters + sp.c0, 1u) == (unsigned)(sp.c1 - sp.c0);
-            if (last_s) a.counters[sp.c0] = 0;
-            __threadfence();
-        }
+        if (tid == 0) last_s = arrive_last(a.counters + sp.c0, (unsigned)(sp.c1 - sp.c0 + 1));
         __syncthreads();
         if (last_s) merge_parts<T, ROWS, TOK>(a, p, sp, tid, kThreads);
     }

@@ -37,7 +37,7 @@ struct Tc {
     static constexpr int NG = DP / 64;               // 64-element groups of the head dimension
     static constexpr int kRows = 128 * MT;
     static constexpr int kSlot = BN * DP * 2;
-    static constexpr int kSlots = DP == 64 ? 6 : 4;  // even: a producer sees keys only or values only
+    static constexpr int kSlots = DP == 64 && MT == 1 ? 6 : 4;  // even: a producer sees keys only or values only
     static constexpr int kQTile = 128 * DP * 2;
     static constexpr int kQBufs = MT == 2 ? 2 : DP == 256 ? 1 : 2;  // MT 2: one for each row tile
     static constexpr int kParts = BN / 32;           // copies of the rows when there are few
@@ -55,6 +55,20 @@ struct Tc {
 template <int ROWS>
 PP_DEVINL int all_see(const AttnArgs& a, const Part& p) {
     return a.mask ? p.seq.ctx : p.seq.ctx + (int)((unsigned)p.j * ROWS / (unsigned)a.group) + 1;
+}
+
+// Key tiles [p.t0, tile_end) of the part are of use to row tile m (MT 2: the
+// first one's rows end earlier in a prompt; a short item leaves the second
+// one empty).
+template <int BN, int MT>
+PP_DEVINL int tile_end(const AttnArgs& a, const Part& p, int m) {
+    if (MT == 1) return p.t1;
+    const int rows = p.seq.n * a.group - p.j * 128 * MT;
+    if (128 * m >= rows) return p.t0;
+    if (a.mask) return p.t1;
+    const unsigned last = ((unsigned)p.j * (128 * MT) + 128u * (unsigned)(m + 1) - 1u) / (unsigned)a.group;
+    const int end = p.seq.ctx + min(p.seq.n, (int)last + 1);
+    return max(p.t0, min(p.t1, (end + BN - 1) / BN));
 }
 
 // Bits of the 32 entries from k0 on that new token `tok` sees.
@@ -85,27 +99,64 @@ PP_DEVINL bool sees(const AttnArgs& a, const Part& p, int tok, int j) {  // new 
     return j < 32 * a.mask_words && (a.mask[(size_t)(p.seq.q0 + tok) * a.mask_words + (j >> 5)] >> (j & 31) & 1u);
 }
 
-// Position in a CTA's stretch: tile t of part p.
+// A warp's walk over the CTA's stretch, in shared memory: it changes once a
+// part, and the registers are the scores'.
 template <int ROWS, int TOK>
-struct Cursor {
+struct WarpWalk {
     Walk<ROWS, TOK> w;
     Part p;
     int t;
-    PP_DEVINL explicit Cursor(const Walk<ROWS, TOK>& walk) : w(walk) {
+    PP_DEVINL void begin(const Walk<ROWS, TOK>& walk) {  // lane 0
+        w = walk;
+        w.begin();
         w.next(p);
-        t = p.t0;
     }
-    // k tiles further; the caller stays inside the stretch.  True if a new part began.
-    PP_DEVINL bool advance(int k) {
-        t += k;
-        bool moved = false;
-        while (t >= p.t1) {
-            const int over = t - p.t1;
-            if (!w.next(p)) break;
-            t = p.t0 + over;
-            moved = true;
+    PP_DEVINL bool step_part(int lane) {  // whole warp: the next part
+        __syncwarp();
+        int more = 0;
+        if (lane == 0) more = w.next(p);
+        more = __shfl_sync(kFull, more, 0);
+        __syncwarp();
+        return more;
+    }
+    // one thread: the part that tile t of the line of parts lies in; t becomes
+    // its tile there
+    __device__ __noinline__ void pass(int from) {
+        int over = from - p.t1;
+        while (w.next(p)) {
+            if (p.t0 + over < p.t1) break;
+            over -= p.t1 - p.t0;
         }
-        return moved;
+        t = p.t0 + over;
+    }
+};
+
+// A position in the stretch, in registers: tile t of the part [t0, t1).
+template <int ROWS, int TOK>
+struct TileAt {
+    WarpWalk<ROWS, TOK>& ww;
+    int t, t0, t1;
+    PP_DEVINL explicit TileAt(WarpWalk<ROWS, TOK>& w) : ww(w), t(w.p.t0), t0(w.p.t0), t1(w.p.t1) {}
+    PP_DEVINL void reload() {
+        t = ww.t;
+        t0 = ww.p.t0;
+        t1 = ww.p.t1;
+    }
+    // k tiles further (the caller stays inside the stretch); true in another part
+    PP_DEVINL bool step(int k) {  // one thread
+        t += k;
+        if (t < t1) return false;
+        ww.pass(t);
+        reload();
+        return true;
+    }
+    PP_DEVINL void step_warp(int k, int lane) {
+        t += k;
+        if (t < t1) return;
+        __syncwarp();
+        if (lane == 0) ww.pass(t);
+        __syncwarp();
+        reload();
     }
 };
 
@@ -198,10 +249,66 @@ PP_DEVINL void add_nonfinite(const AttnArgs& a, const Part& p, int row, int d, i
     for (int i = 0; i < 8; i++) o[i] = t[i];
 }
 
+// Scores of 32 N keys of one row, from t_s in TMEM (this warp's lanes).
+template <int N>
+struct Scores {
+    uint32_t s[32 * N];
+    PP_DEVINL void load(uint32_t t_s) {
+#pragma unroll
+        for (int c = 0; c < N; c++) tmem_ld32(t_s + 32 * c, *reinterpret_cast<uint32_t(*)[32]>(s + 32 * c));
+        tmem_ld_wait();
+    }
+    PP_DEVINL void hide(const AttnArgs& a, const Part& p, int tok, int k0) {
+#pragma unroll
+        for (int c = 0; c < N; c++) {
+            const uint32_t see = seen_bits(a, p, tok, k0 + 32 * c);
+#pragma unroll
+            for (int i = 0; i < 32; i++)
+                if (!(see >> i & 1u)) s[32 * c + i] = __float_as_uint(-INFINITY);
+        }
+    }
+    PP_DEVINL float max() const {
+        float t[4] = {__uint_as_float(s[0]), __uint_as_float(s[1]), __uint_as_float(s[2]), __uint_as_float(s[3])};
+#pragma unroll
+        for (int i = 4; i < 32 * N - 4; i += 8)
+#pragma unroll
+            for (int k = 0; k < 4; k++)
+                t[k] = max3(t[k], __uint_as_float(s[i + 2 * k]), __uint_as_float(s[i + 2 * k + 1]));
+        float u = max3(t[0], t[1], __uint_as_float(s[32 * N - 4])), v = max3(t[2], t[3], __uint_as_float(s[32 * N - 3]));
+        return max3(max3(u, v, __uint_as_float(s[32 * N - 2])), __uint_as_float(s[32 * N - 1]), u);
+    }
+    // weights 2^(s scale - base) to t_p as bf16 pairs; returns their sum
+    PP_DEVINL float weigh(uint32_t t_p, float scale, float base) {
+        const unsigned long long sc = pair2(scale, scale), nb = pair2(-base, -base);
+        unsigned long long sum0 = 0ull, sum1 = 0ull;
+#pragma unroll
+        for (int c = 0; c < N; c++) {
+            uint32_t w[16];
+#pragma unroll
+            for (int i = 0; i < 16; i++) {
+                const int e = 32 * c + 2 * i;
+                float x, y;
+                unpair2(fma2(pair2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), sc, nb), x, y);
+                x = ex2(x);
+                y = ex2(y);
+                w[i] = pack_bf16x2(x, y);
+                if (i & 1)
+                    sum1 = add2(sum1, pair2(x, y));
+                else
+                    sum0 = add2(sum0, pair2(x, y));
+            }
+            tmem_st16(t_p + 16 * c, w);
+        }
+        float x, y;
+        unpair2(add2(sum0, sum1), x, y);
+        return x + y;
+    }
+};
+
 template <int DP, int MT>
 __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
     attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensorMap map_k,
-                   const __grid_constant__ CUtensorMap map_v) {
+                   const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_q) {
     using C = Tc<DP, MT>;
     constexpr int BN = C::BN, NG = C::NG, ROWS = C::kRows, NS = C::kSlots;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
@@ -215,6 +322,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
     __shared__ float stat_m[4][32], stat_l[4][32];
     __shared__ unsigned last_s;
     __shared__ volatile unsigned bad_s;  // a value was taken out of a tile
+    __shared__ WarpWalk<ROWS, BN> walks[C::kWarps + 1];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint64_t lim = a.timeout_ns;
     pdl_launch_dependents();
@@ -243,8 +351,18 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
     tc_fence_after();
     const uint32_t tmem = taddr_s;
     pdl_wait();
-    const Walk<ROWS, BN> walk = start_walk<ROWS, BN>(&a, scratch);
-    const int tiles = (int)(walk.end - walk.at);  // of this CTA
+    int tiles;  // of this CTA
+    WarpWalk<ROWS, BN>& ww = walks[warp];
+    {
+        const Walk<ROWS, BN> walk = start_walk<ROWS, BN>(&a, scratch);
+        tiles = (int)(walk.end - walk.at);
+        if (lane == 0 && tiles > 0) {
+            ww.begin(walk);
+            if (warp == C::kSoftWarps) walks[C::kWarps].begin(walk);
+        }
+        __syncwarp();
+    }
+    const Part& p = ww.p;
 
     if (tiles <= 0) {
         // nothing for this CTA
@@ -252,7 +370,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
         // ------------------------------------------------- producer of one slot
         const int slot = warp - (C::kSoftWarps + 2);
         unsigned char* dst = ring + slot * C::kSlot;
-        Cursor<ROWS, BN> cur(walk);
+        TileAt<ROWS, BN> pt(ww);
         int at = 0, uses = 0, fixes = 0;
         for (int pos = slot;; pos += NS, uses++) {
             // order of the loads: K0 K1 V0 K2 V1 K3 ... (MT 1: scores run two
@@ -260,10 +378,9 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
             const bool key = MT == 1 ? pos == 0 || (pos & 1) : !(pos & 1);
             const int g = MT == 1 ? (pos == 0 ? 0 : key ? (pos + 1) / 2 : (pos - 2) / 2) : pos / 2;
             if (g >= tiles) break;
-            cur.advance(g - at);
+            pt.step_warp(g - at, lane);
             at = g;
-            const Part& p = cur.p;
-            const int k0 = cur.t * BN;
+            const int k0 = pt.t * BN;
             const int end = min(p.key_end - k0, BN);  // rows of the tile that exist
             // values: rows that some row of queries does not see are looked through, rows past the end set to zero
             const int open = key ? BN : max(all_see<ROWS>(a, p) - k0, 0);
@@ -322,15 +439,27 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
         }
     } else if (warp == C::kSoftWarps + 1) {
         // --------------------------------------------------------- rows of q
-        Walk<ROWS, BN> w = walk;
-        Part p;
-        for (int n = 0; w.next(p); n++) {
+        int n = 0;
+        do {
             const int rows = p.seq.n * a.group - p.j * ROWS;
 #pragma unroll 1
             for (int m = 0; m < MT; m++) {
                 const int buf = MT == 2 ? m : n % C::kQBufs, use = MT == 2 ? n : n / C::kQBufs;
                 const bool few = MT == 1 && rows <= 32;
                 if (use > 0) mbar_wait(&qempty[buf], (uint32_t)(use - 1) & 1u, a.status, lim);
+                if (a.q_box) {
+                    // boxes of 32 rows; past the item's rows they hold other tokens' (rows that nobody reads)
+                    if (lane == 0) mbar_arrive_expect_tx(&qfull[buf], C::kQTile);
+                    __syncwarp();
+                    if (lane < 4 * NG) {
+                        const int x = lane / NG, grp = lane % NG;
+                        const int row = p.j * ROWS + 128 * m + (few ? 0 : 32 * x);
+                        tma_load_3d(qs + buf * C::kQTile + grp * 128 * 128 + x * 32 * 128, &map_q, grp * 64,
+                                    p.h * a.group, p.seq.q0 + row / a.group, &qfull[buf]);
+                    }
+                    __syncwarp();
+                    continue;
+                }
                 __syncwarp();
 #pragma unroll 1
                 for (int x = 0; x < 4; x++) {
@@ -344,73 +473,75 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&qfull[buf]);
             }
-        }
+            n++;
+        } while (ww.step_part(lane));
     } else if (warp == C::kSoftWarps) {
         // ---------------------------------------------------------- products
         if (lane == 0) {
             constexpr uint32_t id_s = idesc_bf16_m128(BN), id_o = idesc_bf16_m128_bn(DP);
-            Cursor<ROWS, BN> cs(walk), co(walk);  // scores, values
+            TileAt<ROWS, BN> cs(ww), co(walks[C::kWarps]);  // scores, values
             int part_s = 0;
+            int end_s[2], end_o[2];     // of the cursors' parts
+            uint32_t n_o[2] = {0u, 0u};  // value products issued
+            auto ends = [&](const TileAt<ROWS, BN>& c, int (&e)[2]) {
+                e[0] = tile_end<BN, MT>(a, c.ww.p, 0);
+                e[1] = MT == 1 ? 0 : tile_end<BN, MT>(a, c.ww.p, 1);
+            };
+            ends(cs, end_s);
+            ends(co, end_o);
             // scores of tile g for row tile m
             auto scores = [&](int g, int m) {
                 const int buf = MT == 2 ? m : part_s % C::kQBufs, use = MT == 2 ? part_s : part_s / C::kQBufs;
                 const int pos = MT == 1 ? (g == 0 ? 0 : 2 * g - 1) : 2 * g;
                 const int sl = MT == 1 ? g & 1 : m;
-                if (cs.t == cs.p.t0) mbar_wait(&qfull[buf], (uint32_t)use & 1u, a.status, lim);
-                mbar_wait(&full[pos % NS], (uint32_t)(pos / NS) & 1u, a.status, lim);
-                tc_fence_after();
-                const unsigned char* kt = ring + (pos % NS) * C::kSlot;
-                const unsigned char* qt = qs + buf * C::kQTile;
+                if (cs.t == cs.t0) mbar_wait(&qfull[buf], (uint32_t)use & 1u, a.status, lim);
+                if (cs.t < (m ? end_s[1] : end_s[0])) {
+                    mbar_wait(&full[pos % NS], (uint32_t)(pos / NS) & 1u, a.status, lim);
+                    tc_fence_after();
+                    const unsigned char* kt = ring + (pos % NS) * C::kSlot;
+                    const unsigned char* qt = qs + buf * C::kQTile;
 #pragma unroll
-                for (int d = 0; d < NG; d++)
-                    umma_k64(tmem + (uint32_t)(sl * BN), qt + d * 128 * 128, kt + d * BN * 128, id_s, d > 0);
-                umma_commit(&sfull[sl]);
-                if (cs.t + 1 == cs.p.t1) umma_commit(&qempty[buf]);
+                    for (int d = 0; d < NG; d++)
+                        umma_k64(tmem + (uint32_t)(sl * BN), qt + d * 128 * 128, kt + d * BN * 128, id_s, d > 0);
+                    umma_commit(&sfull[sl]);
+                }
+                if (cs.t + 1 == cs.t1) umma_commit(&qempty[buf]);
                 if (m == MT - 1) umma_commit(&empty[pos % NS]);
             };
             auto values = [&](int g, int m) {
                 const int pos = MT == 1 ? 2 * g + 2 : 2 * g + 1;
                 const int sl = MT == 1 ? g & 1 : m;
-                const uint32_t par = (uint32_t)(MT == 1 ? g >> 1 : g) & 1u;
-                mbar_wait(&full[pos % NS], (uint32_t)(pos / NS) & 1u, a.status, lim);
-                mbar_wait(&pfull[sl], par, a.status, lim);
-                tc_fence_after();
-                const uint64_t vd = sdesc_sw128_n(ring + (pos % NS) * C::kSlot, BN * 128);
+                if (co.t < (m ? end_o[1] : end_o[0])) {
+                    mbar_wait(&full[pos % NS], (uint32_t)(pos / NS) & 1u, a.status, lim);
+                    const uint32_t n = m ? n_o[1]++ : n_o[0]++;
+                    mbar_wait(&pfull[sl], (MT == 1 ? n >> 1 : n) & 1u, a.status, lim);
+                    tc_fence_after();
+                    const uint64_t vd = sdesc_sw128_n(ring + (pos % NS) * C::kSlot, BN * 128);
 #pragma unroll
-                for (int k = 0; k < BN / 16; k++)
-                    umma_bf16_ta(tmem + C::kTmemO + (uint32_t)(m * DP), tmem + (uint32_t)(sl * BN + 8 * k),
-                                 vd + (uint64_t)(k * 128), id_o, (co.t > co.p.t0 || k > 0) ? 1u : 0u);
-                umma_commit(&odone[sl]);
+                    for (int k = 0; k < BN / 16; k++)
+                        umma_bf16_ta(tmem + C::kTmemO + (uint32_t)(m * DP), tmem + (uint32_t)(sl * BN + 8 * k),
+                                     vd + (uint64_t)(k * 128), id_o, (co.t > co.t0 || k > 0) ? 1u : 0u);
+                    umma_commit(&odone[sl]);
+                }
                 if (m == MT - 1) umma_commit(&empty[pos % NS]);
             };
-            auto step = [&]() {
-                if (cs.advance(1)) part_s++;
-            };
-            if (MT == 1) {
-                scores(0, 0);
-                step();
-                if (tiles > 1) {
-                    scores(1, 0);
-                    step();
+            // MT 1: scores run two tiles ahead of the values, MT 2: one, row tile by row tile
+            constexpr int kAhead = MT == 1 ? 2 : 1;
+#pragma unroll 1
+            for (int g = 0; g < tiles + kAhead; g++) {
+                // at a new part its queries may still be on their way: the old part's values go first
+                const bool fresh = MT == 2 && cs.t == cs.t0;
+#pragma unroll 1
+                for (int i = 0; i < 2 * MT; i++) {
+                    const int m = MT == 1 ? 0 : fresh ? i & 1 : i >> 1;
+                    const bool values_now = MT == 1 ? i == 0 : fresh ? i < 2 : !(i & 1);
+                    if (values_now && g >= kAhead) values(g - kAhead, m);
+                    if (!values_now && g < tiles) scores(g, m);
                 }
-                for (int g = 0; g < tiles; g++) {
-                    values(g, 0);
-                    co.advance(1);
-                    if (g + 2 < tiles) {
-                        scores(g + 2, 0);
-                        step();
-                    }
-                }
-            } else {
-                for (int m = 0; m < MT; m++) scores(0, m);
-                step();
-                for (int g = 0; g < tiles; g++) {
-                    for (int m = 0; m < MT; m++) {
-                        values(g, m);
-                        if (g + 1 < tiles) scores(g + 1, m);
-                    }
-                    co.advance(1);
-                    step();
+                if (g >= kAhead && g - kAhead + 1 < tiles && co.step(1)) ends(co, end_o);
+                if (g + 1 < tiles && cs.step(1)) {
+                    part_s++;
+                    ends(cs, end_s);
                 }
             }
         }
@@ -420,8 +551,6 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
         const int m = warp >> 2, wq = warp & 3;  // row tile, quarter of its lanes
         const uint32_t lanes = (uint32_t)(32 * wq) << 16;
         const uint32_t t_o = tmem + C::kTmemO + (uint32_t)(m * DP) + lanes;
-        Walk<ROWS, BN> w = walk;
-        Part p;
         int g = 0;  // tile of the stretch
         // O holds the products up to tile x (the last or last but one whose
         // scores this warp has seen, so a parity names its phase)
@@ -429,7 +558,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
             mbar_wait(&odone[MT == 1 ? x & 1 : m], (uint32_t)(MT == 1 ? x >> 1 : x) & 1u, a.status, lim);
             tc_fence_after();
         };
-        while (w.next(p)) {
+        do {
             const int rows = min(ROWS, p.seq.n * a.group - p.j * ROWS);
             const bool few = MT == 1 && rows <= 32;
             const int r = few ? lane : tid;  // row of the item
@@ -437,99 +566,80 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
             const int tok = min((p.j * ROWS + r) / a.group, p.seq.n - 1);
             const int open = all_see<ROWS>(a, p);
             float mx = -INFINITY, sum = 0.f;
-            for (int t = p.t0; t < p.t1; t++, g++) {
+            const int t_end = tile_end<BN, MT>(a, p, m);
+            // the running maximum after tile t, whose largest score is tm
+            auto raise = [&](float tm, int t) {
+                tm *= a.scale_log2;
+                const bool grow = tm > mx + kLazy || (mx == -INFINITY && tm > mx);
+                if (t == p.t0) {
+                    mx = tm;
+                } else if (__any_sync(kFull, grow)) {
+                    // every product before this tile's is done; this tile's waits for us
+                    products_done(g - 1);
+                    const float top = grow ? tm : mx;
+                    const float f = grow ? ex2(mx - top) : 1.f;  // 0 from -inf
+                    mx = top;
+                    sum *= f;
+#pragma unroll 1
+                    for (int c = 0; c < DP; c += 16) {
+                        uint32_t o[16];
+                        tmem_ld16(t_o + c, o);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 16; i++) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                        tmem_st16(t_o + c, o);
+                    }
+                }
+                return mx == -INFINITY ? 0.f : mx;
+            };
+            for (int t = p.t0; t < t_end; t++, g++) {
                 const int sl = MT == 1 ? g & 1 : m;
                 const uint32_t par = (uint32_t)(MT == 1 ? g >> 1 : g) & 1u;
                 const uint32_t t_s = tmem + (uint32_t)(sl * BN) + lanes;
-                const int k0 = t * BN;
-                const bool masked = k0 + BN > open;
                 mbar_wait(&sfull[sl], par, a.status, lim);
                 tc_fence_after();
                 if (active) {
-                    // the tile's maximum (chunks of 32 keys; few rows: this warp's only)
-                    const int c0 = few ? wq : 0, c1 = few ? wq + 1 : BN / 32;
-                    float tm = -INFINITY;
-#pragma unroll 1
-                    for (int c = c0; c < c1; c++) {
-                        uint32_t s[32];
-                        tmem_ld32(t_s + 32 * c, s);
-                        const uint32_t see = masked ? seen_bits(a, p, tok, k0 + 32 * c) : 0xffffffffu;
-                        tmem_ld_wait();
-                        if (masked) {
-#pragma unroll
-                            for (int i = 0; i < 32; i++)
-                                if (!(see >> i & 1u)) s[i] = __float_as_uint(-INFINITY);
-                        }
-                        float tn = -INFINITY;
-#pragma unroll
-                        for (int i = 0; i < 32; i += 2) {
-                            tm = fmaxf(tm, __uint_as_float(s[i]));
-                            tn = fmaxf(tn, __uint_as_float(s[i + 1]));
-                        }
-                        tm = fmaxf(tm, tn);
-                    }
-                    tm *= a.scale_log2;
-                    const bool grow = tm > mx + kLazy || (mx == -INFINITY && tm > mx);
-                    if (t == p.t0) {
-                        mx = tm;
-                    } else if (__any_sync(kFull, grow)) {
-                        // every product before this tile's is done; this tile's waits for us
-                        products_done(g - 1);
-                        const float top = grow ? tm : mx;
-                        const float f = grow ? ex2(mx - top) : 1.f;  // 0 from -inf
-                        mx = top;
-                        sum *= f;
-#pragma unroll 1
-                        for (int c = 0; c < DP; c += 32) {
-                            uint32_t o[32];
-                            tmem_ld32(t_o + c, o);
-                            tmem_ld_wait();
-#pragma unroll
-                            for (int i = 0; i < 32; i++) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                            tmem_st32(t_o + c, o);
-                        }
-                    }
-                    const float base = mx == -INFINITY ? 0.f : mx;
-                    // weights over the scores: chunk c of P lies in columns that chunk c of S has left
-                    float s0 = 0.f, s1 = 0.f;
-#pragma unroll 1
-                    for (int c = c0; c < c1; c++) {
-                        uint32_t s[32], pw[16];
-                        tmem_ld32(t_s + 32 * c, s);
-                        const uint32_t see = masked ? seen_bits(a, p, tok, k0 + 32 * c) : 0xffffffffu;
-                        tmem_ld_wait();
-                        if (masked) {
-#pragma unroll
-                            for (int i = 0; i < 32; i++)
-                                if (!(see >> i & 1u)) s[i] = __float_as_uint(-INFINITY);
-                        }
-#pragma unroll
-                        for (int i = 0; i < 16; i++) {
-                            const float x0 = ex2(fmaf(__uint_as_float(s[2 * i]), a.scale_log2, -base));
-                            const float x1 = ex2(fmaf(__uint_as_float(s[2 * i + 1]), a.scale_log2, -base));
-                            pw[i] = pack_bf16x2(x0, x1);
-                            s0 += bf16lo(pw[i]);  // the sum of the weights as the product sees them
-                            s1 += bf16hi(pw[i]);
-                        }
-                        tmem_st16(t_s + 16 * c, pw);
-                    }
-                    if (few) {  // the other warps' keys
-                        const uint32_t z[16] = {};
+                    const int k0 = t * BN;
+                    const bool masked = k0 + BN > open;
+                    if (few) {
+                        Scores<1> s;
+                        s.load(t_s + 32 * wq);
+                        if (masked) s.hide(a, p, tok, k0 + 32 * wq);
+                        sum += s.weigh(t_s + 16 * wq, a.scale_log2, raise(s.max(), t));
+                        const uint32_t z[16] = {};  // the other warps' keys
 #pragma unroll 1
                         for (int c = 0; c < BN / 32; c++)
                             if (c != wq) tmem_st16(t_s + 16 * c, z);
+                    } else {
+                        // 64 scores in registers at a time; the first half's weights leave the second half's scores in place
+                        Scores<2> s;
+                        float tm = -INFINITY, part = 0.f;
+#pragma unroll 1
+                        for (int c = 0; c < BN; c += 64) {
+                            s.load(t_s + c);
+                            if (masked) s.hide(a, p, tok, k0 + c);
+                            tm = fmaxf(tm, s.max());
+                        }
+                        const float base = raise(tm, t);
+#pragma unroll 1
+                        for (int c = 0; c < BN; c += 64) {
+                            s.load(t_s + c);
+                            if (masked) s.hide(a, p, tok, k0 + c);
+                            part += s.weigh(t_s + c / 2, a.scale_log2, base);
+                        }
+                        sum += part;
                     }
-                    sum += s0 + s1;
                     tmem_st_wait();
                 }
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&pfull[sl]);
             }
+            const bool none = t_end == p.t0;  // no tile of use to this row tile
             // ------------------------------------------------ end of the part
-            products_done(g - 1);
+            if (!none) products_done(g - 1);
             const bool whole = p.whole(), bad = bad_s != 0;
-            const Split<ROWS, BN> sp = whole ? Split<ROWS, BN>() : Split<ROWS, BN>(w.sched, p);
+            const Split<ROWS, BN> sp = whole ? Split<ROWS, BN>() : Split<ROWS, BN>(ww.w.sched, p);
             float* place = whole ? nullptr : sp.place(a, blockIdx.x);
             const int D = a.head_dim;
             if (few) {
@@ -588,16 +698,17 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                 const float inv = sum == 0.f ? 0.f : 1.f / sum;
                 char* dst = a.out + row_offset(a, p, p.j * ROWS + min(r, rows - 1), a.out_stride, 2);
 #pragma unroll 1
-                for (int c = 0; c < D; c += 32) {
-                    uint32_t u[32];
-                    tmem_ld32(t_o + c, u);
+                for (int c = 0; c < D; c += 16) {
+                    uint32_t u[16];
+                    tmem_ld16(t_o + c, u);
                     tmem_ld_wait();
                     if (r >= rows) continue;
-                    for (int i = 0; i < 32; i += 8) {
+#pragma unroll
+                    for (int i = 0; i < 16; i += 8) {
                         if (c + i >= D) break;
                         float o[8];
 #pragma unroll
-                        for (int x = 0; x < 8; x++) o[x] = __uint_as_float(u[i + x]);
+                        for (int x = 0; x < 8; x++) o[x] = none ? 0.f : __uint_as_float(u[i + x]);
                         if (bad) add_nonfinite(a, p, p.j * ROWS + r, c + i, BN, o);
                         if (whole) {
 #pragma unroll
@@ -617,17 +728,12 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
             }
             tc_fence_before();
             if (!whole) {
-                __threadfence();
                 named_bar_sync(1, 32 * C::kSoftWarps);
-                if (tid == 0) {
-                    last_s = atomicAdd(a.counters + sp.c0, 1u) == (unsigned)(sp.c1 - sp.c0);
-                    if (last_s) a.counters[sp.c0] = 0;
-                    __threadfence();
-                }
+                if (tid == 0) last_s = arrive_last(a.counters + sp.c0, (unsigned)(sp.c1 - sp.c0 + 1));
                 named_bar_sync(1, 32 * C::kSoftWarps);
                 if (last_s) merge_parts<__nv_bfloat16, ROWS, BN>(a, p, sp, tid, 32 * C::kSoftWarps);
             }
-        }
+        } while (ww.step_part(lane));
     }
     tc_fence_before();
     __syncthreads();
@@ -655,6 +761,20 @@ bool cache_map(CUtensorMap* map, const AttnArgs& a, const char* base) {
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// q as a 3-D tensor (element, head, token), boxes of 64 elements x 32 rows of
+// one key head's group, token-major.
+bool query_map(CUtensorMap* map, const AttnArgs& a) {
+    auto enc = tensor_map_encoder();
+    if (!enc) return false;
+    const cuuint64_t dims[3] = {(cuuint64_t)a.head_dim, (cuuint64_t)a.n_kv_heads * a.group, (cuuint64_t)a.batch.n_tokens};
+    const cuuint64_t strides[2] = {(cuuint64_t)a.head_dim * 2, (cuuint64_t)a.q_stride};
+    const cuuint32_t box[3] = {64, (cuuint32_t)a.group, (cuuint32_t)(32 / a.group)};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<char*>(a.q), dims, strides, box, estr,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int DP, int MT>
 cudaError_t go(AttnArgs a, int sms, cudaStream_t st) {
     using C = Tc<DP, MT>;
@@ -665,10 +785,12 @@ cudaError_t go(AttnArgs a, int sms, cudaStream_t st) {
     // whole 8-row swizzle atoms; else 16-byte cp.async, for any page
     const int ps = a.batch.page_size;
     a.box = ps >= 8 && (C::BN % ps == 0 || ps % C::BN == 0) ? (ps < C::BN ? ps : C::BN) : 0;
-    CUtensorMap mk{}, mv{};
+    CUtensorMap mk{}, mv{}, mq{};
     if (a.box && (!cache_map(&mk, a, a.cache.k) || !cache_map(&mv, a, a.cache.v))) a.box = 0;
+    // rows of q: 32 of one key head are whole tokens where the group divides 32
+    a.q_box = 32 % a.group == 0 && query_map(&mq, a);
     return launch_overlapped(kern, dim3((unsigned)(sms < kAttnTcGrid ? sms : kAttnTcGrid)), dim3(C::kWarps * 32),
-                             C::kSmem, st, a, mk, mv);
+                             C::kSmem, st, a, mk, mv, mq);
 }
 
 }  // namespace

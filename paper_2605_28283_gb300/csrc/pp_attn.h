@@ -66,7 +66,8 @@ struct AttnArgs {
     const uint32_t* mask;
     int mask_words;
     int n_kv_heads, group, head_dim;
-    int box;             // tokens of a TMA box, 0: copied row by row
+    int box;             // tokens of a TMA box of the cache, 0: copied row by row
+    int q_box;           // whether the rows of q go by TMA
     float scale_log2;    // scale * log2(e): softmax in powers of two
     float* part;         // partial results of split items
     unsigned* counters;  // arrivals per split item, zero at rest

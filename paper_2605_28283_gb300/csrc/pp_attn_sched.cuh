@@ -91,7 +91,7 @@ struct Walk {
     Seq seq;
     int m;
 
-    PP_DEVINL void enter(int b_, long long base_) {
+    __device__ __noinline__ void enter(int b_, long long base_) {
         b = b_;
         base = base_;
         seq = load_seq(sched.a->batch, b);
@@ -110,8 +110,13 @@ struct Walk {
         }
     }
 
-    // The next part; false at the end of the stretch.
-    PP_DEVINL bool next(Part& p) {
+    // Into the sequence that start_walk found.
+    PP_DEVINL void begin() { enter(b, base); }
+
+    // The next part; false at the end of the stretch.  Out of line: it runs
+    // once a part, at several places of a kernel that is short of instruction
+    // cache.
+    __device__ __noinline__ bool next(Part& p) {
         if (at >= end) return false;
         while (m == 0 || h >= sched.a->n_kv_heads) enter(b + 1, m == 0 ? base : head_base);
         p.b = b;
@@ -135,64 +140,76 @@ struct Walk {
     }
 };
 
+// Sum over the CTA's threads before this one; *all is the sum over all.
+// sums: one word a warp.  Out of line, like what follows: run once, and short
+// code is what makes it quick.
+static __device__ __noinline__ long long scan_threads(long long v, long long* sums, long long* all) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nwarps = (int)blockDim.x / 32;
+    long long inc = v;
+#pragma unroll 1
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long u = __shfl_up_sync(kFull, inc, o);
+        if (lane >= o) inc += u;
+    }
+    if (lane == 31) sums[warp] = inc;
+    __syncthreads();
+    long long pre = inc - v, total = 0;
+#pragma unroll 1
+    for (int i = 0; i < nwarps; i++) {
+        const long long u = sums[i];
+        if (i < warp) pre += u;
+        total += u;
+    }
+    __syncthreads();
+    *all = total;
+    return pre;
+}
+
+template <int ROWS, int TOK>
+__device__ __noinline__ long long seq_tiles(const Sched<ROWS, TOK>& s, int b, bool report) {
+    const Seq q = load_seq(s.a->batch, b);
+    if (report && q.bad) record_status(s.a->status, PP_ERR_INVALID_ARG);
+    return s.head_tiles(q) * s.a->n_kv_heads;
+}
+
 // The line's length and this CTA's first sequence, by all threads of the CTA.
-// scratch: 3 * 32 + 4 words of shared memory (8-byte aligned).
+// scratch: 34 words of shared memory.
 template <int ROWS, int TOK>
 PP_DEVINL Walk<ROWS, TOK> start_walk(const AttnArgs* a, long long* scratch) {
     Walk<ROWS, TOK> w;
     w.sched.a = a;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nwarps = (int)blockDim.x / 32;
-    const int B = a->batch.n_seqs;
-    long long* sums = scratch;       // [32]
+    const int tid = threadIdx.x, B = a->batch.n_seqs, n = (int)blockDim.x;
     long long* found = scratch + 32;  // sequence, its line position
-    // pass 0: the total; pass 1: the sequence that holds this CTA's first tile
-    long long lo = 0, mine = 0;
-    for (int pass = 0; pass < 2; pass++) {
-        long long before = 0;
-        for (int b0 = 0; b0 < B; b0 += (int)blockDim.x) {
-            if (pass == 0 || B > (int)blockDim.x) {
-                mine = 0;
-                if (b0 + tid < B) {
-                    const Seq s = load_seq(a->batch, b0 + tid);
-                    if (pass == 0 && s.bad && blockIdx.x == 0) record_status(a->status, PP_ERR_INVALID_ARG);
-                    mine = w.sched.head_tiles(s) * a->n_kv_heads;
-                }
-            }
-            long long inc = mine;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const long long v = __shfl_up_sync(kFull, inc, o);
-                if (lane >= o) inc += v;
-            }
-            if (lane == 31) sums[warp] = inc;
-            __syncthreads();
-            long long pre = before, chunk = 0;
-            for (int i = 0; i < nwarps; i++) {
-                if (i < warp) pre += sums[i];
-                chunk += sums[i];
-            }
-            if (pass == 1) {
-                const long long e = pre + inc, s = e - mine;
-                if (s <= lo && lo < e) {
-                    found[0] = b0 + tid;
-                    found[1] = s;
-                }
-            }
-            before += chunk;
-            __syncthreads();
-        }
-        if (pass == 0) {
-            w.sched.deal(before, (int)gridDim.x);
-            if ((int)blockIdx.x >= w.sched.ctas) break;  // uniform over the CTA
-            lo = w.sched.begin_of(blockIdx.x);
-        }
+    // the total; with no more sequences than threads the counts and their
+    // sums are kept for the search
+    long long mine = 0, pre = 0, before = 0, all;
+    for (int b0 = 0; b0 < B; b0 += n) {
+        mine = b0 + tid < B ? seq_tiles(w.sched, b0 + tid, blockIdx.x == 0) : 0;
+        pre = before + scan_threads(mine, scratch, &all);
+        before += all;
     }
+    w.sched.deal(before, (int)gridDim.x);
     w.at = w.end = 0;
     w.m = 0;
-    if ((int)blockIdx.x < w.sched.ctas) {
+    if ((int)blockIdx.x < w.sched.ctas) {  // uniform over the CTA
+        const long long lo = w.sched.begin_of(blockIdx.x);
+        before = 0;
+        for (int b0 = 0; b0 < B; b0 += n) {
+            if (B > n) {
+                mine = b0 + tid < B ? seq_tiles(w.sched, b0 + tid, false) : 0;
+                pre = before + scan_threads(mine, scratch, &all);
+                before += all;
+            }
+            if (pre <= lo && lo < pre + mine) {
+                found[0] = b0 + tid;
+                found[1] = pre;
+            }
+        }
+        __syncthreads();
         w.at = lo;
         w.end = w.sched.begin_of((int)blockIdx.x + 1);
-        w.enter((int)found[0], found[1]);
+        w.b = (int)found[0];
+        w.base = found[1];
     }
     return w;
 }
@@ -219,6 +236,17 @@ struct Split {
     }
     PP_DEVINL float* place(const AttnArgs& a, int c) const { return part_place<ROWS>(a, c, c == c0 && c0_tail); }
 };
+
+// Arrival of one part's CTA at its item, after a barrier behind the stores of
+// the part; true for the last one, which then sees every part.  (The barrier
+// orders the other threads' stores before this thread's release.)
+PP_DEVINL bool arrive_last(unsigned* counter, unsigned parts) {
+    unsigned old;
+    asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(old) : "l"(counter) : "memory");
+    if (old + 1 != parts) return false;
+    *counter = 0;  // at rest again; the next launch on the workspace is ordered behind this one
+    return true;
+}
 
 // Address of row r of an item in out (or q, with its own stride).
 PP_DEVINL long long row_offset(const AttnArgs& a, const Part& p, int row, long long stride, int esz) {
