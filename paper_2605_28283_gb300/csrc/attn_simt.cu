@@ -54,7 +54,6 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_consta
     const int s_key = tid % TOK, s_rg = tid / TOK % L::kRG, s_ds = tid / L::kScoreCols;
     // value threads: 4 elements, row group, part of the keys
     const int v_d = tid % L::kD4 * 4, v_rg = tid / L::kD4 % L::kRG, v_ts = tid / (L::kD4 * L::kRG);
-    if (walk.at < walk.end) walk.begin();
     Part p;
     while (walk.next(p)) {
         const int rows = min(ROWS, p.seq.n * a.group - p.j * ROWS);

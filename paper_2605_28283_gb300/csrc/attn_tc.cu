@@ -44,7 +44,8 @@ struct Tc {
     static constexpr int kStage = MT == 1 ? 4 * 32 * 33 * 4 : 0;
     static constexpr int kSmem = kSlots * kSlot + kQBufs * kQTile + kStage + 1024;
     static constexpr int kSoftWarps = 4 * MT;
-    static constexpr int kWarps = kSoftWarps + 2 + kSlots;
+    static constexpr int kWarps = kSoftWarps + 2 + kSlots + 1;  // the last: schedule
+    static constexpr int kReaders = kSoftWarps + 2 + kSlots;    // that free a part
     static constexpr uint32_t kTmemO = 2 * BN;       // S / P slots first
     static constexpr uint32_t kTmemCols = 512;
     static_assert(kTmemO + MT * DP <= 512, "TMEM columns");
@@ -99,64 +100,50 @@ PP_DEVINL bool sees(const AttnArgs& a, const Part& p, int tok, int j) {  // new 
     return j < 32 * a.mask_words && (a.mask[(size_t)(p.seq.q0 + tok) * a.mask_words + (j >> 5)] >> (j & 31) & 1u);
 }
 
-// A warp's walk over the CTA's stretch, in shared memory: it changes once a
-// part, and the registers are the scores'.
+// A part as the warps of the CTA get it from the scheduling warp, in a ring in
+// shared memory: walking the stretch takes divisions and dependent loads that
+// the others' loops are spared.
 template <int ROWS, int TOK>
-struct WarpWalk {
-    Walk<ROWS, TOK> w;
-    Part p;
-    int t;
-    PP_DEVINL void begin(const Walk<ROWS, TOK>& walk) {  // lane 0
-        w = walk;
-        w.begin();
-        w.next(p);
-    }
-    PP_DEVINL bool step_part(int lane) {  // whole warp: the next part
-        __syncwarp();
-        int more = 0;
-        if (lane == 0) more = w.next(p);
-        more = __shfl_sync(kFull, more, 0);
-        __syncwarp();
-        return more;
-    }
-    // one thread: the part that tile t of the line of parts lies in; t becomes
-    // its tile there
-    __device__ __noinline__ void pass(int from) {
-        int over = from - p.t1;
-        while (w.next(p)) {
-            if (p.t0 + over < p.t1) break;
-            over -= p.t1 - p.t0;
-        }
-        t = p.t0 + over;
-    }
+struct Item : Part {
+    int rows;    // query rows of the item
+    int open;    // all_see
+    int end[2];  // tile_end of the row tiles
+    Split<ROWS, TOK> split;  // of a part that is not the whole item
 };
+constexpr int kItems = 8;
 
-// A position in the stretch, in registers: tile t of the part [t0, t1).
+// A reader of the ring, at tile t of part n.
 template <int ROWS, int TOK>
-struct TileAt {
-    WarpWalk<ROWS, TOK>& ww;
-    int t, t0, t1;
-    PP_DEVINL explicit TileAt(WarpWalk<ROWS, TOK>& w) : ww(w), t(w.p.t0), t0(w.p.t0), t1(w.p.t1) {}
-    PP_DEVINL void reload() {
-        t = ww.t;
-        t0 = ww.p.t0;
-        t1 = ww.p.t1;
+struct ItemAt {
+    const Item<ROWS, TOK>* ring;
+    uint64_t *full, *empty;
+    unsigned* status;
+    uint64_t lim;
+    int n, t, t0, t1;
+    PP_DEVINL const Item<ROWS, TOK>& item() const { return ring[n % kItems]; }
+    PP_DEVINL void enter(int n_) {
+        n = n_;
+        mbar_wait(&full[n % kItems], (uint32_t)(n / kItems) & 1u, status, lim);
+        t = t0 = item().t0;
+        t1 = item().t1;
+    }
+    // The next part, by a whole warp (lane) or one thread (-1).  `release`:
+    // this reader counts among those that free an entry.
+    PP_DEVINL void next(int lane, bool release) {
+        if (lane >= 0) __syncwarp();
+        if (release && lane <= 0) mbar_arrive(&empty[n % kItems]);
+        enter(n + 1);
     }
     // k tiles further (the caller stays inside the stretch); true in another part
-    PP_DEVINL bool step(int k) {  // one thread
+    PP_DEVINL bool step(int k, int lane, bool release) {
         t += k;
         if (t < t1) return false;
-        ww.pass(t);
-        reload();
+        do {
+            const int over = t - t1;
+            next(lane, release);
+            t += over;
+        } while (t >= t1);
         return true;
-    }
-    PP_DEVINL void step_warp(int k, int lane) {
-        t += k;
-        if (t < t1) return;
-        __syncwarp();
-        if (lane == 0) ww.pass(t);
-        __syncwarp();
-        reload();
     }
 };
 
@@ -224,29 +211,30 @@ PP_DEVINL bool drop_nonfinite(unsigned char* tile, int r0, int r1, int lane) {
     return __any_sync(kFull, any);
 }
 
-// o[0..7] += the non-finite values at elements d..d+7 of the part's new
-// tokens that row's token sees (their weights are positive).
-__device__ __noinline__ void add_nonfinite_slow(const AttnArgs& a, const Part& p, int row, int d, int bn, float* o) {
+// o[0..N) += the non-finite values at elements d.. of the part's new tokens
+// that row's token sees (their weights are positive).
+__device__ __noinline__ void add_nonfinite_slow(const AttnArgs& a, const Part& p, int row, int d, int n, int bn, float* o) {
     const int tok = row / a.group;
     const int k1 = min(p.key_end, p.t1 * bn);
     for (int k = max(p.seq.ctx, p.t0 * bn); k < k1; k++) {
         if (!sees(a, p, tok, k - p.seq.ctx)) continue;
         const int page = entry_page(a.batch, p.b, k);
         if (page < 0) continue;
-        float v[8];
-        Elem<__nv_bfloat16>::unpack(*reinterpret_cast<const uint4*>(a.cache.v + entry_offset(a.batch, a.cache, page, k) +
-                                                                    (long long)p.h * a.cache.head_stride + d * 2),
-                                    v);
-        for (int i = 0; i < 8; i++)
-            if ((__float_as_uint(v[i]) & 0x7f800000u) == 0x7f800000u) o[i] += v[i];
+        const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(
+            a.cache.v + entry_offset(a.batch, a.cache, page, k) + (long long)p.h * a.cache.head_stride);
+        for (int i = 0; i < n && d + i < a.head_dim; i++) {
+            const float x = __bfloat162float(v[d + i]);
+            if ((__float_as_uint(x) & 0x7f800000u) == 0x7f800000u) o[i] += x;
+        }
     }
 }
 
-PP_DEVINL void add_nonfinite(const AttnArgs& a, const Part& p, int row, int d, int bn, float (&o)[8]) {
-    float t[8];  // in memory only when there is something to add
-    for (int i = 0; i < 8; i++) t[i] = o[i];
-    add_nonfinite_slow(a, p, row, d, bn, t);
-    for (int i = 0; i < 8; i++) o[i] = t[i];
+template <int N>
+PP_DEVINL void add_nonfinite(const AttnArgs& a, const Part& p, int row, int d, int bn, float (&o)[N]) {
+    float t[N];  // in memory only when there is something to add
+    for (int i = 0; i < N; i++) t[i] = o[i];
+    add_nonfinite_slow(a, p, row, d, N, bn, t);
+    for (int i = 0; i < N; i++) o[i] = t[i];
 }
 
 // Scores of 32 N keys of one row, from t_s in TMEM (this warp's lanes).
@@ -322,7 +310,8 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
     __shared__ float stat_m[4][32], stat_l[4][32];
     __shared__ unsigned last_s;
     __shared__ volatile unsigned bad_s;  // a value was taken out of a tile
-    __shared__ WarpWalk<ROWS, BN> walks[C::kWarps + 1];
+    __shared__ Item<ROWS, BN> items[kItems];
+    __shared__ uint64_t ifull[kItems], iempty[kItems];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint64_t lim = a.timeout_ns;
     pdl_launch_dependents();
@@ -339,6 +328,10 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
             mbar_init(&pfull[i], 4);
             mbar_init(&odone[i], 1);
         }
+        for (int i = 0; i < kItems; i++) {
+            mbar_init(&ifull[i], 1);
+            mbar_init(&iempty[i], C::kReaders);
+        }
         fence_mbar_init();
         bad_s = 0;
     }
@@ -351,39 +344,48 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
     tc_fence_after();
     const uint32_t tmem = taddr_s;
     pdl_wait();
-    int tiles;  // of this CTA
-    WarpWalk<ROWS, BN>& ww = walks[warp];
-    {
-        const Walk<ROWS, BN> walk = start_walk<ROWS, BN>(&a, scratch);
-        tiles = (int)(walk.end - walk.at);
-        if (lane == 0 && tiles > 0) {
-            ww.begin(walk);
-            if (warp == C::kSoftWarps) walks[C::kWarps].begin(walk);
-        }
-        __syncwarp();
-    }
-    const Part& p = ww.p;
+    Walk<ROWS, BN> walk = start_walk<ROWS, BN>(&a, scratch);
+    const int tiles = (int)(walk.end - walk.at);  // of this CTA
+    ItemAt<ROWS, BN> at{items, ifull, iempty, a.status, lim, 0, 0, 0, 0};
 
     if (tiles <= 0) {
         // nothing for this CTA
+    } else if (warp == C::kWarps - 1) {
+        // ---------------------------------------------------------- schedule
+        if (lane == 0) {
+            Part p;
+            for (int n = 0; walk.next(p); n++) {
+                Item<ROWS, BN>& it = items[n % kItems];
+                if (n >= kItems) mbar_wait(&iempty[n % kItems], (uint32_t)(n / kItems - 1) & 1u, a.status, lim);
+                static_cast<Part&>(it) = p;
+                it.rows = min(ROWS, p.seq.n * a.group - p.j * ROWS);
+                it.open = all_see<ROWS>(a, p);
+#pragma unroll 1
+                for (int m = 0; m < MT; m++) it.end[m] = tile_end<BN, MT>(a, p, m);
+                if (!p.whole()) it.split = Split<ROWS, BN>(walk.sched, p);
+                mbar_arrive(&ifull[n % kItems]);
+            }
+        }
+        __syncwarp();
     } else if (warp >= C::kSoftWarps + 2) {
         // ------------------------------------------------- producer of one slot
         const int slot = warp - (C::kSoftWarps + 2);
         unsigned char* dst = ring + slot * C::kSlot;
-        TileAt<ROWS, BN> pt(ww);
-        int at = 0, uses = 0, fixes = 0;
+        at.enter(0);
+        int g_at = 0, uses = 0, fixes = 0;
         for (int pos = slot;; pos += NS, uses++) {
             // order of the loads: K0 K1 V0 K2 V1 K3 ... (MT 1: scores run two
             // tiles ahead), K0 V0 K1 V1 ... (MT 2)
             const bool key = MT == 1 ? pos == 0 || (pos & 1) : !(pos & 1);
             const int g = MT == 1 ? (pos == 0 ? 0 : key ? (pos + 1) / 2 : (pos - 2) / 2) : pos / 2;
             if (g >= tiles) break;
-            pt.step_warp(g - at, lane);
-            at = g;
-            const int k0 = pt.t * BN;
+            at.step(g - g_at, lane, true);
+            g_at = g;
+            const Item<ROWS, BN>& p = at.item();
+            const int k0 = at.t * BN;
             const int end = min(p.key_end - k0, BN);  // rows of the tile that exist
             // values: rows that some row of queries does not see are looked through, rows past the end set to zero
-            const int open = key ? BN : max(all_see<ROWS>(a, p) - k0, 0);
+            const int open = key ? BN : max(p.open - k0, 0);
             if (a.box > 0) {
                 // boxes of 64 elements x min(page, BN) tokens, one for a lane at a time
                 const int boxes = (end + a.box - 1) / a.box * NG;
@@ -439,9 +441,10 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
         }
     } else if (warp == C::kSoftWarps + 1) {
         // --------------------------------------------------------- rows of q
-        int n = 0;
-        do {
-            const int rows = p.seq.n * a.group - p.j * ROWS;
+        at.enter(0);
+        for (int left = tiles;;) {
+            const Item<ROWS, BN>& p = at.item();
+            const int rows = p.rows, n = at.n;
 #pragma unroll 1
             for (int m = 0; m < MT; m++) {
                 const int buf = MT == 2 ? m : n % C::kQBufs, use = MT == 2 ? n : n / C::kQBufs;
@@ -464,7 +467,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
 #pragma unroll 1
                 for (int x = 0; x < 4; x++) {
                     const int r = few ? (x < C::kParts ? lane : ROWS) : 128 * m + 32 * x + lane;
-                    const long long off = r < rows && r < ROWS ? row_offset(a, p, p.j * ROWS + r, a.q_stride, 2) : -1;
+                    const long long off = r < rows ? row_offset(a, p, p.j * ROWS + r, a.q_stride, 2) : -1;
                     copy_rows32<DP>(qs + buf * C::kQTile + x * 32 * 128, 128 * 128, a.q, off, a.head_dim, lane);
                 }
                 cp_async_commit();
@@ -473,25 +476,28 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&qfull[buf]);
             }
-            n++;
-        } while (ww.step_part(lane));
+            left -= at.t1 - at.t0;
+            if (left <= 0) break;
+            at.next(lane, true);
+        }
     } else if (warp == C::kSoftWarps) {
         // ---------------------------------------------------------- products
         if (lane == 0) {
             constexpr uint32_t id_s = idesc_bf16_m128(BN), id_o = idesc_bf16_m128_bn(DP);
-            TileAt<ROWS, BN> cs(ww), co(walks[C::kWarps]);  // scores, values
-            int part_s = 0;
-            int end_s[2], end_o[2];     // of the cursors' parts
-            uint32_t n_o[2] = {0u, 0u};  // value products issued
-            auto ends = [&](const TileAt<ROWS, BN>& c, int (&e)[2]) {
-                e[0] = tile_end<BN, MT>(a, c.ww.p, 0);
-                e[1] = MT == 1 ? 0 : tile_end<BN, MT>(a, c.ww.p, 1);
+            ItemAt<ROWS, BN> cs = at, co = at;  // scores, values
+            int end_s[2], end_o[2];             // of the cursors' parts
+            uint32_t n_o[2] = {0u, 0u};         // value products issued
+            auto ends = [&](const ItemAt<ROWS, BN>& c, int (&e)[2]) {
+                e[0] = c.item().end[0];
+                e[1] = c.item().end[MT - 1];
             };
+            cs.enter(0);
+            co.enter(0);
             ends(cs, end_s);
             ends(co, end_o);
             // scores of tile g for row tile m
             auto scores = [&](int g, int m) {
-                const int buf = MT == 2 ? m : part_s % C::kQBufs, use = MT == 2 ? part_s : part_s / C::kQBufs;
+                const int buf = MT == 2 ? m : cs.n % C::kQBufs, use = MT == 2 ? cs.n : cs.n / C::kQBufs;
                 const int pos = MT == 1 ? (g == 0 ? 0 : 2 * g - 1) : 2 * g;
                 const int sl = MT == 1 ? g & 1 : m;
                 if (cs.t == cs.t0) mbar_wait(&qfull[buf], (uint32_t)use & 1u, a.status, lim);
@@ -538,11 +544,8 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                     if (values_now && g >= kAhead) values(g - kAhead, m);
                     if (!values_now && g < tiles) scores(g, m);
                 }
-                if (g >= kAhead && g - kAhead + 1 < tiles && co.step(1)) ends(co, end_o);
-                if (g + 1 < tiles && cs.step(1)) {
-                    part_s++;
-                    ends(cs, end_s);
-                }
+                if (g >= kAhead && g - kAhead + 1 < tiles && co.step(1, -1, true)) ends(co, end_o);
+                if (g + 1 < tiles && cs.step(1, -1, false)) ends(cs, end_s);
             }
         }
         __syncwarp();
@@ -558,20 +561,22 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
             mbar_wait(&odone[MT == 1 ? x & 1 : m], (uint32_t)(MT == 1 ? x >> 1 : x) & 1u, a.status, lim);
             tc_fence_after();
         };
-        do {
-            const int rows = min(ROWS, p.seq.n * a.group - p.j * ROWS);
+        at.enter(0);
+        for (int left = tiles;;) {
+            const Item<ROWS, BN>& p = at.item();
+            const int rows = p.rows;
             const bool few = MT == 1 && rows <= 32;
             const int r = few ? lane : tid;  // row of the item
             const bool active = few ? wq < C::kParts : 32 * warp < rows;
             const int tok = min((p.j * ROWS + r) / a.group, p.seq.n - 1);
-            const int open = all_see<ROWS>(a, p);
+            const int open = p.open, t0 = at.t0;
             float mx = -INFINITY, sum = 0.f;
-            const int t_end = tile_end<BN, MT>(a, p, m);
+            const int t_end = p.end[m];
             // the running maximum after tile t, whose largest score is tm
             auto raise = [&](float tm, int t) {
                 tm *= a.scale_log2;
                 const bool grow = tm > mx + kLazy || (mx == -INFINITY && tm > mx);
-                if (t == p.t0) {
+                if (t == t0) {
                     mx = tm;
                 } else if (__any_sync(kFull, grow)) {
                     // every product before this tile's is done; this tile's waits for us
@@ -592,7 +597,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                 }
                 return mx == -INFINITY ? 0.f : mx;
             };
-            for (int t = p.t0; t < t_end; t++, g++) {
+            for (int t = t0; t < t_end; t++, g++) {
                 const int sl = MT == 1 ? g & 1 : m;
                 const uint32_t par = (uint32_t)(MT == 1 ? g >> 1 : g) & 1u;
                 const uint32_t t_s = tmem + (uint32_t)(sl * BN) + lanes;
@@ -635,11 +640,11 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&pfull[sl]);
             }
-            const bool none = t_end == p.t0;  // no tile of use to this row tile
+            const bool none = t_end == t0;  // no tile of use to this row tile
             // ------------------------------------------------ end of the part
             if (!none) products_done(g - 1);
             const bool whole = p.whole(), bad = bad_s != 0;
-            const Split<ROWS, BN> sp = whole ? Split<ROWS, BN>() : Split<ROWS, BN>(ww.w.sched, p);
+            const Split<ROWS, BN>& sp = p.split;
             float* place = whole ? nullptr : sp.place(a, blockIdx.x);
             const int D = a.head_dim;
             if (few) {
@@ -698,27 +703,29 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                 const float inv = sum == 0.f ? 0.f : 1.f / sum;
                 char* dst = a.out + row_offset(a, p, p.j * ROWS + min(r, rows - 1), a.out_stride, 2);
 #pragma unroll 1
-                for (int c = 0; c < D; c += 16) {
-                    uint32_t u[16];
-                    tmem_ld16(t_o + c, u);
+                for (int c = 0; c < D; c += 32) {
+                    uint32_t u[32];
+                    tmem_ld32(t_o + c, u);
                     tmem_ld_wait();
                     if (r >= rows) continue;
+                    float o[32];
 #pragma unroll
-                    for (int i = 0; i < 16; i += 8) {
-                        if (c + i >= D) break;
-                        float o[8];
+                    for (int i = 0; i < 32; i++) o[i] = none ? 0.f : __uint_as_float(u[i]);
+                    if (bad) add_nonfinite(a, p, p.j * ROWS + r, c, BN, o);
+                    if (whole) {
 #pragma unroll
-                        for (int x = 0; x < 8; x++) o[x] = none ? 0.f : __uint_as_float(u[i + x]);
-                        if (bad) add_nonfinite(a, p, p.j * ROWS + r, c + i, BN, o);
-                        if (whole) {
+                        for (int i = 0; i < 32; i += 8) {
+                            if (c + i >= D) break;
 #pragma unroll
-                            for (int x = 0; x < 8; x++) o[x] *= inv;
-                            *reinterpret_cast<uint4*>(dst + (c + i) * 2) = Elem<__nv_bfloat16>::pack(o);
-                        } else {
-                            float4* out = reinterpret_cast<float4*>(place + (size_t)r * D + c + i);
-                            out[0] = make_float4(o[0], o[1], o[2], o[3]);
-                            out[1] = make_float4(o[4], o[5], o[6], o[7]);
+                            for (int x = 0; x < 8; x++) o[i + x] *= inv;
+                            *reinterpret_cast<uint4*>(dst + (c + i) * 2) = Elem<__nv_bfloat16>::pack(o + i);
                         }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4)
+                            if (c + i < D)
+                                *reinterpret_cast<float4*>(place + (size_t)r * D + c + i) =
+                                    make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
                     }
                 }
                 if (!whole && r < rows) {
@@ -733,7 +740,10 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                 named_bar_sync(1, 32 * C::kSoftWarps);
                 if (last_s) merge_parts<__nv_bfloat16, ROWS, BN>(a, p, sp, tid, 32 * C::kSoftWarps);
             }
-        } while (ww.step_part(lane));
+            left -= at.t1 - at.t0;
+            if (left <= 0) break;
+            at.next(lane, true);
+        }
     }
     tc_fence_before();
     __syncthreads();

@@ -91,7 +91,7 @@ struct Walk {
     Seq seq;
     int m;
 
-    __device__ __noinline__ void enter(int b_, long long base_) {
+    PP_DEVINL void enter(int b_, long long base_) {
         b = b_;
         base = base_;
         seq = load_seq(sched.a->batch, b);
@@ -110,13 +110,8 @@ struct Walk {
         }
     }
 
-    // Into the sequence that start_walk found.
-    PP_DEVINL void begin() { enter(b, base); }
-
-    // The next part; false at the end of the stretch.  Out of line: it runs
-    // once a part, at several places of a kernel that is short of instruction
-    // cache.
-    __device__ __noinline__ bool next(Part& p) {
+    // The next part; false at the end of the stretch.
+    PP_DEVINL bool next(Part& p) {
         if (at >= end) return false;
         while (m == 0 || h >= sched.a->n_kv_heads) enter(b + 1, m == 0 ? base : head_base);
         p.b = b;
@@ -208,7 +203,7 @@ PP_DEVINL Walk<ROWS, TOK> start_walk(const AttnArgs* a, long long* scratch) {
         __syncthreads();
         w.at = lo;
         w.end = w.sched.begin_of((int)blockIdx.x + 1);
-        w.b = (int)found[0];
+        w.b = (int)found[0] - 1;  // next() enters the sequence
         w.base = found[1];
     }
     return w;
@@ -228,7 +223,7 @@ template <int ROWS, int TOK>
 struct Split {
     int c0, c1;
     bool c0_tail;  // the first part lies in c0's second place
-    PP_DEVINL Split() : c0(0), c1(0), c0_tail(false) {}
+    Split() = default;
     PP_DEVINL Split(const Sched<ROWS, TOK>& s, const Part& p) {
         c0 = s.cta_of(p.first);
         c1 = s.cta_of(p.first + p.tiles - 1);
