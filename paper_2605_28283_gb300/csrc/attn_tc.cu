@@ -44,8 +44,10 @@ struct Tc {
     static constexpr int kStage = MT == 1 ? 4 * 32 * 33 * 4 : 0;
     static constexpr int kSmem = kSlots * kSlot + kQBufs * kQTile + kStage + 1024;
     static constexpr int kSoftWarps = 4 * MT;
-    static constexpr int kWarps = kSoftWarps + 2 + kSlots + 1;  // the last: schedule
-    static constexpr int kReaders = kSoftWarps + 2 + kSlots;    // that free a part
+    // warps after the softmax ones: two that issue products, the rows of q, the slots' producers, the schedule
+    static constexpr int kWarpMma = kSoftWarps, kWarpQ = kSoftWarps + 2, kWarpSlot = kSoftWarps + 3;
+    static constexpr int kWarps = kWarpSlot + kSlots + 1;
+    static constexpr int kReaders = kWarps - 1;  // that free a part
     static constexpr uint32_t kTmemO = 2 * BN;       // S / P slots first
     static constexpr uint32_t kTmemCols = 512;
     static_assert(kTmemO + MT * DP <= 512, "TMEM columns");
@@ -318,7 +320,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
     if (tid == 0) {
         for (int i = 0; i < NS; i++) {
             mbar_init(&full[i], 1);
-            mbar_init(&empty[i], 1);
+            mbar_init(&empty[i], MT);
             mbar_init(&landed[i], 1);
         }
         for (int i = 0; i < 2; i++) {
@@ -335,7 +337,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
         fence_mbar_init();
         bad_s = 0;
     }
-    if (warp == C::kSoftWarps) {
+    if (warp == C::kWarpMma) {
         tmem_alloc(&taddr_s, C::kTmemCols);
         tmem_relinquish();
     }
@@ -367,9 +369,9 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
             }
         }
         __syncwarp();
-    } else if (warp >= C::kSoftWarps + 2) {
+    } else if (warp >= C::kWarpSlot) {
         // ------------------------------------------------- producer of one slot
-        const int slot = warp - (C::kSoftWarps + 2);
+        const int slot = warp - C::kWarpSlot;
         unsigned char* dst = ring + slot * C::kSlot;
         at.enter(0);
         int g_at = 0, uses = 0, fixes = 0;
@@ -439,7 +441,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                 if (lane == 0) mbar_arrive(&full[slot]);
             }
         }
-    } else if (warp == C::kSoftWarps + 1) {
+    } else if (warp == C::kWarpQ) {
         // --------------------------------------------------------- rows of q
         at.enter(0);
         for (int left = tiles;;) {
@@ -480,75 +482,80 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
             if (left <= 0) break;
             at.next(lane, true);
         }
-    } else if (warp == C::kSoftWarps) {
+    } else if (warp >= C::kWarpMma) {
         // ---------------------------------------------------------- products
-        if (lane == 0) {
-            constexpr uint32_t id_s = idesc_bf16_m128(BN), id_o = idesc_bf16_m128_bn(DP);
-            ItemAt<ROWS, BN> cs = at, co = at;  // scores, values
-            int end_s[2], end_o[2];             // of the cursors' parts
-            uint32_t n_o[2] = {0u, 0u};         // value products issued
-            auto ends = [&](const ItemAt<ROWS, BN>& c, int (&e)[2]) {
-                e[0] = c.item().end[0];
-                e[1] = c.item().end[MT - 1];
-            };
-            cs.enter(0);
-            co.enter(0);
-            ends(cs, end_s);
-            ends(co, end_o);
-            // scores of tile g for row tile m
-            auto scores = [&](int g, int m) {
-                const int buf = MT == 2 ? m : cs.n % C::kQBufs, use = MT == 2 ? cs.n : cs.n / C::kQBufs;
-                const int pos = MT == 1 ? (g == 0 ? 0 : 2 * g - 1) : 2 * g;
-                const int sl = MT == 1 ? g & 1 : m;
-                if (cs.t == cs.t0) mbar_wait(&qfull[buf], (uint32_t)use & 1u, a.status, lim);
-                if (cs.t < (m ? end_s[1] : end_s[0])) {
-                    mbar_wait(&full[pos % NS], (uint32_t)(pos / NS) & 1u, a.status, lim);
-                    tc_fence_after();
+        // Two warps, so that one's waits and address arithmetic (every wake-up
+        // fetches its code anew) run under the other's products.  MT 2: one
+        // for each row tile, scores one tile ahead of the values; MT 1: one
+        // for the scores (two S slots), one for the values.
+        constexpr uint32_t id_s = idesc_bf16_m128(BN), id_o = idesc_bf16_m128_bn(DP);
+        const int who = __shfl_sync(kFull, warp - C::kWarpMma, 0);
+        const int m = MT == 2 ? who : 0;
+        const bool one = lane == 0;
+        const uint32_t tm = __shfl_sync(kFull, tmem, 0);
+        ItemAt<ROWS, BN> cs = at, co = at;  // scores, values
+        cs.enter(0);
+        co.enter(0);
+        int end_s = cs.item().end[m], end_o = co.item().end[m];
+        auto scores = [&](int g) {
+            const int buf = MT == 2 ? m : cs.n % C::kQBufs, use = MT == 2 ? cs.n : cs.n / C::kQBufs;
+            const int pos = MT == 1 ? (g == 0 ? 0 : 2 * g - 1) : 2 * g;
+            const int sl = MT == 1 ? g & 1 : m;
+            if (cs.t == cs.t0) mbar_wait(&qfull[buf], (uint32_t)use & 1u, a.status, lim);
+            if (cs.t < end_s) {
+                // MT 1: the slot's last weights have been multiplied (MT 2: issued by this warp, in order)
+                if (MT == 1 && g >= 2) mbar_wait(&odone[sl], (uint32_t)((g - 2) >> 1) & 1u, a.status, lim);
+                mbar_wait(&full[pos % NS], (uint32_t)(pos / NS) & 1u, a.status, lim);
+                tc_fence_after();
+                if (one) {
                     const unsigned char* kt = ring + (pos % NS) * C::kSlot;
                     const unsigned char* qt = qs + buf * C::kQTile;
 #pragma unroll
                     for (int d = 0; d < NG; d++)
-                        umma_k64(tmem + (uint32_t)(sl * BN), qt + d * 128 * 128, kt + d * BN * 128, id_s, d > 0);
+                        umma_k64(tm + (uint32_t)(sl * BN), qt + d * 128 * 128, kt + d * BN * 128, id_s, d > 0);
                     umma_commit(&sfull[sl]);
                 }
+            }
+            if (one) {
+                umma_commit(&empty[pos % NS]);
                 if (cs.t + 1 == cs.t1) umma_commit(&qempty[buf]);
-                if (m == MT - 1) umma_commit(&empty[pos % NS]);
-            };
-            auto values = [&](int g, int m) {
-                const int pos = MT == 1 ? 2 * g + 2 : 2 * g + 1;
-                const int sl = MT == 1 ? g & 1 : m;
-                if (co.t < (m ? end_o[1] : end_o[0])) {
-                    mbar_wait(&full[pos % NS], (uint32_t)(pos / NS) & 1u, a.status, lim);
-                    const uint32_t n = m ? n_o[1]++ : n_o[0]++;
-                    mbar_wait(&pfull[sl], (MT == 1 ? n >> 1 : n) & 1u, a.status, lim);
-                    tc_fence_after();
+            }
+            __syncwarp();
+            if (g + 1 < tiles && cs.step(1, lane, MT == 1)) end_s = cs.item().end[m];
+        };
+        uint32_t n_o = 0;  // value products issued
+        auto values = [&](int g) {
+            const int pos = MT == 1 ? 2 * g + 2 : 2 * g + 1;
+            const int sl = MT == 1 ? g & 1 : m;
+            if (co.t < end_o) {
+                mbar_wait(&full[pos % NS], (uint32_t)(pos / NS) & 1u, a.status, lim);
+                mbar_wait(&pfull[sl], (MT == 1 ? n_o >> 1 : n_o) & 1u, a.status, lim);
+                n_o++;
+                tc_fence_after();
+                if (one) {
                     const uint64_t vd = sdesc_sw128_n(ring + (pos % NS) * C::kSlot, BN * 128);
 #pragma unroll
                     for (int k = 0; k < BN / 16; k++)
-                        umma_bf16_ta(tmem + C::kTmemO + (uint32_t)(m * DP), tmem + (uint32_t)(sl * BN + 8 * k),
+                        umma_bf16_ta(tm + C::kTmemO + (uint32_t)(m * DP), tm + (uint32_t)(sl * BN + 8 * k),
                                      vd + (uint64_t)(k * 128), id_o, (co.t > co.t0 || k > 0) ? 1u : 0u);
                     umma_commit(&odone[sl]);
                 }
-                if (m == MT - 1) umma_commit(&empty[pos % NS]);
-            };
-            // MT 1: scores run two tiles ahead of the values, MT 2: one, row tile by row tile
-            constexpr int kAhead = MT == 1 ? 2 : 1;
+            }
+            if (one) umma_commit(&empty[pos % NS]);
+            __syncwarp();
+            if (g + 1 < tiles && co.step(1, lane, true)) end_o = co.item().end[m];
+        };
+        if (MT == 1 && who == 0) {
 #pragma unroll 1
-            for (int g = 0; g < tiles + kAhead; g++) {
-                // at a new part its queries may still be on their way: the old part's values go first
-                const bool fresh = MT == 2 && cs.t == cs.t0;
+            for (int g = 0; g < tiles; g++) scores(g);
+        } else {
 #pragma unroll 1
-                for (int i = 0; i < 2 * MT; i++) {
-                    const int m = MT == 1 ? 0 : fresh ? i & 1 : i >> 1;
-                    const bool values_now = MT == 1 ? i == 0 : fresh ? i < 2 : !(i & 1);
-                    if (values_now && g >= kAhead) values(g - kAhead, m);
-                    if (!values_now && g < tiles) scores(g, m);
-                }
-                if (g >= kAhead && g - kAhead + 1 < tiles && co.step(1, -1, true)) ends(co, end_o);
-                if (g + 1 < tiles && cs.step(1, -1, false)) ends(cs, end_s);
+            for (int g = 0; g < tiles + MT - 1; g++) {
+                // MT 2: at a new part its queries may still be on their way, so the old part's values go first
+                if (MT == 1 || g > 0) values(MT == 1 ? g : g - 1);
+                if (MT == 2 && g < tiles) scores(g);
             }
         }
-        __syncwarp();
     } else {
         // ----------------------------------------------------------- softmax
         const int m = warp >> 2, wq = warp & 3;  // row tile, quarter of its lanes
@@ -747,7 +754,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == C::kSoftWarps) {
+    if (warp == C::kWarpMma) {
         tc_fence_after();
         tmem_dealloc(tmem, C::kTmemCols);
     }
