@@ -211,11 +211,7 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_consta
                     if (r >= rows) break;
                     const float l = Sum[r], inv = l == 0.f ? 0.f : 1.f / l;
                     char* dst = a.out + row_offset(a, p, p.j * ROWS + r, a.out_stride, (int)sizeof(T)) + v_d * (int)sizeof(T);
-                    if (sizeof(T) == 4)
-                        *reinterpret_cast<float4*>(dst) = make_float4(o[i][0] * inv, o[i][1] * inv, o[i][2] * inv, o[i][3] * inv);
-                    else
-                        *reinterpret_cast<uint2*>(dst) = make_uint2(Elem<__nv_bfloat16>::pair(o[i][0] * inv, o[i][1] * inv),
-                                                                    Elem<__nv_bfloat16>::pair(o[i][2] * inv, o[i][3] * inv));
+                    store4<T>(dst, make_float4(o[i][0], o[i][1], o[i][2], o[i][3]), inv);
                 }
             }
             continue;
@@ -234,7 +230,7 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_consta
         __syncthreads();
         if (tid == 0) last_s = arrive_last(a.counters + sp.c0, (unsigned)(sp.c1 - sp.c0 + 1));
         __syncthreads();
-        if (last_s) merge_parts<T, ROWS, TOK>(a, p, sp, tid, kThreads);
+        if (last_s) merge_parts<T, ROWS, TOK, false, 1>(a, p, sp, tid, kThreads);
     }
 }
 

@@ -731,7 +731,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
 #pragma unroll
                         for (int i = 0; i < 32; i += 4)
                             if (c + i < D)
-                                *reinterpret_cast<float4*>(place + (size_t)r * D + c + i) =
+                                *reinterpret_cast<float4*>(place + part_at<ROWS>(true, D, r, (c + i) / 4)) =
                                     make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
                     }
                 }
@@ -745,7 +745,12 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                 named_bar_sync(1, 32 * C::kSoftWarps);
                 if (tid == 0) last_s = arrive_last(a.counters + sp.c0, (unsigned)(sp.c1 - sp.c0 + 1));
                 named_bar_sync(1, 32 * C::kSoftWarps);
-                if (last_s) merge_parts<__nv_bfloat16, ROWS, BN>(a, p, sp, tid, 32 * C::kSoftWarps);
+                if (last_s) {
+                    if (few)
+                        merge_parts<__nv_bfloat16, ROWS, BN, false, 1>(a, p, sp, tid, 32 * C::kSoftWarps);
+                    else
+                        merge_parts<__nv_bfloat16, ROWS, BN, true, 4>(a, p, sp, tid, 32 * C::kSoftWarps);
+                }
             }
             left -= at.t1 - at.t0;
             if (left <= 0) break;

@@ -249,36 +249,79 @@ PP_DEVINL long long row_offset(const AttnArgs& a, const Part& p, int row, long l
     return (long long)(p.seq.q0 + tok) * stride + ((long long)p.h * a.group + g) * a.head_dim * esz;
 }
 
+template <typename T>
+PP_DEVINL void store4(char* dst, const float4& o, float f) {
+    if (sizeof(T) == 4)
+        *reinterpret_cast<float4*>(dst) = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
+    else
+        *reinterpret_cast<uint2*>(dst) = make_uint2(Elem<__nv_bfloat16>::pair(o.x * f, o.y * f),
+                                                    Elem<__nv_bfloat16>::pair(o.z * f, o.w * f));
+}
+
+// Place of 4 sums, elements 4 d4.. of row r.  Many rows (by_row): a thread
+// has a row, and the rows of a warp lie side by side; few: a row's elements do.
+template <int ROWS>
+PP_DEVINL size_t part_at(bool by_row, int D, int r, int d4) {
+    return by_row ? ((size_t)d4 * ROWS + r) * 4 : (size_t)r * D + d4 * 4;
+}
+
 // Adds up the parts of an item and writes its rows, by `nthr` threads (tid of
-// them).  The caller has made the parts visible (arrival counter).
-template <typename T, int ROWS, int TOK>
+// them).  The caller has made the parts visible (arrival counter).  Bound by
+// the latency of the loads: kE elements (of 4 floats) of up to four parts are
+// in flight at once in a thread.
+template <typename T, int ROWS, int TOK, bool by_row, int kE>
 PP_DEVINL void merge_parts(const AttnArgs& a, const Part& p, const Split<ROWS, TOK>& sp, int tid, int nthr) {
+    const int D = a.head_dim, d4s = D / 4;
     const int rows = min(ROWS, p.seq.n * a.group - p.j * ROWS);
-    const int d4s = a.head_dim / 4, D = a.head_dim;
-    for (int e = tid; e < rows * d4s; e += nthr) {
-        const int r = e / d4s, d = (e - r * d4s) * 4;
-        float m = -INFINITY;
-        for (int c = sp.c0; c <= sp.c1; c++) m = fmaxf(m, __ldcg(sp.place(a, c) + (size_t)ROWS * D + r));
-        if (m == -INFINITY) m = 0.f;  // nothing seen (or NaN scores only, whose sums stay NaN)
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        float l = 0.f;
+    // threads over rows first (by_row) or over a row's elements first
+    const int per = by_row ? rows : d4s;
+    const int lines = by_row ? d4s : rows;
+    for (int e = tid; e < per * ((lines + kE - 1) / kE); e += nthr) {
+        const int x = e % per, y0 = e / per * kE;
+        float4 o[kE];
+        float l[kE], m[kE];
+#pragma unroll
+        for (int i = 0; i < kE; i++) {
+            o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            l[i] = 0.f;
+            m[i] = -INFINITY;
+        }
+        const int nm = by_row ? 1 : kE;  // distinct rows of the elements
+#pragma unroll 4
+        for (int c = sp.c0; c <= sp.c1; c++) {
+            const float* pm = sp.place(a, c) + (size_t)ROWS * D;
+#pragma unroll
+            for (int i = 0; i < kE; i++)
+                if (i < nm && (by_row || y0 + i < rows)) m[i] = fmaxf(m[i], __ldcg(pm + (by_row ? x : y0 + i)));
+        }
+#pragma unroll
+        for (int i = 0; i < kE; i++) {
+            if (by_row && i > 0) m[i] = m[0];
+            if (m[i] == -INFINITY) m[i] = 0.f;  // nothing seen (or NaN scores only, whose sums stay NaN)
+        }
+#pragma unroll 4
         for (int c = sp.c0; c <= sp.c1; c++) {
             const float* pl = sp.place(a, c);
-            const float w = exp2f(__ldcg(pl + (size_t)ROWS * D + r) - m);
-            const float4 v = __ldcg(reinterpret_cast<const float4*>(pl + (size_t)r * D + d));
-            l += w * __ldcg(pl + (size_t)ROWS * (D + 1) + r);
-            o.x += w * v.x;
-            o.y += w * v.y;
-            o.z += w * v.z;
-            o.w += w * v.w;
+#pragma unroll
+            for (int i = 0; i < kE; i++) {
+                if (y0 + i >= lines) break;
+                const int r = by_row ? x : y0 + i, d4 = by_row ? y0 + i : x;
+                const float w = exp2f(__ldcg(pl + (size_t)ROWS * D + r) - m[i]);
+                const float4 v = __ldcg(reinterpret_cast<const float4*>(pl + part_at<ROWS>(by_row, D, r, d4)));
+                l[i] += w * __ldcg(pl + (size_t)ROWS * (D + 1) + r);
+                o[i].x += w * v.x;
+                o[i].y += w * v.y;
+                o[i].z += w * v.z;
+                o[i].w += w * v.w;
+            }
         }
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        char* dst = a.out + row_offset(a, p, p.j * ROWS + r, a.out_stride, (int)sizeof(T)) + d * (int)sizeof(T);
-        if (sizeof(T) == 4)
-            *reinterpret_cast<float4*>(dst) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-        else
-            *reinterpret_cast<uint2*>(dst) = make_uint2(Elem<__nv_bfloat16>::pair(o.x * inv, o.y * inv),
-                                                        Elem<__nv_bfloat16>::pair(o.z * inv, o.w * inv));
+#pragma unroll
+        for (int i = 0; i < kE; i++) {
+            if (y0 + i >= lines) break;
+            const int r = by_row ? x : y0 + i, d4 = by_row ? y0 + i : x;
+            store4<T>(a.out + row_offset(a, p, p.j * ROWS + r, a.out_stride, (int)sizeof(T)) + d4 * 4 * (int)sizeof(T),
+                      o[i], l[i] == 0.f ? 0.f : 1.f / l[i]);
+        }
     }
 }
 
