@@ -41,14 +41,13 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_consta
     using L = Simt<T, ROWS, TOK, DP>;
     constexpr int kVec = Elem<T>::kPer16B;
     extern __shared__ __align__(16) float sm[];
-    __shared__ long long scratch[36];
     __shared__ unsigned last_s;
     float *Qs = sm + L::kQ, *Ks = sm + L::kK, *Vs = sm + L::kV, *Ss = sm + L::kS, *Ps = sm + L::kP;
     float *Mx = sm + L::kStat, *Sum = Mx + ROWS, *Fac = Sum + ROWS;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     pdl_launch_dependents();
     pdl_wait();
-    Walk<ROWS, TOK> walk = start_walk<ROWS, TOK>(&a, scratch);
+    Walk<ROWS, TOK> walk = start_walk<ROWS, TOK>(&a, lane, blockIdx.x == 0 && warp == 0);
     const int D = a.head_dim;
     // score threads: key, row group, part of the head dimension
     const int s_key = tid % TOK, s_rg = tid / TOK % L::kRG, s_ds = tid / L::kScoreCols;
@@ -230,7 +229,7 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_consta
         __syncthreads();
         if (tid == 0) last_s = arrive_last(a.counters + sp.c0, (unsigned)(sp.c1 - sp.c0 + 1));
         __syncthreads();
-        if (last_s) merge_parts<T, ROWS, TOK, false, 1>(a, p, sp, tid, kThreads);
+        if (last_s) merge_few<T, ROWS, TOK>(a, p, sp, tid, kThreads);
     }
 }
 

@@ -306,14 +306,14 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
     unsigned char* ring = smem;
     unsigned char* qs = smem + NS * C::kSlot;
     float* stage = reinterpret_cast<float*>(qs + C::kQBufs * C::kQTile);
-    __shared__ long long scratch[36];
     __shared__ uint64_t full[NS], empty[NS], landed[NS], qfull[2], qempty[2], sfull[2], pfull[2], odone[2];
     __shared__ uint32_t taddr_s;
     __shared__ float stat_m[4][32], stat_l[4][32];
     __shared__ unsigned last_s;
     __shared__ volatile unsigned bad_s;  // a value was taken out of a tile
     __shared__ Item<ROWS, BN> items[kItems];
-    __shared__ uint64_t ifull[kItems], iempty[kItems];
+    __shared__ uint64_t ifull[kItems], iempty[kItems], stretch;
+    __shared__ int tiles_s;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint64_t lim = a.timeout_ns;
     pdl_launch_dependents();
@@ -334,6 +334,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
             mbar_init(&ifull[i], 1);
             mbar_init(&iempty[i], C::kReaders);
         }
+        mbar_init(&stretch, 1);
         fence_mbar_init();
         bad_s = 0;
     }
@@ -346,15 +347,19 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
     tc_fence_after();
     const uint32_t tmem = taddr_s;
     pdl_wait();
-    Walk<ROWS, BN> walk = start_walk<ROWS, BN>(&a, scratch);
-    const int tiles = (int)(walk.end - walk.at);  // of this CTA
     ItemAt<ROWS, BN> at{items, ifull, iempty, a.status, lim, 0, 0, 0, 0};
+    int tiles = 0;  // of this CTA
+    if (warp < C::kWarps - 1) {
+        mbar_wait(&stretch, 0, a.status, lim);
+        tiles = tiles_s;
+    }
 
-    if (tiles <= 0) {
-        // nothing for this CTA
-    } else if (warp == C::kWarps - 1) {
+    if (warp == C::kWarps - 1) {
         // ---------------------------------------------------------- schedule
+        Walk<ROWS, BN> walk = start_walk<ROWS, BN>(&a, lane, blockIdx.x == 0);
         if (lane == 0) {
+            tiles_s = (int)(walk.end - walk.at);
+            mbar_arrive(&stretch);
             Part p;
             for (int n = 0; walk.next(p); n++) {
                 Item<ROWS, BN>& it = items[n % kItems];
@@ -369,6 +374,8 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
             }
         }
         __syncwarp();
+    } else if (tiles <= 0) {
+        // nothing for this CTA
     } else if (warp >= C::kWarpSlot) {
         // ------------------------------------------------- producer of one slot
         const int slot = warp - C::kWarpSlot;
@@ -747,9 +754,9 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                 named_bar_sync(1, 32 * C::kSoftWarps);
                 if (last_s) {
                     if (few)
-                        merge_parts<__nv_bfloat16, ROWS, BN, false, 1>(a, p, sp, tid, 32 * C::kSoftWarps);
+                        merge_few<__nv_bfloat16, ROWS, BN>(a, p, sp, tid, 32 * C::kSoftWarps);
                     else
-                        merge_parts<__nv_bfloat16, ROWS, BN, true, 4>(a, p, sp, tid, 32 * C::kSoftWarps);
+                        merge_rows<__nv_bfloat16, ROWS, BN>(a, p, sp, r);
                 }
             }
             left -= at.t1 - at.t0;

@@ -135,77 +135,50 @@ struct Walk {
     }
 };
 
-// Sum over the CTA's threads before this one; *all is the sum over all.
-// sums: one word a warp.  Out of line, like what follows: run once, and short
-// code is what makes it quick.
-static __device__ __noinline__ long long scan_threads(long long v, long long* sums, long long* all) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nwarps = (int)blockDim.x / 32;
-    long long inc = v;
-#pragma unroll 1
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long u = __shfl_up_sync(kFull, inc, o);
-        if (lane >= o) inc += u;
-    }
-    if (lane == 31) sums[warp] = inc;
-    __syncthreads();
-    long long pre = inc - v, total = 0;
-#pragma unroll 1
-    for (int i = 0; i < nwarps; i++) {
-        const long long u = sums[i];
-        if (i < warp) pre += u;
-        total += u;
-    }
-    __syncthreads();
-    *all = total;
-    return pre;
-}
-
+// The line's length and this CTA's first sequence, by one whole warp: a lane
+// counts a run of sequences, a scan over the lanes gives the total, and the
+// lane whose run holds this CTA's first tile looks for its sequence.  Short
+// code on purpose: it runs once, from a cold instruction cache.
 template <int ROWS, int TOK>
-__device__ __noinline__ long long seq_tiles(const Sched<ROWS, TOK>& s, int b, bool report) {
-    const Seq q = load_seq(s.a->batch, b);
-    if (report && q.bad) record_status(s.a->status, PP_ERR_INVALID_ARG);
-    return s.head_tiles(q) * s.a->n_kv_heads;
-}
-
-// The line's length and this CTA's first sequence, by all threads of the CTA.
-// scratch: 34 words of shared memory.
-template <int ROWS, int TOK>
-PP_DEVINL Walk<ROWS, TOK> start_walk(const AttnArgs* a, long long* scratch) {
+PP_DEVINL Walk<ROWS, TOK> start_walk(const AttnArgs* a, int lane, bool report) {
     Walk<ROWS, TOK> w;
     w.sched.a = a;
-    const int tid = threadIdx.x, B = a->batch.n_seqs, n = (int)blockDim.x;
-    long long* found = scratch + 32;  // sequence, its line position
-    // the total; with no more sequences than threads the counts and their
-    // sums are kept for the search
-    long long mine = 0, pre = 0, before = 0, all;
-    for (int b0 = 0; b0 < B; b0 += n) {
-        mine = b0 + tid < B ? seq_tiles(w.sched, b0 + tid, blockIdx.x == 0) : 0;
-        pre = before + scan_threads(mine, scratch, &all);
-        before += all;
+    const int B = a->batch.n_seqs, run = (B + 31) / 32;
+    const int b0 = min(lane * run, B), b1 = min(b0 + run, B);
+    long long mine = 0;
+#pragma unroll 2
+    for (int b = b0; b < b1; b++) {
+        const Seq q = load_seq(a->batch, b);
+        if (report && q.bad) record_status(a->status, PP_ERR_INVALID_ARG);
+        mine += w.sched.head_tiles(q);
     }
-    w.sched.deal(before, (int)gridDim.x);
+    mine *= a->n_kv_heads;
+    long long sum = mine;
+#pragma unroll 1
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long u = __shfl_up_sync(kFull, sum, o);
+        if (lane >= o) sum += u;
+    }
+    w.sched.deal(__shfl_sync(kFull, sum, 31), (int)gridDim.x);
     w.at = w.end = 0;
     w.m = 0;
-    if ((int)blockIdx.x < w.sched.ctas) {  // uniform over the CTA
-        const long long lo = w.sched.begin_of(blockIdx.x);
-        before = 0;
-        for (int b0 = 0; b0 < B; b0 += n) {
-            if (B > n) {
-                mine = b0 + tid < B ? seq_tiles(w.sched, b0 + tid, false) : 0;
-                pre = before + scan_threads(mine, scratch, &all);
-                before += all;
-            }
-            if (pre <= lo && lo < pre + mine) {
-                found[0] = b0 + tid;
-                found[1] = pre;
-            }
+    if ((int)blockIdx.x >= w.sched.ctas) return w;
+    w.at = w.sched.begin_of(blockIdx.x);
+    w.end = w.sched.begin_of((int)blockIdx.x + 1);
+    long long base = sum - mine;
+    int b = b0;
+    const bool here = base <= w.at && w.at < sum;
+    if (here) {
+#pragma unroll 1
+        for (; b + 1 < b1; b++) {
+            const long long t = w.sched.head_tiles(load_seq(a->batch, b)) * a->n_kv_heads;
+            if (base + t > w.at) break;
+            base += t;
         }
-        __syncthreads();
-        w.at = lo;
-        w.end = w.sched.begin_of((int)blockIdx.x + 1);
-        w.b = (int)found[0] - 1;  // next() enters the sequence
-        w.base = found[1];
     }
+    const int owner = __ffs(__ballot_sync(kFull, here)) - 1;
+    w.b = __shfl_sync(kFull, b, owner) - 1;  // next() enters the sequence
+    w.base = __shfl_sync(kFull, base, owner);
     return w;
 }
 
@@ -267,61 +240,78 @@ PP_DEVINL size_t part_at(bool by_row, int D, int r, int d4) {
 
 // Adds up the parts of an item and writes its rows, by `nthr` threads (tid of
 // them).  The caller has made the parts visible (arrival counter).  Bound by
-// the latency of the loads: kE elements (of 4 floats) of up to four parts are
-// in flight at once in a thread.
-template <typename T, int ROWS, int TOK, bool by_row, int kE>
-PP_DEVINL void merge_parts(const AttnArgs& a, const Part& p, const Split<ROWS, TOK>& sp, int tid, int nthr) {
+// the latency of the loads, so that many are in flight at once.  Few rows: a
+// thread has four elements of a row and takes the parts as they come.
+template <typename T, int ROWS, int TOK>
+PP_DEVINL void merge_few(const AttnArgs& a, const Part& p, const Split<ROWS, TOK>& sp, int tid, int nthr) {
     const int D = a.head_dim, d4s = D / 4;
     const int rows = min(ROWS, p.seq.n * a.group - p.j * ROWS);
-    // threads over rows first (by_row) or over a row's elements first
-    const int per = by_row ? rows : d4s;
-    const int lines = by_row ? d4s : rows;
-    for (int e = tid; e < per * ((lines + kE - 1) / kE); e += nthr) {
-        const int x = e % per, y0 = e / per * kE;
-        float4 o[kE];
-        float l[kE], m[kE];
-#pragma unroll
-        for (int i = 0; i < kE; i++) {
-            o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-            l[i] = 0.f;
-            m[i] = -INFINITY;
-        }
-        const int nm = by_row ? 1 : kE;  // distinct rows of the elements
-#pragma unroll 4
-        for (int c = sp.c0; c <= sp.c1; c++) {
-            const float* pm = sp.place(a, c) + (size_t)ROWS * D;
-#pragma unroll
-            for (int i = 0; i < kE; i++)
-                if (i < nm && (by_row || y0 + i < rows)) m[i] = fmaxf(m[i], __ldcg(pm + (by_row ? x : y0 + i)));
-        }
-#pragma unroll
-        for (int i = 0; i < kE; i++) {
-            if (by_row && i > 0) m[i] = m[0];
-            if (m[i] == -INFINITY) m[i] = 0.f;  // nothing seen (or NaN scores only, whose sums stay NaN)
-        }
+    for (int e = tid; e < rows * d4s; e += nthr) {
+        const int r = e / d4s, d4 = e - r * d4s;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        float l = 0.f, m = -INFINITY;
 #pragma unroll 4
         for (int c = sp.c0; c <= sp.c1; c++) {
             const float* pl = sp.place(a, c);
+            const float mc = __ldcg(pl + (size_t)ROWS * D + r), lc = __ldcg(pl + (size_t)ROWS * (D + 1) + r);
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(pl + part_at<ROWS>(false, D, r, d4)));
+            const float top = fmaxf(m, mc);
+            const float base = top == -INFINITY ? 0.f : top;  // nothing seen (or NaN scores only: the sums stay NaN)
+            const float f = exp2f(m - base), w = exp2f(mc - base);
+            m = top;
+            l = l * f + lc * w;
+            o.x = o.x * f + v.x * w;
+            o.y = o.y * f + v.y * w;
+            o.z = o.z * f + v.z * w;
+            o.w = o.w * f + v.w * w;
+        }
+        store4<T>(a.out + row_offset(a, p, p.j * ROWS + r, a.out_stride, (int)sizeof(T)) + d4 * 4 * (int)sizeof(T), o,
+                  l == 0.f ? 0.f : 1.f / l);
+    }
+}
+
+// Many rows: a thread has a row (nthr >= its rows), finds the parts' common
+// maximum and sum first, and then adds 32 elements at a time.
+template <typename T, int ROWS, int TOK>
+PP_DEVINL void merge_rows(const AttnArgs& a, const Part& p, const Split<ROWS, TOK>& sp, int r) {
+    const int D = a.head_dim, d4s = D / 4;
+    if (r >= p.seq.n * a.group - p.j * ROWS) return;
+    float m = -INFINITY, l = 0.f;
+#pragma unroll 4
+    for (int c = sp.c0; c <= sp.c1; c++) m = fmaxf(m, __ldcg(sp.place(a, c) + (size_t)ROWS * D + r));
+    if (m == -INFINITY) m = 0.f;
+#pragma unroll 4
+    for (int c = sp.c0; c <= sp.c1; c++) {
+        const float* pm = sp.place(a, c) + (size_t)ROWS * D + r;
+        l += __ldcg(pm + ROWS) * exp2f(__ldcg(pm) - m);
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    char* dst = a.out + row_offset(a, p, p.j * ROWS + r, a.out_stride, (int)sizeof(T));
+    for (int d0 = 0; d0 < d4s; d0 += 8) {
+        float4 o[8];
 #pragma unroll
-            for (int i = 0; i < kE; i++) {
-                if (y0 + i >= lines) break;
-                const int r = by_row ? x : y0 + i, d4 = by_row ? y0 + i : x;
-                const float w = exp2f(__ldcg(pl + (size_t)ROWS * D + r) - m[i]);
-                const float4 v = __ldcg(reinterpret_cast<const float4*>(pl + part_at<ROWS>(by_row, D, r, d4)));
-                l[i] += w * __ldcg(pl + (size_t)ROWS * (D + 1) + r);
-                o[i].x += w * v.x;
-                o[i].y += w * v.y;
-                o[i].z += w * v.z;
-                o[i].w += w * v.w;
+        for (int i = 0; i < 8; i++) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+        for (int c = sp.c0; c <= sp.c1; c++) {
+            const float* pl = sp.place(a, c);
+            const float mc = __ldcg(pl + (size_t)ROWS * D + r);
+            float4 v[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++)
+                if (d0 + i < d4s) v[i] = __ldcg(reinterpret_cast<const float4*>(pl + part_at<ROWS>(true, D, r, d0 + i)));
+            const float w = exp2f(mc - m);
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                if (d0 + i >= d4s) continue;
+                o[i].x += w * v[i].x;
+                o[i].y += w * v[i].y;
+                o[i].z += w * v[i].z;
+                o[i].w += w * v[i].w;
             }
         }
 #pragma unroll
-        for (int i = 0; i < kE; i++) {
-            if (y0 + i >= lines) break;
-            const int r = by_row ? x : y0 + i, d4 = by_row ? y0 + i : x;
-            store4<T>(a.out + row_offset(a, p, p.j * ROWS + r, a.out_stride, (int)sizeof(T)) + d4 * 4 * (int)sizeof(T),
-                      o[i], l[i] == 0.f ? 0.f : 1.f / l[i]);
-        }
+        for (int i = 0; i < 8; i++)
+            if (d0 + i < d4s) store4<T>(dst + (d0 + i) * 4 * (int)sizeof(T), o[i], inv);
     }
 }
 
