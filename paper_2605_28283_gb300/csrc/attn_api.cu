@@ -107,13 +107,14 @@ bool rows_overlap(const void* a, int64_t la, int64_t sa, const void* b, int64_t 
 }
 
 struct AttnLayout {
-    size_t counters, part, total;
+    size_t counters, tails, part, total;
 };
 
 AttnLayout attn_layout(const pp_cache& c) {
     AttnLayout L;
     L.counters = sizeof(Control);
-    L.part = (L.counters + kAttnMaxGrid * 4 + 255) & ~(size_t)255;
+    L.tails = (L.counters + kAttnMaxGrid * 4 + 255) & ~(size_t)255;
+    L.part = (L.tails + kAttnTcGrid * kAttnTail + 255) & ~(size_t)255;
     L.total = (L.part + attn_part_floats(c.head_dim) * 4 + 255) & ~(size_t)255;
     return L;
 }
@@ -304,6 +305,7 @@ pp_status pp_tree_attention(const pp_cache* cache, const pp_batch* batch, const 
     a.head_dim = cache->head_dim;
     a.scale_log2 = (float)((double)scale * 1.4426950408889634);
     a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + L.part);
+    a.tails = static_cast<char*>(ws) + L.tails;
     a.counters = reinterpret_cast<unsigned*>(static_cast<char*>(ws) + L.counters);
     a.status = status_of(ws);
     a.timeout_ns = kWaitLimitNs;

@@ -41,7 +41,7 @@ struct Tc {
     static constexpr int kQTile = 128 * DP * 2;
     static constexpr int kQBufs = MT == 2 ? 2 : DP == 256 ? 1 : 2;  // MT 2: one for each row tile
     static constexpr int kParts = BN / 32;           // copies of the rows when there are few
-    static constexpr int kStage = MT == 1 ? 4 * 32 * 33 * 4 : 0;
+    static constexpr int kStage = MT == 1 ? 4 * 32 * 36 * 4 : 0;  // 4 warps x 32 rows x 32 elements, or 8 x 128
     static constexpr int kSmem = kSlots * kSlot + kQBufs * kQTile + kStage + 1024;
     static constexpr int kSoftWarps = 4 * MT;
     // warps after the softmax ones: two that issue products, the rows of q, the slots' producers, the schedule
@@ -360,6 +360,8 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
         if (lane == 0) {
             tiles_s = (int)(walk.end - walk.at);
             mbar_arrive(&stretch);
+            Item<ROWS, BN>* tail = reinterpret_cast<Item<ROWS, BN>*>(a.tails) + blockIdx.x;
+            if (a.join_later) tail->rows = 0;
             Part p;
             for (int n = 0; walk.next(p); n++) {
                 Item<ROWS, BN>& it = items[n % kItems];
@@ -370,6 +372,8 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
 #pragma unroll 1
                 for (int m = 0; m < MT; m++) it.end[m] = tile_end<BN, MT>(a, p, m);
                 if (!p.whole()) it.split = Split<ROWS, BN>(walk.sched, p);
+                // an item that begins here and goes on in other stretches
+                if (a.join_later && p.t0 == 0 && !p.whole()) *tail = it;
                 mbar_arrive(&ifull[n % kItems]);
             }
         }
@@ -662,43 +666,55 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
             float* place = whole ? nullptr : sp.place(a, blockIdx.x);
             const int D = a.head_dim;
             if (few) {
-                // add up the warps' copies, 32 elements at a time
+                // add up the warps' copies through shared memory: 128 elements
+                // of up to 8 rows at a time, or 32 of 32
                 stat_m[wq][lane] = active ? mx : -INFINITY;
                 stat_l[wq][lane] = active ? sum : 0.f;
                 named_bar_sync(1, 128);
-                float top = -INFINITY;
+                float top = -INFINITY, l = 0.f;
 #pragma unroll
                 for (int i = 0; i < C::kParts; i++) top = fmaxf(top, stat_m[i][lane]);
-                if (top == -INFINITY) top = 0.f;
-                const float f = ex2(mx - top);
-                const int er = tid >> 2, ed = (tid & 3) * 8;
-                float etop = -INFINITY, l = 0.f;
+                const float base = top == -INFINITY ? 0.f : top;
 #pragma unroll
-                for (int i = 0; i < C::kParts; i++) etop = fmaxf(etop, stat_m[i][er]);
-                const float ebase = etop == -INFINITY ? 0.f : etop;
-#pragma unroll
-                for (int i = 0; i < C::kParts; i++) l += stat_l[i][er] * ex2(stat_m[i][er] - ebase);
-                const float inv = l == 0.f ? 0.f : 1.f / l;
+                for (int i = 0; i < C::kParts; i++) l += stat_l[i][lane] * ex2(stat_m[i][lane] - base);
+                const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
+                const float f = ex2(mx - base) * inv;
+                const int wide = rows <= 8 ? 128 : 32, pitch = wide + 4, per = rows <= 8 ? 8 : 32;
 #pragma unroll 1
-                for (int c = 0; c < D; c += 32) {
+                for (int c = 0; c < D; c += wide) {
                     if (active) {
-                        uint32_t o[32];
-                        tmem_ld32(t_o + c, o);
-                        tmem_ld_wait();
+#pragma unroll 1
+                        for (int x = 0; x < wide && c + x < D; x += 32) {
+                            uint32_t o[32];
+                            tmem_ld32(t_o + c + x, o);
+                            tmem_ld_wait();
+                            float4* dst = reinterpret_cast<float4*>(stage + (wq * per + lane) * pitch + x);
+                            if (lane < rows) {
 #pragma unroll
-                        for (int i = 0; i < 32; i++) stage[(wq * 32 + lane) * 33 + i] = __uint_as_float(o[i]) * f;
+                                for (int i = 0; i < 8; i++)
+                                    dst[i] = make_float4(__uint_as_float(o[4 * i]) * f, __uint_as_float(o[4 * i + 1]) * f,
+                                                         __uint_as_float(o[4 * i + 2]) * f, __uint_as_float(o[4 * i + 3]) * f);
+                            }
+                        }
                     }
                     named_bar_sync(1, 128);
-                    if (er < rows && c + ed < D) {
+#pragma unroll 1
+                    for (int e = tid; e < rows * (wide / 8); e += 128) {
+                        const int er = e / (wide / 8), ed = (e - er * (wide / 8)) * 8;
+                        if (c + ed >= D) continue;
                         float o[8] = {};
 #pragma unroll
                         for (int x = 0; x < C::kParts; x++)
 #pragma unroll
-                            for (int i = 0; i < 8; i++) o[i] += stage[(x * 32 + er) * 33 + ed + i];
+                            for (int i = 0; i < 8; i += 4) {
+                                const float4 v = *reinterpret_cast<const float4*>(stage + (x * per + er) * pitch + ed + i);
+                                o[i] += v.x;
+                                o[i + 1] += v.y;
+                                o[i + 2] += v.z;
+                                o[i + 3] += v.w;
+                            }
                         if (bad) add_nonfinite(a, p, p.j * ROWS + er, c + ed, BN, o);
                         if (whole) {
-#pragma unroll
-                            for (int i = 0; i < 8; i++) o[i] *= inv;
                             *reinterpret_cast<uint4*>(a.out + row_offset(a, p, p.j * ROWS + er, a.out_stride, 2) + (c + ed) * 2) =
                                 Elem<__nv_bfloat16>::pack(o);
                         } else {
@@ -709,9 +725,9 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                     }
                     named_bar_sync(1, 128);
                 }
-                if (!whole && (tid & 3) == 0) {
-                    place[(size_t)ROWS * D + er] = etop;
-                    place[(size_t)ROWS * (D + 1) + er] = l;
+                if (!whole && wq == 0) {
+                    place[(size_t)ROWS * D + lane] = top;
+                    place[(size_t)ROWS * (D + 1) + lane] = l;
                 }
             } else if (active) {
                 const float inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -748,15 +764,16 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                 }
             }
             tc_fence_before();
-            if (!whole) {
+            if (!whole && !a.join_later) {
                 named_bar_sync(1, 32 * C::kSoftWarps);
                 if (tid == 0) last_s = arrive_last(a.counters + sp.c0, (unsigned)(sp.c1 - sp.c0 + 1));
                 named_bar_sync(1, 32 * C::kSoftWarps);
                 if (last_s) {
                     if (few)
                         merge_few<__nv_bfloat16, ROWS, BN>(a, p, sp, tid, 32 * C::kSoftWarps);
-                    else
-                        merge_rows<__nv_bfloat16, ROWS, BN>(a, p, sp, r);
+                    else if (r < rows)
+#pragma unroll 1
+                        for (int d = 0; d < D / 4; d += 4) merge_row<__nv_bfloat16, ROWS, BN, 4>(a, p, sp, r, d);
                 }
             }
             left -= at.t1 - at.t0;
@@ -769,6 +786,25 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
     if (warp == C::kWarpMma) {
         tc_fence_after();
         tmem_dealloc(tmem, C::kTmemCols);
+    }
+}
+
+// Joins the split items of a launch whose items mostly have many rows: block
+// (c, y) the one that begins in stretch c (if any), 16 elements of 128 rows
+// each.  In the attention kernel the last CTA to arrive would do it alone: 7 to
+// 11 us for 128 rows of 128, against 2 to 3 us here, all SMs at once.
+template <int DP, int MT>
+__global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ AttnArgs a) {
+    using C = Tc<DP, MT>;
+    pdl_launch_dependents();
+    pdl_wait();
+    const Item<C::kRows, C::BN>& it = reinterpret_cast<const Item<C::kRows, C::BN>*>(a.tails)[blockIdx.x];
+    const int r = 128 * (int)(blockIdx.y % MT) + (int)threadIdx.x;
+    const int few = MT == 1 && it.rows <= 32;
+    if (few) {  // laid out row by row
+        if (blockIdx.y == 0) merge_few<__nv_bfloat16, C::kRows, C::BN>(a, it, it.split, threadIdx.x, 128);
+    } else if (r < it.rows) {
+        merge_row<__nv_bfloat16, C::kRows, C::BN, 4>(a, it, it.split, r, (int)(blockIdx.y / MT) * 4);
     }
 }
 
@@ -805,7 +841,7 @@ bool query_map(CUtensorMap* map, const AttnArgs& a) {
 }
 
 template <int DP, int MT>
-cudaError_t go(AttnArgs a, int sms, cudaStream_t st) {
+cudaError_t go(AttnArgs a, bool join_later, int sms, cudaStream_t st) {
     using C = Tc<DP, MT>;
     auto* kern = attn_tc_kernel<DP, MT>;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
@@ -818,8 +854,12 @@ cudaError_t go(AttnArgs a, int sms, cudaStream_t st) {
     if (a.box && (!cache_map(&mk, a, a.cache.k) || !cache_map(&mv, a, a.cache.v))) a.box = 0;
     // rows of q: 32 of one key head are whole tokens where the group divides 32
     a.q_box = 32 % a.group == 0 && query_map(&mq, a);
-    return launch_overlapped(kern, dim3((unsigned)(sms < kAttnTcGrid ? sms : kAttnTcGrid)), dim3(C::kWarps * 32),
-                             C::kSmem, st, a, mk, mv, mq);
+    a.join_later = join_later;
+    static_assert(sizeof(Item<C::kRows, C::BN>) <= kAttnTail, "a stretch's last item in the workspace");
+    const unsigned grid = (unsigned)(sms < kAttnTcGrid ? sms : kAttnTcGrid);
+    e = launch_overlapped(kern, dim3(grid), dim3(C::kWarps * 32), C::kSmem, st, a, mk, mv, mq);
+    if (e != cudaSuccess || !join_later) return e;
+    return launch_overlapped(join_kernel<DP, MT>, dim3(grid, (unsigned)(MT * ((a.head_dim + 15) / 16))), dim3(128), 0, st, a);
 }
 
 }  // namespace
@@ -829,9 +869,11 @@ cudaError_t attn_tc_launch(const AttnArgs& a, int sms, cudaStream_t st) {
     // each key tile where one does not hold them
     const long long rows = ((long long)a.batch.n_tokens * a.group + a.batch.n_seqs - 1) / a.batch.n_seqs;
     const bool two = rows > 128;
-    if (a.head_dim <= 64) return two ? go<64, 2>(a, sms, st) : go<64, 1>(a, sms, st);
-    if (a.head_dim <= 128) return two ? go<128, 2>(a, sms, st) : go<128, 1>(a, sms, st);
-    return go<256, 1>(a, sms, st);
+    // split items of a few rows are joined by the CTA that finishes last, those of many by a second kernel
+    const bool later = rows > 32;
+    if (a.head_dim <= 64) return two ? go<64, 2>(a, later, sms, st) : go<64, 1>(a, later, sms, st);
+    if (a.head_dim <= 128) return two ? go<128, 2>(a, later, sms, st) : go<128, 1>(a, later, sms, st);
+    return go<256, 1>(a, later, sms, st);
 }
 
 }  // namespace pp

@@ -15,6 +15,7 @@ constexpr int kAttnMaxGrid = 608;      // CUDA-core kernel: up to 4 CTAs on each
 constexpr int kAttnSimtRows = 16;      // rows (token, head of the group) of its largest tile
 constexpr int kAttnTcGrid = 152;       // tensor-core kernel: one CTA per SM ...
 constexpr int kAttnTcRows = 256;       // ... and two tiles of 128 rows
+constexpr int kAttnTail = 128;         // bytes of AttnArgs.tails per CTA
 
 struct BatchArgs {
     const int32_t* q_start;
@@ -70,6 +71,8 @@ struct AttnArgs {
     int q_box;           // whether the rows of q go by TMA
     float scale_log2;    // scale * log2(e): softmax in powers of two
     float* part;         // partial results of split items
+    char* tails;         // [kAttnTcGrid] the split item that begins in each stretch (joined by a second kernel)
+    int join_later;      // whether split items are joined by that kernel
     unsigned* counters;  // arrivals per split item, zero at rest
     unsigned* status;
     uint64_t timeout_ns;

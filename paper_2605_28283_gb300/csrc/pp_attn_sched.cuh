@@ -270,49 +270,42 @@ PP_DEVINL void merge_few(const AttnArgs& a, const Part& p, const Split<ROWS, TOK
     }
 }
 
-// Many rows: a thread has a row (nthr >= its rows), finds the parts' common
-// maximum and sum first, and then adds 32 elements at a time.
-template <typename T, int ROWS, int TOK>
-PP_DEVINL void merge_rows(const AttnArgs& a, const Part& p, const Split<ROWS, TOK>& sp, int r) {
+// Many rows: a thread has a row (r of the item, whose place is the row's in a
+// row tile) and 4 N elements from d0 on.
+template <typename T, int ROWS, int TOK, int N>
+PP_DEVINL void merge_row(const AttnArgs& a, const Part& p, const Split<ROWS, TOK>& sp, int r, int d0) {
     const int D = a.head_dim, d4s = D / 4;
-    if (r >= p.seq.n * a.group - p.j * ROWS) return;
     float m = -INFINITY, l = 0.f;
 #pragma unroll 4
     for (int c = sp.c0; c <= sp.c1; c++) m = fmaxf(m, __ldcg(sp.place(a, c) + (size_t)ROWS * D + r));
-    if (m == -INFINITY) m = 0.f;
+    if (m == -INFINITY) m = 0.f;  // nothing seen (or NaN scores only, whose sums stay NaN)
+    float4 o[N];
+#pragma unroll
+    for (int i = 0; i < N; i++) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
     for (int c = sp.c0; c <= sp.c1; c++) {
-        const float* pm = sp.place(a, c) + (size_t)ROWS * D + r;
-        l += __ldcg(pm + ROWS) * exp2f(__ldcg(pm) - m);
+        const float* pl = sp.place(a, c);
+        const float mc = __ldcg(pl + (size_t)ROWS * D + r), lc = __ldcg(pl + (size_t)ROWS * (D + 1) + r);
+        float4 v[N];
+#pragma unroll
+        for (int i = 0; i < N; i++)
+            if (d0 + i < d4s) v[i] = __ldcg(reinterpret_cast<const float4*>(pl + part_at<ROWS>(true, D, r, d0 + i)));
+        const float w = exp2f(mc - m);
+        l += w * lc;
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            if (d0 + i >= d4s) continue;
+            o[i].x += w * v[i].x;
+            o[i].y += w * v[i].y;
+            o[i].z += w * v[i].z;
+            o[i].w += w * v[i].w;
+        }
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
     char* dst = a.out + row_offset(a, p, p.j * ROWS + r, a.out_stride, (int)sizeof(T));
-    for (int d0 = 0; d0 < d4s; d0 += 8) {
-        float4 o[8];
 #pragma unroll
-        for (int i = 0; i < 8; i++) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
-        for (int c = sp.c0; c <= sp.c1; c++) {
-            const float* pl = sp.place(a, c);
-            const float mc = __ldcg(pl + (size_t)ROWS * D + r);
-            float4 v[8];
-#pragma unroll
-            for (int i = 0; i < 8; i++)
-                if (d0 + i < d4s) v[i] = __ldcg(reinterpret_cast<const float4*>(pl + part_at<ROWS>(true, D, r, d0 + i)));
-            const float w = exp2f(mc - m);
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                if (d0 + i >= d4s) continue;
-                o[i].x += w * v[i].x;
-                o[i].y += w * v[i].y;
-                o[i].z += w * v[i].z;
-                o[i].w += w * v[i].w;
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 8; i++)
-            if (d0 + i < d4s) store4<T>(dst + (d0 + i) * 4 * (int)sizeof(T), o[i], inv);
-    }
+    for (int i = 0; i < N; i++)
+        if (d0 + i < d4s) store4<T>(dst + (d0 + i) * 4 * (int)sizeof(T), o[i], inv);
 }
 
 }  // namespace pp
