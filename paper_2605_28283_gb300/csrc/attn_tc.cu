@@ -400,25 +400,26 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
             // values: rows that some row of queries does not see are looked through, rows past the end set to zero
             const int open = key ? BN : max(p.open - k0, 0);
             if (a.box > 0) {
-                // boxes of 64 elements x min(page, BN) tokens, one for a lane at a time
+                // boxes of 64 elements x min(page, BN) tokens, one for each of up to 32 lanes
+                static_assert(BN / 8 * NG <= 32, "a lane for each box");
                 const int boxes = (end + a.box - 1) / a.box * NG;
                 const bool fix = !key && (end < BN || open < end);
                 uint64_t* bar = fix ? &landed[slot] : &full[slot];
-                int page = 0, b = lane;
-                if (b < boxes) page = entry_page(a.batch, p.b, k0 + b / NG * a.box);
+                const int row = lane / NG * a.box, grp = lane % NG;
+                const int in_page = (int)((unsigned)(k0 + row) % (unsigned)a.batch.page_size);
+                int page = 0;
+                if (lane < boxes) {
+                    page = entry_page(a.batch, p.b, k0 + row);
+                    if (page < 0) {  // lies past the last page: zeros
+                        record_status(a.status, PP_ERR_INVALID_ARG);
+                        page = a.batch.n_pages;
+                    }
+                }
                 if (uses > 0) mbar_wait(&empty[slot], (uint32_t)(uses - 1) & 1u, a.status, lim);
                 if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(boxes * a.box * 128));
                 __syncwarp();
-                while (b < boxes) {
-                    const int row = b / NG * a.box, grp = b % NG;
-                    if (page < 0) record_status(a.status, PP_ERR_INVALID_ARG);
-                    // a page that does not exist lies past the last one: zeros
-                    tma_load_4d(dst + grp * BN * 128 + row * 128, key ? &map_k : &map_v, grp * 64, p.h,
-                                (int)((unsigned)(k0 + row) % (unsigned)a.batch.page_size),
-                                page < 0 ? a.batch.n_pages : page, bar);
-                    b += 32;
-                    if (b < boxes) page = entry_page(a.batch, p.b, k0 + b / NG * a.box);
-                }
+                if (lane < boxes)
+                    tma_load_4d(dst + grp * BN * 128 + row * 128, key ? &map_k : &map_v, grp * 64, p.h, in_page, page, bar);
                 if (fix) {
                     mbar_wait(bar, (uint32_t)fixes++ & 1u, a.status, lim);
                     if (open < end && drop_nonfinite<DP, BN>(dst, open, end, lane) && lane == 0) bad_s = 1;
@@ -508,63 +509,82 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
         cs.enter(0);
         co.enter(0);
         int end_s = cs.item().end[m], end_o = co.item().end[m];
-        auto scores = [&](int g) {
-            const int buf = MT == 2 ? m : cs.n % C::kQBufs, use = MT == 2 ? cs.n : cs.n / C::kQBufs;
-            const int pos = MT == 1 ? (g == 0 ? 0 : 2 * g - 1) : 2 * g;
-            const int sl = MT == 1 ? g & 1 : m;
-            if (cs.t == cs.t0) mbar_wait(&qfull[buf], (uint32_t)use & 1u, a.status, lim);
-            if (cs.t < end_s) {
-                // MT 1: the slot's last weights have been multiplied (MT 2: issued by this warp, in order)
-                if (MT == 1 && g >= 2) mbar_wait(&odone[sl], (uint32_t)((g - 2) >> 1) & 1u, a.status, lim);
-                mbar_wait(&full[pos % NS], (uint32_t)(pos / NS) & 1u, a.status, lim);
-                tc_fence_after();
-                if (one) {
-                    const unsigned char* kt = ring + (pos % NS) * C::kSlot;
-                    const unsigned char* qt = qs + buf * C::kQTile;
+        auto k_pos = [&](int g) { return MT == 1 ? (g == 0 ? 0 : 2 * g - 1) : 2 * g; };
+        auto v_pos = [&](int g) { return MT == 1 ? 2 * g + 2 : 2 * g + 1; };
+        auto s_slot = [&](int g) { return MT == 1 ? g & 1 : m; };
+        auto wait_full = [&](int pos) { mbar_wait(&full[pos % NS], (uint32_t)(pos / NS) & 1u, a.status, lim); };
+        auto q_buf = [&]() { return MT == 2 ? m : cs.n % C::kQBufs; };
+        auto wait_q = [&]() { mbar_wait(&qfull[q_buf()], (uint32_t)(MT == 2 ? cs.n : cs.n / C::kQBufs) & 1u, a.status, lim); };
+        auto issue_scores = [&](int g) {
+            const unsigned char* kt = ring + (k_pos(g) % NS) * C::kSlot;
+            const unsigned char* qt = qs + q_buf() * C::kQTile;
 #pragma unroll
-                    for (int d = 0; d < NG; d++)
-                        umma_k64(tm + (uint32_t)(sl * BN), qt + d * 128 * 128, kt + d * BN * 128, id_s, d > 0);
-                    umma_commit(&sfull[sl]);
-                }
-            }
-            if (one) {
-                umma_commit(&empty[pos % NS]);
-                if (cs.t + 1 == cs.t1) umma_commit(&qempty[buf]);
-            }
-            __syncwarp();
-            if (g + 1 < tiles && cs.step(1, lane, MT == 1)) end_s = cs.item().end[m];
+            for (int d = 0; d < NG; d++)
+                umma_k64(tm + (uint32_t)(s_slot(g) * BN), qt + d * 128 * 128, kt + d * BN * 128, id_s, d > 0);
+            umma_commit(&sfull[s_slot(g)]);
         };
-        uint32_t n_o = 0;  // value products issued
-        auto values = [&](int g) {
-            const int pos = MT == 1 ? 2 * g + 2 : 2 * g + 1;
-            const int sl = MT == 1 ? g & 1 : m;
-            if (co.t < end_o) {
-                mbar_wait(&full[pos % NS], (uint32_t)(pos / NS) & 1u, a.status, lim);
-                mbar_wait(&pfull[sl], (MT == 1 ? n_o >> 1 : n_o) & 1u, a.status, lim);
-                n_o++;
-                tc_fence_after();
-                if (one) {
-                    const uint64_t vd = sdesc_sw128_n(ring + (pos % NS) * C::kSlot, BN * 128);
+        auto release_scores = [&](int g) {  // the key slot and, behind the part's last tile, the rows of q
+            umma_commit(&empty[k_pos(g) % NS]);
+            if (cs.t + 1 == cs.t1) umma_commit(&qempty[q_buf()]);
+        };
+        auto issue_values = [&](int g) {
+            const uint64_t vd = sdesc_sw128_n(ring + (v_pos(g) % NS) * C::kSlot, BN * 128);
 #pragma unroll
-                    for (int k = 0; k < BN / 16; k++)
-                        umma_bf16_ta(tm + C::kTmemO + (uint32_t)(m * DP), tm + (uint32_t)(sl * BN + 8 * k),
-                                     vd + (uint64_t)(k * 128), id_o, (co.t > co.t0 || k > 0) ? 1u : 0u);
-                    umma_commit(&odone[sl]);
-                }
-            }
-            if (one) umma_commit(&empty[pos % NS]);
-            __syncwarp();
-            if (g + 1 < tiles && co.step(1, lane, true)) end_o = co.item().end[m];
+            for (int k = 0; k < BN / 16; k++)
+                umma_bf16_ta(tm + C::kTmemO + (uint32_t)(m * DP), tm + (uint32_t)(s_slot(g) * BN + 8 * k),
+                             vd + (uint64_t)(k * 128), id_o, (co.t > co.t0 || k > 0) ? 1u : 0u);
+            umma_commit(&odone[s_slot(g)]);
         };
-        if (MT == 1 && who == 0) {
+        if (MT == 2) {
+            uint32_t n_o = 0;  // value products issued
 #pragma unroll 1
-            for (int g = 0; g < tiles; g++) scores(g);
+            for (int g = -1; g < tiles; g++) {  // values of tile g, scores of the next: every wait but the weights' first
+                const bool v = g >= 0 && co.t < end_o, more = g + 1 < tiles, sc = more && cs.t < end_s;
+                const bool fresh = more && cs.t == cs.t0;  // its queries may still be on their way: values do not wait for them
+                if (v) wait_full(v_pos(g));
+                if (sc && !fresh) wait_full(k_pos(g + 1));
+                if (v) mbar_wait(&pfull[m], n_o++ & 1u, a.status, lim);
+                tc_fence_after();
+                if (one && v) issue_values(g);
+                if (one && g >= 0) umma_commit(&empty[v_pos(g) % NS]);
+                if (fresh) {
+                    wait_q();
+                    if (sc) wait_full(k_pos(g + 1));
+                    tc_fence_after();
+                }
+                if (one && sc) issue_scores(g + 1);
+                if (one && more) release_scores(g + 1);
+                __syncwarp();
+                if (g >= 0 && more && co.step(1, lane, true)) end_o = co.item().end[m];
+                if (g + 2 < tiles && cs.step(1, lane, false)) end_s = cs.item().end[m];
+            }
+        } else if (who == 0) {
+#pragma unroll 1
+            for (int g = 0; g < tiles; g++) {
+                if (cs.t == cs.t0) wait_q();
+                wait_full(k_pos(g));
+                // the slot's last weights have been multiplied
+                if (g >= 2) mbar_wait(&odone[g & 1], (uint32_t)((g - 2) >> 1) & 1u, a.status, lim);
+                tc_fence_after();
+                if (one) {
+                    issue_scores(g);
+                    release_scores(g);
+                }
+                __syncwarp();
+                if (g + 1 < tiles) cs.step(1, lane, true);
+            }
         } else {
 #pragma unroll 1
-            for (int g = 0; g < tiles + MT - 1; g++) {
-                // MT 2: at a new part its queries may still be on their way, so the old part's values go first
-                if (MT == 1 || g > 0) values(MT == 1 ? g : g - 1);
-                if (MT == 2 && g < tiles) scores(g);
+            for (int g = 0; g < tiles; g++) {
+                wait_full(v_pos(g));
+                mbar_wait(&pfull[g & 1], (uint32_t)(g >> 1) & 1u, a.status, lim);
+                tc_fence_after();
+                if (one) {
+                    issue_values(g);
+                    umma_commit(&empty[v_pos(g) % NS]);
+                }
+                __syncwarp();
+                if (g + 1 < tiles) co.step(1, lane, true);
             }
         }
     } else {
@@ -634,11 +654,12 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                         for (int c = 0; c < BN / 32; c++)
                             if (c != wq) tmem_st16(t_s + 16 * c, z);
                     } else {
-                        // 64 scores in registers at a time; the first half's weights leave the second half's scores in place
+                        // 64 scores in registers at a time: the upper half's maximum, the lower half's (which
+                        // stay), then their weights, which leave the upper half's scores in place, then the upper's
                         Scores<2> s;
                         float tm = -INFINITY, part = 0.f;
 #pragma unroll 1
-                        for (int c = 0; c < BN; c += 64) {
+                        for (int c = BN - 64; c >= 0; c -= 64) {
                             s.load(t_s + c);
                             if (masked) s.hide(a, p, tok, k0 + c);
                             tm = fmaxf(tm, s.max());
@@ -646,8 +667,10 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                         const float base = raise(tm, t);
 #pragma unroll 1
                         for (int c = 0; c < BN; c += 64) {
-                            s.load(t_s + c);
-                            if (masked) s.hide(a, p, tok, k0 + c);
+                            if (c > 0) {
+                                s.load(t_s + c);
+                                if (masked) s.hide(a, p, tok, k0 + c);
+                            }
                             part += s.weigh(t_s + c / 2, a.scale_log2, base);
                         }
                         sum += part;
