@@ -31,6 +31,8 @@ namespace {
 
 constexpr float kLazy = 8.0f;  // growth of a row's maximum (log2) that O and the sum absorb unscaled
 
+constexpr int kTurn = 5;  // 16-byte words a row of 32 bf16 takes in the turning area (one of padding)
+
 template <int DP, int MT>
 struct Tc {
     static constexpr int BN = DP == 256 ? 64 : 128;  // keys of a tile
@@ -41,7 +43,8 @@ struct Tc {
     static constexpr int kQTile = 128 * DP * 2;
     static constexpr int kQBufs = MT == 2 ? 2 : DP == 256 ? 1 : 2;  // MT 2: one for each row tile
     static constexpr int kParts = BN / 32;           // copies of the rows when there are few
-    static constexpr int kStage = MT == 1 ? 4 * 32 * 36 * 4 : 0;  // 4 warps x 32 rows x 32 elements, or 8 x 128
+    // few rows: 4 warps x 32 rows x 32 elements, or 8 x 128 (fp32); else 32 rows x 32 elements (bf16) a warp
+    static constexpr int kStage = MT == 1 ? 4 * 32 * 36 * 4 : 8 * 32 * kTurn * 16;
     static constexpr int kSmem = kSlots * kSlot + kQBufs * kQTile + kStage + 1024;
     static constexpr int kSoftWarps = 4 * MT;
     // warps after the softmax ones: two that issue products, the rows of q, the slots' producers, the schedule
@@ -183,60 +186,36 @@ PP_DEVINL void zero_rows(unsigned char* tile, int r0, int r1, int lane) {
             *reinterpret_cast<uint4*>(tile + g * BN * 128 + e * 16) = make_uint4(0u, 0u, 0u, 0u);
 }
 
-// Non-finite values of entries that not every row sees would reach all rows
-// of the product (0 * NaN): they are taken out of the tile here and added to
-// the rows that do see them at the end (add_nonfinite).  Rows [r0, r1) of a
-// value tile in shared memory; true if there were any.
-template <int DP, int BN>
-PP_DEVINL bool drop_nonfinite(unsigned char* tile, int r0, int r1, int lane) {
-    bool any = false;
-#pragma unroll 1
-    for (int e = r0 * 8 + lane; e < r1 * 8; e += 32) {
-#pragma unroll
-        for (int g = 0; g < DP / 64; g++) {
-            uint4* at = reinterpret_cast<uint4*>(tile + g * BN * 128 + e * 16);
-            uint4 v = *at;
-            uint32_t* w = reinterpret_cast<uint32_t*>(&v);
-            const uint32_t m = __vmaxu2(__vmaxu2(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu),
-                                        __vmaxu2(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu));
-            if ((m & 0xffffu) >= 0x7f80u || (m >> 16) >= 0x7f80u) {
-                any = true;
-#pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    if ((w[i] & 0x7f80u) == 0x7f80u) w[i] &= 0xffff0000u;
-                    if ((w[i] & 0x7f800000u) == 0x7f800000u) w[i] &= 0x0000ffffu;
-                }
-                *at = v;
-            }
-        }
-    }
-    return __any_sync(kFull, any);
-}
-
-// o[0..N) += the non-finite values at elements d.. of the part's new tokens
-// that row's token sees (their weights are positive).
-__device__ __noinline__ void add_nonfinite_slow(const AttnArgs& a, const Part& p, int row, int d, int n, int bn, float* o) {
-    const int tok = row / a.group;
+// o[0..n) = sum over the part's keys that the row sees of 2^(score - base) v,
+// elements d.., one key after the other.  For a row whose sum from the
+// products is not finite although it does not see all of the part's keys: a
+// value that it does not see may be NaN or infinite, and 0 * NaN is NaN.
+__device__ __noinline__ void careful_sum(const AttnArgs& a, const Part& p, int row, float base, int d, int n, int bn,
+                                         float* o) {
+    const int tok = row / a.group, D = a.head_dim;
+    const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(a.q + row_offset(a, p, row, a.q_stride, 2));
+    for (int i = 0; i < n; i++) o[i] = 0.f;
     const int k1 = min(p.key_end, p.t1 * bn);
-    for (int k = max(p.seq.ctx, p.t0 * bn); k < k1; k++) {
-        if (!sees(a, p, tok, k - p.seq.ctx)) continue;
+    for (int k = p.t0 * bn; k < k1; k++) {
+        if (k >= p.seq.ctx && !sees(a, p, tok, k - p.seq.ctx)) continue;
         const int page = entry_page(a.batch, p.b, k);
         if (page < 0) continue;
-        const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(
-            a.cache.v + entry_offset(a.batch, a.cache, page, k) + (long long)p.h * a.cache.head_stride);
-        for (int i = 0; i < n && d + i < a.head_dim; i++) {
-            const float x = __bfloat162float(v[d + i]);
-            if ((__float_as_uint(x) & 0x7f800000u) == 0x7f800000u) o[i] += x;
-        }
+        const long long at = entry_offset(a.batch, a.cache, page, k) + (long long)p.h * a.cache.head_stride;
+        const __nv_bfloat16* kk = reinterpret_cast<const __nv_bfloat16*>(a.cache.k + at);
+        const __nv_bfloat16* vv = reinterpret_cast<const __nv_bfloat16*>(a.cache.v + at);
+        float s = 0.f;
+        for (int i = 0; i < D; i++) s = fmaf(__bfloat162float(q[i]), __bfloat162float(kk[i]), s);
+        const float w = exp2f(fmaf(s, a.scale_log2, -base));
+        for (int i = 0; i < n && d + i < D; i++) o[i] = fmaf(w, __bfloat162float(vv[d + i]), o[i]);
     }
 }
 
 template <int N>
-PP_DEVINL void add_nonfinite(const AttnArgs& a, const Part& p, int row, int d, int bn, float (&o)[N]) {
-    float t[N];  // in memory only when there is something to add
-    for (int i = 0; i < N; i++) t[i] = o[i];
-    add_nonfinite_slow(a, p, row, d, N, bn, t);
-    for (int i = 0; i < N; i++) o[i] = t[i];
+PP_DEVINL bool all_finite(const float (&o)[N]) {
+    float x = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; i++) x = fmaf(o[i], 0.f, x);  // NaN once one is not finite
+    return x == 0.f;
 }
 
 // Scores of 32 N keys of one row, from t_s in TMEM (this warp's lanes).
@@ -252,6 +231,7 @@ struct Scores {
 #pragma unroll
         for (int c = 0; c < N; c++) {
             const uint32_t see = seen_bits(a, p, tok, k0 + 32 * c);
+            if (__all_sync(kFull, see == 0xffffffffu)) continue;
 #pragma unroll
             for (int i = 0; i < 32; i++)
                 if (!(see >> i & 1u)) s[32 * c + i] = __float_as_uint(-INFINITY);
@@ -267,7 +247,7 @@ struct Scores {
         float u = max3(t[0], t[1], __uint_as_float(s[32 * N - 4])), v = max3(t[2], t[3], __uint_as_float(s[32 * N - 3]));
         return max3(max3(u, v, __uint_as_float(s[32 * N - 2])), __uint_as_float(s[32 * N - 1]), u);
     }
-    // weights 2^(s scale - base) to t_p as bf16 pairs; returns their sum
+    // Weights 2^(s scale - base) to t_p as bf16 pairs; returns their sum.
     PP_DEVINL float weigh(uint32_t t_p, float scale, float base) {
         const unsigned long long sc = pair2(scale, scale), nb = pair2(-base, -base);
         unsigned long long sum0 = 0ull, sum1 = 0ull;
@@ -277,8 +257,9 @@ struct Scores {
 #pragma unroll
             for (int i = 0; i < 16; i++) {
                 const int e = 32 * c + 2 * i;
+                const unsigned long long x2 = fma2(pair2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), sc, nb);
                 float x, y;
-                unpair2(fma2(pair2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), sc, nb), x, y);
+                unpair2(x2, x, y);
                 x = ex2(x);
                 y = ex2(y);
                 w[i] = pack_bf16x2(x, y);
@@ -310,7 +291,6 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
     __shared__ uint32_t taddr_s;
     __shared__ float stat_m[4][32], stat_l[4][32];
     __shared__ unsigned last_s;
-    __shared__ volatile unsigned bad_s;  // a value was taken out of a tile
     __shared__ Item<ROWS, BN> items[kItems];
     __shared__ uint64_t ifull[kItems], iempty[kItems], stretch;
     __shared__ int tiles_s;
@@ -336,7 +316,6 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
         }
         mbar_init(&stretch, 1);
         fence_mbar_init();
-        bad_s = 0;
     }
     if (warp == C::kWarpMma) {
         tmem_alloc(&taddr_s, C::kTmemCols);
@@ -397,13 +376,11 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
             const Item<ROWS, BN>& p = at.item();
             const int k0 = at.t * BN;
             const int end = min(p.key_end - k0, BN);  // rows of the tile that exist
-            // values: rows that some row of queries does not see are looked through, rows past the end set to zero
-            const int open = key ? BN : max(p.open - k0, 0);
             if (a.box > 0) {
                 // boxes of 64 elements x min(page, BN) tokens, one for each of up to 32 lanes
                 static_assert(BN / 8 * NG <= 32, "a lane for each box");
                 const int boxes = (end + a.box - 1) / a.box * NG;
-                const bool fix = !key && (end < BN || open < end);
+                const bool fix = !key && end < BN;  // rows past the end: zeros (a weight of zero does not outweigh NaN)
                 uint64_t* bar = fix ? &landed[slot] : &full[slot];
                 const int row = lane / NG * a.box, grp = lane % NG;
                 const int in_page = (int)((unsigned)(k0 + row) % (unsigned)a.batch.page_size);
@@ -422,7 +399,6 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                     tma_load_4d(dst + grp * BN * 128 + row * 128, key ? &map_k : &map_v, grp * 64, p.h, in_page, page, bar);
                 if (fix) {
                     mbar_wait(bar, (uint32_t)fixes++ & 1u, a.status, lim);
-                    if (open < end && drop_nonfinite<DP, BN>(dst, open, end, lane) && lane == 0) bad_s = 1;
                     zero_rows<DP, BN>(dst, end, BN, lane);
                     fence_proxy_async_smem();
                     __syncwarp();
@@ -446,8 +422,6 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                 }
                 cp_async_commit();
                 cp_async_wait<0>();
-                __syncwarp();
-                if (open < end && drop_nonfinite<DP, BN>(dst, open, end, lane) && lane == 0) bad_s = 1;
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&full[slot]);
@@ -684,7 +658,8 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
             const bool none = t_end == t0;  // no tile of use to this row tile
             // ------------------------------------------------ end of the part
             if (!none) products_done(g - 1);
-            const bool whole = p.whole(), bad = bad_s != 0;
+            const bool whole = p.whole();
+            const bool hidden = min(p.key_end, p.t1 * BN) > open;  // some row does not see some key
             const Split<ROWS, BN>& sp = p.split;
             float* place = whole ? nullptr : sp.place(a, blockIdx.x);
             const int D = a.head_dim;
@@ -736,7 +711,14 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                                 o[i + 2] += v.z;
                                 o[i + 3] += v.w;
                             }
-                        if (bad) add_nonfinite(a, p, p.j * ROWS + er, c + ed, BN, o);
+                        if (hidden && !all_finite(o)) {
+                            float t[8], m0 = -INFINITY, l0 = 0.f;
+                            for (int i = 0; i < C::kParts; i++) m0 = fmaxf(m0, stat_m[i][er]);
+                            if (m0 == -INFINITY) m0 = 0.f;
+                            for (int i = 0; i < C::kParts; i++) l0 += stat_l[i][er] * ex2(stat_m[i][er] - m0);
+                            careful_sum(a, p, p.j * ROWS + er, m0, c + ed, 8, BN, t);
+                            for (int i = 0; i < 8; i++) o[i] = !whole ? t[i] : l0 == 0.f ? 0.f : t[i] / l0;
+                        }
                         if (whole) {
                             *reinterpret_cast<uint4*>(a.out + row_offset(a, p, p.j * ROWS + er, a.out_stride, 2) + (c + ed) * 2) =
                                 Elem<__nv_bfloat16>::pack(o);
@@ -753,27 +735,43 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                     place[(size_t)ROWS * (D + 1) + lane] = l;
                 }
             } else if (active) {
+                // 32 elements of the warp's 32 rows at a time, turned through shared memory so that four lanes write
+                // 64 bytes of a row (a lane a row: 5.3 us an item of 256 rows)
                 const float inv = sum == 0.f ? 0.f : 1.f / sum;
-                char* dst = a.out + row_offset(a, p, p.j * ROWS + min(r, rows - 1), a.out_stride, 2);
+                uint4* turn = reinterpret_cast<uint4*>(stage) + warp * 32 * kTurn;
+                const char* mine = a.out + row_offset(a, p, p.j * ROWS + min(r, rows - 1), a.out_stride, 2);
+                char* dst[4];
+#pragma unroll
+                for (int k = 0; k < 4; k++)
+                    dst[k] = reinterpret_cast<char*>(__shfl_sync(kFull, reinterpret_cast<unsigned long long>(mine), 8 * k + (lane >> 2)));
 #pragma unroll 1
                 for (int c = 0; c < D; c += 32) {
                     uint32_t u[32];
                     tmem_ld32(t_o + c, u);
                     tmem_ld_wait();
-                    if (r >= rows) continue;
                     float o[32];
 #pragma unroll
                     for (int i = 0; i < 32; i++) o[i] = none ? 0.f : __uint_as_float(u[i]);
-                    if (bad) add_nonfinite(a, p, p.j * ROWS + r, c, BN, o);
+                    if (hidden && r < rows && !all_finite(o)) {
+                        float t[32];
+                        careful_sum(a, p, p.j * ROWS + r, mx == -INFINITY ? 0.f : mx, c, 32, BN, t);
+#pragma unroll
+                        for (int i = 0; i < 32; i++) o[i] = t[i];
+                    }
                     if (whole) {
 #pragma unroll
-                        for (int i = 0; i < 32; i += 8) {
-                            if (c + i >= D) break;
+                        for (int i = 0; i < 32; i++) o[i] *= inv;
+                        __syncwarp();
 #pragma unroll
-                            for (int x = 0; x < 8; x++) o[i + x] *= inv;
-                            *reinterpret_cast<uint4*>(dst + (c + i) * 2) = Elem<__nv_bfloat16>::pack(o + i);
+                        for (int i = 0; i < 4; i++) turn[lane * kTurn + i] = Elem<__nv_bfloat16>::pack(o + 8 * i);
+                        __syncwarp();
+#pragma unroll
+                        for (int k = 0; k < 4; k++) {
+                            const int row = 8 * k + (lane >> 2), d = c + (lane & 3) * 8;
+                            if (r - lane + row < rows && d < D)
+                                *reinterpret_cast<uint4*>(dst[k] + d * 2) = turn[row * kTurn + (lane & 3)];
                         }
-                    } else {
+                    } else if (r < rows) {
 #pragma unroll
                         for (int i = 0; i < 32; i += 4)
                             if (c + i < D)
