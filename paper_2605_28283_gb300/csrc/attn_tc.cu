@@ -287,7 +287,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
     unsigned char* ring = smem;
     unsigned char* qs = smem + NS * C::kSlot;
     float* stage = reinterpret_cast<float*>(qs + C::kQBufs * C::kQTile);
-    __shared__ uint64_t full[NS], empty[NS], landed[NS], qfull[2], qempty[2], sfull[2], pfull[2], odone[2];
+    __shared__ uint64_t full[NS], empty[NS], landed[NS], qfull[2], qempty[2], sfull[2], pfull[2], odone[2], turn[2];
     __shared__ uint32_t taddr_s;
     __shared__ float stat_m[4][32], stat_l[4][32];
     __shared__ unsigned last_s;
@@ -309,6 +309,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
             mbar_init(&sfull[i], 1);
             mbar_init(&pfull[i], 4);
             mbar_init(&odone[i], 1);
+            mbar_init(&turn[i], 1);
         }
         for (int i = 0; i < kItems; i++) {
             mbar_init(&ifull[i], 1);
@@ -518,15 +519,21 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                 if (v) wait_full(v_pos(g));
                 if (sc && !fresh) wait_full(k_pos(g + 1));
                 if (v) mbar_wait(&pfull[m], n_o++ & 1u, a.status, lim);
+                // the row tiles take turns: products of both at once would end at once, and then both softmaxes
+                // run at once with the tensor cores idle
+                // (the first after the second's last burst, the second after the first's of the same tile)
+                if (g + m >= 0) mbar_wait(&turn[m], (uint32_t)(g + m) & 1u, a.status, lim);
                 tc_fence_after();
                 if (one && v) issue_values(g);
                 if (one && g >= 0) umma_commit(&empty[v_pos(g) % NS]);
                 if (fresh) {
+                    if (one) mbar_arrive(&turn[1 - m]);
                     wait_q();
                     if (sc) wait_full(k_pos(g + 1));
                     tc_fence_after();
                 }
                 if (one && sc) issue_scores(g + 1);
+                if (one && !fresh) mbar_arrive(&turn[1 - m]);
                 if (one && more) release_scores(g + 1);
                 __syncwarp();
                 if (g >= 0 && more && co.step(1, lane, true)) end_o = co.item().end[m];
