@@ -287,7 +287,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
     unsigned char* ring = smem;
     unsigned char* qs = smem + NS * C::kSlot;
     float* stage = reinterpret_cast<float*>(qs + C::kQBufs * C::kQTile);
-    __shared__ uint64_t full[NS], empty[NS], landed[NS], qfull[2], qempty[2], sfull[2], pfull[2], odone[2], turn[2];
+    __shared__ uint64_t full[NS], empty[NS], landed[NS], qfull[2], qempty[2], sfull[2], pfull[2], odone[4], turn[2];
     __shared__ uint32_t taddr_s;
     __shared__ float stat_m[4][32], stat_l[4][32];
     __shared__ unsigned last_s;
@@ -309,6 +309,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
             mbar_init(&sfull[i], 1);
             mbar_init(&pfull[i], 4);
             mbar_init(&odone[i], 1);
+            mbar_init(&odone[2 + i], 1);
             mbar_init(&turn[i], 1);
         }
         for (int i = 0; i < kItems; i++) {
@@ -498,6 +499,11 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                 umma_k64(tm + (uint32_t)(s_slot(g) * BN), qt + d * 128 * 128, kt + d * BN * 128, id_s, d > 0);
             umma_commit(&sfull[s_slot(g)]);
         };
+        // n: the tile's number among those of use to the row tile
+        auto release_values = [&](int g, int n, bool live) {
+            if (live) umma_commit(&odone[2 * m + (n & 1)]);
+            umma_commit(&empty[v_pos(g) % NS]);
+        };
         auto release_scores = [&](int g) {  // the key slot and, behind the part's last tile, the rows of q
             umma_commit(&empty[k_pos(g) % NS]);
             if (cs.t + 1 == cs.t1) umma_commit(&qempty[q_buf()]);
@@ -508,7 +514,6 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
             for (int k = 0; k < BN / 16; k++)
                 umma_bf16_ta(tm + C::kTmemO + (uint32_t)(m * DP), tm + (uint32_t)(s_slot(g) * BN + 8 * k),
                              vd + (uint64_t)(k * 128), id_o, (co.t > co.t0 || k > 0) ? 1u : 0u);
-            umma_commit(&odone[s_slot(g)]);
         };
         if (MT == 2) {
             uint32_t n_o = 0;  // value products issued
@@ -525,8 +530,8 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                 if (g + m >= 0) mbar_wait(&turn[m], (uint32_t)(g + m) & 1u, a.status, lim);
                 tc_fence_after();
                 if (one && v) issue_values(g);
-                if (one && g >= 0) umma_commit(&empty[v_pos(g) % NS]);
                 if (fresh) {
+                    if (one && g >= 0) release_values(g, (int)n_o - 1, v);
                     if (one) mbar_arrive(&turn[1 - m]);
                     wait_q();
                     if (sc) wait_full(k_pos(g + 1));
@@ -534,6 +539,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                 }
                 if (one && sc) issue_scores(g + 1);
                 if (one && !fresh) mbar_arrive(&turn[1 - m]);
+                if (one && !fresh && g >= 0) release_values(g, (int)n_o - 1, v);  // behind the scores: commits cost issue time
                 if (one && more) release_scores(g + 1);
                 __syncwarp();
                 if (g >= 0 && more && co.step(1, lane, true)) end_o = co.item().end[m];
@@ -562,7 +568,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                 tc_fence_after();
                 if (one) {
                     issue_values(g);
-                    umma_commit(&empty[v_pos(g) % NS]);
+                    release_values(g, g, true);
                 }
                 __syncwarp();
                 if (g + 1 < tiles) co.step(1, lane, true);
@@ -574,10 +580,10 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
         const uint32_t lanes = (uint32_t)(32 * wq) << 16;
         const uint32_t t_o = tmem + C::kTmemO + (uint32_t)(m * DP) + lanes;
         int g = 0;  // tile of the stretch
-        // O holds the products up to tile x (the last or last but one whose
-        // scores this warp has seen, so a parity names its phase)
+        // O holds the products up to tile x of this row tile (barriers take turns, so that a parity cannot stand
+        // for the last phase but one)
         auto products_done = [&](int x) {
-            mbar_wait(&odone[MT == 1 ? x & 1 : m], (uint32_t)(MT == 1 ? x >> 1 : x) & 1u, a.status, lim);
+            mbar_wait(&odone[2 * m + (x & 1)], (uint32_t)(x >> 1) & 1u, a.status, lim);
             tc_fence_after();
         };
         at.enter(0);
