@@ -138,10 +138,28 @@ def _ptr(t):
     return ctypes.c_void_p(t.data_ptr())
 
 
+_raw_stream = None
+
+
+def _current_stream() -> int:
+    """Handle of torch's current stream on the current device.  torch.cuda.current_stream() builds a Stream object in
+    about 3 us, half of a small call; the raw handle takes a tenth of a microsecond."""
+    global _raw_stream
+    if _raw_stream is None:
+        import torch
+        torch.cuda.init()
+        get = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        dev = getattr(torch._C, "_cuda_getDevice", None)
+        if get is not None and dev is not None:
+            _raw_stream = lambda: get(dev())  # noqa: E731
+        else:
+            _raw_stream = lambda: torch.cuda.current_stream().cuda_stream  # noqa: E731
+    return _raw_stream()
+
+
 def _stream(stream):
     if stream is None:
-        import torch
-        return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+        return ctypes.c_void_p(_current_stream())
     if isinstance(stream, int):
         return ctypes.c_void_p(stream)
     return ctypes.c_void_p(stream.cuda_stream)
@@ -291,14 +309,16 @@ def _torch_dtype(t) -> int:
 def _rows(t, n_tokens, n_heads, head_dim, dtype, what):
     """Pointer and token stride of a token tensor [n_tokens, heads, head_dim] (or [n_tokens, heads * head_dim])
     whose tokens are each contiguous."""
+    shape, stride = t.shape, t.stride()
+    if t.dtype == dtype and shape == (n_tokens, n_heads, head_dim) and stride[1:] == (head_dim, 1):
+        return t.data_ptr(), (stride[0] if n_tokens > 1 else n_heads * head_dim)
     if t.dtype != dtype:
         raise PPError(PP_ERR_DTYPE, what)
-    if t.numel() != n_tokens * n_heads * head_dim or (t.dim() == 3 and t.shape[1] != n_heads) or \
-            t.dim() not in (2, 3) or t.shape[0] != n_tokens:
+    if shape != (n_tokens, n_heads, head_dim) and shape != (n_tokens, n_heads * head_dim):
         raise PPError(PP_ERR_SHAPE, what)
-    if t.stride(-1) != 1 or (t.dim() == 3 and n_heads > 1 and t.stride(1) != head_dim):
+    if (head_dim > 1 and stride[-1] != 1) or (len(shape) == 3 and n_heads > 1 and stride[1] != head_dim):
         raise PPError(PP_ERR_INVALID_ARG, what + ": the heads of a token must be contiguous")
-    return t.data_ptr(), (t.stride(0) if n_tokens > 1 else n_heads * head_dim)
+    return t.data_ptr(), (stride[0] if n_tokens > 1 else n_heads * head_dim)
 
 
 def _int32(t, what):
@@ -320,6 +340,7 @@ class Rotation:
         self.inv_freq = inv_freq
         self.c = pp_rotation(2 * inv_freq.numel(), ROPE_LAYOUTS.get(layout, layout), float(scale),
                              inv_freq.data_ptr())
+        self.ref = ctypes.byref(self.c)
 
     @classmethod
     def make(cls, rot_dim, base=10000.0, layout="half", scaling="none", factor=1.0, low=1.0, high=32.0,
@@ -344,6 +365,9 @@ class KVCache:
         self.k, self.v = k, v
         self.c = pp_cache(_torch_dtype(k), int(n_heads), k.shape[2], k.shape[3], k.shape[1], k.shape[0], k.stride(0),
                           k.stride(1), k.stride(2), k.data_ptr(), v.data_ptr())
+        self.ref = ctypes.byref(self.c)
+        # what the calls compare their tensors with
+        self.dtype, self.n_heads, self.n_kv_heads, self.head_dim = k.dtype, int(n_heads), k.shape[2], k.shape[3]
 
 
 class Batch:
@@ -356,6 +380,7 @@ class Batch:
         self.q_start, self.ctx_len, self.pages = q_start, ctx_len, pages
         self.c = pp_batch(n, int(n_tokens), pages.shape[1], _int32(q_start, "q_start"), _int32(ctx_len, "ctx_len"),
                           _int32(pages, "pages"))
+        self.ref, self.n_tokens, self.n_seqs = ctypes.byref(self.c), int(n_tokens), n
 
 
 def pp_rope_frequencies(scaling, rot_dim, base=10000.0, factor=1.0, low=1.0, high=32.0, trained_len=0):
@@ -376,14 +401,15 @@ def pp_rope(rot, positions, x, y, inverse=False, stream=None):
     T, H, D = x.shape
     if positions.numel() != T:
         raise PPError(PP_ERR_SHAPE, "pp_rope: positions")
-    px, sx = _rows(x, T, H, D, x.dtype, "pp_rope: x")
-    py, sy = _rows(y, T, H, D, x.dtype, "pp_rope: y")
-    _check(load().pp_rope(_torch_dtype(x), ctypes.byref(rot.c), _int32(positions, "positions"), T, H, D, px, sx, py,
-                          sy, 1 if inverse else 0, _stream(stream)), "pp_rope")
+    dt = x.dtype
+    px, sx = _rows(x, T, H, D, dt, "pp_rope: x")
+    py, sy = _rows(y, T, H, D, dt, "pp_rope: y")
+    _check(load().pp_rope(_torch_dtype(x), rot.ref, _int32(positions, "positions"), T, H, D, px, sx, py, sy,
+                          1 if inverse else 0, _stream(stream)), "pp_rope")
 
 
 def pp_attn_workspace_size(cache) -> int:
-    return int(load().pp_attn_workspace_size(ctypes.byref(cache.c)))
+    return int(load().pp_attn_workspace_size(cache.ref))
 
 
 def alloc_attn_workspace(cache, device=None, stream=None):
@@ -396,48 +422,46 @@ def alloc_attn_workspace(cache, device=None, stream=None):
 
 def pp_kv_append(cache, batch, rot, positions, q, k, v, q_out, ws, stream=None):
     """Append k, v [T, n_kv_heads, head_dim] to their pages, keys rotated; q_out = q rotated (both may be None)."""
-    c, T = cache.c, batch.c.n_tokens
-    dt = cache.k.dtype
+    T, D, dt = batch.n_tokens, cache.head_dim, cache.dtype
     pq, sq, po, so = None, 0, None, 0
     if q is not None:
-        pq, sq = _rows(q, T, c.n_heads, c.head_dim, dt, "pp_kv_append: q")
+        pq, sq = _rows(q, T, cache.n_heads, D, dt, "pp_kv_append: q")
     if q_out is not None:
-        po, so = _rows(q_out, T, c.n_heads, c.head_dim, dt, "pp_kv_append: q_out")
-    pk, sk = _rows(k, T, c.n_kv_heads, c.head_dim, dt, "pp_kv_append: k")
-    pv, sv = _rows(v, T, c.n_kv_heads, c.head_dim, dt, "pp_kv_append: v")
+        po, so = _rows(q_out, T, cache.n_heads, D, dt, "pp_kv_append: q_out")
+    pk, sk = _rows(k, T, cache.n_kv_heads, D, dt, "pp_kv_append: k")
+    pv, sv = _rows(v, T, cache.n_kv_heads, D, dt, "pp_kv_append: v")
     pos = None
     if positions is not None:
         if positions.numel() != T:
             raise PPError(PP_ERR_SHAPE, "pp_kv_append: positions")
         pos = _int32(positions, "positions")
-    _check(load().pp_kv_append(ctypes.byref(c), ctypes.byref(batch.c), None if rot is None else ctypes.byref(rot.c),
-                               pos, pq, sq, pk, sk, pv, sv, po, so, *_wsargs(ws), _stream(stream)), "pp_kv_append")
+    _check(load().pp_kv_append(cache.ref, batch.ref, None if rot is None else rot.ref, pos, pq, sq, pk, sk, pv, sv, po,
+                               so, ws.data_ptr(), ws.nbytes, _stream(stream)), "pp_kv_append")
 
 
 def pp_tree_attention(cache, batch, q, mask, scale, out, ws, stream=None):
     """out = attention of q [T, n_heads, head_dim] over the cache; mask [T, words] int32 bits, or None (chains)."""
-    c, T = cache.c, batch.c.n_tokens
-    pq, sq = _rows(q, T, c.n_heads, c.head_dim, cache.k.dtype, "pp_tree_attention: q")
-    po, so = _rows(out, T, c.n_heads, c.head_dim, cache.k.dtype, "pp_tree_attention: out")
+    T, D, dt = batch.n_tokens, cache.head_dim, cache.dtype
+    pq, sq = _rows(q, T, cache.n_heads, D, dt, "pp_tree_attention: q")
+    po, so = _rows(out, T, cache.n_heads, D, dt, "pp_tree_attention: out")
     pm, words = None, 0
     if mask is not None:
         if mask.dim() != 2 or mask.shape[0] != T:
             raise PPError(PP_ERR_SHAPE, "pp_tree_attention: mask")
         pm, words = _int32(mask, "mask"), mask.shape[1]
-    _check(load().pp_tree_attention(ctypes.byref(c), ctypes.byref(batch.c), pq, sq, pm, words, float(scale), po, so,
-                                    *_wsargs(ws), _stream(stream)), "pp_tree_attention")
+    _check(load().pp_tree_attention(cache.ref, batch.ref, pq, sq, pm, words, scale, po, so, ws.data_ptr(), ws.nbytes,
+                                    _stream(stream)), "pp_tree_attention")
 
 
 def pp_kv_commit(cache, batch, path, n_accept, ws, new_len=None, n_layers=1, layer_stride=0, stream=None):
     """Move the accepted path [n_seqs, max_path] of each tree behind its context, in every layer's cache."""
-    n = batch.c.n_seqs
+    n = batch.n_seqs
     if path.dim() != 2 or path.shape[0] != n or n_accept.numel() != n or \
             (new_len is not None and new_len.numel() != n):
         raise PPError(PP_ERR_SHAPE, "pp_kv_commit")
-    _check(load().pp_kv_commit(ctypes.byref(cache.c), ctypes.byref(batch.c), int(n_layers), int(layer_stride),
-                               _int32(path, "path"), path.shape[1], _int32(n_accept, "n_accept"),
-                               None if new_len is None else _int32(new_len, "new_len"), *_wsargs(ws),
-                               _stream(stream)), "pp_kv_commit")
+    _check(load().pp_kv_commit(cache.ref, batch.ref, n_layers, layer_stride, _int32(path, "path"), path.shape[1],
+                               _int32(n_accept, "n_accept"), None if new_len is None else _int32(new_len, "new_len"),
+                               ws.data_ptr(), ws.nbytes, _stream(stream)), "pp_kv_commit")
 
 
 def pp_get_device_status(ws, stream=None) -> int:

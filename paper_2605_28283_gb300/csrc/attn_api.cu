@@ -1,5 +1,6 @@
 // C ABI of the attention side: argument checks, workspace layout, dispatch.
 // Nothing here allocates, synchronises or lets an exception out.
+#include <atomic>
 #include <cmath>
 #include <cstring>
 
@@ -19,15 +20,21 @@ constexpr uint64_t kWaitLimitNs = 2000000000ull;  // bounded waits give up after
 
 bool aligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 
-// SM count of the current device, which must be a GB300.
+// SM count of the current device, which must be a GB300.  Asked for once a
+// device: what is kept is a property of the device, written as one word.
 pp_status device_sms(int* sms) {
+    static std::atomic<int> known[64];
     int dev = 0, major = 0, minor = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess ||
-        cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
+    if (cudaGetDevice(&dev) != cudaSuccess) return PP_ERR_CUDA;
+    const bool keep = dev >= 0 && dev < 64;
+    if (keep && (*sms = known[dev].load(std::memory_order_relaxed)) > 0) return PP_OK;
+    if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
         cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev) != cudaSuccess ||
         cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
         return PP_ERR_CUDA;
-    return major == 10 && minor == 3 ? PP_OK : PP_ERR_UNSUPPORTED;
+    if (major != 10 || minor != 3) return PP_ERR_UNSUPPORTED;
+    if (keep) known[dev].store(*sms, std::memory_order_relaxed);
+    return PP_OK;
 }
 
 pp_status cuda_status(cudaError_t e) { return e == cudaSuccess ? PP_OK : PP_ERR_CUDA; }

@@ -238,7 +238,8 @@ cudaError_t go(const AttnArgs& a, int sms, cudaStream_t st) {
     using L = Simt<T, ROWS, TOK, DP>;
     auto* kern = attn_simt_kernel<T, ROWS, TOK, DP>;
     constexpr int kBytes = L::kFloats * 4;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+    static std::atomic<bool> allowed[64];
+    cudaError_t e = allow_smem(kern, kBytes, allowed);
     if (e != cudaSuccess) return e;
     const int per_sm = 227 * 1024 / (kBytes + 2048);
     int grid = sms * (per_sm < 1 ? 1 : per_sm > 4 ? 4 : per_sm);

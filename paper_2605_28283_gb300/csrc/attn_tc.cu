@@ -878,7 +878,8 @@ template <int DP, int MT>
 cudaError_t go(AttnArgs a, bool join_later, int sms, cudaStream_t st) {
     using C = Tc<DP, MT>;
     auto* kern = attn_tc_kernel<DP, MT>;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
+    static std::atomic<bool> allowed[64];
+    cudaError_t e = allow_smem(kern, C::kSmem, allowed);
     if (e != cudaSuccess) return e;
     // TMA boxes where pages and key tiles divide one another and a box fills
     // whole 8-row swizzle atoms; else 16-byte cp.async, for any page
