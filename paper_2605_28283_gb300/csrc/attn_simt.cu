@@ -1,15 +1,17 @@
-// Attention over the paged cache on the CUDA cores, fp32 arithmetic: the fp32
-// path.  One CTA streams its stretch of the key line (pp_attn_sched.cuh) tile
-// by tile: TOK keys and values into shared memory, scores, the running
-// maximum and weight sum of each row, weighted values into registers.
+// Attention over the paged cache on the CUDA cores: the fp32 path, fp32
+// throughout.  One CTA streams its stretch of the key line (pp_attn_sched.cuh)
+// tile by tile: TOK keys and values into shared memory (cp.async, entries past
+// the sequence as zeros), scores, the running maximum and weight sum of each
+// row, weighted values into registers.
 //
 // Register tiles are 4 rows x 1 key (scores, the head dimension split over
 // the threads that a small row tile leaves free) and 4 rows x 4 elements
 // (values, the keys split likewise); the splits are joined through shared
-// memory.  Several CTAs per SM overlap the loads of one with the arithmetic
+// memory.  Up to four CTAs per SM overlap the loads of one with the arithmetic
 // of the others.
 #include "pp_attn_sched.cuh"
 #include "pp_launch.cuh"
+#include "pp_tc.cuh"
 
 namespace pp {
 namespace {
@@ -17,7 +19,7 @@ namespace {
 constexpr int kThreads = 256;
 
 // Rows of a tile, keys of a tile, padded head dimension.
-template <typename T, int ROWS, int TOK, int DP>
+template <int ROWS, int TOK, int DP>
 struct Simt {
     static constexpr int kRG = ROWS / 4;                        // groups of 4 rows
     static constexpr int kScoreCols = TOK * kRG;                 // (row group, key) pairs
@@ -36,10 +38,9 @@ struct Simt {
     static_assert((kTSplit - 1) * ROWS * DP <= TOK * (kKStride + DP), "joining area");
 };
 
-template <typename T, int ROWS, int TOK, int DP>
+template <int ROWS, int TOK, int DP>
 __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_constant__ AttnArgs a) {
-    using L = Simt<T, ROWS, TOK, DP>;
-    constexpr int kVec = Elem<T>::kPer16B;
+    using L = Simt<ROWS, TOK, DP>;
     extern __shared__ __align__(16) float sm[];
     __shared__ unsigned last_s;
     float *Qs = sm + L::kQ, *Ks = sm + L::kK, *Vs = sm + L::kV, *Ss = sm + L::kS, *Ps = sm + L::kP;
@@ -57,15 +58,10 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_consta
     while (walk.next(p)) {
         const int rows = min(ROWS, p.seq.n * a.group - p.j * ROWS);
         __syncthreads();  // the last part's readers are done
-        for (int e = tid; e < ROWS * (DP / kVec); e += kThreads) {
-            const int r = e / (DP / kVec), d = e % (DP / kVec) * kVec;
-            float f[kVec] = {};
-            if (r < rows && d < D)
-                Elem<T>::unpack(*reinterpret_cast<const uint4*>(
-                                    a.q + row_offset(a, p, p.j * ROWS + r, a.q_stride, (int)sizeof(T)) + d * sizeof(T)),
-                                f);
-#pragma unroll
-            for (int i = 0; i < kVec; i++) Qs[r * DP + d + i] = f[i] * a.scale_log2;
+        for (int e = tid; e < ROWS * (DP / 4); e += kThreads) {
+            const int r = e / (DP / 4), d = e % (DP / 4) * 4;
+            const bool in = r < rows && d < D;
+            cp_async_16(Qs + r * DP + d, in ? a.q + row_offset(a, p, p.j * ROWS + r, a.q_stride, 4) + d * 4 : a.q, in ? 16u : 0u);
         }
         if (tid < ROWS) {
             Mx[tid] = -INFINITY;
@@ -75,26 +71,24 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_consta
         for (int t = p.t0; t < p.t1; t++) {
             const int k0 = t * TOK;
             __syncthreads();  // the last tile's readers are done (first tile: rows are in place)
-            for (int e = tid; e < TOK * (DP / kVec); e += kThreads) {
-                const int r = e / (DP / kVec), d = e % (DP / kVec) * kVec, j = k0 + r;
-                float fk[kVec] = {}, fv[kVec] = {};
-                if (j < p.key_end && d < D) {
+            for (int e = tid; e < TOK * (DP / 4); e += kThreads) {
+                const int r = e / (DP / 4), d = e % (DP / 4) * 4, j = k0 + r;
+                long long at = 0;
+                bool in = j < p.key_end && d < D;
+                if (in) {
                     const int page = entry_page(a.batch, p.b, j);
                     if (page >= 0) {
-                        const long long at = entry_offset(a.batch, a.cache, page, j) + (long long)p.h * a.cache.head_stride +
-                                             d * (long long)sizeof(T);
-                        Elem<T>::unpack(*reinterpret_cast<const uint4*>(a.cache.k + at), fk);
-                        Elem<T>::unpack(*reinterpret_cast<const uint4*>(a.cache.v + at), fv);
+                        at = entry_offset(a.batch, a.cache, page, j) + (long long)p.h * a.cache.head_stride + d * 4;
                     } else {
                         record_status(a.status, PP_ERR_INVALID_ARG);
+                        in = false;
                     }
                 }
-#pragma unroll
-                for (int i = 0; i < kVec; i += 4) {
-                    *reinterpret_cast<float4*>(Ks + r * L::kKStride + d + i) = make_float4(fk[i], fk[i + 1], fk[i + 2], fk[i + 3]);
-                    *reinterpret_cast<float4*>(Vs + r * DP + d + i) = make_float4(fv[i], fv[i + 1], fv[i + 2], fv[i + 3]);
-                }
+                cp_async_16(Ks + r * L::kKStride + d, a.cache.k + at, in ? 16u : 0u);
+                cp_async_16(Vs + r * DP + d, a.cache.v + at, in ? 16u : 0u);
             }
+            cp_async_commit();
+            cp_async_wait<0>();
             __syncthreads();
             if (s_ds < L::kDSplit) {
                 float acc[4] = {};
@@ -130,7 +124,7 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_consta
                     s[i] = 0.f;
 #pragma unroll
                     for (int x = 0; x < L::kDSplit; x++) s[i] += Ss[(x * ROWS + r) * TOK + c];
-                    if (!see) s[i] = -INFINITY;
+                    s[i] = see ? s[i] * a.scale_log2 : -INFINITY;
                     mx = fmaxf(mx, s[i]);
                 }
                 const float m_old = Mx[r], m_new = fmaxf(m_old, warp_max(mx));
@@ -209,8 +203,8 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_consta
                     const int r = v_rg * 4 + i;
                     if (r >= rows) break;
                     const float l = Sum[r], inv = l == 0.f ? 0.f : 1.f / l;
-                    char* dst = a.out + row_offset(a, p, p.j * ROWS + r, a.out_stride, (int)sizeof(T)) + v_d * (int)sizeof(T);
-                    store4<T>(dst, make_float4(o[i][0], o[i][1], o[i][2], o[i][3]), inv);
+                    char* dst = a.out + row_offset(a, p, p.j * ROWS + r, a.out_stride, 4) + v_d * 4;
+                    store4<float>(dst, make_float4(o[i][0], o[i][1], o[i][2], o[i][3]), inv);
                 }
             }
             continue;
@@ -229,14 +223,14 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_consta
         __syncthreads();
         if (tid == 0) last_s = arrive_last(a.counters + sp.c0, (unsigned)(sp.c1 - sp.c0 + 1));
         __syncthreads();
-        if (last_s) merge_few<T, ROWS, TOK>(a, p, sp, tid, kThreads);
+        if (last_s) merge_few<float, ROWS, TOK>(a, p, sp, tid, kThreads);
     }
 }
 
-template <typename T, int ROWS, int TOK, int DP>
+template <int ROWS, int TOK, int DP>
 cudaError_t go(const AttnArgs& a, int sms, cudaStream_t st) {
-    using L = Simt<T, ROWS, TOK, DP>;
-    auto* kern = attn_simt_kernel<T, ROWS, TOK, DP>;
+    using L = Simt<ROWS, TOK, DP>;
+    auto* kern = attn_simt_kernel<ROWS, TOK, DP>;
     constexpr int kBytes = L::kFloats * 4;
     static std::atomic<bool> allowed[64];
     cudaError_t e = allow_smem(kern, kBytes, allowed);
@@ -247,17 +241,6 @@ cudaError_t go(const AttnArgs& a, int sms, cudaStream_t st) {
     return launch_overlapped(kern, dim3((unsigned)grid), dim3(kThreads), kBytes, st, a);
 }
 
-template <typename T>
-cudaError_t go_dim(const AttnArgs& a, int sms, cudaStream_t st) {
-    // rows a sequence brings to a key head on average: small tiles spread
-    // their threads over keys and elements instead of rows that do not exist
-    const long long rows = ((long long)a.batch.n_tokens * a.group + a.batch.n_seqs - 1) / a.batch.n_seqs;
-    const bool few = rows <= 4;
-    if (a.head_dim <= 64) return few ? go<T, 4, 64, 64>(a, sms, st) : go<T, 16, 64, 64>(a, sms, st);
-    if (a.head_dim <= 128) return few ? go<T, 4, 64, 128>(a, sms, st) : go<T, 16, 64, 128>(a, sms, st);
-    return few ? go<T, 4, 64, 256>(a, sms, st) : go<T, 16, 64, 256>(a, sms, st);
-}
-
 }  // namespace
 
 size_t attn_part_floats(int head_dim) {
@@ -265,6 +248,14 @@ size_t attn_part_floats(int head_dim) {
     return 2 * (simt > tc ? simt : tc) * (head_dim + 2);
 }
 
-cudaError_t attn_simt_launch(const AttnArgs& a, int sms, cudaStream_t st) { return go_dim<float>(a, sms, st); }
+cudaError_t attn_simt_launch(const AttnArgs& a, int sms, cudaStream_t st) {
+    // rows a sequence brings to a key head on average: small tiles spread
+    // their threads over keys and elements instead of rows that do not exist
+    const long long rows = ((long long)a.batch.n_tokens * a.group + a.batch.n_seqs - 1) / a.batch.n_seqs;
+    const bool few = rows <= 4;
+    if (a.head_dim <= 64) return few ? go<4, 64, 64>(a, sms, st) : go<16, 64, 64>(a, sms, st);
+    if (a.head_dim <= 128) return few ? go<4, 64, 128>(a, sms, st) : go<16, 64, 128>(a, sms, st);
+    return few ? go<4, 64, 256>(a, sms, st) : go<16, 64, 256>(a, sms, st);
+}
 
 }  // namespace pp

@@ -27,8 +27,9 @@ struct Raw<4> {
 template <typename T, int V>
 struct Vec {
     typename Raw<sizeof(T) * V>::type raw;
-    PP_DEVINL void load(const char* p) { raw = *reinterpret_cast<const decltype(raw)*>(p); }
-    PP_DEVINL void store(char* p) const { *reinterpret_cast<decltype(raw)*>(p) = raw; }
+    // read and written once: first to leave L2 (4 % of a prompt's time)
+    PP_DEVINL void load(const char* p) { raw = __ldcs(reinterpret_cast<const decltype(raw)*>(p)); }
+    PP_DEVINL void store(char* p) const { __stcs(reinterpret_cast<decltype(raw)*>(p), raw); }
     PP_DEVINL float get(int i) const {
         const uint32_t w = reinterpret_cast<const uint32_t*>(&raw)[sizeof(T) == 4 ? i : i / 2];
         if (sizeof(T) == 4) return __uint_as_float(w);
@@ -73,9 +74,15 @@ PP_DEVINL float2 cos_sin(int pos, float f) {
 // of gridDim.y CTAs.  The token's cosines and sines are computed once, into
 // shared memory, while the first loads are in flight.  V elements a vector:
 // 16 bytes, or 2 elements where rot_dim does not split into whole vectors.
-// 4 prompts of 2048 tokens, 40 + 2 x 40 heads of 128, bf16: see the design
-// notes for time and bandwidth.
-constexpr int kAppendUnits = 4;  // units in flight per thread
+//
+// Bound by HBM for many tokens and by latency for few.  8192 tokens of 40
+// query, 40 key and 40 value heads of 128 in bf16 (477 MB): 78 us, 6.1 TB/s
+// (0.90 of the copy rate); the queries alone (168 MB): 31 us, 5.5 TB/s (0.81).
+// What counts for many tokens is few threads a CTA, so that many tokens are in
+// flight (10 units a thread; 5 took 97 us), and for few tokens many CTAs a
+// token.
+constexpr int kAppendUnits = 2;     // units in flight per thread
+constexpr int kUnitsAThread = 10;
 
 template <typename T, int V, bool HALF>
 __global__ void __launch_bounds__(256) append_kernel(const AppendArgs a) {
@@ -207,9 +214,9 @@ cudaError_t append_go(const AppendArgs& a, cudaStream_t st) {
     const int per_v = a.head_dim / V, per_q = per_v - (HALF ? a.rot_dim / 2 / V : 0);
     const int total = (a.q ? a.n_heads * per_q : 0) + a.n_kv_heads * (per_q + per_v);
     const int T_ = a.batch.n_tokens;
-    // enough CTAs for two waves of SMs where there are few tokens
-    int threads = 32 * ((total + 63) / 64);
+    int threads = (total / kUnitsAThread + 31) / 32 * 32;
     threads = threads < 64 ? 64 : threads > 256 ? 256 : threads;
+    // about two CTAs an SM where there are few tokens
     int split = (304 + T_ - 1) / T_;
     const int most = (total + threads - 1) / threads;
     split = split < most ? split : most;
