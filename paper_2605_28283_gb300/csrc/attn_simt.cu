@@ -17,6 +17,7 @@ namespace pp {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kLeastTiles = 2;  // a stretch's key tiles: 1 took 22.5 us, 2 18.7, 3 22.9 for 3 drafted trees over 100 to 1000 entries
 
 // Rows of a tile, keys of a tile, padded head dimension.
 template <int ROWS, int TOK, int DP>
@@ -48,7 +49,7 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_consta
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     pdl_launch_dependents();
     pdl_wait();
-    Walk<ROWS, TOK> walk = start_walk<ROWS, TOK>(&a, lane, blockIdx.x == 0 && warp == 0);
+    Walk<ROWS, TOK> walk = start_walk<ROWS, TOK>(&a, lane, blockIdx.x == 0 && warp == 0, kLeastTiles);
     const int D = a.head_dim;
     // score threads: key, row group, part of the head dimension
     const int s_key = tid % TOK, s_rg = tid / TOK % L::kRG, s_ds = tid / L::kScoreCols;

@@ -337,7 +337,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
 
     if (warp == C::kWarps - 1) {
         // ---------------------------------------------------------- schedule
-        Walk<ROWS, BN> walk = start_walk<ROWS, BN>(&a, lane, blockIdx.x == 0);
+        Walk<ROWS, BN> walk = start_walk<ROWS, BN>(&a, lane, blockIdx.x == 0, 1);
         if (lane == 0) {
             tiles_s = (int)(walk.end - walk.at);
             mbar_arrive(&stretch);
