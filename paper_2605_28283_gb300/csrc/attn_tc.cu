@@ -292,7 +292,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
     __shared__ float stat_m[4][32], stat_l[4][32];
     __shared__ unsigned last_s;
     __shared__ Item<ROWS, BN> items[kItems];
-    __shared__ uint64_t ifull[kItems], iempty[kItems], stretch;
+    __shared__ uint64_t ifull[kItems], isplit[kItems], iempty[kItems], stretch;
     __shared__ int tiles_s;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint64_t lim = a.timeout_ns;
@@ -314,6 +314,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
         }
         for (int i = 0; i < kItems; i++) {
             mbar_init(&ifull[i], 1);
+            mbar_init(&isplit[i], 1);
             mbar_init(&iempty[i], C::kReaders);
         }
         mbar_init(&stretch, 1);
@@ -323,6 +324,11 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
         tmem_alloc(&taddr_s, C::kTmemCols);
         tmem_relinquish();
     }
+    if (tid == C::kWarpSlot * 32 && a.box) {
+        prefetch_map(&map_k);
+        prefetch_map(&map_v);
+    }
+    if (tid == C::kWarpQ * 32 && a.q_box) prefetch_map(&map_q);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -352,10 +358,16 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                 it.open = all_see<ROWS>(a, p);
 #pragma unroll 1
                 for (int m = 0; m < MT; m++) it.end[m] = tile_end<BN, MT>(a, p, m);
-                if (!p.whole()) it.split = Split<ROWS, BN>(walk.sched, p);
-                // an item that begins here and goes on in other stretches
-                if (a.join_later && p.t0 == 0 && !p.whole()) *tail = it;
                 mbar_arrive(&ifull[n % kItems]);
+                // the rest is for the end of the part
+                if (!p.whole()) {
+                    it.split = Split<ROWS, BN>(walk.sched, p);
+                    mbar_arrive(&isplit[n % kItems]);
+                    // an item that begins here and goes on in other stretches
+                    if (a.join_later && p.t0 == 0) *tail = it;
+                } else {
+                    mbar_arrive(&isplit[n % kItems]);
+                }
             }
         }
         __syncwarp();
@@ -674,7 +686,11 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
             const bool whole = p.whole();
             const bool hidden = min(p.key_end, p.t1 * BN) > open;  // some row does not see some key
             const Split<ROWS, BN>& sp = p.split;
-            float* place = whole ? nullptr : sp.place(a, blockIdx.x);
+            float* place = nullptr;
+            if (!whole) {
+                mbar_wait(&isplit[at.n % kItems], (uint32_t)(at.n / kItems) & 1u, a.status, lim);
+                place = sp.place(a, blockIdx.x);
+            }
             const int D = a.head_dim;
             if (few) {
                 // add up the warps' copies through shared memory: 128 elements
@@ -832,7 +848,7 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ AttnA
     using C = Tc<DP, MT>;
     pdl_launch_dependents();
     pdl_wait();
-    const Item<C::kRows, C::BN>& it = reinterpret_cast<const Item<C::kRows, C::BN>*>(a.tails)[blockIdx.x];
+    const Item<C::kRows, C::BN> it = reinterpret_cast<const Item<C::kRows, C::BN>*>(a.tails)[blockIdx.x];  // a copy, in registers
     const int r = 128 * (int)(blockIdx.y % MT) + (int)threadIdx.x;
     const int few = MT == 1 && it.rows <= 32;
     if (few) {  // laid out row by row

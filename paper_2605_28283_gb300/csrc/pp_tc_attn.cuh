@@ -72,6 +72,11 @@ PP_DEVINL void tma_load_3d(void* dst, const CUtensorMap* map, int c0, int c1, in
         : "memory");
 }
 
+// Fetch a tensor map ahead of its first use.
+PP_DEVINL void prefetch_map(const CUtensorMap* map) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
+}
+
 // 2^x, flushing subnormals (softmax weights below 2^-126 count as zero).
 PP_DEVINL float ex2(float x) {
     float y;
