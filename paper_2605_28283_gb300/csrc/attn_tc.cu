@@ -820,10 +820,10 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                 named_bar_sync(1, 32 * C::kSoftWarps);
                 if (last_s) {
                     if (few)
-                        merge_few<__nv_bfloat16, ROWS, BN>(a, p, sp, tid, 32 * C::kSoftWarps);
+                        merge_few<__nv_bfloat16, ROWS, BN, 4>(a, p, sp, tid, 32 * C::kSoftWarps);
                     else if (r < rows)
 #pragma unroll 1
-                        for (int d = 0; d < D / 4; d += 4) merge_row<__nv_bfloat16, ROWS, BN, 4>(a, p, sp, r, d);
+                        for (int d = 0; d < D / 4; d += 4) merge_row<__nv_bfloat16, ROWS, BN, 4, 2, true>(a, p, sp, r, d);
                 }
             }
             left -= at.t1 - at.t0;
@@ -852,9 +852,9 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ AttnA
     const int r = 128 * (int)(blockIdx.y % MT) + (int)threadIdx.x;
     const int few = MT == 1 && it.rows <= 32;
     if (few) {  // laid out row by row
-        if (blockIdx.y == 0) merge_few<__nv_bfloat16, C::kRows, C::BN>(a, it, it.split, threadIdx.x, 128);
+        if (blockIdx.y == 0) merge_few<__nv_bfloat16, C::kRows, C::BN, 4>(a, it, it.split, threadIdx.x, 128);
     } else if (r < it.rows) {
-        merge_row<__nv_bfloat16, C::kRows, C::BN, 4>(a, it, it.split, r, (int)(blockIdx.y / MT) * 4);
+        merge_row<__nv_bfloat16, C::kRows, C::BN, 4, 4, true>(a, it, it.split, r, (int)(blockIdx.y / MT) * 4);
     }
 }
 
