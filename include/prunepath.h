@@ -397,10 +397,12 @@ pp_status pp_kv_append(const pp_cache *cache, const pp_batch *batch, const pp_ro
                  as tokens (a drafted tree: the node's ancestors and itself).
    A token that sees nothing gets zeros.  Entries that a token does not see
    do not reach its output, whatever they hold.  Scores, maxima, sums and
-   outputs are fp32; the bf16 path rounds the softmax weights to bf16 for the
-   product with v (and divides by the sum of the rounded weights), out is
-   rounded once.  The same call gives the same bits every time.  out must not
-   overlap q.  scale: positive and finite. */
+   outputs are fp32 (weights below 2^-126 of their maximum count as zero); the
+   bf16 path rounds the softmax weights to bf16 for the product with v, and out
+   is rounded once.  The same call gives the same bits every time.  out must
+   not overlap q.  scale: positive and finite.  bf16 runs on the tensor cores,
+   fp32 on the CUDA cores; one launch, or two where sequences bring many query
+   rows a key head. */
 pp_status pp_tree_attention(const pp_cache *cache, const pp_batch *batch, const void *q, int64_t q_stride,
                             const uint32_t *mask, int mask_words, float scale, void *out, int64_t out_stride,
                             void *ws, size_t ws_bytes, void *stream);
