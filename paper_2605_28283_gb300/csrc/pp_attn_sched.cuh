@@ -9,8 +9,8 @@
 // host knowing a length.  A stretch covers whole items and at most one part
 // of an item at each end.  A part that is not its whole item leaves its
 // unnormalised sum, maximum and weight sum in the workspace; the CTA that
-// arrives last adds an item's parts up in stretch order (so the result does
-// not depend on who that is).
+// arrives last, or a second kernel, adds an item's parts up in stretch order
+// (so the result does not depend on who does it).
 #pragma once
 
 #include "pp_batch.cuh"
@@ -30,7 +30,7 @@ template <int ROWS, int TOK>
 struct Sched {
     const AttnArgs* a;
     long long total;  // key tiles of the call
-    int ctas;         // CTAs with work: min(grid, total)
+    int ctas;         // CTAs with work
 
     PP_DEVINL int row_tiles(const Seq& s) const { return (int)(((unsigned)s.n * (unsigned)a->group + ROWS - 1) / ROWS); }
 
