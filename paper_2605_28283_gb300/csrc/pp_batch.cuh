@@ -18,10 +18,10 @@ PP_DEVINL Seq load_seq(const BatchArgs& B, int b) {
     const int q0 = B.q_start[b], q1 = B.q_start[b + 1], ctx = B.ctx_len[b];
     Seq s{q0, 0, ctx, true};
     if (q0 < 0 || q1 < q0 || q1 > B.n_tokens || ctx < 0) return s;
-    // 64-bit: max_pages * page_size may pass 2^31, entry numbers may not
+    // 64-bit: max_pages * page_size may pass 2^31
     const long long cap = (long long)B.max_pages * B.page_size;
     const long long need = (long long)ctx + (q1 - q0);
-    if (need > cap || need > 0x7fffffffll) return s;
+    if (need > cap || need > 0x7fffff00ll) return s;  // entry numbers, rounded up to a key tile, stay in 32 bits
     s.n = q1 - q0;
     s.bad = false;
     return s;

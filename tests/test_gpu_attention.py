@@ -128,6 +128,39 @@ def test_masks(pp, dtype, mask, heads, kv, dim):
          seed=heads).check(pp)
 
 
+@pytest.mark.parametrize("page", [8, 128, 256, 384])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_pages_around_the_key_tile(pp, page, dim):
+    """Pages of part of a key tile, of one and of several (bf16: boxes of one page; 384 is no multiple of 256)."""
+    Case([(2, 127), (1, 128), (3, 390), (1, 0), (40, 700)], 4, 2, dim, page, "bf16", seed=page + dim).check(pp)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,kv", [(64, 1), (48, 2), (40, 1), (7, 7)])
+def test_large_and_odd_groups(pp, dtype, heads, kv):
+    """Groups of more heads than a row tile's quarter holds, and groups that do not divide it."""
+    Case([(1, 150), (3, 20), (7, 0)], heads, kv, 64, 16, dtype).check(pp)
+    Case([(5, 130), (9, 1)], heads, kv, 64, 16, dtype, mask="tree").check(pp)
+
+
+@pytest.mark.parametrize("mask", ["chain", "tree", "random"])
+def test_two_row_tiles_with_hidden_values(pp, mask):
+    """More than 128 query rows a key head, a non-finite value that some rows do not see, items that are split."""
+    c = Case([(200, 900), (129, 3)], 4, 2, 64, 16, "bf16", mask=mask, seed=8)
+    clean = Case([(200, 900), (129, 3)], 4, 2, 64, 16, "bf16", mask=mask, seed=8)
+    blind = np.zeros(c.T, bool)
+    for b in range(2):
+        n, ctx = int(c.starts[b + 1] - c.starts[b]), int(c.ctx[b])
+        j = ctx + 70
+        c.v[c.pages[b, j // 16], j % 16, :, 5] = np.inf
+        blind[c.starts[b]:c.starts[b + 1]] = ~ref.visible(n, ctx, c.mask, int(c.starts[b]))[:, j]
+    want, tol = ref.attend(clean.q, clean.k, clean.v, clean.starts, clean.ctx, clean.pages, clean.mask, clean.scale, "bf16")
+    got, status, _ = c.run(pp)
+    assert status == pp.PP_OK and blind.any() and not blind.all()
+    assert (np.abs(got - want)[blind] <= tol[blind]).all()
+    assert not np.isfinite(got[~blind][..., 5]).any()
+
+
 def test_rows_that_see_nothing_are_zero(pp):
     for dtype in ("bf16", "f32"):
         c = Case([(5, 0), (3, 10), (40, 0)], 4, 2, 64, 16, dtype, mask="none")
