@@ -296,14 +296,25 @@ def pp_moefy_permute(desc, perm, W_gate, W_up, W_down, W_gate_out, W_up_out, W_d
                                    _stream(stream)), "pp_moefy_permute")
 
 
-def _torch_dtype(t) -> int:
-    """pp_dtype of a tensor (PP_ERR_DTYPE for any other)."""
-    import torch
-    if t.dtype == torch.bfloat16:
-        return PP_BF16
-    if t.dtype == torch.float32:
-        return PP_F32
-    raise PPError(PP_ERR_DTYPE, "dtype %s" % t.dtype)
+_INT32 = None
+_TORCH_DTYPES = {}
+
+
+def _torch_types():
+    """torch's types, once (importing this module does not import torch)."""
+    global _INT32
+    if _INT32 is None:
+        import torch
+        _TORCH_DTYPES.update({torch.bfloat16: PP_BF16, torch.float32: PP_F32})
+        _INT32 = torch.int32
+
+
+def _torch_dtype(dtype) -> int:
+    """pp_dtype of a torch dtype (PP_ERR_DTYPE for any other)."""
+    d = _TORCH_DTYPES.get(dtype)
+    if d is None:
+        raise PPError(PP_ERR_DTYPE, "dtype %s" % dtype)
+    return d
 
 
 def _rows(t, n_tokens, n_heads, head_dim, dtype, what):
@@ -322,12 +333,17 @@ def _rows(t, n_tokens, n_heads, head_dim, dtype, what):
 
 
 def _int32(t, what):
-    import torch
-    if t.dtype != torch.int32:
+    if t.dtype is not _INT32:
         raise PPError(PP_ERR_DTYPE, what + " must be int32")
     if not t.is_contiguous():
         raise PPError(PP_ERR_INVALID_ARG, what + " must be contiguous")
     return t.data_ptr()
+
+
+def _stream_handle(stream) -> int:
+    if stream is None:
+        return _current_stream()
+    return stream if isinstance(stream, int) else stream.cuda_stream
 
 
 class Rotation:
@@ -335,6 +351,7 @@ class Rotation:
 
     def __init__(self, inv_freq, layout="half", scale=1.0):
         import torch
+        _torch_types()
         if inv_freq.dtype != torch.float32 or not inv_freq.is_contiguous():
             raise PPError(PP_ERR_DTYPE, "inv_freq must be contiguous float32")
         self.inv_freq = inv_freq
@@ -356,6 +373,7 @@ class KVCache:
     both) with contiguous head_dim.  Pages stored head by head are passed as their transposed view."""
 
     def __init__(self, k, v, n_heads):
+        _torch_types()
         if k.dim() != 4 or k.shape != v.shape:
             raise PPError(PP_ERR_SHAPE, "KVCache")
         if k.dtype != v.dtype:
@@ -363,7 +381,7 @@ class KVCache:
         if k.stride() != v.stride() or k.stride(3) != 1:
             raise PPError(PP_ERR_INVALID_ARG, "KVCache: strides")
         self.k, self.v = k, v
-        self.c = pp_cache(_torch_dtype(k), int(n_heads), k.shape[2], k.shape[3], k.shape[1], k.shape[0], k.stride(0),
+        self.c = pp_cache(_torch_dtype(k.dtype), int(n_heads), k.shape[2], k.shape[3], k.shape[1], k.shape[0], k.stride(0),
                           k.stride(1), k.stride(2), k.data_ptr(), v.data_ptr())
         self.ref = ctypes.byref(self.c)
         # what the calls compare their tensors with
@@ -374,6 +392,7 @@ class Batch:
     """The sequences of a step: q_start [n_seqs + 1], ctx_len [n_seqs], pages [n_seqs, max_pages] (device, int32)."""
 
     def __init__(self, q_start, ctx_len, pages, n_tokens):
+        _torch_types()
         n = ctx_len.numel()
         if q_start.numel() != n + 1 or pages.dim() != 2 or pages.shape[0] != n:
             raise PPError(PP_ERR_SHAPE, "Batch")
@@ -396,16 +415,17 @@ def pp_rope_frequencies(scaling, rot_dim, base=10000.0, factor=1.0, low=1.0, hig
 
 def pp_rope(rot, positions, x, y, inverse=False, stream=None):
     """y = x [T, heads, head_dim] rotated by positions [T] (back, with inverse: the gradient); y may be x."""
-    if x.dim() != 3:
+    shape = x.shape
+    if len(shape) != 3:
         raise PPError(PP_ERR_SHAPE, "pp_rope: x")
-    T, H, D = x.shape
+    T, H, D = shape
     if positions.numel() != T:
         raise PPError(PP_ERR_SHAPE, "pp_rope: positions")
     dt = x.dtype
     px, sx = _rows(x, T, H, D, dt, "pp_rope: x")
     py, sy = _rows(y, T, H, D, dt, "pp_rope: y")
-    _check(load().pp_rope(_torch_dtype(x), rot.ref, _int32(positions, "positions"), T, H, D, px, sx, py, sy,
-                          1 if inverse else 0, _stream(stream)), "pp_rope")
+    _check(load().pp_rope(_torch_dtype(dt), rot.ref, _int32(positions, "positions"), T, H, D, px, sx, py, sy,
+                          1 if inverse else 0, _stream_handle(stream)), "pp_rope")
 
 
 def pp_attn_workspace_size(cache) -> int:
@@ -436,7 +456,7 @@ def pp_kv_append(cache, batch, rot, positions, q, k, v, q_out, ws, stream=None):
             raise PPError(PP_ERR_SHAPE, "pp_kv_append: positions")
         pos = _int32(positions, "positions")
     _check(load().pp_kv_append(cache.ref, batch.ref, None if rot is None else rot.ref, pos, pq, sq, pk, sk, pv, sv, po,
-                               so, ws.data_ptr(), ws.nbytes, _stream(stream)), "pp_kv_append")
+                               so, ws.data_ptr(), ws.nbytes, _stream_handle(stream)), "pp_kv_append")
 
 
 def pp_tree_attention(cache, batch, q, mask, scale, out, ws, stream=None):
@@ -450,7 +470,7 @@ def pp_tree_attention(cache, batch, q, mask, scale, out, ws, stream=None):
             raise PPError(PP_ERR_SHAPE, "pp_tree_attention: mask")
         pm, words = _int32(mask, "mask"), mask.shape[1]
     _check(load().pp_tree_attention(cache.ref, batch.ref, pq, sq, pm, words, scale, po, so, ws.data_ptr(), ws.nbytes,
-                                    _stream(stream)), "pp_tree_attention")
+                                    _stream_handle(stream)), "pp_tree_attention")
 
 
 def pp_kv_commit(cache, batch, path, n_accept, ws, new_len=None, n_layers=1, layer_stride=0, stream=None):
@@ -461,7 +481,7 @@ def pp_kv_commit(cache, batch, path, n_accept, ws, new_len=None, n_layers=1, lay
         raise PPError(PP_ERR_SHAPE, "pp_kv_commit")
     _check(load().pp_kv_commit(cache.ref, batch.ref, n_layers, layer_stride, _int32(path, "path"), path.shape[1],
                                _int32(n_accept, "n_accept"), None if new_len is None else _int32(new_len, "new_len"),
-                               ws.data_ptr(), ws.nbytes, _stream(stream)), "pp_kv_commit")
+                               ws.data_ptr(), ws.nbytes, _stream_handle(stream)), "pp_kv_commit")
 
 
 def pp_get_device_status(ws, stream=None) -> int:
