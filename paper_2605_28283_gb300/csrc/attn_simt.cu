@@ -226,7 +226,7 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_consta
         __syncthreads();
         if (tid == 0) last_s = arrive_last(a.counters + sp.c0, (unsigned)(sp.c1 - sp.c0 + 1));
         __syncthreads();
-        if (last_s) merge_few<float, ROWS, TOK, 1>(a, p, sp, tid, kThreads);
+        if (last_s) merge_few<float, ROWS, TOK, 1>(a, p, sp, rows, tid, kThreads);
     }
 }
 

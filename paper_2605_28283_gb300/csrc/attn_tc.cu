@@ -358,6 +358,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
         if (lane == 0) {
             tiles_s = (int)(walk.end - walk.at);
             mbar_arrive(&stretch);
+            // the record that the second kernel joins by: no rows until an item is split here
             Item<ROWS, BN>* tail = reinterpret_cast<Item<ROWS, BN>*>(a.tails) + blockIdx.x;
             if (a.join_later) tail->rows = 0;
             Part p;
@@ -831,7 +832,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                 named_bar_sync(1, 32 * C::kSoftWarps);
                 if (last_s) {
                     if (few)
-                        merge_few<__nv_bfloat16, ROWS, BN, 4>(a, p, sp, tid, 32 * C::kSoftWarps);
+                        merge_few<__nv_bfloat16, ROWS, BN, 4>(a, p, sp, rows, tid, 32 * C::kSoftWarps);
                     else if (r < rows)
 #pragma unroll 1
                         for (int d = 0; d < D / 4; d += 4) merge_row<__nv_bfloat16, ROWS, BN, 4, 2, true>(a, p, sp, r, d);
@@ -860,10 +861,12 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ AttnA
     pdl_launch_dependents();
     pdl_wait();
     const Item<C::kRows, C::BN> it = reinterpret_cast<const Item<C::kRows, C::BN>*>(a.tails)[blockIdx.x];  // a copy, in registers
+    // no split item begins in this stretch: the rest of the record is of an earlier launch on the workspace
+    if (it.rows == 0) return;
     const int r = 128 * (int)(blockIdx.y % MT) + (int)threadIdx.x;
-    const int few = MT == 1 && it.rows <= 32;
+    const bool few = MT == 1 && it.rows <= 32;
     if (few) {  // laid out row by row
-        if (blockIdx.y == 0) merge_few<__nv_bfloat16, C::kRows, C::BN, 4>(a, it, it.split, threadIdx.x, 128);
+        if (blockIdx.y == 0) merge_few<__nv_bfloat16, C::kRows, C::BN, 4>(a, it, it.split, it.rows, threadIdx.x, 128);
     } else if (r < it.rows) {
         merge_row<__nv_bfloat16, C::kRows, C::BN, 4, 4, true>(a, it, it.split, r, (int)(blockIdx.y / MT) * 4);
     }

@@ -308,11 +308,10 @@ PP_DEVINL void merge_row(const AttnArgs& a, const Part& p, const Split<ROWS, TOK
         if (d0 + i < d4s) store4<T>(dst + (d0 + i) * 4 * (int)sizeof(T), o[i], inv);
 }
 
-// All rows of an item of few, four elements a thread.
+// All `rows` rows of an item of few, four elements a thread.
 template <typename T, int ROWS, int TOK, int U>
-PP_DEVINL void merge_few(const AttnArgs& a, const Part& p, const Split<ROWS, TOK>& sp, int tid, int nthr) {
+PP_DEVINL void merge_few(const AttnArgs& a, const Part& p, const Split<ROWS, TOK>& sp, int rows, int tid, int nthr) {
     const int d4s = a.head_dim / 4;
-    const int rows = min(ROWS, p.seq.n * a.group - p.j * ROWS);
 #pragma unroll 1
     for (int e = tid; e < rows * d4s; e += nthr) merge_row<T, ROWS, TOK, 1, U, false>(a, p, sp, e / d4s, e % d4s);
 }

@@ -1,0 +1,103 @@
+"""GPU tests of tree attention as a serving loop calls it: batches of other
+lengths one after the other on one workspace, as calls and as replays of one
+graph.  Each call is compared with the fp64 definition within its derived
+bound (attn_ref.attend), with sentinel bands around its output."""
+import numpy as np
+import pytest
+
+import attn_ref as ref
+from test_gpu_attention import Case, to_dev
+from test_gpu_canaries import Guarded
+
+pytestmark = pytest.mark.gpu
+
+# (sequences, mask) of successive steps: long and empty contexts, growing and shrinking batches, and items of few
+# rows, of 33 to 128 and of more than 128 rows a key head (4 query heads share one)
+STEPS = [([(32, 4000)], "tree"), ([(32, 0)], "tree"), ([(9, 100)], "tree"), ([(20, 5000), (12, 700)], "tree"),
+         ([(12, 5050)], "chain"), ([(1, 3000), (1, 3001)], "chain"), ([(32, 4100)], "tree"), ([(200, 900)], "chain"),
+         ([(31, 2)], "chain"), ([(9, 2500), (30, 17), (25, 1300)], "tree"), ([(9, 2)], "tree")]
+
+
+def step(pp, case, ws, what):
+    """One call on the workspace, checked."""
+    import torch
+    cache, batch, q, mask, _ = case.device(pp)
+    g = Guarded(tuple(q.shape), q.dtype)
+    g.t.fill_(77.0)
+    pp.pp_tree_attention(cache, batch, q, mask, case.scale, g.t, ws)
+    torch.cuda.synchronize()
+    want, tol = ref.attend(case.q, case.k, case.v, case.starts, case.ctx, case.pages, case.mask, case.scale, case.dtype)
+    off = np.abs(g.t.float().cpu().numpy() - want) - tol
+    assert off.max() <= 0, (what, float(off.max()), np.unravel_index(off.argmax(), off.shape))
+    assert g.bands_intact(), what
+    assert pp.pp_get_device_status(ws) == pp.PP_OK
+
+
+@pytest.mark.parametrize("dtype,dim", [("bf16", 64), ("bf16", 128), ("bf16", 256), ("f32", 64), ("f32", 128)])
+def test_batches_of_other_lengths_on_one_workspace(pp, dtype, dim):
+    first = Case(STEPS[0][0], 4, 1, dim, 16, dtype, mask=STEPS[0][1], stale=0.0)
+    ws = pp.alloc_attn_workspace(first.device(pp)[0])
+    for i, (seqs, mask) in enumerate(STEPS):
+        step(pp, Case(seqs, 4, 1, dim, 16, dtype, mask=mask, seed=i), ws, (i, seqs))
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_steps_with_and_without_split_items(pp, dim):
+    """Every key head's item split, then none split, then fewer tokens (records of the earlier call past the end)."""
+    ws = None
+    for i, seqs in enumerate([[(40, 4000)], [(40, 0)], [(33, 0)], [(40, 4100)], [(33, 50)], [(40, 3900), (35, 10)]]):
+        c = Case(seqs, 4, 4, dim, 32, "bf16", mask="tree", seed=20 + i)
+        ws = pp.alloc_attn_workspace(c.device(pp)[0]) if ws is None else ws
+        step(pp, c, ws, (i, seqs))
+
+
+@pytest.mark.parametrize("dtype,dim", [("bf16", 64), ("bf16", 128), ("bf16", 256), ("f32", 64)])
+@pytest.mark.parametrize("heads,kv", [(2, 2), (8, 1)])
+def test_graph_replays_follow_moving_contexts(pp, dtype, dim, heads, kv):
+    """One captured call of 40-row and 320-row items over contexts that grow and shrink."""
+    import torch
+    c = Case([(40, 4200), (40, 600)], heads, kv, dim, 16, dtype, mask="tree", seed=dim + heads, stale=0.0)
+    cache, batch, q, mask, _ = c.device(pp)
+    g = Guarded(tuple(q.shape), q.dtype)
+    ws = pp.alloc_attn_workspace(cache)
+    pp.pp_tree_attention(cache, batch, q, mask, c.scale, g.t, ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        pp.pp_tree_attention(cache, batch, q, mask, c.scale, g.t, ws)
+    for ctx in ([4200, 600], [0, 0], [4100, 599], [60, 600], [2000, 0], [4200, 1]):
+        c.ctx = np.array(ctx, np.int32)
+        batch.ctx_len.copy_(to_dev(c.ctx))
+        g.t.fill_(77.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        want, tol = ref.attend(c.q, c.k, c.v, c.starts, c.ctx, c.pages, c.mask, c.scale, dtype)
+        assert (np.abs(g.t.float().cpu().numpy() - want) <= tol).all(), ctx
+        assert g.bands_intact() and pp.pp_get_device_status(ws) == pp.PP_OK
+
+
+def test_example_steps_split_items_in_bf16(pp):
+    """The decoding example's layer stack in bf16 with a context long enough that tree steps split their items: the
+    logits of a step computed on a workspace that earlier steps used are the bits of a fresh workspace."""
+    import os
+    import sys
+    import torch
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import tree_decode as td
+    model = td.TreeDecoder(dtype="bf16", heads=4, kv_heads=1, max_tokens=2048)
+    text = [(7 * i) % 23 for i in range(1400)]
+    for i in range(0, 1200, 60):
+        model.forward(text[i:i + 60])
+        model.commit(list(range(60)))
+    lengths = [31, 12, 24, 9]
+    for i, n in enumerate(lengths):
+        nodes = [(text[1200 + i], -1)] + [(text[j], (5 * j + 3) % j) for j in range(1, n)]
+        depths, mask = td.tree_tensors(nodes)
+        tokens = [t for t, _ in nodes]
+        used = model.forward(tokens, depths, mask)
+        kept, model.ws = model.ws, pp.alloc_attn_workspace(model.caches[0])
+        fresh = model.forward(tokens, depths, mask)
+        model.ws = kept
+        assert torch.equal(used, fresh), n
+        model.commit([0])
+    model.check()
