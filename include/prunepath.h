@@ -372,7 +372,9 @@ pp_status pp_rope(int dtype, const pp_rotation *rot, const int32_t *positions, i
 /* Workspace bytes of pp_kv_append, pp_tree_attention and pp_kv_commit for
    this cache, whatever the batch (0 for an unsupported one).  Initialise it
    with pp_workspace_init; errors found on the device are read with
-   pp_get_device_status. */
+   pp_get_device_status.  A recorded bad argument does not keep this call or
+   later ones from computing what is right; after PP_ERR_TIMEOUT (which
+   replaces an earlier code) initialise the workspace again. */
 size_t pp_attn_workspace_size(const pp_cache *cache);
 
 /* Append the new tokens' keys and values to the cache and rotate on the way:

@@ -139,7 +139,7 @@ struct ItemAt {
     PP_DEVINL const Item<ROWS, TOK>& item() const { return ring[n % kItems]; }
     PP_DEVINL void enter(int n_) {
         n = n_;
-        mbar_wait(&full[n % kItems], (uint32_t)(n / kItems) & 1u, status, lim);
+        attn_wait(&full[n % kItems], (uint32_t)(n / kItems) & 1u, status, lim);
         t = t0 = item().t0;
         t1 = item().t1;
     }
@@ -348,7 +348,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
     ItemAt<ROWS, BN> at{items, ifull, iempty, a.status, lim, 0, 0, 0, 0};
     int tiles = 0;  // of this CTA
     if (warp < C::kWarps - 1) {
-        mbar_wait(&stretch, 0, a.status, lim);
+        attn_wait(&stretch, 0, a.status, lim);
         tiles = tiles_s;
     }
 
@@ -364,7 +364,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
             Part p;
             for (int n = 0; walk.next(p); n++) {
                 Item<ROWS, BN>& it = items[n % kItems];
-                if (n >= kItems) mbar_wait(&iempty[n % kItems], (uint32_t)(n / kItems - 1) & 1u, a.status, lim);
+                if (n >= kItems) attn_wait(&iempty[n % kItems], (uint32_t)(n / kItems - 1) & 1u, a.status, lim);
                 static_cast<Part&>(it) = p;
                 it.rows = min(ROWS, p.seq.n * a.group - p.j * ROWS);
                 it.open = all_see<ROWS>(a, p);
@@ -418,20 +418,20 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                         page = a.batch.n_pages;
                     }
                 }
-                if (uses > 0) mbar_wait(&empty[slot], (uint32_t)(uses - 1) & 1u, a.status, lim);
+                if (uses > 0) attn_wait(&empty[slot], (uint32_t)(uses - 1) & 1u, a.status, lim);
                 if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(boxes * a.box * 128));
                 __syncwarp();
                 if (lane < boxes)
                     tma_load_4d(dst + grp * BN * 128 + row * 128, key ? &map_k : &map_v, grp * 64, p.h, in_page, page, bar);
                 if (fix) {
-                    mbar_wait(bar, (uint32_t)fixes++ & 1u, a.status, lim);
+                    attn_wait(bar, (uint32_t)fixes++ & 1u, a.status, lim);
                     zero_rows<DP, BN>(dst, end, BN, lane);
                     fence_proxy_async_smem();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&full[slot]);
                 }
             } else {
-                if (uses > 0) mbar_wait(&empty[slot], (uint32_t)(uses - 1) & 1u, a.status, lim);
+                if (uses > 0) attn_wait(&empty[slot], (uint32_t)(uses - 1) & 1u, a.status, lim);
                 __syncwarp();
 #pragma unroll 1
                 for (int x = 0; x < BN; x += 32) {
@@ -463,7 +463,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
             for (int m = 0; m < MT; m++) {
                 const int buf = MT == 2 ? m : n % C::kQBufs, use = MT == 2 ? n : n / C::kQBufs;
                 const bool few = MT == 1 && rows <= 32;
-                if (use > 0) mbar_wait(&qempty[buf], (uint32_t)(use - 1) & 1u, a.status, lim);
+                if (use > 0) attn_wait(&qempty[buf], (uint32_t)(use - 1) & 1u, a.status, lim);
                 if (a.q_box) {
                     // boxes of 32 rows; past the item's rows they hold other tokens' (rows that nobody reads)
                     if (lane == 0) mbar_arrive_expect_tx(&qfull[buf], C::kQTile);
@@ -512,9 +512,9 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
         auto k_pos = [&](int g) { return MT == 1 ? (g == 0 ? 0 : 2 * g - 1) : 2 * g; };
         auto v_pos = [&](int g) { return MT == 1 ? 2 * g + 2 : 2 * g + 1; };
         auto s_slot = [&](int g) { return MT == 1 ? g & 1 : m; };
-        auto wait_full = [&](int pos) { mbar_wait(&full[pos % NS], (uint32_t)(pos / NS) & 1u, a.status, lim); };
+        auto wait_full = [&](int pos) { attn_wait(&full[pos % NS], (uint32_t)(pos / NS) & 1u, a.status, lim); };
         auto q_buf = [&]() { return MT == 2 ? m : cs.n % C::kQBufs; };
-        auto wait_q = [&]() { mbar_wait(&qfull[q_buf()], (uint32_t)(MT == 2 ? cs.n : cs.n / C::kQBufs) & 1u, a.status, lim); };
+        auto wait_q = [&]() { attn_wait(&qfull[q_buf()], (uint32_t)(MT == 2 ? cs.n : cs.n / C::kQBufs) & 1u, a.status, lim); };
         auto issue_scores = [&](int g) {
             const unsigned char* kt = ring + (k_pos(g) % NS) * C::kSlot;
             const unsigned char* qt = qs + q_buf() * C::kQTile;
@@ -547,11 +547,11 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                 const bool fresh = more && cs.t == cs.t0;  // its queries may still be on their way: values do not wait for them
                 if (v) wait_full(v_pos(g));
                 if (sc && !fresh) wait_full(k_pos(g + 1));
-                if (v) mbar_wait(&pfull[m], n_o++ & 1u, a.status, lim);
+                if (v) attn_wait(&pfull[m], n_o++ & 1u, a.status, lim);
                 // the row tiles take turns: products of both at once would end at once, and then both softmaxes
                 // run at once with the tensor cores idle
                 // (the first after the second's last burst, the second after the first's of the same tile)
-                if (g + m >= 0) mbar_wait(&turn[m], (uint32_t)(g + m) & 1u, a.status, lim);
+                if (g + m >= 0) attn_wait(&turn[m], (uint32_t)(g + m) & 1u, a.status, lim);
                 tc_fence_after();
                 if (one && v) issue_values(g);
                 if (fresh) {
@@ -575,7 +575,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                 if (cs.t == cs.t0) wait_q();
                 wait_full(k_pos(g));
                 // the slot's last weights have been multiplied
-                if (g >= 2) mbar_wait(&odone[g & 1], (uint32_t)((g - 2) >> 1) & 1u, a.status, lim);
+                if (g >= 2) attn_wait(&odone[g & 1], (uint32_t)((g - 2) >> 1) & 1u, a.status, lim);
                 tc_fence_after();
                 if (one) {
                     issue_scores(g);
@@ -588,7 +588,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
 #pragma unroll 1
             for (int g = 0; g < tiles; g++) {
                 wait_full(v_pos(g));
-                mbar_wait(&pfull[g & 1], (uint32_t)(g >> 1) & 1u, a.status, lim);
+                attn_wait(&pfull[g & 1], (uint32_t)(g >> 1) & 1u, a.status, lim);
                 tc_fence_after();
                 if (one) {
                     issue_values(g);
@@ -607,7 +607,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
         // O holds the products up to tile x of this row tile (barriers take turns, so that a parity cannot stand
         // for the last phase but one)
         auto products_done = [&](int x) {
-            mbar_wait(&odone[2 * m + (x & 1)], (uint32_t)(x >> 1) & 1u, a.status, lim);
+            attn_wait(&odone[2 * m + (x & 1)], (uint32_t)(x >> 1) & 1u, a.status, lim);
             tc_fence_after();
         };
         at.enter(0);
@@ -650,7 +650,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                 const int sl = MT == 1 ? g & 1 : m;
                 const uint32_t par = (uint32_t)(MT == 1 ? g >> 1 : g) & 1u;
                 const uint32_t t_s = tmem + (uint32_t)(sl * BN) + lanes;
-                mbar_wait(&sfull[sl], par, a.status, lim);
+                attn_wait(&sfull[sl], par, a.status, lim);
                 tc_fence_after();
                 if (active) {
                     const int k0 = t * BN;
@@ -700,7 +700,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
             const Split<ROWS, BN>& sp = p.split;
             float* place = nullptr;
             if (!whole) {
-                mbar_wait(&isplit[at.n % kItems], (uint32_t)(at.n / kItems) & 1u, a.status, lim);
+                attn_wait(&isplit[at.n % kItems], (uint32_t)(at.n / kItems) & 1u, a.status, lim);
                 place = sp.place(a, blockIdx.x);
             }
             const int D = a.head_dim;

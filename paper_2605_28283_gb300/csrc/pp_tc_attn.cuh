@@ -77,6 +77,27 @@ PP_DEVINL void prefetch_map(const CUtensorMap* map) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
 }
 
+// Wait for a barrier's phase, for at most limit_ns.  On expiry PP_ERR_TIMEOUT
+// is recorded, over an earlier code: the call's results are lost.  Waits that
+// have lasted over 1 ms give up once that is recorded, and only then: a bad
+// page or length recorded by this call or an earlier one leaves the other
+// sequences to be computed, and a wait of several ms is regular (the rows of q
+// wait for a whole item: 1 ms at 64 thousand entries).
+static __device__ __noinline__ void attn_wait_slow(uint64_t* bar, uint32_t parity, unsigned* status, uint64_t limit_ns) {
+    const uint64_t t0 = globaltimer_ns();
+    while (!mbar_try_wait(bar, parity)) {
+        const uint64_t dt = globaltimer_ns() - t0;
+        if (dt > limit_ns) {
+            atomicExch(status, (unsigned)PP_ERR_TIMEOUT);
+            return;
+        }
+        if (dt > 1000000ull && *reinterpret_cast<volatile unsigned*>(status) == PP_ERR_TIMEOUT) return;
+    }
+}
+PP_DEVINL void attn_wait(uint64_t* bar, uint32_t parity, unsigned* status, uint64_t limit_ns) {
+    if (!mbar_try_wait(bar, parity)) attn_wait_slow(bar, parity, status, limit_ns);
+}
+
 // 2^x, flushing subnormals (softmax weights below 2^-126 count as zero).
 PP_DEVINL float ex2(float x) {
     float y;

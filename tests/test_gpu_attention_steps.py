@@ -101,3 +101,54 @@ def test_example_steps_split_items_in_bf16(pp):
         assert torch.equal(used, fresh), n
         model.commit([0])
     model.check()
+
+
+def test_a_recorded_error_does_not_end_long_waits(pp):
+    """A bad length beside a sequence whose items take several ms: warps wait that long for one another, and the
+    recorded error must not end the waits.  152 key heads of 8 over 262144 entries, which are 512 different ones 512
+    times over, so that the definition has 512 + n distinct entries with known multiplicities."""
+    import torch
+    H, D, page, uniq, times, n = 152, 8, 128, 512, 512, 300
+    ctx = uniq * times
+    rng = np.random.default_rng(0)
+
+    def bf16(a):
+        return torch.from_numpy(a.astype(np.float32)).to(torch.bfloat16).float().numpy()
+
+    n_pages = uniq // page + 3
+    k, v = (bf16(rng.standard_normal((n_pages, page, H, D)) + shift) for shift in (0.0, 0.5))
+    q = bf16(rng.standard_normal((n + 1, H, D)))
+    table = np.full((2, ctx // page + 3), -1, np.int32)
+    table[0, :ctx // page] = np.tile(np.arange(uniq // page), times)
+    table[0, ctx // page:] = uniq // page + np.arange(3)
+    cache = pp.KVCache(to_dev(k, "bf16"), to_dev(v, "bf16"), H)
+    batch = pp.Batch(to_dev(np.array([0, n, n + 1], np.int32)), to_dev(np.array([ctx, -1], np.int32)), to_dev(table), n + 1)
+    out = torch.full((n + 1, H, D), 77.0, dtype=torch.bfloat16, device="cuda")
+    ws = pp.alloc_attn_workspace(cache)
+    scale = float(np.float32(D ** -0.5))
+    begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    qd = to_dev(q, "bf16")
+    torch.cuda.synchronize()
+    begin.record()
+    pp.pp_tree_attention(cache, batch, qd, None, scale, out, ws)
+    end.record()
+    assert pp.pp_get_device_status(ws) == pp.PP_ERR_INVALID_ARG
+    # the items of a key head (256 and 44 rows) take about half of it each: waits over 1 ms
+    assert begin.elapsed_time(end) > 4.0
+    got = out.float().cpu().numpy()
+    assert (got[n] == 77.0).all()
+    kk, vv = (a.reshape(-1, H, D).astype(np.float64)[:uniq + n] for a in (k, v))
+    weight = np.concatenate([np.full(uniq, float(times)), np.ones(n)])
+    see = np.concatenate([np.ones((n, uniq), bool), np.tril(np.ones((n, n), bool))], 1)
+    for h in range(0, H, 7):
+        s = scale * (q[:n, h].astype(np.float64) @ kk[:, h].T)
+        top = np.where(see, s, -np.inf).max(1, keepdims=True)
+        p = np.where(see, weight * np.exp(s - top), 0.0)
+        p /= p.sum(1, keepdims=True)
+        want, a = p @ vv[:, h], p @ np.abs(vv[:, h])
+        # attn_ref.attend's bound, the sums over all ctx + n entries
+        eps = ref.F32_HALF_ULP * ((D + 4) * scale * (np.abs(q[:n, h]) @ np.abs(kk[:, h]).T).max(1, keepdims=True)
+                                  + 4 * np.abs(s).max(1, keepdims=True))
+        t = (2 * np.expm1(2 * eps) + 2.0 ** -20 + 2 * ref.F32_HALF_ULP * ((ctx + n) / 32 + 32) + 2 * ref.BF16_HALF_ULP) * a
+        tol = t + ref.BF16_HALF_ULP * (np.abs(want) + t)
+        assert (np.abs(got[:n, h] - want) <= tol).all(), h
