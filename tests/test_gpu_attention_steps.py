@@ -152,3 +152,77 @@ def test_a_recorded_error_does_not_end_long_waits(pp):
         t = (2 * np.expm1(2 * eps) + 2.0 ** -20 + 2 * ref.F32_HALF_ULP * ((ctx + n) / 32 + 32) + 2 * ref.BF16_HALF_ULP) * a
         tol = t + ref.BF16_HALF_ULP * (np.abs(want) + t)
         assert (np.abs(got[:n, h] - want) <= tol).all(), h
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,heads", [(5, 4), (40, 2), (90, 4)])
+def test_pages_that_do_not_exist_read_as_zeros_beside_hidden_values(pp, dtype, n, heads):
+    """A page number out of range in the context of rows that do not see a NaN: its entries are zeros for them too."""
+    c = Case([(n, 100), (2, 9)], heads, 1, 64, 16, dtype, mask="tree", seed=n, stale=0.0)
+    j = 100 + n // 2
+    blind = ~ref.visible(n, 100, c.mask, 0)[:, j]
+    k, v = (np.concatenate([a, np.zeros_like(a[:1])]) for a in (c.k, c.v))
+    c.pages[0, 2] = c.k.shape[0]
+    want, tol = ref.attend(c.q, k, v, c.starts, c.ctx, c.pages, c.mask, c.scale, dtype)
+    c.v[c.pages[0, j // 16], j % 16, :, 3] = np.nan
+    got, status, _ = c.run(pp)
+    assert status == pp.PP_ERR_INVALID_ARG and blind.any() and not blind.all()
+    ok = np.abs(got - want) <= tol
+    assert ok[:n][blind].all() and ok[n:].all()
+    ok[:n, :, 3] = True
+    assert ok.all() and np.isnan(got[:n][~blind][..., 3]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("mask", ["chain", "tree"])
+@pytest.mark.parametrize("n,heads,ctx,page", [(3, 4, 70, 16), (20, 4, 500, 7), (40, 1, 300, 64), (150, 2, 40, 16), (300, 1, 0, 16)])
+def test_non_finite_values_reach_the_rows_that_see_them(pp, dtype, mask, n, heads, ctx, page):
+    """NaN and infinities of both signs in elements of several new tokens' values, a tile's edges among them: an
+    element is what the definition gives (an infinity of a seen value, NaN where both signs or a NaN are seen), every
+    other element and row stays within the bound."""
+    c = Case([(n, ctx), (4, 33)], heads, 1, 64, page, dtype, mask=mask, seed=n, stale=0.0)
+    want, tol = ref.attend(c.q, c.k, c.v, c.starts, c.ctx, c.pages, c.mask, c.scale, dtype)
+    see = ref.visible(n, ctx, c.mask, 0)
+    hit = np.zeros((n, 64))
+    places = {(node, elem): bad for node, elem, bad in  # where two meet, the last stays
+              [(0, 0, np.nan), (n // 2, 9, np.inf), (n - 1, 17, -np.inf), (n // 3, 63, np.inf), (n // 2, 63, -np.inf),
+               (min(n - 1, 127), 31, np.inf), (min(n - 1, 128), 32, -np.inf)]}
+    for (node, elem), bad in places.items():
+        j = ctx + node
+        c.v[c.pages[0, j // page], j % page, :, elem] = bad
+        with np.errstate(invalid="ignore"):
+            hit[see[:, j], elem] += bad
+    got, status, _ = c.run(pp)
+    assert status == pp.PP_OK
+    fine = np.isfinite(hit)
+    assert fine.any() and not fine.all()
+    for h in range(heads):
+        assert (np.abs(got[:n, h] - want[:n, h]) <= tol[:n, h])[fine].all()
+        assert not np.isfinite(got[:n, h][~fine]).any()
+        assert np.isnan(got[:n, h][np.isnan(hit)]).all()
+    assert (np.abs(got[n:] - want[n:]) <= tol[n:]).all()
+
+
+@pytest.mark.parametrize("heads", [1, 4])
+def test_a_non_finite_value_costs_no_pass_over_the_context(pp, heads):
+    """Rows that see a NaN of a drafted token, over a long context: at most 4 times the time without it."""
+    import torch
+    times = []
+    for bad in (0.0, np.nan):
+        c = Case([(40, 150000)], heads, 1, 128, 64, "bf16", mask="tree", seed=1, stale=0.0)
+        for j in range(150000, 150040):
+            c.v[c.pages[0, j // 64], j % 64, :, 0] = bad
+        cache, batch, q, mask, out = c.device(pp)
+        ws = pp.alloc_attn_workspace(cache)
+        best = 1e9
+        for _ in range(6):
+            a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            a.record()
+            pp.pp_tree_attention(cache, batch, q, mask, c.scale, out, ws)
+            b.record()
+            torch.cuda.synchronize()
+            best = min(best, a.elapsed_time(b))
+        times.append(best)
+        assert pp.pp_get_device_status(ws) == pp.PP_OK
+    assert torch.isnan(out[..., 0]).all() and torch.isfinite(out[..., 1:]).all()
+    assert times[1] <= 4 * times[0], times
