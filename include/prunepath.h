@@ -291,7 +291,10 @@ pp_status pp_moefy_permute(const pp_desc *desc, const int32_t *perm, const void 
    (strides in elements, multiples of 16 bytes; the same for k and v).  The
    strides give both usual orders of a page, [page_size][n_kv_heads][D] and
    [n_kv_heads][page_size][D].  What pages hold past a sequence's length may
-   be anything, NaN included. */
+   be anything, NaN included.  The calls that write (pp_kv_append,
+   pp_kv_commit) want entries apart: from the smallest stride up, pages,
+   tokens, heads and layers each step past all that the ones before span
+   (PP_ERR_INVALID_ARG; a dimension of one may carry any stride). */
 typedef struct pp_cache {
     int dtype;        /* pp_dtype of the pages and of q, k, v, out */
     int n_heads;      /* query heads, a multiple of n_kv_heads     */
@@ -414,7 +417,8 @@ pp_status pp_tree_attention(const pp_cache *cache, const pp_batch *batch, const 
    within the sequence's new tokens) move to the entries ctx_len[b],
    ctx_len[b] + 1, ..., and new_len[b] = ctx_len[b] + n_accept[b] (new_len may
    be NULL; it must not overlap the inputs).  cache gives the first layer's
-   pages; layer l's lie l * layer_stride elements further; n_layers >= 1.  A
+   pages; layer l's lie l * layer_stride elements further (not read for one
+   layer; 0 is refused for more); n_layers >= 1.  A
    path that is not ascending or leaves the sequence's new tokens, or
    n_accept outside [0, max_path], records PP_ERR_INVALID_ARG and leaves the
    sequence as it was (new_len[b] = ctx_len[b]).  One launch for all layers. */

@@ -474,7 +474,8 @@ def pp_tree_attention(cache, batch, q, mask, scale, out, ws, stream=None):
 
 
 def pp_kv_commit(cache, batch, path, n_accept, ws, new_len=None, n_layers=1, layer_stride=0, stream=None):
-    """Move the accepted path [n_seqs, max_path] of each tree behind its context, in every layer's cache."""
+    """Move the accepted path [n_seqs, max_path] of each tree behind its context, in every layer's cache (layer_stride:
+    elements from one layer's pages to the next one's, for more than one layer)."""
     n = batch.n_seqs
     if path.dim() != 2 or path.shape[0] != n or n_accept.numel() != n or \
             (new_len is not None and new_len.numel() != n):

@@ -1,5 +1,6 @@
 // C ABI of the attention side: argument checks, workspace layout, dispatch.
 // Nothing here allocates, synchronises or lets an exception out.
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <cstring>
@@ -70,6 +71,25 @@ pp_status check_cache(const pp_cache* c) {
     }
     if (!aligned(c->k, 16) || !aligned(c->v, 16)) return PP_ERR_ALIGN;
     return PP_OK;
+}
+
+// Whether no two entries (page, offset, head, layer) of a cache that is to be
+// written share memory.  Taken from the smallest stride up, each dimension has
+// to step past all that the ones before it span, as in any dense array and its
+// parts, whatever the order of its dimensions.
+bool entries_apart(const pp_cache& c, int n_layers, int64_t layer_stride) {
+    struct Dim {
+        int64_t n, stride;
+    } dims[4] = {{c.n_pages, c.page_stride}, {c.page_size, c.token_stride}, {c.n_kv_heads, c.head_stride},
+                 {n_layers, layer_stride}};
+    std::sort(dims, dims + 4, [](const Dim& x, const Dim& y) { return x.stride < y.stride; });
+    __int128 span = c.head_dim;  // 2^31 strides of 2^40
+    for (const Dim& d : dims) {
+        if (d.n == 1) continue;
+        if (d.stride < span) return false;
+        span += (__int128)d.stride * (d.n - 1);
+    }
+    return true;
 }
 
 pp_status check_batch(const pp_batch* b, const pp_cache* c) {
@@ -230,6 +250,7 @@ pp_status pp_kv_append(const pp_cache* cache, const pp_batch* batch, const pp_ro
                        const void* v, int64_t v_stride, void* q_out, int64_t q_out_stride, void* ws,
                        size_t ws_bytes, void* stream) {
     PP_TRY(check_cache(cache));
+    if (!entries_apart(*cache, 1, 0)) return PP_ERR_INVALID_ARG;
     PP_TRY(check_batch(batch, cache));
     if (rot) PP_TRY(check_rotation(rot, cache->head_dim));
     const int e = elem_size(cache->dtype), D = cache->head_dim, T = batch->n_tokens;
@@ -331,6 +352,7 @@ pp_status pp_kv_commit(const pp_cache* cache, const pp_batch* batch, int n_layer
         if (layer_stride < 0 || layer_stride > (int64_t)1 << 40) return PP_ERR_INVALID_ARG;
         if (layer_stride * e % 16 != 0) return PP_ERR_ALIGN;
     }
+    if (!entries_apart(*cache, n_layers, layer_stride)) return PP_ERR_INVALID_ARG;
     if (!path || !n_accept) return PP_ERR_INVALID_ARG;
     if (!aligned(path, 4) || !aligned(n_accept, 4) || !aligned(new_len, 4)) return PP_ERR_ALIGN;
     const int B = batch->n_seqs;
