@@ -92,15 +92,20 @@ bool entries_apart(const pp_cache& c, int n_layers, int64_t layer_stride) {
     return true;
 }
 
+pp_status check_batch_pointers(const pp_batch* b) {
+    if (!b->q_start || !b->ctx_len || !b->pages) return PP_ERR_INVALID_ARG;
+    if (!aligned(b->q_start, 4) || !aligned(b->ctx_len, 4) || !aligned(b->pages, 4)) return PP_ERR_ALIGN;
+    return PP_OK;
+}
+
+// The pointers of a batch of no tokens are looked at by the one call that reads it all the same (pp_kv_commit).
 pp_status check_batch(const pp_batch* b, const pp_cache* c) {
     if (!b) return PP_ERR_INVALID_ARG;
     if (b->n_seqs < 0 || b->n_tokens < 0 || b->max_pages < 0) return PP_ERR_SHAPE;
     // query rows are numbered in 32 bits
     if ((long long)b->n_tokens * c->n_heads > 0x7fffffffll) return PP_ERR_SHAPE;
     if (b->n_seqs == 0 || b->n_tokens == 0) return PP_OK;
-    if (!b->q_start || !b->ctx_len || !b->pages) return PP_ERR_INVALID_ARG;
-    if (!aligned(b->q_start, 4) || !aligned(b->ctx_len, 4) || !aligned(b->pages, 4)) return PP_ERR_ALIGN;
-    return PP_OK;
+    return check_batch_pointers(b);
 }
 
 // A token tensor's rows (of no tokens: not looked at).
@@ -356,6 +361,7 @@ pp_status pp_kv_commit(const pp_cache* cache, const pp_batch* batch, int n_layer
     if (!path || !n_accept) return PP_ERR_INVALID_ARG;
     if (!aligned(path, 4) || !aligned(n_accept, 4) || !aligned(new_len, 4)) return PP_ERR_ALIGN;
     const int B = batch->n_seqs;
+    if (B > 0) PP_TRY(check_batch_pointers(batch));
     if (new_len) {
         auto over = [&](const void* p, int64_t bytes) { return rows_overlap(new_len, 4ll * B, 4ll * B, p, bytes, bytes, B ? 1 : 0); };
         if (over(batch->ctx_len, 4ll * B) || over(n_accept, 4ll * B) || over(path, 4ll * B * max_path) ||
@@ -367,7 +373,6 @@ pp_status pp_kv_commit(const pp_cache* cache, const pp_batch* batch, int n_layer
     int sms = 0;
     PP_TRY(device_sms(&sms));
     if (B == 0) return PP_OK;
-    if (!batch->q_start || !batch->ctx_len || !batch->pages) return PP_ERR_INVALID_ARG;
     CommitArgs a;
     std::memset(&a, 0, sizeof a);
     a.batch = batch_args(*batch, *cache);

@@ -45,3 +45,11 @@ def test_reading_entries_that_share_memory_is_allowed(lib):  # noqa: F811
     """Attention over one key head under several heads' names."""
     from test_attn_abi import attend
     assert accepted(attend(lib, c=cache(head_stride=0)))
+
+
+@pytest.mark.parametrize("kw,want", [(dict(q_start=0), pp.PP_ERR_INVALID_ARG), (dict(ctx_len=0), pp.PP_ERR_INVALID_ARG),
+                                     (dict(pages=0), pp.PP_ERR_INVALID_ARG), (dict(q_start=A + 2), pp.PP_ERR_ALIGN),
+                                     (dict(ctx_len=A + 1), pp.PP_ERR_ALIGN), (dict(pages=A + 2), pp.PP_ERR_ALIGN)])
+def test_commit_checks_its_pointers_when_no_token_is_new(lib, kw, want):  # noqa: F811
+    """A commit of no new tokens still runs (it writes new_len), so it reads the batch."""
+    assert commit(lib, b=batch(n_tokens=0, **kw)) == want
