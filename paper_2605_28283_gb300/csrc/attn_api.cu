@@ -358,9 +358,9 @@ pp_status pp_kv_commit(const pp_cache* cache, const pp_batch* batch, int n_layer
         if (layer_stride * e % 16 != 0) return PP_ERR_ALIGN;
     }
     if (!entries_apart(*cache, n_layers, layer_stride)) return PP_ERR_INVALID_ARG;
-    if (!path || !n_accept) return PP_ERR_INVALID_ARG;
-    if (!aligned(path, 4) || !aligned(n_accept, 4) || !aligned(new_len, 4)) return PP_ERR_ALIGN;
     const int B = batch->n_seqs;
+    if (B > 0 && (!n_accept || (!path && max_path > 0))) return PP_ERR_INVALID_ARG;
+    if (!aligned(path, 4) || !aligned(n_accept, 4) || !aligned(new_len, 4)) return PP_ERR_ALIGN;
     if (B > 0) PP_TRY(check_batch_pointers(batch));
     if (new_len) {
         auto over = [&](const void* p, int64_t bytes) { return rows_overlap(new_len, 4ll * B, 4ll * B, p, bytes, bytes, B ? 1 : 0); };

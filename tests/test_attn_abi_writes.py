@@ -53,3 +53,28 @@ def test_reading_entries_that_share_memory_is_allowed(lib):  # noqa: F811
 def test_commit_checks_its_pointers_when_no_token_is_new(lib, kw, want):  # noqa: F811
     """A commit of no new tokens still runs (it writes new_len), so it reads the batch."""
     assert commit(lib, b=batch(n_tokens=0, **kw)) == want
+
+
+@needs_no_gpu
+def test_commit_of_nothing_needs_no_path(lib):  # noqa: F811
+    """Paths of length zero, and no sequences: tensors without elements have no address."""
+    assert accepted(commit(lib, path=None, mp=0))
+    assert accepted(commit(lib, b=batch(n_seqs=0, q_start=0, ctx_len=0, pages=0), path=None, acc=None))
+    assert commit(lib, path=None, mp=1) == pp.PP_ERR_INVALID_ARG
+    assert commit(lib, path=None, mp=0, acc=None) == pp.PP_ERR_INVALID_ARG
+
+
+@pytest.mark.gpu
+def test_commit_of_nothing_on_the_gpu():
+    import torch
+    ints = lambda *shape, fill=0: torch.full(shape, fill, dtype=torch.int32, device="cuda")  # noqa: E731
+    k = torch.randn(4, 16, 2, 64, device="cuda")
+    c = pp.KVCache(k.clone(), k.clone(), 2)
+    ws = pp.alloc_attn_workspace(c)
+    b = pp.Batch(torch.tensor([0, 3, 3], dtype=torch.int32, device="cuda"), ints(2, fill=5), ints(2, 2), 3)
+    new_len = ints(2, fill=-1)
+    pp.pp_kv_commit(c, b, ints(2, 0), ints(2), ws, new_len=new_len)
+    assert new_len.tolist() == [5, 5] and torch.equal(c.k, k) and torch.equal(c.v, k)
+    none = pp.Batch(ints(1), ints(0), ints(0, 1), 0)
+    pp.pp_kv_commit(c, none, ints(0, 4), ints(0), ws, new_len=ints(0))
+    assert pp.pp_get_device_status(ws) == pp.PP_OK
