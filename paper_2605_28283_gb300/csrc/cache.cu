@@ -110,9 +110,7 @@ __global__ void __launch_bounds__(256) append_kernel(const AppendArgs a) {
             const int b = find_seq(a.batch, t, lane);
             const Seq s = load_seq(a.batch, b);
             const int i = t - s.q0;
-            if (s.bad) {
-                if (lane == 0 && t < a.batch.q_start[a.batch.n_seqs]) record_status(a.status, PP_ERR_INVALID_ARG);
-            } else if (i >= 0 && i < s.n) {
+            if (!s.bad && i >= 0 && i < s.n) {
                 const int page = entry_page(a.batch, b, s.ctx + i);
                 if (page >= 0)
                     dst = entry_offset(a.batch, a.cache, page, s.ctx + i);
@@ -127,6 +125,10 @@ __global__ void __launch_bounds__(256) append_kernel(const AppendArgs a) {
             pos_s = pos;
             dst_s = dst;
         }
+    } else if (tid == 32 && blockIdx.y == 0 && a.n_kv_heads) {
+        // every sequence is looked at once, also one that no token belongs to
+        for (int b = t; b < a.batch.n_seqs; b += gridDim.x)
+            if (load_seq(a.batch, b).bad) record_status(a.status, PP_ERR_INVALID_ARG);
     }
     bool ready = false;
     for (int u0 = blockIdx.y * blockDim.x + tid; u0 - tid < total; u0 += kAppendUnits * stride) {
