@@ -129,26 +129,25 @@ struct Item : Part {
 };
 constexpr int kItems = 8;
 
-// A reader of the ring, at tile t of part n.
+// A reader of the ring (a whole warp), at tile t of part n.
 template <int ROWS, int TOK>
 struct ItemAt {
     const Item<ROWS, TOK>* ring;
     uint64_t *full, *empty;
-    unsigned* status;
-    uint64_t lim;
+    Waits w;
     int n, t, t0, t1;
+    bool lost;  // the part did not come: nothing of item() may be used, and the part has no end
     PP_DEVINL const Item<ROWS, TOK>& item() const { return ring[n % kItems]; }
     PP_DEVINL void enter(int n_) {
         n = n_;
-        attn_wait(&full[n % kItems], (uint32_t)(n / kItems) & 1u, status, lim);
-        t = t0 = item().t0;
-        t1 = item().t1;
+        lost = __any_sync(kFull, !attn_wait(&full[n % kItems], (uint32_t)(n / kItems) & 1u, w));
+        t = t0 = lost ? 0 : item().t0;
+        t1 = lost ? 0x7fffffff : item().t1;
     }
-    // The next part, by a whole warp (lane) or one thread (-1).  `release`:
-    // this reader counts among those that free an entry.
+    // The next part.  `release`: this reader counts among those that free an entry.
     PP_DEVINL void next(int lane, bool release) {
-        if (lane >= 0) __syncwarp();
-        if (release && lane <= 0) mbar_arrive(&empty[n % kItems]);
+        __syncwarp();
+        if (release && lane == 0) mbar_arrive(&empty[n % kItems]);
         enter(n + 1);
     }
     // k tiles further (the caller stays inside the stretch); true in another part
@@ -339,8 +338,9 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
     __shared__ Item<ROWS, BN> items[kItems];
     __shared__ uint64_t ifull[kItems], isplit[kItems], iempty[kItems], stretch;
     __shared__ int tiles_s;
+    __shared__ unsigned lost_s;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const uint64_t lim = a.timeout_ns;
+    const Waits w{a.status, a.timeout_ns, &lost_s};
     pdl_launch_dependents();
     if (tid == 0) {
         for (int i = 0; i < NS; i++) {
@@ -363,6 +363,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
             mbar_init(&iempty[i], C::kReaders);
         }
         mbar_init(&stretch, 1);
+        lost_s = 0u;
         fence_mbar_init();
     }
     if (warp == C::kWarpMma) {
@@ -379,11 +380,17 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
     tc_fence_after();
     const uint32_t tmem = taddr_s;
     pdl_wait();
-    ItemAt<ROWS, BN> at{items, ifull, iempty, a.status, lim, 0, 0, 0, 0};
+    // A wait that gives up ends the CTA's work, its results lost: the scheduling
+    // warp hands out no further part (nor overwrites one that others read), the
+    // warps that load stop, those that issue products run through their tiles on
+    // what lies there, and the softmax warps of a row tile, which meet in
+    // barriers, agree before each part whether to go on.
+    ItemAt<ROWS, BN> at{items, ifull, iempty, w, 0, 0, 0, 0, false};
     int tiles = 0;  // of this CTA
     if (warp < C::kWarps - 1) {
-        attn_wait(&stretch, 0, a.status, lim);
-        tiles = tiles_s;
+        bool lost = !attn_wait(&stretch, 0, w);
+        lost = warp < C::kSoftWarps ? named_bar_or(2 + (warp >> 2), 128, lost) : __any_sync(kFull, lost);
+        if (!lost) tiles = tiles_s;
     }
 
     if (warp == C::kWarps - 1) {
@@ -398,7 +405,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
             Part p;
             for (int n = 0; walk.next(p); n++) {
                 Item<ROWS, BN>& it = items[n % kItems];
-                if (n >= kItems) attn_wait(&iempty[n % kItems], (uint32_t)(n / kItems - 1) & 1u, a.status, lim);
+                if (n >= kItems && !attn_wait(&iempty[n % kItems], (uint32_t)(n / kItems - 1) & 1u, w)) break;
                 static_cast<Part&>(it) = p;
                 it.rows = min(ROWS, p.seq.n * a.group - p.j * ROWS);
                 it.open = all_see<ROWS>(a, p);
@@ -434,6 +441,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
             const int g = MT == 1 ? (pos == 0 ? 0 : key ? (pos + 1) / 2 : (pos - 2) / 2) : pos / 2;
             if (g >= tiles) break;
             at.step(g - g_at, lane, true);
+            if (at.lost) break;
             g_at = g;
             const Item<ROWS, BN>& p = at.item();
             const int k0 = at.t * BN;
@@ -457,13 +465,13 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                         page = a.batch.n_pages;
                     }
                 }
-                if (uses > 0) attn_wait(&empty[slot], (uint32_t)(uses - 1) & 1u, a.status, lim);
+                if (__any_sync(kFull, uses > 0 && !attn_wait(&empty[slot], (uint32_t)(uses - 1) & 1u, w))) break;
                 if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(boxes * a.box * 128));
                 __syncwarp();
                 if (lane < boxes)
                     tma_load_4d(dst + grp * BN * 128 + row * 128, key ? &map_k : &map_v, grp * 64, p.h, in_page, page, bar);
                 if (fix) {
-                    attn_wait(bar, (uint32_t)fixes++ & 1u, a.status, lim);
+                    if (__any_sync(kFull, !attn_wait(bar, (uint32_t)fixes++ & 1u, w))) break;
                     finite_rows<DP, BN>(dst, open, end, lane, k0, &it.odd0, &it.odd1);
                     zero_rows<DP, BN>(dst, end, BN, lane);
                     fence_proxy_async_smem();
@@ -471,8 +479,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                     if (lane == 0) mbar_arrive(&full[slot]);
                 }
             } else {
-                if (uses > 0) attn_wait(&empty[slot], (uint32_t)(uses - 1) & 1u, a.status, lim);
-                __syncwarp();
+                if (__any_sync(kFull, uses > 0 && !attn_wait(&empty[slot], (uint32_t)(uses - 1) & 1u, w))) break;
 #pragma unroll 1
                 for (int x = 0; x < BN; x += 32) {
                     const int j = k0 + x + lane;
@@ -498,14 +505,16 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
     } else if (warp == C::kWarpQ) {
         // --------------------------------------------------------- rows of q
         at.enter(0);
-        for (int left = tiles;;) {
+        bool lost = at.lost;
+        for (int left = tiles; !lost;) {
             const Item<ROWS, BN>& p = at.item();
             const int rows = p.rows, n = at.n;
 #pragma unroll 1
             for (int m = 0; m < MT; m++) {
                 const int buf = MT == 2 ? m : n % C::kQBufs, use = MT == 2 ? n : n / C::kQBufs;
                 const bool few = MT == 1 && rows <= 32;
-                if (use > 0) attn_wait(&qempty[buf], (uint32_t)(use - 1) & 1u, a.status, lim);
+                lost = __any_sync(kFull, use > 0 && !attn_wait(&qempty[buf], (uint32_t)(use - 1) & 1u, w));
+                if (lost) break;
                 if (a.q_box) {
                     // boxes of 32 rows; past the item's rows they hold other tokens' (rows that nobody reads)
                     if (lane == 0) mbar_arrive_expect_tx(&qfull[buf], C::kQTile);
@@ -533,8 +542,9 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                 if (lane == 0) mbar_arrive(&qfull[buf]);
             }
             left -= at.t1 - at.t0;
-            if (left <= 0) break;
+            if (lost || left <= 0) break;
             at.next(lane, true);
+            lost = at.lost;
         }
     } else if (warp >= C::kWarpMma) {
         // ---------------------------------------------------------- products
@@ -554,9 +564,9 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
         auto k_pos = [&](int g) { return MT == 1 ? (g == 0 ? 0 : 2 * g - 1) : 2 * g; };
         auto v_pos = [&](int g) { return MT == 1 ? 2 * g + 2 : 2 * g + 1; };
         auto s_slot = [&](int g) { return MT == 1 ? g & 1 : m; };
-        auto wait_full = [&](int pos) { attn_wait(&full[pos % NS], (uint32_t)(pos / NS) & 1u, a.status, lim); };
+        auto wait_full = [&](int pos) { attn_wait(&full[pos % NS], (uint32_t)(pos / NS) & 1u, w); };
         auto q_buf = [&]() { return MT == 2 ? m : cs.n % C::kQBufs; };
-        auto wait_q = [&]() { attn_wait(&qfull[q_buf()], (uint32_t)(MT == 2 ? cs.n : cs.n / C::kQBufs) & 1u, a.status, lim); };
+        auto wait_q = [&]() { attn_wait(&qfull[q_buf()], (uint32_t)(MT == 2 ? cs.n : cs.n / C::kQBufs) & 1u, w); };
         auto issue_scores = [&](int g) {
             const unsigned char* kt = ring + (k_pos(g) % NS) * C::kSlot;
             const unsigned char* qt = qs + q_buf() * C::kQTile;
@@ -589,11 +599,11 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                 const bool fresh = more && cs.t == cs.t0;  // its queries may still be on their way: values do not wait for them
                 if (v) wait_full(v_pos(g));
                 if (sc && !fresh) wait_full(k_pos(g + 1));
-                if (v) attn_wait(&pfull[m], n_o++ & 1u, a.status, lim);
+                if (v) attn_wait(&pfull[m], n_o++ & 1u, w);
                 // the row tiles take turns: products of both at once would end at once, and then both softmaxes
                 // run at once with the tensor cores idle
                 // (the first after the second's last burst, the second after the first's of the same tile)
-                if (g + m >= 0) attn_wait(&turn[m], (uint32_t)(g + m) & 1u, a.status, lim);
+                if (g + m >= 0) attn_wait(&turn[m], (uint32_t)(g + m) & 1u, w);
                 tc_fence_after();
                 if (one && v) issue_values(g);
                 if (fresh) {
@@ -617,7 +627,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                 if (cs.t == cs.t0) wait_q();
                 wait_full(k_pos(g));
                 // the slot's last weights have been multiplied
-                if (g >= 2) attn_wait(&odone[g & 1], (uint32_t)((g - 2) >> 1) & 1u, a.status, lim);
+                if (g >= 2) attn_wait(&odone[g & 1], (uint32_t)((g - 2) >> 1) & 1u, w);
                 tc_fence_after();
                 if (one) {
                     issue_scores(g);
@@ -630,7 +640,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
 #pragma unroll 1
             for (int g = 0; g < tiles; g++) {
                 wait_full(v_pos(g));
-                attn_wait(&pfull[g & 1], (uint32_t)(g >> 1) & 1u, a.status, lim);
+                attn_wait(&pfull[g & 1], (uint32_t)(g >> 1) & 1u, w);
                 tc_fence_after();
                 if (one) {
                     issue_values(g);
@@ -649,11 +659,11 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
         // O holds the products up to tile x of this row tile (barriers take turns, so that a parity cannot stand
         // for the last phase but one)
         auto products_done = [&](int x) {
-            attn_wait(&odone[2 * m + (x & 1)], (uint32_t)(x >> 1) & 1u, a.status, lim);
+            attn_wait(&odone[2 * m + (x & 1)], (uint32_t)(x >> 1) & 1u, w);
             tc_fence_after();
         };
         at.enter(0);
-        for (int left = tiles;;) {
+        for (int left = tiles; !named_bar_or(2 + m, 128, at.lost);) {
             const Item<ROWS, BN>& p = at.item();
             const int rows = p.rows;
             const bool few = MT == 1 && rows <= 32;
@@ -692,7 +702,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
                 const int sl = MT == 1 ? g & 1 : m;
                 const uint32_t par = (uint32_t)(MT == 1 ? g >> 1 : g) & 1u;
                 const uint32_t t_s = tmem + (uint32_t)(sl * BN) + lanes;
-                attn_wait(&sfull[sl], par, a.status, lim);
+                attn_wait(&sfull[sl], par, w);
                 tc_fence_after();
                 if (active) {
                     const int k0 = t * BN;
@@ -743,7 +753,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
             const Split<ROWS, BN>& sp = p.split;
             float* place = nullptr;
             if (!whole) {
-                attn_wait(&isplit[at.n % kItems], (uint32_t)(at.n / kItems) & 1u, a.status, lim);
+                attn_wait(&isplit[at.n % kItems], (uint32_t)(at.n / kItems) & 1u, w);
                 place = sp.place(a, blockIdx.x);
             }
             const int D = a.head_dim;
@@ -868,7 +878,8 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
             tc_fence_before();
             if (!whole && !a.join_later) {
                 named_bar_sync(1, 32 * C::kSoftWarps);
-                if (tid == 0) last_s = arrive_last(a.counters + sp.c0, (unsigned)(sp.c1 - sp.c0 + 1));
+                // (a part whose split did not come has set lost_s before the barrier)
+                if (tid == 0) last_s = !*w.lost && arrive_last(a.counters + sp.c0, (unsigned)(sp.c1 - sp.c0 + 1));
                 named_bar_sync(1, 32 * C::kSoftWarps);
                 if (last_s) {
                     if (few)
@@ -883,6 +894,8 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
             at.next(lane, true);
         }
     }
+    if (*w.lost)  // copies and products that may still be on their way: 1 ms is a hundred times what they take
+        for (const uint64_t t0 = globaltimer_ns(); globaltimer_ns() - t0 < 1000000ull;) __nanosleep(10000);
     tc_fence_before();
     __syncthreads();
     if (warp == C::kWarpMma) {

@@ -77,25 +77,49 @@ PP_DEVINL void prefetch_map(const CUtensorMap* map) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
 }
 
-// Wait for a barrier's phase, for at most limit_ns.  On expiry PP_ERR_TIMEOUT
-// is recorded, over an earlier code: the call's results are lost.  Waits that
-// have lasted over 1 ms give up once that is recorded, and only then: a bad
-// page or length recorded by this call or an earlier one leaves the other
-// sequences to be computed, and a wait of several ms is regular (the rows of q
-// wait for a whole item: 1 ms at 64 thousand entries).
-static __device__ __noinline__ void attn_wait_slow(uint64_t* bar, uint32_t parity, unsigned* status, uint64_t limit_ns) {
+// Wait for a barrier's phase, for at most limit_ns; false when it gave up.  On
+// expiry PP_ERR_TIMEOUT is recorded, over an earlier code: the call's results
+// are lost.  Waits that have lasted over 1 ms give up once that is recorded,
+// and only then: a bad page or length recorded by this call or an earlier one
+// leaves the other sequences to be computed, and a wait of several ms is
+// regular (the rows of q wait for a whole item: 1 ms at 64 thousand entries).
+// The first wait of a CTA that gives up sets *lost (shared memory), and the
+// CTA's other waits give up after one try each.
+struct Waits {
+    unsigned* status;
+    uint64_t limit_ns;
+    volatile unsigned* lost;
+};
+static __device__ __noinline__ bool attn_wait_slow(uint64_t* bar, uint32_t parity, Waits w) {
     const uint64_t t0 = globaltimer_ns();
     while (!mbar_try_wait(bar, parity)) {
+        if (*w.lost) return false;
         const uint64_t dt = globaltimer_ns() - t0;
-        if (dt > limit_ns) {
-            atomicExch(status, (unsigned)PP_ERR_TIMEOUT);
-            return;
+        const bool expired = dt > w.limit_ns;
+        if (expired) atomicExch(w.status, (unsigned)PP_ERR_TIMEOUT);
+        if (expired || (dt > 1000000ull && *reinterpret_cast<volatile unsigned*>(w.status) == PP_ERR_TIMEOUT)) {
+            *w.lost = 1u;
+            return false;
         }
-        if (dt > 1000000ull && *reinterpret_cast<volatile unsigned*>(status) == PP_ERR_TIMEOUT) return;
     }
+    return true;
 }
-PP_DEVINL void attn_wait(uint64_t* bar, uint32_t parity, unsigned* status, uint64_t limit_ns) {
-    if (!mbar_try_wait(bar, parity)) attn_wait_slow(bar, parity, status, limit_ns);
+PP_DEVINL bool attn_wait(uint64_t* bar, uint32_t parity, const Waits& w) {
+    return mbar_try_wait(bar, parity) || attn_wait_slow(bar, parity, w);
+}
+
+// Barrier over n threads of whole warps; true for all where any brings true.
+PP_DEVINL bool named_bar_or(int id, int n, bool any) {
+    unsigned r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.u32 q, %1, 0;\n\t"
+        "bar.red.or.pred p, %2, %3, q;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(r)
+        : "r"(any ? 1u : 0u), "r"(id), "r"(n)
+        : "memory");
+    return r != 0u;
 }
 
 // 2^x, flushing subnormals (softmax weights below 2^-126 count as zero).

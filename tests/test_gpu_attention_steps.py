@@ -226,3 +226,40 @@ def test_a_non_finite_value_costs_no_pass_over_the_context(pp, heads):
         assert pp.pp_get_device_status(ws) == pp.PP_OK
     assert torch.isnan(out[..., 0]).all() and torch.isfinite(out[..., 1:]).all()
     assert times[1] <= 4 * times[0], times
+
+
+@pytest.mark.parametrize("n,heads", [(300, 152), (20, 456)])
+def test_waits_that_give_up_end_the_call(pp, n, heads):
+    """Waits over 1 ms give up on a workspace that has a timeout recorded: the call returns with that status, writes
+    nothing beside its output, and leaves the GPU usable; on the workspace initialised anew it comes out right."""
+    import torch
+    D, page, uniq, times = 8, 128, 512, 1024
+    ctx = uniq * times
+    g = torch.Generator(device="cuda").manual_seed(1)
+    k, v = (torch.randn((uniq // page + 3, page, heads, D), generator=g, device="cuda").bfloat16() for _ in range(2))
+    q = torch.randn((n, heads, D), generator=g, device="cuda").bfloat16()
+    table = torch.cat([torch.arange(uniq // page).repeat(times), uniq // page + torch.arange(3)]).int()[None].cuda()
+    cache = pp.KVCache(k, v, heads)
+    batch = pp.Batch(torch.tensor([0, n], dtype=torch.int32, device="cuda"),
+                     torch.tensor([ctx], dtype=torch.int32, device="cuda"), table, n)
+    ws = pp.alloc_attn_workspace(cache)
+    out = Guarded((n, heads, D), torch.bfloat16)
+    pp.pp_debug_wait_timeout(ws, 1000)
+    pp.pp_tree_attention(cache, batch, q, None, D ** -0.5, out.t, ws)
+    assert pp.pp_get_device_status(ws) == pp.PP_ERR_TIMEOUT
+    assert out.bands_intact()
+    pp.pp_workspace_init(ws)
+    pp.pp_tree_attention(cache, batch, q, None, D ** -0.5, out.t, ws)
+    assert pp.pp_get_device_status(ws) == pp.PP_OK and out.bands_intact()
+    fresh = torch.empty_like(out.t)
+    pp.pp_tree_attention(cache, batch, q, None, D ** -0.5, fresh, pp.alloc_attn_workspace(cache))
+    assert torch.equal(out.t, fresh) and torch.isfinite(fresh).all()
+    # every cached entry counts `times` times; the first head in fp64
+    kk, vv = (a.reshape(-1, heads, D)[:uniq + n, 0].double() for a in (k, v))
+    s = q[:, 0].double() @ kk.T * D ** -0.5
+    s[:, uniq:].masked_fill_(torch.ones((n, n), dtype=torch.bool, device="cuda").triu(1), float("-inf"))
+    p = torch.softmax(s + torch.cat([torch.full((uniq,), np.log(times)), torch.zeros(n)]).cuda().double(), -1)
+    want, a = p @ vv, p @ vv.abs()
+    # two roundings to bf16 of the weights and one of the output, sums of ctx + n terms (attn_ref.attend's bound)
+    rel = 3 * ref.BF16_HALF_ULP + 2.0 ** -20 + 2 * ref.F32_HALF_ULP * ((ctx + n) / 32 + 32) + 1e-4
+    assert ((fresh[:, 0].double() - want).abs() <= rel * a).all()
