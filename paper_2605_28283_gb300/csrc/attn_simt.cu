@@ -19,7 +19,14 @@ namespace pp {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kLeastTiles = 2;  // a stretch's key tiles: 1 took 22.5 us, 2 18.7, 3 22.9 for 3 drafted trees over 100 to 1000 entries
+// A stretch's key tiles.  A tile takes 2 to 4 us and every further part of an
+// item a join, and stretches that do not divide the items' tiles cut more of
+// them, so no number is best everywhere.  1 / 2 / 3 tiles, 16 heads of 64: one
+// token over 400 entries 10.0 / 12.4 / 14.3 us, 3 tokens over 400 16.2 / 13.6 /
+// 15.5, 3 over 1000 21.7 / 21.6 / 17.5; 13 tokens over 400 12.1 / 16.3 / 18.9, 3
+// times 13 over 400 20.5 / 18.2 / 21.0, over 1000 31.2 / 30.8 / 24.1, 3 trees of 9
+// to 13 over 100 to 1000 23.3 / 19.2 / 23.6; alike from about 4000 entries on.
+constexpr int kLeastTiles = 2;
 
 // Rows of a tile, keys of a tile, padded head dimension.
 template <int ROWS, int TOK, int DP>
@@ -254,6 +261,9 @@ size_t attn_part_floats(int head_dim) {
 cudaError_t attn_simt_launch(const AttnArgs& a, int sms, cudaStream_t st) {
     // rows a sequence brings to a key head on average: small tiles spread
     // their threads over keys and elements instead of rows that do not exist
+    // (tiles of 16 / 4 rows, 3 sequences over 100 to 1000 entries: 4 rows 19.2 /
+    // 14.9 us for 16 heads of 64, 44.0 / 36.9 for 32 of 128; 5 rows 19.0 / 23.5,
+    // 44.0 / 49.5)
     const long long rows = ((long long)a.batch.n_tokens * a.group + a.batch.n_seqs - 1) / a.batch.n_seqs;
     const bool few = rows <= 4;
     if (a.head_dim <= 64) return few ? go<4, 64, 64>(a, sms, st) : go<16, 64, 64>(a, sms, st);

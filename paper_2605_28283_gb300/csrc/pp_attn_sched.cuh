@@ -55,9 +55,12 @@ struct Sched {
     long long each;
     int longer;
     // Short stretches: as few CTAs as finish with the longest of them, and
-    // `least` tiles each, since every part of a split item costs (one token
-    // over 1024 entries of 32 key heads: 12.5 -> 12.1 us).  Long ones: all
-    // CTAs (8 drafted trees, 16 tiles a CTA: 45.6 us against 48.2).
+    // `least` tiles each, since every part of a split item costs.  Long ones:
+    // all CTAs.  "Short" as up to 1 / 4 / 16 tiles, bf16: one token over 2048
+    // entries of 32 key heads 16.2 / 13.5 / 13.5 us, two trees of 32 tokens over
+    // 4000 (8 key heads) 21.0 / 18.6 / 18.5, 8 trees of 32 over 500 to 6000 35.1 /
+    // 35.3 / 37.5; fp32: one token over 1024 22.8 / 16.3 / 16.3, over 2048 35.4 /
+    // 40.8 / 40.5, over 4096 56.4 / 57.1 / 61.2.
     PP_DEVINL void deal(long long total_, int grid, int least) {
         total = total_;
         const long long longest = max(quotient(total + grid - 1, grid), (long long)least);
