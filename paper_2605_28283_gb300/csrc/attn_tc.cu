@@ -25,11 +25,11 @@
 // More than 128 rows on average (MT = 2): two row tiles share each key tile.
 //
 // Measured (GB300): one token for each of 64 ragged sequences of 64 to 8191
-// entries, 32 heads on 8 key heads of 128: 170 us, 6.3 TB/s (0.94 of the copy
-// rate), bound by HBM.  One token over 1024 entries: 11.5 us, a chain of
-// latencies.  8 drafted trees of 17 to 48 tokens over 500 to 6000 entries: 42
+// entries, 32 heads on 8 key heads of 128: 168 us, 6.4 TB/s (0.94 of the copy
+// rate), bound by HBM.  One token over 1024 entries: 11.8 us, a chain of
+// latencies.  8 drafted trees of 17 to 48 tokens over 500 to 6000 entries: 43
 // us, bound by the softmax warps and the ends of parts.  4 prompts of 2048
-// tokens, 40 heads of 128: 196 us, 879 TFLOP/s (0.46 of the bf16 rate), the
+// tokens, 40 heads of 128: 196 us, 877 TFLOP/s (0.46 of the bf16 rate), the
 // row tiles' softmaxes and products in turns.  The code is long for its cache:
 // loops stay rolled unless straight-line code was measured to be faster.
 #include "pp_attn_sched.cuh"
