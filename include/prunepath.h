@@ -372,6 +372,43 @@ pp_status pp_rope(int dtype, const pp_rotation *rot, const int32_t *positions, i
                   int head_dim, const void *x, int64_t x_stride, void *y, int64_t y_stride, int inverse,
                   void *stream);
 
+/* Norm of each query and key head ahead of its rotation: a head's row x
+   becomes x / sqrt(mean(x^2) + eps) * gamma, with one weight vector for all
+   query heads and one for all key heads.  Squares are summed in fp32. */
+typedef struct pp_head_norm {
+    float eps;            /* >= 0                                              */
+    const void *q_gamma;  /* [head_dim] device, in the tensors' dtype; NULL: ones */
+    const void *k_gamma;
+} pp_head_norm;
+
+/* q_out, k_out = q, k normed and then rotated by their tokens' positions, in
+   one pass: q [n_tokens][n_heads][head_dim], k [n_tokens][n_kv_heads][head_dim]
+   (n_kv_heads 0: no keys, any n_heads; k, k_out are not looked at).  rot NULL:
+   no rotation, and positions are not looked at.  An output may be its own
+   input with the same stride; other overlaps are PP_ERR_INVALID_ARG.
+   Arithmetic in fp32, rounded once at the end. */
+pp_status pp_head_norm_rope(int dtype, const pp_head_norm *norm, const pp_rotation *rot, const int32_t *positions,
+                            int n_tokens, int n_heads, int n_kv_heads, int head_dim, const void *q, int64_t q_stride,
+                            const void *k, int64_t k_stride, void *q_out, int64_t q_out_stride, void *k_out,
+                            int64_t k_out_stride, void *stream);
+
+/* Backward pass of pp_head_norm_rope: from q, k as they went in and the
+   gradients q_grad, k_grad of its outputs, the gradients dq, dk of q, k and
+   (each unless NULL; written, not added to) dq_gamma, dk_gamma [head_dim] fp32
+   of the weights, summed in fp32 over all tokens and heads in a fixed order.
+   dq may be q_grad (or q) itself with the same stride, dk likewise.
+   Workspace: pp_head_norm_workspace_size bytes, 256-byte aligned; it need not
+   be initialised, and is not looked at where no weight gradient is asked for. */
+pp_status pp_head_norm_rope_grad(int dtype, const pp_head_norm *norm, const pp_rotation *rot, const int32_t *positions,
+                                 int n_tokens, int n_heads, int n_kv_heads, int head_dim, const void *q,
+                                 int64_t q_stride, const void *k, int64_t k_stride, const void *q_grad,
+                                 int64_t q_grad_stride, const void *k_grad, int64_t k_grad_stride, void *dq,
+                                 int64_t dq_stride, void *dk, int64_t dk_stride, float *dq_gamma, float *dk_gamma,
+                                 void *ws, size_t ws_bytes, void *stream);
+
+/* Workspace bytes of pp_head_norm_rope_grad (0 for an unsupported head_dim). */
+size_t pp_head_norm_workspace_size(int head_dim);
+
 /* Workspace bytes of pp_kv_append, pp_tree_attention and pp_kv_commit for
    this cache, whatever the batch (0 for an unsupported one).  Initialise it
    with pp_workspace_init; errors found on the device are read with

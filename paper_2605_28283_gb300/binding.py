@@ -59,6 +59,10 @@ class pp_rotation(ctypes.Structure):
                 ("inv_freq", ctypes.c_void_p)]
 
 
+class pp_head_norm(ctypes.Structure):
+    _fields_ = [("eps", ctypes.c_float), ("q_gamma", ctypes.c_void_p), ("k_gamma", ctypes.c_void_p)]
+
+
 class PPError(RuntimeError):
     def __init__(self, status, what):
         super().__init__("%s failed: %s" % (what, status_name(status)))
@@ -71,6 +75,7 @@ _PD = ctypes.POINTER(pp_desc)
 _PS = ctypes.POINTER(pp_selection)
 _D = ctypes.c_double
 _PC, _PB, _PR = ctypes.POINTER(pp_cache), ctypes.POINTER(pp_batch), ctypes.POINTER(pp_rotation)
+_PN = ctypes.POINTER(pp_head_norm)
 
 EXPORTS = {
     "pp_workspace_size": (_Z, [_PD, _I]),
@@ -87,6 +92,10 @@ EXPORTS = {
     "pp_moefy_permute": (_I, [_PD, _P, _P, _P, _P, _P, _P, _P, _P, _Z, _P]),
     "pp_rope_frequencies": (_I, [_I, _I, _D, _D, _D, _D, _I, _P, _P]),
     "pp_rope": (_I, [_I, _PR, _P, _I, _I, _I, _P, _LL, _P, _LL, _I, _P]),
+    "pp_head_norm_rope": (_I, [_I, _PN, _PR, _P, _I, _I, _I, _I, _P, _LL, _P, _LL, _P, _LL, _P, _LL, _P]),
+    "pp_head_norm_rope_grad": (_I, [_I, _PN, _PR, _P, _I, _I, _I, _I, _P, _LL, _P, _LL, _P, _LL, _P, _LL, _P, _LL, _P, _LL,
+                                    _P, _P, _P, _Z, _P]),
+    "pp_head_norm_workspace_size": (_Z, [_I]),
     "pp_attn_workspace_size": (_Z, [_PC]),
     "pp_kv_append": (_I, [_PC, _PB, _PR, _P, _P, _LL, _P, _LL, _P, _LL, _P, _LL, _P, _Z, _P]),
     "pp_tree_attention": (_I, [_PC, _PB, _P, _LL, _P, _I, _F, _P, _LL, _P, _Z, _P]),
@@ -368,6 +377,31 @@ class Rotation:
         return cls(torch.from_numpy(freq).to(device), layout, scale)
 
 
+class HeadNorm:
+    """Norm of query and key heads: weights [head_dim] in the heads' dtype (None: ones), eps."""
+
+    def __init__(self, q_gamma=None, k_gamma=None, eps=1e-6):
+        _torch_types()
+        for g in (q_gamma, k_gamma):
+            if g is not None and (g.dim() != 1 or not g.is_contiguous()):
+                raise PPError(PP_ERR_SHAPE, "HeadNorm: a weight vector is contiguous [head_dim]")
+            if g is not None:
+                _torch_dtype(g.dtype)
+        self.q_gamma, self.k_gamma = q_gamma, k_gamma
+        self.c = pp_head_norm(float(eps), None if q_gamma is None else q_gamma.data_ptr(),
+                              None if k_gamma is None else k_gamma.data_ptr())
+        self.ref = ctypes.byref(self.c)
+        # (dtype, head_dim) of each weight vector, for the calls to compare with
+        self.kinds = [(g.dtype, g.shape[0]) for g in (q_gamma, k_gamma) if g is not None]
+
+    def check(self, dtype, head_dim, what):
+        for kind in self.kinds:
+            if kind[0] != dtype:
+                raise PPError(PP_ERR_DTYPE, what + ": weights of another type")
+            if kind[1] != head_dim:
+                raise PPError(PP_ERR_SHAPE, what + ": weights of another head_dim")
+
+
 class KVCache:
     """A layer's key and value pages: k, v [n_pages, page_size, n_kv_heads, head_dim] of any strides (the same for
     both) with contiguous head_dim.  Pages stored head by head are passed as their transposed view."""
@@ -426,6 +460,83 @@ def pp_rope(rot, positions, x, y, inverse=False, stream=None):
     py, sy = _rows(y, T, H, D, dt, "pp_rope: y")
     _check(load().pp_rope(_torch_dtype(dt), rot.ref, _int32(positions, "positions"), T, H, D, px, sx, py, sy,
                           1 if inverse else 0, _stream_handle(stream)), "pp_rope")
+
+
+def _heads_of(q, k, what):
+    """(tokens, query heads, key heads, head_dim, dtype) of q [T, heads, head_dim] and k [T, kv_heads, head_dim] or None."""
+    if q.dim() != 3 or (k is not None and (k.dim() != 3 or k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2])):
+        raise PPError(PP_ERR_SHAPE, what)
+    return q.shape[0], q.shape[1], 0 if k is None else k.shape[1], q.shape[2], q.dtype
+
+
+def _positions_of(rot, positions, T, what):
+    if rot is None:
+        return None
+    if positions is None:
+        raise PPError(PP_ERR_INVALID_ARG, what + ": positions")
+    if positions.numel() != T:
+        raise PPError(PP_ERR_SHAPE, what + ": positions")
+    return _int32(positions, "positions")
+
+
+def pp_head_norm_rope(norm, rot, positions, q, k, q_out, k_out, stream=None):
+    """q_out, k_out = q, k [T, heads, head_dim] normed and rotated by positions [T] (rot None: normed only; k None: no
+    keys).  An output may be its input."""
+    what = "pp_head_norm_rope"
+    T, H, Hkv, D, dt = _heads_of(q, k, what)
+    norm.check(dt, D, what)
+    pq, sq = _rows(q, T, H, D, dt, "pp_head_norm_rope: q")
+    po, so = _rows(q_out, T, H, D, dt, "pp_head_norm_rope: q_out")
+    pk, sk, pko, sko = None, 0, None, 0
+    if k is not None:
+        pk, sk = _rows(k, T, Hkv, D, dt, "pp_head_norm_rope: k")
+        pko, sko = _rows(k_out, T, Hkv, D, dt, "pp_head_norm_rope: k_out")
+    _check(load().pp_head_norm_rope(_torch_dtype(dt), norm.ref, None if rot is None else rot.ref,
+                                    _positions_of(rot, positions, T, what), T, H, Hkv, D, pq, sq, pk, sk, po, so, pko, sko,
+                                    _stream_handle(stream)), what)
+
+
+def pp_head_norm_workspace_size(head_dim) -> int:
+    return int(load().pp_head_norm_workspace_size(int(head_dim)))
+
+
+def alloc_head_norm_workspace(head_dim, device="cuda"):
+    """A workspace tensor of pp_head_norm_rope_grad."""
+    import torch
+    return torch.empty(max(256, pp_head_norm_workspace_size(head_dim)), dtype=torch.uint8, device=device)
+
+
+def _gamma_grad(t, D, what):
+    import torch
+    if t is None:
+        return None
+    if t.dtype != torch.float32:
+        raise PPError(PP_ERR_DTYPE, what)
+    if t.shape != (D,) or not t.is_contiguous():
+        raise PPError(PP_ERR_SHAPE, what)
+    return t.data_ptr()
+
+
+def pp_head_norm_rope_grad(norm, rot, positions, q, k, q_grad, k_grad, dq, dk, dq_gamma, dk_gamma, ws, stream=None):
+    """dq, dk: gradients of q, k from the gradients q_grad, k_grad of pp_head_norm_rope's outputs; dq_gamma, dk_gamma
+    [head_dim] float32 (each may be None; ws too where both are): gradients of the weights.  dq may be q_grad."""
+    what = "pp_head_norm_rope_grad"
+    T, H, Hkv, D, dt = _heads_of(q, k, what)
+    norm.check(dt, D, what)
+    pq, sq = _rows(q, T, H, D, dt, what + ": q")
+    pg, sg = _rows(q_grad, T, H, D, dt, what + ": q_grad")
+    po, so = _rows(dq, T, H, D, dt, what + ": dq")
+    pk, sk, pkg, skg, pko, sko = None, 0, None, 0, None, 0
+    if k is not None:
+        pk, sk = _rows(k, T, Hkv, D, dt, what + ": k")
+        pkg, skg = _rows(k_grad, T, Hkv, D, dt, what + ": k_grad")
+        pko, sko = _rows(dk, T, Hkv, D, dt, what + ": dk")
+    _check(load().pp_head_norm_rope_grad(_torch_dtype(dt), norm.ref, None if rot is None else rot.ref,
+                                         _positions_of(rot, positions, T, what), T, H, Hkv, D, pq, sq, pk, sk, pg, sg, pkg,
+                                         skg, po, so, pko, sko, _gamma_grad(dq_gamma, D, what + ": dq_gamma"),
+                                         _gamma_grad(dk_gamma, D, what + ": dk_gamma"),
+                                         None if ws is None else ws.data_ptr(), 0 if ws is None else ws.nbytes,
+                                         _stream_handle(stream)), what)
 
 
 def pp_attn_workspace_size(cache) -> int:

@@ -30,6 +30,27 @@ struct PageArgs {
     long long page_stride, token_stride, head_stride;  // bytes
 };
 
+// What is done to a head's row: norm (where `norm`) and rotation (where
+// rot_dim > 0).  `group` lanes hold a row (pp_head.cuh).
+struct HeadArgs {
+    const int32_t* positions;
+    const float* inv_freq;
+    float scale, eps;
+    int head_dim, rot_dim, group;
+    bool norm;
+};
+
+struct NormArgs {
+    HeadArgs head;
+    const char *q, *k, *q_gamma, *k_gamma;
+    const char *q_grad, *k_grad;  // gradients of the outputs (backward)
+    char *q_out, *k_out;          // outputs, or the gradients of q and k
+    long long q_stride, k_stride, q_grad_stride, k_grad_stride, q_out_stride, k_out_stride;  // bytes
+    int n_tokens, n_heads, n_kv_heads;
+    int ctas_q, ctas_k;  // backward: CTAs that take the rows of q and of k
+    float* part;         // backward: sums of the weights' gradients, a row of head_dim a CTA
+};
+
 struct AppendArgs {
     BatchArgs batch;
     PageArgs cache;
@@ -77,6 +98,10 @@ struct AttnArgs {
     unsigned* status;
     uint64_t timeout_ns;
 };
+
+constexpr int kNormGrid = 608;  // CTAs of the norms' backward pass at most
+cudaError_t norm_launch(const NormArgs& a, int dtype, int layout, cudaStream_t st);
+cudaError_t norm_grad_launch(NormArgs a, int dtype, int layout, float* q_gamma, float* k_gamma, int sms, cudaStream_t st);
 
 cudaError_t append_launch(const AppendArgs& a, int dtype, int layout, cudaStream_t st);
 cudaError_t commit_launch(const CommitArgs& a, cudaStream_t st);
