@@ -59,6 +59,14 @@ class pp_rotation(ctypes.Structure):
                 ("inv_freq", ctypes.c_void_p)]
 
 
+class pp_cache8(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("n_heads", ctypes.c_int), ("n_kv_heads", ctypes.c_int),
+                ("head_dim", ctypes.c_int), ("page_size", ctypes.c_int), ("n_pages", ctypes.c_int),
+                ("block", ctypes.c_int), ("page_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
 class pp_head_norm(ctypes.Structure):
     _fields_ = [("eps", ctypes.c_float), ("q_gamma", ctypes.c_void_p), ("k_gamma", ctypes.c_void_p)]
 
@@ -75,7 +83,7 @@ _PD = ctypes.POINTER(pp_desc)
 _PS = ctypes.POINTER(pp_selection)
 _D = ctypes.c_double
 _PC, _PB, _PR = ctypes.POINTER(pp_cache), ctypes.POINTER(pp_batch), ctypes.POINTER(pp_rotation)
-_PN = ctypes.POINTER(pp_head_norm)
+_PN, _PC8 = ctypes.POINTER(pp_head_norm), ctypes.POINTER(pp_cache8)
 
 EXPORTS = {
     "pp_workspace_size": (_Z, [_PD, _I]),
@@ -100,6 +108,11 @@ EXPORTS = {
     "pp_kv_append": (_I, [_PC, _PB, _PR, _P, _P, _LL, _P, _LL, _P, _LL, _P, _LL, _P, _Z, _P]),
     "pp_tree_attention": (_I, [_PC, _PB, _P, _LL, _P, _I, _F, _P, _LL, _P, _Z, _P]),
     "pp_kv_commit": (_I, [_PC, _PB, _I, _LL, _P, _I, _P, _P, _P, _Z, _P]),
+    "pp_attn8_workspace_size": (_Z, [_PC8]),
+    "pp_kv8_append": (_I, [_PC8, _PB, _PN, _PR, _P, _P, _LL, _P, _LL, _P, _LL, _P, _LL, _P, _Z, _P]),
+    "pp_kv8_read": (_I, [_PC8, _PB, _P, _LL, _P, _LL, _P, _Z, _P]),
+    "pp_tree_attention8": (_I, [_PC8, _PB, _P, _LL, _P, _I, _F, _P, _LL, _P, _Z, _P]),
+    "pp_kv8_commit": (_I, [_PC8, _PB, _I, _LL, _LL, _P, _I, _P, _P, _P, _Z, _P]),
     "pp_get_device_status": (_I, [_P, _P]),
     "pp_debug_wait_timeout": (_I, [_P, _Z, _LL, _P]),
     "pp_debug_decode_timeline": (_I, [_PD, _P, _P, _P, _P, _P, _F, _P, _P, _Z, _P, _Z, _P]),
@@ -422,6 +435,46 @@ class KVCache:
         self.dtype, self.n_heads, self.n_kv_heads, self.head_dim = k.dtype, int(n_heads), k.shape[2], k.shape[3]
 
 
+class KVCache8:
+    """A layer's key and value pages in 8 bits: codes k, v [n_pages, page_size, n_kv_heads, head_dim] (float8_e4m3fn, or
+    uint8 of its bits) of any strides (the same for both) with contiguous head_dim; scales k_scale, v_scale [n_pages,
+    n_kv_heads, page_size / block] (float32, contiguous), one for each block of tokens and head.  dtype: of the calls'
+    q, k, v and out."""
+
+    def __init__(self, k, v, k_scale, v_scale, n_heads, dtype):
+        import torch
+        _torch_types()
+        if k.dim() != 4 or k.shape != v.shape:
+            raise PPError(PP_ERR_SHAPE, "KVCache8")
+        if k.dtype != v.dtype or k.dtype not in (torch.uint8, torch.float8_e4m3fn):
+            raise PPError(PP_ERR_DTYPE, "KVCache8: codes")
+        if k.stride() != v.stride() or k.stride(3) != 1:
+            raise PPError(PP_ERR_INVALID_ARG, "KVCache8: strides")
+        if k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32:
+            raise PPError(PP_ERR_DTYPE, "KVCache8: scales")
+        if not k_scale.is_contiguous() or not v_scale.is_contiguous():
+            raise PPError(PP_ERR_INVALID_ARG, "KVCache8: scales must be contiguous")
+        n_pages, page, kv_heads, dim = k.shape
+        blocks = k_scale.shape[2] if k_scale.dim() == 3 else 0
+        if k_scale.shape != v_scale.shape or k_scale.shape != (n_pages, kv_heads, blocks) or blocks < 1 or page % blocks:
+            raise PPError(PP_ERR_SHAPE, "KVCache8: scales are [n_pages, n_kv_heads, page_size / block]")
+        self.k, self.v, self.k_scale, self.v_scale, self.block = k, v, k_scale, v_scale, page // blocks
+        self.c = pp_cache8(_torch_dtype(dtype), int(n_heads), kv_heads, dim, page, n_pages, self.block, k.stride(0), k.stride(1),
+                           k.stride(2), k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
+        self.ref = ctypes.byref(self.c)
+        self.dtype, self.n_heads, self.n_kv_heads, self.head_dim = dtype, int(n_heads), kv_heads, dim
+
+    @classmethod
+    def empty(cls, n_pages, page_size, n_heads, n_kv_heads, head_dim, dtype, block=16, device="cuda"):
+        """A cache of new tensors (no entry in it)."""
+        import torch
+        if block < 1 or page_size % block:
+            raise PPError(PP_ERR_SHAPE, "KVCache8: page_size is a multiple of block")
+        code = [torch.zeros((n_pages, page_size, n_kv_heads, head_dim), dtype=torch.uint8, device=device) for _ in range(2)]
+        scale = [torch.ones((n_pages, n_kv_heads, page_size // block), dtype=torch.float32, device=device) for _ in range(2)]
+        return cls(*code, *scale, n_heads, dtype)
+
+
 class Batch:
     """The sequences of a step: q_start [n_seqs + 1], ctx_len [n_seqs], pages [n_seqs, max_pages] (device, int32)."""
 
@@ -594,6 +647,78 @@ def pp_kv_commit(cache, batch, path, n_accept, ws, new_len=None, n_layers=1, lay
     _check(load().pp_kv_commit(cache.ref, batch.ref, n_layers, layer_stride, _int32(path, "path"), path.shape[1],
                                _int32(n_accept, "n_accept"), None if new_len is None else _int32(new_len, "new_len"),
                                ws.data_ptr(), ws.nbytes, _stream_handle(stream)), "pp_kv_commit")
+
+
+def pp_attn8_workspace_size(cache) -> int:
+    return int(load().pp_attn8_workspace_size(cache.ref))
+
+
+def alloc_attn8_workspace(cache, device=None, stream=None):
+    """A zero-initialised workspace tensor for the calls on 8-bit caches of this shape."""
+    import torch
+    ws = torch.empty(max(256, pp_attn8_workspace_size(cache)), dtype=torch.uint8, device=device or cache.k.device)
+    pp_workspace_init(ws, stream)
+    return ws
+
+
+def pp_kv8_append(cache, batch, norm, rot, positions, q, k, v, q_out, ws, stream=None):
+    """Append k, v [T, n_kv_heads, head_dim] to their pages in 8 bits, keys normed (norm may be None) and rotated;
+    q_out = q normed and rotated (both may be None)."""
+    T, D, dt = batch.n_tokens, cache.head_dim, cache.dtype
+    pq, sq, po, so = None, 0, None, 0
+    if norm is not None:
+        norm.check(dt, D, "pp_kv8_append")
+    if q is not None:
+        pq, sq = _rows(q, T, cache.n_heads, D, dt, "pp_kv8_append: q")
+    if q_out is not None:
+        po, so = _rows(q_out, T, cache.n_heads, D, dt, "pp_kv8_append: q_out")
+    pk, sk = _rows(k, T, cache.n_kv_heads, D, dt, "pp_kv8_append: k")
+    pv, sv = _rows(v, T, cache.n_kv_heads, D, dt, "pp_kv8_append: v")
+    pos = None
+    if positions is not None:
+        if positions.numel() != T:
+            raise PPError(PP_ERR_SHAPE, "pp_kv8_append: positions")
+        pos = _int32(positions, "positions")
+    _check(load().pp_kv8_append(cache.ref, batch.ref, None if norm is None else norm.ref, None if rot is None else rot.ref,
+                                pos, pq, sq, pk, sk, pv, sv, po, so, ws.data_ptr(), ws.nbytes, _stream_handle(stream)),
+           "pp_kv8_append")
+
+
+def pp_kv8_read(cache, batch, k_out, v_out, ws, stream=None):
+    """Rows of k_out, v_out [T, n_kv_heads, head_dim]: the values of the entries of the batch's tokens."""
+    T, D, dt = batch.n_tokens, cache.head_dim, cache.dtype
+    pk, sk = _rows(k_out, T, cache.n_kv_heads, D, dt, "pp_kv8_read: k_out")
+    pv, sv = _rows(v_out, T, cache.n_kv_heads, D, dt, "pp_kv8_read: v_out")
+    _check(load().pp_kv8_read(cache.ref, batch.ref, pk, sk, pv, sv, ws.data_ptr(), ws.nbytes, _stream_handle(stream)),
+           "pp_kv8_read")
+
+
+def pp_tree_attention8(cache, batch, q, mask, scale, out, ws, stream=None):
+    """out = attention of q [T, n_heads, head_dim] over the 8-bit cache; mask [T, words] int32 bits, or None (chains)."""
+    T, D, dt = batch.n_tokens, cache.head_dim, cache.dtype
+    pq, sq = _rows(q, T, cache.n_heads, D, dt, "pp_tree_attention8: q")
+    po, so = _rows(out, T, cache.n_heads, D, dt, "pp_tree_attention8: out")
+    pm, words = None, 0
+    if mask is not None:
+        if mask.dim() != 2 or mask.shape[0] != T:
+            raise PPError(PP_ERR_SHAPE, "pp_tree_attention8: mask")
+        pm, words = _int32(mask, "mask"), mask.shape[1]
+    _check(load().pp_tree_attention8(cache.ref, batch.ref, pq, sq, pm, words, scale, po, so, ws.data_ptr(), ws.nbytes,
+                                     _stream_handle(stream)), "pp_tree_attention8")
+
+
+def pp_kv8_commit(cache, batch, path, n_accept, ws, new_len=None, n_layers=1, layer_stride=0, scale_layer_stride=0,
+                  stream=None):
+    """Move the accepted path [n_seqs, max_path] of each tree behind its context, in every layer's 8-bit cache
+    (layer_stride, scale_layer_stride: elements from one layer's codes and scales to the next one's)."""
+    n = batch.n_seqs
+    if path.dim() != 2 or path.shape[0] != n or n_accept.numel() != n or \
+            (new_len is not None and new_len.numel() != n):
+        raise PPError(PP_ERR_SHAPE, "pp_kv8_commit")
+    _check(load().pp_kv8_commit(cache.ref, batch.ref, n_layers, layer_stride, scale_layer_stride, _int32(path, "path"),
+                                path.shape[1], _int32(n_accept, "n_accept"),
+                                None if new_len is None else _int32(new_len, "new_len"), ws.data_ptr(), ws.nbytes,
+                                _stream_handle(stream)), "pp_kv8_commit")
 
 
 def pp_get_device_status(ws, stream=None) -> int:

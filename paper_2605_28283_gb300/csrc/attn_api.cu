@@ -5,23 +5,8 @@
 namespace pp {
 namespace {
 
-constexpr uint64_t kWaitLimitNs = 2000000000ull;  // bounded waits give up after 2 s
-
-struct AttnLayout {
-    size_t counters, tails, part, total;
-};
-
-AttnLayout attn_layout(const pp_cache& c) {
-    AttnLayout L;
-    L.counters = sizeof(Control);
-    L.tails = (L.counters + kAttnMaxGrid * 4 + 255) & ~(size_t)255;
-    L.part = (L.tails + kAttnTcGrid * kAttnTail + 255) & ~(size_t)255;
-    L.total = (L.part + attn_part_floats(c.head_dim) * 4 + 255) & ~(size_t)255;
-    return L;
-}
-
 pp_status check_attn_ws(const pp_cache* c, const void* ws, size_t ws_bytes) {
-    if (!ws || !aligned(ws, 256) || ws_bytes < attn_layout(*c).total) return PP_ERR_WORKSPACE;
+    if (!ws || !aligned(ws, 256) || ws_bytes < attn_layout(c->head_dim).total) return PP_ERR_WORKSPACE;
     return PP_OK;
 }
 
@@ -114,7 +99,7 @@ pp_status pp_rope(int dtype, const pp_rotation* rot, const int32_t* positions, i
 }
 
 size_t pp_attn_workspace_size(const pp_cache* cache) {
-    return check_cache_shape(cache) == PP_OK ? attn_layout(*cache).total : 0;
+    return check_cache_shape(cache) == PP_OK ? attn_layout(cache->head_dim).total : 0;
 }
 
 pp_status pp_kv_append(const pp_cache* cache, const pp_batch* batch, const pp_rotation* rot,
@@ -176,39 +161,14 @@ pp_status pp_tree_attention(const pp_cache* cache, const pp_batch* batch, const 
                             void* ws, size_t ws_bytes, void* stream) {
     PP_TRY(check_cache(cache));
     PP_TRY(check_batch(batch, cache));
-    if (!(scale > 0.0f) || !std::isfinite(scale)) return PP_ERR_INVALID_ARG;
-    if (mask && mask_words < 1) return PP_ERR_INVALID_ARG;
-    if (mask && !aligned(mask, 4)) return PP_ERR_ALIGN;
-    if (mask && mask_words > 1 << 20) return PP_ERR_SHAPE;
-    const int e = elem_size(cache->dtype), row = cache->n_heads * cache->head_dim;
-    PP_TRY(check_rows(q, q_stride, row, e, batch->n_tokens));
-    PP_TRY(check_rows(out, out_stride, row, e, batch->n_tokens));
-    if (rows_overlap(q, (int64_t)row * e, q_stride * e, out, (int64_t)row * e, out_stride * e, batch->n_tokens))
-        return PP_ERR_INVALID_ARG;
+    PP_TRY(check_attention(*batch, cache->dtype, cache->n_heads * cache->head_dim, q, q_stride, mask, mask_words, scale, out,
+                           out_stride));
     PP_TRY(check_attn_ws(cache, ws, ws_bytes));
     int sms = 0;
     PP_TRY(device_sms(&sms));
     if (batch->n_seqs == 0 || batch->n_tokens == 0) return PP_OK;
-    const AttnLayout L = attn_layout(*cache);
-    AttnArgs a;
-    std::memset(&a, 0, sizeof a);
-    a.batch = batch_args(*batch, *cache);
-    a.cache = page_args(*cache);
-    a.q = static_cast<const char*>(q);
-    a.out = static_cast<char*>(out);
-    a.q_stride = q_stride * e;
-    a.out_stride = out_stride * e;
-    a.mask = mask;
-    a.mask_words = mask_words;
-    a.n_kv_heads = cache->n_kv_heads;
-    a.group = cache->n_heads / cache->n_kv_heads;
-    a.head_dim = cache->head_dim;
-    a.scale_log2 = (float)((double)scale * 1.4426950408889634);
-    a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + L.part);
-    a.tails = static_cast<char*>(ws) + L.tails;
-    a.counters = reinterpret_cast<unsigned*>(static_cast<char*>(ws) + L.counters);
-    a.status = status_of(ws);
-    a.timeout_ns = kWaitLimitNs;
+    const AttnArgs a = attn_args(*cache, batch_args(*batch, *cache), page_args(*cache), q, q_stride, mask, mask_words, scale, out,
+                                 out_stride, ws);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     return cuda_status(cache->dtype == PP_BF16 ? attn_tc_launch(a, sms, st) : attn_simt_launch(a, sms, st));
 }
@@ -225,16 +185,8 @@ pp_status pp_kv_commit(const pp_cache* cache, const pp_batch* batch, int n_layer
         if (layer_stride * e % 16 != 0) return PP_ERR_ALIGN;
     }
     if (!entries_apart(*cache, n_layers, layer_stride)) return PP_ERR_INVALID_ARG;
+    PP_TRY(check_path(*batch, path, max_path, n_accept, new_len));
     const int B = batch->n_seqs;
-    if (B > 0 && (!n_accept || (!path && max_path > 0))) return PP_ERR_INVALID_ARG;
-    if (!aligned(path, 4) || !aligned(n_accept, 4) || !aligned(new_len, 4)) return PP_ERR_ALIGN;
-    if (B > 0) PP_TRY(check_batch_pointers(batch));
-    if (new_len) {
-        auto over = [&](const void* p, int64_t bytes) { return rows_overlap(new_len, 4ll * B, 4ll * B, p, bytes, bytes, B ? 1 : 0); };
-        if (over(batch->ctx_len, 4ll * B) || over(n_accept, 4ll * B) || over(path, 4ll * B * max_path) ||
-            over(batch->q_start, 4ll * (B + 1)) || over(batch->pages, 4ll * B * batch->max_pages))
-            return PP_ERR_INVALID_ARG;
-    }
     if ((long long)B * n_layers > 0x7fffffffll) return PP_ERR_SHAPE;
     PP_TRY(check_attn_ws(cache, ws, ws_bytes));
     int sms = 0;

@@ -1,5 +1,6 @@
 // Attention over the paged cache on the CUDA cores: the fp32 path, fp32
-// throughout.  One CTA streams its stretch of the key line (pp_attn_sched.cuh)
+// throughout, over pages of fp32 elements or of e4m3 codes (Q8; widened as they
+// go into shared memory, by ordinary loads).  One CTA streams its stretch of the key line (pp_attn_sched.cuh)
 // tile by tile: TOK keys and values into shared memory (cp.async, entries past
 // the sequence as zeros), scores, the running maximum and weight sum of each
 // row, weighted values into registers.
@@ -11,7 +12,10 @@
 // of the others.  3 drafted trees of 9 to 13 tokens over 100 to 1000 entries,
 // 16 heads of 64: 19 us, a chain of latencies (16 MB, 2.4 us of HBM); for
 // many rows the score loop's shared-memory loads bound it.
+#include <cuda_fp16.h>
+
 #include "pp_attn_sched.cuh"
+#include "pp_cache8.cuh"
 #include "pp_launch.cuh"
 #include "pp_tc.cuh"
 
@@ -48,7 +52,17 @@ struct Simt {
     static_assert((kTSplit - 1) * ROWS * DP <= TOK * (kKStride + DP), "joining area");
 };
 
-template <int ROWS, int TOK, int DP>
+// 16 codes times their scale, to shared memory.
+PP_DEVINL void widen16(float* dst, const uint4& w, float scale) {
+    const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const float2 a = from_codes(x[i] & 0xffffu), b = from_codes(x[i] >> 16);
+        reinterpret_cast<float4*>(dst)[i] = make_float4(a.x * scale, a.y * scale, b.x * scale, b.y * scale);
+    }
+}
+
+template <bool Q8, int ROWS, int TOK, int DP>
 __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_constant__ AttnArgs a) {
     using L = Simt<ROWS, TOK, DP>;
     extern __shared__ __align__(16) float sm[];
@@ -81,21 +95,45 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_consta
         for (int t = p.t0; t < p.t1; t++) {
             const int k0 = t * TOK;
             __syncthreads();  // the last tile's readers are done (first tile: rows are in place)
-            for (int e = tid; e < TOK * (DP / 4); e += kThreads) {
-                const int r = e / (DP / 4), d = e % (DP / 4) * 4, j = k0 + r;
-                long long at = 0;
-                bool in = j < p.key_end && d < D;
-                if (in) {
-                    const int page = entry_page(a.batch, p.b, j);
-                    if (page >= 0) {
-                        at = entry_offset(a.batch, a.cache, page, j) + (long long)p.h * a.cache.head_stride + d * 4;
-                    } else {
-                        record_status(a.status, PP_ERR_INVALID_ARG);
-                        in = false;
+            if constexpr (Q8) {
+#pragma unroll 2
+                for (int e = tid; e < TOK * (DP / 16); e += kThreads) {
+                    const int r = e / (DP / 16), d = e % (DP / 16) * 16, j = k0 + r;
+                    uint4 k{}, v{};
+                    float ks = 0.f, vs = 0.f;
+                    if (j < p.key_end && d < D) {
+                        const int page = entry_page(a.batch, p.b, j);
+                        if (page >= 0) {
+                            const long long at = entry_offset(a.batch, a.cache, page, j) + (long long)p.h * a.cache.head_stride + d;
+                            const long long sc = scale_index(a.batch, a.scales, a.n_kv_heads, page, p.h, j);
+                            k = *reinterpret_cast<const uint4*>(a.cache.k + at);
+                            v = *reinterpret_cast<const uint4*>(a.cache.v + at);
+                            ks = a.scales.k[sc];
+                            vs = a.scales.v[sc];
+                        } else {
+                            record_status(a.status, PP_ERR_INVALID_ARG);
+                        }
                     }
+                    widen16(Ks + r * L::kKStride + d, k, ks);
+                    widen16(Vs + r * DP + d, v, vs);
                 }
-                cp_async_16(Ks + r * L::kKStride + d, a.cache.k + at, in ? 16u : 0u);
-                cp_async_16(Vs + r * DP + d, a.cache.v + at, in ? 16u : 0u);
+            } else {
+                for (int e = tid; e < TOK * (DP / 4); e += kThreads) {
+                    const int r = e / (DP / 4), d = e % (DP / 4) * 4, j = k0 + r;
+                    long long at = 0;
+                    bool in = j < p.key_end && d < D;
+                    if (in) {
+                        const int page = entry_page(a.batch, p.b, j);
+                        if (page >= 0) {
+                            at = entry_offset(a.batch, a.cache, page, j) + (long long)p.h * a.cache.head_stride + d * 4;
+                        } else {
+                            record_status(a.status, PP_ERR_INVALID_ARG);
+                            in = false;
+                        }
+                    }
+                    cp_async_16(Ks + r * L::kKStride + d, a.cache.k + at, in ? 16u : 0u);
+                    cp_async_16(Vs + r * DP + d, a.cache.v + at, in ? 16u : 0u);
+                }
             }
             cp_async_commit();
             cp_async_wait<0>();
@@ -237,10 +275,10 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_consta
     }
 }
 
-template <int ROWS, int TOK, int DP>
+template <bool Q8, int ROWS, int TOK, int DP>
 cudaError_t go(const AttnArgs& a, int sms, cudaStream_t st) {
     using L = Simt<ROWS, TOK, DP>;
-    auto* kern = attn_simt_kernel<ROWS, TOK, DP>;
+    auto* kern = attn_simt_kernel<Q8, ROWS, TOK, DP>;
     constexpr int kBytes = L::kFloats * 4;
     static std::atomic<bool> allowed[64];
     cudaError_t e = allow_smem(kern, kBytes, allowed);
@@ -251,14 +289,8 @@ cudaError_t go(const AttnArgs& a, int sms, cudaStream_t st) {
     return launch_overlapped(kern, dim3((unsigned)grid), dim3(kThreads), kBytes, st, a);
 }
 
-}  // namespace
-
-size_t attn_part_floats(int head_dim) {
-    const size_t simt = (size_t)kAttnMaxGrid * kAttnSimtRows, tc = (size_t)kAttnTcGrid * kAttnTcRows;
-    return 2 * (simt > tc ? simt : tc) * (head_dim + 2);
-}
-
-cudaError_t attn_simt_launch(const AttnArgs& a, int sms, cudaStream_t st) {
+template <bool Q8>
+cudaError_t launch(const AttnArgs& a, int sms, cudaStream_t st) {
     // rows a sequence brings to a key head on average: small tiles spread
     // their threads over keys and elements instead of rows that do not exist
     // (tiles of 16 / 4 rows, 3 sequences over 100 to 1000 entries: 4 rows 19.2 /
@@ -266,9 +298,19 @@ cudaError_t attn_simt_launch(const AttnArgs& a, int sms, cudaStream_t st) {
     // 44.0 / 49.5)
     const long long rows = ((long long)a.batch.n_tokens * a.group + a.batch.n_seqs - 1) / a.batch.n_seqs;
     const bool few = rows <= 4;
-    if (a.head_dim <= 64) return few ? go<4, 64, 64>(a, sms, st) : go<16, 64, 64>(a, sms, st);
-    if (a.head_dim <= 128) return few ? go<4, 64, 128>(a, sms, st) : go<16, 64, 128>(a, sms, st);
-    return few ? go<4, 64, 256>(a, sms, st) : go<16, 64, 256>(a, sms, st);
+    if (a.head_dim <= 64) return few ? go<Q8, 4, 64, 64>(a, sms, st) : go<Q8, 16, 64, 64>(a, sms, st);
+    if (a.head_dim <= 128) return few ? go<Q8, 4, 64, 128>(a, sms, st) : go<Q8, 16, 64, 128>(a, sms, st);
+    return few ? go<Q8, 4, 64, 256>(a, sms, st) : go<Q8, 16, 64, 256>(a, sms, st);
 }
+
+}  // namespace
+
+size_t attn_part_floats(int head_dim) {
+    const size_t simt = (size_t)kAttnMaxGrid * kAttnSimtRows, tc = (size_t)kAttnTcGrid * kAttnTcRows;
+    return 2 * (simt > tc ? simt : tc) * (head_dim + 2);
+}
+
+cudaError_t attn_simt_launch(const AttnArgs& a, int sms, cudaStream_t st) { return launch<false>(a, sms, st); }
+cudaError_t attn8_simt_launch(const AttnArgs& a, int sms, cudaStream_t st) { return launch<true>(a, sms, st); }
 
 }  // namespace pp

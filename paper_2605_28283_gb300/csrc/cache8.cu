@@ -1,0 +1,548 @@
+// The paged key/value cache in 8 bits: append, entries read back, and the
+// commit of a drafted tree's accepted path.  All move bytes and compute little,
+// so HBM bounds them (and launch latency, for a few tokens).
+#include <algorithm>
+
+#include <cuda_fp16.h>
+
+#include "pp_cache8.cuh"
+#include "pp_head.cuh"
+#include "pp_launch.cuh"
+
+namespace pp {
+namespace {
+
+// ------------------------------------------------------------------- append
+// Two kinds of CTAs in one launch.  The first slots * parts take the keys and
+// values: a slot is a block of one sequence's entries, dealt without the host
+// knowing a length: sequence b's slots start at q_start[b] / block + 2 b, which
+// leaves it the (n - 1) / block + 2 blocks that n new entries can touch.  A
+// strip of R rows of one head's keys or values is held by one warp, in
+// registers: its largest magnitude is known before anything is written, and
+// every element is read once.  The strips of a longer block meet in shared
+// memory.  The other CTAs take a token's query heads, as in norm_kernel.
+constexpr int kMaxStrips = 16;  // warps of a CTA at most
+
+struct Slot {
+    int page, lo;      // the block's page and first entry; page -1: nothing to do
+    int e0, e1;        // its new entries
+    int token;         // of entry e0
+    int ctx;
+};
+
+// By one warp.
+PP_DEVINL Slot find_slot(const BatchArgs& B, int shift, int slot, int lane, unsigned* status) {
+    int lo = 0, hi = B.n_seqs;
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 31) / 32, at = lo + lane * step;
+        const int i = at < hi ? at : lo;
+        const unsigned le = __ballot_sync(kFull, at < hi && (long long)(B.q_start[i] >> shift) + 2ll * i <= slot);
+        const int c = __popc(le);
+        if (c == 0) break;
+        lo += (c - 1) * step;
+        hi = min(hi, lo + step);
+    }
+    Slot s{-1, 0, 0, 0, 0, 0};
+    const Seq q = load_seq(B, lo);
+    const long long j = (long long)slot - (q.q0 >> shift) - 2ll * lo;
+    if (q.bad || q.n == 0 || j < 0 || j > (q.n >> shift) + 1) return s;
+    const long long first = (((long long)q.ctx >> shift) + j) << shift;
+    if (first >= (long long)q.ctx + q.n) return s;
+    s.lo = (int)first;
+    s.ctx = q.ctx;
+    s.e0 = max(s.lo, q.ctx);
+    s.e1 = (int)min(first + (1 << shift), (long long)q.ctx + q.n);
+    s.token = q.q0 + s.e0 - q.ctx;
+    s.page = entry_page(B, lo, s.lo);
+    if (s.page < 0 && lane == 0) record_status(status, PP_ERR_INVALID_ARG);
+    return s;
+}
+
+template <int V>
+PP_DEVINL void store_codes(char* p, const float (&f)[V], float inv) {
+    uint32_t w[V > 4 ? V / 4 : 1] = {};
+#pragma unroll
+    for (int i = 0; i < V; i += 2) w[i / 4] |= to_codes(to_hold(f[i]) * inv, to_hold(f[i + 1]) * inv) << (i % 4 * 8);
+    if constexpr (V == 8)
+        *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+    else if constexpr (V == 4)
+        *reinterpret_cast<uint32_t*>(p) = w[0];
+    else
+        *reinterpret_cast<uint16_t*>(p) = (uint16_t)w[0];
+}
+// V codes at p rounded again at another scale.
+template <int V>
+PP_DEVINL void again(char* p, float ratio) {
+    float f[V];
+#pragma unroll
+    for (int i = 0; i < V; i += 2) {
+        const float2 v = from_codes(*reinterpret_cast<const uint16_t*>(p + i));
+        f[i] = v.x;
+        f[i + 1] = v.y;
+    }
+    store_codes<V>(p, f, ratio);
+}
+
+template <typename T, int V, bool HALF, int UPL, int ITER>
+__global__ void __launch_bounds__(32 * kMaxStrips) append8_kernel(const Append8Args a) {
+    using Lane = HeadLane<T, V, HALF, UPL>;
+    extern __shared__ __align__(16) float2 cs[];
+    __shared__ Slot slot_s;
+    __shared__ int pos_s;
+    __shared__ float amax_s[kMaxStrips];
+    pdl_launch_dependents();
+    pdl_wait();
+    const HeadArgs& h = a.head;
+    const int tid = threadIdx.x, warp = tid >> 5, l32 = tid & 31, D = h.head_dim;
+    const Lane lane(h, l32 % h.group);
+    const int kv_ctas = a.slots * a.parts;
+    if ((int)blockIdx.x >= kv_ctas) {
+        // ------------------------------------------------------------ queries
+        const int t = ((int)blockIdx.x - kv_ctas) / a.split, y = ((int)blockIdx.x - kv_ctas) % a.split;
+        const int groups = (int)blockDim.x / h.group, step = groups * a.split;
+        const char* q = a.q + t * a.q_stride;
+        char* out = a.q_out + t * a.q_out_stride;
+        if (warp == 0) {
+            const int b = find_seq(a.batch, t, l32);
+            const Seq s = load_seq(a.batch, b);
+            const int i = t - s.q0;
+            const bool in = !s.bad && i >= 0 && i < s.n;
+            if (l32 == 0) {
+                slot_s.page = in ? 0 : -1;
+                pos_s = h.positions ? h.positions[t] : s.ctx + i;
+            }
+        }
+        float2 c[UPL][V];
+        bool ready = false;
+        for (int r0 = y * groups; r0 < a.n_heads; r0 += 2 * step) {
+            Vec<T, V> x[2][UPL][2];
+#pragma unroll
+            for (int n = 0; n < 2; n++) {
+                const int r = r0 + n * step + tid / h.group;
+                if (r < a.n_heads) lane.load(q + (long long)r * D * (int)sizeof(T), x[n]);
+            }
+            if (!ready) {
+                __syncthreads();
+                if (slot_s.page < 0) return;  // padding, or a skipped sequence: nothing is written
+                if (h.rot_dim > 0) {
+                    fill_pairs(cs, h, V, pos_s, false, tid, blockDim.x);
+                    __syncthreads();
+                    lane.factors(cs, h, c);
+                }
+                ready = true;
+            }
+#pragma unroll
+            for (int n = 0; n < 2; n++) {
+                const int r = r0 + n * step + tid / h.group;
+                float f[UPL][2][V], g[UPL][2][V];
+                lane.widen(x[n], f);
+                if (h.norm) {
+                    const float inv = inverse_rms(Lane::group_sum(r < a.n_heads ? Lane::dot(f, f) : 0.f, h.group), h);
+                    lane.weights(a.q_gamma, g);
+                    Lane::scale_by(f, inv, g);
+                }
+                if (r >= a.n_heads) continue;
+                if (h.rot_dim > 0) lane.rotate(f, c);
+                if (h.norm || h.rot_dim > 0) lane.narrow(f, x[n]);
+                lane.store(out + (long long)r * D * (int)sizeof(T), x[n]);
+            }
+        }
+        return;
+    }
+    // --------------------------------------------------------- keys and values
+    const int slot = (int)blockIdx.x / a.parts, part = (int)blockIdx.x % a.parts, block = 1 << a.scales.shift;
+    if (warp == 0) {
+        const Slot s = find_slot(a.batch, a.scales.shift, slot, l32, a.status);
+        if (l32 == 0) slot_s = s;
+    } else if (tid == 32 && part == 0) {
+        // every sequence is looked at once, also one that no token belongs to
+        for (int b = slot; b < a.batch.n_seqs; b += a.slots)
+            if (load_seq(a.batch, b).bad) record_status(a.status, PP_ERR_INVALID_ARG);
+    }
+    __syncthreads();
+    const Slot s = slot_s;
+    if (s.page < 0) return;
+    const int per = 32 / h.group, R = ITER * per;  // rows of a warp at once, of a strip
+    const int strips = max(1, block / R), units = (int)blockDim.x / 32 / strips;
+    const int strip = warp % strips;
+    const int pitch = (h.rot_dim / 2 + V - 1) / V, row_pairs = pitch * V;  // factors of a row
+    const int factors = part * units < a.n_kv_heads ? (s.e1 - s.e0) * (h.rot_dim / 2) : 0;  // values need none
+    for (int i = tid; i < factors; i += blockDim.x) {
+        const int row = i / (h.rot_dim / 2), p = i - row * (h.rot_dim / 2), t = s.token + row;
+        const float2 v = cos_sin(h.positions ? h.positions[t] : s.e0 + row, h.inv_freq[p]);
+        cs[(s.e0 - s.lo + row) * row_pairs + pair_slot(p, V, pitch)] = make_float2(v.x * h.scale, v.y * h.scale);
+    }
+    __syncthreads();
+    for (int u0 = part * units; u0 < 2 * a.n_kv_heads; u0 += units * a.parts) {
+        const int u = u0 + warp / strips;
+        const bool have = u < 2 * a.n_kv_heads, key = u < a.n_kv_heads;
+        const int head = key ? u : u - a.n_kv_heads;
+        const int first = s.lo + strip * R + l32 / h.group;  // entry of the lane's first row
+        const long long at = scale_index(a.batch, a.scales, a.n_kv_heads, s.page, head, s.lo);
+        float* scale_p = (key ? a.scales.k : a.scales.v) + at;
+        const bool cached = s.lo < s.ctx;
+        float old = have && cached && l32 == 0 ? *scale_p : 0.f;
+        float f[ITER][UPL][2][V];
+        if (have) {
+            Vec<T, V> x[ITER][UPL][2];
+            const char* src = (key ? a.k : a.v) + (long long)head * D * (int)sizeof(T);
+            const long long stride = key ? a.k_stride : a.v_stride;
+#pragma unroll
+            for (int n = 0; n < ITER; n++) {
+                const int e = first + n * per;
+                if (e >= s.e0 && e < s.e1) lane.load(src + (s.token + e - s.e0) * stride, x[n]);
+            }
+#pragma unroll
+            for (int n = 0; n < ITER; n++) {
+                const int e = first + n * per;
+                const bool in = e >= s.e0 && e < s.e1;
+                lane.widen(x[n], f[n]);
+                if (!in) {
+#pragma unroll
+                    for (int k = 0; k < UPL; k++)
+#pragma unroll
+                        for (int i = 0; i < V; i++) f[n][k][0][i] = f[n][k][1][i] = 0.f;
+                }
+                if (!key) continue;
+                if (h.norm) {
+                    float g[UPL][2][V];
+                    const float inv = inverse_rms(Lane::group_sum(Lane::dot(f[n], f[n]), h.group), h);
+                    lane.weights(a.k_gamma, g);
+                    if (in) Lane::scale_by(f[n], inv, g);
+                }
+                if (h.rot_dim > 0 && in) {
+                    float2 c[UPL][V];
+                    lane.factors(cs + (e - s.lo) * row_pairs, h, c);
+                    lane.rotate(f[n], c);
+                }
+            }
+        }
+        float amax = 0.f;
+        if (have) {
+#pragma unroll
+            for (int n = 0; n < ITER; n++)
+#pragma unroll
+                for (int k = 0; k < UPL; k++)
+#pragma unroll
+                    for (int i = 0; i < V; i++)
+                        amax = fmaxf(amax, fmaxf(magnitude(f[n][k][0][i]), magnitude(f[n][k][1][i])));
+            amax = warp_max(amax);
+            old = __shfl_sync(kFull, old, 0);
+        }
+        if (strips > 1) {
+            __syncthreads();  // the last unit's readers are done
+            if (l32 == 0) amax_s[warp] = amax;
+            __syncthreads();
+            for (int i = 0; i < strips; i++) amax = fmaxf(amax, amax_s[warp - strip + i]);
+        }
+        if (!have) continue;
+        const float now = block_scale(amax, old, cached);
+        char* dst = (key ? a.cache.k : a.cache.v) + entry_offset(a.batch, a.cache, s.page, s.lo) + head * a.cache.head_stride;
+        if (cached && now != old) {
+#pragma unroll 1
+            for (int n = 0; n < ITER; n++) {
+                const int e = first + n * per;
+                if (e >= s.ctx || e >= s.lo + block) break;
+                char* row = dst + (e - s.lo) * a.cache.token_stride;
+#pragma unroll
+                for (int k = 0; k < UPL; k++) {
+                    if (lane.va[k] >= 0) again<V>(row + lane.va[k] * V, old / now);
+                    if (lane.vb[k] >= 0) again<V>(row + lane.vb[k] * V, old / now);
+                }
+            }
+        }
+        const float inv = 1.0f / now;
+#pragma unroll
+        for (int n = 0; n < ITER; n++) {
+            const int e = first + n * per;
+            if (e < s.e0 || e >= s.e1) continue;
+            char* row = dst + (e - s.lo) * a.cache.token_stride;
+#pragma unroll
+            for (int k = 0; k < UPL; k++) {
+                if (lane.va[k] >= 0) store_codes<V>(row + lane.va[k] * V, f[n][k][0], inv);
+                if (lane.vb[k] >= 0) store_codes<V>(row + lane.vb[k] * V, f[n][k][1], inv);
+            }
+        }
+        if (l32 == 0 && strip == 0 && now != old) *scale_p = now;
+    }
+}
+
+template <typename T, int V, bool HALF, int UPL, int ITER>
+cudaError_t append8_run(Append8Args& a, int block, cudaStream_t st) {
+    const int R = ITER * 32 / a.head.group, strips = std::max(1, block / R), warps = std::max(8, strips);
+    const int units = warps / strips, passes = (2 * a.n_kv_heads + units - 1) / units;
+    const long long T_ = a.batch.n_tokens;
+    a.slots = (int)(T_ / block + 2ll * a.batch.n_seqs);
+    // about two CTAs an SM where there are few blocks
+    a.parts = std::min(passes, std::max(1, (304 + a.slots - 1) / a.slots));
+    const int rows = warps * 32 / a.head.group;  // query rows of a CTA at once
+    a.split = a.n_heads ? (int)std::min<long long>((a.n_heads + rows - 1) / rows, std::max<long long>(1, 304 / T_)) : 1;
+    const long long ctas = (long long)a.slots * a.parts + (a.n_heads ? T_ * a.split : 0);
+    if (ctas > 0x7fffffffll) return cudaErrorInvalidValue;
+    const int pairs = (a.head.rot_dim / 2 + V - 1) / V * V;
+    const int smem = std::max(1, block) * pairs * 8;
+    auto* kern = append8_kernel<T, V, HALF, UPL, ITER>;
+    if (smem > 40 * 1024) {
+        static std::atomic<bool> allowed[64];
+        const cudaError_t e = allow_smem(kern, 128 * 128 * 8, allowed);
+        if (e != cudaSuccess) return e;
+    }
+    return launch_overlapped(kern, dim3((unsigned)ctas), dim3((unsigned)(warps * 32)), (size_t)smem, st, a);
+}
+
+template <typename T, int V, bool HALF>
+cudaError_t append8_go(Append8Args a, int block, cudaStream_t st) {
+    const int units = head_units<V>(a.head);
+    int group = 4;
+    while (group < 32 && group < units) group *= 2;
+    a.head.group = group;
+    // strips of up to 64 fp32 values a lane
+    if constexpr (V == 2) {
+        if (units > 32) return append8_run<T, V, HALF, 2, 8>(a, block, st);
+        return append8_run<T, V, HALF, 1, 8>(a, block, st);
+    } else if constexpr (V == 4) {
+        return group <= 8 ? append8_run<T, V, HALF, 1, 4>(a, block, st) : append8_run<T, V, HALF, 1, 8>(a, block, st);
+    } else {
+        return append8_run<T, V, HALF, 1, 4>(a, block, st);
+    }
+}
+
+template <typename T>
+cudaError_t append8_typed(const Append8Args& a, int layout, int block, cudaStream_t st) {
+    constexpr int V = 16 / (int)sizeof(T);
+    const bool half = layout == PP_ROPE_HALF;
+    const bool whole = half ? a.head.rot_dim % (2 * V) == 0 : a.head.rot_dim % V == 0;
+    if (whole) return half ? append8_go<T, V, true>(a, block, st) : append8_go<T, V, false>(a, block, st);
+    return half ? append8_go<T, 2, true>(a, block, st) : append8_go<T, 2, false>(a, block, st);
+}
+
+// --------------------------------------------------------------------- read
+// kReadTokens tokens a CTA: a warp looks each one's entry up, then all threads
+// go over their rows, V codes (a 16-byte store) at a time.
+constexpr int kReadTokens = 8, kReadUnits = 4;
+
+template <typename T>
+__global__ void __launch_bounds__(256) read8_kernel(const Read8Args a) {
+    constexpr int V = 16 / (int)sizeof(T);
+    __shared__ long long code_s[kReadTokens], scale_s[kReadTokens];  // -1: zeros, -2: left alone
+    pdl_launch_dependents();
+    pdl_wait();
+    const int t0 = (int)blockIdx.x * kReadTokens, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (t0 + warp < a.batch.n_tokens) {
+        const int t = t0 + warp, b = find_seq(a.batch, t, lane);
+        const Seq s = load_seq(a.batch, b);
+        const int i = t - s.q0, e = s.ctx + i;
+        long long code = -2, sc = 0;
+        if (!s.bad && i >= 0 && i < s.n) {
+            const int page = entry_page(a.batch, b, e);
+            code = -1;
+            if (page >= 0) {
+                code = entry_offset(a.batch, a.cache, page, e);
+                sc = scale_index(a.batch, a.scales, a.n_kv_heads, page, 0, e);
+            } else if (lane == 0) {
+                record_status(a.status, PP_ERR_INVALID_ARG);
+            }
+        }
+        if (lane == 0) {
+            code_s[warp] = code;
+            scale_s[warp] = sc;
+        }
+    }
+    if (tid == 0)
+        for (int b = blockIdx.x; b < a.batch.n_seqs; b += gridDim.x)
+            if (load_seq(a.batch, b).bad) record_status(a.status, PP_ERR_INVALID_ARG);
+    __syncthreads();
+    const int tokens = min(kReadTokens, a.batch.n_tokens - t0);
+    const int per = a.head_dim / V, row = a.n_kv_heads * per, total = tokens * 2 * row;
+    for (int u0 = tid; u0 < total; u0 += kReadUnits * 256) {
+        typename Raw<V>::type w[kReadUnits];
+        float sc[kReadUnits];
+        char* dst[kReadUnits];
+#pragma unroll
+        for (int k = 0; k < kReadUnits; k++) {
+            const int u = u0 + k * 256;
+            dst[k] = nullptr;
+            w[k] = {};
+            sc[k] = 0.f;
+            if (u >= total) continue;
+            const int n = u / (2 * row), r = u - n * 2 * row, key = r < row, x = key ? r : r - row;
+            const int head = x / per, c = x - head * per;
+            const long long code = code_s[n];
+            if (code == -2) continue;
+            dst[k] = (key ? a.k_out + (t0 + n) * a.k_stride : a.v_out + (t0 + n) * a.v_stride) + (long long)x * 16;
+            if (code < 0) continue;
+            w[k] = __ldcs(reinterpret_cast<const typename Raw<V>::type*>((key ? a.cache.k : a.cache.v) + code +
+                                                                        head * a.cache.head_stride + c * V));
+            sc[k] = (key ? a.scales.k : a.scales.v)[scale_s[n] + (long long)head * a.scales.blocks];
+        }
+#pragma unroll
+        for (int k = 0; k < kReadUnits; k++) {
+            if (!dst[k]) continue;
+            Vec<T, V> out;
+            const uint32_t* words = reinterpret_cast<const uint32_t*>(&w[k]);
+#pragma unroll
+            for (int i = 0; i < V; i += 2) {
+                const float2 v = from_codes(words[i / 4] >> (i % 4 * 8) & 0xffffu);
+                out.set2(i, v.x * sc[k], v.y * sc[k]);
+            }
+            out.store(dst[k]);
+        }
+    }
+}
+
+// ------------------------------------------------------------------- commit
+// One CTA for each (sequence, layer); a warp takes one head's keys or values
+// and moves their accepted entries a destination block at a time: first their
+// largest magnitude, and with it the block's scale, then the codes, kBatch rows
+// of a lane read before they are written.  In place and without a barrier
+// between warps: path[j] >= j, so what is read lies at or past what is written,
+// and rows of one batch are read by the whole warp before any is written.
+constexpr int kMoveBatch = 4;
+constexpr int kMoveChunk = 128;  // entries of a destination block at most
+
+__global__ void __launch_bounds__(512) commit8_kernel(const Commit8Args a8) {
+    const CommitArgs& a = a8.c;
+    __shared__ long long src_s[kMoveChunk], scale_s[kMoveChunk];  // of an accepted entry; code -1: in its place already
+    __shared__ int bad_s, inplace_s;
+    pdl_launch_dependents();
+    pdl_wait();
+    const int b = blockIdx.x % a.batch.n_seqs, layer = blockIdx.x / a.batch.n_seqs;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = (int)blockDim.x >> 5;
+    const int32_t* path = a.path + (size_t)b * a.max_path;
+    const Seq s = load_seq(a.batch, b);
+    const int acc = a.n_accept[b];
+    if (tid == 0) bad_s = s.bad || acc < 0 || acc > a.max_path || acc > s.n;
+    __syncthreads();
+    if (!bad_s) {
+        bool bad = false;
+        for (int j = tid; j < acc && !bad; j += blockDim.x) {
+            const int p = path[j], before = j > 0 ? path[j - 1] : -1;
+            bad = p < 0 || p >= s.n || p <= before || entry_page(a.batch, b, s.ctx + p) < 0 || entry_page(a.batch, b, s.ctx + j) < 0;
+        }
+        if (bad) bad_s = 1;
+    }
+    __syncthreads();
+    const bool bad = bad_s != 0;
+    if (layer == 0 && tid == 0) {
+        if (bad) record_status(a.status, PP_ERR_INVALID_ARG);
+        if (a.new_len) a.new_len[b] = bad ? s.ctx : s.ctx + acc;
+    }
+    if (bad) return;
+    const int D = a.head_bytes, shift = a8.scales.shift, block = 1 << shift;
+    int group = 1;  // lanes of a row, 16 codes each
+    while (group * 16 < D) group *= 2;
+    const int per = 32 / group, col = lane % group * 16;
+    const bool on = col < D;
+    for (int j0 = 0; j0 < acc;) {
+        const int lo = (s.ctx + j0) >> shift << shift, j1 = min(acc, lo + block - s.ctx), n = j1 - j0;
+        __syncthreads();  // the last block's readers are done
+        if (tid == 0) inplace_s = 0;
+        __syncthreads();
+        for (int i = tid; i < n; i += blockDim.x) {
+            const int p = path[j0 + i], e = s.ctx + p, page = entry_page(a.batch, b, e);
+            src_s[i] = p == j0 + i ? -1 : entry_offset(a.batch, a.cache, page, e);
+            scale_s[i] = scale_index(a.batch, a8.scales, a.n_kv_heads, page, 0, e);
+            if (p == j0 + i) inplace_s = 1;
+        }
+        __syncthreads();
+        const int page = entry_page(a.batch, b, lo);
+        const long long dst0 = entry_offset(a.batch, a.cache, page, lo), to = scale_index(a.batch, a8.scales, a.n_kv_heads, page, 0, lo);
+        const bool stays = lo < s.ctx || inplace_s;
+        for (int u = warp; u < 2 * a.n_kv_heads; u += warps) {
+            const bool key = u < a.n_kv_heads;
+            const int head = key ? u : u - a.n_kv_heads;
+            char* codes = (key ? a.cache.k : a.cache.v) + (long long)layer * a.layer_stride + (long long)head * a.cache.head_stride + col;
+            float* scales = (key ? a8.scales.k : a8.scales.v) + (long long)layer * a8.scale_layer_stride + (long long)head * a8.scales.blocks;
+            const float old = stays ? scales[to] : 0.f;
+            float amax = 0.f;
+            for (int i0 = lane / group; i0 < n; i0 += kMoveBatch * per) {
+                uint4 w[kMoveBatch] = {};
+                float sc[kMoveBatch] = {};
+#pragma unroll
+                for (int k = 0; k < kMoveBatch; k++) {
+                    const int i = i0 + k * per;
+                    if (i >= n || src_s[i] < 0 || !on) continue;
+                    w[k] = *reinterpret_cast<const uint4*>(codes + src_s[i]);
+                    sc[k] = scales[scale_s[i]];
+                }
+#pragma unroll
+                for (int k = 0; k < kMoveBatch; k++) {
+                    const uint32_t x[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+#pragma unroll
+                    for (int i = 0; i < 8; i++) {
+                        const float2 v = from_codes(x[i / 2] >> (i % 2 * 16) & 0xffffu);
+                        amax = fmaxf(amax, fmaxf(magnitude(v.x * sc[k]), magnitude(v.y * sc[k])));
+                    }
+                }
+            }
+            amax = warp_max(amax);
+            const float now = block_scale(amax, old, stays);
+            if (stays && now != old && on) {
+                // entries that stay: cached ones, and accepted ones in their place
+                for (int e = max(lo, 0) + lane / group; e < s.ctx + j1; e += per) {
+                    if (e >= s.ctx && (e < s.ctx + j0 || src_s[e - s.ctx - j0] >= 0)) continue;
+                    uint4* p = reinterpret_cast<uint4*>(codes + dst0 + (e - lo) * a.cache.token_stride);
+                    const uint4 w = *p;
+                    const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+                    uint32_t y[4] = {};
+#pragma unroll
+                    for (int i = 0; i < 8; i++) {
+                        const float2 v = from_codes(x[i / 2] >> (i % 2 * 16) & 0xffffu);
+                        y[i / 2] |= to_codes(v.x * (old / now), v.y * (old / now)) << (i % 2 * 16);
+                    }
+                    *p = make_uint4(y[0], y[1], y[2], y[3]);
+                }
+            }
+            for (int i0 = lane / group; i0 - lane / group < n; i0 += kMoveBatch * per) {
+                uint4 w[kMoveBatch] = {};
+                float sc[kMoveBatch] = {};
+#pragma unroll
+                for (int k = 0; k < kMoveBatch; k++) {
+                    const int i = i0 + k * per;
+                    if (i >= n || src_s[i] < 0 || !on) continue;
+                    w[k] = *reinterpret_cast<const uint4*>(codes + src_s[i]);
+                    sc[k] = scales[scale_s[i]];
+                }
+                __syncwarp();
+#pragma unroll
+                for (int k = 0; k < kMoveBatch; k++) {
+                    const int i = i0 + k * per;
+                    if (i >= n || src_s[i] < 0 || !on) continue;
+                    const float ratio = sc[k] / now;
+                    const uint32_t x[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+                    uint32_t y[4] = {};
+#pragma unroll
+                    for (int c = 0; c < 8; c++) {
+                        const float2 v = from_codes(x[c / 2] >> (c % 2 * 16) & 0xffffu);
+                        y[c / 2] |= to_codes(v.x * ratio, v.y * ratio) << (c % 2 * 16);
+                    }
+                    *reinterpret_cast<uint4*>(codes + dst0 + (s.ctx + j0 + i - lo) * a.cache.token_stride) = make_uint4(y[0], y[1], y[2], y[3]);
+                }
+                __syncwarp();
+            }
+            if (lane == 0 && now != old) scales[to] = now;
+            __syncwarp();
+        }
+        j0 = j1;
+    }
+}
+
+}  // namespace
+
+cudaError_t append8_launch(const Append8Args& a, int dtype, int layout, int block, cudaStream_t st) {
+    return dtype == PP_BF16 ? append8_typed<__nv_bfloat16>(a, layout, block, st) : append8_typed<float>(a, layout, block, st);
+}
+
+cudaError_t read8_launch(const Read8Args& a, int dtype, cudaStream_t st) {
+    const unsigned ctas = (unsigned)((a.batch.n_tokens + kReadTokens - 1) / kReadTokens);
+    auto* kern = dtype == PP_BF16 ? read8_kernel<__nv_bfloat16> : read8_kernel<float>;
+    return launch_overlapped(kern, dim3(ctas), dim3(256), 0, st, a);
+}
+
+cudaError_t commit8_launch(const Commit8Args& a, cudaStream_t st) {
+    const long long ctas = (long long)a.c.batch.n_seqs * a.c.n_layers;
+    const int warps = std::min(16, std::max(2, 2 * a.c.n_kv_heads));
+    return launch_overlapped(commit8_kernel, dim3((unsigned)ctas), dim3((unsigned)(warps * 32)), 0, st, a);
+}
+
+}  // namespace pp

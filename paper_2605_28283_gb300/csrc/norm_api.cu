@@ -18,18 +18,10 @@ bool clash(const Rows& out, const Rows& x, int T, bool may_be) {
     return rows_overlap(out.p, out.row, out.stride, x.p, x.row, x.stride, T);
 }
 
-pp_status check_norm(const pp_head_norm* n, int dtype, int head_dim) {
-    if (!n || !(n->eps >= 0.0f) || !std::isfinite(n->eps)) return PP_ERR_INVALID_ARG;
-    if (dtype == PP_BF16 || dtype == PP_F32) {
-        if (!aligned(n->q_gamma, 16) || !aligned(n->k_gamma, 16)) return PP_ERR_ALIGN;
-    }
-    return check_heads(dtype, 1, head_dim);
-}
-
 pp_status check_call(int dtype, const pp_head_norm* norm, const pp_rotation* rot, const int32_t* positions, int T, int H,
                      int Hkv, int D) {
     PP_TRY(check_heads(dtype, H, D));
-    PP_TRY(check_norm(norm, dtype, D));
+    PP_TRY(check_norm(norm));
     if (rot) PP_TRY(check_rotation(rot, D));
     if (T < 0 || Hkv < 0 || Hkv > kMaxHeads) return PP_ERR_SHAPE;
     if (rot && !positions && T > 0) return PP_ERR_INVALID_ARG;

@@ -79,9 +79,48 @@ struct CommitArgs {
     unsigned* status;
 };
 
+// Scales of an 8-bit cache (PageArgs then holds its codes).
+struct ScaleArgs {
+    float* k;
+    float* v;
+    int shift;   // block == 1 << shift
+    int blocks;  // of a page
+};
+
+struct Append8Args {
+    BatchArgs batch;
+    PageArgs cache;
+    ScaleArgs scales;
+    HeadArgs head;
+    const char *q, *k, *v, *q_gamma, *k_gamma;
+    char* q_out;
+    long long q_stride, k_stride, v_stride, q_out_stride;  // bytes
+    int n_heads, n_kv_heads;  // n_heads 0: no queries
+    int slots, parts;         // blocks of tokens that may be new, CTAs of each
+    int split;                // CTAs of a token's queries
+    unsigned* status;
+};
+
+struct Read8Args {
+    BatchArgs batch;
+    PageArgs cache;
+    ScaleArgs scales;
+    char *k_out, *v_out;
+    long long k_stride, v_stride;  // bytes
+    int n_kv_heads, head_dim;
+    unsigned* status;
+};
+
+struct Commit8Args {
+    CommitArgs c;
+    ScaleArgs scales;
+    long long scale_layer_stride;  // floats
+};
+
 struct AttnArgs {
     BatchArgs batch;
     PageArgs cache;
+    ScaleArgs scales;    // 8-bit cache
     const char* q;
     char* out;
     long long q_stride, out_stride;  // bytes
@@ -106,8 +145,14 @@ cudaError_t norm_grad_launch(NormArgs a, int dtype, int layout, float* q_gamma, 
 cudaError_t append_launch(const AppendArgs& a, int dtype, int layout, cudaStream_t st);
 cudaError_t commit_launch(const CommitArgs& a, cudaStream_t st);
 
+cudaError_t append8_launch(const Append8Args& a, int dtype, int layout, int block, cudaStream_t st);
+cudaError_t read8_launch(const Read8Args& a, int dtype, cudaStream_t st);
+cudaError_t commit8_launch(const Commit8Args& a, cudaStream_t st);
+
 size_t attn_part_floats(int head_dim);  // floats behind AttnArgs.part
 cudaError_t attn_simt_launch(const AttnArgs& a, int sms, cudaStream_t st);  // fp32
 cudaError_t attn_tc_launch(const AttnArgs& a, int sms, cudaStream_t st);    // bf16
+cudaError_t attn8_simt_launch(const AttnArgs& a, int sms, cudaStream_t st);  // the same over 8-bit pages
+cudaError_t attn8_tc_launch(const AttnArgs& a, int sms, cudaStream_t st);
 
 }  // namespace pp

@@ -125,6 +125,12 @@ pp_status check_rotation(const pp_rotation* r, int head_dim) {
     return PP_OK;
 }
 
+pp_status check_norm(const pp_head_norm* n) {
+    if (!n || !(n->eps >= 0.0f) || !std::isfinite(n->eps)) return PP_ERR_INVALID_ARG;
+    if (!aligned(n->q_gamma, 16) || !aligned(n->k_gamma, 16)) return PP_ERR_ALIGN;
+    return PP_OK;
+}
+
 // Rows [T] of `la` bytes `sa` apart at a against rows of `lb` bytes `sb`
 // apart at b: whether any byte is shared.  Rows of one stride may be the
 // parts of one buffer.
@@ -138,7 +144,79 @@ bool rows_overlap(const void* a, int64_t la, int64_t sa, const void* b, int64_t 
     return d < la || d + lb > sa;
 }
 
+constexpr uint64_t kWaitLimitNs = 2000000000ull;  // bounded waits give up after 2 s
+
+// Workspace of the calls on a cache.
+struct AttnLayout {
+    size_t counters, tails, part, total;
+};
+
+AttnLayout attn_layout(int head_dim) {
+    AttnLayout L;
+    L.counters = sizeof(Control);
+    L.tails = (L.counters + kAttnMaxGrid * 4 + 255) & ~(size_t)255;
+    L.part = (L.tails + kAttnTcGrid * kAttnTail + 255) & ~(size_t)255;
+    L.total = (L.part + attn_part_floats(head_dim) * 4 + 255) & ~(size_t)255;
+    return L;
+}
+
 unsigned* status_of(void* ws) { return &static_cast<Control*>(ws)->status; }
+
+// The tensors and the mask of an attention call; rows of `row` elements.
+pp_status check_attention(const pp_batch& batch, int dtype, int row, const void* q, int64_t q_stride, const uint32_t* mask,
+                          int mask_words, float scale, const void* out, int64_t out_stride) {
+    if (!(scale > 0.0f) || !std::isfinite(scale)) return PP_ERR_INVALID_ARG;
+    if (mask && mask_words < 1) return PP_ERR_INVALID_ARG;
+    if (mask && !aligned(mask, 4)) return PP_ERR_ALIGN;
+    if (mask && mask_words > 1 << 20) return PP_ERR_SHAPE;
+    const int e = elem_size(dtype);
+    PP_TRY(check_rows(q, q_stride, row, e, batch.n_tokens));
+    PP_TRY(check_rows(out, out_stride, row, e, batch.n_tokens));
+    if (rows_overlap(q, (int64_t)row * e, q_stride * e, out, (int64_t)row * e, out_stride * e, batch.n_tokens))
+        return PP_ERR_INVALID_ARG;
+    return PP_OK;
+}
+
+AttnArgs attn_args(const pp_cache& c, const BatchArgs& batch, const PageArgs& pages, const void* q, int64_t q_stride,
+                   const uint32_t* mask, int mask_words, float scale, void* out, int64_t out_stride, void* ws) {
+    const AttnLayout L = attn_layout(c.head_dim);
+    const int e = elem_size(c.dtype);
+    AttnArgs a;
+    std::memset(&a, 0, sizeof a);
+    a.batch = batch;
+    a.cache = pages;
+    a.q = static_cast<const char*>(q);
+    a.out = static_cast<char*>(out);
+    a.q_stride = q_stride * e;
+    a.out_stride = out_stride * e;
+    a.mask = mask;
+    a.mask_words = mask_words;
+    a.n_kv_heads = c.n_kv_heads;
+    a.group = c.n_heads / c.n_kv_heads;
+    a.head_dim = c.head_dim;
+    a.scale_log2 = (float)((double)scale * 1.4426950408889634);
+    a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + L.part);
+    a.tails = static_cast<char*>(ws) + L.tails;
+    a.counters = reinterpret_cast<unsigned*>(static_cast<char*>(ws) + L.counters);
+    a.status = status_of(ws);
+    a.timeout_ns = kWaitLimitNs;
+    return a;
+}
+
+// The accepted paths of a commit.
+pp_status check_path(const pp_batch& batch, const int32_t* path, int max_path, const int32_t* n_accept, const int32_t* new_len) {
+    const int B = batch.n_seqs;
+    if (B > 0 && (!n_accept || (!path && max_path > 0))) return PP_ERR_INVALID_ARG;
+    if (!aligned(path, 4) || !aligned(n_accept, 4) || !aligned(new_len, 4)) return PP_ERR_ALIGN;
+    if (B > 0) PP_TRY(check_batch_pointers(&batch));
+    if (new_len) {
+        auto over = [&](const void* p, int64_t bytes) { return rows_overlap(new_len, 4ll * B, 4ll * B, p, bytes, bytes, B ? 1 : 0); };
+        if (over(batch.ctx_len, 4ll * B) || over(n_accept, 4ll * B) || over(path, 4ll * B * max_path) ||
+            over(batch.q_start, 4ll * (B + 1)) || over(batch.pages, 4ll * B * batch.max_pages))
+            return PP_ERR_INVALID_ARG;
+    }
+    return PP_OK;
+}
 
 }  // namespace
 }  // namespace pp

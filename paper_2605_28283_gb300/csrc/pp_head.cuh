@@ -111,7 +111,7 @@ struct HeadLane {
             for (int s = 0; s < 2; s++) {
                 const int v = s ? vb[k] : va[k];
                 typename Raw<kBytes>::type w{};
-                if (gamma && v >= 0) w = __ldg(reinterpret_cast<const typename Raw<kBytes>::type*>(gamma + v * kBytes));
+                if (gamma && v >= 0) w = *reinterpret_cast<const typename Raw<kBytes>::type*>(gamma + v * kBytes);
                 Vec<T, V> x;
                 x.raw = w;
 #pragma unroll
