@@ -476,7 +476,7 @@ pp_status pp_kv_commit(const pp_cache *cache, const pp_batch *batch, int n_layer
    256).  `block` consecutive entries (16, 32, 64 or 128; page_size is a
    multiple of it) share a scale: that of page p, head h and the block that
    starts at offset i block is scale[(p n_kv_heads + h) (page_size / block) + i].
-   The scales that pp_kv8_append and pp_kv8_commit write are powers of two, at
+   The scales that pp_kvq_append and pp_kvq_commit write are powers of two, at
    least 2^-60; others (a cache filled elsewhere) may be any positive normal
    number.  What is not finite is held as the NaN code. */
 typedef struct pp_cache8 {
@@ -490,7 +490,7 @@ typedef struct pp_cache8 {
 
 /* Workspace bytes of the calls on this cache (0 for an unsupported one), used
    as that of pp_attn_workspace_size. */
-size_t pp_attn8_workspace_size(const pp_cache8 *cache);
+size_t pp_kvq_workspace_size(const pp_cache8 *cache);
 
 /* pp_kv_append to an 8-bit cache.  norm (may be NULL) is applied to the heads
    of q and k ahead of the rotation; what is written is rounded once, from the
@@ -500,7 +500,7 @@ size_t pp_attn8_workspace_size(const pp_cache8 *cache);
    its scale unless 448 times it is less than that, and then gets the new
    entries' scale, its cached codes rounded again at it.  So the block that the
    first new token falls into is rewritten: it belongs to one sequence. */
-pp_status pp_kv8_append(const pp_cache8 *cache, const pp_batch *batch, const pp_head_norm *norm, const pp_rotation *rot,
+pp_status pp_kvq_append(const pp_cache8 *cache, const pp_batch *batch, const pp_head_norm *norm, const pp_rotation *rot,
                         const int32_t *positions, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
                         const void *v, int64_t v_stride, void *q_out, int64_t q_out_stride, void *ws, size_t ws_bytes,
                         void *stream);
@@ -511,12 +511,12 @@ pp_status pp_kv8_append(const pp_cache8 *cache, const pp_batch *batch, const pp_
    lengths, whole sequences; with a step's own batch, what it appended.  Values
    are rounded once (powers of two as scales: not at all).  Rows of padding and
    of skipped sequences are left as they are; entries of a bad page give zeros. */
-pp_status pp_kv8_read(const pp_cache8 *cache, const pp_batch *batch, void *k_out, int64_t k_out_stride, void *v_out,
+pp_status pp_kvq_read(const pp_cache8 *cache, const pp_batch *batch, void *k_out, int64_t k_out_stride, void *v_out,
                       int64_t v_out_stride, void *ws, size_t ws_bytes, void *stream);
 
 /* pp_tree_attention over an 8-bit cache: the same masks, shapes and results,
    with code * scale for the keys and values. */
-pp_status pp_tree_attention8(const pp_cache8 *cache, const pp_batch *batch, const void *q, int64_t q_stride,
+pp_status pp_kvq_tree_attention(const pp_cache8 *cache, const pp_batch *batch, const void *q, int64_t q_stride,
                              const uint32_t *mask, int mask_words, float scale, void *out, int64_t out_stride, void *ws,
                              size_t ws_bytes, void *stream);
 
@@ -524,9 +524,9 @@ pp_status pp_tree_attention8(const pp_cache8 *cache, const pp_batch *batch, cons
    and its scales l * scale_layer_stride floats further.  The entries' values
    move.  Of the blocks that they move into, one in which entries stay (cached
    ones, or accepted ones in their place already) keeps its scale as in
-   pp_kv8_append, any other gets the scale that its entries need.  Entries past
+   pp_kvq_append, any other gets the scale that its entries need.  Entries past
    the accepted ones are lost. */
-pp_status pp_kv8_commit(const pp_cache8 *cache, const pp_batch *batch, int n_layers, int64_t layer_stride,
+pp_status pp_kvq_commit(const pp_cache8 *cache, const pp_batch *batch, int n_layers, int64_t layer_stride,
                         int64_t scale_layer_stride, const int32_t *path, int max_path, const int32_t *n_accept,
                         int32_t *new_len, void *ws, size_t ws_bytes, void *stream);
 

@@ -108,11 +108,11 @@ EXPORTS = {
     "pp_kv_append": (_I, [_PC, _PB, _PR, _P, _P, _LL, _P, _LL, _P, _LL, _P, _LL, _P, _Z, _P]),
     "pp_tree_attention": (_I, [_PC, _PB, _P, _LL, _P, _I, _F, _P, _LL, _P, _Z, _P]),
     "pp_kv_commit": (_I, [_PC, _PB, _I, _LL, _P, _I, _P, _P, _P, _Z, _P]),
-    "pp_attn8_workspace_size": (_Z, [_PC8]),
-    "pp_kv8_append": (_I, [_PC8, _PB, _PN, _PR, _P, _P, _LL, _P, _LL, _P, _LL, _P, _LL, _P, _Z, _P]),
-    "pp_kv8_read": (_I, [_PC8, _PB, _P, _LL, _P, _LL, _P, _Z, _P]),
-    "pp_tree_attention8": (_I, [_PC8, _PB, _P, _LL, _P, _I, _F, _P, _LL, _P, _Z, _P]),
-    "pp_kv8_commit": (_I, [_PC8, _PB, _I, _LL, _LL, _P, _I, _P, _P, _P, _Z, _P]),
+    "pp_kvq_workspace_size": (_Z, [_PC8]),
+    "pp_kvq_append": (_I, [_PC8, _PB, _PN, _PR, _P, _P, _LL, _P, _LL, _P, _LL, _P, _LL, _P, _Z, _P]),
+    "pp_kvq_read": (_I, [_PC8, _PB, _P, _LL, _P, _LL, _P, _Z, _P]),
+    "pp_kvq_tree_attention": (_I, [_PC8, _PB, _P, _LL, _P, _I, _F, _P, _LL, _P, _Z, _P]),
+    "pp_kvq_commit": (_I, [_PC8, _PB, _I, _LL, _LL, _P, _I, _P, _P, _P, _Z, _P]),
     "pp_get_device_status": (_I, [_P, _P]),
     "pp_debug_wait_timeout": (_I, [_P, _Z, _LL, _P]),
     "pp_debug_decode_timeline": (_I, [_PD, _P, _P, _P, _P, _P, _F, _P, _P, _Z, _P, _Z, _P]),
@@ -649,76 +649,76 @@ def pp_kv_commit(cache, batch, path, n_accept, ws, new_len=None, n_layers=1, lay
                                ws.data_ptr(), ws.nbytes, _stream_handle(stream)), "pp_kv_commit")
 
 
-def pp_attn8_workspace_size(cache) -> int:
-    return int(load().pp_attn8_workspace_size(cache.ref))
+def pp_kvq_workspace_size(cache) -> int:
+    return int(load().pp_kvq_workspace_size(cache.ref))
 
 
-def alloc_attn8_workspace(cache, device=None, stream=None):
+def alloc_kvq_workspace(cache, device=None, stream=None):
     """A zero-initialised workspace tensor for the calls on 8-bit caches of this shape."""
     import torch
-    ws = torch.empty(max(256, pp_attn8_workspace_size(cache)), dtype=torch.uint8, device=device or cache.k.device)
+    ws = torch.empty(max(256, pp_kvq_workspace_size(cache)), dtype=torch.uint8, device=device or cache.k.device)
     pp_workspace_init(ws, stream)
     return ws
 
 
-def pp_kv8_append(cache, batch, norm, rot, positions, q, k, v, q_out, ws, stream=None):
+def pp_kvq_append(cache, batch, norm, rot, positions, q, k, v, q_out, ws, stream=None):
     """Append k, v [T, n_kv_heads, head_dim] to their pages in 8 bits, keys normed (norm may be None) and rotated;
     q_out = q normed and rotated (both may be None)."""
     T, D, dt = batch.n_tokens, cache.head_dim, cache.dtype
     pq, sq, po, so = None, 0, None, 0
     if norm is not None:
-        norm.check(dt, D, "pp_kv8_append")
+        norm.check(dt, D, "pp_kvq_append")
     if q is not None:
-        pq, sq = _rows(q, T, cache.n_heads, D, dt, "pp_kv8_append: q")
+        pq, sq = _rows(q, T, cache.n_heads, D, dt, "pp_kvq_append: q")
     if q_out is not None:
-        po, so = _rows(q_out, T, cache.n_heads, D, dt, "pp_kv8_append: q_out")
-    pk, sk = _rows(k, T, cache.n_kv_heads, D, dt, "pp_kv8_append: k")
-    pv, sv = _rows(v, T, cache.n_kv_heads, D, dt, "pp_kv8_append: v")
+        po, so = _rows(q_out, T, cache.n_heads, D, dt, "pp_kvq_append: q_out")
+    pk, sk = _rows(k, T, cache.n_kv_heads, D, dt, "pp_kvq_append: k")
+    pv, sv = _rows(v, T, cache.n_kv_heads, D, dt, "pp_kvq_append: v")
     pos = None
     if positions is not None:
         if positions.numel() != T:
-            raise PPError(PP_ERR_SHAPE, "pp_kv8_append: positions")
+            raise PPError(PP_ERR_SHAPE, "pp_kvq_append: positions")
         pos = _int32(positions, "positions")
-    _check(load().pp_kv8_append(cache.ref, batch.ref, None if norm is None else norm.ref, None if rot is None else rot.ref,
+    _check(load().pp_kvq_append(cache.ref, batch.ref, None if norm is None else norm.ref, None if rot is None else rot.ref,
                                 pos, pq, sq, pk, sk, pv, sv, po, so, ws.data_ptr(), ws.nbytes, _stream_handle(stream)),
-           "pp_kv8_append")
+           "pp_kvq_append")
 
 
-def pp_kv8_read(cache, batch, k_out, v_out, ws, stream=None):
+def pp_kvq_read(cache, batch, k_out, v_out, ws, stream=None):
     """Rows of k_out, v_out [T, n_kv_heads, head_dim]: the values of the entries of the batch's tokens."""
     T, D, dt = batch.n_tokens, cache.head_dim, cache.dtype
-    pk, sk = _rows(k_out, T, cache.n_kv_heads, D, dt, "pp_kv8_read: k_out")
-    pv, sv = _rows(v_out, T, cache.n_kv_heads, D, dt, "pp_kv8_read: v_out")
-    _check(load().pp_kv8_read(cache.ref, batch.ref, pk, sk, pv, sv, ws.data_ptr(), ws.nbytes, _stream_handle(stream)),
-           "pp_kv8_read")
+    pk, sk = _rows(k_out, T, cache.n_kv_heads, D, dt, "pp_kvq_read: k_out")
+    pv, sv = _rows(v_out, T, cache.n_kv_heads, D, dt, "pp_kvq_read: v_out")
+    _check(load().pp_kvq_read(cache.ref, batch.ref, pk, sk, pv, sv, ws.data_ptr(), ws.nbytes, _stream_handle(stream)),
+           "pp_kvq_read")
 
 
-def pp_tree_attention8(cache, batch, q, mask, scale, out, ws, stream=None):
+def pp_kvq_tree_attention(cache, batch, q, mask, scale, out, ws, stream=None):
     """out = attention of q [T, n_heads, head_dim] over the 8-bit cache; mask [T, words] int32 bits, or None (chains)."""
     T, D, dt = batch.n_tokens, cache.head_dim, cache.dtype
-    pq, sq = _rows(q, T, cache.n_heads, D, dt, "pp_tree_attention8: q")
-    po, so = _rows(out, T, cache.n_heads, D, dt, "pp_tree_attention8: out")
+    pq, sq = _rows(q, T, cache.n_heads, D, dt, "pp_kvq_tree_attention: q")
+    po, so = _rows(out, T, cache.n_heads, D, dt, "pp_kvq_tree_attention: out")
     pm, words = None, 0
     if mask is not None:
         if mask.dim() != 2 or mask.shape[0] != T:
-            raise PPError(PP_ERR_SHAPE, "pp_tree_attention8: mask")
+            raise PPError(PP_ERR_SHAPE, "pp_kvq_tree_attention: mask")
         pm, words = _int32(mask, "mask"), mask.shape[1]
-    _check(load().pp_tree_attention8(cache.ref, batch.ref, pq, sq, pm, words, scale, po, so, ws.data_ptr(), ws.nbytes,
-                                     _stream_handle(stream)), "pp_tree_attention8")
+    _check(load().pp_kvq_tree_attention(cache.ref, batch.ref, pq, sq, pm, words, scale, po, so, ws.data_ptr(), ws.nbytes,
+                                     _stream_handle(stream)), "pp_kvq_tree_attention")
 
 
-def pp_kv8_commit(cache, batch, path, n_accept, ws, new_len=None, n_layers=1, layer_stride=0, scale_layer_stride=0,
+def pp_kvq_commit(cache, batch, path, n_accept, ws, new_len=None, n_layers=1, layer_stride=0, scale_layer_stride=0,
                   stream=None):
     """Move the accepted path [n_seqs, max_path] of each tree behind its context, in every layer's 8-bit cache
     (layer_stride, scale_layer_stride: elements from one layer's codes and scales to the next one's)."""
     n = batch.n_seqs
     if path.dim() != 2 or path.shape[0] != n or n_accept.numel() != n or \
             (new_len is not None and new_len.numel() != n):
-        raise PPError(PP_ERR_SHAPE, "pp_kv8_commit")
-    _check(load().pp_kv8_commit(cache.ref, batch.ref, n_layers, layer_stride, scale_layer_stride, _int32(path, "path"),
+        raise PPError(PP_ERR_SHAPE, "pp_kvq_commit")
+    _check(load().pp_kvq_commit(cache.ref, batch.ref, n_layers, layer_stride, scale_layer_stride, _int32(path, "path"),
                                 path.shape[1], _int32(n_accept, "n_accept"),
                                 None if new_len is None else _int32(new_len, "new_len"), ws.data_ptr(), ws.nbytes,
-                                _stream_handle(stream)), "pp_kv8_commit")
+                                _stream_handle(stream)), "pp_kvq_commit")
 
 
 def pp_get_device_status(ws, stream=None) -> int:

@@ -71,11 +71,11 @@ using namespace pp;
 
 extern "C" {
 
-size_t pp_attn8_workspace_size(const pp_cache8* cache) {
+size_t pp_kvq_workspace_size(const pp_cache8* cache) {
     return check_shape8(cache) == PP_OK ? attn_layout(cache->head_dim).total : 0;
 }
 
-pp_status pp_kv8_append(const pp_cache8* cache, const pp_batch* batch, const pp_head_norm* norm, const pp_rotation* rot,
+pp_status pp_kvq_append(const pp_cache8* cache, const pp_batch* batch, const pp_head_norm* norm, const pp_rotation* rot,
                         const int32_t* positions, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
                         const void* v, int64_t v_stride, void* q_out, int64_t q_out_stride, void* ws, size_t ws_bytes,
                         void* stream) {
@@ -140,7 +140,7 @@ pp_status pp_kv8_append(const pp_cache8* cache, const pp_batch* batch, const pp_
                                       static_cast<cudaStream_t>(stream)));
 }
 
-pp_status pp_kv8_read(const pp_cache8* cache, const pp_batch* batch, void* k_out, int64_t k_out_stride, void* v_out,
+pp_status pp_kvq_read(const pp_cache8* cache, const pp_batch* batch, void* k_out, int64_t k_out_stride, void* v_out,
                       int64_t v_out_stride, void* ws, size_t ws_bytes, void* stream) {
     PP_TRY(check_cache8(cache));
     const pp_cache codes = codes_of(*cache);
@@ -169,7 +169,7 @@ pp_status pp_kv8_read(const pp_cache8* cache, const pp_batch* batch, void* k_out
     return cuda_status(read8_launch(a, cache->dtype, static_cast<cudaStream_t>(stream)));
 }
 
-pp_status pp_tree_attention8(const pp_cache8* cache, const pp_batch* batch, const void* q, int64_t q_stride,
+pp_status pp_kvq_tree_attention(const pp_cache8* cache, const pp_batch* batch, const void* q, int64_t q_stride,
                              const uint32_t* mask, int mask_words, float scale, void* out, int64_t out_stride, void* ws,
                              size_t ws_bytes, void* stream) {
     PP_TRY(check_cache8(cache));
@@ -188,7 +188,7 @@ pp_status pp_tree_attention8(const pp_cache8* cache, const pp_batch* batch, cons
     return cuda_status(cache->dtype == PP_BF16 ? attn8_tc_launch(a, sms, st) : attn8_simt_launch(a, sms, st));
 }
 
-pp_status pp_kv8_commit(const pp_cache8* cache, const pp_batch* batch, int n_layers, int64_t layer_stride,
+pp_status pp_kvq_commit(const pp_cache8* cache, const pp_batch* batch, int n_layers, int64_t layer_stride,
                         int64_t scale_layer_stride, const int32_t* path, int max_path, const int32_t* n_accept,
                         int32_t* new_len, void* ws, size_t ws_bytes, void* stream) {
     PP_TRY(check_cache8(cache));

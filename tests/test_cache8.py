@@ -42,19 +42,19 @@ C, B = cache(), batch()
 
 def append(lib, c=C, b=B, n=None, rot=None, pos=None, q=5 * A, qs=4096, k=6 * A, ks=1024, v=7 * A, vs=1024, o=8 * A, os_=4096,
            ws=A, size=BIG):
-    return lib.pp_kv8_append(r(c), r(b), r(n), r(rot), pos, q, qs, k, ks, v, vs, o, os_, ws, size, None)
+    return lib.pp_kvq_append(r(c), r(b), r(n), r(rot), pos, q, qs, k, ks, v, vs, o, os_, ws, size, None)
 
 
 def read(lib, c=C, b=B, k=6 * A, ks=1024, v=7 * A, vs=1024, ws=A, size=BIG):
-    return lib.pp_kv8_read(r(c), r(b), k, ks, v, vs, ws, size, None)
+    return lib.pp_kvq_read(r(c), r(b), k, ks, v, vs, ws, size, None)
 
 
 def attend(lib, c=C, b=B, q=5 * A, qs=4096, mask=None, words=0, scale=0.1, o=8 * A, os_=4096, ws=A, size=BIG):
-    return lib.pp_tree_attention8(r(c), r(b), q, qs, mask, words, scale, o, os_, ws, size, None)
+    return lib.pp_kvq_tree_attention(r(c), r(b), q, qs, mask, words, scale, o, os_, ws, size, None)
 
 
 def commit(lib, c=C, b=B, layers=1, ls=0, sls=0, path=A, mp=8, acc=2 * A, new=None, ws=A, size=BIG):
-    return lib.pp_kv8_commit(r(c), r(b), layers, ls, sls, path, mp, acc, new, ws, size, None)
+    return lib.pp_kvq_commit(r(c), r(b), layers, ls, sls, path, mp, acc, new, ws, size, None)
 
 
 BAD_CACHES = [(None, pp.PP_ERR_INVALID_ARG), (dict(dtype=5), pp.PP_ERR_DTYPE), (dict(n_heads=0), pp.PP_ERR_SHAPE),
@@ -78,10 +78,10 @@ def test_caches_batches_and_workspaces(lib, call):
         assert call(lib, b=None if kw is None else batch(**kw)) == want, kw
     assert call(lib, ws=0) == pp.PP_ERR_WORKSPACE
     assert call(lib, ws=A + 16) == pp.PP_ERR_WORKSPACE
-    need = lib.pp_attn8_workspace_size(r(C))
+    need = lib.pp_kvq_workspace_size(r(C))
     assert need % 256 == 0 and need > 0
     assert call(lib, size=need - 1) == pp.PP_ERR_WORKSPACE
-    assert lib.pp_attn8_workspace_size(None) == 0 and lib.pp_attn8_workspace_size(r(cache(head_dim=8))) == 0
+    assert lib.pp_kvq_workspace_size(None) == 0 and lib.pp_kvq_workspace_size(r(cache(head_dim=8))) == 0
 
 
 @pytest.mark.parametrize("call", [append, commit])
@@ -143,13 +143,13 @@ def test_binding_refuses_wrong_tensors(lib):
     ws, kv = torch.zeros(256, dtype=torch.uint8), torch.zeros((2, 2, 64), dtype=torch.bfloat16)
     for bad in (kv.float(), kv[:1], kv[:, :1]):
         with pytest.raises(pp.PPError):
-            pp.pp_kv8_read(ok, b, bad, kv.clone(), ws, stream=0)
+            pp.pp_kvq_read(ok, b, bad, kv.clone(), ws, stream=0)
         with pytest.raises(pp.PPError):
-            pp.pp_kv8_append(ok, b, None, None, None, None, kv, bad, None, ws, stream=0)
+            pp.pp_kvq_append(ok, b, None, None, None, None, kv, bad, None, ws, stream=0)
     with pytest.raises(pp.PPError):
-        pp.pp_kv8_append(ok, b, pp.HeadNorm(torch.ones(64)), None, None, None, kv, kv, None, ws, stream=0)
+        pp.pp_kvq_append(ok, b, pp.HeadNorm(torch.ones(64)), None, None, None, kv, kv, None, ws, stream=0)
     with pytest.raises(pp.PPError):
-        pp.pp_kv8_commit(ok, b, i32(0, 1)[None], i32(1, 1), ws, stream=0)
+        pp.pp_kvq_commit(ok, b, i32(0, 1)[None], i32(1, 1), ws, stream=0)
 
 
 def test_restated_codes_against_torch():

@@ -53,8 +53,8 @@ class Case8(Case):
     def run(self, pp, stream=None):
         import torch
         cache, batch, q, mask, out = self.device(pp)
-        ws = pp.alloc_attn8_workspace(cache)
-        pp.pp_tree_attention8(cache, batch, q, mask, self.scale, out, ws, stream)
+        ws = pp.alloc_kvq_workspace(cache)
+        pp.pp_kvq_tree_attention(cache, batch, q, mask, self.scale, out, ws, stream)
         torch.cuda.synchronize()
         return out.float().cpu().numpy(), pp.pp_get_device_status(ws), ws
 
@@ -190,7 +190,7 @@ def test_bits_streams_bands_and_graphs(pp, dtype, n):
     a = c.run(pp)[0]
     assert np.array_equal(a, c.run(pp)[0])
     cache, batch, q, mask, _ = c.device(pp)
-    ws = pp.alloc_attn8_workspace(cache)
+    ws = pp.alloc_kvq_workspace(cache)
     out = Guarded(tuple(q.shape), q.dtype)
     torch.cuda.synchronize()
     st = torch.cuda.Stream()
@@ -200,12 +200,12 @@ def test_bits_streams_bands_and_graphs(pp, dtype, n):
         for _ in range(20):
             busy = busy @ busy * 1e-3
         late.copy_(q)
-        pp.pp_tree_attention8(cache, batch, late, mask, c.scale, out.t, ws)
+        pp.pp_kvq_tree_attention(cache, batch, late, mask, c.scale, out.t, ws)
     torch.cuda.synchronize()
     assert np.array_equal(a, out.t.float().cpu().numpy()) and out.bands_intact()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
-        pp.pp_tree_attention8(cache, batch, q, mask, c.scale, out.t, ws)
+        pp.pp_kvq_tree_attention(cache, batch, q, mask, c.scale, out.t, ws)
     c.ctx = np.array([777, 300, 0], np.int32)
     batch.ctx_len.copy_(to_dev(c.ctx))
     graph.replay()
@@ -243,11 +243,11 @@ def test_strided_tokens(pp, dtype):
     for seqs in ([(1, 90), (1, 4)], [(3, 90), (17, 4)]):
         c = Case8(seqs, 4, 2, 64, 16, 16, dtype, mask="tree")
         cache, batch, q, mask, _ = c.device(pp)
-        ws = pp.alloc_attn8_workspace(cache)
+        ws = pp.alloc_kvq_workspace(cache)
         wide = torch.full((c.T, 8 * 64), 3.0, dtype=q.dtype, device="cuda")
         wide[:, 128:384] = q.flatten(1)
         wout = torch.full((c.T, 300 + 20), 5.0, dtype=q.dtype, device="cuda")
-        pp.pp_tree_attention8(cache, batch, wide[:, 128:384], mask, c.scale, wout[:, 32:288], ws)
+        pp.pp_kvq_tree_attention(cache, batch, wide[:, 128:384], mask, c.scale, wout[:, 32:288], ws)
         want, tol = c.want()
         got = wout.float().cpu().numpy()
         assert (np.abs(got[:, 32:288].reshape(want.shape) - want) <= tol).all()
@@ -264,7 +264,7 @@ def test_steps_of_a_decode_loop(pp, dtype):
     dt = torch.bfloat16 if dtype == "bf16" else torch.float32
     cache = pp.KVCache8.empty(3 * 8, page, heads, kv, dim, dt, block)
     table = rng.permutation(24).astype(np.int32).reshape(B, 8)
-    ws = pp.alloc_attn8_workspace(cache)
+    ws = pp.alloc_kvq_workspace(cache)
     rot = pp.Rotation.make(dim)
     gamma = torch.ones(dim, dtype=dt, device="cuda")
     norm = pp.HeadNorm(gamma, gamma)
@@ -281,11 +281,11 @@ def test_steps_of_a_decode_loop(pp, dtype):
         q, k, v = qkv[:, :heads * dim], qkv[:, heads * dim:(heads + kv) * dim], qkv[:, (heads + kv) * dim:]
         batch = pp.Batch(to_dev(starts), to_dev(ctx), to_dev(table), T)
         pos = to_dev((np.repeat(ctx, new) + depth).astype(np.int32))
-        pp.pp_kv8_append(cache, batch, norm, rot, pos, q, k, v, q, ws)
+        pp.pp_kvq_append(cache, batch, norm, rot, pos, q, k, v, q, ws)
         out = torch.empty((T, heads, dim), dtype=dt, device="cuda")
-        pp.pp_tree_attention8(cache, batch, q, None if chain else to_dev(mask.view(np.int32)), dim ** -0.5, out, ws)
+        pp.pp_kvq_tree_attention(cache, batch, q, None if chain else to_dev(mask.view(np.int32)), dim ** -0.5, out, ws)
         kr, vr = (torch.empty((T, kv, dim), dtype=dt, device="cuda") for _ in range(2))
-        pp.pp_kv8_read(cache, batch, kr, vr, ws)
+        pp.pp_kvq_read(cache, batch, kr, vr, ws)
         held = [ref.Cache(c.cpu().numpy(), s.cpu().numpy(), block) for c, s in ((cache.k, cache.k_scale), (cache.v, cache.v_scale))]
         values = [h.values() for h in held]
         want, tol = attn_ref.attend(q.float().cpu().numpy().reshape(T, heads, dim), *values, starts, ctx, table,
@@ -302,7 +302,7 @@ def test_steps_of_a_decode_loop(pp, dtype):
             path[b, :len(p)] = p
         acc = np.array([len(p) for p in paths], np.int32)
         new_len = torch.empty(B, dtype=torch.int32, device="cuda")
-        pp.pp_kv8_commit(cache, batch, to_dev(path), to_dev(acc), ws, new_len=new_len)
+        pp.pp_kvq_commit(cache, batch, to_dev(path), to_dev(acc), ws, new_len=new_len)
         for b, p in enumerate(paths):
             for h in held:
                 h.commit(table[b], int(ctx[b]), p)

@@ -105,10 +105,10 @@ class Append8(AppendCase):
         import torch
         cache = self.cache8(pp)
         batch, rot, norm = self.handles(pp)
-        ws = pp.alloc_attn8_workspace(cache)
+        ws = pp.alloc_kvq_workspace(cache)
         q = to_dev(self.q, self.dtype)
         out = torch.full_like(q, 55.0)
-        pp.pp_kv8_append(cache, batch, norm, rot, None if pos is None else to_dev(pos), q, to_dev(self.k, self.dtype),
+        pp.pp_kvq_append(cache, batch, norm, rot, None if pos is None else to_dev(pos), q, to_dev(self.k, self.dtype),
                          to_dev(self.v, self.dtype), out, ws)
         torch.cuda.synchronize()
         assert pp.pp_get_device_status(ws) == pp.PP_OK
@@ -162,7 +162,7 @@ def test_append_again_gives_the_same(pp):
     cache, batch, ws, out = c.check(pp)
     first = [t.clone() for t in (cache.k, cache.v, cache.k_scale.view(torch.int32), cache.v_scale.view(torch.int32), out)]
     _, rot, norm = c.handles(pp)
-    pp.pp_kv8_append(cache, batch, norm, rot, None, to_dev(c.q, "bf16"), to_dev(c.k, "bf16"), to_dev(c.v, "bf16"), out, ws)
+    pp.pp_kvq_append(cache, batch, norm, rot, None, to_dev(c.q, "bf16"), to_dev(c.k, "bf16"), to_dev(c.v, "bf16"), out, ws)
     again = (cache.k, cache.v, cache.k_scale.view(torch.int32), cache.v_scale.view(torch.int32), out)
     assert all(torch.equal(a, b) for a, b in zip(first, again))
 
@@ -174,13 +174,13 @@ def test_append_without_queries_and_in_place(pp):
     batch, rot, norm = c.handles(pp)
     fresh = Append8([(3, 5), (4, 0)], 4, 2, 64, 16, 16, "bf16", 64, "half", norm=True)
     other = fresh.cache8(pp)
-    pp.pp_kv8_append(other, batch, norm, rot, None, None, to_dev(c.k, "bf16"), to_dev(c.v, "bf16"), None, ws)
+    pp.pp_kvq_append(other, batch, norm, rot, None, None, to_dev(c.k, "bf16"), to_dev(c.v, "bf16"), None, ws)
     assert torch.equal(other.k, cache.k) and torch.equal(other.v, cache.v)
     # one fused projection, queries done where they lie
     other = fresh.cache8(pp)
     qkv = torch.cat([to_dev(a, "bf16").flatten(1) for a in (c.q, c.k, c.v)], 1).contiguous()
     q, k, v = qkv[:, :256], qkv[:, 256:384], qkv[:, 384:]
-    pp.pp_kv8_append(other, batch, norm, rot, None, q, k, v, q, ws)
+    pp.pp_kvq_append(other, batch, norm, rot, None, q, k, v, q, ws)
     assert torch.equal(other.k, cache.k) and torch.equal(other.v, cache.v)
     assert torch.equal(q, out.flatten(1)) and torch.equal(v, to_dev(c.v, "bf16").flatten(1))
 
@@ -215,10 +215,10 @@ def test_append_bad_lengths_and_pages(pp):
             c.starts[3] = c.T + 1
         cache = c.cache8(pp)
         batch, rot, norm = c.handles(pp)
-        ws = pp.alloc_attn8_workspace(cache)
+        ws = pp.alloc_kvq_workspace(cache)
         q, v = to_dev(c.q), to_dev(c.v)
         out = torch.full_like(q, 55.0)
-        pp.pp_kv8_append(cache, batch, norm, rot, None, q, to_dev(c.k), v, out, ws)
+        pp.pp_kvq_append(cache, batch, norm, rot, None, q, to_dev(c.k), v, out, ws)
         assert pp.pp_get_device_status(ws) == pp.PP_ERR_INVALID_ARG, how
         good = [0, 1] if how == "start_high" else [0, 2]
         for b in good:
@@ -249,11 +249,11 @@ def test_read(pp, dtype, heads, kv, dim, page, block, order):
     bad = c.pages[4, -(-133 // page) - 1]
     c.pages[4, -(-133 // page) - 1] = -1
     batch, _, _ = c.handles(pp)
-    ws = pp.alloc_attn8_workspace(cache)
+    ws = pp.alloc_kvq_workspace(cache)
     dt = torch.bfloat16 if dtype == "bf16" else torch.float32
     wide = torch.full((c.T, 2 * kv * dim + 32), 9.0, dtype=dt, device="cuda")
     ko, vo = wide[:, :kv * dim], wide[:, kv * dim + 16:2 * kv * dim + 16]
-    pp.pp_kv8_read(cache, batch, ko, vo, ws)
+    pp.pp_kvq_read(cache, batch, ko, vo, ws)
     assert pp.pp_get_device_status(ws) == pp.PP_ERR_INVALID_ARG
     got = wide.float().cpu().numpy()
     assert (got[c.used:] == 9.0).all() and (got[:, kv * dim:kv * dim + 16] == 9.0).all() and (got[:, 2 * kv * dim + 16:] == 9.0).all()
@@ -309,8 +309,8 @@ def test_commit(pp, dtype, kv, dim, page, block, order, layers):
     batch = pp.Batch(to_dev(starts), to_dev(ctx), to_dev(pages), int(starts[-1]))
     acc = np.array([len(p) for p in paths], np.int32)
     new_len = torch.full((len(n),), -1, dtype=torch.int32, device="cuda")
-    ws = pp.alloc_attn8_workspace(cache)
-    pp.pp_kv8_commit(cache, batch, to_dev(path), to_dev(acc), ws, new_len=new_len, n_layers=layers,
+    ws = pp.alloc_kvq_workspace(cache)
+    pp.pp_kvq_commit(cache, batch, to_dev(path), to_dev(acc), ws, new_len=new_len, n_layers=layers,
                      layer_stride=code[0].stride(0), scale_layer_stride=scale[0].stride(0))
     assert pp.pp_get_device_status(ws) == pp.PP_OK
     assert np.array_equal(new_len.cpu().numpy(), ctx + acc)
@@ -330,8 +330,8 @@ def test_commit_refuses_bad_paths_on_the_device(pp):
         cache = pp.KVCache8(*[to_dev(a) for a in (k.code, v.code, k.scale, v.scale)], 2, torch.float32)
         batch = pp.Batch(to_dev(np.array([0, 6, 12], np.int32)), to_dev(ctx), to_dev(pages), 12)
         new_len = torch.full((2,), -1, dtype=torch.int32, device="cuda")
-        ws = pp.alloc_attn8_workspace(cache)
-        pp.pp_kv8_commit(cache, batch, to_dev(np.array([path, [1, 2, 4]], np.int32)), to_dev(np.array([acc, 3], np.int32)), ws,
+        ws = pp.alloc_kvq_workspace(cache)
+        pp.pp_kvq_commit(cache, batch, to_dev(np.array([path, [1, 2, 4]], np.int32)), to_dev(np.array([acc, 3], np.int32)), ws,
                          new_len=new_len)
         assert pp.pp_get_device_status(ws) == pp.PP_ERR_INVALID_ARG
         assert new_len.tolist() == [20, 6]
@@ -342,14 +342,14 @@ def test_commit_refuses_bad_paths_on_the_device(pp):
 def test_nothing_to_do(pp):
     import torch
     cache = pp.KVCache8.empty(2, 16, 4, 2, 64, torch.bfloat16)
-    ws = pp.alloc_attn8_workspace(cache)
+    ws = pp.alloc_kvq_workspace(cache)
     i32 = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")
     for B, q_start in ((0, i32(1)), (2, i32(3))):
         batch = pp.Batch(q_start, i32(B), i32(B, 1), 0)
         e = torch.empty((0, 2, 64), dtype=torch.bfloat16, device="cuda")
-        pp.pp_kv8_append(cache, batch, None, None, None, None, e, e, None, ws)
-        pp.pp_kv8_read(cache, batch, e, e.clone(), ws)
-        pp.pp_kv8_commit(cache, batch, i32(B, 1), i32(B), ws)
+        pp.pp_kvq_append(cache, batch, None, None, None, None, e, e, None, ws)
+        pp.pp_kvq_read(cache, batch, e, e.clone(), ws)
+        pp.pp_kvq_commit(cache, batch, i32(B, 1), i32(B), ws)
     assert pp.pp_get_device_status(ws) == pp.PP_OK
     assert int(cache.k.sum()) == 0
 
@@ -367,12 +367,12 @@ def test_bands_and_graphs(pp, dtype):
         a.t.copy_(t)
     cache = pp.KVCache8(*[a.t for a in g[:4]], 4, dt)
     batch, rot, norm = c.handles(pp)
-    ws = pp.alloc_attn8_workspace(cache)
+    ws = pp.alloc_kvq_workspace(cache)
     q, k, v = to_dev(c.q, dtype), to_dev(c.k, dtype), to_dev(c.v, dtype)
 
     def step(cache, out, ko, vo):
-        pp.pp_kv8_append(cache, batch, norm, rot, None, q, k, v, out, ws)
-        pp.pp_kv8_read(cache, batch, ko, vo, ws)
+        pp.pp_kvq_append(cache, batch, norm, rot, None, q, k, v, out, ws)
+        pp.pp_kvq_read(cache, batch, ko, vo, ws)
     fresh = [torch.empty_like(a.t) for a in g[4:]]
     step(want, *fresh)
     step(cache, *[a.t for a in g[4:]])
