@@ -192,42 +192,62 @@ PP_DEVINL void copy_rows32(unsigned char* dst, int group, const char* base, long
     }
 }
 
-// The same for an 8-bit cache: rows of DP codes, by ordinary loads, times their
-// row's scale as bf16 (exact for scales that are powers of two).
-template <int DP>
-PP_DEVINL void widen_rows32(unsigned char* dst, int group, const char* base, long long off, float scale, int D, int lane) {
-    constexpr int kLanes = DP / 16, kPer = 32 / kLanes, kFlight = 4;  // lanes of a row, rows of the warp at once
+// An 8-bit cache: codes land by cp.async in the tile itself, each row's in the
+// back half of the places that its bf16 elements will take (chunk c of row r at
+// code_place), and are widened in place, times their row's scale (exact for
+// scales that are powers of two).  No registers are tied up by loads on their
+// way: with ordinary loads, 4 in flight a lane, 8 trees took 120 us.
+template <int DP, int BN>
+PP_DEVINL int code_place(int r, int c) {
+    if (DP == 64) return r * 128 + 64 + c * 16;
+    return (DP / 128 + (c >> 3)) * BN * 128 + r * 128 + (c & 7) * 16;
+}
+
+// One warp: 32 rows from row r0 on; off as for copy_rows32.
+template <int DP, int BN>
+PP_DEVINL void fetch_codes32(unsigned char* tile, int r0, const char* base, long long off, int D, int lane) {
+    constexpr int kLanes = DP / 16, kPer = 32 / kLanes;  // lanes of a row, rows of the warp at once
+    const int sub = lane / kLanes, c = lane % kLanes;
+#pragma unroll 2
+    for (int i = 0; i < kLanes; i++) {
+        const long long o = __shfl_sync(kFull, off, kPer * i + sub);
+        const bool in = o >= 0 && c * 16 < D;
+        cp_async_16(tile + code_place<DP, BN>(r0 + kPer * i + sub, c), in ? base + o + c * 16 : base, in ? 16u : 0u);
+    }
+}
+
+template <int DP, int BN>
+PP_DEVINL void widen_codes32(unsigned char* tile, int r0, float scale, int lane) {
+    constexpr int kLanes = DP / 16, kPer = 32 / kLanes, kFlight = 4;
     const int sub = lane / kLanes, c = lane % kLanes;
     // 16 codes are two 16-byte chunks of bf16; lanes of the tile's odd groups write theirs in the other order, so
     // that 8 lanes' stores hit all banks
-    unsigned char* col = dst + (c >> 2) * group;
     const int swap = c >> 2 & 1;
 #pragma unroll 1
     for (int i = 0; i < kLanes; i += kFlight) {
         uint4 w[kFlight];
-        float sc[kFlight];
+#pragma unroll
+        for (int k = 0; k < kFlight; k++)
+            w[k] = *reinterpret_cast<const uint4*>(tile + code_place<DP, BN>(r0 + kPer * (i + k) + sub, c));
+        __syncwarp();  // a row's codes are read before its elements are written
 #pragma unroll
         for (int k = 0; k < kFlight; k++) {
-            const int r = kPer * (i + k) + sub;
-            const long long o = __shfl_sync(kFull, off, r);
-            sc[k] = __shfl_sync(kFull, scale, r);
-            w[k] = make_uint4(0u, 0u, 0u, 0u);
-            if (o >= 0 && c * 16 < D) w[k] = *reinterpret_cast<const uint4*>(base + o + c * 16);
-        }
-#pragma unroll
-        for (int k = 0; k < kFlight; k++) {
-            const int r = kPer * (i + k) + sub;
+            const int at = kPer * (i + k) + sub, r = r0 + at;
+            const float sc = __shfl_sync(kFull, scale, at);
+            const unsigned long long sc2 = pair2(sc, sc);
             const uint32_t x[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
-            uint4 out[2];
-            uint32_t* y = reinterpret_cast<uint32_t*>(out);
+            uint32_t y[8];
 #pragma unroll
             for (int n = 0; n < 8; n++) {
                 const float2 v = from_codes(x[n / 2] >> (n % 2 * 16) & 0xffffu);
-                y[n] = pack_bf16x2(v.x * sc[k], v.y * sc[k]);
+                float a, b;
+                unpair2(mul2(pair2(v.x, v.y), sc2), a, b);
+                y[n] = pack_bf16x2(a, b);
             }
-#pragma unroll
-            for (int n = 0; n < 2; n++)
-                *reinterpret_cast<uint4*>(col + r * 128 + ((((c & 3) * 2 + (n ^ swap)) ^ (r & 7)) << 4)) = swap ? out[n ^ 1] : out[n];
+            unsigned char* row = tile + (c >> 2) * BN * 128 + r * 128;
+            const uint4 lo = make_uint4(y[0], y[1], y[2], y[3]), hi = make_uint4(y[4], y[5], y[6], y[7]);
+            *reinterpret_cast<uint4*>(row + ((((c & 3) * 2 + swap) ^ (r & 7)) << 4)) = swap ? hi : lo;
+            *reinterpret_cast<uint4*>(row + ((((c & 3) * 2 + 1 - swap) ^ (r & 7)) << 4)) = swap ? lo : hi;
         }
     }
 }
@@ -505,23 +525,34 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
             const int open = max(p.open - k0, 0);     // values from here on: not every row of the item sees them
             Item<ROWS, BN>& it = items[at.n % kItems];
             if constexpr (Q8) {
-                if (__any_sync(kFull, uses > 0 && !attn_wait(&empty[slot], (uint32_t)(uses - 1) & 1u, w))) break;
-#pragma unroll 1
-                for (int x = 0; x < BN; x += 32) {
-                    const int j = k0 + x + lane;
-                    long long off = -1;
-                    float scale = 0.f;
-                    if (x + lane < end) {
+                constexpr int kGroups = BN / 32;  // of 32 rows
+                const char* base = key ? a.cache.k : a.cache.v;
+                const float* scales = key ? a.scales.k : a.scales.v;
+                long long off[kGroups];
+                float scale[kGroups];
+#pragma unroll
+                for (int x = 0; x < kGroups; x++) {
+                    const int j = k0 + 32 * x + lane;
+                    off[x] = -1;
+                    scale[x] = 0.f;
+                    if (32 * x + lane < end) {
                         const int page = entry_page(a.batch, p.b, j);
                         if (page >= 0) {
-                            off = entry_offset(a.batch, a.cache, page, j) + (long long)p.h * a.cache.head_stride;
-                            scale = (key ? a.scales.k : a.scales.v)[scale_index(a.batch, a.scales, a.n_kv_heads, page, p.h, j)];
+                            off[x] = entry_offset(a.batch, a.cache, page, j) + (long long)p.h * a.cache.head_stride;
+                            scale[x] = scales[scale_index(a.batch, a.scales, a.n_kv_heads, page, p.h, j)];
                         } else {
                             record_status(a.status, PP_ERR_INVALID_ARG);
                         }
                     }
-                    widen_rows32<DP>(dst + x * 128, BN * 128, key ? a.cache.k : a.cache.v, off, scale, a.head_dim, lane);
                 }
+                if (__any_sync(kFull, uses > 0 && !attn_wait(&empty[slot], (uint32_t)(uses - 1) & 1u, w))) break;
+#pragma unroll
+                for (int x = 0; x < kGroups; x++) fetch_codes32<DP, BN>(dst, 32 * x, base, off[x], a.head_dim, lane);
+                cp_async_commit();
+                cp_async_wait<0>();
+                __syncwarp();
+#pragma unroll
+                for (int x = 0; x < kGroups; x++) widen_codes32<DP, BN>(dst, 32 * x, scale[x], lane);
                 __syncwarp();
                 if (!key) finite_rows<DP, BN>(dst, open, end, lane, k0, &it.odd0, &it.odd1);
                 fence_proxy_async_smem();
