@@ -1,0 +1,675 @@
+// Attention of few rows over the 8-bit cache on the tensor cores (bf16 queries,
+// e4m3 keys and values): the codes go into the products as they lie in the
+// cache, so that a step is bound by reading half the bytes of a bf16 cache.
+//
+// The other operand of each product is 16 bits wide and is split exactly, or
+// nearly so, into two e4m3 numbers: x = hi + lo / 16, hi the nearest code, lo
+// that of 16 times the rest.  A bf16 number has 8 significant bits and a code
+// 4, so hi + lo / 16 holds a query element exactly down to 2^-6 of its row's
+// scale, and to 2^-14 of it below; a softmax weight is held to 2^-8 of itself, as
+// in bf16, or 2^-20 of the largest.  The 128 rows of a product are filled with
+// those pieces: lane i of each softmax warp holds hi of row i (i < 16), lane
+// 16 + i its lo; the warps hold copies, each weighing its own 32 keys of the
+// tile (as for few rows in attn_tc.cuh).  So a tile of 128 keys costs two
+// products of 256 cycles, where reading it takes 1400.
+//
+// Scales: S = hi.k + lo.k / 16 in codes; a key's score is S times its row's and
+// its block's scale.  A weight is multiplied by its block's value scale before
+// it is split; the running base of these products (b, per row) is apart from
+// the scores' running maximum (m), since scales may differ widely between
+// blocks: w = 2^(z - m) vs 2^(m - b), and the sum of weights is that of 2^(z - m).
+//
+// Warps: four softmax, two that issue products, one that splits the rows of q,
+// one producer for each ring slot (TMA, a box a page; else cp.async), one that
+// walks the stretch.  P has columns of its own in TMEM: a score slot is free as
+// soon as its scores are in registers.
+#include "attn_tc.cuh"
+#include "pp_tc_f8.cuh"
+
+namespace pp {
+namespace {
+
+constexpr int kFewRows = 16;        // rows of an item
+constexpr float kLazy8 = 2.0f;      // growth of the base (log2) that O absorbs unscaled
+constexpr float kTopWeight = 64.f;  // the largest weight at its base, in codes: 2^kLazy8 times that stays below 448
+constexpr int kFacTiles = 8;        // tiles whose scales are held
+constexpr int kFac = 24;            // floats of a tile: 8 blocks of 16 keys each: score factor, value scale, its log2
+
+template <int DP>
+struct Few {
+    static constexpr int BN = DP == 256 ? 64 : 128, NG = DP / 128;
+    static constexpr int kSlots = DP == 256 ? 6 : 8, kSlot = BN * DP;  // even: keys and values keep to slots of their own
+    static constexpr int kQBufs = 2, kQTile = 128 * DP;
+    static constexpr int kParts = BN / 32;      // warps with keys of their own
+    static constexpr int kPitch = 128 + 4;      // floats of a staged row
+    static constexpr int kStage = 4 * kFewRows * kPitch * 4;
+    static constexpr int kSmem = kSlots * kSlot + kQBufs * kQTile + kStage + 1024;
+    static constexpr int kWarpMma = 4, kWarpQ = 6, kWarpSlot = 7, kWarps = kWarpSlot + kSlots + 1;
+    static constexpr int kReaders = kWarps - 1;
+    static constexpr uint32_t kTmemO = 2 * BN, kTmemP = 2 * BN + DP;  // two score slots, O, two weight slots
+    static_assert(kTmemP + 2 * (BN / 4) <= 512, "TMEM columns");
+    static_assert(kFacTiles >= kSlots, "a tile's scales outlive its softmax");
+};
+
+// 32 rows of DP codes into a swizzled tile, by 16-byte cp.async (as copy_rows32).
+template <int DP, int BN>
+PP_DEVINL void copy_codes32(unsigned char* tile, int r0, const char* base, long long off, int D, int lane) {
+    constexpr int kLanes = DP / 16, kPer = 32 / kLanes;
+    const int sub = lane / kLanes, c = lane % kLanes;
+#pragma unroll 2
+    for (int i = 0; i < kLanes; i++) {
+        const long long o = __shfl_sync(kFull, off, kPer * i + sub);
+        const int r = r0 + kPer * i + sub;
+        const bool in = o >= 0 && c * 16 < D;
+        cp_async_16(tile + (c >> 3) * BN * 128 + r * 128 + (((c & 7) ^ (r & 7)) << 4), in ? base + o + c * 16 : base, in ? 16u : 0u);
+    }
+}
+
+template <int DP, int BN>
+PP_DEVINL void zero_codes(unsigned char* tile, int r0, int r1, int lane) {
+#pragma unroll 1
+    for (int e = r0 * 8 + lane; e < r1 * 8; e += 32)
+#pragma unroll
+        for (int g = 0; g < DP / 128; g++) *reinterpret_cast<uint4*>(tile + g * BN * 128 + e * 16) = make_uint4(0u, 0u, 0u, 0u);
+}
+
+// NaN codes of rows [r0, r1) of a value tile set to zero, and the entries that
+// held any noted (as finite_rows).  A byte's low 7 bits are all ones exactly if
+// adding one carries into the eighth.
+template <int DP, int BN>
+PP_DEVINL void finite_codes(unsigned char* tile, int r0, int r1, int lane, int k0, int* odd0, int* odd1) {
+    auto nan_bytes = [](uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; };
+    uint32_t any = 0;
+#pragma unroll 2
+    for (int e = r0 * 8 + lane; e < r1 * 8; e += 32)
+#pragma unroll
+        for (int g = 0; g < DP / 128; g++) {
+            const uint4 v = *reinterpret_cast<const uint4*>(tile + g * BN * 128 + e * 16);
+            any |= nan_bytes(v.x) | nan_bytes(v.y) | nan_bytes(v.z) | nan_bytes(v.w);
+        }
+    if (any == 0) return;
+#pragma unroll 1
+    for (int e = r0 * 8 + lane; e < r1 * 8; e += 32) {
+        bool odd = false;
+#pragma unroll 1
+        for (int i = 0; i < 4 * (DP / 128); i++) {
+            uint32_t* w = reinterpret_cast<uint32_t*>(tile + (i >> 2) * BN * 128 + e * 16) + (i & 3);
+            const uint32_t bad = nan_bytes(*w);
+            if (!bad) continue;
+            *w &= ~((bad >> 7) * 255u);
+            odd = true;
+        }
+        if (!odd) continue;
+        atomicMin(odd0, k0 + (e >> 3));
+        atomicMax(odd1, k0 + (e >> 3) + 1);
+    }
+}
+
+// Four values as codes, and 16 times what the codes leave of them.
+PP_DEVINL void split4(const float (&x)[4], uint32_t& hi, uint32_t& lo) {
+    const uint32_t a = to_codes(x[0], x[1]), b = to_codes(x[2], x[3]);
+    const float2 va = from_codes(a), vb = from_codes(b);
+    hi = a | b << 16;
+    lo = to_codes((x[0] - va.x) * 16.f, (x[1] - va.y) * 16.f) | to_codes((x[2] - vb.x) * 16.f, (x[3] - vb.y) * 16.f) << 16;
+}
+
+template <int DP>
+__global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
+    attn8_few_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
+    using C = Few<DP>;
+    constexpr int BN = C::BN, NG = C::NG, ROWS = kFewRows, NS = C::kSlots;
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    unsigned char* ring = smem;
+    unsigned char* qs = smem + NS * C::kSlot;
+    float* stage = reinterpret_cast<float*>(qs + C::kQBufs * C::kQTile);
+    __shared__ uint64_t full[NS], empty[NS], landed[NS], qfull[2], qempty[2], sfull[2], sfree[2], pfull[2], odone[2], ffull[kFacTiles];
+    __shared__ uint32_t taddr_s;
+    __shared__ float stat_m[4][ROWS], stat_b[4][ROWS], stat_l[4][ROWS], q_scale[kItems][ROWS];
+    __shared__ __align__(16) float fac[kFacTiles][kFac];
+    __shared__ unsigned last_s;
+    __shared__ Item<ROWS, BN> items[kItems];
+    __shared__ uint64_t ifull[kItems], isplit[kItems], iempty[kItems], stretch;
+    __shared__ int tiles_s;
+    __shared__ unsigned lost_s;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const Waits w{a.status, a.timeout_ns, &lost_s};
+    pdl_launch_dependents();
+    if (tid == 0) {
+        for (int i = 0; i < NS; i++) {
+            mbar_init(&full[i], 1);
+            mbar_init(&empty[i], 1);
+            mbar_init(&landed[i], 1);
+        }
+        for (int i = 0; i < 2; i++) {
+            mbar_init(&qfull[i], 1);
+            mbar_init(&qempty[i], 1);
+            mbar_init(&sfull[i], 1);
+            mbar_init(&sfree[i], C::kParts);
+            mbar_init(&pfull[i], C::kParts);
+            mbar_init(&odone[i], 1);
+        }
+        for (int i = 0; i < kFacTiles; i++) mbar_init(&ffull[i], 1);
+        for (int i = 0; i < kItems; i++) {
+            mbar_init(&ifull[i], 1);
+            mbar_init(&isplit[i], 1);
+            mbar_init(&iempty[i], C::kReaders);
+        }
+        mbar_init(&stretch, 1);
+        lost_s = 0u;
+        fence_mbar_init();
+    }
+    if (warp == C::kWarpMma) {
+        tmem_alloc(&taddr_s, 512);
+        tmem_relinquish();
+    }
+    if (tid == C::kWarpSlot * 32 && a.box) {
+        prefetch_map(&map_k);
+        prefetch_map(&map_v);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = taddr_s;
+    pdl_wait();
+    // a wait that gives up ends the CTA's work in order, as in attn_tc_kernel
+    ItemAt<ROWS, BN> at{items, ifull, iempty, w, 0, 0, 0, 0, false};
+    int tiles = 0;
+    if (warp < C::kWarps - 1) {
+        bool lost = !attn_wait(&stretch, 0, w);
+        lost = warp < 4 ? named_bar_or(2, 128, lost) : __any_sync(kFull, lost);
+        if (!lost) tiles = tiles_s;
+    }
+    // order of the loads: K0 K1 V0 K2 V1 K3 ... (scores run two tiles ahead)
+    auto k_pos = [](int g) { return g == 0 ? 0 : 2 * g - 1; };
+    auto v_pos = [](int g) { return 2 * g + 2; };
+
+    if (warp == C::kWarps - 1) {
+        // ---------------------------------------------------------- schedule
+        Walk<ROWS, BN> walk = start_walk<ROWS, BN>(&a, lane, blockIdx.x == 0, 1);
+        if (lane == 0) {
+            tiles_s = (int)(walk.end - walk.at);
+            mbar_arrive(&stretch);
+            Part p;
+            for (int n = 0; walk.next(p); n++) {
+                Item<ROWS, BN>& it = items[n % kItems];
+                if (n >= kItems && !attn_wait(&iempty[n % kItems], (uint32_t)(n / kItems - 1) & 1u, w)) break;
+                static_cast<Part&>(it) = p;
+                it.rows = min(ROWS, p.seq.n * a.group - p.j * ROWS);
+                it.open = all_see<ROWS>(a, p);
+                it.odd0 = 0x7fffffff;
+                it.odd1 = 0;
+                mbar_arrive(&ifull[n % kItems]);
+                if (!p.whole()) it.split = Split<ROWS, BN>(walk.sched, p);
+                mbar_arrive(&isplit[n % kItems]);
+            }
+        }
+        __syncwarp();
+    } else if (tiles <= 0) {
+        // nothing for this CTA
+    } else if (warp >= C::kWarpSlot) {
+        // ------------------------------------------------- producer of one slot
+        const int slot = warp - C::kWarpSlot;
+        unsigned char* dst = ring + slot * C::kSlot;
+        at.enter(0);
+        int g_at = 0, uses = 0, fixes = 0;
+        for (int pos = slot;; pos += NS, uses++) {
+            const bool key = pos == 0 || (pos & 1);
+            const int g = pos == 0 ? 0 : key ? (pos + 1) / 2 : (pos - 2) / 2;
+            if (g >= tiles) break;
+            at.step(g - g_at, lane, true);
+            if (at.lost) break;
+            g_at = g;
+            const Item<ROWS, BN>& p = at.item();
+            const int k0 = at.t * BN;
+            const int end = min(p.key_end - k0, BN);  // rows of the tile that exist
+            const int open = max(p.open - k0, 0);     // values from here on: not every row of the item sees them
+            Item<ROWS, BN>& it = items[at.n % kItems];
+            // rows past the end: zeros (a weight of zero does not outweigh NaN); hidden ones: finite
+            const bool fix = !key && (end < BN || open < end);
+            if (a.box > 0) {
+                // boxes of 128 elements x min(page, BN) tokens
+                const int boxes = (end + a.box - 1) / a.box * NG;
+                uint64_t* bar = fix ? &landed[slot] : &full[slot];
+                const int row = lane / NG * a.box, grp = lane % NG;
+                const int in_page = (int)((unsigned)(k0 + row) % (unsigned)a.batch.page_size);
+                int page = 0;
+                if (lane < boxes) {
+                    page = entry_page(a.batch, p.b, k0 + row);
+                    if (page < 0) {  // lies past the last page: zeros
+                        record_status(a.status, PP_ERR_INVALID_ARG);
+                        page = a.batch.n_pages;
+                    }
+                }
+                if (__any_sync(kFull, uses > 0 && !attn_wait(&empty[slot], (uint32_t)(uses - 1) & 1u, w))) break;
+                if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(boxes * a.box * 128));
+                __syncwarp();
+                if (lane < boxes)
+                    tma_load_4d(dst + grp * BN * 128 + row * 128, key ? &map_k : &map_v, grp * 128, p.h, in_page, page, bar);
+            } else {
+                if (__any_sync(kFull, uses > 0 && !attn_wait(&empty[slot], (uint32_t)(uses - 1) & 1u, w))) break;
+#pragma unroll 1
+                for (int x = 0; x < BN; x += 32) {
+                    const int j = k0 + x + lane;
+                    long long off = -1;
+                    if (x + lane < end) {
+                        const int page = entry_page(a.batch, p.b, j);
+                        if (page >= 0)
+                            off = entry_offset(a.batch, a.cache, page, j) + (long long)p.h * a.cache.head_stride;
+                        else
+                            record_status(a.status, PP_ERR_INVALID_ARG);
+                    }
+                    copy_codes32<DP, BN>(dst, x, key ? a.cache.k : a.cache.v, off, a.head_dim, lane);
+                }
+                cp_async_commit();
+            }
+            if (key) {
+                // the tile's scales, keys' and values', 16 keys apart
+                float f = 1.f, lg = 0.f;
+                const int x = (lane & 7) * 16;
+                if (lane < 16 && x < end) {
+                    const int page = entry_page(a.batch, p.b, k0 + x);
+                    if (page >= 0) f = (lane < 8 ? a.scales.k : a.scales.v)[scale_index(a.batch, a.scales, a.n_kv_heads, page, p.h, k0 + x)];
+                    lg = __log2f(f);
+                }
+                float* to = fac[g % kFacTiles];
+                if (lane < 8) to[lane] = f * a.scale_log2;
+                if (lane >= 8 && lane < 16) {
+                    to[lane] = f;
+                    to[lane + 8] = lg;
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&ffull[g % kFacTiles]);
+            }
+            if (a.box > 0) {
+                if (!fix) continue;
+                if (__any_sync(kFull, !attn_wait(&landed[slot], (uint32_t)fixes++ & 1u, w))) break;
+            } else {
+                cp_async_wait<0>();
+                __syncwarp();
+            }
+            if (fix) {
+                finite_codes<DP, BN>(dst, open, end, lane, k0, &it.odd0, &it.odd1);
+                zero_codes<DP, BN>(dst, end, BN, lane);
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&full[slot]);
+        }
+    } else if (warp == C::kWarpQ) {
+        // ------------------------------------- rows of q: two pieces, four copies
+        at.enter(0);
+        bool lost = at.lost;
+        constexpr int kE = DP / 32;  // elements of a lane
+        for (int left = tiles; !lost;) {
+            const Item<ROWS, BN>& p = at.item();
+            const int n = at.n, buf = n & 1;
+            lost = __any_sync(kFull, n > 1 && !attn_wait(&qempty[buf], (uint32_t)(n / 2 - 1) & 1u, w));
+            if (lost) break;
+            const int d = lane * kE;
+#pragma unroll 4
+            for (int r = 0; r < ROWS; r++) {
+                float x[kE] = {};
+                if (r < p.rows && d < a.head_dim) {
+                    const char* src = a.q + row_offset(a, p, p.j * ROWS + r, a.q_stride, 2) + d * 2;
+                    uint32_t v[kE / 2];
+#pragma unroll
+                    for (int i = 0; i < kE / 4; i++) {
+                        const uint2 u = reinterpret_cast<const uint2*>(src)[i];
+                        v[2 * i] = u.x;
+                        v[2 * i + 1] = u.y;
+                    }
+#pragma unroll
+                    for (int i = 0; i < kE / 2; i++) {
+                        x[2 * i] = bf16lo(v[i]);
+                        x[2 * i + 1] = bf16hi(v[i]);
+                    }
+                }
+                float amax = 0.f;
+#pragma unroll
+                for (int i = 0; i < kE; i++) amax = fmaxf(amax, magnitude(x[i]));
+                const float sc = scale_for(warp_max(amax)), inv = 1.f / sc;
+                if (lane == 0) q_scale[n % kItems][r] = sc;
+#pragma unroll
+                for (int i = 0; i < kE; i += 4) {
+                    float y[4];
+#pragma unroll
+                    for (int u = 0; u < 4; u++) y[u] = to_hold(x[i + u]) * inv;
+                    uint32_t hi, lo;
+                    split4(y, hi, lo);
+                    const int e = d + i;  // element: 16-byte chunk e / 16 of group e / 128
+                    unsigned char* base = qs + buf * C::kQTile + (e >> 7) * 128 * 128 + (e & 15);
+#pragma unroll
+                    for (int c = 0; c < 4; c++) {
+                        const int rh = 32 * c + r, rl = rh + 16, ch = (e & 127) >> 4;
+                        *reinterpret_cast<uint32_t*>(base + rh * 128 + ((ch ^ (rh & 7)) << 4)) = hi;
+                        *reinterpret_cast<uint32_t*>(base + rl * 128 + ((ch ^ (rl & 7)) << 4)) = lo;
+                    }
+                }
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&qfull[buf]);
+            left -= at.t1 - at.t0;
+            if (left <= 0) break;
+            at.next(lane, true);
+            lost = at.lost;
+        }
+    } else if (warp >= C::kWarpMma) {
+        // ---------------------------------------------------------- products
+        const uint32_t id_s = idesc_f8_m128(BN, false), id_o = idesc_f8_m128(a.head_dim, true);
+        const int who = __shfl_sync(kFull, warp - C::kWarpMma, 0);
+        const bool one = lane == 0;
+        const uint32_t tm = __shfl_sync(kFull, tmem, 0);
+        const int steps = (a.head_dim + 31) / 32;  // of K = 32
+        at.enter(0);
+        auto wait_full = [&](int pos) { attn_wait(&full[pos % NS], (uint32_t)(pos / NS) & 1u, w); };
+        if (who == 0) {
+#pragma unroll 1
+            for (int g = 0; g < tiles; g++) {
+                const int buf = at.n & 1;
+                if (at.t == at.t0) attn_wait(&qfull[buf], (uint32_t)(at.n / 2) & 1u, w);
+                wait_full(k_pos(g));
+                if (g >= 2) attn_wait(&sfree[g & 1], (uint32_t)((g - 2) >> 1) & 1u, w);  // the slot's last scores have been read
+                tc_fence_after();
+                if (one) {
+                    const unsigned char* kt = ring + (k_pos(g) % NS) * C::kSlot;
+                    const unsigned char* qt = qs + buf * C::kQTile;
+#pragma unroll 1
+                    for (int d = 0; d < steps; d++) {
+                        const uint64_t ad = sdesc_sw128(qt + (d >> 2) * 128 * 128), bd = sdesc_sw128(kt + (d >> 2) * BN * 128);
+                        umma_f8(tm + (uint32_t)((g & 1) * BN), ad + 2ull * (d & 3), bd + 2ull * (d & 3), id_s, d > 0 ? 1u : 0u);
+                    }
+                    umma_commit(&sfull[g & 1]);
+                    umma_commit(&empty[k_pos(g) % NS]);
+                    if (at.t + 1 == at.t1) umma_commit(&qempty[buf]);
+                }
+                __syncwarp();
+                if (g + 1 < tiles) at.step(1, lane, true);
+            }
+        } else {
+#pragma unroll 1
+            for (int g = 0; g < tiles; g++) {
+                wait_full(v_pos(g));
+                attn_wait(&pfull[g & 1], (uint32_t)(g >> 1) & 1u, w);
+                tc_fence_after();
+                if (one) {
+                    const uint64_t vd = sdesc_sw128_n(ring + (v_pos(g) % NS) * C::kSlot, BN * 128);
+#pragma unroll
+                    for (int k = 0; k < BN / 32; k++)
+                        umma_f8_ta(tm + C::kTmemO, tm + C::kTmemP + (uint32_t)((g & 1) * (BN / 4) + 8 * k), vd + (uint64_t)(k * 256),
+                                   id_o, (at.t > at.t0 || k > 0) ? 1u : 0u);
+                    umma_commit(&odone[g & 1]);
+                    umma_commit(&empty[v_pos(g) % NS]);
+                }
+                __syncwarp();
+                if (g + 1 < tiles) at.step(1, lane, true);
+            }
+        }
+    } else {
+        // ----------------------------------------------------------- softmax
+        const int wq = warp, row = lane & 15;
+        const bool low = lane >= 16, active = wq < C::kParts;
+        const uint32_t lanes = (uint32_t)(32 * wq) << 16;
+        const uint32_t t_o = tmem + C::kTmemO + lanes, t_p = tmem + C::kTmemP + lanes;
+        const float c_own = low ? 0.0625f : 1.f, c_other = low ? 1.f : 0.0625f;
+        {  // the other warps' keys never have weight in this warp's lanes
+            const uint32_t z[8] = {};
+#pragma unroll 1
+            for (int c = 0; c < 2 * C::kParts; c++) tmem_st8(t_p + 8 * c, z);
+            tmem_st_wait();
+            tc_fence_before();
+        }
+        int g = 0;  // tile of the stretch
+        auto products_done = [&](int x) {
+            attn_wait(&odone[x & 1], (uint32_t)(x >> 1) & 1u, w);
+            tc_fence_after();
+        };
+        at.enter(0);
+        for (int left = tiles; !named_bar_or(2, 128, at.lost);) {
+            const Item<ROWS, BN>& p = at.item();
+            const int rows = p.rows;
+            const int tok = min((p.j * ROWS + row) / a.group, p.seq.n - 1);
+            const int open = p.open, t0 = at.t0, t1 = at.t1;
+            float m = -INFINITY, b = -INFINITY, sum = 0.f, qsc = 0.f;
+            // (warps without keys of their own meet the others at the part's end)
+            if (!active) g += t1 - t0;
+            for (int t = active ? t0 : t1; t < t1; t++, g++) {
+                const int sl = g & 1;
+                attn_wait(&sfull[sl], (uint32_t)(g >> 1) & 1u, w);
+                tc_fence_after();
+                uint32_t s[32];
+                tmem_ld32(tmem + (uint32_t)(sl * BN + 32 * wq) + lanes, s);
+                tmem_ld_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sfree[sl]);
+                attn_wait(&ffull[g % kFacTiles], (uint32_t)(g / kFacTiles) & 1u, w);
+                if (t == t0) qsc = q_scale[at.n % kItems][row];  // written ahead of the products
+                const float* fc = fac[g % kFacTiles] + 2 * wq;
+                const float2 fk = *reinterpret_cast<const float2*>(fc), vs = *reinterpret_cast<const float2*>(fc + 8),
+                             lv = *reinterpret_cast<const float2*>(fc + 16);
+#pragma unroll
+                for (int i = 0; i < 32; i++) {
+                    const float own = __uint_as_float(s[i]), other = __shfl_xor_sync(kFull, own, 16);
+                    s[i] = __float_as_uint(fmaf(other, c_other, own * c_own));
+                }
+                const int k0 = t * BN + 32 * wq;
+                if (k0 + 32 > open) {
+                    const uint32_t see = seen_bits(a, p, tok, k0);
+                    if (!__all_sync(kFull, see == 0xffffffffu)) {
+#pragma unroll
+                        for (int i = 0; i < 32; i++)
+                            if (!(see >> i & 1u)) s[i] = __float_as_uint(-INFINITY);
+                    }
+                }
+                const float f0 = fmaxf(fk.x * qsc, 0x1p-126f), f1 = fmaxf(fk.y * qsc, 0x1p-126f);  // > 0: -inf stays
+                float x0 = __uint_as_float(s[0]), x1 = __uint_as_float(s[16]);
+#pragma unroll
+                for (int i = 1; i < 15; i += 2) {
+                    x0 = max3(x0, __uint_as_float(s[i]), __uint_as_float(s[i + 1]));
+                    x1 = max3(x1, __uint_as_float(s[16 + i]), __uint_as_float(s[17 + i]));
+                }
+                x0 = fmaxf(x0, __uint_as_float(s[15])) * f0;
+                x1 = fmaxf(x1, __uint_as_float(s[31])) * f1;
+                // the scores' maximum moves with every tile (a register), O's base when it has to
+                const float m_new = max3(x0, x1, m), mb = m_new == -INFINITY ? 0.f : m_new;
+                sum *= ex2(m - mb);
+                m = m_new;
+                const float top = fmaxf(x0 + lv.x, x1 + lv.y);
+                const bool grow = top > b + kLazy8 || (b == -INFINITY && top > b);
+                if (t == t0) {
+                    b = top;
+                } else if (__any_sync(kFull, grow)) {
+                    products_done(g - 1);
+                    const float to = grow ? top : b;
+                    const float f = grow ? ex2(b - top) : 1.f;  // 0 from -inf
+                    b = to;
+#pragma unroll 1
+                    for (int c = 0; c < a.head_dim; c += 16) {
+                        uint32_t o[16];
+                        tmem_ld16(t_o + c, o);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 16; i++) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                        tmem_st16(t_o + c, o);
+                    }
+                }
+                const float shift = ex2(fminf(mb - (b == -INFINITY ? 0.f : b), 100.f)) * kTopWeight;
+                const float w0 = shift * vs.x, w1 = shift * vs.y;
+                unsigned long long part = 0ull;
+                uint32_t out[8];
+                const unsigned long long nb = pair2(-mb, -mb);
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const float f = i < 4 ? f0 : f1, wt = i < 4 ? w0 : w1;
+                    const unsigned long long f2 = pair2(f, f), w2 = pair2(wt, wt);
+                    float y[4];
+#pragma unroll
+                    for (int u = 0; u < 4; u += 2) {
+                        float e0, e1;
+                        unpair2(fma2(pair2(__uint_as_float(s[4 * i + u]), __uint_as_float(s[4 * i + u + 1])), f2, nb), e0, e1);
+                        const unsigned long long e = pair2(ex2(e0), ex2(e1));
+                        part = add2(part, e);
+                        unpair2(mul2(e, w2), y[u], y[u + 1]);
+                    }
+                    uint32_t hi, lo;
+                    split4(y, hi, lo);
+                    out[i] = low ? lo : hi;
+                }
+                float e0, e1;
+                unpair2(part, e0, e1);
+                sum += e0 + e1;
+                if (g >= 2) products_done(g - 2);  // the weights' slot has been read
+                tmem_st8(t_p + (uint32_t)(sl * (BN / 4) + 8 * wq), out);
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&pfull[sl]);
+            }
+            // ------------------------------------------------ end of the part
+            if (active) products_done(g - 1);
+            const bool whole = p.whole();
+            const Split<ROWS, BN>& sp = p.split;
+            float* place = nullptr;
+            if (!whole) {
+                attn_wait(&isplit[at.n % kItems], (uint32_t)(at.n / kItems) & 1u, w);
+                place = sp.place(a, blockIdx.x);
+            }
+            const int D = a.head_dim;
+            if (!low) {
+                stat_m[wq][row] = active ? m : -INFINITY;
+                stat_b[wq][row] = active ? b : -INFINITY;
+                stat_l[wq][row] = active ? sum : 0.f;
+            }
+            named_bar_sync(1, 128);
+            // written by the producers ahead of the products
+            const int odd0 = *const_cast<const volatile int*>(&p.odd0), odd1 = *const_cast<const volatile int*>(&p.odd1);
+            float top = -INFINITY, l = 0.f;
+#pragma unroll
+            for (int i = 0; i < C::kParts; i++) top = fmaxf(top, stat_m[i][row]);
+            const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+            for (int i = 0; i < C::kParts; i++) l += stat_l[i][row] * ex2(stat_m[i][row] - base);
+            const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
+            // from this copy's base (a power of two that may be far from the row's maximum: in two steps) to the row's
+            // (nothing seen: zeros; scores that are all NaN: O, which is NaN)
+            const bool none = !active || (b == -INFINITY && sum == sum);
+            const float e = b == -INFINITY ? 0.f : b - base, half = 0.5f * e;
+            const float f1 = ex2(half) * c_own * inv / kTopWeight, f2 = ex2(e - half);
+#pragma unroll 1
+            for (int c = 0; c < D; c += 128) {
+                if (active) {
+#pragma unroll 1
+                    for (int x = 0; x < 128 && c + x < D; x += 32) {
+                        uint32_t o[32];
+                        tmem_ld32(t_o + c + x, o);
+                        tmem_ld_wait();
+                        float* dst = stage + (wq * ROWS + row) * C::kPitch + x + (low ? 16 : 0);
+#pragma unroll
+                        for (int i = 0; i < 16; i++) {
+                            const float u = none ? 0.f : __uint_as_float(o[i]) * f1 * f2;
+                            const float v = none ? 0.f : __uint_as_float(o[16 + i]) * f1 * f2;
+                            const float got = __shfl_xor_sync(kFull, low ? u : v, 16);
+                            dst[i] = (low ? v : u) + got;
+                        }
+                    }
+                }
+                named_bar_sync(1, 128);
+#pragma unroll 1
+                for (int i = tid; i < rows * 16; i += 128) {
+                    const int er = i >> 4, ed = (i & 15) * 8;
+                    if (c + ed >= D) continue;
+                    float o[8] = {};
+#pragma unroll
+                    for (int x = 0; x < C::kParts; x++)
+#pragma unroll
+                        for (int k = 0; k < 8; k += 4) {
+                            const float4 v = *reinterpret_cast<const float4*>(stage + (x * ROWS + er) * C::kPitch + ed + k);
+                            o[k] += v.x;
+                            o[k + 1] += v.y;
+                            o[k + 2] += v.z;
+                            o[k + 3] += v.w;
+                        }
+                    if (odd0 < odd1) {
+                        float t[8];
+                        odd_values<true, 8>(a, p, odd0, odd1, p.j * ROWS + er, c + ed, t);
+                        for (int k = 0; k < 8; k++) o[k] += t[k];
+                    }
+                    if (whole) {
+                        *reinterpret_cast<uint4*>(a.out + row_offset(a, p, p.j * ROWS + er, a.out_stride, 2) + (c + ed) * 2) =
+                            Elem<__nv_bfloat16>::pack(o);
+                    } else {
+                        float4* dst = reinterpret_cast<float4*>(place + (size_t)er * D + c + ed);
+                        dst[0] = make_float4(o[0], o[1], o[2], o[3]);
+                        dst[1] = make_float4(o[4], o[5], o[6], o[7]);
+                    }
+                }
+                named_bar_sync(1, 128);
+            }
+            if (!whole && tid < ROWS) {
+                place[(size_t)ROWS * D + tid] = top;
+                place[(size_t)ROWS * (D + 1) + tid] = l;
+            }
+            tc_fence_before();
+            if (!whole) {
+                named_bar_sync(1, 128);
+                // (a part whose split did not come has set lost_s before the barrier)
+                if (tid == 0) last_s = !*w.lost && arrive_last(a.counters + sp.c0, (unsigned)(sp.c1 - sp.c0 + 1));
+                named_bar_sync(1, 128);
+                if (last_s) merge_few<__nv_bfloat16, ROWS, BN, 4>(a, p, sp, rows, tid, 128);
+            }
+            left -= t1 - t0;
+            if (left <= 0) break;
+            at.next(lane, true);
+        }
+    }
+    if (*w.lost)  // copies and products that may still be on their way: 1 ms is a hundred times what they take
+        for (const uint64_t t0 = globaltimer_ns(); globaltimer_ns() - t0 < 1000000ull;) __nanosleep(10000);
+    tc_fence_before();
+    __syncthreads();
+    if (warp == C::kWarpMma) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+// Codes as a 4-D tensor (element, head, offset in the page, page), boxes of 128
+// elements x `box` tokens of one head and page.
+bool code_map(CUtensorMap* map, const AttnArgs& a, const char* base) {
+    auto enc = tensor_map_encoder();
+    if (!enc) return false;
+    const cuuint64_t dims[4] = {(cuuint64_t)a.head_dim, (cuuint64_t)a.n_kv_heads, (cuuint64_t)a.batch.page_size,
+                                (cuuint64_t)a.batch.n_pages};
+    const long long steps[3] = {a.cache.head_stride, a.cache.token_stride, a.cache.page_stride};
+    cuuint64_t strides[3];
+    for (int i = 0; i < 3; i++) strides[i] = dims[i + 1] == 1 && steps[i] < 16 ? 16 : (cuuint64_t)steps[i];
+    const cuuint32_t box[4] = {128, 1, (cuuint32_t)a.box, 1};
+    const cuuint32_t estr[4] = {1, 1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<char*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int DP>
+cudaError_t few_go(AttnArgs a, int sms, cudaStream_t st) {
+    using C = Few<DP>;
+    auto* kern = attn8_few_kernel<DP>;
+    static std::atomic<bool> allowed[64];
+    cudaError_t e = allow_smem(kern, C::kSmem, allowed);
+    if (e != cudaSuccess) return e;
+    // TMA boxes where pages and key tiles divide one another; else 16-byte cp.async
+    const int ps = a.batch.page_size;
+    a.box = C::BN % ps == 0 || ps % C::BN == 0 ? (ps < C::BN ? ps : C::BN) : 0;
+    CUtensorMap mk{}, mv{};
+    if (a.box && (!code_map(&mk, a, a.cache.k) || !code_map(&mv, a, a.cache.v))) a.box = 0;
+    const unsigned grid = (unsigned)(sms < kAttnTcGrid ? sms : kAttnTcGrid);
+    return launch_overlapped(kern, dim3(grid), dim3(C::kWarps * 32), C::kSmem, st, a, mk, mv);
+}
+
+}  // namespace
+
+cudaError_t attn8_few_launch(const AttnArgs& a, int sms, cudaStream_t st) {
+    return a.head_dim <= 128 ? few_go<128>(a, sms, st) : few_go<256>(a, sms, st);
+}
+
+}  // namespace pp

@@ -1,9 +1,15 @@
 // Attention over the paged cache on the tensor cores: pages of e4m3 codes, made
-// bf16 on their way into shared memory.
+// bf16 on their way into shared memory; or, for few rows a key head, multiplied
+// as they are (attn8_few.cu).
 #include "attn_tc.cuh"
 
 namespace pp {
 
-cudaError_t attn8_tc_launch(const AttnArgs& a, int sms, cudaStream_t st) { return launch<true>(a, sms, st); }
+cudaError_t attn8_tc_launch(const AttnArgs& a, int sms, cudaStream_t st) {
+    // rows a sequence brings to a key head on average, as in attn_tc.cuh
+    const long long rows = ((long long)a.batch.n_tokens * a.group + a.batch.n_seqs - 1) / a.batch.n_seqs;
+    if (rows <= 16) return attn8_few_launch(a, sms, st);
+    return launch<true>(a, sms, st);
+}
 
 }  // namespace pp

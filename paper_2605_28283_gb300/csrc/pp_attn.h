@@ -154,5 +154,6 @@ cudaError_t attn_simt_launch(const AttnArgs& a, int sms, cudaStream_t st);  // f
 cudaError_t attn_tc_launch(const AttnArgs& a, int sms, cudaStream_t st);    // bf16
 cudaError_t attn8_simt_launch(const AttnArgs& a, int sms, cudaStream_t st);  // the same over 8-bit pages
 cudaError_t attn8_tc_launch(const AttnArgs& a, int sms, cudaStream_t st);
+cudaError_t attn8_few_launch(const AttnArgs& a, int sms, cudaStream_t st);  // bf16, few rows a key head
 
 }  // namespace pp
