@@ -8,21 +8,26 @@
 // 4, so hi + lo / 16 holds a query element exactly down to 2^-6 of its row's
 // scale, and to 2^-14 of it below; a softmax weight is held to 2^-8 of itself, as
 // in bf16, or 2^-20 of the largest.  The 128 rows of a product are filled with
-// those pieces: lane i of each softmax warp holds hi of row i (i < 16), lane
-// 16 + i its lo; the warps hold copies, each weighing its own 32 keys of the
-// tile (as for few rows in attn_tc.cuh).  So a tile of 128 keys costs two
-// products of 256 cycles, where reading it takes 1400.
+// those pieces: lane i of each quarter holds hi of row i (i < 16), lane 16 + i
+// its lo; the quarters hold copies, each with its own 32 keys of the tile (as
+// for few rows in attn_tc.cuh).  So a tile of 128 keys costs two products of 256
+// cycles, where reading it takes 1400.
 //
-// Scales: S = hi.k + lo.k / 16 in codes; a key's score is S times its row's and
-// its block's scale.  A weight is multiplied by its block's value scale before
-// it is split; the running base of these products (b, per row) is apart from
-// the scores' running maximum (m), since scales may differ widely between
-// blocks: w = 2^(z - m) vs 2^(m - b), and the sum of weights is that of 2^(z - m).
+// The two lanes of a row share its 32 keys: lane i weighs the first 16, lane
+// 16 + i the others (a scale's block each).  They hand each other the halves of
+// the scores, S = hi.k + lo.k / 16, that they need, and the codes of the weights.
 //
-// Warps: four softmax, two that issue products, one that splits the rows of q,
-// one producer for each ring slot (TMA, a box a page; else cp.async), one that
-// walks the stretch.  P has columns of its own in TMEM: a score slot is free as
-// soon as its scores are in registers.
+// Scales: a key's score is S times its row's and its block's scale.  A weight is
+// multiplied by its block's value scale before it is split; the running base of
+// these products (b, per row and quarter) is apart from the scores' running
+// maximum (m, per lane), since scales may differ widely between blocks:
+// w = 2^(z - m) vs 2^(m - b), and the sum of weights is that of 2^(z - m).
+//
+// Warps: four softmax, four that finish parts (O has two buffers for that, up to
+// 128 elements), two that issue products, one that splits the rows of q, four
+// producers of the ring (TMA, a box a page; else cp.async), one that walks the
+// stretch.  P has columns of its own in TMEM: a score slot is free as soon as its
+// scores are in registers, so one is enough beside two O.
 #include "attn_tc.cuh"
 #include "pp_tc_f8.cuh"
 
@@ -40,13 +45,14 @@ struct Few {
     static constexpr int BN = DP == 256 ? 64 : 128, NG = DP / 128;
     static constexpr int kSlots = DP == 256 ? 6 : 8, kSlot = BN * DP;  // even: keys and values keep to slots of their own
     static constexpr int kQBufs = 2, kQTile = 128 * DP;
-    static constexpr int kParts = BN / 32;      // warps with keys of their own
+    static constexpr int kParts = BN / 32;      // quarters with keys of their own
+    static constexpr int kScores = DP == 256 ? 2 : 1, kOuts = DP == 256 ? 1 : 2;  // buffers in TMEM
     static constexpr int kPitch = 128 + 4;      // floats of a staged row
     static constexpr int kStage = 4 * kFewRows * kPitch * 4;
     static constexpr int kSmem = kSlots * kSlot + kQBufs * kQTile + kStage + 1024;
-    static constexpr int kWarpMma = 4, kWarpQ = 6, kWarpSlot = 7, kWarps = kWarpSlot + kSlots + 1;
+    static constexpr int kWarpOut = 4, kWarpMma = 8, kWarpQ = 10, kWarpLoad = 11, kLoads = 4, kWarps = kWarpLoad + kLoads + 1;
     static constexpr int kReaders = kWarps - 1;
-    static constexpr uint32_t kTmemO = 2 * BN, kTmemP = 2 * BN + DP;  // two score slots, O, two weight slots
+    static constexpr uint32_t kTmemO = kScores * BN, kTmemP = kTmemO + kOuts * DP;  // scores, O, two weight slots
     static_assert(kTmemP + 2 * (BN / 4) <= 512, "TMEM columns");
     static_assert(kFacTiles >= kSlots, "a tile's scales outlive its softmax");
 };
@@ -123,9 +129,10 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
     unsigned char* ring = smem;
     unsigned char* qs = smem + NS * C::kSlot;
     float* stage = reinterpret_cast<float*>(qs + C::kQBufs * C::kQTile);
-    __shared__ uint64_t full[NS], empty[NS], landed[NS], qfull[2], qempty[2], sfull[2], sfree[2], pfull[2], odone[2], ffull[kFacTiles];
+    __shared__ uint64_t full[NS], empty[NS], landed[C::kLoads], qfull[2], qempty[2], sfull[2], sfree[2], pfull[2], odone[2], ffull[kFacTiles];
+    __shared__ uint64_t opart[2], ofull[2], ofree[2];
     __shared__ uint32_t taddr_s;
-    __shared__ float stat_m[4][ROWS], stat_b[4][ROWS], stat_l[4][ROWS], q_scale[kItems][ROWS];
+    __shared__ float stat_m[2][4][32], stat_b[2][4][32], stat_l[2][4][32], q_scale[kItems][ROWS];
     __shared__ __align__(16) float fac[kFacTiles][kFac];
     __shared__ unsigned last_s;
     __shared__ Item<ROWS, BN> items[kItems];
@@ -139,8 +146,8 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
         for (int i = 0; i < NS; i++) {
             mbar_init(&full[i], 1);
             mbar_init(&empty[i], 1);
-            mbar_init(&landed[i], 1);
         }
+        for (int i = 0; i < C::kLoads; i++) mbar_init(&landed[i], 1);
         for (int i = 0; i < 2; i++) {
             mbar_init(&qfull[i], 1);
             mbar_init(&qempty[i], 1);
@@ -148,6 +155,9 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
             mbar_init(&sfree[i], C::kParts);
             mbar_init(&pfull[i], C::kParts);
             mbar_init(&odone[i], 1);
+            mbar_init(&opart[i], 1);
+            mbar_init(&ofull[i], C::kParts);
+            mbar_init(&ofree[i], 4);
         }
         for (int i = 0; i < kFacTiles; i++) mbar_init(&ffull[i], 1);
         for (int i = 0; i < kItems; i++) {
@@ -163,7 +173,11 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
         tmem_alloc(&taddr_s, 512);
         tmem_relinquish();
     }
-    if (tid == C::kWarpSlot * 32 && a.box) {
+    // rows that an item does not fill: finite
+    for (int i = tid; i < C::kQBufs * C::kQTile / 16; i += C::kWarps * 32) reinterpret_cast<uint4*>(qs)[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (tid < kItems * ROWS) q_scale[tid / ROWS][tid % ROWS] = 1.f;
+    fence_proxy_async_smem();
+    if (tid == C::kWarpLoad * 32 && a.box) {
         prefetch_map(&map_k);
         prefetch_map(&map_v);
     }
@@ -177,7 +191,8 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
     int tiles = 0;
     if (warp < C::kWarps - 1) {
         bool lost = !attn_wait(&stretch, 0, w);
-        lost = warp < 4 ? named_bar_or(2, 128, lost) : __any_sync(kFull, lost);
+        // (warps that meet in barriers agree)
+        lost = warp < C::kWarpMma ? named_bar_or(1 + warp / 4, 128, lost) : __any_sync(kFull, lost);
         if (!lost) tiles = tiles_s;
     }
     // order of the loads: K0 K1 V0 K2 V1 K3 ... (scores run two tiles ahead)
@@ -207,94 +222,95 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
         __syncwarp();
     } else if (tiles <= 0) {
         // nothing for this CTA
-    } else if (warp >= C::kWarpSlot) {
-        // ------------------------------------------------- producer of one slot
-        const int slot = warp - C::kWarpSlot;
-        unsigned char* dst = ring + slot * C::kSlot;
+    } else if (warp >= C::kWarpLoad) {
+        // ----------------------------------- producer of every fourth load
+        const int me = warp - C::kWarpLoad;
         at.enter(0);
-        int g_at = 0, uses = 0, fixes = 0;
-        for (int pos = slot;; pos += NS, uses++) {
-            const bool key = pos == 0 || (pos & 1);
-            const int g = pos == 0 ? 0 : key ? (pos + 1) / 2 : (pos - 2) / 2;
-            if (g >= tiles) break;
+        int g_at = 0, fixes = 0, page = 0;
+        // tile of load pos; page of the lane's 16 keys of it (lanes 8 apart hold the same)
+        auto tile_of = [](int pos) { return pos == 0 ? 0 : pos & 1 ? (pos + 1) / 2 : (pos - 2) / 2; };
+        auto go_to = [&](int pos) {
+            const int g = tile_of(pos);
+            if (g >= tiles) return false;
             at.step(g - g_at, lane, true);
-            if (at.lost) break;
+            if (at.lost) return false;
             g_at = g;
+            const int k = at.t * BN + (lane & 7) * 16;
+            page = (lane & 7) * 16 < BN && k < at.item().key_end ? entry_page(a.batch, at.item().b, k) : 0;
+            return true;
+        };
+        bool more = go_to(me);
+        for (int pos = me; more; pos += C::kLoads) {
+            const int slot = pos % NS, g = g_at;
+            unsigned char* dst = ring + slot * C::kSlot;
+            const bool key = pos == 0 || (pos & 1);
             const Item<ROWS, BN>& p = at.item();
-            const int k0 = at.t * BN;
+            const int k0 = at.t * BN, h = p.h;
             const int end = min(p.key_end - k0, BN);  // rows of the tile that exist
             const int open = max(p.open - k0, 0);     // values from here on: not every row of the item sees them
-            Item<ROWS, BN>& it = items[at.n % kItems];
+            // the tile's scales, keys' (lanes 0 to 7) and values' (8 to 15), on their way while the slot is waited for
+            float f = 1.f;
+            const int x = (lane & 7) * 16;
+            if (key && lane < 16 && x < end && page >= 0)
+                f = (lane < 8 ? a.scales.k : a.scales.v)[scale_index(a.batch, a.scales, a.n_kv_heads, page, h, k0 + x)];
+            if (page < 0) record_status(a.status, PP_ERR_INVALID_ARG);
+            if (__any_sync(kFull, pos >= NS && !attn_wait(&empty[slot], (uint32_t)(pos / NS - 1) & 1u, w))) break;
             // rows past the end: zeros (a weight of zero does not outweigh NaN); hidden ones: finite
             const bool fix = !key && (end < BN || open < end);
             if (a.box > 0) {
                 // boxes of 128 elements x min(page, BN) tokens
                 const int boxes = (end + a.box - 1) / a.box * NG;
-                uint64_t* bar = fix ? &landed[slot] : &full[slot];
+                uint64_t* bar = fix ? &landed[me] : &full[slot];
                 const int row = lane / NG * a.box, grp = lane % NG;
                 const int in_page = (int)((unsigned)(k0 + row) % (unsigned)a.batch.page_size);
-                int page = 0;
-                if (lane < boxes) {
-                    page = entry_page(a.batch, p.b, k0 + row);
-                    if (page < 0) {  // lies past the last page: zeros
-                        record_status(a.status, PP_ERR_INVALID_ARG);
-                        page = a.batch.n_pages;
-                    }
-                }
-                if (__any_sync(kFull, uses > 0 && !attn_wait(&empty[slot], (uint32_t)(uses - 1) & 1u, w))) break;
+                const int of = __shfl_sync(kFull, page, (row >> 4) & 7);
                 if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(boxes * a.box * 128));
                 __syncwarp();
-                if (lane < boxes)
-                    tma_load_4d(dst + grp * BN * 128 + row * 128, key ? &map_k : &map_v, grp * 128, p.h, in_page, page, bar);
+                if (lane < boxes)  // a page that does not exist lies past the last one: zeros
+                    tma_load_4d(dst + grp * BN * 128 + row * 128, key ? &map_k : &map_v, grp * 128, h, in_page,
+                                of < 0 ? a.batch.n_pages : of, bar);
             } else {
-                if (__any_sync(kFull, uses > 0 && !attn_wait(&empty[slot], (uint32_t)(uses - 1) & 1u, w))) break;
 #pragma unroll 1
-                for (int x = 0; x < BN; x += 32) {
-                    const int j = k0 + x + lane;
-                    long long off = -1;
-                    if (x + lane < end) {
-                        const int page = entry_page(a.batch, p.b, j);
-                        if (page >= 0)
-                            off = entry_offset(a.batch, a.cache, page, j) + (long long)p.h * a.cache.head_stride;
-                        else
-                            record_status(a.status, PP_ERR_INVALID_ARG);
-                    }
-                    copy_codes32<DP, BN>(dst, x, key ? a.cache.k : a.cache.v, off, a.head_dim, lane);
+                for (int r0 = 0; r0 < BN; r0 += 32) {
+                    const int of = __shfl_sync(kFull, page, (r0 + lane) >> 4 & 7);
+                    const long long off = r0 + lane < end && of >= 0
+                        ? entry_offset(a.batch, a.cache, of, k0 + r0 + lane) + (long long)h * a.cache.head_stride : -1;
+                    copy_codes32<DP, BN>(dst, r0, key ? a.cache.k : a.cache.v, off, a.head_dim, lane);
                 }
                 cp_async_commit();
             }
-            if (key) {
-                // the tile's scales, keys' and values', 16 keys apart
-                float f = 1.f, lg = 0.f;
-                const int x = (lane & 7) * 16;
-                if (lane < 16 && x < end) {
-                    const int page = entry_page(a.batch, p.b, k0 + x);
-                    if (page >= 0) f = (lane < 8 ? a.scales.k : a.scales.v)[scale_index(a.batch, a.scales, a.n_kv_heads, page, p.h, k0 + x)];
-                    lg = __log2f(f);
+            if (!key || a.box == 0) {
+                // landed, and mended where it has to be
+                bool gone = false;
+                if (a.box == 0) {
+                    cp_async_wait<0>();
+                    __syncwarp();
+                } else if (fix) {
+                    gone = __any_sync(kFull, !attn_wait(&landed[me], (uint32_t)fixes++ & 1u, w));
                 }
+                if (gone) break;
+                if (fix) {
+                    Item<ROWS, BN>& it = items[at.n % kItems];
+                    finite_codes<DP, BN>(dst, open, end, lane, k0, &it.odd0, &it.odd1);
+                    zero_codes<DP, BN>(dst, end, BN, lane);
+                }
+                if (a.box == 0 || fix) {
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&full[slot]);
+                }
+            }
+            more = go_to(pos + C::kLoads);
+            if (key) {
                 float* to = fac[g % kFacTiles];
                 if (lane < 8) to[lane] = f * a.scale_log2;
                 if (lane >= 8 && lane < 16) {
                     to[lane] = f;
-                    to[lane + 8] = lg;
+                    to[lane + 8] = __log2f(f);
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&ffull[g % kFacTiles]);
             }
-            if (a.box > 0) {
-                if (!fix) continue;
-                if (__any_sync(kFull, !attn_wait(&landed[slot], (uint32_t)fixes++ & 1u, w))) break;
-            } else {
-                cp_async_wait<0>();
-                __syncwarp();
-            }
-            if (fix) {
-                finite_codes<DP, BN>(dst, open, end, lane, k0, &it.odd0, &it.odd1);
-                zero_codes<DP, BN>(dst, end, BN, lane);
-            }
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&full[slot]);
         }
     } else if (warp == C::kWarpQ) {
         // ------------------------------------- rows of q: two pieces, four copies
@@ -308,9 +324,9 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
             if (lost) break;
             const int d = lane * kE;
 #pragma unroll 4
-            for (int r = 0; r < ROWS; r++) {
+            for (int r = 0; r < p.rows; r++) {
                 float x[kE] = {};
-                if (r < p.rows && d < a.head_dim) {
+                if (d < a.head_dim) {
                     const char* src = a.q + row_offset(a, p, p.j * ROWS + r, a.q_stride, 2) + d * 2;
                     uint32_t v[kE / 2];
 #pragma unroll
@@ -370,7 +386,8 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
                 const int buf = at.n & 1;
                 if (at.t == at.t0) attn_wait(&qfull[buf], (uint32_t)(at.n / 2) & 1u, w);
                 wait_full(k_pos(g));
-                if (g >= 2) attn_wait(&sfree[g & 1], (uint32_t)((g - 2) >> 1) & 1u, w);  // the slot's last scores have been read
+                const int sl = g % C::kScores;
+                if (g >= C::kScores) attn_wait(&sfree[sl], (uint32_t)(g / C::kScores - 1) & 1u, w);  // the slot's last scores have been read
                 tc_fence_after();
                 if (one) {
                     const unsigned char* kt = ring + (k_pos(g) % NS) * C::kSlot;
@@ -378,9 +395,9 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
 #pragma unroll 1
                     for (int d = 0; d < steps; d++) {
                         const uint64_t ad = sdesc_sw128(qt + (d >> 2) * 128 * 128), bd = sdesc_sw128(kt + (d >> 2) * BN * 128);
-                        umma_f8(tm + (uint32_t)((g & 1) * BN), ad + 2ull * (d & 3), bd + 2ull * (d & 3), id_s, d > 0 ? 1u : 0u);
+                        umma_f8(tm + (uint32_t)(sl * BN), ad + 2ull * (d & 3), bd + 2ull * (d & 3), id_s, d > 0 ? 1u : 0u);
                     }
-                    umma_commit(&sfull[g & 1]);
+                    umma_commit(&sfull[sl]);
                     umma_commit(&empty[k_pos(g) % NS]);
                     if (at.t + 1 == at.t1) umma_commit(&qempty[buf]);
                 }
@@ -397,164 +414,188 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
                     const uint64_t vd = sdesc_sw128_n(ring + (v_pos(g) % NS) * C::kSlot, BN * 128);
 #pragma unroll
                     for (int k = 0; k < BN / 32; k++)
-                        umma_f8_ta(tm + C::kTmemO, tm + C::kTmemP + (uint32_t)((g & 1) * (BN / 4) + 8 * k), vd + (uint64_t)(k * 256),
+                        umma_f8_ta(tm + C::kTmemO + (uint32_t)(at.n % C::kOuts * DP), tm + C::kTmemP + (uint32_t)((g & 1) * (BN / 4) + 8 * k), vd + (uint64_t)(k * 256),
                                    id_o, (at.t > at.t0 || k > 0) ? 1u : 0u);
                     umma_commit(&odone[g & 1]);
+                    if (at.t + 1 == at.t1) umma_commit(&opart[at.n % C::kOuts]);
                     umma_commit(&empty[v_pos(g) % NS]);
                 }
                 __syncwarp();
                 if (g + 1 < tiles) at.step(1, lane, true);
             }
         }
-    } else {
+    } else if (warp < C::kWarpOut) {
         // ----------------------------------------------------------- softmax
         const int wq = warp, row = lane & 15;
-        const bool low = lane >= 16, active = wq < C::kParts;
+        const bool low = lane >= 16;
         const uint32_t lanes = (uint32_t)(32 * wq) << 16;
-        const uint32_t t_o = tmem + C::kTmemO + lanes, t_p = tmem + C::kTmemP + lanes;
+        const uint32_t t_p = tmem + C::kTmemP + lanes;
         const float c_own = low ? 0.0625f : 1.f, c_other = low ? 1.f : 0.0625f;
-        {  // the other warps' keys never have weight in this warp's lanes
+        {  // the other quarters' keys never have weight in this one's lanes
             const uint32_t z[8] = {};
 #pragma unroll 1
             for (int c = 0; c < 2 * C::kParts; c++) tmem_st8(t_p + 8 * c, z);
             tmem_st_wait();
             tc_fence_before();
         }
+        // every quarter's lanes are zero ahead of the first products
+        named_bar_sync(1, 128);
         int g = 0;  // tile of the stretch
         auto products_done = [&](int x) {
             attn_wait(&odone[x & 1], (uint32_t)(x >> 1) & 1u, w);
             tc_fence_after();
         };
-        at.enter(0);
-        for (int left = tiles; !named_bar_or(2, 128, at.lost);) {
+        if (wq < C::kParts) at.enter(0);
+        for (int left = tiles; wq < C::kParts && !at.lost;) {
             const Item<ROWS, BN>& p = at.item();
-            const int rows = p.rows;
             const int tok = min((p.j * ROWS + row) / a.group, p.seq.n - 1);
-            const int open = p.open, t0 = at.t0, t1 = at.t1;
+            const int open = p.open, t0 = at.t0, t1 = at.t1, ob = at.n % C::kOuts;
+            const uint32_t t_o = tmem + C::kTmemO + (uint32_t)(ob * DP) + lanes;
             float m = -INFINITY, b = -INFINITY, sum = 0.f, qsc = 0.f;
-            // (warps without keys of their own meet the others at the part's end)
-            if (!active) g += t1 - t0;
-            for (int t = active ? t0 : t1; t < t1; t++, g++) {
-                const int sl = g & 1;
-                attn_wait(&sfull[sl], (uint32_t)(g >> 1) & 1u, w);
+            // the buffer's last part has been read
+            if (at.n >= C::kOuts) attn_wait(&ofree[ob], (uint32_t)(at.n / C::kOuts - 1) & 1u, w);
+            for (int t = t0; t < t1; t++, g++) {
+                const int sl = g % C::kScores;
+                attn_wait(&sfull[sl], (uint32_t)(g / C::kScores) & 1u, w);
                 tc_fence_after();
-                uint32_t s[32];
-                tmem_ld32(tmem + (uint32_t)(sl * BN + 32 * wq) + lanes, s);
+                uint32_t u[32];
+                tmem_ld32(tmem + (uint32_t)(sl * BN + 32 * wq) + lanes, u);
                 tmem_ld_wait();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sfree[sl]);
                 attn_wait(&ffull[g % kFacTiles], (uint32_t)(g / kFacTiles) & 1u, w);
                 if (t == t0) qsc = q_scale[at.n % kItems][row];  // written ahead of the products
-                const float* fc = fac[g % kFacTiles] + 2 * wq;
-                const float2 fk = *reinterpret_cast<const float2*>(fc), vs = *reinterpret_cast<const float2*>(fc + 8),
-                             lv = *reinterpret_cast<const float2*>(fc + 16);
+                const float* fc = fac[g % kFacTiles] + 2 * wq + (low ? 1 : 0);
+                const float f = fmaxf(fc[0] * qsc, 0x1p-126f), vs = fc[8], lv = fc[16];  // f > 0: -inf stays
+                float s[16];
 #pragma unroll
-                for (int i = 0; i < 32; i++) {
-                    const float own = __uint_as_float(s[i]), other = __shfl_xor_sync(kFull, own, 16);
-                    s[i] = __float_as_uint(fmaf(other, c_other, own * c_own));
+                for (int i = 0; i < 16; i++) {
+                    const float own = __uint_as_float(low ? u[16 + i] : u[i]);
+                    const float other = __shfl_xor_sync(kFull, __uint_as_float(low ? u[i] : u[16 + i]), 16);
+                    s[i] = fmaf(other, c_other, own * c_own);
                 }
                 const int k0 = t * BN + 32 * wq;
                 if (k0 + 32 > open) {
-                    const uint32_t see = seen_bits(a, p, tok, k0);
-                    if (!__all_sync(kFull, see == 0xffffffffu)) {
+                    const uint32_t see = seen_bits(a, p, tok, k0) >> (low ? 16 : 0);
 #pragma unroll
-                        for (int i = 0; i < 32; i++)
-                            if (!(see >> i & 1u)) s[i] = __float_as_uint(-INFINITY);
-                    }
+                    for (int i = 0; i < 16; i++)
+                        if (!(see >> i & 1u)) s[i] = -INFINITY;
                 }
-                const float f0 = fmaxf(fk.x * qsc, 0x1p-126f), f1 = fmaxf(fk.y * qsc, 0x1p-126f);  // > 0: -inf stays
-                float x0 = __uint_as_float(s[0]), x1 = __uint_as_float(s[16]);
-#pragma unroll
-                for (int i = 1; i < 15; i += 2) {
-                    x0 = max3(x0, __uint_as_float(s[i]), __uint_as_float(s[i + 1]));
-                    x1 = max3(x1, __uint_as_float(s[16 + i]), __uint_as_float(s[17 + i]));
-                }
-                x0 = fmaxf(x0, __uint_as_float(s[15])) * f0;
-                x1 = fmaxf(x1, __uint_as_float(s[31])) * f1;
+                float x0 = max3(s[0], s[1], s[2]), x1 = max3(s[3], s[4], s[5]);
+                x0 = max3(x0, s[6], s[7]);
+                x1 = max3(x1, s[8], s[9]);
+                x0 = max3(x0, s[10], s[11]);
+                x1 = max3(x1, s[12], s[13]);
+                const float x = max3(fmaxf(x0, x1), s[14], s[15]) * f;
                 // the scores' maximum moves with every tile (a register), O's base when it has to
-                const float m_new = max3(x0, x1, m), mb = m_new == -INFINITY ? 0.f : m_new;
+                const float m_new = fmaxf(x, m), mb = m_new == -INFINITY ? 0.f : m_new;
                 sum *= ex2(m - mb);
                 m = m_new;
-                const float top = fmaxf(x0 + lv.x, x1 + lv.y);
+                float top = x + lv;
+                top = fmaxf(top, __shfl_xor_sync(kFull, top, 16));
                 const bool grow = top > b + kLazy8 || (b == -INFINITY && top > b);
                 if (t == t0) {
                     b = top;
                 } else if (__any_sync(kFull, grow)) {
                     products_done(g - 1);
-                    const float to = grow ? top : b;
-                    const float f = grow ? ex2(b - top) : 1.f;  // 0 from -inf
-                    b = to;
+                    const float fo = grow ? ex2(b - top) : 1.f;  // 0 from -inf
+                    b = grow ? top : b;
 #pragma unroll 1
                     for (int c = 0; c < a.head_dim; c += 16) {
                         uint32_t o[16];
                         tmem_ld16(t_o + c, o);
                         tmem_ld_wait();
 #pragma unroll
-                        for (int i = 0; i < 16; i++) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                        for (int i = 0; i < 16; i++) o[i] = __float_as_uint(__uint_as_float(o[i]) * fo);
                         tmem_st16(t_o + c, o);
                     }
                 }
-                const float shift = ex2(fminf(mb - (b == -INFINITY ? 0.f : b), 100.f)) * kTopWeight;
-                const float w0 = shift * vs.x, w1 = shift * vs.y;
+                const float weight = ex2(fminf(mb - (b == -INFINITY ? 0.f : b), 100.f)) * kTopWeight * vs;
+                const unsigned long long f2 = pair2(f, f), w2 = pair2(weight, weight), nb = pair2(-mb, -mb);
                 unsigned long long part = 0ull;
-                uint32_t out[8];
-                const unsigned long long nb = pair2(-mb, -mb);
+                uint32_t hi[4], lo[4];
 #pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    const float f = i < 4 ? f0 : f1, wt = i < 4 ? w0 : w1;
-                    const unsigned long long f2 = pair2(f, f), w2 = pair2(wt, wt);
+                for (int i = 0; i < 4; i++) {
                     float y[4];
 #pragma unroll
-                    for (int u = 0; u < 4; u += 2) {
+                    for (int v = 0; v < 4; v += 2) {
                         float e0, e1;
-                        unpair2(fma2(pair2(__uint_as_float(s[4 * i + u]), __uint_as_float(s[4 * i + u + 1])), f2, nb), e0, e1);
+                        unpair2(fma2(pair2(s[4 * i + v], s[4 * i + v + 1]), f2, nb), e0, e1);
                         const unsigned long long e = pair2(ex2(e0), ex2(e1));
                         part = add2(part, e);
-                        unpair2(mul2(e, w2), y[u], y[u + 1]);
+                        unpair2(mul2(e, w2), y[v], y[v + 1]);
                     }
-                    uint32_t hi, lo;
-                    split4(y, hi, lo);
-                    out[i] = low ? lo : hi;
+                    split4(y, hi[i], lo[i]);
                 }
                 float e0, e1;
                 unpair2(part, e0, e1);
                 sum += e0 + e1;
+                // a row's first lane stores hi of all 32 keys, its second lo
+                uint32_t out[8];
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const uint32_t got = __shfl_xor_sync(kFull, low ? hi[i] : lo[i], 16);
+                    out[i] = low ? got : hi[i];
+                    out[4 + i] = low ? lo[i] : got;
+                }
                 if (g >= 2) products_done(g - 2);  // the weights' slot has been read
-                tmem_st8(t_p + (uint32_t)(sl * (BN / 4) + 8 * wq), out);
+                tmem_st8(t_p + (uint32_t)((g & 1) * (BN / 4) + 8 * wq), out);
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&pfull[sl]);
+                if (lane == 0) mbar_arrive(&pfull[g & 1]);
             }
-            // ------------------------------------------------ end of the part
-            if (active) products_done(g - 1);
+            stat_m[ob][wq][lane] = m;
+            stat_b[ob][wq][lane] = b;
+            stat_l[ob][wq][lane] = sum;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&ofull[ob]);
+            left -= t1 - t0;
+            if (left <= 0) break;
+            at.next(lane, true);
+        }
+        // (quarters without keys free the parts all the same)
+        if (wq >= C::kParts) {
+            at.enter(0);
+            for (int left = tiles - (at.t1 - at.t0); left > 0 && !at.lost; left -= at.t1 - at.t0) at.next(lane, true);
+        }
+    } else {
+        // ------------------------------------------------------- ends of parts
+        const int wq = warp - C::kWarpOut, row = lane & 15, otid = tid - 32 * C::kWarpOut;
+        const bool low = lane >= 16, active = wq < C::kParts;
+        const uint32_t lanes = (uint32_t)(32 * wq) << 16;
+        const float c_own = low ? 0.0625f : 1.f;
+        const int D = a.head_dim;
+        at.enter(0);
+        for (int left = tiles; !named_bar_or(2, 128, at.lost);) {
+            const Item<ROWS, BN>& p = at.item();
+            const int rows = p.rows, ob = at.n % C::kOuts;
+            const uint32_t t_o = tmem + C::kTmemO + (uint32_t)(ob * DP) + lanes, par = (uint32_t)(at.n / C::kOuts) & 1u;
+            attn_wait(&ofull[ob], par, w);
+            attn_wait(&opart[ob], par, w);
+            tc_fence_after();
             const bool whole = p.whole();
+            // written by the producers ahead of the products
+            const int odd0 = *const_cast<const volatile int*>(&p.odd0), odd1 = *const_cast<const volatile int*>(&p.odd1);
             const Split<ROWS, BN>& sp = p.split;
             float* place = nullptr;
             if (!whole) {
                 attn_wait(&isplit[at.n % kItems], (uint32_t)(at.n / kItems) & 1u, w);
                 place = sp.place(a, blockIdx.x);
             }
-            const int D = a.head_dim;
-            if (!low) {
-                stat_m[wq][row] = active ? m : -INFINITY;
-                stat_b[wq][row] = active ? b : -INFINITY;
-                stat_l[wq][row] = active ? sum : 0.f;
-            }
-            named_bar_sync(1, 128);
-            // written by the producers ahead of the products
-            const int odd0 = *const_cast<const volatile int*>(&p.odd0), odd1 = *const_cast<const volatile int*>(&p.odd1);
             float top = -INFINITY, l = 0.f;
 #pragma unroll
-            for (int i = 0; i < C::kParts; i++) top = fmaxf(top, stat_m[i][row]);
+            for (int i = 0; i < C::kParts; i++) top = max3(top, stat_m[ob][i][row], stat_m[ob][i][row + 16]);
             const float base = top == -INFINITY ? 0.f : top;
 #pragma unroll
-            for (int i = 0; i < C::kParts; i++) l += stat_l[i][row] * ex2(stat_m[i][row] - base);
+            for (int i = 0; i < C::kParts; i++)
+                l += stat_l[ob][i][row] * ex2(stat_m[ob][i][row] - base) + stat_l[ob][i][row + 16] * ex2(stat_m[ob][i][row + 16] - base);
             const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
             // from this copy's base (a power of two that may be far from the row's maximum: in two steps) to the row's
             // (nothing seen: zeros; scores that are all NaN: O, which is NaN)
-            const bool none = !active || (b == -INFINITY && sum == sum);
+            const float b = stat_b[ob][wq][lane], both = stat_l[ob][wq][row] + stat_l[ob][wq][row + 16];
+            const bool none = !active || (b == -INFINITY && both == both);
             const float e = b == -INFINITY ? 0.f : b - base, half = 0.5f * e;
             const float f1 = ex2(half) * c_own * inv / kTopWeight, f2 = ex2(e - half);
 #pragma unroll 1
@@ -575,9 +616,14 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
                         }
                     }
                 }
-                named_bar_sync(1, 128);
+                if (c + 128 >= D) {  // O and the statistics have been read
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&ofree[ob]);
+                }
+                named_bar_sync(2, 128);
 #pragma unroll 1
-                for (int i = tid; i < rows * 16; i += 128) {
+                for (int i = otid; i < rows * 16; i += 128) {
                     const int er = i >> 4, ed = (i & 15) * 8;
                     if (c + ed >= D) continue;
                     float o[8] = {};
@@ -605,21 +651,20 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
                         dst[1] = make_float4(o[4], o[5], o[6], o[7]);
                     }
                 }
-                named_bar_sync(1, 128);
+                if (c + 128 < D) named_bar_sync(2, 128);  // (the next part's barrier otherwise)
             }
-            if (!whole && tid < ROWS) {
-                place[(size_t)ROWS * D + tid] = top;
-                place[(size_t)ROWS * (D + 1) + tid] = l;
+            if (!whole && otid < ROWS) {
+                place[(size_t)ROWS * D + otid] = top;
+                place[(size_t)ROWS * (D + 1) + otid] = l;
             }
-            tc_fence_before();
             if (!whole) {
-                named_bar_sync(1, 128);
+                named_bar_sync(2, 128);
                 // (a part whose split did not come has set lost_s before the barrier)
-                if (tid == 0) last_s = !*w.lost && arrive_last(a.counters + sp.c0, (unsigned)(sp.c1 - sp.c0 + 1));
-                named_bar_sync(1, 128);
-                if (last_s) merge_few<__nv_bfloat16, ROWS, BN, 4>(a, p, sp, rows, tid, 128);
+                if (otid == 0) last_s = !*w.lost && arrive_last(a.counters + sp.c0, (unsigned)(sp.c1 - sp.c0 + 1));
+                named_bar_sync(2, 128);
+                if (last_s) merge_few<__nv_bfloat16, ROWS, BN, 4>(a, p, sp, rows, otid, 128);
             }
-            left -= t1 - t0;
+            left -= at.t1 - at.t0;
             if (left <= 0) break;
             at.next(lane, true);
         }
