@@ -129,7 +129,7 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
     unsigned char* ring = smem;
     unsigned char* qs = smem + NS * C::kSlot;
     float* stage = reinterpret_cast<float*>(qs + C::kQBufs * C::kQTile);
-    __shared__ uint64_t full[NS], empty[NS], landed[C::kLoads], qfull[2], qempty[2], sfull[2], sfree[2], pfull[2], odone[2], ffull[kFacTiles];
+    __shared__ uint64_t full[NS], empty[NS], landed[C::kLoads], qfull[2], qempty[2], sfull[2], sfree[2], pfull[2], odone[2];
     __shared__ uint64_t opart[2], ofull[2], ofree[2];
     __shared__ uint32_t taddr_s;
     __shared__ float stat_m[2][4][32], stat_b[2][4][32], stat_l[2][4][32], q_scale[kItems][ROWS];
@@ -159,7 +159,6 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
             mbar_init(&ofull[i], C::kParts);
             mbar_init(&ofree[i], 4);
         }
-        for (int i = 0; i < kFacTiles; i++) mbar_init(&ffull[i], 1);
         for (int i = 0; i < kItems; i++) {
             mbar_init(&ifull[i], 1);
             mbar_init(&isplit[i], 1);
@@ -239,6 +238,15 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
             page = (lane & 7) * 16 < BN && k < at.item().key_end ? entry_page(a.batch, at.item().b, k) : 0;
             return true;
         };
+        auto put_scales = [&](int g, float f) {
+            float* to = fac[g % kFacTiles];
+            if (lane < 8) to[lane] = f * a.scale_log2;
+            if (lane >= 8 && lane < 16) {
+                to[lane] = f;
+                to[lane + 8] = __log2f(f);
+            }
+            __syncwarp();
+        };
         bool more = go_to(me);
         for (int pos = me; more; pos += C::kLoads) {
             const int slot = pos % NS, g = g_at;
@@ -264,11 +272,12 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
                 const int row = lane / NG * a.box, grp = lane % NG;
                 const int in_page = (int)((unsigned)(k0 + row) % (unsigned)a.batch.page_size);
                 const int of = __shfl_sync(kFull, page, (row >> 4) & 7);
-                if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(boxes * a.box * 128));
-                __syncwarp();
                 if (lane < boxes)  // a page that does not exist lies past the last one: zeros
                     tma_load_4d(dst + grp * BN * 128 + row * 128, key ? &map_k : &map_v, grp * 128, h, in_page,
                                 of < 0 ? a.batch.n_pages : of, bar);
+                if (key) put_scales(g, f);
+                // (bytes may have landed before they are expected: the phase waits for this arrival)
+                if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(boxes * a.box * 128));
             } else {
 #pragma unroll 1
                 for (int r0 = 0; r0 < BN; r0 += 32) {
@@ -278,6 +287,7 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
                     copy_codes32<DP, BN>(dst, r0, key ? a.cache.k : a.cache.v, off, a.head_dim, lane);
                 }
                 cp_async_commit();
+                if (key) put_scales(g, f);
             }
             if (!key || a.box == 0) {
                 // landed, and mended where it has to be
@@ -301,67 +311,66 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
                 }
             }
             more = go_to(pos + C::kLoads);
-            if (key) {
-                float* to = fac[g % kFacTiles];
-                if (lane < 8) to[lane] = f * a.scale_log2;
-                if (lane >= 8 && lane < 16) {
-                    to[lane] = f;
-                    to[lane + 8] = __log2f(f);
-                }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&ffull[g % kFacTiles]);
-            }
         }
     } else if (warp == C::kWarpQ) {
         // ------------------------------------- rows of q: two pieces, four copies
         at.enter(0);
         bool lost = at.lost;
-        constexpr int kE = DP / 32;  // elements of a lane
+        constexpr int kE = DP / 32, kAhead = 4;  // elements of a lane, rows on their way
+        const int d = lane * kE;
+        auto fetch = [&](const Item<ROWS, BN>& p, int r, uint2 (&v)[kE / 4]) {
+#pragma unroll
+            for (int i = 0; i < kE / 4; i++) v[i] = make_uint2(0u, 0u);
+            if (r >= p.rows || d >= a.head_dim) return;
+            const uint2* src = reinterpret_cast<const uint2*>(a.q + row_offset(a, p, p.j * ROWS + r, a.q_stride, 2) + d * 2);
+#pragma unroll
+            for (int i = 0; i < kE / 4; i++) v[i] = src[i];
+        };
         for (int left = tiles; !lost;) {
             const Item<ROWS, BN>& p = at.item();
             const int n = at.n, buf = n & 1;
+            uint2 v[kAhead][kE / 4];
+#pragma unroll
+            for (int k = 0; k < kAhead; k++) fetch(p, k, v[k]);  // while the buffer is waited for
             lost = __any_sync(kFull, n > 1 && !attn_wait(&qempty[buf], (uint32_t)(n / 2 - 1) & 1u, w));
             if (lost) break;
-            const int d = lane * kE;
-#pragma unroll 4
-            for (int r = 0; r < p.rows; r++) {
-                float x[kE] = {};
-                if (d < a.head_dim) {
-                    const char* src = a.q + row_offset(a, p, p.j * ROWS + r, a.q_stride, 2) + d * 2;
-                    uint32_t v[kE / 2];
+#pragma unroll 1
+            for (int r0 = 0; r0 < p.rows; r0 += kAhead) {
+#pragma unroll
+                for (int k = 0; k < kAhead; k++) {
+                    const int r = r0 + k;
+                    if (r >= p.rows) break;
+                    float x[kE], amax = 0.f;
 #pragma unroll
                     for (int i = 0; i < kE / 4; i++) {
-                        const uint2 u = reinterpret_cast<const uint2*>(src)[i];
-                        v[2 * i] = u.x;
-                        v[2 * i + 1] = u.y;
+                        x[4 * i] = bf16lo(v[k][i].x);
+                        x[4 * i + 1] = bf16hi(v[k][i].x);
+                        x[4 * i + 2] = bf16lo(v[k][i].y);
+                        x[4 * i + 3] = bf16hi(v[k][i].y);
                     }
 #pragma unroll
-                    for (int i = 0; i < kE / 2; i++) {
-                        x[2 * i] = bf16lo(v[i]);
-                        x[2 * i + 1] = bf16hi(v[i]);
-                    }
-                }
-                float amax = 0.f;
+                    for (int i = 0; i < kE; i++) amax = fmaxf(amax, magnitude(x[i]));
+                    const float sc = scale_for(warp_max(amax)), inv = 1.f / sc;
+                    if (lane == 0) q_scale[n % kItems][r] = sc;
 #pragma unroll
-                for (int i = 0; i < kE; i++) amax = fmaxf(amax, magnitude(x[i]));
-                const float sc = scale_for(warp_max(amax)), inv = 1.f / sc;
-                if (lane == 0) q_scale[n % kItems][r] = sc;
+                    for (int i = 0; i < kE; i += 4) {
+                        float y[4];
 #pragma unroll
-                for (int i = 0; i < kE; i += 4) {
-                    float y[4];
+                        for (int u = 0; u < 4; u++) y[u] = to_hold(x[i + u]) * inv;
+                        uint32_t hi, lo;
+                        split4(y, hi, lo);
+                        const int e = d + i;  // element: 16-byte chunk e / 16 of group e / 128
+                        unsigned char* base = qs + buf * C::kQTile + (e >> 7) * 128 * 128 + (e & 15) + r * 128 +
+                                              ((((e & 127) >> 4) ^ (r & 7)) << 4);
 #pragma unroll
-                    for (int u = 0; u < 4; u++) y[u] = to_hold(x[i + u]) * inv;
-                    uint32_t hi, lo;
-                    split4(y, hi, lo);
-                    const int e = d + i;  // element: 16-byte chunk e / 16 of group e / 128
-                    unsigned char* base = qs + buf * C::kQTile + (e >> 7) * 128 * 128 + (e & 15);
-#pragma unroll
-                    for (int c = 0; c < 4; c++) {
-                        const int rh = 32 * c + r, rl = rh + 16, ch = (e & 127) >> 4;
-                        *reinterpret_cast<uint32_t*>(base + rh * 128 + ((ch ^ (rh & 7)) << 4)) = hi;
-                        *reinterpret_cast<uint32_t*>(base + rl * 128 + ((ch ^ (rl & 7)) << 4)) = lo;
+                        for (int c = 0; c < 4; c++) {
+                            *reinterpret_cast<uint32_t*>(base + 32 * c * 128) = hi;
+                            *reinterpret_cast<uint32_t*>(base + (32 * c + 16) * 128) = lo;
+                        }
                     }
                 }
+#pragma unroll
+                for (int k = 0; k < kAhead; k++) fetch(p, r0 + kAhead + k, v[k]);
             }
             fence_proxy_async_smem();
             __syncwarp();
@@ -388,15 +397,16 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
                 wait_full(k_pos(g));
                 const int sl = g % C::kScores;
                 if (g >= C::kScores) attn_wait(&sfree[sl], (uint32_t)(g / C::kScores - 1) & 1u, w);  // the slot's last scores have been read
+                // ... and the weights' slot, which the softmax takes for free once these scores are there
+                if (g >= 2) attn_wait(&odone[g & 1], (uint32_t)((g - 2) >> 1) & 1u, w);
                 tc_fence_after();
                 if (one) {
-                    const unsigned char* kt = ring + (k_pos(g) % NS) * C::kSlot;
-                    const unsigned char* qt = qs + buf * C::kQTile;
-#pragma unroll 1
-                    for (int d = 0; d < steps; d++) {
-                        const uint64_t ad = sdesc_sw128(qt + (d >> 2) * 128 * 128), bd = sdesc_sw128(kt + (d >> 2) * BN * 128);
-                        umma_f8(tm + (uint32_t)(sl * BN), ad + 2ull * (d & 3), bd + 2ull * (d & 3), id_s, d > 0 ? 1u : 0u);
-                    }
+                    const uint64_t ad = sdesc_sw128(qs + buf * C::kQTile), bd = sdesc_sw128(ring + (k_pos(g) % NS) * C::kSlot);
+#pragma unroll
+                    for (int d = 0; d < DP / 32; d++)  // 32 bytes a step, in descriptors' units of 16
+                        if (d < steps)
+                            umma_f8(tm + (uint32_t)(sl * BN), ad + (uint64_t)((d >> 2) * 1024 + 2 * (d & 3)),
+                                    bd + (uint64_t)((d >> 2) * BN * 8 + 2 * (d & 3)), id_s, d > 0 ? 1u : 0u);
                     umma_commit(&sfull[sl]);
                     umma_commit(&empty[k_pos(g) % NS]);
                     if (at.t + 1 == at.t1) umma_commit(&qempty[buf]);
@@ -464,8 +474,8 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sfree[sl]);
-                attn_wait(&ffull[g % kFacTiles], (uint32_t)(g / kFacTiles) & 1u, w);
-                if (t == t0) qsc = q_scale[at.n % kItems][row];  // written ahead of the products
+                // scales of the row and the tile: written ahead of the products
+                if (t == t0) qsc = q_scale[at.n % kItems][row];
                 const float* fc = fac[g % kFacTiles] + 2 * wq + (low ? 1 : 0);
                 const float f = fmaxf(fc[0] * qsc, 0x1p-126f), vs = fc[8], lv = fc[16];  // f > 0: -inf stays
                 float s[16];
@@ -539,7 +549,6 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
                     out[i] = low ? got : hi[i];
                     out[4 + i] = low ? lo[i] : got;
                 }
-                if (g >= 2) products_done(g - 2);  // the weights' slot has been read
                 tmem_st8(t_p + (uint32_t)((g & 1) * (BN / 4) + 8 * wq), out);
                 tmem_st_wait();
                 tc_fence_before();
@@ -691,8 +700,10 @@ bool code_map(CUtensorMap* map, const AttnArgs& a, const char* base) {
     for (int i = 0; i < 3; i++) strides[i] = dims[i + 1] == 1 && steps[i] < 16 ? 16 : (cuuint64_t)steps[i];
     const cuuint32_t box[4] = {128, 1, (cuuint32_t)a.box, 1};
     const cuuint32_t estr[4] = {1, 1, 1, 1};
+    // no more than a head's row from HBM: what lies beside it is another head's, which another CTA reads at another time
+    const CUtensorMapL2promotion promote = a.head_dim > 128 ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B : CU_TENSOR_MAP_L2_PROMOTION_L2_128B;
     return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<char*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+               CU_TENSOR_MAP_SWIZZLE_128B, promote, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int DP>
