@@ -26,8 +26,8 @@
 // Warps: four softmax, four that finish parts (O has two buffers for that, up to
 // 128 elements), two that issue products, one that splits the rows of q, four
 // producers of the ring (TMA, a box a page; else cp.async), one that walks the
-// stretch.  P has columns of its own in TMEM: a score slot is free as soon as its
-// scores are in registers, so one is enough beside two O.
+// stretch.  A quarter's weights of a tile take 8 of the 32 columns that its scores
+// had, and zeros the same columns of the other quarters' keys.
 #include "attn_tc.cuh"
 #include "pp_tc_f8.cuh"
 
@@ -35,6 +35,8 @@ namespace pp {
 namespace {
 
 constexpr int kFewRows = 16;        // rows of an item
+// Tiles that an item counts more than it has: 0 / 2 / 4 / 8, 64 ragged single tokens 112.5 / 104.7 / 106.3 / 107.9 us.
+constexpr int kPad = 2;
 constexpr float kLazy8 = 2.0f;      // growth of the base (log2) that O absorbs unscaled
 constexpr float kTopWeight = 64.f;  // the largest weight at its base, in codes: 2^kLazy8 times that stays below 448
 constexpr int kFacTiles = 8;        // tiles whose scales are held
@@ -46,14 +48,14 @@ struct Few {
     static constexpr int kSlots = DP == 256 ? 6 : 8, kSlot = BN * DP;  // even: keys and values keep to slots of their own
     static constexpr int kQBufs = 2, kQTile = 128 * DP;
     static constexpr int kParts = BN / 32;      // quarters with keys of their own
-    static constexpr int kScores = DP == 256 ? 2 : 1, kOuts = DP == 256 ? 1 : 2;  // buffers in TMEM
+    static constexpr int kOuts = DP == 256 ? 1 : 2;  // O buffers in TMEM, behind two slots of scores and weights
     static constexpr int kPitch = 128 + 4;      // floats of a staged row
     static constexpr int kStage = 4 * kFewRows * kPitch * 4;
     static constexpr int kSmem = kSlots * kSlot + kQBufs * kQTile + kStage + 1024;
     static constexpr int kWarpOut = 4, kWarpMma = 8, kWarpQ = 10, kWarpLoad = 11, kLoads = 4, kWarps = kWarpLoad + kLoads + 1;
     static constexpr int kReaders = kWarps - 1;
-    static constexpr uint32_t kTmemO = kScores * BN, kTmemP = kTmemO + kOuts * DP;  // scores, O, two weight slots
-    static_assert(kTmemP + 2 * (BN / 4) <= 512, "TMEM columns");
+    static constexpr uint32_t kTmemO = 2 * BN;
+    static_assert(kTmemO + kOuts * DP <= 512, "TMEM columns");
     static_assert(kFacTiles >= kSlots, "a tile's scales outlive its softmax");
 };
 
@@ -129,15 +131,14 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
     unsigned char* ring = smem;
     unsigned char* qs = smem + NS * C::kSlot;
     float* stage = reinterpret_cast<float*>(qs + C::kQBufs * C::kQTile);
-    __shared__ uint64_t full[NS], empty[NS], landed[C::kLoads], qfull[2], qempty[2], sfull[2], sfree[2], pfull[2], odone[2];
+    __shared__ uint64_t full[NS], empty[NS], landed[C::kLoads], qfull[2], qempty[2], sfull[2], pfull[2], odone[2];
     __shared__ uint64_t opart[2], ofull[2], ofree[2];
     __shared__ uint32_t taddr_s;
     __shared__ float stat_m[2][4][32], stat_b[2][4][32], stat_l[2][4][32], q_scale[kItems][ROWS];
     __shared__ __align__(16) float fac[kFacTiles][kFac];
     __shared__ unsigned last_s;
     __shared__ Item<ROWS, BN> items[kItems];
-    __shared__ uint64_t ifull[kItems], isplit[kItems], iempty[kItems], stretch;
-    __shared__ int tiles_s;
+    __shared__ uint64_t ifull[kItems], isplit[kItems], iempty[kItems];
     __shared__ unsigned lost_s;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const Waits w{a.status, a.timeout_ns, &lost_s};
@@ -152,7 +153,6 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
             mbar_init(&qfull[i], 1);
             mbar_init(&qempty[i], 1);
             mbar_init(&sfull[i], 1);
-            mbar_init(&sfree[i], C::kParts);
             mbar_init(&pfull[i], C::kParts);
             mbar_init(&odone[i], 1);
             mbar_init(&opart[i], 1);
@@ -164,7 +164,6 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
             mbar_init(&isplit[i], 1);
             mbar_init(&iempty[i], C::kReaders);
         }
-        mbar_init(&stretch, 1);
         lost_s = 0u;
         fence_mbar_init();
     }
@@ -186,28 +185,25 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
     const uint32_t tmem = taddr_s;
     pdl_wait();
     // a wait that gives up ends the CTA's work in order, as in attn_tc_kernel
-    ItemAt<ROWS, BN> at{items, ifull, iempty, w, 0, 0, 0, 0, false};
-    int tiles = 0;
-    if (warp < C::kWarps - 1) {
-        bool lost = !attn_wait(&stretch, 0, w);
-        // (warps that meet in barriers agree)
-        lost = warp < C::kWarpMma ? named_bar_or(1 + warp / 4, 128, lost) : __any_sync(kFull, lost);
-        if (!lost) tiles = tiles_s;
-    }
+    ItemAt<ROWS, BN, true> at{items, ifull, iempty, w, 0, 0, 0, 0, false};
     // order of the loads: K0 K1 V0 K2 V1 K3 ... (scores run two tiles ahead)
     auto k_pos = [](int g) { return g == 0 ? 0 : 2 * g - 1; };
     auto v_pos = [](int g) { return 2 * g + 2; };
 
     if (warp == C::kWarps - 1) {
         // ---------------------------------------------------------- schedule
-        Walk<ROWS, BN> walk = start_walk<ROWS, BN>(&a, lane, blockIdx.x == 0, 1);
+        Walk<ROWS, BN, true> walk = start_walk<ROWS, BN, true>(&a, lane, blockIdx.x == 0, 1, kPad);
         if (lane == 0) {
-            tiles_s = (int)(walk.end - walk.at);
-            mbar_arrive(&stretch);
             Part p;
-            for (int n = 0; walk.next(p); n++) {
+            for (int n = 0;; n++) {
+                const bool some = walk.next(p);
                 Item<ROWS, BN>& it = items[n % kItems];
                 if (n >= kItems && !attn_wait(&iempty[n % kItems], (uint32_t)(n / kItems - 1) & 1u, w)) break;
+                if (!some) {  // the stretch's end: a part of no rows
+                    it.rows = 0;
+                    mbar_arrive(&ifull[n % kItems]);
+                    break;
+                }
                 static_cast<Part&>(it) = p;
                 it.rows = min(ROWS, p.seq.n * a.group - p.j * ROWS);
                 it.open = all_see<ROWS>(a, p);
@@ -219,8 +215,6 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
             }
         }
         __syncwarp();
-    } else if (tiles <= 0) {
-        // nothing for this CTA
     } else if (warp >= C::kWarpLoad) {
         // ----------------------------------- producer of every fourth load
         const int me = warp - C::kWarpLoad;
@@ -230,7 +224,6 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
         auto tile_of = [](int pos) { return pos == 0 ? 0 : pos & 1 ? (pos + 1) / 2 : (pos - 2) / 2; };
         auto go_to = [&](int pos) {
             const int g = tile_of(pos);
-            if (g >= tiles) return false;
             at.step(g - g_at, lane, true);
             if (at.lost) return false;
             g_at = g;
@@ -326,7 +319,7 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
 #pragma unroll
             for (int i = 0; i < kE / 4; i++) v[i] = src[i];
         };
-        for (int left = tiles; !lost;) {
+        while (!lost) {
             const Item<ROWS, BN>& p = at.item();
             const int n = at.n, buf = n & 1;
             uint2 v[kAhead][kE / 4];
@@ -375,8 +368,6 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(&qfull[buf]);
-            left -= at.t1 - at.t0;
-            if (left <= 0) break;
             at.next(lane, true);
             lost = at.lost;
         }
@@ -391,14 +382,13 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
         auto wait_full = [&](int pos) { attn_wait(&full[pos % NS], (uint32_t)(pos / NS) & 1u, w); };
         if (who == 0) {
 #pragma unroll 1
-            for (int g = 0; g < tiles; g++) {
+            for (int g = 0; !at.lost; g++) {
                 const int buf = at.n & 1;
                 if (at.t == at.t0) attn_wait(&qfull[buf], (uint32_t)(at.n / 2) & 1u, w);
                 wait_full(k_pos(g));
-                const int sl = g % C::kScores;
-                if (g >= C::kScores) attn_wait(&sfree[sl], (uint32_t)(g / C::kScores - 1) & 1u, w);  // the slot's last scores have been read
-                // ... and the weights' slot, which the softmax takes for free once these scores are there
-                if (g >= 2) attn_wait(&odone[g & 1], (uint32_t)((g - 2) >> 1) & 1u, w);
+                const int sl = g & 1;
+                if (g >= 2)  // the slot's last weights have been multiplied
+                    attn_wait(&odone[g & 1], (uint32_t)((g - 2) >> 1) & 1u, w);
                 tc_fence_after();
                 if (one) {
                     const uint64_t ad = sdesc_sw128(qs + buf * C::kQTile), bd = sdesc_sw128(ring + (k_pos(g) % NS) * C::kSlot);
@@ -412,11 +402,11 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
                     if (at.t + 1 == at.t1) umma_commit(&qempty[buf]);
                 }
                 __syncwarp();
-                if (g + 1 < tiles) at.step(1, lane, true);
+                at.step(1, lane, true);
             }
         } else {
 #pragma unroll 1
-            for (int g = 0; g < tiles; g++) {
+            for (int g = 0; !at.lost; g++) {
                 wait_full(v_pos(g));
                 attn_wait(&pfull[g & 1], (uint32_t)(g >> 1) & 1u, w);
                 tc_fence_after();
@@ -424,14 +414,14 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
                     const uint64_t vd = sdesc_sw128_n(ring + (v_pos(g) % NS) * C::kSlot, BN * 128);
 #pragma unroll
                     for (int k = 0; k < BN / 32; k++)
-                        umma_f8_ta(tm + C::kTmemO + (uint32_t)(at.n % C::kOuts * DP), tm + C::kTmemP + (uint32_t)((g & 1) * (BN / 4) + 8 * k), vd + (uint64_t)(k * 256),
+                        umma_f8_ta(tm + C::kTmemO + (uint32_t)(at.n % C::kOuts * DP), tm + (uint32_t)((g & 1) * BN + 32 * k), vd + (uint64_t)(k * 256),
                                    id_o, (at.t > at.t0 || k > 0) ? 1u : 0u);
                     umma_commit(&odone[g & 1]);
                     if (at.t + 1 == at.t1) umma_commit(&opart[at.n % C::kOuts]);
                     umma_commit(&empty[v_pos(g) % NS]);
                 }
                 __syncwarp();
-                if (g + 1 < tiles) at.step(1, lane, true);
+                at.step(1, lane, true);
             }
         }
     } else if (warp < C::kWarpOut) {
@@ -439,24 +429,14 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
         const int wq = warp, row = lane & 15;
         const bool low = lane >= 16;
         const uint32_t lanes = (uint32_t)(32 * wq) << 16;
-        const uint32_t t_p = tmem + C::kTmemP + lanes;
         const float c_own = low ? 0.0625f : 1.f, c_other = low ? 1.f : 0.0625f;
-        {  // the other quarters' keys never have weight in this one's lanes
-            const uint32_t z[8] = {};
-#pragma unroll 1
-            for (int c = 0; c < 2 * C::kParts; c++) tmem_st8(t_p + 8 * c, z);
-            tmem_st_wait();
-            tc_fence_before();
-        }
-        // every quarter's lanes are zero ahead of the first products
-        named_bar_sync(1, 128);
         int g = 0;  // tile of the stretch
         auto products_done = [&](int x) {
             attn_wait(&odone[x & 1], (uint32_t)(x >> 1) & 1u, w);
             tc_fence_after();
         };
         if (wq < C::kParts) at.enter(0);
-        for (int left = tiles; wq < C::kParts && !at.lost;) {
+        while (wq < C::kParts && !at.lost) {
             const Item<ROWS, BN>& p = at.item();
             const int tok = min((p.j * ROWS + row) / a.group, p.seq.n - 1);
             const int open = p.open, t0 = at.t0, t1 = at.t1, ob = at.n % C::kOuts;
@@ -465,15 +445,12 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
             // the buffer's last part has been read
             if (at.n >= C::kOuts) attn_wait(&ofree[ob], (uint32_t)(at.n / C::kOuts - 1) & 1u, w);
             for (int t = t0; t < t1; t++, g++) {
-                const int sl = g % C::kScores;
-                attn_wait(&sfull[sl], (uint32_t)(g / C::kScores) & 1u, w);
+                const uint32_t t_s = tmem + (uint32_t)((g & 1) * BN) + lanes;
+                attn_wait(&sfull[g & 1], (uint32_t)(g >> 1) & 1u, w);
                 tc_fence_after();
                 uint32_t u[32];
-                tmem_ld32(tmem + (uint32_t)(sl * BN + 32 * wq) + lanes, u);
+                tmem_ld32(t_s + 32 * wq, u);
                 tmem_ld_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&sfree[sl]);
                 // scales of the row and the tile: written ahead of the products
                 if (t == t0) qsc = q_scale[at.n % kItems][row];
                 const float* fc = fac[g % kFacTiles] + 2 * wq + (low ? 1 : 0);
@@ -549,7 +526,10 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
                     out[i] = low ? got : hi[i];
                     out[4 + i] = low ? lo[i] : got;
                 }
-                tmem_st8(t_p + (uint32_t)((g & 1) * (BN / 4) + 8 * wq), out);
+                const uint32_t zero[8] = {};
+#pragma unroll
+                for (int c = 1; c < C::kParts; c++) tmem_st8(t_s + 32 * ((wq + c) % C::kParts), zero);
+                tmem_st8(t_s + 32 * wq, out);
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
@@ -560,14 +540,12 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
             stat_l[ob][wq][lane] = sum;
             __syncwarp();
             if (lane == 0) mbar_arrive(&ofull[ob]);
-            left -= t1 - t0;
-            if (left <= 0) break;
             at.next(lane, true);
         }
         // (quarters without keys free the parts all the same)
         if (wq >= C::kParts) {
             at.enter(0);
-            for (int left = tiles - (at.t1 - at.t0); left > 0 && !at.lost; left -= at.t1 - at.t0) at.next(lane, true);
+            while (!at.lost) at.next(lane, true);
         }
     } else {
         // ------------------------------------------------------- ends of parts
@@ -577,7 +555,7 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
         const float c_own = low ? 0.0625f : 1.f;
         const int D = a.head_dim;
         at.enter(0);
-        for (int left = tiles; !named_bar_or(2, 128, at.lost);) {
+        while (!named_bar_or(2, 128, at.lost)) {
             const Item<ROWS, BN>& p = at.item();
             const int rows = p.rows, ob = at.n % C::kOuts;
             const uint32_t t_o = tmem + C::kTmemO + (uint32_t)(ob * DP) + lanes, par = (uint32_t)(at.n / C::kOuts) & 1u;
@@ -673,8 +651,6 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
                 named_bar_sync(2, 128);
                 if (last_s) merge_few<__nv_bfloat16, ROWS, BN, 4>(a, p, sp, rows, otid, 128);
             }
-            left -= at.t1 - at.t0;
-            if (left <= 0) break;
             at.next(lane, true);
         }
     }

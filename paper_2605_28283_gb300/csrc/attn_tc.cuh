@@ -135,17 +135,19 @@ struct Item : Part {
 constexpr int kItems = 8;
 
 // A reader of the ring (a whole warp), at tile t of part n.
-template <int ROWS, int TOK>
+template <int ROWS, int TOK, bool ENDS = false>
 struct ItemAt {
     const Item<ROWS, TOK>* ring;
     uint64_t *full, *empty;
     Waits w;
     int n, t, t0, t1;
-    bool lost;  // the part did not come: nothing of item() may be used, and the part has no end
+    bool lost;  // the part did not come (or, where the stretch's end is handed out as a part of no rows, it is that):
+                // nothing of item() may be used, and the part has no end
     PP_DEVINL const Item<ROWS, TOK>& item() const { return ring[n % kItems]; }
     PP_DEVINL void enter(int n_) {
         n = n_;
         lost = __any_sync(kFull, !attn_wait(&full[n % kItems], (uint32_t)(n / kItems) & 1u, w));
+        if (ENDS && !lost) lost = item().rows == 0;
         t = t0 = lost ? 0 : item().t0;
         t1 = lost ? 0x7fffffff : item().t1;
     }

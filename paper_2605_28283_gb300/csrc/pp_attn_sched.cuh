@@ -17,6 +17,8 @@
 
 namespace pp {
 
+constexpr int kLongStretch = 16;  // tiles of a stretch from which items are padded
+
 // Quotient of two non-negative numbers, in 32 bits where they fit (a 64-bit
 // division is a call of a hundred instructions).
 PP_DEVINL long long quotient(long long a, long long b) {
@@ -25,12 +27,16 @@ PP_DEVINL long long quotient(long long a, long long b) {
 }
 
 // Tiles of the key line: the schedule is recomputed by whoever walks it, from
-// the lengths alone.
-template <int ROWS, int TOK>
+// the lengths alone.  PADDED: where stretches are long, an item counts `pad`
+// tiles more than it has (ahead of its own), for what starting and finishing it
+// costs, so that CTAs with many short items get fewer tiles.
+template <int ROWS, int TOK, bool PADDED = false>
 struct Sched {
     const AttnArgs* a;
     long long total;  // key tiles of the call
     int ctas;         // CTAs with work
+    int pad_;
+    PP_DEVINL int pad() const { return PADDED ? pad_ : 0; }
 
     PP_DEVINL int row_tiles(const Seq& s) const { return (int)(((unsigned)s.n * (unsigned)a->group + ROWS - 1) / ROWS); }
 
@@ -42,12 +48,15 @@ struct Sched {
     }
     PP_DEVINL int key_tiles(const Seq& s, int j) const { return max(1, (key_end(s, j) + TOK - 1) / TOK); }
 
-    // Key tiles of one key head of a sequence.
+    // An item's length on the line.
+    PP_DEVINL int length(const Seq& s, int j) const { return key_tiles(s, j) + pad(); }
+
+    // Length of one key head of a sequence on the line.
     PP_DEVINL long long head_tiles(const Seq& s) const {
         const int m = row_tiles(s);
-        if (a->mask || m <= 1) return m ? (long long)m * key_tiles(s, m - 1) : 0;
+        if (a->mask || m <= 1) return m ? (long long)m * length(s, m - 1) : 0;
         long long sum = 0;
-        for (int j = 0; j < m; j++) sum += key_tiles(s, j);
+        for (int j = 0; j < m; j++) sum += length(s, j);
         return sum;
     }
 
@@ -89,9 +98,9 @@ struct Part {
 };
 
 // Walks the parts of one CTA's stretch.
-template <int ROWS, int TOK>
+template <int ROWS, int TOK, bool PADDED = false>
 struct Walk {
-    Sched<ROWS, TOK> sched;
+    Sched<ROWS, TOK, PADDED> sched;
     long long at, end;  // the rest of the stretch
     long long base;     // line position of sequence b
     int b, h, j;
@@ -112,33 +121,37 @@ struct Walk {
             h = (int)quotient(at - base, per);
             head_base = base + (long long)h * per;
         }
-        while (m > 0 && j + 1 < m && head_base + sched.key_tiles(seq, j) <= at) {
-            head_base += sched.key_tiles(seq, j);
+        while (m > 0 && j + 1 < m && head_base + sched.length(seq, j) <= at) {
+            head_base += sched.length(seq, j);
             j++;
         }
     }
 
     // The next part; false at the end of the stretch.
     PP_DEVINL bool next(Part& p) {
-        if (at >= end) return false;
-        while (m == 0 || h >= sched.a->n_kv_heads) enter(b + 1, m == 0 ? base : head_base);
-        p.b = b;
-        p.h = h;
-        p.j = j;
-        p.seq = seq;
-        p.key_end = sched.key_end(seq, j);
-        p.tiles = sched.key_tiles(seq, j);
-        p.first = head_base;
-        p.t0 = (int)(at - head_base);
-        p.t1 = (int)min((long long)p.tiles, end - head_base);
-        at = head_base + p.t1;
-        if (p.t1 == p.tiles) {
-            head_base += p.tiles;
-            if (++j == m) {
-                j = 0;
-                h++;
+        do {
+            if (at >= end) return false;
+            while (m == 0 || h >= sched.a->n_kv_heads) enter(b + 1, m == 0 ? base : head_base);
+            const int pad = sched.pad();
+            p.b = b;
+            p.h = h;
+            p.j = j;
+            p.seq = seq;
+            p.key_end = sched.key_end(seq, j);
+            p.tiles = sched.key_tiles(seq, j);
+            p.first = head_base;
+            const int len = p.tiles + pad, u1 = (int)min((long long)len, end - head_base);
+            p.t0 = max((int)(at - head_base) - pad, 0);
+            p.t1 = max(u1 - pad, 0);
+            at = head_base + u1;
+            if (u1 == len) {
+                head_base += len;
+                if (++j == m) {
+                    j = 0;
+                    h++;
+                }
             }
-        }
+        } while (PADDED && p.t1 == 0);  // the stretch ends ahead of the item's first tile
         return true;
     }
 };
@@ -147,20 +160,30 @@ struct Walk {
 // counts a run of sequences, a scan over the lanes gives the total, and the
 // lane whose run holds this CTA's first tile looks for its sequence.  Short
 // code on purpose: it runs once, from a cold instruction cache.
-template <int ROWS, int TOK>
-PP_DEVINL Walk<ROWS, TOK> start_walk(const AttnArgs* a, int lane, bool report, int least) {
-    Walk<ROWS, TOK> w;
+template <int ROWS, int TOK, bool PADDED = false>
+PP_DEVINL Walk<ROWS, TOK, PADDED> start_walk(const AttnArgs* a, int lane, bool report, int least, int pad = 0) {
+    Walk<ROWS, TOK, PADDED> w;
     w.sched.a = a;
+    w.sched.pad_ = 0;
     const int B = a->batch.n_seqs, run = (B + 31) / 32;
     const int b0 = min(lane * run, B), b1 = min(b0 + run, B);
-    long long mine = 0;
+    long long mine = 0, items = 0;
 #pragma unroll 2
     for (int b = b0; b < b1; b++) {
         const Seq q = load_seq(a->batch, b);
         if (report && q.bad) record_status(a->status, PP_ERR_INVALID_ARG);
         mine += w.sched.head_tiles(q);
+        if (PADDED) items += w.sched.row_tiles(q);
     }
     mine *= a->n_kv_heads;
+    if (PADDED) {
+        // stretches of at least kLongStretch tiles
+        long long all = mine;
+#pragma unroll 1
+        for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(kFull, all, o);
+        if (all >= (long long)kLongStretch * gridDim.x) w.sched.pad_ = pad;
+        mine += items * a->n_kv_heads * w.sched.pad_;
+    }
     long long sum = mine;
 #pragma unroll 1
     for (int o = 1; o < 32; o <<= 1) {
@@ -205,10 +228,11 @@ struct Split {
     int c0, c1;
     bool c0_tail;  // the first part lies in c0's second place
     Split() = default;
-    PP_DEVINL Split(const Sched<ROWS, TOK>& s, const Part& p) {
-        c0 = s.cta_of(p.first);
-        c1 = s.cta_of(p.first + p.tiles - 1);
-        c0_tail = s.begin_of(c0) != p.first;
+    template <bool PADDED>
+    PP_DEVINL Split(const Sched<ROWS, TOK, PADDED>& s, const Part& p) {
+        c0 = s.cta_of(p.first + s.pad());
+        c1 = s.cta_of(p.first + s.pad() + p.tiles - 1);
+        c0_tail = s.begin_of(c0) < p.first;
     }
     PP_DEVINL float* place(const AttnArgs& a, int c) const { return part_place<ROWS>(a, c, c == c0 && c0_tail); }
 };
