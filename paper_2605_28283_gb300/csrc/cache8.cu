@@ -8,6 +8,7 @@
 #include "pp_cache8.cuh"
 #include "pp_head.cuh"
 #include "pp_launch.cuh"
+#include "pp_tc.cuh"
 
 namespace pp {
 namespace {
@@ -21,7 +22,8 @@ namespace {
 // registers: its largest magnitude is known before anything is written, and
 // every element is read once.  The strips of a longer block meet in shared
 // memory.  The other CTAs take a token's query heads, as in norm_kernel.
-constexpr int kMaxStrips = 16;  // warps of a CTA at most
+constexpr int kMaxStrips = 16;  // warps of a CTA at most (8 where that does)
+constexpr int kAppend8Smem = 216 * 1024;
 
 struct Slot {
     int page, lo;      // the block's page and first entry; page -1: nothing to do
@@ -83,12 +85,12 @@ PP_DEVINL void again(char* p, float ratio) {
     store_codes<V>(p, f, ratio);
 }
 
-template <typename T, int V, bool HALF, int UPL, int ITER>
-__global__ void __launch_bounds__(32 * kMaxStrips) append8_kernel(const Append8Args a) {
+template <typename T, int V, bool HALF, int UPL, int ITER, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 2 : 1) append8_kernel(const Append8Args a) {
     using Lane = HeadLane<T, V, HALF, UPL>;
     extern __shared__ __align__(16) float2 cs[];
     __shared__ Slot slot_s;
-    __shared__ int pos_s;
+    __shared__ int pos_s[kMaxStrips], in_s[kMaxStrips];
     __shared__ float amax_s[kMaxStrips];
     pdl_launch_dependents();
     pdl_wait();
@@ -98,50 +100,55 @@ __global__ void __launch_bounds__(32 * kMaxStrips) append8_kernel(const Append8A
     const int kv_ctas = a.slots * a.parts;
     if ((int)blockIdx.x >= kv_ctas) {
         // ------------------------------------------------------------ queries
-        const int t = ((int)blockIdx.x - kv_ctas) / a.split, y = ((int)blockIdx.x - kv_ctas) % a.split;
-        const int groups = (int)blockDim.x / h.group, step = groups * a.split;
+        // a team of a.team threads takes a token; with one team a CTA, a.split CTAs share a token
+        const int q_cta = (int)blockIdx.x - kv_ctas, team = tid / a.team, teams = (int)blockDim.x / a.team;
+        const int t = q_cta / a.split * teams + team, y = q_cta % a.split, in_team = tid - team * a.team;
+        const int groups = a.team / h.group, step = groups * a.split;
+        const bool exists = t < a.batch.n_tokens;
         const char* q = a.q + t * a.q_stride;
         char* out = a.q_out + t * a.q_out_stride;
-        if (warp == 0) {
+        const int pitch = (h.rot_dim / 2 + V - 1) / V;
+        float2* table = cs + team * (pitch * V);
+        if (in_team < 32 && exists) {
             const int b = find_seq(a.batch, t, l32);
             const Seq s = load_seq(a.batch, b);
             const int i = t - s.q0;
             const bool in = !s.bad && i >= 0 && i < s.n;
             if (l32 == 0) {
-                slot_s.page = in ? 0 : -1;
-                pos_s = h.positions ? h.positions[t] : s.ctx + i;
+                pos_s[team] = h.positions ? h.positions[t] : s.ctx + i;
+                in_s[team] = in;
             }
         }
         float2 c[UPL][V];
-        bool ready = false;
+        bool ready = false, in = false;
         for (int r0 = y * groups; r0 < a.n_heads; r0 += 2 * step) {
             Vec<T, V> x[2][UPL][2];
 #pragma unroll
             for (int n = 0; n < 2; n++) {
-                const int r = r0 + n * step + tid / h.group;
-                if (r < a.n_heads) lane.load(q + (long long)r * D * (int)sizeof(T), x[n]);
+                const int r = r0 + n * step + in_team / h.group;
+                if (r < a.n_heads && exists) lane.load(q + (long long)r * D * (int)sizeof(T), x[n]);
             }
             if (!ready) {
                 __syncthreads();
-                if (slot_s.page < 0) return;  // padding, or a skipped sequence: nothing is written
+                in = exists && in_s[team];  // padding, or a skipped sequence: nothing is written
                 if (h.rot_dim > 0) {
-                    fill_pairs(cs, h, V, pos_s, false, tid, blockDim.x);
+                    if (in) fill_pairs(table, h, V, pos_s[team], false, in_team, a.team);
                     __syncthreads();
-                    lane.factors(cs, h, c);
+                    lane.factors(table, h, c);
                 }
                 ready = true;
             }
 #pragma unroll
             for (int n = 0; n < 2; n++) {
-                const int r = r0 + n * step + tid / h.group;
+                const int r = r0 + n * step + in_team / h.group;
                 float f[UPL][2][V], g[UPL][2][V];
                 lane.widen(x[n], f);
                 if (h.norm) {
-                    const float inv = inverse_rms(Lane::group_sum(r < a.n_heads ? Lane::dot(f, f) : 0.f, h.group), h);
+                    const float inv = inverse_rms(Lane::group_sum(r < a.n_heads && exists ? Lane::dot(f, f) : 0.f, h.group), h);
                     lane.weights(a.q_gamma, g);
                     Lane::scale_by(f, inv, g);
                 }
-                if (r >= a.n_heads) continue;
+                if (r >= a.n_heads || !in) continue;
                 if (h.rot_dim > 0) lane.rotate(f, c);
                 if (h.norm || h.rot_dim > 0) lane.narrow(f, x[n]);
                 lane.store(out + (long long)r * D * (int)sizeof(T), x[n]);
@@ -172,31 +179,77 @@ __global__ void __launch_bounds__(32 * kMaxStrips) append8_kernel(const Append8A
         const float2 v = cos_sin(h.positions ? h.positions[t] : s.e0 + row, h.inv_freq[p]);
         cs[(s.e0 - s.lo + row) * row_pairs + pair_slot(p, V, pitch)] = make_float2(v.x * h.scale, v.y * h.scale);
     }
+    // A thread's vectors of the next units on their way into shared memory, for itself alone: loads in registers would
+    // leave too few of them in flight (8192 tokens, 40 heads of 128: 199 us).
+    constexpr int kVecs = ITER * UPL * 2;
+    unsigned char* stages = reinterpret_cast<unsigned char*>(cs) + a.table_bytes + tid * Lane::kBytes;
+    const int stage_bytes = kVecs * (int)blockDim.x * Lane::kBytes;
+    const int first = s.lo + strip * R + l32 / h.group;  // entry of the lane's first row
+    auto rows_of = [&](int u) {
+        const bool key = u < a.n_kv_heads;
+        return (key ? a.k : a.v) + (long long)(key ? u : u - a.n_kv_heads) * D * (int)sizeof(T);
+    };
+    auto fetch = [&](int u0, int stage) {
+        const int u = u0 + warp / strips;
+        if (u < 2 * a.n_kv_heads) {
+            const char* src = rows_of(u);
+            const long long stride = u < a.n_kv_heads ? a.k_stride : a.v_stride;
+            unsigned char* to = stages + stage * stage_bytes;
+#pragma unroll
+            for (int n = 0; n < ITER; n++) {
+                const int e = first + n * per;
+                if (e < s.e0 || e >= s.e1) continue;
+                const char* row = src + (s.token + e - s.e0) * stride;
+#pragma unroll
+                for (int k = 0; k < UPL; k++) {
+                    const int at = (n * UPL + k) * 2 * (int)blockDim.x * Lane::kBytes;
+                    if (lane.va[k] >= 0) cp_async_small<Lane::kBytes>(to + at, row + lane.va[k] * Lane::kBytes);
+                    if (lane.vb[k] >= 0) cp_async_small<Lane::kBytes>(to + at + (int)blockDim.x * Lane::kBytes, row + lane.vb[k] * Lane::kBytes);
+                }
+            }
+        }
+        cp_async_commit();
+    };
+    int turn = 0;
+    for (int i = 0; i + 1 < a.stages; i++) fetch((part + i * a.parts) * units, i);
     __syncthreads();
     for (int u0 = part * units; u0 < 2 * a.n_kv_heads; u0 += units * a.parts) {
         const int u = u0 + warp / strips;
         const bool have = u < 2 * a.n_kv_heads, key = u < a.n_kv_heads;
         const int head = key ? u : u - a.n_kv_heads;
-        const int first = s.lo + strip * R + l32 / h.group;  // entry of the lane's first row
         const long long at = scale_index(a.batch, a.scales, a.n_kv_heads, s.page, head, s.lo);
         float* scale_p = (key ? a.scales.k : a.scales.v) + at;
         const bool cached = s.lo < s.ctx;
         float old = have && cached && l32 == 0 ? *scale_p : 0.f;
         float f[ITER][UPL][2][V];
+        if (a.stages) {
+            fetch(u0 + (a.stages - 1) * a.parts * units, (turn + a.stages - 1) % a.stages);
+            if (a.stages == 1)
+                cp_async_wait<0>();
+            else if (a.stages == 2)
+                cp_async_wait<1>();
+            else
+                cp_async_wait<2>();
+        }
+        const unsigned char* from = stages + turn * stage_bytes;
+        turn = turn + 1 >= a.stages ? 0 : turn + 1;
         if (have) {
-            Vec<T, V> x[ITER][UPL][2];
-            const char* src = (key ? a.k : a.v) + (long long)head * D * (int)sizeof(T);
-            const long long stride = key ? a.k_stride : a.v_stride;
-#pragma unroll
-            for (int n = 0; n < ITER; n++) {
-                const int e = first + n * per;
-                if (e >= s.e0 && e < s.e1) lane.load(src + (s.token + e - s.e0) * stride, x[n]);
-            }
 #pragma unroll
             for (int n = 0; n < ITER; n++) {
                 const int e = first + n * per;
                 const bool in = e >= s.e0 && e < s.e1;
-                lane.widen(x[n], f[n]);
+                Vec<T, V> x[UPL][2];
+                if (a.stages) {
+#pragma unroll
+                    for (int k = 0; k < UPL; k++)
+#pragma unroll
+                        for (int v = 0; v < 2; v++)
+                            x[k][v].raw = *reinterpret_cast<const decltype(x[0][0].raw)*>(
+                                from + ((n * UPL + k) * 2 + v) * (int)blockDim.x * Lane::kBytes);
+                } else if (in) {  // no room beside the factors
+                    lane.load(rows_of(u) + (s.token + e - s.e0) * (key ? a.k_stride : a.v_stride), x);
+                }
+                lane.widen(x, f[n]);
                 if (!in) {
 #pragma unroll
                     for (int k = 0; k < UPL; k++)
@@ -267,27 +320,40 @@ __global__ void __launch_bounds__(32 * kMaxStrips) append8_kernel(const Append8A
     }
 }
 
-template <typename T, int V, bool HALF, int UPL, int ITER>
+template <typename T, int V, bool HALF, int UPL, int ITER, int WARPS>
 cudaError_t append8_run(Append8Args& a, int block, cudaStream_t st) {
-    const int R = ITER * 32 / a.head.group, strips = std::max(1, block / R), warps = std::max(8, strips);
+    constexpr int warps = WARPS;
+    const int R = ITER * 32 / a.head.group, strips = std::max(1, block / R);
+    if constexpr (WARPS == 8) {
+        if (strips > 8) return append8_run<T, V, HALF, UPL, ITER, 16>(a, block, st);
+    }
     const int units = warps / strips, passes = (2 * a.n_kv_heads + units - 1) / units;
     const long long T_ = a.batch.n_tokens;
     a.slots = (int)(T_ / block + 2ll * a.batch.n_seqs);
-    // about two CTAs an SM where there are few blocks
-    a.parts = std::min(passes, std::max(1, (304 + a.slots - 1) / a.slots));
-    const int rows = warps * 32 / a.head.group;  // query rows of a CTA at once
+    // a pass of all heads a CTA where there are few blocks; else about four CTAs an SM
+    a.parts = std::min(passes, std::max(1, (608 + a.slots - 1) / a.slots));
+    const int threads = warps * 32, pairs = (a.head.rot_dim / 2 + V - 1) / V * V;
+    // queries: ten rows' lanes a thread where there are many tokens; few tokens: several CTAs each
+    const int rows = threads / a.head.group;  // query rows of a CTA at once
     a.split = a.n_heads ? (int)std::min<long long>((a.n_heads + rows - 1) / rows, std::max<long long>(1, 304 / T_)) : 1;
-    const long long ctas = (long long)a.slots * a.parts + (a.n_heads ? T_ * a.split : 0);
+    a.team = threads;
+    if (a.split == 1 && T_ > 608)
+        while (a.team > 64 && a.team / 2 * 10 >= a.n_heads * a.head.group) a.team /= 2;
+    const int teams = threads / a.team;
+    const long long ctas = (long long)a.slots * a.parts + (a.n_heads ? (T_ + teams - 1) / teams * a.split : 0);
     if (ctas > 0x7fffffffll) return cudaErrorInvalidValue;
-    const int pairs = (a.head.rot_dim / 2 + V - 1) / V * V;
-    const int smem = std::max(1, block) * pairs * 8;
-    auto* kern = append8_kernel<T, V, HALF, UPL, ITER>;
-    if (smem > 40 * 1024) {
-        static std::atomic<bool> allowed[64];
-        const cudaError_t e = allow_smem(kern, 128 * 128 * 8, allowed);
-        if (e != cudaSuccess) return e;
-    }
-    return launch_overlapped(kern, dim3((unsigned)ctas), dim3((unsigned)(warps * 32)), (size_t)smem, st, a);
+    a.table_bytes = std::max(block, teams) * pairs * 8;
+    const int stage = ITER * UPL * 2 * threads * V * (int)sizeof(T);
+    // two CTAs an SM where that leaves two stages, else as many as fit
+    a.stages = (kAppend8Smem / 2 - a.table_bytes) / stage;
+    if (a.stages < 2) a.stages = (kAppend8Smem - a.table_bytes) / stage;
+    a.stages = std::max(0, std::min({a.stages, 3, passes / a.parts + 1}));
+    const int smem = a.table_bytes + a.stages * stage;
+    auto* kern = append8_kernel<T, V, HALF, UPL, ITER, WARPS>;
+    static std::atomic<bool> allowed[64];
+    const cudaError_t e = allow_smem(kern, kAppend8Smem, allowed);
+    if (e != cudaSuccess) return e;
+    return launch_overlapped(kern, dim3((unsigned)ctas), dim3((unsigned)threads), (size_t)smem, st, a);
 }
 
 template <typename T, int V, bool HALF>
@@ -298,12 +364,12 @@ cudaError_t append8_go(Append8Args a, int block, cudaStream_t st) {
     a.head.group = group;
     // strips of up to 64 fp32 values a lane
     if constexpr (V == 2) {
-        if (units > 32) return append8_run<T, V, HALF, 2, 8>(a, block, st);
-        return append8_run<T, V, HALF, 1, 8>(a, block, st);
+        if (units > 32) return append8_run<T, V, HALF, 2, 8, 8>(a, block, st);
+        return append8_run<T, V, HALF, 1, 8, 8>(a, block, st);
     } else if constexpr (V == 4) {
-        return group <= 8 ? append8_run<T, V, HALF, 1, 4>(a, block, st) : append8_run<T, V, HALF, 1, 8>(a, block, st);
+        return group <= 8 ? append8_run<T, V, HALF, 1, 4, 8>(a, block, st) : append8_run<T, V, HALF, 1, 8, 8>(a, block, st);
     } else {
-        return append8_run<T, V, HALF, 1, 4>(a, block, st);
+        return append8_run<T, V, HALF, 1, 4, 8>(a, block, st);
     }
 }
 
@@ -317,35 +383,38 @@ cudaError_t append8_typed(const Append8Args& a, int layout, int block, cudaStrea
 }
 
 // --------------------------------------------------------------------- read
-// kReadTokens tokens a CTA: a warp looks each one's entry up, then all threads
-// go over their rows, V codes (a 16-byte store) at a time.
-constexpr int kReadTokens = 8, kReadUnits = 4;
+// kReadTokens tokens a CTA: a warp looks the entries of its share up, then all
+// threads go over the rows, V codes (a 16-byte store) at a time.
+constexpr int kReadTokens = 32, kReadUnits = 4;
 
 template <typename T>
 __global__ void __launch_bounds__(256) read8_kernel(const Read8Args a) {
-    constexpr int V = 16 / (int)sizeof(T);
+    constexpr int V = 16 / (int)sizeof(T), kShare = kReadTokens / 8;
     __shared__ long long code_s[kReadTokens], scale_s[kReadTokens];  // -1: zeros, -2: left alone
     pdl_launch_dependents();
     pdl_wait();
     const int t0 = (int)blockIdx.x * kReadTokens, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (t0 + warp < a.batch.n_tokens) {
-        const int t = t0 + warp, b = find_seq(a.batch, t, lane);
-        const Seq s = load_seq(a.batch, b);
-        const int i = t - s.q0, e = s.ctx + i;
-        long long code = -2, sc = 0;
-        if (!s.bad && i >= 0 && i < s.n) {
-            const int page = entry_page(a.batch, b, e);
-            code = -1;
-            if (page >= 0) {
-                code = entry_offset(a.batch, a.cache, page, e);
-                sc = scale_index(a.batch, a.scales, a.n_kv_heads, page, 0, e);
-            } else if (lane == 0) {
-                record_status(a.status, PP_ERR_INVALID_ARG);
+    if (t0 + warp * kShare < a.batch.n_tokens) {
+        // the sequence of the share's first token; from there a lane for each token
+        int b = find_seq(a.batch, t0 + warp * kShare, lane);
+        const int t = t0 + warp * kShare + lane;
+        if (lane < kShare && t < a.batch.n_tokens) {
+            while (b + 1 < a.batch.n_seqs && a.batch.q_start[b + 1] <= t) b++;
+            const Seq s = load_seq(a.batch, b);
+            const int i = t - s.q0, e = s.ctx + i;
+            long long code = -2, sc = 0;
+            if (!s.bad && i >= 0 && i < s.n) {
+                const int page = entry_page(a.batch, b, e);
+                code = -1;
+                if (page >= 0) {
+                    code = entry_offset(a.batch, a.cache, page, e);
+                    sc = scale_index(a.batch, a.scales, a.n_kv_heads, page, 0, e);
+                } else {
+                    record_status(a.status, PP_ERR_INVALID_ARG);
+                }
             }
-        }
-        if (lane == 0) {
-            code_s[warp] = code;
-            scale_s[warp] = sc;
+            code_s[warp * kShare + lane] = code;
+            scale_s[warp * kShare + lane] = sc;
         }
     }
     if (tid == 0)

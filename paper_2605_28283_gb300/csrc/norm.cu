@@ -11,6 +11,7 @@
 
 #include "pp_head.cuh"
 #include "pp_launch.cuh"
+#include "pp_tc.cuh"
 
 namespace pp {
 namespace {
@@ -65,19 +66,27 @@ __global__ void __launch_bounds__(256) norm_kernel(const NormArgs a) {
     }
 }
 
-// Backward: the first ctas_q CTAs take the rows of q, the others those of k,
-// each every ctas-th token; a thread adds its columns' part of dgamma up over
-// all its rows, and the CTA leaves one row of sums, so that the result does
+// Backward: the first ctas_q CTAs take the rows of q, the others those of k, in
+// steps of as many rows as the CTA has groups (a few tokens' rows, or part of
+// one's), every ctas-th step.  A thread copies what it will use of the next
+// kStages - 1 steps into shared memory by cp.async, for itself alone, so that
+// enough is on its way without registers; the factors of the next step's tokens
+// are computed behind the present one.  It adds its columns' part of dgamma up
+// over all its rows, and the CTA leaves one row of sums, so that the result does
 // not depend on the order in which CTAs run.
+constexpr int kStages = 4;
+constexpr int kGradSmem = 200 * 1024;  // 64 KB of stages, and up to 64 tokens' factors twice
+
 template <typename T, int V, bool HALF, int UPL>
 __global__ void __launch_bounds__(256) norm_grad_kernel(const NormArgs a) {
     using Lane = HeadLane<T, V, HALF, UPL>;
-    __shared__ __align__(16) float2 cs[128];
+    constexpr int kBytes = Lane::kBytes, kVecs = 4 * UPL;  // vectors of x and dy a thread and step
+    extern __shared__ __align__(16) unsigned char smem[];
     __shared__ float sums[256 * UPL * 2 * V];
     pdl_launch_dependents();
     pdl_wait();
     const HeadArgs& h = a.head;
-    const int tid = threadIdx.x, groups = (int)blockDim.x / h.group, D = h.head_dim;
+    const int tid = threadIdx.x, groups = (int)blockDim.x / h.group, D = h.head_dim, pairs = h.rot_dim / 2;
     const bool key = (int)blockIdx.x >= a.ctas_q;
     const int first = key ? (int)blockIdx.x - a.ctas_q : (int)blockIdx.x, ctas = key ? a.ctas_k : a.ctas_q;
     const int rows = key ? a.n_kv_heads : a.n_heads;
@@ -87,61 +96,119 @@ __global__ void __launch_bounds__(256) norm_grad_kernel(const NormArgs a) {
     const long long xstr = key ? a.k_stride : a.q_stride, gstr = key ? a.k_grad_stride : a.q_grad_stride,
                     ostr = key ? a.k_out_stride : a.q_out_stride;
     const Lane lane(h, tid % h.group);
+    const int gi = tid / h.group, chunks = (rows + groups - 1) / groups, tokens = max(1, groups / rows);
+    const int my_token = chunks == 1 ? gi / rows : 0, my_row = gi - my_token * rows;
+    const int steps = (a.n_tokens + tokens - 1) / tokens * chunks;
+    const int pitch = (pairs + V - 1) / V, table = V * pitch;  // factors of a token
+    unsigned char* mine = smem + tid * kBytes;                 // vector v of stage s at ((s * kVecs + v) * 256 + tid)
+    float2* cs = reinterpret_cast<float2*>(smem + kStages * kVecs * 256 * kBytes);  // two steps' tables
+    // token and row of this thread in step s; false: none
+    auto place = [&](int s, int& t, int& r) {
+        const int c = chunks == 1 ? 0 : s % chunks;
+        t = (chunks == 1 ? s : s / chunks) * tokens + my_token;
+        r = c * groups + my_row;
+        return s < steps && my_token < tokens && t < a.n_tokens && r < rows;
+    };
+    auto fetch = [&](int s, int stage) {
+        int t, r;
+        if (place(s, t, r)) {
+            const char* x = xs + t * xstr + (long long)r * D * (int)sizeof(T);
+            const char* g = gs + t * gstr + (long long)r * D * (int)sizeof(T);
+            unsigned char* to = mine + stage * kVecs * 256 * kBytes;
+#pragma unroll
+            for (int k = 0; k < UPL; k++) {
+                if (lane.va[k] >= 0) {
+                    cp_async_small<kBytes>(to + (4 * k) * 256 * kBytes, x + lane.va[k] * kBytes);
+                    cp_async_small<kBytes>(to + (4 * k + 1) * 256 * kBytes, g + lane.va[k] * kBytes);
+                }
+                if (lane.vb[k] >= 0) {
+                    cp_async_small<kBytes>(to + (4 * k + 2) * 256 * kBytes, x + lane.vb[k] * kBytes);
+                    cp_async_small<kBytes>(to + (4 * k + 3) * 256 * kBytes, g + lane.vb[k] * kBytes);
+                }
+            }
+        }
+        cp_async_commit();
+    };
+    // factor i of a step's table: token i / pairs of the step
+    auto position = [&](int s, int i) {
+        const int t = (chunks == 1 ? s : s / chunks) * tokens + i / pairs;
+        return s < steps && i < tokens * pairs && t < a.n_tokens ? h.positions[t] : 0;
+    };
+    auto fill = [&](int s, int buf, int i, int pos) {
+        const int n = i / pairs, p = i - n * pairs;
+        const float2 v = cos_sin(pos, h.inv_freq[p]);
+        cs[(buf * tokens + n) * table + pair_slot(p, V, pitch)] = make_float2(v.x * h.scale, -v.y * h.scale);
+    };
     float gamma[UPL][2][V], acc[UPL][2][V] = {};
     lane.weights(key ? a.k_gamma : a.q_gamma, gamma);
-    float2 c[UPL][V];
-    for (int t = first; t < a.n_tokens; t += ctas) {
-        if (h.rot_dim > 0) {
-            __syncthreads();  // the last token's factors have been read
-            fill_pairs(cs, h, V, h.positions[t], true, tid, blockDim.x);
-            __syncthreads();
-            lane.factors(cs, h, c);
-        }
-        for (int r0 = 0; r0 < rows; r0 += groups) {
-            const int r = r0 + tid / h.group;
-            const bool in = r < rows;
-            const long long head = (long long)r * D * (int)sizeof(T);
-            Vec<T, V> x[UPL][2], dy[UPL][2];
-            float f[UPL][2][V] = {}, g[UPL][2][V] = {}, u[UPL][2][V];
-            if (in) {
-                lane.load(xs + t * xstr + head, x);
-                lane.load(gs + t * gstr + head, dy);
-                lane.widen(x, f);
-                lane.widen(dy, g);
-                if (h.rot_dim > 0) lane.rotate(g, c);
+#pragma unroll
+    for (int i = 0; i < kStages - 1; i++) fetch(first + i * ctas, i);
+    for (int i = tid; i < tokens * pairs; i += 256) fill(first, 0, i, position(first, i));
+    int n = 0;
+    for (int s = first; s < steps; s += ctas, n++) {
+        fetch(s + (kStages - 1) * ctas, (n + kStages - 1) % kStages);
+        const int next = s + ctas, pos = pairs ? position(next, tid) : 0;
+        cp_async_wait<kStages - 1>();
+        __syncthreads();  // this step's factors are there, the last step's have been read
+        int t, r;
+        const bool in = place(s, t, r);
+        float f[UPL][2][V] = {}, g[UPL][2][V] = {};
+        Vec<T, V> x[UPL][2], dy[UPL][2];
+        if (in) {
+            const unsigned char* from = mine + n % kStages * kVecs * 256 * kBytes;
+#pragma unroll
+            for (int k = 0; k < UPL; k++) {
+                x[k][0].raw = *reinterpret_cast<const decltype(x[0][0].raw)*>(from + (4 * k) * 256 * kBytes);
+                dy[k][0].raw = *reinterpret_cast<const decltype(x[0][0].raw)*>(from + (4 * k + 1) * 256 * kBytes);
+                x[k][1].raw = *reinterpret_cast<const decltype(x[0][0].raw)*>(from + (4 * k + 2) * 256 * kBytes);
+                dy[k][1].raw = *reinterpret_cast<const decltype(x[0][0].raw)*>(from + (4 * k + 3) * 256 * kBytes);
             }
+            lane.widen(x, f);
+            lane.widen(dy, g);
+            if (pairs) {
+                float2 c[UPL][V];
+                lane.factors(cs + ((n & 1) * tokens + my_token) * table, h, c);
+                lane.rotate(g, c);
+            }
+        }
+        float ux = 0.f;
 #pragma unroll
-            for (int k = 0; k < UPL; k++)
+        for (int k = 0; k < UPL; k++)
 #pragma unroll
-                for (int i = 0; i < V; i++) {
-                    u[k][0][i] = g[k][0][i] * gamma[k][0][i];
-                    u[k][1][i] = g[k][1][i] * gamma[k][1][i];
-                }
-            const float ss = Lane::group_sum(Lane::dot(f, f), h.group), ux = Lane::group_sum(Lane::dot(u, f), h.group);
-            if (!in) continue;
+            for (int v = 0; v < 2; v++)
+#pragma unroll
+                for (int i = 0; i < V; i++) ux = fmaf(g[k][v][i] * gamma[k][v][i], f[k][v][i], ux);
+        const float ss = Lane::group_sum(Lane::dot(f, f), h.group);
+        ux = Lane::group_sum(ux, h.group);
+        if (in) {
             const float inv = inverse_rms(ss, h), along = inv * inv * ux / (float)D;
 #pragma unroll
             for (int k = 0; k < UPL; k++)
 #pragma unroll
-                for (int s = 0; s < 2; s++)
+                for (int v = 0; v < 2; v++)
 #pragma unroll
                     for (int i = 0; i < V; i++) {
-                        acc[k][s][i] = fmaf(g[k][s][i], f[k][s][i] * inv, acc[k][s][i]);
-                        f[k][s][i] = inv * (u[k][s][i] - f[k][s][i] * along);
+                        acc[k][v][i] = fmaf(g[k][v][i], f[k][v][i] * inv, acc[k][v][i]);
+                        f[k][v][i] = inv * (g[k][v][i] * gamma[k][v][i] - f[k][v][i] * along);
                     }
             lane.narrow(f, x);
-            lane.store(os + t * ostr + head, x);
+            lane.store(os + t * ostr + (long long)r * D * (int)sizeof(T), x);
+        }
+        if (next < steps) {
+            if (tid < tokens * pairs) fill(next, (n + 1) & 1, tid, pos);
+            for (int i = tid + 256; i < tokens * pairs; i += 256) fill(next, (n + 1) & 1, i, position(next, i));
         }
     }
+    cp_async_wait<0>();
     if (!a.part) return;
 #pragma unroll
     for (int k = 0; k < UPL; k++)
 #pragma unroll
-        for (int s = 0; s < 2; s++) {
-            const int v = s ? lane.vb[k] : lane.va[k];
-            if (v < 0) continue;
+        for (int v = 0; v < 2; v++) {
+            const int at = v ? lane.vb[k] : lane.va[k];
+            if (at < 0) continue;
 #pragma unroll
-            for (int i = 0; i < V; i++) sums[tid / h.group * D + v * V + i] = acc[k][s][i];
+            for (int i = 0; i < V; i++) sums[gi * D + at * V + i] = acc[k][v][i];
         }
     __syncthreads();
     for (int d = tid; d < D; d += blockDim.x) {
@@ -183,8 +250,16 @@ cudaError_t norm_go(NormArgs a, bool grad, cudaStream_t st) {
     constexpr int kMost = V == 2 ? 2 : 1;  // two units a lane: more than 128 elements in vectors of 2
     const bool two = units > group;
     if (grad) {
+        const int groups = 256 / group, pairs = (a.head.rot_dim / 2 + V - 1) / V * V;
+        // tables of two steps' tokens (fewer heads: more tokens a step)
+        int tokens = std::max(1, groups / a.n_heads);
+        if (a.n_kv_heads) tokens = std::max(tokens, std::max(1, groups / a.n_kv_heads));
+        const int smem = kStages * 4 * (two ? 2 : 1) * 256 * V * (int)sizeof(T) + 2 * tokens * pairs * 8;
         auto* kern = two ? norm_grad_kernel<T, V, HALF, kMost> : norm_grad_kernel<T, V, HALF, 1>;
-        return launch_overlapped(kern, dim3((unsigned)(a.ctas_q + a.ctas_k)), dim3(256), 0, st, a);
+        static std::atomic<bool> allowed[2][64];
+        const cudaError_t e = allow_smem(kern, kGradSmem, allowed[two]);
+        if (e != cudaSuccess) return e;
+        return launch_overlapped(kern, dim3((unsigned)(a.ctas_q + a.ctas_k)), dim3(256), (size_t)smem, st, a);
     }
     const int rows = a.n_heads + a.n_kv_heads;
     int threads = (rows * group / 10 + 31) / 32 * 32;

@@ -45,6 +45,15 @@ struct Vec {
     }
 };
 
+// cp.async of 4, 8 or 16 bytes.
+template <int BYTES>
+PP_DEVINL void cp_async_small(void* dst, const void* src) {
+    if constexpr (BYTES == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+    else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(smem_u32(dst)), "l"(src), "n"(BYTES) : "memory");
+}
+
 // cos and sin of pos * f (f in radians) at any 32-bit position: the frequency
 // is taken in units of 2^-64 turn, where the product with the position wraps
 // at whole turns by itself, so that the angle is rounded only once, when the
