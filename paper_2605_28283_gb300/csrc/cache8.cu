@@ -60,11 +60,23 @@ PP_DEVINL Slot find_slot(const BatchArgs& B, int shift, int slot, int lane, unsi
     return s;
 }
 
-template <int V>
-PP_DEVINL void store_codes(char* p, const float (&f)[V], float inv) {
+// Values times inv as codes.  ODD: some may not be finite (infinities would be
+// held as 448 otherwise; NaN is the NaN code either way).
+template <int V, bool ODD = false>
+PP_DEVINL void store_codes(char* p, const F2 (&f)[V / 2], float inv) {
     uint32_t w[V > 4 ? V / 4 : 1] = {};
+    const F2 inv2 = pair2(inv, inv);
 #pragma unroll
-    for (int i = 0; i < V; i += 2) w[i / 4] |= to_codes(to_hold(f[i]) * inv, to_hold(f[i + 1]) * inv) << (i % 4 * 8);
+    for (int i = 0; i < V; i += 2) {
+        float a, b;
+        unpair2(f[i / 2], a, b);
+        if (ODD) {
+            a = to_hold(a);
+            b = to_hold(b);
+        }
+        unpair2(mul2(pair2(a, b), inv2), a, b);
+        w[i / 4] |= to_codes(a, b) << (i % 4 * 8);
+    }
     if constexpr (V == 8)
         *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
     else if constexpr (V == 4)
@@ -75,12 +87,11 @@ PP_DEVINL void store_codes(char* p, const float (&f)[V], float inv) {
 // V codes at p rounded again at another scale.
 template <int V>
 PP_DEVINL void again(char* p, float ratio) {
-    float f[V];
+    F2 f[V / 2];
 #pragma unroll
     for (int i = 0; i < V; i += 2) {
         const float2 v = from_codes(*reinterpret_cast<const uint16_t*>(p + i));
-        f[i] = v.x;
-        f[i + 1] = v.y;
+        f[i / 2] = pair2(v.x, v.y);
     }
     store_codes<V>(p, f, ratio);
 }
@@ -88,7 +99,7 @@ PP_DEVINL void again(char* p, float ratio) {
 template <typename T, int V, bool HALF, int UPL, int ITER, int WARPS>
 __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 2 : 1) append8_kernel(const Append8Args a) {
     using Lane = HeadLane<T, V, HALF, UPL>;
-    extern __shared__ __align__(16) float2 cs[];
+    extern __shared__ __align__(16) float cs[];
     __shared__ Slot slot_s;
     __shared__ int pos_s[kMaxStrips], in_s[kMaxStrips];
     __shared__ float amax_s[kMaxStrips];
@@ -108,7 +119,7 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 2 : 1) append8_kernel
         const char* q = a.q + t * a.q_stride;
         char* out = a.q_out + t * a.q_out_stride;
         const int pitch = (h.rot_dim / 2 + V - 1) / V;
-        float2* table = cs + team * (pitch * V);
+        float* table = cs + team * (pitch * V * 2);
         if (in_team < 32 && exists) {
             const int b = find_seq(a.batch, t, l32);
             const Seq s = load_seq(a.batch, b);
@@ -119,7 +130,7 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 2 : 1) append8_kernel
                 in_s[team] = in;
             }
         }
-        float2 c[UPL][V];
+        typename Lane::Factors c;
         bool ready = false, in = false;
         for (int r0 = y * groups; r0 < a.n_heads; r0 += 2 * step) {
             Vec<T, V> x[2][UPL][2];
@@ -132,7 +143,7 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 2 : 1) append8_kernel
                 __syncthreads();
                 in = exists && in_s[team];  // padding, or a skipped sequence: nothing is written
                 if (h.rot_dim > 0) {
-                    if (in) fill_pairs(table, h, V, pos_s[team], false, in_team, a.team);
+                    if (in) fill_pairs(table, h, V, pos_s[team], in_team, a.team);
                     __syncthreads();
                     lane.factors(table, h, c);
                 }
@@ -141,7 +152,7 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 2 : 1) append8_kernel
 #pragma unroll
             for (int n = 0; n < 2; n++) {
                 const int r = r0 + n * step + in_team / h.group;
-                float f[UPL][2][V], g[UPL][2][V];
+                F2 f[UPL][2][V / 2], g[UPL][2][V / 2];
                 lane.widen(x[n], f);
                 if (h.norm) {
                     const float inv = inverse_rms(Lane::group_sum(r < a.n_heads && exists ? Lane::dot(f, f) : 0.f, h.group), h);
@@ -150,7 +161,7 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 2 : 1) append8_kernel
                 }
                 if (r >= a.n_heads || !in) continue;
                 if (h.rot_dim > 0) lane.rotate(f, c);
-                if (h.norm || h.rot_dim > 0) lane.narrow(f, x[n]);
+                if (h.norm || h.rot_dim > 0) Lane::narrow(f, x[n]);
                 lane.store(out + (long long)r * D * (int)sizeof(T), x[n]);
             }
         }
@@ -177,7 +188,7 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 2 : 1) append8_kernel
     for (int i = tid; i < factors; i += blockDim.x) {
         const int row = i / (h.rot_dim / 2), p = i - row * (h.rot_dim / 2), t = s.token + row;
         const float2 v = cos_sin(h.positions ? h.positions[t] : s.e0 + row, h.inv_freq[p]);
-        cs[(s.e0 - s.lo + row) * row_pairs + pair_slot(p, V, pitch)] = make_float2(v.x * h.scale, v.y * h.scale);
+        put_pair(cs + (s.e0 - s.lo + row) * row_pairs * 2, p, V, pitch, make_float2(v.x * h.scale, v.y * h.scale));
     }
     // A thread's vectors of the next units on their way into shared memory, for itself alone: loads in registers would
     // leave too few of them in flight (8192 tokens, 40 heads of 128: 199 us).
@@ -221,7 +232,7 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 2 : 1) append8_kernel
         float* scale_p = (key ? a.scales.k : a.scales.v) + at;
         const bool cached = s.lo < s.ctx;
         float old = have && cached && l32 == 0 ? *scale_p : 0.f;
-        float f[ITER][UPL][2][V];
+        F2 f[ITER][UPL][2][V / 2];
         if (a.stages) {
             fetch(u0 + (a.stages - 1) * a.parts * units, (turn + a.stages - 1) % a.stages);
             if (a.stages == 1)
@@ -254,31 +265,57 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 2 : 1) append8_kernel
 #pragma unroll
                     for (int k = 0; k < UPL; k++)
 #pragma unroll
-                        for (int i = 0; i < V; i++) f[n][k][0][i] = f[n][k][1][i] = 0.f;
+                        for (int i = 0; i < V / 2; i++) f[n][k][0][i] = f[n][k][1][i] = 0ull;
                 }
                 if (!key) continue;
                 if (h.norm) {
-                    float g[UPL][2][V];
+                    F2 g[UPL][2][V / 2];
                     const float inv = inverse_rms(Lane::group_sum(Lane::dot(f[n], f[n]), h.group), h);
                     lane.weights(a.k_gamma, g);
                     if (in) Lane::scale_by(f[n], inv, g);
                 }
                 if (h.rot_dim > 0 && in) {
-                    float2 c[UPL][V];
-                    lane.factors(cs + (e - s.lo) * row_pairs, h, c);
+                    typename Lane::Factors c;
+                    lane.factors(cs + (e - s.lo) * row_pairs * 2, h, c);
                     lane.rotate(f[n], c);
                 }
             }
         }
         float amax = 0.f;
+        bool odd = false;
         if (have) {
+            // 0 x summed is zero for finite values alone
+            F2 zero = 0ull;
 #pragma unroll
             for (int n = 0; n < ITER; n++)
 #pragma unroll
                 for (int k = 0; k < UPL; k++)
 #pragma unroll
-                    for (int i = 0; i < V; i++)
-                        amax = fmaxf(amax, fmaxf(magnitude(f[n][k][0][i]), magnitude(f[n][k][1][i])));
+                    for (int v = 0; v < 2; v++)
+#pragma unroll
+                        for (int i = 0; i < V / 2; i++) {
+                            float x, y;
+                            unpair2(f[n][k][v][i], x, y);
+                            amax = max3(amax, fabsf(x), fabsf(y));
+                            zero = fma2(f[n][k][v][i], 0ull, zero);
+                        }
+            float x, y;
+            unpair2(zero, x, y);
+            odd = __any_sync(kFull, x != 0.f || y != 0.f);
+            if (odd) {
+                amax = 0.f;
+#pragma unroll
+                for (int n = 0; n < ITER; n++)
+#pragma unroll
+                    for (int k = 0; k < UPL; k++)
+#pragma unroll
+                        for (int v = 0; v < 2; v++)
+#pragma unroll
+                            for (int i = 0; i < V / 2; i++) {
+                                unpair2(f[n][k][v][i], x, y);
+                                amax = max3(amax, magnitude(x), magnitude(y));
+                            }
+            }
             amax = warp_max(amax);
             old = __shfl_sync(kFull, old, 0);
         }
@@ -312,8 +349,13 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 2 : 1) append8_kernel
             char* row = dst + (e - s.lo) * a.cache.token_stride;
 #pragma unroll
             for (int k = 0; k < UPL; k++) {
-                if (lane.va[k] >= 0) store_codes<V>(row + lane.va[k] * V, f[n][k][0], inv);
-                if (lane.vb[k] >= 0) store_codes<V>(row + lane.vb[k] * V, f[n][k][1], inv);
+                if (!odd) {
+                    if (lane.va[k] >= 0) store_codes<V>(row + lane.va[k] * V, f[n][k][0], inv);
+                    if (lane.vb[k] >= 0) store_codes<V>(row + lane.vb[k] * V, f[n][k][1], inv);
+                } else {
+                    if (lane.va[k] >= 0) store_codes<V, true>(row + lane.va[k] * V, f[n][k][0], inv);
+                    if (lane.vb[k] >= 0) store_codes<V, true>(row + lane.vb[k] * V, f[n][k][1], inv);
+                }
             }
         }
         if (l32 == 0 && strip == 0 && now != old) *scale_p = now;
@@ -383,22 +425,23 @@ cudaError_t append8_typed(const Append8Args& a, int layout, int block, cudaStrea
 }
 
 // --------------------------------------------------------------------- read
-// kReadTokens tokens a CTA: a warp looks the entries of its share up, then all
-// threads go over the rows, V codes (a 16-byte store) at a time.
+// 8 * share tokens a CTA (gridDim.y of them share the tokens' rows, where there
+// are few): a warp looks the entries of its share up, then all threads go over
+// the rows, V codes (a 16-byte store) at a time.
 constexpr int kReadTokens = 32, kReadUnits = 4;
 
 template <typename T>
-__global__ void __launch_bounds__(256) read8_kernel(const Read8Args a) {
-    constexpr int V = 16 / (int)sizeof(T), kShare = kReadTokens / 8;
+__global__ void __launch_bounds__(256) read8_kernel(const Read8Args a, const int share) {
+    constexpr int V = 16 / (int)sizeof(T);
     __shared__ long long code_s[kReadTokens], scale_s[kReadTokens];  // -1: zeros, -2: left alone
     pdl_launch_dependents();
     pdl_wait();
-    const int t0 = (int)blockIdx.x * kReadTokens, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (t0 + warp * kShare < a.batch.n_tokens) {
+    const int t0 = (int)blockIdx.x * 8 * share, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (t0 + warp * share < a.batch.n_tokens) {
         // the sequence of the share's first token; from there a lane for each token
-        int b = find_seq(a.batch, t0 + warp * kShare, lane);
-        const int t = t0 + warp * kShare + lane;
-        if (lane < kShare && t < a.batch.n_tokens) {
+        int b = find_seq(a.batch, t0 + warp * share, lane);
+        const int t = t0 + warp * share + lane;
+        if (lane < share && t < a.batch.n_tokens) {
             while (b + 1 < a.batch.n_seqs && a.batch.q_start[b + 1] <= t) b++;
             const Seq s = load_seq(a.batch, b);
             const int i = t - s.q0, e = s.ctx + i;
@@ -413,48 +456,61 @@ __global__ void __launch_bounds__(256) read8_kernel(const Read8Args a) {
                     record_status(a.status, PP_ERR_INVALID_ARG);
                 }
             }
-            code_s[warp * kShare + lane] = code;
-            scale_s[warp * kShare + lane] = sc;
+            code_s[warp * share + lane] = code;
+            scale_s[warp * share + lane] = sc;
         }
     }
-    if (tid == 0)
+    if (tid == 0 && blockIdx.y == 0)
         for (int b = blockIdx.x; b < a.batch.n_seqs; b += gridDim.x)
             if (load_seq(a.batch, b).bad) record_status(a.status, PP_ERR_INVALID_ARG);
     __syncthreads();
-    const int tokens = min(kReadTokens, a.batch.n_tokens - t0);
-    const int per = a.head_dim / V, row = a.n_kv_heads * per, total = tokens * 2 * row;
-    for (int u0 = tid; u0 < total; u0 += kReadUnits * 256) {
-        typename Raw<V>::type w[kReadUnits];
+    // a thread keeps to one place of a row of keys and values and goes over the tokens; rows shorter than the CTA: as
+    // many tokens at once as fit
+    const int tokens = min(8 * share, a.batch.n_tokens - t0);
+    const int per = a.head_dim / V, row = 2 * a.n_kv_heads * per;
+    const int width = min(row, 256), at_once = 256 / width, lines = (tokens + at_once - 1) / at_once;
+    const int mine = tid / width, col0 = tid - mine * width;
+    if (mine >= at_once) return;
+    // (columns, lines) of the CTA in chunks of kReadUnits lines, dealt over gridDim.y
+    const int chunks = (lines + kReadUnits - 1) / kReadUnits, cols = (row + width - 1) / width;
+    for (int w = blockIdx.y; w < chunks * cols; w += gridDim.y) {
+        const int c = w % cols, u = c * width + col0, n0 = w / cols * kReadUnits;
+        if (u >= row) continue;
+        const bool key = u < row / 2;
+        const int x = key ? u : u - row / 2, head = x / per;
+        const char* codes = (key ? a.cache.k : a.cache.v) + head * a.cache.head_stride + (x - head * per) * V;
+        const float* scales = (key ? a.scales.k : a.scales.v) + (long long)head * a.scales.blocks;
+        const long long stride = key ? a.k_stride : a.v_stride;
+        char* out = (key ? a.k_out : a.v_out) + t0 * stride + (long long)x * 16;
+        typename Raw<V>::type code[kReadUnits];
         float sc[kReadUnits];
-        char* dst[kReadUnits];
+        int n[kReadUnits];
 #pragma unroll
         for (int k = 0; k < kReadUnits; k++) {
-            const int u = u0 + k * 256;
-            dst[k] = nullptr;
-            w[k] = {};
+            n[k] = (n0 + k) * at_once + mine;
+            code[k] = {};
             sc[k] = 0.f;
-            if (u >= total) continue;
-            const int n = u / (2 * row), r = u - n * 2 * row, key = r < row, x = key ? r : r - row;
-            const int head = x / per, c = x - head * per;
-            const long long code = code_s[n];
-            if (code == -2) continue;
-            dst[k] = (key ? a.k_out + (t0 + n) * a.k_stride : a.v_out + (t0 + n) * a.v_stride) + (long long)x * 16;
-            if (code < 0) continue;
-            w[k] = __ldcs(reinterpret_cast<const typename Raw<V>::type*>((key ? a.cache.k : a.cache.v) + code +
-                                                                        head * a.cache.head_stride + c * V));
-            sc[k] = (key ? a.scales.k : a.scales.v)[scale_s[n] + (long long)head * a.scales.blocks];
+            if (n[k] >= tokens || code_s[n[k]] == -2) {
+                n[k] = -1;
+            } else if (code_s[n[k]] >= 0) {
+                code[k] = __ldcs(reinterpret_cast<const typename Raw<V>::type*>(codes + code_s[n[k]]));
+                sc[k] = scales[scale_s[n[k]]];
+            }
         }
 #pragma unroll
         for (int k = 0; k < kReadUnits; k++) {
-            if (!dst[k]) continue;
-            Vec<T, V> out;
-            const uint32_t* words = reinterpret_cast<const uint32_t*>(&w[k]);
+            if (n[k] < 0) continue;
+            Vec<T, V> y;
+            const uint32_t* words = reinterpret_cast<const uint32_t*>(&code[k]);
+            const F2 sc2 = pair2(sc[k], sc[k]);
 #pragma unroll
             for (int i = 0; i < V; i += 2) {
                 const float2 v = from_codes(words[i / 4] >> (i % 4 * 8) & 0xffffu);
-                out.set2(i, v.x * sc[k], v.y * sc[k]);
+                float p, q;
+                unpair2(mul2(pair2(v.x, v.y), sc2), p, q);
+                y.set2(i, p, q);
             }
-            out.store(dst[k]);
+            y.store(out + n[k] * stride);
         }
     }
 }
@@ -603,9 +659,15 @@ cudaError_t append8_launch(const Append8Args& a, int dtype, int layout, int bloc
 }
 
 cudaError_t read8_launch(const Read8Args& a, int dtype, cudaStream_t st) {
-    const unsigned ctas = (unsigned)((a.batch.n_tokens + kReadTokens - 1) / kReadTokens);
+    // four CTAs an SM at least, where there is that much to do
+    int share = kReadTokens / 8;
+    while (share > 1 && (a.batch.n_tokens + 8 * share - 1) / (8 * share) < 608) share /= 2;
+    const long long ctas = (a.batch.n_tokens + 8ll * share - 1) / (8 * share);
+    const int row = 2 * a.n_kv_heads * (a.head_dim / (dtype == PP_BF16 ? 8 : 4)), at_once = std::max(1, 256 / row);
+    const int chunks = ((8 * share + at_once - 1) / at_once + kReadUnits - 1) / kReadUnits * ((row + 255) / 256);
+    const long long split = std::min<long long>(chunks, (608 + ctas - 1) / ctas);
     auto* kern = dtype == PP_BF16 ? read8_kernel<__nv_bfloat16> : read8_kernel<float>;
-    return launch_overlapped(kern, dim3(ctas), dim3(256), 0, st, a);
+    return launch_overlapped(kern, dim3((unsigned)ctas, (unsigned)split), dim3(256), 0, st, a, share);
 }
 
 cudaError_t commit8_launch(const Commit8Args& a, cudaStream_t st) {

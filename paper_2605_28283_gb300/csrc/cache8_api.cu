@@ -114,6 +114,7 @@ pp_status pp_kvq_append(const pp_cache8* cache, const pp_batch* batch, const pp_
     a.scales = scale_args(*cache);
     a.head.positions = positions;
     a.head.head_dim = D;
+    a.head.inv_dim = 1.0f / (float)D;
     if (norm) {
         a.head.norm = true;
         a.head.eps = norm->eps;

@@ -23,14 +23,14 @@ constexpr int kRowsInFlight = 2;  // rows a group has in flight
 template <typename T, int V, bool HALF, int UPL>
 __global__ void __launch_bounds__(256) norm_kernel(const NormArgs a) {
     using Lane = HeadLane<T, V, HALF, UPL>;
-    __shared__ __align__(16) float2 cs[128];
+    __shared__ __align__(16) float cs[256];
     pdl_launch_dependents();
     pdl_wait();
     const HeadArgs& h = a.head;
     const int t = blockIdx.x, tid = threadIdx.x, groups = (int)blockDim.x / h.group;
     const Lane lane(h, tid % h.group);
     const int rows = a.n_heads + a.n_kv_heads, step = groups * (int)gridDim.y;
-    float2 c[UPL][V];
+    typename Lane::Factors c;
     bool ready = false;
     for (int r0 = (int)blockIdx.y * groups; r0 < rows; r0 += step * kRowsInFlight) {
         Vec<T, V> x[kRowsInFlight][UPL][2];
@@ -43,7 +43,7 @@ __global__ void __launch_bounds__(256) norm_kernel(const NormArgs a) {
             lane.load((key ? a.k + t * a.k_stride : a.q + t * a.q_stride) + head, x[n]);
         }
         if (!ready && h.rot_dim > 0) {
-            fill_pairs(cs, h, V, h.positions[t], false, tid, blockDim.x);
+            fill_pairs(cs, h, V, h.positions[t], tid, blockDim.x);
             __syncthreads();
             lane.factors(cs, h, c);
         }
@@ -52,7 +52,7 @@ __global__ void __launch_bounds__(256) norm_kernel(const NormArgs a) {
         for (int n = 0; n < kRowsInFlight; n++) {
             const int r = r0 + n * step + tid / h.group;
             const bool in = r < rows, key = r >= a.n_heads;
-            float f[UPL][2][V], g[UPL][2][V];
+            F2 f[UPL][2][V / 2], g[UPL][2][V / 2];
             lane.widen(x[n], f);
             const float inv = inverse_rms(Lane::group_sum(in ? Lane::dot(f, f) : 0.f, h.group), h);
             if (!in) continue;
@@ -101,7 +101,7 @@ __global__ void __launch_bounds__(256) norm_grad_kernel(const NormArgs a) {
     const int steps = (a.n_tokens + tokens - 1) / tokens * chunks;
     const int pitch = (pairs + V - 1) / V, table = V * pitch;  // factors of a token
     unsigned char* mine = smem + tid * kBytes;                 // vector v of stage s at ((s * kVecs + v) * 256 + tid)
-    float2* cs = reinterpret_cast<float2*>(smem + kStages * kVecs * 256 * kBytes);  // two steps' tables
+    float* cs = reinterpret_cast<float*>(smem + kStages * kVecs * 256 * kBytes);  // two steps' tables
     // token and row of this thread in step s; false: none
     auto place = [&](int s, int& t, int& r) {
         const int c = chunks == 1 ? 0 : s % chunks;
@@ -137,9 +137,9 @@ __global__ void __launch_bounds__(256) norm_grad_kernel(const NormArgs a) {
     auto fill = [&](int s, int buf, int i, int pos) {
         const int n = i / pairs, p = i - n * pairs;
         const float2 v = cos_sin(pos, h.inv_freq[p]);
-        cs[(buf * tokens + n) * table + pair_slot(p, V, pitch)] = make_float2(v.x * h.scale, -v.y * h.scale);
+        put_pair(cs + (buf * tokens + n) * table * 2, p, V, pitch, make_float2(v.x * h.scale, v.y * h.scale));
     };
-    float gamma[UPL][2][V], acc[UPL][2][V] = {};
+    F2 gamma[UPL][2][V / 2], acc[UPL][2][V / 2] = {};
     lane.weights(key ? a.k_gamma : a.q_gamma, gamma);
 #pragma unroll
     for (int i = 0; i < kStages - 1; i++) fetch(first + i * ctas, i);
@@ -152,7 +152,7 @@ __global__ void __launch_bounds__(256) norm_grad_kernel(const NormArgs a) {
         __syncthreads();  // this step's factors are there, the last step's have been read
         int t, r;
         const bool in = place(s, t, r);
-        float f[UPL][2][V] = {}, g[UPL][2][V] = {};
+        F2 f[UPL][2][V / 2] = {}, g[UPL][2][V / 2] = {};
         Vec<T, V> x[UPL][2], dy[UPL][2];
         if (in) {
             const unsigned char* from = mine + n % kStages * kVecs * 256 * kBytes;
@@ -166,30 +166,32 @@ __global__ void __launch_bounds__(256) norm_grad_kernel(const NormArgs a) {
             lane.widen(x, f);
             lane.widen(dy, g);
             if (pairs) {
-                float2 c[UPL][V];
-                lane.factors(cs + ((n & 1) * tokens + my_token) * table, h, c);
-                lane.rotate(g, c);
+                typename Lane::Factors c;
+                lane.factors(cs + ((n & 1) * tokens + my_token) * table * 2, h, c);
+                lane.template rotate<true>(g, c);
             }
         }
-        float ux = 0.f;
+        F2 u[UPL][2][V / 2];
 #pragma unroll
         for (int k = 0; k < UPL; k++)
 #pragma unroll
             for (int v = 0; v < 2; v++)
 #pragma unroll
-                for (int i = 0; i < V; i++) ux = fmaf(g[k][v][i] * gamma[k][v][i], f[k][v][i], ux);
-        const float ss = Lane::group_sum(Lane::dot(f, f), h.group);
-        ux = Lane::group_sum(ux, h.group);
+                for (int i = 0; i < V / 2; i++) u[k][v][i] = mul2(g[k][v][i], gamma[k][v][i]);
+        const float ss = Lane::group_sum(Lane::dot(f, f), h.group), ux = Lane::group_sum(Lane::dot(u, f), h.group);
         if (in) {
-            const float inv = inverse_rms(ss, h), along = inv * inv * ux / (float)D;
+            // with x r in place of x: dx = r (u - x r (r ux / D))
+            const float inv = inverse_rms(ss, h), along = -inv * ux * h.inv_dim;
+            const F2 inv2 = pair2(inv, inv), along2 = pair2(along, along);
 #pragma unroll
             for (int k = 0; k < UPL; k++)
 #pragma unroll
                 for (int v = 0; v < 2; v++)
 #pragma unroll
-                    for (int i = 0; i < V; i++) {
-                        acc[k][v][i] = fmaf(g[k][v][i], f[k][v][i] * inv, acc[k][v][i]);
-                        f[k][v][i] = inv * (g[k][v][i] * gamma[k][v][i] - f[k][v][i] * along);
+                    for (int i = 0; i < V / 2; i++) {
+                        const F2 xr = mul2(f[k][v][i], inv2);
+                        acc[k][v][i] = fma2(g[k][v][i], xr, acc[k][v][i]);
+                        f[k][v][i] = mul2(fma2(xr, along2, u[k][v][i]), inv2);
                     }
             lane.narrow(f, x);
             lane.store(os + t * ostr + (long long)r * D * (int)sizeof(T), x);
@@ -208,7 +210,8 @@ __global__ void __launch_bounds__(256) norm_grad_kernel(const NormArgs a) {
             const int at = v ? lane.vb[k] : lane.va[k];
             if (at < 0) continue;
 #pragma unroll
-            for (int i = 0; i < V; i++) sums[gi * D + at * V + i] = acc[k][v][i];
+            for (int i = 0; i < V / 2; i++)
+                unpair2(acc[k][v][i], sums[gi * D + at * V + 2 * i], sums[gi * D + at * V + 2 * i + 1]);
         }
     __syncthreads();
     for (int d = tid; d < D; d += blockDim.x) {

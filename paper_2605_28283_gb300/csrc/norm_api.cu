@@ -35,6 +35,7 @@ NormArgs norm_args(const pp_head_norm* norm, const pp_rotation* rot, const int32
     a.head.norm = true;
     a.head.eps = norm->eps;
     a.head.head_dim = D;
+    a.head.inv_dim = 1.0f / (float)D;
     if (rot) {
         a.head.positions = positions;
         a.head.inv_freq = rot->inv_freq;

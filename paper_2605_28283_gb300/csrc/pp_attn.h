@@ -35,7 +35,7 @@ struct PageArgs {
 struct HeadArgs {
     const int32_t* positions;
     const float* inv_freq;
-    float scale, eps;
+    float scale, eps, inv_dim;  // inv_dim: 1 / head_dim
     int head_dim, rot_dim, group;
     bool norm;
 };

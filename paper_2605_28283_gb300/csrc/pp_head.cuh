@@ -10,6 +10,7 @@
 #pragma once
 
 #include "pp_attn.h"
+#include "pp_tc_attn.cuh"
 #include "pp_vec.cuh"
 
 namespace pp {
@@ -20,24 +21,31 @@ int head_units(const HeadArgs& h) {
     return (h.head_dim / V + 1) / 2;
 }
 
-// Per-token factors (cos, sin) in shared memory, laid out so that the 16-byte
-// reads of neighbouring units lie side by side: two pairs of unit u at
-// 16 (i / 2 * pitch + u).
-PP_DEVINL int pair_slot(int p, int V, int pitch) { return (p % V / 2 * pitch + p / V) * 2 + (p & 1); }
+// Per-token factors of the rotated pairs in shared memory: pairs p and p + 1 of
+// a unit side by side as (cos, cos, sin, sin), 16 bytes, and the units' side by
+// side for each such two, so that the 16-byte reads of neighbouring lanes do not
+// meet in a bank.
+PP_DEVINL void put_pair(float* cs, int p, int V, int pitch, float2 v) {
+    float* at = cs + (p % V / 2 * pitch + p / V) * 4 + (p & 1);
+    at[0] = v.x;
+    at[2] = v.y;
+}
 
 // Factors of one token by `n` threads.
-PP_DEVINL void fill_pairs(float2* cs, const HeadArgs& h, int V, int pos, bool inverse, int tid, int n) {
+PP_DEVINL void fill_pairs(float* cs, const HeadArgs& h, int V, int pos, int tid, int n) {
     const int pitch = (h.rot_dim / 2 + V - 1) / V;
     for (int p = tid; p < h.rot_dim / 2; p += n) {
         const float2 v = cos_sin(pos, h.inv_freq[p]);
-        cs[pair_slot(p, V, pitch)] = make_float2(v.x * h.scale, (inverse ? -v.y : v.y) * h.scale);
+        put_pair(cs, p, V, pitch, make_float2(v.x * h.scale, v.y * h.scale));
     }
 }
 
+using F2 = unsigned long long;  // two fp32 values, for the instructions that take two at once
+
 template <typename T, int V, bool HALF, int UPL>
 struct HeadLane {
-    static constexpr int kBytes = V * (int)sizeof(T);
-    int va[UPL], vb[UPL];          // vectors of the lane's units, or -1
+    static constexpr int kBytes = V * (int)sizeof(T), V2 = V / 2;
+    int va[UPL], vb[UPL];           // vectors of the lane's units, or -1
     bool turn_a[UPL], turn_b[UPL];  // rotated
     int unit[UPL];
 
@@ -55,8 +63,11 @@ struct HeadLane {
             if (vb[k] >= nvec) vb[k] = -1;
         }
     }
-    // (cos, sin) of the lane's pairs, from a token's table
-    PP_DEVINL void factors(const float2* cs, const HeadArgs& h, float2 (&f)[UPL][V]) const {
+    // cosines and sines of the lane's pairs, from a token's table
+    struct Factors {
+        float c[UPL][V], s[UPL][V];
+    };
+    PP_DEVINL void factors(const float* cs, const HeadArgs& h, Factors& f) const {
         const int pitch = (h.rot_dim / 2 + V - 1) / V;
 #pragma unroll
         for (int k = 0; k < UPL; k++) {
@@ -64,9 +75,11 @@ struct HeadLane {
 #pragma unroll
             for (int i = 0; i < V; i += 2) {
                 if (!HALF && i * 2 >= V && !turn_b[k]) continue;
-                const float4 v = *reinterpret_cast<const float4*>(cs + (i / 2 * pitch + unit[k]) * 2);
-                f[k][i] = make_float2(v.x, v.y);
-                f[k][i + 1] = make_float2(v.z, v.w);
+                const float4 v = *reinterpret_cast<const float4*>(cs + (i / 2 * pitch + unit[k]) * 4);
+                f.c[k][i] = v.x;
+                f.c[k][i + 1] = v.y;
+                f.s[k][i] = v.z;
+                f.s[k][i + 1] = v.w;
             }
         }
     }
@@ -85,37 +98,39 @@ struct HeadLane {
         }
     }
     // fp32 values (zeros where the lane holds nothing)
-    PP_DEVINL void widen(const Vec<T, V> (&x)[UPL][2], float (&f)[UPL][2][V]) const {
+    PP_DEVINL void widen(const Vec<T, V> (&x)[UPL][2], F2 (&f)[UPL][2][V2]) const {
 #pragma unroll
         for (int k = 0; k < UPL; k++)
 #pragma unroll
-            for (int i = 0; i < V; i++) {
-                f[k][0][i] = va[k] >= 0 ? x[k][0].get(i) : 0.f;
-                f[k][1][i] = vb[k] >= 0 ? x[k][1].get(i) : 0.f;
+            for (int i = 0; i < V2; i++) {
+                f[k][0][i] = va[k] >= 0 ? pair2(x[k][0].get(2 * i), x[k][0].get(2 * i + 1)) : 0ull;
+                f[k][1][i] = vb[k] >= 0 ? pair2(x[k][1].get(2 * i), x[k][1].get(2 * i + 1)) : 0ull;
             }
     }
-    PP_DEVINL void narrow(const float (&f)[UPL][2][V], Vec<T, V> (&x)[UPL][2]) const {
+    PP_DEVINL static void narrow(const F2 (&f)[UPL][2][V2], Vec<T, V> (&x)[UPL][2]) {
 #pragma unroll
         for (int k = 0; k < UPL; k++)
 #pragma unroll
-            for (int i = 0; i < V; i += 2) {
-                x[k][0].set2(i, f[k][0][i], f[k][0][i + 1]);
-                x[k][1].set2(i, f[k][1][i], f[k][1][i + 1]);
-            }
+            for (int v = 0; v < 2; v++)
+#pragma unroll
+                for (int i = 0; i < V2; i++) {
+                    float a, b;
+                    unpair2(f[k][v][i], a, b);
+                    x[k][v].set2(2 * i, a, b);
+                }
     }
     // weights of a norm (of elements, in T); ones without
-    PP_DEVINL void weights(const char* gamma, float (&g)[UPL][2][V]) const {
+    PP_DEVINL void weights(const char* gamma, F2 (&g)[UPL][2][V2]) const {
 #pragma unroll
         for (int k = 0; k < UPL; k++)
 #pragma unroll
             for (int s = 0; s < 2; s++) {
                 const int v = s ? vb[k] : va[k];
-                typename Raw<kBytes>::type w{};
-                if (gamma && v >= 0) w = *reinterpret_cast<const typename Raw<kBytes>::type*>(gamma + v * kBytes);
                 Vec<T, V> x;
-                x.raw = w;
+                x.raw = typename Raw<kBytes>::type{};
+                if (gamma && v >= 0) x.raw = *reinterpret_cast<const typename Raw<kBytes>::type*>(gamma + v * kBytes);
 #pragma unroll
-                for (int i = 0; i < V; i++) g[k][s][i] = gamma ? x.get(i) : 1.f;
+                for (int i = 0; i < V2; i++) g[k][s][i] = gamma ? pair2(x.get(2 * i), x.get(2 * i + 1)) : pair2(1.f, 1.f);
             }
     }
     // the group's sum of a value a lane
@@ -123,54 +138,62 @@ struct HeadLane {
         for (int o = group >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
         return v;
     }
-    PP_DEVINL static float dot(const float (&a)[UPL][2][V], const float (&b)[UPL][2][V]) {
-        float s[2] = {0.f, 0.f};
+    PP_DEVINL static float dot(const F2 (&a)[UPL][2][V2], const F2 (&b)[UPL][2][V2]) {
+        F2 s[2] = {0ull, 0ull};
 #pragma unroll
         for (int k = 0; k < UPL; k++)
 #pragma unroll
-            for (int i = 0; i < V; i++) {
-                s[0] = fmaf(a[k][0][i], b[k][0][i], s[0]);
-                s[1] = fmaf(a[k][1][i], b[k][1][i], s[1]);
+            for (int i = 0; i < V2; i++) {
+                s[0] = fma2(a[k][0][i], b[k][0][i], s[0]);
+                s[1] = fma2(a[k][1][i], b[k][1][i], s[1]);
             }
-        return s[0] + s[1];
+        float x, y;
+        unpair2(add2(s[0], s[1]), x, y);
+        return x + y;
     }
-    PP_DEVINL void rotate(float (&f)[UPL][2][V], const float2 (&c)[UPL][V]) const {
+    // BACK: rotated by the negative angle
+    template <bool BACK = false>
+    PP_DEVINL void rotate(F2 (&f)[UPL][2][V2], const Factors& w) const {
 #pragma unroll
         for (int k = 0; k < UPL; k++) {
             if (HALF) {
                 if (!turn_a[k]) continue;
 #pragma unroll
-                for (int i = 0; i < V; i++) {
-                    const float a = f[k][0][i], b = f[k][1][i];
-                    f[k][0][i] = a * c[k][i].x - b * c[k][i].y;
-                    f[k][1][i] = b * c[k][i].x + a * c[k][i].y;
+                for (int i = 0; i < V2; i++) {
+                    const F2 c = pair2(w.c[k][2 * i], w.c[k][2 * i + 1]), s = pair2(w.s[k][2 * i], w.s[k][2 * i + 1]),
+                             n = pair2(-w.s[k][2 * i], -w.s[k][2 * i + 1]);
+                    const F2 a = f[k][0][i], b = f[k][1][i];
+                    f[k][0][i] = fma2(a, c, mul2(b, BACK ? s : n));
+                    f[k][1][i] = fma2(b, c, mul2(a, BACK ? n : s));
                 }
             } else {
 #pragma unroll
-                for (int s = 0; s < 2; s++) {
-                    if (!(s ? turn_b[k] : turn_a[k])) continue;
+                for (int v = 0; v < 2; v++) {
+                    if (!(v ? turn_b[k] : turn_a[k])) continue;
 #pragma unroll
-                    for (int i = 0; i < V; i += 2) {
-                        const float2 w = c[k][(s * V + i) / 2];
-                        const float a = f[k][s][i], b = f[k][s][i + 1];
-                        f[k][s][i] = a * w.x - b * w.y;
-                        f[k][s][i + 1] = b * w.x + a * w.y;
+                    for (int i = 0; i < V2; i++) {
+                        const float c = w.c[k][v * V2 + i], s = BACK ? -w.s[k][v * V2 + i] : w.s[k][v * V2 + i];
+                        float a, b;
+                        unpair2(f[k][v][i], a, b);
+                        f[k][v][i] = fma2(f[k][v][i], pair2(c, c), mul2(pair2(b, a), pair2(-s, s)));
                     }
                 }
             }
         }
     }
-    PP_DEVINL static void scale_by(float (&f)[UPL][2][V], float r, const float (&g)[UPL][2][V]) {
+    PP_DEVINL static void scale_by(F2 (&f)[UPL][2][V2], float r, const F2 (&g)[UPL][2][V2]) {
+        const F2 r2 = pair2(r, r);
 #pragma unroll
         for (int k = 0; k < UPL; k++)
 #pragma unroll
             for (int s = 0; s < 2; s++)
 #pragma unroll
-                for (int i = 0; i < V; i++) f[k][s][i] = f[k][s][i] * r * g[k][s][i];
+                for (int i = 0; i < V2; i++) f[k][s][i] = mul2(mul2(f[k][s][i], r2), g[k][s][i]);
     }
 };
 
 // 1 / root mean square of a row whose squares sum to ss.
-PP_DEVINL float inverse_rms(float ss, const HeadArgs& h) { return 1.0f / sqrtf(ss / (float)h.head_dim + h.eps); }
+// (rsqrtf is good to 2 ulp; 1 / D is rounded on the host.)
+PP_DEVINL float inverse_rms(float ss, const HeadArgs& h) { return rsqrtf(fmaf(ss, h.inv_dim, h.eps)); }
 
 }  // namespace pp

@@ -32,8 +32,8 @@ def _pair_sum(x, n, layout):
 
 def forward_bound(x, gamma, eps, freq, layout, scale, dtype, want):
     """Largest |error| of a correct kernel.  The sum of squares: a lane adds up to 16 products, the group 5 partial
-    sums: 21 roundings, half of them felt in the root; quotient, sum, root and reciprocal: 4; two products: 2; together
-    17 * 2^-24 < 1.1e-6 of the normed value w.  The rotation: 1e-6 of |a| + |b| (attn_ref) and w's own error, which
+    sums: 21 roundings, times 1 / D (rounded) plus eps: 2, half of these felt in the root; a reciprocal root good to 2
+    ulp: 4; two products: 2; together 17.5 * 2^-24 < 1.1e-6 of the normed value w.  The rotation: 1e-6 of |a| + |b| (attn_ref) and w's own error, which
     1.1e-6 (|a| + |b|) covers.  Then one rounding to the type."""
     w = forward(x, gamma, eps, None, None, layout, 1.0)
     tol = 1.1e-6 * np.abs(w)
@@ -46,8 +46,8 @@ def forward_bound(x, gamma, eps, freq, layout, scale, dtype, want):
 
 def backward_bound(x, gamma, eps, freq, layout, scale, dy, dtype, dx, per_thread):
     """Bounds of (dx, dgamma).  g is off by 1e-6 of its pair's |a| + |b| (e_g).  S = sum u x over the row: its terms'
-    errors and 21 roundings of the absolute sum (e_s).  dx = r (u - x r^2 S / D): the terms' errors, r's 11 * 2^-24
-    (three times in the second) and 6 roundings: 5e-6 of both terms covers these.  dgamma: each term g x r is off by
+    errors and 21 roundings of the absolute sum (e_s).  dx = r (u - x r^2 S / D): the terms' errors, r's 15.5 *
+    2^-24 (three times in the second) and 6 roundings: 5e-6 of both terms covers these.  dgamma: each term g x r is off by
     e_g |x| r + 1e-6 |g x r|; sums of at most per_thread terms in a thread, then 64 groups, 20 parts and 32 rows of parts,
     as many roundings of the absolute sum."""
     x, dy = np.asarray(x, np.float64), np.asarray(dy, np.float64)
