@@ -516,14 +516,37 @@ __global__ void __launch_bounds__(256) read8_kernel(const Read8Args a, const int
 }
 
 // ------------------------------------------------------------------- commit
-// One CTA for each (sequence, layer); a warp takes one head's keys or values
-// and moves their accepted entries a destination block at a time: first their
-// largest magnitude, and with it the block's scale, then the codes, kBatch rows
-// of a lane read before they are written.  In place and without a barrier
-// between warps: path[j] >= j, so what is read lies at or past what is written,
-// and rows of one batch are read by the whole warp before any is written.
+// One CTA for a few layers of a sequence: the path is looked up once, then a
+// warp takes one layer's and head's keys or values at a time, two of them side
+// by side, and moves their accepted entries a destination block at a time: first
+// their largest magnitude, and with it the block's scale, then the codes.  Rows
+// are read once where a warp holds a block's (16 rows of 128), else twice.  In
+// place and without a barrier between warps: path[j] >= j, so what is read lies
+// at or past what is written, and rows of one batch are read by the whole warp
+// before any is written.
 constexpr int kMoveBatch = 4;
 constexpr int kMoveChunk = 128;  // entries of a destination block at most
+
+// 16 codes: their part in a largest magnitude, and rounded again.
+PP_DEVINL float largest_of(const uint4& w, float scale, float amax) {
+    const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const float2 v = from_codes(x[i / 2] >> (i % 2 * 16) & 0xffffu);
+        amax = max3(amax, magnitude(v.x * scale), magnitude(v.y * scale));
+    }
+    return amax;
+}
+PP_DEVINL uint4 recode(const uint4& w, float ratio) {
+    const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+    uint32_t y[4] = {};
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const float2 v = from_codes(x[i / 2] >> (i % 2 * 16) & 0xffffu);
+        y[i / 2] |= to_codes(v.x * ratio, v.y * ratio) << (i % 2 * 16);
+    }
+    return make_uint4(y[0], y[1], y[2], y[3]);
+}
 
 __global__ void __launch_bounds__(512) commit8_kernel(const Commit8Args a8) {
     const CommitArgs& a = a8.c;
@@ -531,9 +554,12 @@ __global__ void __launch_bounds__(512) commit8_kernel(const Commit8Args a8) {
     __shared__ int bad_s, inplace_s;
     pdl_launch_dependents();
     pdl_wait();
-    const int b = blockIdx.x % a.batch.n_seqs, layer = blockIdx.x / a.batch.n_seqs;
+    const int b = blockIdx.x % a.batch.n_seqs, layer0 = blockIdx.x / a.batch.n_seqs * a8.layers;
+    const int layers = min(a8.layers, a.n_layers - layer0);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = (int)blockDim.x >> 5;
     const int32_t* path = a.path + (size_t)b * a.max_path;
+    // the first path entries are asked for together with the lengths, not behind them
+    const int first = tid < a.max_path ? path[tid] : 0, before = tid > 0 && tid < a.max_path ? path[tid - 1] : -1;
     const Seq s = load_seq(a.batch, b);
     const int acc = a.n_accept[b];
     if (tid == 0) bad_s = s.bad || acc < 0 || acc > a.max_path || acc > s.n;
@@ -541,14 +567,14 @@ __global__ void __launch_bounds__(512) commit8_kernel(const Commit8Args a8) {
     if (!bad_s) {
         bool bad = false;
         for (int j = tid; j < acc && !bad; j += blockDim.x) {
-            const int p = path[j], before = j > 0 ? path[j - 1] : -1;
-            bad = p < 0 || p >= s.n || p <= before || entry_page(a.batch, b, s.ctx + p) < 0 || entry_page(a.batch, b, s.ctx + j) < 0;
+            const int p = j == tid ? first : path[j], prev = j == tid ? before : path[j - 1];
+            bad = p < 0 || p >= s.n || p <= prev || entry_page(a.batch, b, s.ctx + p) < 0 || entry_page(a.batch, b, s.ctx + j) < 0;
         }
         if (bad) bad_s = 1;
     }
     __syncthreads();
     const bool bad = bad_s != 0;
-    if (layer == 0 && tid == 0) {
+    if (layer0 == 0 && tid == 0) {
         if (bad) record_status(a.status, PP_ERR_INVALID_ARG);
         if (a.new_len) a.new_len[b] = bad ? s.ctx : s.ctx + acc;
     }
@@ -556,15 +582,16 @@ __global__ void __launch_bounds__(512) commit8_kernel(const Commit8Args a8) {
     const int D = a.head_bytes, shift = a8.scales.shift, block = 1 << shift;
     int group = 1;  // lanes of a row, 16 codes each
     while (group * 16 < D) group *= 2;
-    const int per = 32 / group, col = lane % group * 16;
+    const int per = 32 / group, col = lane % group * 16, row = lane / group;
     const bool on = col < D;
+    const int units = layers * 2 * a.n_kv_heads;
     for (int j0 = 0; j0 < acc;) {
         const int lo = (s.ctx + j0) >> shift << shift, j1 = min(acc, lo + block - s.ctx), n = j1 - j0;
         __syncthreads();  // the last block's readers are done
         if (tid == 0) inplace_s = 0;
         __syncthreads();
         for (int i = tid; i < n; i += blockDim.x) {
-            const int p = path[j0 + i], e = s.ctx + p, page = entry_page(a.batch, b, e);
+            const int p = j0 + i == tid ? first : path[j0 + i], e = s.ctx + p, page = entry_page(a.batch, b, e);
             src_s[i] = p == j0 + i ? -1 : entry_offset(a.batch, a.cache, page, e);
             scale_s[i] = scale_index(a.batch, a8.scales, a.n_kv_heads, page, 0, e);
             if (p == j0 + i) inplace_s = 1;
@@ -572,81 +599,71 @@ __global__ void __launch_bounds__(512) commit8_kernel(const Commit8Args a8) {
         __syncthreads();
         const int page = entry_page(a.batch, b, lo);
         const long long dst0 = entry_offset(a.batch, a.cache, page, lo), to = scale_index(a.batch, a8.scales, a.n_kv_heads, page, 0, lo);
-        const bool stays = lo < s.ctx || inplace_s;
-        for (int u = warp; u < 2 * a.n_kv_heads; u += warps) {
-            const bool key = u < a.n_kv_heads;
-            const int head = key ? u : u - a.n_kv_heads;
-            char* codes = (key ? a.cache.k : a.cache.v) + (long long)layer * a.layer_stride + (long long)head * a.cache.head_stride + col;
-            float* scales = (key ? a8.scales.k : a8.scales.v) + (long long)layer * a8.scale_layer_stride + (long long)head * a8.scales.blocks;
-            const float old = stays ? scales[to] : 0.f;
-            float amax = 0.f;
-            for (int i0 = lane / group; i0 < n; i0 += kMoveBatch * per) {
-                uint4 w[kMoveBatch] = {};
-                float sc[kMoveBatch] = {};
+        const bool stays = lo < s.ctx || inplace_s, once = n <= kMoveBatch * per;
+        for (int u0 = warp; u0 < units; u0 += 2 * warps) {
+            char* codes[2];
+            float* scales[2];
+            float old[2], amax[2] = {0.f, 0.f};
+            uint4 w[2][kMoveBatch];
+            float sc[2][kMoveBatch];
+            bool have[2];
+            auto fetch = [&](int k, int i0) {
 #pragma unroll
-                for (int k = 0; k < kMoveBatch; k++) {
-                    const int i = i0 + k * per;
-                    if (i >= n || src_s[i] < 0 || !on) continue;
-                    w[k] = *reinterpret_cast<const uint4*>(codes + src_s[i]);
-                    sc[k] = scales[scale_s[i]];
+                for (int x = 0; x < kMoveBatch; x++) {
+                    const int i = i0 + x * per;
+                    w[k][x] = make_uint4(0u, 0u, 0u, 0u);
+                    sc[k][x] = 0.f;
+                    if (!have[k] || i >= n || src_s[i] < 0 || !on) continue;
+                    w[k][x] = *reinterpret_cast<const uint4*>(codes[k] + src_s[i]);
+                    sc[k][x] = scales[k][scale_s[i]];
                 }
+            };
 #pragma unroll
-                for (int k = 0; k < kMoveBatch; k++) {
-                    const uint32_t x[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
-#pragma unroll
-                    for (int i = 0; i < 8; i++) {
-                        const float2 v = from_codes(x[i / 2] >> (i % 2 * 16) & 0xffffu);
-                        amax = fmaxf(amax, fmaxf(magnitude(v.x * sc[k]), magnitude(v.y * sc[k])));
-                    }
-                }
+            for (int k = 0; k < 2; k++) {
+                const int u = u0 + k * warps, layer = u / (2 * a.n_kv_heads), v = u - layer * 2 * a.n_kv_heads;
+                have[k] = u < units;
+                const bool key = v < a.n_kv_heads;
+                const int head = key ? v : v - a.n_kv_heads;
+                codes[k] = (key ? a.cache.k : a.cache.v) + (long long)(layer0 + layer) * a.layer_stride +
+                           (long long)head * a.cache.head_stride + col;
+                scales[k] = (key ? a8.scales.k : a8.scales.v) + (long long)(layer0 + layer) * a8.scale_layer_stride +
+                            (long long)head * a8.scales.blocks;
+                old[k] = have[k] && stays ? scales[k][to] : 0.f;
+                if (once) fetch(k, row);
             }
-            amax = warp_max(amax);
-            const float now = block_scale(amax, old, stays);
-            if (stays && now != old && on) {
-                // entries that stay: cached ones, and accepted ones in their place
-                for (int e = max(lo, 0) + lane / group; e < s.ctx + j1; e += per) {
-                    if (e >= s.ctx && (e < s.ctx + j0 || src_s[e - s.ctx - j0] >= 0)) continue;
-                    uint4* p = reinterpret_cast<uint4*>(codes + dst0 + (e - lo) * a.cache.token_stride);
-                    const uint4 w = *p;
-                    const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-                    uint32_t y[4] = {};
 #pragma unroll
-                    for (int i = 0; i < 8; i++) {
-                        const float2 v = from_codes(x[i / 2] >> (i % 2 * 16) & 0xffffu);
-                        y[i / 2] |= to_codes(v.x * (old / now), v.y * (old / now)) << (i % 2 * 16);
+            for (int k = 0; k < 2; k++) {
+                if (!have[k]) continue;
+                for (int i0 = row; i0 - row < n; i0 += kMoveBatch * per) {
+                    if (!once) fetch(k, i0);
+#pragma unroll
+                    for (int x = 0; x < kMoveBatch; x++) amax[k] = largest_of(w[k][x], sc[k][x], amax[k]);
+                }
+                amax[k] = warp_max(amax[k]);
+                const float now = block_scale(amax[k], old[k], stays);
+                if (stays && now != old[k] && on) {
+                    // entries that stay: cached ones, and accepted ones in their place
+                    for (int e = lo + row; e < s.ctx + j1; e += per) {
+                        if (e >= s.ctx && (e < s.ctx + j0 || src_s[e - s.ctx - j0] >= 0)) continue;
+                        uint4* p = reinterpret_cast<uint4*>(codes[k] + dst0 + (e - lo) * a.cache.token_stride);
+                        *p = recode(*p, old[k] / now);
                     }
-                    *p = make_uint4(y[0], y[1], y[2], y[3]);
                 }
-            }
-            for (int i0 = lane / group; i0 - lane / group < n; i0 += kMoveBatch * per) {
-                uint4 w[kMoveBatch] = {};
-                float sc[kMoveBatch] = {};
+                for (int i0 = row; i0 - row < n; i0 += kMoveBatch * per) {
+                    if (!once) fetch(k, i0);
+                    __syncwarp();
 #pragma unroll
-                for (int k = 0; k < kMoveBatch; k++) {
-                    const int i = i0 + k * per;
-                    if (i >= n || src_s[i] < 0 || !on) continue;
-                    w[k] = *reinterpret_cast<const uint4*>(codes + src_s[i]);
-                    sc[k] = scales[scale_s[i]];
-                }
-                __syncwarp();
-#pragma unroll
-                for (int k = 0; k < kMoveBatch; k++) {
-                    const int i = i0 + k * per;
-                    if (i >= n || src_s[i] < 0 || !on) continue;
-                    const float ratio = sc[k] / now;
-                    const uint32_t x[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
-                    uint32_t y[4] = {};
-#pragma unroll
-                    for (int c = 0; c < 8; c++) {
-                        const float2 v = from_codes(x[c / 2] >> (c % 2 * 16) & 0xffffu);
-                        y[c / 2] |= to_codes(v.x * ratio, v.y * ratio) << (c % 2 * 16);
+                    for (int x = 0; x < kMoveBatch; x++) {
+                        const int i = i0 + x * per;
+                        if (i >= n || src_s[i] < 0 || !on) continue;
+                        *reinterpret_cast<uint4*>(codes[k] + dst0 + (s.ctx + j0 + i - lo) * a.cache.token_stride) =
+                            recode(w[k][x], sc[k][x] / now);
                     }
-                    *reinterpret_cast<uint4*>(codes + dst0 + (s.ctx + j0 + i - lo) * a.cache.token_stride) = make_uint4(y[0], y[1], y[2], y[3]);
+                    __syncwarp();
                 }
+                if (lane == 0 && now != old[k]) scales[k][to] = now;
                 __syncwarp();
             }
-            if (lane == 0 && now != old) scales[to] = now;
-            __syncwarp();
         }
         j0 = j1;
     }
@@ -670,9 +687,12 @@ cudaError_t read8_launch(const Read8Args& a, int dtype, cudaStream_t st) {
     return launch_overlapped(kern, dim3((unsigned)ctas, (unsigned)split), dim3(256), 0, st, a, share);
 }
 
-cudaError_t commit8_launch(const Commit8Args& a, cudaStream_t st) {
-    const long long ctas = (long long)a.c.batch.n_seqs * a.c.n_layers;
-    const int warps = std::min(16, std::max(2, 2 * a.c.n_kv_heads));
+cudaError_t commit8_launch(Commit8Args a, cudaStream_t st) {
+    // layers of a CTA: about two CTAs an SM in all
+    const long long all = (long long)a.c.batch.n_seqs * a.c.n_layers;
+    a.layers = (int)std::min<long long>(a.c.n_layers, std::max<long long>(1, all / 304));
+    const long long ctas = (long long)a.c.batch.n_seqs * ((a.c.n_layers + a.layers - 1) / a.layers);
+    const int warps = std::min(16, std::max(2, a.layers * a.c.n_kv_heads));
     return launch_overlapped(commit8_kernel, dim3((unsigned)ctas), dim3((unsigned)(warps * 32)), 0, st, a);
 }
 

@@ -70,12 +70,19 @@ __global__ void __launch_bounds__(256) norm_kernel(const NormArgs a) {
 // steps of as many rows as the CTA has groups (a few tokens' rows, or part of
 // one's), every ctas-th step.  A thread copies what it will use of the next
 // kStages - 1 steps into shared memory by cp.async, for itself alone, so that
-// enough is on its way without registers; the factors of the next step's tokens
-// are computed behind the present one.  It adds its columns' part of dgamma up
+// enough is on its way without registers.  The factors of the next few steps'
+// tokens, one a thread where that many fit, are computed behind the present
+// ones, with one barrier for all (a step at a time left six of eight warps
+// waiting for two: 81 us).  It adds its columns' part of dgamma up
 // over all its rows, and the CTA leaves one row of sums, so that the result does
 // not depend on the order in which CTAs run.
 constexpr int kStages = 4;
 constexpr int kGradSmem = 200 * 1024;  // 64 KB of stages, and up to 64 tokens' factors twice
+
+// Steps whose factors are computed together, from those of a step.
+__host__ __device__ inline int factor_batch(int per_step) {
+    return per_step == 0 || per_step >= 256 ? 1 : 256 / per_step < 4 ? 256 / per_step : 4;
+}
 
 template <typename T, int V, bool HALF, int UPL>
 __global__ void __launch_bounds__(256) norm_grad_kernel(const NormArgs a) {
@@ -101,7 +108,8 @@ __global__ void __launch_bounds__(256) norm_grad_kernel(const NormArgs a) {
     const int steps = (a.n_tokens + tokens - 1) / tokens * chunks;
     const int pitch = (pairs + V - 1) / V, table = V * pitch;  // factors of a token
     unsigned char* mine = smem + tid * kBytes;                 // vector v of stage s at ((s * kVecs + v) * 256 + tid)
-    float* cs = reinterpret_cast<float*>(smem + kStages * kVecs * 256 * kBytes);  // two steps' tables
+    const int batch = factor_batch(tokens * pairs);            // steps between barriers
+    float* cs = reinterpret_cast<float*>(smem + kStages * kVecs * 256 * kBytes);  // two batches' tables
     // token and row of this thread in step s; false: none
     auto place = [&](int s, int& t, int& r) {
         const int c = chunks == 1 ? 0 : s % chunks;
@@ -129,27 +137,30 @@ __global__ void __launch_bounds__(256) norm_grad_kernel(const NormArgs a) {
         }
         cp_async_commit();
     };
-    // factor i of a step's table: token i / pairs of the step
+    // factor i of the batch that begins with step s: its position, and its place in the tables
+    const int per_step = tokens * pairs, entries = batch * per_step;
     auto position = [&](int s, int i) {
-        const int t = (chunks == 1 ? s : s / chunks) * tokens + i / pairs;
-        return s < steps && i < tokens * pairs && t < a.n_tokens ? h.positions[t] : 0;
+        const int j = s + i / per_step * ctas, t = (chunks == 1 ? j : j / chunks) * tokens + i % per_step / pairs;
+        return j < steps && t < a.n_tokens ? h.positions[t] : 0;
     };
-    auto fill = [&](int s, int buf, int i, int pos) {
-        const int n = i / pairs, p = i - n * pairs;
+    auto fill = [&](int buf, int i, int pos) {
+        const int n = i / pairs, p = i - n * pairs;  // token of the batch
         const float2 v = cos_sin(pos, h.inv_freq[p]);
-        put_pair(cs + (buf * tokens + n) * table * 2, p, V, pitch, make_float2(v.x * h.scale, v.y * h.scale));
+        put_pair(cs + (buf * batch * tokens + n) * table * 2, p, V, pitch, make_float2(v.x * h.scale, v.y * h.scale));
     };
     F2 gamma[UPL][2][V / 2], acc[UPL][2][V / 2] = {};
     lane.weights(key ? a.k_gamma : a.q_gamma, gamma);
 #pragma unroll
     for (int i = 0; i < kStages - 1; i++) fetch(first + i * ctas, i);
-    for (int i = tid; i < tokens * pairs; i += 256) fill(first, 0, i, position(first, i));
-    int n = 0;
+    if (pairs)
+        for (int i = tid; i < entries; i += 256) fill(0, i, position(first, i));
+    int n = 0, in_batch = 0, buf = 0, pos = 0;
     for (int s = first; s < steps; s += ctas, n++) {
         fetch(s + (kStages - 1) * ctas, (n + kStages - 1) % kStages);
-        const int next = s + ctas, pos = pairs ? position(next, tid) : 0;
+        const int next = s + ctas;
+        if (in_batch == batch - 1 && pairs && tid < entries) pos = position(next, tid);
         cp_async_wait<kStages - 1>();
-        __syncthreads();  // this step's factors are there, the last step's have been read
+        if (in_batch == 0) __syncthreads();  // this batch's factors are there, the last one's have been read
         int t, r;
         const bool in = place(s, t, r);
         F2 f[UPL][2][V / 2] = {}, g[UPL][2][V / 2] = {};
@@ -167,7 +178,7 @@ __global__ void __launch_bounds__(256) norm_grad_kernel(const NormArgs a) {
             lane.widen(dy, g);
             if (pairs) {
                 typename Lane::Factors c;
-                lane.factors(cs + ((n & 1) * tokens + my_token) * table * 2, h, c);
+                lane.factors(cs + ((buf * batch + in_batch) * tokens + my_token) * table * 2, h, c);
                 lane.template rotate<true>(g, c);
             }
         }
@@ -196,9 +207,13 @@ __global__ void __launch_bounds__(256) norm_grad_kernel(const NormArgs a) {
             lane.narrow(f, x);
             lane.store(os + t * ostr + (long long)r * D * (int)sizeof(T), x);
         }
-        if (next < steps) {
-            if (tid < tokens * pairs) fill(next, (n + 1) & 1, tid, pos);
-            for (int i = tid + 256; i < tokens * pairs; i += 256) fill(next, (n + 1) & 1, i, position(next, i));
+        if (++in_batch == batch) {
+            in_batch = 0;
+            buf ^= 1;
+            if (pairs && next < steps) {
+                if (tid < entries) fill(buf, tid, pos);
+                for (int i = tid + 256; i < entries; i += 256) fill(buf, i, position(next, i));
+            }
         }
     }
     cp_async_wait<0>();
@@ -253,11 +268,14 @@ cudaError_t norm_go(NormArgs a, bool grad, cudaStream_t st) {
     constexpr int kMost = V == 2 ? 2 : 1;  // two units a lane: more than 128 elements in vectors of 2
     const bool two = units > group;
     if (grad) {
-        const int groups = 256 / group, pairs = (a.head.rot_dim / 2 + V - 1) / V * V;
-        // tables of two steps' tokens (fewer heads: more tokens a step)
-        int tokens = std::max(1, groups / a.n_heads);
-        if (a.n_kv_heads) tokens = std::max(tokens, std::max(1, groups / a.n_kv_heads));
-        const int smem = kStages * 4 * (two ? 2 : 1) * 256 * V * (int)sizeof(T) + 2 * tokens * pairs * 8;
+        // tables of two batches' tokens, for the rows of q and of k
+        const int groups = 256 / group, table = (a.head.rot_dim / 2 + V - 1) / V * V;
+        auto tables = [&](int rows) {
+            const int tokens = std::max(1, groups / std::max(1, rows));
+            return 2 * factor_batch(tokens * (a.head.rot_dim / 2)) * tokens * table * 8;
+        };
+        const int smem = kStages * 4 * (two ? 2 : 1) * 256 * V * (int)sizeof(T) +
+                         std::max(tables(a.n_heads), a.n_kv_heads ? tables(a.n_kv_heads) : 0);
         auto* kern = two ? norm_grad_kernel<T, V, HALF, kMost> : norm_grad_kernel<T, V, HALF, 1>;
         static std::atomic<bool> allowed[2][64];
         const cudaError_t e = allow_smem(kern, kGradSmem, allowed[two]);

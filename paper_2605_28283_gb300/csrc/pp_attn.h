@@ -116,6 +116,7 @@ struct Commit8Args {
     CommitArgs c;
     ScaleArgs scales;
     long long scale_layer_stride;  // floats
+    int layers;                    // of a CTA
 };
 
 struct AttnArgs {
@@ -148,7 +149,7 @@ cudaError_t commit_launch(const CommitArgs& a, cudaStream_t st);
 
 cudaError_t append8_launch(const Append8Args& a, int dtype, int layout, int block, cudaStream_t st);
 cudaError_t read8_launch(const Read8Args& a, int dtype, cudaStream_t st);
-cudaError_t commit8_launch(const Commit8Args& a, cudaStream_t st);
+cudaError_t commit8_launch(Commit8Args a, cudaStream_t st);
 
 size_t attn_part_floats(int head_dim);  // floats behind AttnArgs.part
 cudaError_t attn_simt_launch(const AttnArgs& a, int sms, cudaStream_t st);  // fp32
