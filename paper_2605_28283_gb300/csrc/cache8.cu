@@ -516,9 +516,9 @@ __global__ void __launch_bounds__(256) read8_kernel(const Read8Args a, const int
 }
 
 // ------------------------------------------------------------------- commit
-// One CTA for a few layers of a sequence: the path is looked up once, then a
-// warp takes one layer's and head's keys or values at a time, two of them side
-// by side, and moves their accepted entries a destination block at a time: first
+// A CTA takes some of a sequence's units, one layer's and head's keys or values
+// each: the path is looked up once, then a warp takes a unit at a time, two of
+// them side by side, and moves their accepted entries a destination block at a time: first
 // their largest magnitude, and with it the block's scale, then the codes.  Rows
 // are read once where a warp holds a block's (16 rows of 128), else twice.  In
 // place and without a barrier between warps: path[j] >= j, so what is read lies
@@ -527,54 +527,98 @@ __global__ void __launch_bounds__(256) read8_kernel(const Read8Args a, const int
 constexpr int kMoveBatch = 4;
 constexpr int kMoveChunk = 128;  // entries of a destination block at most
 
-// 16 codes: their part in a largest magnitude, and rounded again.
-PP_DEVINL float largest_of(const uint4& w, float scale, float amax) {
+// Largest magnitude among 16 codes times their scale: codes without their sign
+// ascend as numbers do, four of them as two pairs of 16 bits an instruction.
+PP_DEVINL float largest_of(const uint4& w, float scale) {
     const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+    uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
-        const float2 v = from_codes(x[i / 2] >> (i % 2 * 16) & 0xffffu);
-        amax = max3(amax, magnitude(v.x * scale), magnitude(v.y * scale));
+    for (int i = 0; i < 4; i++) {
+        top = __vmaxu2(top, x[i] & 0x007f007fu);
+        top = __vmaxu2(top, x[i] >> 8 & 0x007f007fu);
     }
-    return amax;
+    uint32_t m = max(top & 0xffffu, top >> 16);
+    if (m == 0x7fu) {  // NaN among them, which does not count
+        m = 0;
+#pragma unroll 1
+        for (int i = 0; i < 16; i++) {
+            const uint32_t c = x[i >> 2] >> (i & 3) * 8 & 0x7fu;
+            if (c != 0x7fu) m = max(m, c);
+        }
+    }
+    return from_codes(m).x * scale;
 }
+// 16 codes rounded again at another scale.  The usual ratio, a power of two that
+// fp16 holds, goes in fp16: code * ratio is exact there (a code has four bits,
+// the least 2^-9; results are at most 448).
 PP_DEVINL uint4 recode(const uint4& w, float ratio) {
+    if (ratio == 1.f) return w;
     const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-    uint32_t y[4] = {};
+    uint32_t y[4];
+    const bool power = (__float_as_uint(ratio) & 0x7fffffu) == 0 && ratio >= 0x1p-14f && ratio <= 0x1p15f;
+    if (power) {
+        const __half2 r = __float2half2_rn(ratio);
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
-        const float2 v = from_codes(x[i / 2] >> (i % 2 * 16) & 0xffffu);
-        y[i / 2] |= to_codes(v.x * ratio, v.y * ratio) << (i % 2 * 16);
+        for (int i = 0; i < 4; i++) {
+            uint32_t out = 0;
+#pragma unroll
+            for (int k = 0; k < 2; k++) {
+                uint32_t h;
+                asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)(x[i] >> 16 * k)));
+                const __half2 v = __hmul2(*reinterpret_cast<const __half2*>(&h), r);
+                uint16_t c;
+                asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(c) : "r"(*reinterpret_cast<const uint32_t*>(&v)));
+                out |= (uint32_t)c << 16 * k;
+            }
+            y[i] = out;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const float2 a = from_codes(x[i] & 0xffffu), b = from_codes(x[i] >> 16);
+            y[i] = to_codes(a.x * ratio, a.y * ratio) | to_codes(b.x * ratio, b.y * ratio) << 16;
+        }
     }
     return make_uint4(y[0], y[1], y[2], y[3]);
 }
 
-__global__ void __launch_bounds__(512) commit8_kernel(const Commit8Args a8) {
+__global__ void __launch_bounds__(256, 3) commit8_kernel(const Commit8Args a8) {
     const CommitArgs& a = a8.c;
-    __shared__ long long src_s[kMoveChunk], scale_s[kMoveChunk];  // of an accepted entry; code -1: in its place already
-    __shared__ int bad_s, inplace_s;
+    // of a window of accepted entries: code (-1: in its place already) and scale of the source, page of the destination
+    __shared__ long long src_s[kMoveChunk], scale_s[kMoveChunk];
+    __shared__ int page_s[kMoveChunk], bad_s;
     pdl_launch_dependents();
     pdl_wait();
-    const int b = blockIdx.x % a.batch.n_seqs, layer0 = blockIdx.x / a.batch.n_seqs * a8.layers;
-    const int layers = min(a8.layers, a.n_layers - layer0);
+    const int b = blockIdx.x % a.batch.n_seqs, part = blockIdx.x / a.batch.n_seqs;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = (int)blockDim.x >> 5;
     const int32_t* path = a.path + (size_t)b * a.max_path;
     // the first path entries are asked for together with the lengths, not behind them
     const int first = tid < a.max_path ? path[tid] : 0, before = tid > 0 && tid < a.max_path ? path[tid - 1] : -1;
     const Seq s = load_seq(a.batch, b);
     const int acc = a.n_accept[b];
+    auto look_up = [&](int j, int p, int w0) {  // accepted entry j, p in the tree; false: no such page
+        const int from = entry_page(a.batch, b, s.ctx + p), to = entry_page(a.batch, b, s.ctx + j), i = j - w0;
+        if (from < 0 || to < 0) return false;
+        if (i < kMoveChunk) {
+            src_s[i] = p == j ? -1 : entry_offset(a.batch, a.cache, from, s.ctx + p);
+            scale_s[i] = scale_index(a.batch, a8.scales, a.n_kv_heads, from, 0, s.ctx + p);
+            page_s[i] = to;
+        }
+        return true;
+    };
     if (tid == 0) bad_s = s.bad || acc < 0 || acc > a.max_path || acc > s.n;
     __syncthreads();
     if (!bad_s) {
         bool bad = false;
         for (int j = tid; j < acc && !bad; j += blockDim.x) {
             const int p = j == tid ? first : path[j], prev = j == tid ? before : path[j - 1];
-            bad = p < 0 || p >= s.n || p <= prev || entry_page(a.batch, b, s.ctx + p) < 0 || entry_page(a.batch, b, s.ctx + j) < 0;
+            bad = p < 0 || p >= s.n || p <= prev || !look_up(j, p, 0);
         }
         if (bad) bad_s = 1;
     }
     __syncthreads();
     const bool bad = bad_s != 0;
-    if (layer0 == 0 && tid == 0) {
+    if (part == 0 && tid == 0) {
         if (bad) record_status(a.status, PP_ERR_INVALID_ARG);
         if (a.new_len) a.new_len[b] = bad ? s.ctx : s.ctx + acc;
     }
@@ -584,88 +628,96 @@ __global__ void __launch_bounds__(512) commit8_kernel(const Commit8Args a8) {
     while (group * 16 < D) group *= 2;
     const int per = 32 / group, col = lane % group * 16, row = lane / group;
     const bool on = col < D;
-    const int units = layers * 2 * a.n_kv_heads;
-    for (int j0 = 0; j0 < acc;) {
-        const int lo = (s.ctx + j0) >> shift << shift, j1 = min(acc, lo + block - s.ctx), n = j1 - j0;
-        __syncthreads();  // the last block's readers are done
-        if (tid == 0) inplace_s = 0;
-        __syncthreads();
-        for (int i = tid; i < n; i += blockDim.x) {
-            const int p = j0 + i == tid ? first : path[j0 + i], e = s.ctx + p, page = entry_page(a.batch, b, e);
-            src_s[i] = p == j0 + i ? -1 : entry_offset(a.batch, a.cache, page, e);
-            scale_s[i] = scale_index(a.batch, a8.scales, a.n_kv_heads, page, 0, e);
-            if (p == j0 + i) inplace_s = 1;
+    // one layer's and head's keys or values each
+    const int units = a.n_layers * 2 * a.n_kv_heads, u_end = min(units, (part + 1) * a8.units);
+    for (int w0 = 0, w1; w0 < acc; w0 = w1) {
+        w1 = min(acc, w0 + kMoveChunk);
+        if (w1 < acc) w1 = ((s.ctx + w1) >> shift << shift) - s.ctx;  // whole blocks
+        if (w0 > 0) {
+            __syncthreads();  // the last window's readers are done
+            for (int j = w0 + tid; j < w1; j += blockDim.x) look_up(j, path[j], w0);
+            __syncthreads();
         }
-        __syncthreads();
-        const int page = entry_page(a.batch, b, lo);
-        const long long dst0 = entry_offset(a.batch, a.cache, page, lo), to = scale_index(a.batch, a8.scales, a.n_kv_heads, page, 0, lo);
-        const bool stays = lo < s.ctx || inplace_s, once = n <= kMoveBatch * per;
-        for (int u0 = warp; u0 < units; u0 += 2 * warps) {
+        for (int u0 = part * a8.units + warp; u0 < u_end; u0 += 2 * warps) {
             char* codes[2];
             float* scales[2];
-            float old[2], amax[2] = {0.f, 0.f};
-            uint4 w[2][kMoveBatch];
-            float sc[2][kMoveBatch];
             bool have[2];
-            auto fetch = [&](int k, int i0) {
-#pragma unroll
-                for (int x = 0; x < kMoveBatch; x++) {
-                    const int i = i0 + x * per;
-                    w[k][x] = make_uint4(0u, 0u, 0u, 0u);
-                    sc[k][x] = 0.f;
-                    if (!have[k] || i >= n || src_s[i] < 0 || !on) continue;
-                    w[k][x] = *reinterpret_cast<const uint4*>(codes[k] + src_s[i]);
-                    sc[k][x] = scales[k][scale_s[i]];
-                }
-            };
 #pragma unroll
             for (int k = 0; k < 2; k++) {
                 const int u = u0 + k * warps, layer = u / (2 * a.n_kv_heads), v = u - layer * 2 * a.n_kv_heads;
-                have[k] = u < units;
+                have[k] = u < u_end;
                 const bool key = v < a.n_kv_heads;
                 const int head = key ? v : v - a.n_kv_heads;
-                codes[k] = (key ? a.cache.k : a.cache.v) + (long long)(layer0 + layer) * a.layer_stride +
-                           (long long)head * a.cache.head_stride + col;
-                scales[k] = (key ? a8.scales.k : a8.scales.v) + (long long)(layer0 + layer) * a8.scale_layer_stride +
-                            (long long)head * a8.scales.blocks;
-                old[k] = have[k] && stays ? scales[k][to] : 0.f;
-                if (once) fetch(k, row);
+                codes[k] = (key ? a.cache.k : a.cache.v) + (long long)layer * a.layer_stride + (long long)head * a.cache.head_stride + col;
+                scales[k] = (key ? a8.scales.k : a8.scales.v) + (long long)layer * a8.scale_layer_stride + (long long)head * a8.scales.blocks;
             }
-#pragma unroll
-            for (int k = 0; k < 2; k++) {
-                if (!have[k]) continue;
-                for (int i0 = row; i0 - row < n; i0 += kMoveBatch * per) {
-                    if (!once) fetch(k, i0);
-#pragma unroll
-                    for (int x = 0; x < kMoveBatch; x++) amax[k] = largest_of(w[k][x], sc[k][x], amax[k]);
-                }
-                amax[k] = warp_max(amax[k]);
-                const float now = block_scale(amax[k], old[k], stays);
-                if (stays && now != old[k] && on) {
-                    // entries that stay: cached ones, and accepted ones in their place
-                    for (int e = lo + row; e < s.ctx + j1; e += per) {
-                        if (e >= s.ctx && (e < s.ctx + j0 || src_s[e - s.ctx - j0] >= 0)) continue;
-                        uint4* p = reinterpret_cast<uint4*>(codes[k] + dst0 + (e - lo) * a.cache.token_stride);
-                        *p = recode(*p, old[k] / now);
-                    }
-                }
-                for (int i0 = row; i0 - row < n; i0 += kMoveBatch * per) {
-                    if (!once) fetch(k, i0);
-                    __syncwarp();
+            for (int j0 = w0, j1; j0 < w1; j0 = j1) {
+                const int lo = (s.ctx + j0) >> shift << shift, n = min(w1, lo + block - s.ctx) - j0;
+                j1 = j0 + n;
+                const long long* src = src_s + (j0 - w0);
+                const long long* from = scale_s + (j0 - w0);
+                const int page = page_s[j0 - w0];
+                const long long dst0 = entry_offset(a.batch, a.cache, page, lo),
+                                to = scale_index(a.batch, a8.scales, a.n_kv_heads, page, 0, lo);
+                bool stays = lo < s.ctx;
+                for (int i = lane; i < n; i += 32) stays |= src[i] < 0;
+                stays = __any_sync(kFull, stays);
+                const bool once = n <= kMoveBatch * per;
+                float old[2], amax[2] = {0.f, 0.f};
+                uint4 w[2][kMoveBatch];
+                float sc[2][kMoveBatch];
+                auto fetch = [&](int k, int i0) {
 #pragma unroll
                     for (int x = 0; x < kMoveBatch; x++) {
                         const int i = i0 + x * per;
-                        if (i >= n || src_s[i] < 0 || !on) continue;
-                        *reinterpret_cast<uint4*>(codes[k] + dst0 + (s.ctx + j0 + i - lo) * a.cache.token_stride) =
-                            recode(w[k][x], sc[k][x] / now);
+                        w[k][x] = make_uint4(0u, 0u, 0u, 0u);
+                        sc[k][x] = 0.f;
+                        if (!have[k] || i >= n || src[i] < 0 || !on) continue;
+                        w[k][x] = *reinterpret_cast<const uint4*>(codes[k] + src[i]);
+                        sc[k][x] = scales[k][from[i]];
                     }
+                };
+#pragma unroll
+                for (int k = 0; k < 2; k++) {
+                    old[k] = have[k] && stays ? scales[k][to] : 0.f;
+                    if (once) fetch(k, row);
+                }
+#pragma unroll
+                for (int k = 0; k < 2; k++) {
+                    if (!have[k]) continue;
+                    for (int i0 = row; i0 - row < n; i0 += kMoveBatch * per) {
+                        if (!once) fetch(k, i0);
+#pragma unroll
+                        for (int x = 0; x < kMoveBatch; x++)
+                            if (i0 - row + x * per < n) amax[k] = fmaxf(amax[k], largest_of(w[k][x], sc[k][x]));
+                    }
+                    amax[k] = warp_max(amax[k]);
+                    const float now = block_scale(amax[k], old[k], stays), inv = 1.f / now;
+                    if (stays && now != old[k] && on) {
+                        // entries that stay: cached ones, and accepted ones in their place
+                        for (int e = lo + row; e < s.ctx + j1; e += per) {
+                            if (e >= s.ctx && (e < s.ctx + j0 || src[e - s.ctx - j0] >= 0)) continue;
+                            uint4* p = reinterpret_cast<uint4*>(codes[k] + dst0 + (e - lo) * a.cache.token_stride);
+                            *p = recode(*p, old[k] * inv);
+                        }
+                    }
+                    for (int i0 = row; i0 - row < n; i0 += kMoveBatch * per) {
+                        if (!once) fetch(k, i0);
+                        __syncwarp();
+#pragma unroll
+                        for (int x = 0; x < kMoveBatch; x++) {
+                            const int i = i0 + x * per;
+                            if (i >= n || src[i] < 0 || !on) continue;
+                            *reinterpret_cast<uint4*>(codes[k] + dst0 + (s.ctx + j0 + i - lo) * a.cache.token_stride) =
+                                recode(w[k][x], sc[k][x] * inv);
+                        }
+                        __syncwarp();
+                    }
+                    if (lane == 0 && now != old[k]) scales[k][to] = now;
                     __syncwarp();
                 }
-                if (lane == 0 && now != old[k]) scales[k][to] = now;
-                __syncwarp();
             }
         }
-        j0 = j1;
     }
 }
 
@@ -688,11 +740,12 @@ cudaError_t read8_launch(const Read8Args& a, int dtype, cudaStream_t st) {
 }
 
 cudaError_t commit8_launch(Commit8Args a, cudaStream_t st) {
-    // layers of a CTA: about two CTAs an SM in all
-    const long long all = (long long)a.c.batch.n_seqs * a.c.n_layers;
-    a.layers = (int)std::min<long long>(a.c.n_layers, std::max<long long>(1, all / 304));
-    const long long ctas = (long long)a.c.batch.n_seqs * ((a.c.n_layers + a.layers - 1) / a.layers);
-    const int warps = std::min(16, std::max(2, a.layers * a.c.n_kv_heads));
+    // a unit a warp where that makes few CTAs, else about three CTAs an SM in all
+    const long long units = (long long)a.c.n_layers * 2 * a.c.n_kv_heads;
+    const int warps = (int)std::min<long long>(8, units);
+    const long long most = (units + warps - 1) / warps, parts = std::max<long long>(1, std::min<long long>(most, 456 / a.c.batch.n_seqs));
+    a.units = (int)((units + parts - 1) / parts);
+    const long long ctas = (long long)a.c.batch.n_seqs * ((units + a.units - 1) / a.units);
     return launch_overlapped(commit8_kernel, dim3((unsigned)ctas), dim3((unsigned)(warps * 32)), 0, st, a);
 }
 

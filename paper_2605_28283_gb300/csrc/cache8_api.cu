@@ -204,7 +204,7 @@ pp_status pp_kvq_commit(const pp_cache8* cache, const pp_batch* batch, int n_lay
     PP_TRY(check_written(*cache, n_layers, layer_stride, scale_layer_stride));
     PP_TRY(check_path(*batch, path, max_path, n_accept, new_len));
     const int B = batch->n_seqs;
-    if ((long long)B * n_layers > 0x7fffffffll) return PP_ERR_SHAPE;
+    if ((long long)B * n_layers > 0x7fffffffll || (long long)n_layers * 2 * cache->n_kv_heads > 0x7fffffffll) return PP_ERR_SHAPE;
     PP_TRY(check_ws8(cache, ws, ws_bytes));
     int sms = 0;
     PP_TRY(device_sms(&sms));

@@ -116,7 +116,7 @@ struct Commit8Args {
     CommitArgs c;
     ScaleArgs scales;
     long long scale_layer_stride;  // floats
-    int layers;                    // of a CTA
+    int units;                     // of a CTA: one layer's and head's keys or values each
 };
 
 struct AttnArgs {
