@@ -60,21 +60,15 @@ PP_DEVINL Slot find_slot(const BatchArgs& B, int shift, int slot, int lane, unsi
     return s;
 }
 
-// Values times inv as codes.  ODD: some may not be finite (infinities would be
-// held as 448 otherwise; NaN is the NaN code either way).
-template <int V, bool ODD = false>
+// Finite values (or NaN) times inv as codes.
+template <int V>
 PP_DEVINL void store_codes(char* p, const F2 (&f)[V / 2], float inv) {
     uint32_t w[V > 4 ? V / 4 : 1] = {};
     const F2 inv2 = pair2(inv, inv);
 #pragma unroll
     for (int i = 0; i < V; i += 2) {
         float a, b;
-        unpair2(f[i / 2], a, b);
-        if (ODD) {
-            a = to_hold(a);
-            b = to_hold(b);
-        }
-        unpair2(mul2(pair2(a, b), inv2), a, b);
+        unpair2(mul2(f[i / 2], inv2), a, b);
         w[i / 4] |= to_codes(a, b) << (i % 4 * 8);
     }
     if constexpr (V == 8)
@@ -102,7 +96,7 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 2 : 1) append8_kernel
     extern __shared__ __align__(16) float cs[];
     __shared__ Slot slot_s;
     __shared__ int pos_s[kMaxStrips], in_s[kMaxStrips];
-    __shared__ float amax_s[kMaxStrips];
+    __shared__ float amax_s[2][kMaxStrips];
     pdl_launch_dependents();
     pdl_wait();
     const HeadArgs& h = a.head;
@@ -153,7 +147,7 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 2 : 1) append8_kernel
             for (int n = 0; n < 2; n++) {
                 const int r = r0 + n * step + in_team / h.group;
                 F2 f[UPL][2][V / 2], g[UPL][2][V / 2];
-                lane.widen(x[n], f);
+                Lane::widen(x[n], f);
                 if (h.norm) {
                     const float inv = inverse_rms(Lane::group_sum(r < a.n_heads && exists ? Lane::dot(f, f) : 0.f, h.group), h);
                     lane.weights(a.q_gamma, g);
@@ -196,41 +190,46 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 2 : 1) append8_kernel
     unsigned char* stages = reinterpret_cast<unsigned char*>(cs) + a.table_bytes + tid * Lane::kBytes;
     const int stage_bytes = kVecs * (int)blockDim.x * Lane::kBytes;
     const int first = s.lo + strip * R + l32 / h.group;  // entry of the lane's first row
-    auto rows_of = [&](int u) {
+    uint32_t rows = 0;                                   // which of the lane's rows are new entries
+#pragma unroll
+    for (int n = 0; n < ITER; n++)
+        if (first + n * per >= s.e0 && first + n * per < s.e1) rows |= 1u << n;
+    const int vec_step = (int)blockDim.x * Lane::kBytes;
+    // the lane's first row of unit u (row 0 may lie ahead of the tensor: only new entries' are read)
+    auto row0_of = [&](int u, long long& step) {
         const bool key = u < a.n_kv_heads;
-        return (key ? a.k : a.v) + (long long)(key ? u : u - a.n_kv_heads) * D * (int)sizeof(T);
+        const long long stride = key ? a.k_stride : a.v_stride;
+        step = per * stride;
+        return (key ? a.k : a.v) + (long long)(s.token + first - s.e0) * stride + (long long)(key ? u : u - a.n_kv_heads) * D * (int)sizeof(T);
     };
     auto fetch = [&](int u0, int stage) {
         const int u = u0 + warp / strips;
         if (u < 2 * a.n_kv_heads) {
-            const char* src = rows_of(u);
-            const long long stride = u < a.n_kv_heads ? a.k_stride : a.v_stride;
+            long long step;
+            const char* row = row0_of(u, step);
             unsigned char* to = stages + stage * stage_bytes;
 #pragma unroll
-            for (int n = 0; n < ITER; n++) {
-                const int e = first + n * per;
-                if (e < s.e0 || e >= s.e1) continue;
-                const char* row = src + (s.token + e - s.e0) * stride;
+            for (int n = 0; n < ITER; n++, row += step)
 #pragma unroll
                 for (int k = 0; k < UPL; k++) {
-                    const int at = (n * UPL + k) * 2 * (int)blockDim.x * Lane::kBytes;
-                    if (lane.va[k] >= 0) cp_async_small<Lane::kBytes>(to + at, row + lane.va[k] * Lane::kBytes);
-                    if (lane.vb[k] >= 0) cp_async_small<Lane::kBytes>(to + at + (int)blockDim.x * Lane::kBytes, row + lane.vb[k] * Lane::kBytes);
+                    unsigned char* at = to + (n * UPL + k) * 2 * vec_step;
+                    if ((rows >> n & 1u) && lane.va[k] >= 0) cp_async_small<Lane::kBytes>(at, row + lane.va[k] * Lane::kBytes);
+                    if ((rows >> n & 1u) && lane.vb[k] >= 0) cp_async_small<Lane::kBytes>(at + vec_step, row + lane.vb[k] * Lane::kBytes);
                 }
-            }
         }
         cp_async_commit();
     };
-    int turn = 0;
+    int turn = 0, pass = 0;
+    const bool cached = s.lo < s.ctx;
+    const long long dst0 = entry_offset(a.batch, a.cache, s.page, s.lo) + (first - s.lo) * a.cache.token_stride,
+                    scale0 = scale_index(a.batch, a.scales, a.n_kv_heads, s.page, 0, s.lo);
     for (int i = 0; i + 1 < a.stages; i++) fetch((part + i * a.parts) * units, i);
     __syncthreads();
-    for (int u0 = part * units; u0 < 2 * a.n_kv_heads; u0 += units * a.parts) {
+    for (int u0 = part * units; u0 < 2 * a.n_kv_heads; u0 += units * a.parts, pass ^= 1) {
         const int u = u0 + warp / strips;
         const bool have = u < 2 * a.n_kv_heads, key = u < a.n_kv_heads;
         const int head = key ? u : u - a.n_kv_heads;
-        const long long at = scale_index(a.batch, a.scales, a.n_kv_heads, s.page, head, s.lo);
-        float* scale_p = (key ? a.scales.k : a.scales.v) + at;
-        const bool cached = s.lo < s.ctx;
+        float* scale_p = (key ? a.scales.k : a.scales.v) + scale0 + (long long)head * a.scales.blocks;
         float old = have && cached && l32 == 0 ? *scale_p : 0.f;
         F2 f[ITER][UPL][2][V / 2];
         if (a.stages) {
@@ -244,46 +243,37 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 2 : 1) append8_kernel
         }
         const unsigned char* from = stages + turn * stage_bytes;
         turn = turn + 1 >= a.stages ? 0 : turn + 1;
+        float amax = 0.f;
         if (have) {
+            long long step;
+            const char* row = row0_of(u, step);
 #pragma unroll
-            for (int n = 0; n < ITER; n++) {
-                const int e = first + n * per;
-                const bool in = e >= s.e0 && e < s.e1;
-                Vec<T, V> x[UPL][2];
-                if (a.stages) {
+            for (int n = 0; n < ITER; n++, row += step) {
+                Vec<T, V> x[UPL][2] = {};
+                if (a.stages)
+                    lane.load_own(from + n * UPL * 2 * vec_step, vec_step, rows >> n & 1u, x);
+                else if (rows >> n & 1u)  // no room beside the factors
+                    lane.load(row, x);
+                Lane::widen(x, f[n]);
+            }
+            if (key && h.norm) {
+                F2 g[UPL][2][V / 2];
+                lane.weights(a.k_gamma, g);
 #pragma unroll
-                    for (int k = 0; k < UPL; k++)
-#pragma unroll
-                        for (int v = 0; v < 2; v++)
-                            x[k][v].raw = *reinterpret_cast<const decltype(x[0][0].raw)*>(
-                                from + ((n * UPL + k) * 2 + v) * (int)blockDim.x * Lane::kBytes);
-                } else if (in) {  // no room beside the factors
-                    lane.load(rows_of(u) + (s.token + e - s.e0) * (key ? a.k_stride : a.v_stride), x);
-                }
-                lane.widen(x, f[n]);
-                if (!in) {
-#pragma unroll
-                    for (int k = 0; k < UPL; k++)
-#pragma unroll
-                        for (int i = 0; i < V / 2; i++) f[n][k][0][i] = f[n][k][1][i] = 0ull;
-                }
-                if (!key) continue;
-                if (h.norm) {
-                    F2 g[UPL][2][V / 2];
+                for (int n = 0; n < ITER; n++) {
                     const float inv = inverse_rms(Lane::group_sum(Lane::dot(f[n], f[n]), h.group), h);
-                    lane.weights(a.k_gamma, g);
-                    if (in) Lane::scale_by(f[n], inv, g);
+                    if (rows >> n & 1u) Lane::scale_by(f[n], inv, g);  // (zeros may have no root mean square)
                 }
-                if (h.rot_dim > 0 && in) {
+            }
+            if (key && h.rot_dim > 0) {
+#pragma unroll
+                for (int n = 0; n < ITER; n++) {
+                    if (!(rows >> n & 1u)) continue;
                     typename Lane::Factors c;
-                    lane.factors(cs + (e - s.lo) * row_pairs * 2, h, c);
+                    lane.factors(cs + (first + n * per - s.lo) * row_pairs * 2, h, c);
                     lane.rotate(f[n], c);
                 }
             }
-        }
-        float amax = 0.f;
-        bool odd = false;
-        if (have) {
             // 0 x summed is zero for finite values alone
             F2 zero = 0ull;
 #pragma unroll
@@ -296,13 +286,13 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 2 : 1) append8_kernel
                         for (int i = 0; i < V / 2; i++) {
                             float x, y;
                             unpair2(f[n][k][v][i], x, y);
-                            amax = max3(amax, fabsf(x), fabsf(y));
+                            amax = fmaxf(amax, fmaxf(fabsf(x), fabsf(y)));
                             zero = fma2(f[n][k][v][i], 0ull, zero);
                         }
-            float x, y;
-            unpair2(zero, x, y);
-            odd = __any_sync(kFull, x != 0.f || y != 0.f);
-            if (odd) {
+            float zx, zy;
+            unpair2(zero, zx, zy);
+            if (__any_sync(kFull, zx != 0.f || zy != 0.f)) {
+                // what is not finite does not count, and is held as NaN
                 amax = 0.f;
 #pragma unroll
                 for (int n = 0; n < ITER; n++)
@@ -312,28 +302,27 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 2 : 1) append8_kernel
                         for (int v = 0; v < 2; v++)
 #pragma unroll
                             for (int i = 0; i < V / 2; i++) {
+                                float x, y;
                                 unpair2(f[n][k][v][i], x, y);
-                                amax = max3(amax, magnitude(x), magnitude(y));
+                                amax = fmaxf(amax, fmaxf(magnitude(x), magnitude(y)));
+                                f[n][k][v][i] = pair2(to_hold(x), to_hold(y));
                             }
             }
             amax = warp_max(amax);
             old = __shfl_sync(kFull, old, 0);
         }
-        if (strips > 1) {
-            __syncthreads();  // the last unit's readers are done
-            if (l32 == 0) amax_s[warp] = amax;
+        if (strips > 1) {  // the block's largest magnitude, from all its strips (in turns: one barrier a pass)
+            if (l32 == 0) amax_s[pass][warp] = amax;
             __syncthreads();
-            for (int i = 0; i < strips; i++) amax = fmaxf(amax, amax_s[warp - strip + i]);
+            for (int i = 0; i < strips; i++) amax = fmaxf(amax, amax_s[pass][warp - strip + i]);
         }
         if (!have) continue;
         const float now = block_scale(amax, old, cached);
-        char* dst = (key ? a.cache.k : a.cache.v) + entry_offset(a.batch, a.cache, s.page, s.lo) + head * a.cache.head_stride;
+        char* dst = (key ? a.cache.k : a.cache.v) + dst0 + (long long)head * a.cache.head_stride;
         if (cached && now != old) {
+            char* row = dst;
 #pragma unroll 1
-            for (int n = 0; n < ITER; n++) {
-                const int e = first + n * per;
-                if (e >= s.ctx || e >= s.lo + block) break;
-                char* row = dst + (e - s.lo) * a.cache.token_stride;
+            for (int e = first; e < min(s.ctx, s.lo + strip * R + R); e += per, row += per * a.cache.token_stride) {
 #pragma unroll
                 for (int k = 0; k < UPL; k++) {
                     if (lane.va[k] >= 0) again<V>(row + lane.va[k] * V, old / now);
@@ -343,19 +332,12 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 2 : 1) append8_kernel
         }
         const float inv = 1.0f / now;
 #pragma unroll
-        for (int n = 0; n < ITER; n++) {
-            const int e = first + n * per;
-            if (e < s.e0 || e >= s.e1) continue;
-            char* row = dst + (e - s.lo) * a.cache.token_stride;
+        for (int n = 0; n < ITER; n++, dst += per * a.cache.token_stride) {
+            if (!(rows >> n & 1u)) continue;
 #pragma unroll
             for (int k = 0; k < UPL; k++) {
-                if (!odd) {
-                    if (lane.va[k] >= 0) store_codes<V>(row + lane.va[k] * V, f[n][k][0], inv);
-                    if (lane.vb[k] >= 0) store_codes<V>(row + lane.vb[k] * V, f[n][k][1], inv);
-                } else {
-                    if (lane.va[k] >= 0) store_codes<V, true>(row + lane.va[k] * V, f[n][k][0], inv);
-                    if (lane.vb[k] >= 0) store_codes<V, true>(row + lane.vb[k] * V, f[n][k][1], inv);
-                }
+                if (lane.va[k] >= 0) store_codes<V>(dst + lane.va[k] * V, f[n][k][0], inv);
+                if (lane.vb[k] >= 0) store_codes<V>(dst + lane.vb[k] * V, f[n][k][1], inv);
             }
         }
         if (l32 == 0 && strip == 0 && now != old) *scale_p = now;

@@ -37,7 +37,7 @@ __global__ void __launch_bounds__(256) norm_kernel(const NormArgs a) {
 #pragma unroll
         for (int n = 0; n < kRowsInFlight; n++) {
             const int r = r0 + n * step + tid / h.group;
-            if (r >= rows) continue;
+            if (r >= rows) continue;  // (its values are not used)
             const bool key = r >= a.n_heads;
             const long long head = (long long)(key ? r - a.n_heads : r) * h.head_dim * (int)sizeof(T);
             lane.load((key ? a.k + t * a.k_stride : a.q + t * a.q_stride) + head, x[n]);
@@ -53,13 +53,13 @@ __global__ void __launch_bounds__(256) norm_kernel(const NormArgs a) {
             const int r = r0 + n * step + tid / h.group;
             const bool in = r < rows, key = r >= a.n_heads;
             F2 f[UPL][2][V / 2], g[UPL][2][V / 2];
-            lane.widen(x[n], f);
+            Lane::widen(x[n], f);
             const float inv = inverse_rms(Lane::group_sum(in ? Lane::dot(f, f) : 0.f, h.group), h);
             if (!in) continue;
             lane.weights(key ? a.k_gamma : a.q_gamma, g);
             Lane::scale_by(f, inv, g);
             if (h.rot_dim > 0) lane.rotate(f, c);
-            lane.narrow(f, x[n]);
+            Lane::narrow(f, x[n]);
             const long long head = (long long)(key ? r - a.n_heads : r) * h.head_dim * (int)sizeof(T);
             lane.store((key ? a.k_out + t * a.k_out_stride : a.q_out + t * a.q_out_stride) + head, x[n]);
         }
@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(256) norm_grad_kernel(const NormArgs a) {
     const int my_token = chunks == 1 ? gi / rows : 0, my_row = gi - my_token * rows;
     const int steps = (a.n_tokens + tokens - 1) / tokens * chunks;
     const int pitch = (pairs + V - 1) / V, table = V * pitch;  // factors of a token
-    unsigned char* mine = smem + tid * kBytes;                 // vector v of stage s at ((s * kVecs + v) * 256 + tid)
+    unsigned char* mine = smem + tid * kBytes;                 // vector v of stage s at ((s * kVecs + v) * 256 + tid): x's, then dy's
     const int batch = factor_batch(tokens * pairs);            // steps between barriers
     float* cs = reinterpret_cast<float*>(smem + kStages * kVecs * 256 * kBytes);  // two batches' tables
     // token and row of this thread in step s; false: none
@@ -125,13 +125,14 @@ __global__ void __launch_bounds__(256) norm_grad_kernel(const NormArgs a) {
             unsigned char* to = mine + stage * kVecs * 256 * kBytes;
 #pragma unroll
             for (int k = 0; k < UPL; k++) {
+                unsigned char *tx = to + 2 * k * 256 * kBytes, *tg = tx + 2 * UPL * 256 * kBytes;
                 if (lane.va[k] >= 0) {
-                    cp_async_small<kBytes>(to + (4 * k) * 256 * kBytes, x + lane.va[k] * kBytes);
-                    cp_async_small<kBytes>(to + (4 * k + 1) * 256 * kBytes, g + lane.va[k] * kBytes);
+                    cp_async_small<kBytes>(tx, x + lane.va[k] * kBytes);
+                    cp_async_small<kBytes>(tg, g + lane.va[k] * kBytes);
                 }
                 if (lane.vb[k] >= 0) {
-                    cp_async_small<kBytes>(to + (4 * k + 2) * 256 * kBytes, x + lane.vb[k] * kBytes);
-                    cp_async_small<kBytes>(to + (4 * k + 3) * 256 * kBytes, g + lane.vb[k] * kBytes);
+                    cp_async_small<kBytes>(tx + 256 * kBytes, x + lane.vb[k] * kBytes);
+                    cp_async_small<kBytes>(tg + 256 * kBytes, g + lane.vb[k] * kBytes);
                 }
             }
         }
@@ -167,15 +168,10 @@ __global__ void __launch_bounds__(256) norm_grad_kernel(const NormArgs a) {
         Vec<T, V> x[UPL][2], dy[UPL][2];
         if (in) {
             const unsigned char* from = mine + n % kStages * kVecs * 256 * kBytes;
-#pragma unroll
-            for (int k = 0; k < UPL; k++) {
-                x[k][0].raw = *reinterpret_cast<const decltype(x[0][0].raw)*>(from + (4 * k) * 256 * kBytes);
-                dy[k][0].raw = *reinterpret_cast<const decltype(x[0][0].raw)*>(from + (4 * k + 1) * 256 * kBytes);
-                x[k][1].raw = *reinterpret_cast<const decltype(x[0][0].raw)*>(from + (4 * k + 2) * 256 * kBytes);
-                dy[k][1].raw = *reinterpret_cast<const decltype(x[0][0].raw)*>(from + (4 * k + 3) * 256 * kBytes);
-            }
-            lane.widen(x, f);
-            lane.widen(dy, g);
+            lane.load_own(from, 256 * kBytes, true, x);
+            lane.load_own(from + 2 * UPL * 256 * kBytes, 256 * kBytes, true, dy);
+            Lane::widen(x, f);
+            Lane::widen(dy, g);
             if (pairs) {
                 typename Lane::Factors c;
                 lane.factors(cs + ((buf * batch + in_batch) * tokens + my_token) * table * 2, h, c);
@@ -204,7 +200,7 @@ __global__ void __launch_bounds__(256) norm_grad_kernel(const NormArgs a) {
                         acc[k][v][i] = fma2(g[k][v][i], xr, acc[k][v][i]);
                         f[k][v][i] = mul2(fma2(xr, along2, u[k][v][i]), inv2);
                     }
-            lane.narrow(f, x);
+            Lane::narrow(f, x);
             lane.store(os + t * ostr + (long long)r * D * (int)sizeof(T), x);
         }
         if (++in_batch == batch) {

@@ -83,11 +83,22 @@ struct HeadLane {
             }
         }
     }
+    // the lane's vectors of a row (zeros where it holds nothing)
     PP_DEVINL void load(const char* row, Vec<T, V> (&x)[UPL][2]) const {
 #pragma unroll
         for (int k = 0; k < UPL; k++) {
+            x[k][0].raw = x[k][1].raw = typename Raw<kBytes>::type{};
             if (va[k] >= 0) x[k][0].load(row + va[k] * kBytes);
             if (vb[k] >= 0) x[k][1].load(row + vb[k] * kBytes);
+        }
+    }
+    // ... from a thread's places in shared memory, `step` bytes apart
+    PP_DEVINL void load_own(const unsigned char* from, int step, bool in, Vec<T, V> (&x)[UPL][2]) const {
+#pragma unroll
+        for (int k = 0; k < UPL; k++) {
+            x[k][0].raw = x[k][1].raw = typename Raw<kBytes>::type{};
+            if (in && va[k] >= 0) x[k][0].raw = *reinterpret_cast<const typename Raw<kBytes>::type*>(from + 2 * k * step);
+            if (in && vb[k] >= 0) x[k][1].raw = *reinterpret_cast<const typename Raw<kBytes>::type*>(from + (2 * k + 1) * step);
         }
     }
     PP_DEVINL void store(char* row, const Vec<T, V> (&x)[UPL][2]) const {
@@ -97,15 +108,13 @@ struct HeadLane {
             if (vb[k] >= 0) x[k][1].store(row + vb[k] * kBytes);
         }
     }
-    // fp32 values (zeros where the lane holds nothing)
-    PP_DEVINL void widen(const Vec<T, V> (&x)[UPL][2], F2 (&f)[UPL][2][V2]) const {
+    PP_DEVINL static void widen(const Vec<T, V> (&x)[UPL][2], F2 (&f)[UPL][2][V2]) {
 #pragma unroll
         for (int k = 0; k < UPL; k++)
 #pragma unroll
-            for (int i = 0; i < V2; i++) {
-                f[k][0][i] = va[k] >= 0 ? pair2(x[k][0].get(2 * i), x[k][0].get(2 * i + 1)) : 0ull;
-                f[k][1][i] = vb[k] >= 0 ? pair2(x[k][1].get(2 * i), x[k][1].get(2 * i + 1)) : 0ull;
-            }
+            for (int v = 0; v < 2; v++)
+#pragma unroll
+                for (int i = 0; i < V2; i++) f[k][v][i] = pair2(x[k][v].get(2 * i), x[k][v].get(2 * i + 1));
     }
     PP_DEVINL static void narrow(const F2 (&f)[UPL][2][V2], Vec<T, V> (&x)[UPL][2]) {
 #pragma unroll
