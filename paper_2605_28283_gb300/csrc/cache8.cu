@@ -178,7 +178,9 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 2 : 1) append8_kernel
     const int strips = max(1, block / R), units = (int)blockDim.x / 32 / strips;
     const int strip = warp % strips;
     const int pitch = (h.rot_dim / 2 + V - 1) / V, row_pairs = pitch * V;  // factors of a row
-    const int factors = part * units < a.n_kv_heads ? (s.e1 - s.e0) * (h.rot_dim / 2) : 0;  // values need none
+    // a part takes units side by side, so that most have keys only or values only
+    const int u_first = part * a.passes * units, u_end = min(2 * a.n_kv_heads, u_first + a.passes * units);
+    const int factors = u_first < a.n_kv_heads ? (s.e1 - s.e0) * (h.rot_dim / 2) : 0;  // values need none
     for (int i = tid; i < factors; i += blockDim.x) {
         const int row = i / (h.rot_dim / 2), p = i - row * (h.rot_dim / 2), t = s.token + row;
         const float2 v = cos_sin(h.positions ? h.positions[t] : s.e0 + row, h.inv_freq[p]);
@@ -204,7 +206,7 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 2 : 1) append8_kernel
     };
     auto fetch = [&](int u0, int stage) {
         const int u = u0 + warp / strips;
-        if (u < 2 * a.n_kv_heads) {
+        if (u < u_end) {
             long long step;
             const char* row = row0_of(u, step);
             unsigned char* to = stages + stage * stage_bytes;
@@ -223,17 +225,17 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 2 : 1) append8_kernel
     const bool cached = s.lo < s.ctx;
     const long long dst0 = entry_offset(a.batch, a.cache, s.page, s.lo) + (first - s.lo) * a.cache.token_stride,
                     scale0 = scale_index(a.batch, a.scales, a.n_kv_heads, s.page, 0, s.lo);
-    for (int i = 0; i + 1 < a.stages; i++) fetch((part + i * a.parts) * units, i);
+    for (int i = 0; i + 1 < a.stages; i++) fetch(u_first + i * units, i);
     __syncthreads();
-    for (int u0 = part * units; u0 < 2 * a.n_kv_heads; u0 += units * a.parts, pass ^= 1) {
+    for (int u0 = u_first; u0 < u_end; u0 += units, pass ^= 1) {
         const int u = u0 + warp / strips;
-        const bool have = u < 2 * a.n_kv_heads, key = u < a.n_kv_heads;
+        const bool have = u < u_end, key = u < a.n_kv_heads;
         const int head = key ? u : u - a.n_kv_heads;
         float* scale_p = (key ? a.scales.k : a.scales.v) + scale0 + (long long)head * a.scales.blocks;
         float old = have && cached && l32 == 0 ? *scale_p : 0.f;
         F2 f[ITER][UPL][2][V / 2];
         if (a.stages) {
-            fetch(u0 + (a.stages - 1) * a.parts * units, (turn + a.stages - 1) % a.stages);
+            fetch(u0 + (a.stages - 1) * units, (turn + a.stages - 1) % a.stages);
             if (a.stages == 1)
                 cp_async_wait<0>();
             else if (a.stages == 2)
@@ -354,8 +356,11 @@ cudaError_t append8_run(Append8Args& a, int block, cudaStream_t st) {
     const int units = warps / strips, passes = (2 * a.n_kv_heads + units - 1) / units;
     const long long T_ = a.batch.n_tokens;
     a.slots = (int)(T_ / block + 2ll * a.batch.n_seqs);
-    // a pass of all heads a CTA where there are few blocks; else about four CTAs an SM
-    a.parts = std::min(passes, std::max(1, (608 + a.slots - 1) / a.slots));
+    // a pass of all heads a CTA where there are few blocks; else about two CTAs an SM (8192 tokens: two / four / eight, 107 /
+    // 110 / 119 us)
+    a.parts = std::min(passes, std::max(1, (304 + a.slots - 1) / a.slots));
+    a.passes = (passes + a.parts - 1) / a.parts;
+    a.parts = (passes + a.passes - 1) / a.passes;
     const int threads = warps * 32, pairs = (a.head.rot_dim / 2 + V - 1) / V * V;
     // queries: ten rows' lanes a thread where there are many tokens; few tokens: several CTAs each
     const int rows = threads / a.head.group;  // query rows of a CTA at once
@@ -371,7 +376,7 @@ cudaError_t append8_run(Append8Args& a, int block, cudaStream_t st) {
     // two CTAs an SM where that leaves two stages, else as many as fit
     a.stages = (kAppend8Smem / 2 - a.table_bytes) / stage;
     if (a.stages < 2) a.stages = (kAppend8Smem - a.table_bytes) / stage;
-    a.stages = std::max(0, std::min({a.stages, 3, passes / a.parts + 1}));
+    a.stages = std::max(0, std::min({a.stages, 2, a.passes}));
     const int smem = a.table_bytes + a.stages * stage;
     auto* kern = append8_kernel<T, V, HALF, UPL, ITER, WARPS>;
     static std::atomic<bool> allowed[64];

@@ -97,6 +97,7 @@ struct Append8Args {
     long long q_stride, k_stride, v_stride, q_out_stride;  // bytes
     int n_heads, n_kv_heads;  // n_heads 0: no queries
     int slots, parts;         // blocks of tokens that may be new, CTAs of each
+    int passes;               // of a CTA over heads' keys and values
     int team, split;          // threads of a token's queries, CTAs of them
     int stages, table_bytes;  // shared memory: units of keys and values on their way, behind the factors
     unsigned* status;
