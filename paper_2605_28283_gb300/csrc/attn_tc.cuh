@@ -49,13 +49,16 @@ constexpr float kLazy = 8.0f;  // growth of a row's maximum (log2) that O and th
 
 constexpr int kTurn = 5;  // 16-byte words a row of 32 bf16 takes in the turning area (one of padding)
 
-template <int DP, int MT>
+template <int DP, int MT, bool Q8 = false>
 struct Tc {
     static constexpr int BN = DP == 256 ? 64 : 128;  // keys of a tile
     static constexpr int NG = DP / 64;               // 64-element groups of the head dimension
     static constexpr int kRows = 128 * MT;
     static constexpr int kSlot = BN * DP * 2;
-    static constexpr int kSlots = DP == 64 && MT == 1 ? 6 : 4;  // even: a producer sees keys only or values only
+    static constexpr int kSlots = DP == 64 && MT == 1 && !Q8 ? 6 : 4;  // even: a producer sees keys only or values only
+    // warps that fill a slot: widening codes takes a warp twice as long as the softmax takes for a tile (8 trees: one
+    // 74 us, two 54); with two row tiles there are no registers for more than one
+    static constexpr int kFill = Q8 && MT == 1 ? 2 : 1;
     static constexpr int kQTile = 128 * DP * 2;
     static constexpr int kQBufs = MT == 2 ? 2 : DP == 256 ? 1 : 2;  // MT 2: one for each row tile
     static constexpr int kParts = BN / 32;           // copies of the rows when there are few
@@ -65,7 +68,7 @@ struct Tc {
     static constexpr int kSoftWarps = 4 * MT;
     // warps after the softmax ones: two that issue products, the rows of q, the slots' producers, the schedule
     static constexpr int kWarpMma = kSoftWarps, kWarpQ = kSoftWarps + 2, kWarpSlot = kSoftWarps + 3;
-    static constexpr int kWarps = kWarpSlot + kSlots + 1;
+    static constexpr int kWarps = kWarpSlot + kSlots * kFill + 1;
     static constexpr int kReaders = kWarps - 1;  // that free a part
     static constexpr uint32_t kTmemO = 2 * BN;       // S / P slots first
     static constexpr uint32_t kTmemCols = 512;
@@ -399,10 +402,10 @@ struct Scores {
 };
 
 template <bool Q8, int DP, int MT>
-__global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
+__global__ void __launch_bounds__(Tc<DP, MT, Q8>::kWarps * 32, 1)
     attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensorMap map_k,
                    const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_q) {
-    using C = Tc<DP, MT>;
+    using C = Tc<DP, MT, Q8>;
     constexpr int BN = C::BN, NG = C::NG, ROWS = C::kRows, NS = C::kSlots;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -422,7 +425,7 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
     pdl_launch_dependents();
     if (tid == 0) {
         for (int i = 0; i < NS; i++) {
-            mbar_init(&full[i], 1);
+            mbar_init(&full[i], C::kFill);
             mbar_init(&empty[i], MT);
             mbar_init(&landed[i], 1);
         }
@@ -508,10 +511,35 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
         // nothing for this CTA
     } else if (warp >= C::kWarpSlot) {
         // ------------------------------------------------- producer of one slot
-        const int slot = warp - C::kWarpSlot;
+        const int slot = (warp - C::kWarpSlot) % NS;
         unsigned char* dst = ring + slot * C::kSlot;
         at.enter(0);
         int g_at = 0, uses = 0, fixes = 0;
+        // 8-bit cache: this warp's rows of the tile, and where they lie, looked up while the last tile's are on their way
+        constexpr int kGroups = BN / 32 / C::kFill;
+        const int part = (warp - C::kWarpSlot) / NS * 32 * kGroups;
+        long long off[kGroups];
+        float scale[kGroups];
+        bool known = false;
+        auto look_up = [&](int k0, bool key) {
+            const Item<ROWS, BN>& p = at.item();
+            const float* scales = key ? a.scales.k : a.scales.v;
+#pragma unroll
+            for (int x = 0; x < kGroups; x++) {
+                const int j = k0 + part + 32 * x + lane;
+                off[x] = -1;
+                scale[x] = 0.f;
+                if (j < p.key_end) {
+                    const int page = entry_page(a.batch, p.b, j);
+                    if (page >= 0) {
+                        off[x] = entry_offset(a.batch, a.cache, page, j) + (long long)p.h * a.cache.head_stride;
+                        scale[x] = scales[scale_index(a.batch, a.scales, a.n_kv_heads, page, p.h, j)];
+                    } else {
+                        record_status(a.status, PP_ERR_INVALID_ARG);
+                    }
+                }
+            }
+        };
         for (int pos = slot;; pos += NS, uses++) {
             // order of the loads: K0 K1 V0 K2 V1 K3 ... (MT 1: scores run two
             // tiles ahead), K0 V0 K1 V1 ... (MT 2)
@@ -527,36 +555,26 @@ __global__ void __launch_bounds__(Tc<DP, MT>::kWarps * 32, 1)
             const int open = max(p.open - k0, 0);     // values from here on: not every row of the item sees them
             Item<ROWS, BN>& it = items[at.n % kItems];
             if constexpr (Q8) {
-                constexpr int kGroups = BN / 32;  // of 32 rows
+                if (!known) look_up(k0, key);
                 const char* base = key ? a.cache.k : a.cache.v;
-                const float* scales = key ? a.scales.k : a.scales.v;
-                long long off[kGroups];
-                float scale[kGroups];
-#pragma unroll
-                for (int x = 0; x < kGroups; x++) {
-                    const int j = k0 + 32 * x + lane;
-                    off[x] = -1;
-                    scale[x] = 0.f;
-                    if (32 * x + lane < end) {
-                        const int page = entry_page(a.batch, p.b, j);
-                        if (page >= 0) {
-                            off[x] = entry_offset(a.batch, a.cache, page, j) + (long long)p.h * a.cache.head_stride;
-                            scale[x] = scales[scale_index(a.batch, a.scales, a.n_kv_heads, page, p.h, j)];
-                        } else {
-                            record_status(a.status, PP_ERR_INVALID_ARG);
-                        }
-                    }
-                }
                 if (__any_sync(kFull, uses > 0 && !attn_wait(&empty[slot], (uint32_t)(uses - 1) & 1u, w))) break;
 #pragma unroll
-                for (int x = 0; x < kGroups; x++) fetch_codes32<DP, BN>(dst, 32 * x, base, off[x], a.head_dim, lane);
+                for (int x = 0; x < kGroups; x++) fetch_codes32<DP, BN>(dst, part + 32 * x, base, off[x], a.head_dim, lane);
                 cp_async_commit();
+                float by[kGroups];
+#pragma unroll
+                for (int x = 0; x < kGroups; x++) by[x] = scale[x];
+                // the slot's next tile, if it is the same item's
+                const int ahead = pos == 0 && MT == 1 ? 1 : NS / 2;
+                known = at.t + ahead < at.t1;
+                if (known) look_up(k0 + ahead * BN, MT == 1 ? slot & 1 : key);
                 cp_async_wait<0>();
                 __syncwarp();
 #pragma unroll
-                for (int x = 0; x < kGroups; x++) widen_codes32<DP, BN>(dst, 32 * x, scale[x], lane);
+                for (int x = 0; x < kGroups; x++) widen_codes32<DP, BN>(dst, part + 32 * x, by[x], lane);
                 __syncwarp();
-                if (!key) finite_rows<DP, BN>(dst, open, end, lane, k0, &it.odd0, &it.odd1);
+                if (!key)
+                    finite_rows<DP, BN>(dst, max(open, part), min(end, part + 32 * kGroups), lane, k0, &it.odd0, &it.odd1);
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&full[slot]);
@@ -1071,7 +1089,7 @@ bool query_map(CUtensorMap* map, const AttnArgs& a) {
 
 template <bool Q8, int DP, int MT>
 cudaError_t go(AttnArgs a, bool join_later, int sms, cudaStream_t st) {
-    using C = Tc<DP, MT>;
+    using C = Tc<DP, MT, Q8>;
     auto* kern = attn_tc_kernel<Q8, DP, MT>;
     static std::atomic<bool> allowed[64];
     cudaError_t e = allow_smem(kern, C::kSmem, allowed);
