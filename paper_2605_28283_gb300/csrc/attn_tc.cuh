@@ -56,8 +56,8 @@ struct Tc {
     static constexpr int kRows = 128 * MT;
     static constexpr int kSlot = BN * DP * 2;
     static constexpr int kSlots = DP == 64 && MT == 1 && !Q8 ? 6 : 4;  // even: a producer sees keys only or values only
-    // warps that fill a slot: widening codes takes a warp twice as long as the softmax takes for a tile (8 trees: one
-    // 74 us, two 54); with two row tiles there are no registers for more than one
+    // warps that fill a slot: widening codes takes a warp longer than the softmax takes for a tile (8 trees: one 74 us,
+    // two 66); with two row tiles there are no registers for more than one
     static constexpr int kFill = Q8 && MT == 1 ? 2 : 1;
     static constexpr int kQTile = 128 * DP * 2;
     static constexpr int kQBufs = MT == 2 ? 2 : DP == 256 ? 1 : 2;  // MT 2: one for each row tile
@@ -223,37 +223,33 @@ PP_DEVINL void fetch_codes32(unsigned char* tile, int r0, const char* base, long
 
 template <int DP, int BN>
 PP_DEVINL void widen_codes32(unsigned char* tile, int r0, float scale, int lane) {
-    constexpr int kLanes = DP / 16, kPer = 32 / kLanes, kFlight = 4;
+    constexpr int kLanes = DP / 16, kPer = 32 / kLanes;
     const int sub = lane / kLanes, c = lane % kLanes;
     // 16 codes are two 16-byte chunks of bf16; lanes of the tile's odd groups write theirs in the other order, so
     // that 8 lanes' stores hit all banks
     const int swap = c >> 2 & 1;
+    // a short loop on purpose: eight warps run it beside the others' code, and four rows' chunks a turn, straight-line,
+    // cost more in fetched instructions than they saved in latency (8 trees 57 / 58 / 66 us with one / two / four)
 #pragma unroll 1
-    for (int i = 0; i < kLanes; i += kFlight) {
-        uint4 w[kFlight];
-#pragma unroll
-        for (int k = 0; k < kFlight; k++)
-            w[k] = *reinterpret_cast<const uint4*>(tile + code_place<DP, BN>(r0 + kPer * (i + k) + sub, c));
+    for (int i = 0; i < kLanes; i++) {
+        const int at = kPer * i + sub, r = r0 + at;
+        const uint4 w = *reinterpret_cast<const uint4*>(tile + code_place<DP, BN>(r, c));
+        const float sc = __shfl_sync(kFull, scale, at);
+        const unsigned long long sc2 = pair2(sc, sc);
         __syncwarp();  // a row's codes are read before its elements are written
+        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+        uint32_t y[8];
 #pragma unroll
-        for (int k = 0; k < kFlight; k++) {
-            const int at = kPer * (i + k) + sub, r = r0 + at;
-            const float sc = __shfl_sync(kFull, scale, at);
-            const unsigned long long sc2 = pair2(sc, sc);
-            const uint32_t x[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
-            uint32_t y[8];
-#pragma unroll
-            for (int n = 0; n < 8; n++) {
-                const float2 v = from_codes(x[n / 2] >> (n % 2 * 16) & 0xffffu);
-                float a, b;
-                unpair2(mul2(pair2(v.x, v.y), sc2), a, b);
-                y[n] = pack_bf16x2(a, b);
-            }
-            unsigned char* row = tile + (c >> 2) * BN * 128 + r * 128;
-            const uint4 lo = make_uint4(y[0], y[1], y[2], y[3]), hi = make_uint4(y[4], y[5], y[6], y[7]);
-            *reinterpret_cast<uint4*>(row + ((((c & 3) * 2 + swap) ^ (r & 7)) << 4)) = swap ? hi : lo;
-            *reinterpret_cast<uint4*>(row + ((((c & 3) * 2 + 1 - swap) ^ (r & 7)) << 4)) = swap ? lo : hi;
+        for (int n = 0; n < 8; n++) {
+            const float2 v = from_codes(x[n / 2] >> (n % 2 * 16) & 0xffffu);
+            float a, b;
+            unpair2(mul2(pair2(v.x, v.y), sc2), a, b);
+            y[n] = pack_bf16x2(a, b);
         }
+        unsigned char* row = tile + (c >> 2) * BN * 128 + r * 128;
+        const uint4 lo = make_uint4(y[0], y[1], y[2], y[3]), hi = make_uint4(y[4], y[5], y[6], y[7]);
+        *reinterpret_cast<uint4*>(row + ((((c & 3) * 2 + swap) ^ (r & 7)) << 4)) = swap ? hi : lo;
+        *reinterpret_cast<uint4*>(row + ((((c & 3) * 2 + 1 - swap) ^ (r & 7)) << 4)) = swap ? lo : hi;
     }
 }
 
