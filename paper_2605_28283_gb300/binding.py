@@ -342,9 +342,10 @@ def _torch_dtype(dtype) -> int:
 def _rows(t, n_tokens, n_heads, head_dim, dtype, what):
     """Pointer and token stride of a token tensor [n_tokens, heads, head_dim] (or [n_tokens, heads * head_dim])
     whose tokens are each contiguous."""
-    shape, stride = t.shape, t.stride()
-    if t.dtype == dtype and shape == (n_tokens, n_heads, head_dim) and stride[1:] == (head_dim, 1):
-        return t.data_ptr(), (stride[0] if n_tokens > 1 else n_heads * head_dim)
+    shape = t.shape
+    if t.dtype == dtype and shape == (n_tokens, n_heads, head_dim) and t.is_contiguous():
+        return t.data_ptr(), n_heads * head_dim
+    stride = t.stride()
     if t.dtype != dtype:
         raise PPError(PP_ERR_DTYPE, what)
     if shape != (n_tokens, n_heads, head_dim) and shape != (n_tokens, n_heads * head_dim):
@@ -408,10 +409,10 @@ class HeadNorm:
         self.kinds = [(g.dtype, g.shape[0]) for g in (q_gamma, k_gamma) if g is not None]
 
     def check(self, dtype, head_dim, what):
-        for kind in self.kinds:
-            if kind[0] != dtype:
+        for kind, dim in self.kinds:
+            if kind != dtype:
                 raise PPError(PP_ERR_DTYPE, what + ": weights of another type")
-            if kind[1] != head_dim:
+            if dim != head_dim:
                 raise PPError(PP_ERR_SHAPE, what + ": weights of another head_dim")
 
 
@@ -517,9 +518,15 @@ def pp_rope(rot, positions, x, y, inverse=False, stream=None):
 
 def _heads_of(q, k, what):
     """(tokens, query heads, key heads, head_dim, dtype) of q [T, heads, head_dim] and k [T, kv_heads, head_dim] or None."""
-    if q.dim() != 3 or (k is not None and (k.dim() != 3 or k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2])):
+    shape = q.shape
+    if len(shape) != 3:
         raise PPError(PP_ERR_SHAPE, what)
-    return q.shape[0], q.shape[1], 0 if k is None else k.shape[1], q.shape[2], q.dtype
+    T, H, D = shape
+    if k is None:
+        return T, H, 0, D, q.dtype
+    if k.dim() != 3:
+        raise PPError(PP_ERR_SHAPE, what)
+    return T, H, k.shape[1], D, q.dtype  # (_rows compares the rest of k's shape)
 
 
 def _positions_of(rot, positions, T, what):

@@ -27,16 +27,21 @@ PP_DEVINL long long quotient(long long a, long long b) {
 }
 
 // Tiles of the key line: the schedule is recomputed by whoever walks it, from
-// the lengths alone.  PADDED: where stretches are long, an item counts `pad`
-// tiles more than it has (ahead of its own), for what starting and finishing it
-// costs, so that CTAs with many short items get fewer tiles.
-template <int ROWS, int TOK, bool PADDED = false>
+// the lengths alone.  GROUPED: 1 << shift CTAs side by side take as many key
+// heads side by side, the same stretch of a line that has one such group of heads
+// for a head, so that what lies together in memory is read at the same time; and
+// where stretches are long, an item counts `pad` tiles more than it has (ahead of
+// its own), for what starting and finishing it costs, so that CTAs with many
+// short items get fewer tiles.
+template <int ROWS, int TOK, bool GROUPED = false>
 struct Sched {
     const AttnArgs* a;
-    long long total;  // key tiles of the call
-    int ctas;         // CTAs with work
-    int pad_;
-    PP_DEVINL int pad() const { return PADDED ? pad_ : 0; }
+    long long total;  // key tiles of the line
+    int ctas;         // CTAs (groups of them) with work
+    int pad_, shift_;
+    PP_DEVINL int pad() const { return GROUPED ? pad_ : 0; }
+    PP_DEVINL int shift() const { return GROUPED ? shift_ : 0; }
+    PP_DEVINL int heads() const { return a->n_kv_heads >> shift(); }
 
     PP_DEVINL int row_tiles(const Seq& s) const { return (int)(((unsigned)s.n * (unsigned)a->group + ROWS - 1) / ROWS); }
 
@@ -98,9 +103,9 @@ struct Part {
 };
 
 // Walks the parts of one CTA's stretch.
-template <int ROWS, int TOK, bool PADDED = false>
+template <int ROWS, int TOK, bool GROUPED = false>
 struct Walk {
-    Sched<ROWS, TOK, PADDED> sched;
+    Sched<ROWS, TOK, GROUPED> sched;
     long long at, end;  // the rest of the stretch
     long long base;     // line position of sequence b
     int b, h, j;
@@ -131,10 +136,10 @@ struct Walk {
     PP_DEVINL bool next(Part& p) {
         do {
             if (at >= end) return false;
-            while (m == 0 || h >= sched.a->n_kv_heads) enter(b + 1, m == 0 ? base : head_base);
+            while (m == 0 || h >= sched.heads()) enter(b + 1, m == 0 ? base : head_base);
             const int pad = sched.pad();
             p.b = b;
-            p.h = h;
+            p.h = h << sched.shift() | ((int)blockIdx.x & ((1 << sched.shift()) - 1));
             p.j = j;
             p.seq = seq;
             p.key_end = sched.key_end(seq, j);
@@ -151,7 +156,7 @@ struct Walk {
                     h++;
                 }
             }
-        } while (PADDED && p.t1 == 0);  // the stretch ends ahead of the item's first tile
+        } while (GROUPED && p.t1 == 0);  // the stretch ends ahead of the item's first tile
         return true;
     }
 };
@@ -160,11 +165,13 @@ struct Walk {
 // counts a run of sequences, a scan over the lanes gives the total, and the
 // lane whose run holds this CTA's first tile looks for its sequence.  Short
 // code on purpose: it runs once, from a cold instruction cache.
-template <int ROWS, int TOK, bool PADDED = false>
-PP_DEVINL Walk<ROWS, TOK, PADDED> start_walk(const AttnArgs* a, int lane, bool report, int least, int pad = 0) {
-    Walk<ROWS, TOK, PADDED> w;
+template <int ROWS, int TOK, bool GROUPED = false>
+PP_DEVINL Walk<ROWS, TOK, GROUPED> start_walk(const AttnArgs* a, int lane, bool report, int least, int pad = 0, int shift = 0) {
+    Walk<ROWS, TOK, GROUPED> w;
     w.sched.a = a;
     w.sched.pad_ = 0;
+    w.sched.shift_ = shift;
+    const int grid = (int)gridDim.x >> w.sched.shift(), me = (int)blockIdx.x >> w.sched.shift();
     const int B = a->batch.n_seqs, run = (B + 31) / 32;
     const int b0 = min(lane * run, B), b1 = min(b0 + run, B);
     long long mine = 0, items = 0;
@@ -173,16 +180,16 @@ PP_DEVINL Walk<ROWS, TOK, PADDED> start_walk(const AttnArgs* a, int lane, bool r
         const Seq q = load_seq(a->batch, b);
         if (report && q.bad) record_status(a->status, PP_ERR_INVALID_ARG);
         mine += w.sched.head_tiles(q);
-        if (PADDED) items += w.sched.row_tiles(q);
+        if (GROUPED) items += w.sched.row_tiles(q);
     }
-    mine *= a->n_kv_heads;
-    if (PADDED) {
+    mine *= w.sched.heads();
+    if (GROUPED) {
         // stretches of at least kLongStretch tiles
         long long all = mine;
 #pragma unroll 1
         for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(kFull, all, o);
-        if (all >= (long long)kLongStretch * gridDim.x) w.sched.pad_ = pad;
-        mine += items * a->n_kv_heads * w.sched.pad_;
+        if (all >= (long long)kLongStretch * grid) w.sched.pad_ = pad;
+        mine += items * w.sched.heads() * w.sched.pad_;
     }
     long long sum = mine;
 #pragma unroll 1
@@ -190,19 +197,19 @@ PP_DEVINL Walk<ROWS, TOK, PADDED> start_walk(const AttnArgs* a, int lane, bool r
         const long long u = __shfl_up_sync(kFull, sum, o);
         if (lane >= o) sum += u;
     }
-    w.sched.deal(__shfl_sync(kFull, sum, 31), (int)gridDim.x, least);
+    w.sched.deal(__shfl_sync(kFull, sum, 31), grid, least);
     w.at = w.end = 0;
     w.m = 0;
-    if ((int)blockIdx.x >= w.sched.ctas) return w;
-    w.at = w.sched.begin_of(blockIdx.x);
-    w.end = w.sched.begin_of((int)blockIdx.x + 1);
+    if (me >= w.sched.ctas) return w;
+    w.at = w.sched.begin_of(me);
+    w.end = w.sched.begin_of(me + 1);
     long long base = sum - mine;
     int b = b0;
     const bool here = base <= w.at && w.at < sum;
     if (here) {
 #pragma unroll 1
         for (; b + 1 < b1; b++) {
-            const long long t = w.sched.head_tiles(load_seq(a->batch, b)) * a->n_kv_heads;
+            const long long t = w.sched.head_tiles(load_seq(a->batch, b)) * w.sched.heads();
             if (base + t > w.at) break;
             base += t;
         }
@@ -225,16 +232,20 @@ PP_DEVINL float* part_place(const AttnArgs& a, int c, bool tail) {
 // Range of CTAs that hold a split item's parts.
 template <int ROWS, int TOK>
 struct Split {
-    int c0, c1;
+    int c0, c1;      // (groups of) CTAs
+    int step, lane;  // of a group: its CTAs, and this item's among them
     bool c0_tail;  // the first part lies in c0's second place
     Split() = default;
-    template <bool PADDED>
-    PP_DEVINL Split(const Sched<ROWS, TOK, PADDED>& s, const Part& p) {
+    template <bool GROUPED>
+    PP_DEVINL Split(const Sched<ROWS, TOK, GROUPED>& s, const Part& p) {
         c0 = s.cta_of(p.first + s.pad());
         c1 = s.cta_of(p.first + s.pad() + p.tiles - 1);
         c0_tail = s.begin_of(c0) < p.first;
+        step = 1 << s.shift();
+        lane = (int)blockIdx.x & (step - 1);
     }
-    PP_DEVINL float* place(const AttnArgs& a, int c) const { return part_place<ROWS>(a, c, c == c0 && c0_tail); }
+    PP_DEVINL int cta(int c) const { return c * step + lane; }
+    PP_DEVINL float* place(const AttnArgs& a, int c) const { return part_place<ROWS>(a, cta(c), c == c0 && c0_tail); }
 };
 
 // Arrival of one part's CTA at its item, after a barrier behind the stores of

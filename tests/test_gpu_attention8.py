@@ -110,6 +110,14 @@ def test_long_and_split_items(pp, dtype, heads, kv, dim):
     Case8([(9, 3000), (1, 900), (2, 1)], heads, kv, dim, 16, 16, dtype, mask="tree").check(pp)
 
 
+@pytest.mark.parametrize("kv,order", [(8, "token"), (6, "token"), (8, "head"), (3, "token")])
+def test_many_heads_over_long_ragged_contexts(pp, kv, order):
+    """Stretches of many tiles: heads taken side by side (8: in fours, 6: in twos), items that count more than their tiles,
+    short and empty sequences among long ones."""
+    seqs = [(1, 9000), (1, 3), (1, 0), (0, 50), (1, 6001), (1, 130), (1, 7777), (2, 4000), (1, 128), (1, 5000), (1, 64)]
+    Case8(seqs * 2, 2 * kv, kv, 128, 64, 16, "bf16", order=order, spread=2, seed=kv).check(pp)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_prompts_and_padding(pp, dtype):
     Case8([(200, 90), (129, 3), (300, 0)], 4, 2, 64, 32, 16, dtype, pad=5).check(pp)
