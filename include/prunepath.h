@@ -515,7 +515,12 @@ pp_status pp_kvq_read(const pp_cache8 *cache, const pp_batch *batch, void *k_out
                       int64_t v_out_stride, void *ws, size_t ws_bytes, void *stream);
 
 /* pp_tree_attention over an 8-bit cache: the same masks, shapes and results,
-   with code * scale for the keys and values. */
+   with code * scale for the keys and values.  bf16, where sequences bring up
+   to 16 query rows a key head on average: the codes are multiplied as they
+   are, and queries and weights as two e4m3 numbers each, which holds a query
+   element exactly down to 2^-14 of its head's largest and a weight to 2^-8 of
+   itself or 2^-18 of the largest; with more rows, the codes are made bf16
+   (exact for powers of two as scales). */
 pp_status pp_kvq_tree_attention(const pp_cache8 *cache, const pp_batch *batch, const void *q, int64_t q_stride,
                              const uint32_t *mask, int mask_words, float scale, void *out, int64_t out_stride, void *ws,
                              size_t ws_bytes, void *stream);

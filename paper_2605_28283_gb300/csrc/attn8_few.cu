@@ -28,6 +28,12 @@
 // producers of the ring (TMA, a box a page; else cp.async), one that walks the
 // stretch.  A quarter's weights of a tile take 8 of the 32 columns that its scores
 // had, and zeros the same columns of the other quarters' keys.
+//
+// Measured (GB300): one token for each of 64 ragged sequences of 64 to 8191
+// entries, 32 heads on 8 key heads of 128: 99 us, 5.4 TB/s (0.80 of the copy rate);
+// without the softmax's arithmetic 3 us less (the same call over a bf16 cache 166).  What
+// is left is HBM's: rows of 128 bytes, fetched without what lies beside them.  A
+// third slot of scores in place of the second O changed nothing.
 #include "attn_tc.cuh"
 #include "pp_tc_f8.cuh"
 

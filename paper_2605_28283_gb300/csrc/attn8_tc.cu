@@ -6,7 +6,8 @@
 namespace pp {
 
 cudaError_t attn8_tc_launch(const AttnArgs& a, int sms, cudaStream_t st) {
-    // rows a sequence brings to a key head on average, as in attn_tc.cuh
+    // Rows a sequence brings to a key head on average, as in attn_tc.cuh.  64 single tokens (4 rows): multiplied as they
+    // are 99 us, made bf16 first 333.
     const long long rows = ((long long)a.batch.n_tokens * a.group + a.batch.n_seqs - 1) / a.batch.n_seqs;
     if (rows <= 16) return attn8_few_launch(a, sms, st);
     return launch<true>(a, sms, st);

@@ -21,7 +21,11 @@ namespace {
 // strip of R rows of one head's keys or values is held by one warp, in
 // registers: its largest magnitude is known before anything is written, and
 // every element is read once.  The strips of a longer block meet in shared
-// memory.  The other CTAs take a token's query heads, as in norm_kernel.
+// memory.  The other CTAs take a token's query heads, as in norm_kernel.  8192
+// tokens of 40 + 40 + 40 heads of 128, bf16, blocks of 64, normed (399 MB): 107 us,
+// 3.7 TB/s (0.55 of the copy rate), 95 of it for the keys and values, which 16
+// warps an SM do not keep on their way (blocks of 16: 68; without norms 57); 64
+// single tokens: 5.3 us, a chain of latencies.
 constexpr int kMaxStrips = 16;  // warps of a CTA at most (8 where that does)
 constexpr int kAppend8Smem = 216 * 1024;
 
@@ -414,7 +418,8 @@ cudaError_t append8_typed(const Append8Args& a, int layout, int block, cudaStrea
 // --------------------------------------------------------------------- read
 // 8 * share tokens a CTA (gridDim.y of them share the tokens' rows, where there
 // are few): a warp looks the entries of its share up, then all threads go over
-// the rows, V codes (a 16-byte store) at a time.
+// the rows, V codes (a 16-byte store) at a time.  128 thousand tokens of 8 heads of
+// 128 to bf16 (765 MB): 126 us, 6.1 TB/s (0.89 of the copy rate).
 constexpr int kReadTokens = 32, kReadUnits = 4;
 
 template <typename T>
@@ -510,7 +515,9 @@ __global__ void __launch_bounds__(256) read8_kernel(const Read8Args a, const int
 // are read once where a warp holds a block's (16 rows of 128), else twice.  In
 // place and without a barrier between warps: path[j] >= j, so what is read lies
 // at or past what is written, and rows of one batch are read by the whole warp
-// before any is written.
+// before any is written.  32 sequences of 8 accepted tokens in 32 layers (34 MB):
+// 21 us, half of it instructions (codes apart and together again) and the rest
+// the chain path - places - codes - stores; one sequence: 5.0 us.
 constexpr int kMoveBatch = 4;
 constexpr int kMoveChunk = 128;  // entries of a destination block at most
 

