@@ -516,7 +516,7 @@ pp_status pp_kvq_read(const pp_cache8 *cache, const pp_batch *batch, void *k_out
 
 /* pp_tree_attention over an 8-bit cache: the same masks, shapes and results,
    with code * scale for the keys and values.  bf16, where sequences bring up
-   to 16 query rows a key head on average: the codes are multiplied as they
+   to 32 query rows a key head on average: the codes are multiplied as they
    are, and queries and weights as two e4m3 numbers each, which holds a query
    element exactly down to 2^-14 of its head's largest and a weight to 2^-8 of
    itself or 2^-18 of the largest; with more rows, the codes are made bf16

@@ -319,3 +319,28 @@ def test_steps_of_a_decode_loop(pp, dtype):
         ctx = ctx + acc
         assert np.array_equal(new_len.cpu().numpy(), ctx)
     assert pp.pp_get_device_status(ws) == pp.PP_OK
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("kv", [8, 16])
+def test_every_code_alone(pp, kv, dim):
+    # one visible entry a sequence: a weight of one, so that the result is code * scale, rounded once
+    scales = np.array([1.0, 2.0 ** -60, 2.0 ** 8, 2.0 ** 119, 1.5, 1 + 2.0 ** -15, 0.75 * 2.0 ** -30, 2.0 ** 100], np.float32)
+    c = Case8([(40, 1)] * (256 // dim) + [(200, 1)], 2 * kv if kv == 16 else kv, kv, dim, 16, 16, "bf16", mask="random")
+    c.mask[:] = 0
+    held = c.held[1]
+    for b in range(len(c.ctx)):
+        page = int(c.pages[b][0])
+        held.code[page, 0] = (dim * b + np.arange(dim)) % 256
+        held.scale[page, :, 0] = np.resize(scales, kv)
+    c.refresh()
+    got, status, _ = c.run(pp)
+    assert status == 0
+    for b in range(len(c.ctx)):
+        code = (dim * b + np.arange(dim)) % 256
+        want = ref.VALUES[code][None] * np.resize(scales, kv)[:, None].astype(np.float64)
+        want = np.repeat(want, c.heads // kv, 0).astype(np.float32)
+        import torch
+        want = torch.from_numpy(want).to(torch.bfloat16).float().numpy()
+        rows = got[c.starts[b]:c.starts[b + 1]].reshape(-1, c.heads, dim)
+        np.testing.assert_array_equal(rows, np.broadcast_to(want, rows.shape))
