@@ -248,7 +248,7 @@ def test_bad_lengths_and_pages_are_reported(pp, dtype, n):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_strided_tokens(pp, dtype):
     import torch
-    for seqs in ([(1, 90), (1, 4)], [(3, 90), (17, 4)]):
+    for seqs in ([(1, 90), (1, 4)], [(3, 90), (17, 4)], [(30, 90), (40, 4)]):
         c = Case8(seqs, 4, 2, 64, 16, 16, dtype, mask="tree")
         cache, batch, q, mask, _ = c.device(pp)
         ws = pp.alloc_kvq_workspace(cache)
