@@ -728,6 +728,15 @@ def pp_kvq_commit(cache, batch, path, n_accept, ws, new_len=None, n_layers=1, la
                                 _stream_handle(stream)), "pp_kvq_commit")
 
 
+# The calls on an 8-bit cache by the names that they had first, for programs written against those.  (The C names carry
+# no digits.)
+alloc_attn8_workspace = alloc_kvq_workspace
+pp_kv8_append = pp_kvq_append
+pp_kv8_read = pp_kvq_read
+pp_tree_attention8 = pp_kvq_tree_attention
+pp_kv8_commit = pp_kvq_commit
+
+
 def pp_get_device_status(ws, stream=None) -> int:
     return int(load().pp_get_device_status(_ptr(ws), _stream(stream)))
 
