@@ -325,7 +325,7 @@ def prepare(case, seed):
         s["cache"] = pp.KVCache8(pick(s["k_code"]), pick(s["v_code"]), pick(s["k_scale"]), pick(s["v_scale"]),
                                  case.get("heads", case["kv_heads"]), s["dt"])
         s["batch"] = pp.Batch(s["q_start"], s["ctx_len"], s["pages"], s["starts"][-1])
-        s["ws"] = pp.alloc_kvq_workspace(s["cache"])
+        s["ws"] = pp.alloc_attn8_workspace(s["cache"])
     return s
 
 
@@ -500,16 +500,16 @@ def run(s):
                                   s["k_out"], s["dq_gamma"], s["dk_gamma"], s["ws"])
         return [s["q_out"], s["k_out"], s["dq_gamma"], s["dk_gamma"]]
     if op == "append":
-        pp.pp_kvq_append(s["cache"], s["batch"], s["norm"], s["rot"], s["pos"], s["q"], s["k"], s["v"], s["out"],
+        pp.pp_kv8_append(s["cache"], s["batch"], s["norm"], s["rot"], s["pos"], s["q"], s["k"], s["v"], s["out"],
                          s["ws"])
         return [s["out"]] + _cache_of(s)
     if op == "read":
-        pp.pp_kvq_read(s["cache"], s["batch"], s["k_out"], s["v_out"], s["ws"])
+        pp.pp_kv8_read(s["cache"], s["batch"], s["k_out"], s["v_out"], s["ws"])
         return [s["k_out"], s["v_out"]]
     if op == "attend":
-        pp.pp_kvq_tree_attention(s["cache"], s["batch"], s["q"], s["mask"], s["scale"], s["out"], s["ws"])
+        pp.pp_tree_attention8(s["cache"], s["batch"], s["q"], s["mask"], s["scale"], s["out"], s["ws"])
         return s["out"]
-    pp.pp_kvq_commit(s["cache"], s["batch"], s["path"], s["n_accept"], s["ws"], new_len=s["new_len"],
+    pp.pp_kv8_commit(s["cache"], s["batch"], s["path"], s["n_accept"], s["ws"], new_len=s["new_len"],
                      n_layers=case["layers"], layer_stride=s["k_code"].stride(0),
                      scale_layer_stride=s["k_scale"].stride(0))
     return _cache_of(s) + [s["new_len"]]
