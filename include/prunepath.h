@@ -516,11 +516,12 @@ pp_status pp_kvq_read(const pp_cache8 *cache, const pp_batch *batch, void *k_out
 
 /* pp_tree_attention over an 8-bit cache: the same masks, shapes and results,
    with code * scale for the keys and values.  bf16, where sequences bring up
-   to 32 query rows a key head on average: the codes are multiplied as they
-   are, and queries and weights as two e4m3 numbers each, which holds a query
-   element exactly down to 2^-14 of its head's largest and a weight to 2^-8 of
-   itself or 2^-18 of the largest; with more rows, the codes are made bf16
-   (exact for powers of two as scales). */
+   to 16 query rows a key head on average: the codes are multiplied as they
+   are, and queries and weights as sums of e4m3 numbers.  That holds a query
+   element exactly down to 2^-14 of its head's largest, and below to 2^-21 of
+   the largest; and a weight, times its block's value scale, to 2^-8 of itself
+   (as in bf16) or 2^-41 of the largest such product of its row.  With more
+   rows, the codes are made bf16 (exact for powers of two as scales). */
 pp_status pp_kvq_tree_attention(const pp_cache8 *cache, const pp_batch *batch, const void *q, int64_t q_stride,
                              const uint32_t *mask, int mask_words, float scale, void *out, int64_t out_stride, void *ws,
                              size_t ws_bytes, void *stream);

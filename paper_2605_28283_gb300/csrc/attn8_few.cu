@@ -2,26 +2,33 @@
 // e4m3 keys and values): the codes go into the products as they lie in the
 // cache, so that a step is bound by reading half the bytes of a bf16 cache.
 //
-// The other operand of each product is 16 bits wide and is split exactly, or
-// nearly so, into two e4m3 numbers: x = hi + lo / 16, hi the nearest code, lo
-// that of 16 times the rest.  A bf16 number has 8 significant bits and a code
-// 4, so hi + lo / 16 holds a query element exactly down to 2^-6 of its row's
-// scale, and to 2^-14 of it below; a softmax weight is held to 2^-8 of itself, as
-// in bf16, or 2^-20 of the largest.  The 128 rows of a product are filled with
-// those pieces: lane i of each quarter holds hi of row i (i < 16), lane 16 + i
-// its lo; the quarters hold copies, each with its own 32 keys of the tile (as
-// for few rows in attn_tc.cuh).  So a tile of 128 keys costs two products of 256
-// cycles, where reading it takes 1400.
+// The other operand of each product is wider and is split into e4m3 numbers.  A
+// code has 4 significant bits.  Queries, x = p0 + p1 / 2^4: p0 the nearest code,
+// p1 that of 16 times the rest, which holds a query element (8 significant bits)
+// exactly down to 2^-14 of its head's largest and to 2^-21 of the largest below.
+// Weights, x = p0 + p1 / 2^4 + p2 / 2^22 + p3 / 2^26: p2 and p3 are the same for
+// what p0 and p1 leave of small numbers, at a second base.  (That is at most
+// 2^-14, half of p1's last place, so 2^22 times it stays below 448.  What is left
+// of a larger number may pass that; p2 then holds part of it.)  So a weight is
+// held to 2^-8 of itself, as in bf16, or 2^-36: 2^-41 of its row's largest (times
+// their value scales, below).  With p0 and p1 alone, to 2^-19 of the largest, the
+// result is lost where one key takes most of a row and has small values, or lies
+// in a block of large scale whose other elements are small.
 //
-// The two lanes of a row share its 32 keys: lane i weighs the first 16, lane
-// 16 + i the others (a scale's block each).  They hand each other the halves of
-// the scores, S = hi.k + lo.k / 16, that they need, and the codes of the weights.
+// The 128 rows of a product are filled with the pieces: lane 8 p + i of each
+// quarter holds piece p of row i's weights (i < 8), and piece p % 2 of its query;
+// the quarters hold copies, each with its own 32 keys of the tile (as for few
+// rows in attn_tc.cuh).  So a tile of 128 keys costs two products of 256 cycles,
+// where reading it takes 1400.  The four lanes of a row share its 32 keys: lane
+// 8 p + i weighs the p-th eight (of one scale's block).  They hand one another
+// the parts of the scores, S = p0.k + p1.k / 16, and the codes of the weights.
 //
 // Scales: a key's score is S times its row's and its block's scale.  A weight is
 // multiplied by its block's value scale before it is split; the running base of
 // these products (b, per row and quarter) is apart from the scores' running
 // maximum (m, per lane), since scales may differ widely between blocks:
-// w = 2^(z - m) vs 2^(m - b), and the sum of weights is that of 2^(z - m).
+// w = 2^(z - x) vs 2^(x - b) with x the tile's largest z, and the sum of weights
+// is that of 2^(z - m).
 //
 // Warps: four softmax, four that finish parts (O has two buffers for that, up to
 // 128 elements), two that issue products, one that splits the rows of q, four
@@ -30,23 +37,25 @@
 // had, and zeros the same columns of the other quarters' keys.
 //
 // Measured (GB300): one token for each of 64 ragged sequences of 64 to 8191
-// entries, 32 heads on 8 key heads of 128: 99 us, 5.4 TB/s (0.80 of the copy rate);
-// without the softmax's arithmetic 3 us less (the same call over a bf16 cache 166).  What
-// is left is HBM's: rows of 128 bytes, fetched without what lies beside them.  A
-// third slot of scores in place of the second O changed nothing.
+// entries, 32 heads on 8 key heads of 128: 99 us, 5.4 TB/s (0.80 of the copy rate;
+// the same call over a bf16 cache 166), 32 key heads 333 us.  Two things are close
+// to one another: HBM's rows of 128 bytes, fetched without what lies beside them,
+// and the softmax of a tile, which one warp a quarter does in a chain (four pieces
+// of the query as well, three times as many exchanged scores: 109 and 386 us).
 #include "attn_tc.cuh"
 #include "pp_tc_f8.cuh"
 
 namespace pp {
 namespace {
 
-constexpr int kFewRows = 16;        // rows of an item
+constexpr int kFewRows = 8;         // rows of an item
 // Tiles that an item counts more than it has: 0 / 2 / 4 / 8, 64 ragged single tokens 112.5 / 104.7 / 106.3 / 107.9 us.
 constexpr int kPad = 2;
 constexpr float kLazy8 = 2.0f;      // growth of the base (log2) that O absorbs unscaled
-constexpr float kTopWeight = 64.f;  // the largest weight at its base, in codes: 2^kLazy8 times that stays below 448
+// The largest weight at its base, in codes: 2^kLazy8 times that, times the fraction of a scale (below 2), stays below 448.
+constexpr float kTopWeight = 32.f;
 constexpr int kFacTiles = 8;        // tiles whose scales are held
-constexpr int kFac = 24;            // floats of a tile: 8 blocks of 16 keys each: score factor, value scale, its log2
+constexpr int kFac = 24;            // floats of a tile: 8 blocks of 16 keys each: score factor, value scale's fraction, its exponent
 
 template <int DP>
 struct Few {
@@ -119,13 +128,32 @@ PP_DEVINL void finite_codes(unsigned char* tile, int r0, int r1, int lane, int k
     }
 }
 
-// Four values as codes, and 16 times what the codes leave of them.
-PP_DEVINL void split4(const float (&x)[4], uint32_t& hi, uint32_t& lo) {
-    const uint32_t a = to_codes(x[0], x[1]), b = to_codes(x[2], x[3]);
-    const float2 va = from_codes(a), vb = from_codes(b);
-    hi = a | b << 16;
-    lo = to_codes((x[0] - va.x) * 16.f, (x[1] - va.y) * 16.f) | to_codes((x[2] - vb.x) * 16.f, (x[3] - vb.y) * 16.f) << 16;
+// Two values in N pieces of two codes each.
+template <int N>
+PP_DEVINL void split2(unsigned long long x, uint32_t (&p)[N]) {
+    constexpr float kUp[4] = {1.f, 0x1p4f, 0x1p22f, 0x1p26f};
+    float a, b;
+    unpair2(x, a, b);
+    p[0] = to_codes(a, b);
+#pragma unroll
+    for (int i = 1; i < N; i++) {
+        const float2 v = from_codes(p[i - 1]);
+        x = fma2(pair2(v.x, v.y), pair2(-1.f / kUp[i - 1], -1.f / kUp[i - 1]), x);
+        unpair2(mul2(x, pair2(kUp[i], kUp[i])), a, b);
+        p[i] = to_codes(a, b);
+    }
 }
+// Four values, a word a piece.
+template <int N>
+PP_DEVINL void split4(unsigned long long x, unsigned long long y, uint32_t (&w)[N]) {
+    uint32_t a[N], b[N];
+    split2(x, a);
+    split2(y, b);
+#pragma unroll
+    for (int i = 0; i < N; i++) w[i] = a[i] | b[i] << 16;
+}
+// A piece's weight.
+PP_DEVINL float piece_weight(int p) { return p == 0 ? 1.f : p == 1 ? 0x1p-4f : p == 2 ? 0x1p-22f : 0x1p-26f; }
 
 template <int DP>
 __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
@@ -240,9 +268,10 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
         auto put_scales = [&](int g, float f) {
             float* to = fac[g % kFacTiles];
             if (lane < 8) to[lane] = f * a.scale_log2;
-            if (lane >= 8 && lane < 16) {
-                to[lane] = f;
-                to[lane + 8] = __log2f(f);
+            if (lane >= 8 && lane < 16) {  // a positive normal number: fraction and exponent
+                const int bits = __float_as_int(f);
+                to[lane] = __int_as_float((bits & 0x7fffff) | 0x3f800000);
+                to[lane + 8] = (float)((bits >> 23) - 127);
             }
             __syncwarp();
         };
@@ -312,7 +341,7 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
             more = go_to(pos + C::kLoads);
         }
     } else if (warp == C::kWarpQ) {
-        // ------------------------------------- rows of q: two pieces, four copies
+        // ------------------------------------- rows of q: two pieces, eight copies
         at.enter(0);
         bool lost = at.lost;
         constexpr int kE = DP / 32, kAhead = 4;  // elements of a lane, rows on their way
@@ -356,16 +385,15 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
                         float y[4];
 #pragma unroll
                         for (int u = 0; u < 4; u++) y[u] = to_hold(x[i + u]) * inv;
-                        uint32_t hi, lo;
-                        split4(y, hi, lo);
+                        uint32_t piece[2];
+                        split4(pair2(y[0], y[1]), pair2(y[2], y[3]), piece);
                         const int e = d + i;  // element: 16-byte chunk e / 16 of group e / 128
                         unsigned char* base = qs + buf * C::kQTile + (e >> 7) * 128 * 128 + (e & 15) + r * 128 +
                                               ((((e & 127) >> 4) ^ (r & 7)) << 4);
 #pragma unroll
-                        for (int c = 0; c < 4; c++) {
-                            *reinterpret_cast<uint32_t*>(base + 32 * c * 128) = hi;
-                            *reinterpret_cast<uint32_t*>(base + (32 * c + 16) * 128) = lo;
-                        }
+                        for (int c = 0; c < 4; c++)
+#pragma unroll
+                            for (int u = 0; u < 4; u++) *reinterpret_cast<uint32_t*>(base + (32 * c + 8 * u) * 128) = piece[u & 1];
                     }
                 }
 #pragma unroll
@@ -432,10 +460,10 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
         }
     } else if (warp < C::kWarpOut) {
         // ----------------------------------------------------------- softmax
-        const int wq = warp, row = lane & 15;
-        const bool low = lane >= 16;
+        const int wq = warp, row = lane & 7, piece = lane >> 3;
+        const bool b1 = lane & 16, b0 = lane & 8;  // the piece's (and the eight keys') bits
         const uint32_t lanes = (uint32_t)(32 * wq) << 16;
-        const float c_own = low ? 0.0625f : 1.f, c_other = low ? 1.f : 0.0625f;
+        const float c_own = b0 ? 0x1p-4f : 1.f, c_other = b0 ? 1.f : 0x1p-4f;  // of the queries' pieces
         int g = 0;  // tile of the stretch
         auto products_done = [&](int x) {
             attn_wait(&odone[x & 1], (uint32_t)(x >> 1) & 1u, w);
@@ -459,79 +487,100 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
                 tmem_ld_wait();
                 // scales of the row and the tile: written ahead of the products
                 if (t == t0) qsc = q_scale[at.n % kItems][row];
-                const float* fc = fac[g % kFacTiles] + 2 * wq + (low ? 1 : 0);
-                const float f = fmaxf(fc[0] * qsc, 0x1p-126f), vs = fc[8], lv = fc[16];  // f > 0: -inf stays
-                float s[16];
+                const float* fc = fac[g % kFacTiles] + 2 * wq + (b1 ? 1 : 0);
+                const float f = fminf(fmaxf(fc[0] * qsc, 0x1p-126f), 0x1p127f);  // positive and finite: -inf stays, and 0
+                const float vs = fc[8], lv = fc[16];
+                // the row's scores of this lane's eight keys, from its piece of the query and that of the lane 8 further
+                float s[8];
 #pragma unroll
-                for (int i = 0; i < 16; i++) {
-                    const float own = __uint_as_float(low ? u[16 + i] : u[i]);
-                    const float other = __shfl_xor_sync(kFull, __uint_as_float(low ? u[i] : u[16 + i]), 16);
-                    s[i] = fmaf(other, c_other, own * c_own);
+                for (int i = 0; i < 8; i += 2) {
+                    float own[2], got[2];
+#pragma unroll
+                    for (int v = 0; v < 2; v++) {
+                        const uint32_t first = b1 ? u[16 + i + v] : u[i + v], second = b1 ? u[24 + i + v] : u[8 + i + v];
+                        got[v] = __shfl_xor_sync(kFull, __uint_as_float(b0 ? first : second), 8);
+                        own[v] = __uint_as_float(b0 ? second : first);
+                    }
+                    unpair2(fma2(pair2(got[0], got[1]), pair2(c_other, c_other), mul2(pair2(own[0], own[1]), pair2(c_own, c_own))), s[i], s[i + 1]);
                 }
                 const int k0 = t * BN + 32 * wq;
                 if (k0 + 32 > open) {
-                    const uint32_t see = seen_bits(a, p, tok, k0) >> (low ? 16 : 0);
+                    const uint32_t see = seen_bits(a, p, tok, k0) >> 8 * piece;
 #pragma unroll
-                    for (int i = 0; i < 16; i++)
+                    for (int i = 0; i < 8; i++)
                         if (!(see >> i & 1u)) s[i] = -INFINITY;
                 }
-                float x0 = max3(s[0], s[1], s[2]), x1 = max3(s[3], s[4], s[5]);
-                x0 = max3(x0, s[6], s[7]);
-                x1 = max3(x1, s[8], s[9]);
-                x0 = max3(x0, s[10], s[11]);
-                x1 = max3(x1, s[12], s[13]);
-                const float x = max3(fmaxf(x0, x1), s[14], s[15]) * f;
+                const float x = max3(max3(s[0], s[1], s[2]), max3(s[3], s[4], s[5]), fmaxf(s[6], s[7])) * f;
+                const float xb = x == -INFINITY ? 0.f : x;
                 // the scores' maximum moves with every tile (a register), O's base when it has to
                 const float m_new = fmaxf(x, m), mb = m_new == -INFINITY ? 0.f : m_new;
-                sum *= ex2(m - mb);
-                m = m_new;
-                float top = x + lv;
-                top = fmaxf(top, __shfl_xor_sync(kFull, top, 16));
-                const bool grow = top > b + kLazy8 || (b == -INFINITY && top > b);
-                if (t == t0) {
-                    b = top;
-                } else if (__any_sync(kFull, grow)) {
-                    products_done(g - 1);
+                const float own_top = x + lv;
+                if (__any_sync(kFull, own_top > b + kLazy8)) {  // (also the first keys that are seen: b is -inf ahead of them)
+                    float top = fmaxf(own_top, __shfl_xor_sync(kFull, own_top, 16));
+                    top = fmaxf(top, __shfl_xor_sync(kFull, top, 8));
+                    const bool grow = top > b + kLazy8;
                     const float fo = grow ? ex2(b - top) : 1.f;  // 0 from -inf
                     b = grow ? top : b;
+                    if (t > t0) {
+                        products_done(g - 1);
 #pragma unroll 1
-                    for (int c = 0; c < a.head_dim; c += 16) {
-                        uint32_t o[16];
-                        tmem_ld16(t_o + c, o);
-                        tmem_ld_wait();
+                        for (int c = 0; c < a.head_dim; c += 16) {
+                            uint32_t o[16];
+                            tmem_ld16(t_o + c, o);
+                            tmem_ld_wait();
 #pragma unroll
-                        for (int i = 0; i < 16; i++) o[i] = __float_as_uint(__uint_as_float(o[i]) * fo);
-                        tmem_st16(t_o + c, o);
+                            for (int i = 0; i < 16; i++) o[i] = __float_as_uint(__uint_as_float(o[i]) * fo);
+                            tmem_st16(t_o + c, o);
+                        }
                     }
                 }
-                const float weight = ex2(fminf(mb - (b == -INFINITY ? 0.f : b), 100.f)) * kTopWeight * vs;
-                const unsigned long long f2 = pair2(f, f), w2 = pair2(weight, weight), nb = pair2(-mb, -mb);
+                // (x + lv is at most b + kLazy8, unless nothing is seen and the weights are zero whatever this is)
+                const float weight = ex2(fminf(xb - (b == -INFINITY ? 0.f : b) + lv, kLazy8 + 1.f)) * kTopWeight * vs;
+                const unsigned long long f2 = pair2(f, f), w2 = pair2(weight, weight), nb = pair2(-xb, -xb);
                 unsigned long long part = 0ull;
-                uint32_t hi[4], lo[4];
+                uint32_t w_own[4][2];  // of a piece: the codes of the eight keys
 #pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    float y[4];
+                for (int i = 0; i < 2; i++) {
+                    unsigned long long y[2];
 #pragma unroll
-                    for (int v = 0; v < 4; v += 2) {
+                    for (int v = 0; v < 2; v++) {
                         float e0, e1;
-                        unpair2(fma2(pair2(s[4 * i + v], s[4 * i + v + 1]), f2, nb), e0, e1);
+                        unpair2(fma2(pair2(s[4 * i + 2 * v], s[4 * i + 2 * v + 1]), f2, nb), e0, e1);
                         const unsigned long long e = pair2(ex2(e0), ex2(e1));
                         part = add2(part, e);
-                        unpair2(mul2(e, w2), y[v], y[v + 1]);
+                        y[v] = mul2(e, w2);
                     }
-                    split4(y, hi[i], lo[i]);
+                    uint32_t word[4];
+                    split4(y[0], y[1], word);
+#pragma unroll
+                    for (int u2 = 0; u2 < 4; u2++) w_own[u2][i] = word[u2];
                 }
                 float e0, e1;
                 unpair2(part, e0, e1);
-                sum += e0 + e1;
-                // a row's first lane stores hi of all 32 keys, its second lo
+                sum = fmaf(e0 + e1, ex2(x - mb), sum * ex2(m - mb));
+                m = m_new;
+                // lane 8 p + i stores piece p of all 32 keys of row i: first pieces 2 b1 and 2 b1 + 1 of this lane's eight
+                // keys and of those of the lane 16 further, then its own piece of all four
+                uint32_t two[2][2][2];  // [keys' upper bit][piece's lower bit][word]
+#pragma unroll
+                for (int v = 0; v < 2; v++)
+#pragma unroll
+                    for (int i = 0; i < 2; i++) {
+                        const uint32_t own = b1 ? w_own[2 + v][i] : w_own[v][i];
+                        const uint32_t got = __shfl_xor_sync(kFull, b1 ? w_own[v][i] : w_own[2 + v][i], 16);
+                        two[0][v][i] = b1 ? got : own;
+                        two[1][v][i] = b1 ? own : got;
+                    }
                 uint32_t out[8];
 #pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    const uint32_t got = __shfl_xor_sync(kFull, low ? hi[i] : lo[i], 16);
-                    out[i] = low ? got : hi[i];
-                    out[4 + i] = low ? lo[i] : got;
-                }
+                for (int v = 0; v < 2; v++)
+#pragma unroll
+                    for (int i = 0; i < 2; i++) {
+                        const uint32_t own = b0 ? two[v][1][i] : two[v][0][i];
+                        const uint32_t got = __shfl_xor_sync(kFull, b0 ? two[v][0][i] : two[v][1][i], 8);
+                        out[4 * v + i] = b0 ? got : own;
+                        out[4 * v + 2 + i] = b0 ? own : got;
+                    }
                 const uint32_t zero[8] = {};
 #pragma unroll
                 for (int c = 1; c < C::kParts; c++) tmem_st8(t_s + 32 * ((wq + c) % C::kParts), zero);
@@ -555,10 +604,10 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
         }
     } else {
         // ------------------------------------------------------- ends of parts
-        const int wq = warp - C::kWarpOut, row = lane & 15, otid = tid - 32 * C::kWarpOut;
-        const bool low = lane >= 16, active = wq < C::kParts;
+        const int wq = warp - C::kWarpOut, row = lane & 7, piece = lane >> 3, otid = tid - 32 * C::kWarpOut;
+        const bool b1 = lane & 16, b0 = lane & 8, active = wq < C::kParts;
         const uint32_t lanes = (uint32_t)(32 * wq) << 16;
-        const float c_own = low ? 0.0625f : 1.f;
+        const float c_own = piece_weight(piece);
         const int D = a.head_dim;
         at.enter(0);
         while (!named_bar_or(2, 128, at.lost)) {
@@ -579,16 +628,20 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
             }
             float top = -INFINITY, l = 0.f;
 #pragma unroll
-            for (int i = 0; i < C::kParts; i++) top = max3(top, stat_m[ob][i][row], stat_m[ob][i][row + 16]);
+            for (int i = 0; i < C::kParts; i++)
+#pragma unroll
+                for (int n = row; n < 32; n += 16) top = max3(top, stat_m[ob][i][n], stat_m[ob][i][n + 8]);
             const float base = top == -INFINITY ? 0.f : top;
 #pragma unroll
             for (int i = 0; i < C::kParts; i++)
-                l += stat_l[ob][i][row] * ex2(stat_m[ob][i][row] - base) + stat_l[ob][i][row + 16] * ex2(stat_m[ob][i][row + 16] - base);
+#pragma unroll
+                for (int n = row; n < 32; n += 8) l = fmaf(stat_l[ob][i][n], ex2(stat_m[ob][i][n] - base), l);
             const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
             // from this copy's base (a power of two that may be far from the row's maximum: in two steps) to the row's
             // (nothing seen: zeros; scores that are all NaN: O, which is NaN)
-            const float b = stat_b[ob][wq][lane], both = stat_l[ob][wq][row] + stat_l[ob][wq][row + 16];
-            const bool none = !active || (b == -INFINITY && both == both);
+            const float b = stat_b[ob][wq][lane], all = stat_l[ob][wq][row] + stat_l[ob][wq][row + 8] + stat_l[ob][wq][row + 16] +
+                        stat_l[ob][wq][row + 24];
+            const bool none = !active || (b == -INFINITY && all == all);
             const float e = b == -INFINITY ? 0.f : b - base, half = 0.5f * e;
             const float f1 = ex2(half) * c_own * inv / kTopWeight, f2 = ex2(e - half);
 #pragma unroll 1
@@ -599,14 +652,23 @@ __global__ void __launch_bounds__(Few<DP>::kWarps * 32, 1)
                         uint32_t o[32];
                         tmem_ld32(t_o + c + x, o);
                         tmem_ld_wait();
-                        float* dst = stage + (wq * ROWS + row) * C::kPitch + x + (low ? 16 : 0);
+                        // a row's four pieces added up, eight elements a lane
+                        float h[16], y[8];
 #pragma unroll
                         for (int i = 0; i < 16; i++) {
                             const float u = none ? 0.f : __uint_as_float(o[i]) * f1 * f2;
                             const float v = none ? 0.f : __uint_as_float(o[16 + i]) * f1 * f2;
-                            const float got = __shfl_xor_sync(kFull, low ? u : v, 16);
-                            dst[i] = (low ? v : u) + got;
+                            const float got = __shfl_xor_sync(kFull, b1 ? u : v, 16);
+                            h[i] = (b1 ? v : u) + got;
                         }
+#pragma unroll
+                        for (int i = 0; i < 8; i++) {
+                            const float got = __shfl_xor_sync(kFull, b0 ? h[i] : h[8 + i], 8);
+                            y[i] = (b0 ? h[8 + i] : h[i]) + got;
+                        }
+                        float* dst = stage + (wq * ROWS + row) * C::kPitch + x + 8 * piece;
+                        reinterpret_cast<float4*>(dst)[0] = make_float4(y[0], y[1], y[2], y[3]);
+                        reinterpret_cast<float4*>(dst)[1] = make_float4(y[4], y[5], y[6], y[7]);
                     }
                 }
                 if (c + 128 >= D) {  // O and the statistics have been read
