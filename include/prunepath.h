@@ -478,7 +478,9 @@ pp_status pp_kv_commit(const pp_cache *cache, const pp_batch *batch, int n_layer
    starts at offset i block is scale[(p n_kv_heads + h) (page_size / block) + i].
    The scales that pp_kvq_append and pp_kvq_commit write are powers of two, at
    least 2^-60; others (a cache filled elsewhere) may be any positive normal
-   number.  What is not finite is held as the NaN code. */
+   number up to 2^119.  What is not finite is held as the NaN code; what is
+   finite stays so (at the scale 2^120 magnitudes from 248 * 2^120 on become
+   240 * 2^120, since the code 256 would be 2^128). */
 typedef struct pp_cache8 {
     int dtype;        /* pp_dtype of q, k, v, out (the tensors, not the pages) */
     int n_heads, n_kv_heads, head_dim, page_size, n_pages;

@@ -82,16 +82,17 @@ PP_DEVINL void store_codes(char* p, const F2 (&f)[V / 2], float inv) {
     else
         *reinterpret_cast<uint16_t*>(p) = (uint16_t)w[0];
 }
-// V codes at p rounded again at another scale.
+// V codes at p rounded again at the scale `now`.
 template <int V>
-PP_DEVINL void again(char* p, float ratio) {
+PP_DEVINL void again(char* p, float ratio, float now) {
+    const float top = top_code(now);
     F2 f[V / 2];
 #pragma unroll
     for (int i = 0; i < V; i += 2) {
         const float2 v = from_codes(*reinterpret_cast<const uint16_t*>(p + i));
-        f[i / 2] = pair2(v.x, v.y);
+        f[i / 2] = pair2(within(v.x * ratio, top), within(v.y * ratio, top));
     }
-    store_codes<V>(p, f, ratio);
+    store_codes<V>(p, f, 1.f);
 }
 
 template <typename T, int V, bool HALF, int UPL, int ITER, int WARPS>
@@ -331,12 +332,27 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 2 : 1) append8_kernel
             for (int e = first; e < min(s.ctx, s.lo + strip * R + R); e += per, row += per * a.cache.token_stride) {
 #pragma unroll
                 for (int k = 0; k < UPL; k++) {
-                    if (lane.va[k] >= 0) again<V>(row + lane.va[k] * V, old / now);
-                    if (lane.vb[k] >= 0) again<V>(row + lane.vb[k] * V, old / now);
+                    if (lane.va[k] >= 0) again<V>(row + lane.va[k] * V, old / now, now);
+                    if (lane.vb[k] >= 0) again<V>(row + lane.vb[k] * V, old / now, now);
                 }
             }
         }
         const float inv = 1.0f / now;
+        if (now >= kLargeScale) {  // what is finite stays so
+            const float top = top_code(now) * now;
+#pragma unroll
+            for (int n = 0; n < ITER; n++)
+#pragma unroll
+                for (int k = 0; k < UPL; k++)
+#pragma unroll
+                    for (int v = 0; v < 2; v++)
+#pragma unroll
+                        for (int i = 0; i < V / 2; i++) {
+                            float x, y;
+                            unpair2(f[n][k][v][i], x, y);
+                            f[n][k][v][i] = pair2(within(x, top), within(y, top));
+                        }
+        }
 #pragma unroll
         for (int n = 0; n < ITER; n++, dst += per * a.cache.token_stride) {
             if (!(rows >> n & 1u)) continue;
@@ -544,7 +560,8 @@ PP_DEVINL float largest_of(const uint4& w, float scale) {
 }
 // 16 codes rounded again at another scale.  The usual ratio, a power of two that
 // fp16 holds, goes in fp16: code * ratio is exact there (a code has four bits,
-// the least 2^-9; results are at most 448).
+// the least 2^-9; results are at most 448).  Numbers stay finite: at powers of two
+// a value stays what it is or becomes less.
 PP_DEVINL uint4 recode(const uint4& w, float ratio) {
     if (ratio == 1.f) return w;
     const uint32_t x[4] = {w.x, w.y, w.z, w.w};

@@ -41,6 +41,17 @@ PP_DEVINL float scale_for(float amax) {
     return __uint_as_float((uint32_t)(max(e, kLeastExponent) + 127) << 23);
 }
 
+// The largest code whose value at this scale is a finite number: 448 below
+// scales of 2^119, 240 at 2^120, where 256 would be 2^128.
+constexpr float kLargeScale = 0x1p119f;
+PP_DEVINL float top_code(float scale) {
+    if (scale < kLargeScale) return kTopCode;
+    // the quotient rounded down, to the four significant bits of a code
+    return fminf(__uint_as_float(__float_as_uint(__fdiv_rd(3.402823466e38f, scale)) & 0xfff00000u), kTopCode);
+}
+// x within [-top, top] (NaN stays).
+PP_DEVINL float within(float x, float top) { return fabsf(x) > top ? copysignf(top, x) : x; }
+
 // Scale of a block whose entries to be written reach amax; `old` is that of
 // entries that stay (`stays`).
 PP_DEVINL float block_scale(float amax, float old, bool stays) {
