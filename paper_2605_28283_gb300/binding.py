@@ -342,6 +342,8 @@ def _torch_dtype(dtype) -> int:
 def _rows(t, n_tokens, n_heads, head_dim, dtype, what):
     """Pointer and token stride of a token tensor [n_tokens, heads, head_dim] (or [n_tokens, heads * head_dim])
     whose tokens are each contiguous."""
+    if t is None:
+        raise PPError(PP_ERR_INVALID_ARG, what + " is missing")
     shape = t.shape
     if t.dtype == dtype and shape == (n_tokens, n_heads, head_dim) and t.is_contiguous():
         return t.data_ptr(), n_heads * head_dim
@@ -356,6 +358,8 @@ def _rows(t, n_tokens, n_heads, head_dim, dtype, what):
 
 
 def _int32(t, what):
+    if t is None:
+        raise PPError(PP_ERR_INVALID_ARG, what + " is missing")
     if t.dtype is not _INT32:
         raise PPError(PP_ERR_DTYPE, what + " must be int32")
     if not t.is_contiguous():
@@ -516,12 +520,23 @@ def pp_rope(rot, positions, x, y, inverse=False, stream=None):
                           1 if inverse else 0, _stream_handle(stream)), "pp_rope")
 
 
-def _heads_of(q, k, what):
-    """(tokens, query heads, key heads, head_dim, dtype) of q [T, heads, head_dim] and k [T, kv_heads, head_dim] or None."""
+def _ws_of(ws, what):
+    """(pointer, bytes) of a workspace."""
+    if ws is None:
+        raise PPError(PP_ERR_WORKSPACE, what + ": ws is missing")
+    return ws.data_ptr(), ws.nbytes
+
+
+def _heads_of(norm, q, k, what):
+    """(tokens, query heads, key heads, head_dim, dtype) of q [T, heads, head_dim] and k [T, kv_heads, head_dim] or None,
+    which norm has to fit."""
+    if norm is None or q is None:
+        raise PPError(PP_ERR_INVALID_ARG, what + (": norm" if norm is None else ": q") + " is missing")
     shape = q.shape
     if len(shape) != 3:
         raise PPError(PP_ERR_SHAPE, what)
     T, H, D = shape
+    norm.check(q.dtype, D, what)
     if k is None:
         return T, H, 0, D, q.dtype
     if k.dim() != 3:
@@ -543,8 +558,7 @@ def pp_head_norm_rope(norm, rot, positions, q, k, q_out, k_out, stream=None):
     """q_out, k_out = q, k [T, heads, head_dim] normed and rotated by positions [T] (rot None: normed only; k None: no
     keys).  An output may be its input."""
     what = "pp_head_norm_rope"
-    T, H, Hkv, D, dt = _heads_of(q, k, what)
-    norm.check(dt, D, what)
+    T, H, Hkv, D, dt = _heads_of(norm, q, k, what)
     pq, sq = _rows(q, T, H, D, dt, "pp_head_norm_rope: q")
     po, so = _rows(q_out, T, H, D, dt, "pp_head_norm_rope: q_out")
     pk, sk, pko, sko = None, 0, None, 0
@@ -581,8 +595,7 @@ def pp_head_norm_rope_grad(norm, rot, positions, q, k, q_grad, k_grad, dq, dk, d
     """dq, dk: gradients of q, k from the gradients q_grad, k_grad of pp_head_norm_rope's outputs; dq_gamma, dk_gamma
     [head_dim] float32 (each may be None; ws too where both are): gradients of the weights.  dq may be q_grad."""
     what = "pp_head_norm_rope_grad"
-    T, H, Hkv, D, dt = _heads_of(q, k, what)
-    norm.check(dt, D, what)
+    T, H, Hkv, D, dt = _heads_of(norm, q, k, what)
     pq, sq = _rows(q, T, H, D, dt, what + ": q")
     pg, sg = _rows(q_grad, T, H, D, dt, what + ": q_grad")
     po, so = _rows(dq, T, H, D, dt, what + ": dq")
@@ -687,7 +700,7 @@ def pp_kvq_append(cache, batch, norm, rot, positions, q, k, v, q_out, ws, stream
             raise PPError(PP_ERR_SHAPE, "pp_kvq_append: positions")
         pos = _int32(positions, "positions")
     _check(load().pp_kvq_append(cache.ref, batch.ref, None if norm is None else norm.ref, None if rot is None else rot.ref,
-                                pos, pq, sq, pk, sk, pv, sv, po, so, ws.data_ptr(), ws.nbytes, _stream_handle(stream)),
+                                pos, pq, sq, pk, sk, pv, sv, po, so, *_ws_of(ws, "pp_kvq_append"), _stream_handle(stream)),
            "pp_kvq_append")
 
 
@@ -696,7 +709,7 @@ def pp_kvq_read(cache, batch, k_out, v_out, ws, stream=None):
     T, D, dt = batch.n_tokens, cache.head_dim, cache.dtype
     pk, sk = _rows(k_out, T, cache.n_kv_heads, D, dt, "pp_kvq_read: k_out")
     pv, sv = _rows(v_out, T, cache.n_kv_heads, D, dt, "pp_kvq_read: v_out")
-    _check(load().pp_kvq_read(cache.ref, batch.ref, pk, sk, pv, sv, ws.data_ptr(), ws.nbytes, _stream_handle(stream)),
+    _check(load().pp_kvq_read(cache.ref, batch.ref, pk, sk, pv, sv, *_ws_of(ws, "pp_kvq_read"), _stream_handle(stream)),
            "pp_kvq_read")
 
 
@@ -710,7 +723,7 @@ def pp_kvq_tree_attention(cache, batch, q, mask, scale, out, ws, stream=None):
         if mask.dim() != 2 or mask.shape[0] != T:
             raise PPError(PP_ERR_SHAPE, "pp_kvq_tree_attention: mask")
         pm, words = _int32(mask, "mask"), mask.shape[1]
-    _check(load().pp_kvq_tree_attention(cache.ref, batch.ref, pq, sq, pm, words, scale, po, so, ws.data_ptr(), ws.nbytes,
+    _check(load().pp_kvq_tree_attention(cache.ref, batch.ref, pq, sq, pm, words, scale, po, so, *_ws_of(ws, "pp_kvq_tree_attention"),
                                      _stream_handle(stream)), "pp_kvq_tree_attention")
 
 
@@ -719,12 +732,14 @@ def pp_kvq_commit(cache, batch, path, n_accept, ws, new_len=None, n_layers=1, la
     """Move the accepted path [n_seqs, max_path] of each tree behind its context, in every layer's 8-bit cache
     (layer_stride, scale_layer_stride: elements from one layer's codes and scales to the next one's)."""
     n = batch.n_seqs
+    if path is None or n_accept is None:
+        raise PPError(PP_ERR_INVALID_ARG, "pp_kvq_commit: path or n_accept is missing")
     if path.dim() != 2 or path.shape[0] != n or n_accept.numel() != n or \
             (new_len is not None and new_len.numel() != n):
         raise PPError(PP_ERR_SHAPE, "pp_kvq_commit")
     _check(load().pp_kvq_commit(cache.ref, batch.ref, n_layers, layer_stride, scale_layer_stride, _int32(path, "path"),
                                 path.shape[1], _int32(n_accept, "n_accept"),
-                                None if new_len is None else _int32(new_len, "new_len"), ws.data_ptr(), ws.nbytes,
+                                None if new_len is None else _int32(new_len, "new_len"), *_ws_of(ws, "pp_kvq_commit"),
                                 _stream_handle(stream)), "pp_kvq_commit")
 
 
