@@ -367,6 +367,26 @@ def _int32(t, what):
     return t.data_ptr()
 
 
+def _device_of(what, *tensors):
+    """Device number of a handle's tensors (-1: CPU; None: no tensor), which have to be on one device."""
+    devices = {(t.device.type, t.get_device()) for t in tensors if t is not None}
+    if len(devices) > 1:
+        raise PPError(PP_ERR_INVALID_ARG, what + ": tensors of several devices")
+    return devices.pop()[1] if devices else None
+
+
+def _on_device(what, device, handles, tensors):
+    """What a call passes on lies on one CUDA device, its first tensor's."""
+    for h in handles:
+        if h is not None and h.device is not None and h.device != device:
+            raise PPError(PP_ERR_INVALID_ARG, what + ": tensors of several devices")
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise PPError(PP_ERR_INVALID_ARG, what + ": tensors of several devices")
+    if device < 0:
+        raise PPError(PP_ERR_INVALID_ARG, what + ": tensors must be on a CUDA device")
+
+
 def _stream_handle(stream) -> int:
     if stream is None:
         return _current_stream()
@@ -382,6 +402,7 @@ class Rotation:
         if inv_freq.dtype != torch.float32 or not inv_freq.is_contiguous():
             raise PPError(PP_ERR_DTYPE, "inv_freq must be contiguous float32")
         self.inv_freq = inv_freq
+        self.device = inv_freq.get_device()
         self.c = pp_rotation(2 * inv_freq.numel(), ROPE_LAYOUTS.get(layout, layout), float(scale),
                              inv_freq.data_ptr())
         self.ref = ctypes.byref(self.c)
@@ -406,6 +427,7 @@ class HeadNorm:
             if g is not None:
                 _torch_dtype(g.dtype)
         self.q_gamma, self.k_gamma = q_gamma, k_gamma
+        self.device = _device_of("HeadNorm", q_gamma, k_gamma)
         self.c = pp_head_norm(float(eps), None if q_gamma is None else q_gamma.data_ptr(),
                               None if k_gamma is None else k_gamma.data_ptr())
         self.ref = ctypes.byref(self.c)
@@ -464,6 +486,7 @@ class KVCache8:
         if k_scale.shape != v_scale.shape or k_scale.shape != (n_pages, kv_heads, blocks) or blocks < 1 or page % blocks:
             raise PPError(PP_ERR_SHAPE, "KVCache8: scales are [n_pages, n_kv_heads, page_size / block]")
         self.k, self.v, self.k_scale, self.v_scale, self.block = k, v, k_scale, v_scale, page // blocks
+        self.device = _device_of("KVCache8", k, v, k_scale, v_scale)
         self.c = pp_cache8(_torch_dtype(dtype), int(n_heads), kv_heads, dim, page, n_pages, self.block, k.stride(0), k.stride(1),
                            k.stride(2), k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
         self.ref = ctypes.byref(self.c)
@@ -492,6 +515,9 @@ class Batch:
         self.c = pp_batch(n, int(n_tokens), pages.shape[1], _int32(q_start, "q_start"), _int32(ctx_len, "ctx_len"),
                           _int32(pages, "pages"))
         self.ref, self.n_tokens, self.n_seqs = ctypes.byref(self.c), int(n_tokens), n
+        device = q_start.get_device()
+        # (tensors of several devices: no device, which the calls on an 8-bit cache refuse)
+        self.device = device if ctx_len.get_device() == device == pages.get_device() else -2
 
 
 def pp_rope_frequencies(scaling, rot_dim, base=10000.0, factor=1.0, low=1.0, high=32.0, trained_len=0):
@@ -565,9 +591,10 @@ def pp_head_norm_rope(norm, rot, positions, q, k, q_out, k_out, stream=None):
     if k is not None:
         pk, sk = _rows(k, T, Hkv, D, dt, "pp_head_norm_rope: k")
         pko, sko = _rows(k_out, T, Hkv, D, dt, "pp_head_norm_rope: k_out")
+    pos = _positions_of(rot, positions, T, what)
+    _on_device(what, q.get_device(), (norm, rot), (k, q_out) + (() if k is None else (k_out,)) + (() if rot is None else (positions,)))
     _check(load().pp_head_norm_rope(_torch_dtype(dt), norm.ref, None if rot is None else rot.ref,
-                                    _positions_of(rot, positions, T, what), T, H, Hkv, D, pq, sq, pk, sk, po, so, pko, sko,
-                                    _stream_handle(stream)), what)
+                                    pos, T, H, Hkv, D, pq, sq, pk, sk, po, so, pko, sko, _stream_handle(stream)), what)
 
 
 def pp_head_norm_workspace_size(head_dim) -> int:
@@ -604,10 +631,12 @@ def pp_head_norm_rope_grad(norm, rot, positions, q, k, q_grad, k_grad, dq, dk, d
         pk, sk = _rows(k, T, Hkv, D, dt, what + ": k")
         pkg, skg = _rows(k_grad, T, Hkv, D, dt, what + ": k_grad")
         pko, sko = _rows(dk, T, Hkv, D, dt, what + ": dk")
-    _check(load().pp_head_norm_rope_grad(_torch_dtype(dt), norm.ref, None if rot is None else rot.ref,
-                                         _positions_of(rot, positions, T, what), T, H, Hkv, D, pq, sq, pk, sk, pg, sg, pkg,
-                                         skg, po, so, pko, sko, _gamma_grad(dq_gamma, D, what + ": dq_gamma"),
-                                         _gamma_grad(dk_gamma, D, what + ": dk_gamma"),
+    pos = _positions_of(rot, positions, T, what)
+    gamma_grads = _gamma_grad(dq_gamma, D, what + ": dq_gamma"), _gamma_grad(dk_gamma, D, what + ": dk_gamma")
+    _on_device(what, q.get_device(), (norm, rot), (k, q_grad, dq, dq_gamma, dk_gamma, ws) + (() if k is None else (k_grad, dk)) +
+               (() if rot is None else (positions,)))
+    _check(load().pp_head_norm_rope_grad(_torch_dtype(dt), norm.ref, None if rot is None else rot.ref, pos, T, H, Hkv, D,
+                                         pq, sq, pk, sk, pg, sg, pkg, skg, po, so, pko, sko, *gamma_grads,
                                          None if ws is None else ws.data_ptr(), 0 if ws is None else ws.nbytes,
                                          _stream_handle(stream)), what)
 
@@ -699,8 +728,10 @@ def pp_kvq_append(cache, batch, norm, rot, positions, q, k, v, q_out, ws, stream
         if positions.numel() != T:
             raise PPError(PP_ERR_SHAPE, "pp_kvq_append: positions")
         pos = _int32(positions, "positions")
+    w = _ws_of(ws, "pp_kvq_append")
+    _on_device("pp_kvq_append", cache.device, (batch, norm, rot), (q, k, v, q_out, positions, ws))
     _check(load().pp_kvq_append(cache.ref, batch.ref, None if norm is None else norm.ref, None if rot is None else rot.ref,
-                                pos, pq, sq, pk, sk, pv, sv, po, so, *_ws_of(ws, "pp_kvq_append"), _stream_handle(stream)),
+                                pos, pq, sq, pk, sk, pv, sv, po, so, *w, _stream_handle(stream)),
            "pp_kvq_append")
 
 
@@ -709,7 +740,9 @@ def pp_kvq_read(cache, batch, k_out, v_out, ws, stream=None):
     T, D, dt = batch.n_tokens, cache.head_dim, cache.dtype
     pk, sk = _rows(k_out, T, cache.n_kv_heads, D, dt, "pp_kvq_read: k_out")
     pv, sv = _rows(v_out, T, cache.n_kv_heads, D, dt, "pp_kvq_read: v_out")
-    _check(load().pp_kvq_read(cache.ref, batch.ref, pk, sk, pv, sv, *_ws_of(ws, "pp_kvq_read"), _stream_handle(stream)),
+    w = _ws_of(ws, "pp_kvq_read")
+    _on_device("pp_kvq_read", cache.device, (batch,), (k_out, v_out, ws))
+    _check(load().pp_kvq_read(cache.ref, batch.ref, pk, sk, pv, sv, *w, _stream_handle(stream)),
            "pp_kvq_read")
 
 
@@ -723,8 +756,10 @@ def pp_kvq_tree_attention(cache, batch, q, mask, scale, out, ws, stream=None):
         if mask.dim() != 2 or mask.shape[0] != T:
             raise PPError(PP_ERR_SHAPE, "pp_kvq_tree_attention: mask")
         pm, words = _int32(mask, "mask"), mask.shape[1]
-    _check(load().pp_kvq_tree_attention(cache.ref, batch.ref, pq, sq, pm, words, scale, po, so, *_ws_of(ws, "pp_kvq_tree_attention"),
-                                     _stream_handle(stream)), "pp_kvq_tree_attention")
+    w = _ws_of(ws, "pp_kvq_tree_attention")
+    _on_device("pp_kvq_tree_attention", cache.device, (batch,), (q, mask, out, ws))
+    _check(load().pp_kvq_tree_attention(cache.ref, batch.ref, pq, sq, pm, words, scale, po, so, *w,
+                                        _stream_handle(stream)), "pp_kvq_tree_attention")
 
 
 def pp_kvq_commit(cache, batch, path, n_accept, ws, new_len=None, n_layers=1, layer_stride=0, scale_layer_stride=0,
@@ -737,9 +772,11 @@ def pp_kvq_commit(cache, batch, path, n_accept, ws, new_len=None, n_layers=1, la
     if path.dim() != 2 or path.shape[0] != n or n_accept.numel() != n or \
             (new_len is not None and new_len.numel() != n):
         raise PPError(PP_ERR_SHAPE, "pp_kvq_commit")
+    w = _ws_of(ws, "pp_kvq_commit")
+    _on_device("pp_kvq_commit", cache.device, (batch,), (path, n_accept, new_len, ws))
     _check(load().pp_kvq_commit(cache.ref, batch.ref, n_layers, layer_stride, scale_layer_stride, _int32(path, "path"),
                                 path.shape[1], _int32(n_accept, "n_accept"),
-                                None if new_len is None else _int32(new_len, "new_len"), *_ws_of(ws, "pp_kvq_commit"),
+                                None if new_len is None else _int32(new_len, "new_len"), *w,
                                 _stream_handle(stream)), "pp_kvq_commit")
 
 
