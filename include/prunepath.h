@@ -385,8 +385,9 @@ typedef struct pp_head_norm {
    one pass: q [n_tokens][n_heads][head_dim], k [n_tokens][n_kv_heads][head_dim]
    (n_kv_heads 0: no keys, any n_heads; k, k_out are not looked at).  rot NULL:
    no rotation, and positions are not looked at.  An output may be its own
-   input with the same stride; other overlaps are PP_ERR_INVALID_ARG.
-   Arithmetic in fp32, rounded once at the end. */
+   input with the same stride; other overlaps, with weights, positions and
+   frequencies too, are PP_ERR_INVALID_ARG.  Arithmetic in fp32, rounded once
+   at the end. */
 pp_status pp_head_norm_rope(int dtype, const pp_head_norm *norm, const pp_rotation *rot, const int32_t *positions,
                             int n_tokens, int n_heads, int n_kv_heads, int head_dim, const void *q, int64_t q_stride,
                             const void *k, int64_t k_stride, void *q_out, int64_t q_out_stride, void *k_out,
@@ -396,7 +397,8 @@ pp_status pp_head_norm_rope(int dtype, const pp_head_norm *norm, const pp_rotati
    gradients q_grad, k_grad of its outputs, the gradients dq, dk of q, k and
    (each unless NULL; written, not added to) dq_gamma, dk_gamma [head_dim] fp32
    of the weights, summed in fp32 over all tokens and heads in a fixed order.
-   dq may be q_grad (or q) itself with the same stride, dk likewise.
+   dq may be q_grad (or q) itself with the same stride, dk likewise; other
+   overlaps of what is written, the workspace included, are PP_ERR_INVALID_ARG.
    Workspace: pp_head_norm_workspace_size bytes, 256-byte aligned; it need not
    be initialised, and is not looked at where no weight gradient is asked for. */
 pp_status pp_head_norm_rope_grad(int dtype, const pp_head_norm *norm, const pp_rotation *rot, const int32_t *positions,

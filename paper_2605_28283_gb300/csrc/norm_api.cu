@@ -18,6 +18,23 @@ bool clash(const Rows& out, const Rows& x, int T, bool may_be) {
     return rows_overlap(out.p, out.row, out.stride, x.p, x.row, x.stride, T);
 }
 
+// Whether T rows share memory with `n` bytes at p (NULL: no).
+bool touches(const Rows& r, int T, const void* p, int64_t n) {
+    if (!p || T < 1) return false;
+    const __int128 at = (__int128)(uintptr_t)p - (__int128)(uintptr_t)r.p;
+    const __int128 i = at < 0 ? 0 : at / r.stride;  // the row that p lies in or behind, or the first one
+    for (__int128 k = i; k < i + 2 && k < T; k++)
+        if (at < k * r.stride + r.row && at + n > k * r.stride) return true;
+    return false;
+}
+
+// Whether an output lies on the weights, the positions or the frequencies.
+bool on_parameters(const Rows& out, int T, const pp_head_norm& norm, const pp_rotation* rot, const int32_t* positions,
+                   int tokens, int64_t weight_bytes) {
+    if (touches(out, T, norm.q_gamma, weight_bytes) || touches(out, T, norm.k_gamma, weight_bytes)) return true;
+    return rot && (touches(out, T, positions, 4ll * tokens) || touches(out, T, rot->inv_freq, 2ll * rot->rot_dim));
+}
+
 pp_status check_call(int dtype, const pp_head_norm* norm, const pp_rotation* rot, const int32_t* positions, int T, int H,
                      int Hkv, int D) {
     PP_TRY(check_heads(dtype, H, D));
@@ -80,6 +97,8 @@ pp_status pp_head_norm_rope(int dtype, const pp_head_norm* norm, const pp_rotati
     for (int o = 0; o < 1 + keys; o++)
         for (int i = 0; i < 1 + keys; i++)
             if (clash(out[o], in[i], T, o == i) || (i != o && clash(out[o], out[i], T, false))) return PP_ERR_INVALID_ARG;
+    for (int o = 0; o < 1 + keys; o++)
+        if (on_parameters(out[o], T, *norm, rot, positions, T, (int64_t)head_dim * e)) return PP_ERR_INVALID_ARG;
     int sms = 0;
     PP_TRY(device_sms(&sms));
     if (T == 0) return PP_OK;
@@ -122,9 +141,12 @@ pp_status pp_head_norm_rope_grad(int dtype, const pp_head_norm* norm, const pp_r
         for (int i = 0; i < 2 + 2 * keys; i++)
             if (clash(out[o], in[i], T, i / 2 == o)) return PP_ERR_INVALID_ARG;
     if (keys && clash(out[0], out[1], T, false)) return PP_ERR_INVALID_ARG;
+    for (int o = 0; o < 1 + keys; o++)
+        if (on_parameters(out[o], T, *norm, rot, positions, T, (int64_t)head_dim * e)) return PP_ERR_INVALID_ARG;
     const float* dg[2] = {dq_gamma, dk_gamma};
     for (int g = 0; g < 2; g++) {
         if (!dg[g]) continue;
+        if (on_parameters({dg[g], lg, lg}, 1, *norm, rot, positions, T, (int64_t)head_dim * e)) return PP_ERR_INVALID_ARG;
         auto over = [&](const Rows& r) { // the rows' whole span
             return r.p && T > 0 && rows_overlap(dg[g], lg, lg, r.p, (int64_t)(T - 1) * r.stride + r.row, r.stride, 1);
         };
@@ -132,13 +154,19 @@ pp_status pp_head_norm_rope_grad(int dtype, const pp_head_norm* norm, const pp_r
             if (over(in[i])) return PP_ERR_INVALID_ARG;
         for (int o = 0; o < 1 + keys; o++)
             if (over(out[o])) return PP_ERR_INVALID_ARG;
-        const void* gm[2] = {norm->q_gamma, norm->k_gamma};
-        for (const void* p : gm)
-            if (p && rows_overlap(dg[g], lg, lg, p, (int64_t)head_dim * e, lg, 1)) return PP_ERR_INVALID_ARG;
         if (ws && rows_overlap(dg[g], lg, lg, ws, (int64_t)norm_ws_bytes(head_dim), lg, 1)) return PP_ERR_INVALID_ARG;
     }
     if (dq_gamma && dk_gamma && rows_overlap(dq_gamma, lg, lg, dk_gamma, lg, lg, 1)) return PP_ERR_INVALID_ARG;
-    if ((dq_gamma || dk_gamma) && (!ws || !aligned(ws, 256) || ws_bytes < norm_ws_bytes(head_dim))) return PP_ERR_WORKSPACE;
+    if (dq_gamma || dk_gamma) {
+        const int64_t n = (int64_t)norm_ws_bytes(head_dim);
+        if (!ws || !aligned(ws, 256) || ws_bytes < (size_t)n) return PP_ERR_WORKSPACE;
+        // written while the others are still read
+        for (int i = 0; i < 2 + 2 * keys; i++)
+            if (touches(in[i], T, ws, n)) return PP_ERR_INVALID_ARG;
+        for (int o = 0; o < 1 + keys; o++)
+            if (touches(out[o], T, ws, n)) return PP_ERR_INVALID_ARG;
+        if (on_parameters({ws, n, n}, 1, *norm, rot, positions, T, (int64_t)head_dim * e)) return PP_ERR_INVALID_ARG;
+    }
     int sms = 0;
     PP_TRY(device_sms(&sms));
     NormArgs a = norm_args(norm, rot, positions, T, n_heads, n_kv_heads, head_dim);
