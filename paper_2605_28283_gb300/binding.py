@@ -339,13 +339,14 @@ def _torch_dtype(dtype) -> int:
     return d
 
 
-def _rows(t, n_tokens, n_heads, head_dim, dtype, what):
+def _rows(t, n_tokens, n_heads, head_dim, dtype, what, shape=None):
     """Pointer and token stride of a token tensor [n_tokens, heads, head_dim] (or [n_tokens, heads * head_dim])
-    whose tokens are each contiguous."""
+    whose tokens are each contiguous.  shape: the tensor's, where it is at hand."""
     if t is None:
         raise PPError(PP_ERR_INVALID_ARG, what + " is missing")
-    shape = t.shape
-    if t.dtype == dtype and shape == (n_tokens, n_heads, head_dim) and t.is_contiguous():
+    if shape is None:
+        shape = t.shape
+    if t.dtype is dtype and shape == (n_tokens, n_heads, head_dim) and t.is_contiguous():
         return t.data_ptr(), n_heads * head_dim
     stride = t.stride()
     if t.dtype != dtype:
@@ -375,16 +376,18 @@ def _device_of(what, *tensors):
     return devices.pop()[1] if devices else None
 
 
-def _on_device(what, device, handles, tensors):
-    """What a call passes on lies on one CUDA device, its first tensor's."""
+# What a call passes on has to lie on one CUDA device.  The calls compare device numbers themselves, spelled out: a loop
+# over the tensors costs a small call a tenth of its time.
+def _devices(what, device):
+    raise PPError(PP_ERR_INVALID_ARG, what + (": tensors must be on a CUDA device" if device < 0 else ": tensors of several devices"))
+
+
+def _handle_off(device, *handles):
+    """Whether a handle (or None) has tensors on another device."""
     for h in handles:
-        if h is not None and h.device is not None and h.device != device:
-            raise PPError(PP_ERR_INVALID_ARG, what + ": tensors of several devices")
-    for t in tensors:
-        if t is not None and t.get_device() != device:
-            raise PPError(PP_ERR_INVALID_ARG, what + ": tensors of several devices")
-    if device < 0:
-        raise PPError(PP_ERR_INVALID_ARG, what + ": tensors must be on a CUDA device")
+        if h is not None and h.device != device and h.device is not None:
+            return True
+    return False
 
 
 def _stream_handle(stream) -> int:
@@ -431,10 +434,14 @@ class HeadNorm:
         self.c = pp_head_norm(float(eps), None if q_gamma is None else q_gamma.data_ptr(),
                               None if k_gamma is None else k_gamma.data_ptr())
         self.ref = ctypes.byref(self.c)
-        # (dtype, head_dim) of each weight vector, for the calls to compare with
+        # (dtype, head_dim) of each weight vector, for the calls to compare with; one pair where there is no other
         self.kinds = [(g.dtype, g.shape[0]) for g in (q_gamma, k_gamma) if g is not None]
 
+        self.kind = self.kinds[0] if self.kinds and self.kinds[0] == self.kinds[-1] else (None, None)
+
     def check(self, dtype, head_dim, what):
+        if self.kind[0] is dtype and self.kind[1] == head_dim:
+            return
         for kind, dim in self.kinds:
             if kind != dtype:
                 raise PPError(PP_ERR_DTYPE, what + ": weights of another type")
@@ -554,8 +561,8 @@ def _ws_of(ws, what):
 
 
 def _heads_of(norm, q, k, what):
-    """(tokens, query heads, key heads, head_dim, dtype) of q [T, heads, head_dim] and k [T, kv_heads, head_dim] or None,
-    which norm has to fit."""
+    """(tokens, query heads, key heads, head_dim, dtype, both shapes) of q [T, heads, head_dim] and k [T, kv_heads,
+    head_dim] or None, which norm has to fit."""
     if norm is None or q is None:
         raise PPError(PP_ERR_INVALID_ARG, what + (": norm" if norm is None else ": q") + " is missing")
     shape = q.shape
@@ -564,10 +571,11 @@ def _heads_of(norm, q, k, what):
     T, H, D = shape
     norm.check(q.dtype, D, what)
     if k is None:
-        return T, H, 0, D, q.dtype
-    if k.dim() != 3:
+        return T, H, 0, D, q.dtype, shape, None
+    k_shape = k.shape
+    if len(k_shape) != 3:
         raise PPError(PP_ERR_SHAPE, what)
-    return T, H, k.shape[1], D, q.dtype  # (_rows compares the rest of k's shape)
+    return T, H, k_shape[1], D, q.dtype, shape, k_shape  # (_rows compares the rest of k's shape)
 
 
 def _positions_of(rot, positions, T, what):
@@ -584,15 +592,18 @@ def pp_head_norm_rope(norm, rot, positions, q, k, q_out, k_out, stream=None):
     """q_out, k_out = q, k [T, heads, head_dim] normed and rotated by positions [T] (rot None: normed only; k None: no
     keys).  An output may be its input."""
     what = "pp_head_norm_rope"
-    T, H, Hkv, D, dt = _heads_of(norm, q, k, what)
-    pq, sq = _rows(q, T, H, D, dt, "pp_head_norm_rope: q")
+    T, H, Hkv, D, dt, q_shape, k_shape = _heads_of(norm, q, k, what)
+    pq, sq = _rows(q, T, H, D, dt, "pp_head_norm_rope: q", q_shape)
     po, so = _rows(q_out, T, H, D, dt, "pp_head_norm_rope: q_out")
     pk, sk, pko, sko = None, 0, None, 0
     if k is not None:
-        pk, sk = _rows(k, T, Hkv, D, dt, "pp_head_norm_rope: k")
+        pk, sk = _rows(k, T, Hkv, D, dt, "pp_head_norm_rope: k", k_shape)
         pko, sko = _rows(k_out, T, Hkv, D, dt, "pp_head_norm_rope: k_out")
     pos = _positions_of(rot, positions, T, what)
-    _on_device(what, q.get_device(), (norm, rot), (k, q_out) + (() if k is None else (k_out,)) + (() if rot is None else (positions,)))
+    d = q.get_device()
+    if d < 0 or q_out.get_device() != d or (k is not None and (k.get_device() != d or k_out.get_device() != d)) or \
+            (rot is not None and (rot.device != d or positions.get_device() != d)) or _handle_off(d, norm):
+        _devices(what, d)
     _check(load().pp_head_norm_rope(_torch_dtype(dt), norm.ref, None if rot is None else rot.ref,
                                     pos, T, H, Hkv, D, pq, sq, pk, sk, po, so, pko, sko, _stream_handle(stream)), what)
 
@@ -622,19 +633,22 @@ def pp_head_norm_rope_grad(norm, rot, positions, q, k, q_grad, k_grad, dq, dk, d
     """dq, dk: gradients of q, k from the gradients q_grad, k_grad of pp_head_norm_rope's outputs; dq_gamma, dk_gamma
     [head_dim] float32 (each may be None; ws too where both are): gradients of the weights.  dq may be q_grad."""
     what = "pp_head_norm_rope_grad"
-    T, H, Hkv, D, dt = _heads_of(norm, q, k, what)
-    pq, sq = _rows(q, T, H, D, dt, what + ": q")
+    T, H, Hkv, D, dt, q_shape, k_shape = _heads_of(norm, q, k, what)
+    pq, sq = _rows(q, T, H, D, dt, what + ": q", q_shape)
     pg, sg = _rows(q_grad, T, H, D, dt, what + ": q_grad")
     po, so = _rows(dq, T, H, D, dt, what + ": dq")
     pk, sk, pkg, skg, pko, sko = None, 0, None, 0, None, 0
     if k is not None:
-        pk, sk = _rows(k, T, Hkv, D, dt, what + ": k")
+        pk, sk = _rows(k, T, Hkv, D, dt, what + ": k", k_shape)
         pkg, skg = _rows(k_grad, T, Hkv, D, dt, what + ": k_grad")
         pko, sko = _rows(dk, T, Hkv, D, dt, what + ": dk")
     pos = _positions_of(rot, positions, T, what)
     gamma_grads = _gamma_grad(dq_gamma, D, what + ": dq_gamma"), _gamma_grad(dk_gamma, D, what + ": dk_gamma")
-    _on_device(what, q.get_device(), (norm, rot), (k, q_grad, dq, dq_gamma, dk_gamma, ws) + (() if k is None else (k_grad, dk)) +
-               (() if rot is None else (positions,)))
+    d = q.get_device()
+    if d < 0 or _handle_off(d, norm, rot) or any(
+            t is not None and t.get_device() != d
+            for t in (k, q_grad, dq, dq_gamma, dk_gamma, ws) + (() if k is None else (k_grad, dk)) + (() if rot is None else (positions,))):
+        _devices(what, d)
     _check(load().pp_head_norm_rope_grad(_torch_dtype(dt), norm.ref, None if rot is None else rot.ref, pos, T, H, Hkv, D,
                                          pq, sq, pk, sk, pg, sg, pkg, skg, po, so, pko, sko, *gamma_grads,
                                          None if ws is None else ws.data_ptr(), 0 if ws is None else ws.nbytes,
@@ -729,7 +743,11 @@ def pp_kvq_append(cache, batch, norm, rot, positions, q, k, v, q_out, ws, stream
             raise PPError(PP_ERR_SHAPE, "pp_kvq_append: positions")
         pos = _int32(positions, "positions")
     w = _ws_of(ws, "pp_kvq_append")
-    _on_device("pp_kvq_append", cache.device, (batch, norm, rot), (q, k, v, q_out, positions, ws))
+    d = cache.device
+    if d < 0 or batch.device != d or k.get_device() != d or v.get_device() != d or ws.get_device() != d or \
+            (q is not None and q.get_device() != d) or (q_out is not None and q_out.get_device() != d) or \
+            (positions is not None and positions.get_device() != d) or _handle_off(d, norm, rot):
+        _devices("pp_kvq_append", d)
     _check(load().pp_kvq_append(cache.ref, batch.ref, None if norm is None else norm.ref, None if rot is None else rot.ref,
                                 pos, pq, sq, pk, sk, pv, sv, po, so, *w, _stream_handle(stream)),
            "pp_kvq_append")
@@ -741,7 +759,9 @@ def pp_kvq_read(cache, batch, k_out, v_out, ws, stream=None):
     pk, sk = _rows(k_out, T, cache.n_kv_heads, D, dt, "pp_kvq_read: k_out")
     pv, sv = _rows(v_out, T, cache.n_kv_heads, D, dt, "pp_kvq_read: v_out")
     w = _ws_of(ws, "pp_kvq_read")
-    _on_device("pp_kvq_read", cache.device, (batch,), (k_out, v_out, ws))
+    d = cache.device
+    if d < 0 or batch.device != d or k_out.get_device() != d or v_out.get_device() != d or ws.get_device() != d:
+        _devices("pp_kvq_read", d)
     _check(load().pp_kvq_read(cache.ref, batch.ref, pk, sk, pv, sv, *w, _stream_handle(stream)),
            "pp_kvq_read")
 
@@ -757,7 +777,10 @@ def pp_kvq_tree_attention(cache, batch, q, mask, scale, out, ws, stream=None):
             raise PPError(PP_ERR_SHAPE, "pp_kvq_tree_attention: mask")
         pm, words = _int32(mask, "mask"), mask.shape[1]
     w = _ws_of(ws, "pp_kvq_tree_attention")
-    _on_device("pp_kvq_tree_attention", cache.device, (batch,), (q, mask, out, ws))
+    d = cache.device
+    if d < 0 or batch.device != d or q.get_device() != d or out.get_device() != d or ws.get_device() != d or \
+            (mask is not None and mask.get_device() != d):
+        _devices("pp_kvq_tree_attention", d)
     _check(load().pp_kvq_tree_attention(cache.ref, batch.ref, pq, sq, pm, words, scale, po, so, *w,
                                         _stream_handle(stream)), "pp_kvq_tree_attention")
 
@@ -773,7 +796,10 @@ def pp_kvq_commit(cache, batch, path, n_accept, ws, new_len=None, n_layers=1, la
             (new_len is not None and new_len.numel() != n):
         raise PPError(PP_ERR_SHAPE, "pp_kvq_commit")
     w = _ws_of(ws, "pp_kvq_commit")
-    _on_device("pp_kvq_commit", cache.device, (batch,), (path, n_accept, new_len, ws))
+    d = cache.device
+    if d < 0 or batch.device != d or path.get_device() != d or n_accept.get_device() != d or ws.get_device() != d or \
+            (new_len is not None and new_len.get_device() != d):
+        _devices("pp_kvq_commit", d)
     _check(load().pp_kvq_commit(cache.ref, batch.ref, n_layers, layer_stride, scale_layer_stride, _int32(path, "path"),
                                 path.shape[1], _int32(n_accept, "n_accept"),
                                 None if new_len is None else _int32(new_len, "new_len"), *w,
