@@ -243,10 +243,8 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 2 : 1) append8_kernel
             fetch(u0 + (a.stages - 1) * units, (turn + a.stages - 1) % a.stages);
             if (a.stages == 1)
                 cp_async_wait<0>();
-            else if (a.stages == 2)
+            else  // two at most
                 cp_async_wait<1>();
-            else
-                cp_async_wait<2>();
         }
         const unsigned char* from = stages + turn * stage_bytes;
         turn = turn + 1 >= a.stages ? 0 : turn + 1;
