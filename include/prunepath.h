@@ -520,8 +520,9 @@ pp_status pp_kvq_read(const pp_cache8 *cache, const pp_batch *batch, void *k_out
 
 /* pp_tree_attention over an 8-bit cache: the same masks, shapes and results,
    with code * scale for the keys and values.  bf16, where sequences bring up
-   to 16 query rows a key head on average: the codes are multiplied as they
-   are, and queries and weights as sums of e4m3 numbers.  That holds a query
+   to 16 query rows a key head on average (where one may bring many, for those
+   with up to 16 alone): the codes are multiplied as they are, and queries and
+   weights as sums of e4m3 numbers; up to three launches.  That holds a query
    element exactly down to 2^-14 of its head's largest, and below to 2^-21 of
    the largest; and a weight, times its block's value scale, to 2^-8 of itself
    (as in bf16) or 2^-41 of the largest such product of its row.  With more

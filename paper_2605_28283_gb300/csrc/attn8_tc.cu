@@ -6,15 +6,28 @@
 namespace pp {
 
 cudaError_t attn8_tc_launch(const AttnArgs& a, int sms, cudaStream_t st) {
-    // Rows a sequence brings to a key head on average, as in attn_tc.cuh.  64 sequences of 64 to 8191 entries, 32 heads on
-    // 8, codes multiplied as they are / made bf16 first: 1 token each (4 rows) 99 / 252 us, 2 (8 rows) 110 / 254, 3 (two
-    // items of 8) 194 / 267, 4 (16 rows) 203 / 268, 5 290 / 270, 8 (32 rows) 394 / 275.  4 sequences of 1000 to 4000: 18 /
-    // 23 at 4 rows, 27 / 28 at 16, 32 / 35 at 32, 40 / 25 at 48.  One key head, 32 rows: 67 / 57.  A prompt beside single
-    // tokens of 64 to 2000 entries, by the mean as well: 440 tokens beside 63 (31 rows) 230 / 127, 1024 beside 255 (20)
-    // 702 / 385, 100 over 2000 entries beside 63 (10) 113 / 98, 50 beside 63 (7) 83 / 94.
-    const long long rows = ((long long)a.batch.n_tokens * a.group + a.batch.n_seqs - 1) / a.batch.n_seqs;
-    if (rows <= 16) return attn8_few_launch(a, sms, st);
-    return launch<true>(a, sms, st);
+    // Rows that a sequence brings to a key head, on average: 64 sequences of 64 to 8191 entries, 32 heads on 8, codes
+    // multiplied as they are / made bf16 first: 1 token each (4 rows) 99 / 252 us, 2 (8 rows) 110 / 254, 3 (two items of 8)
+    // 194 / 267, 4 (16 rows) 203 / 268, 5 290 / 270, 8 (32 rows) 394 / 275.  4 sequences of 1000 to 4000: 18 / 23 at 4 rows,
+    // 27 / 28 at 16, 32 / 35 at 32, 40 / 25 at 48.  One key head, 32 rows: 67 / 57.  Short contexts, where items cost more
+    // than reading: 256 single tokens over 100 entries 77 / 60, 4 tokens each for 40 sequences of 100 to 500 58 / 35.
+    constexpr long long kFew = 16, kLong = 512;
+    const long long mean = mean_rows(a);
+    if (mean > kFew) return launch<true>(a, mean, sms, st);
+    // What the longest sequence brings if every one has a token.  Where that may be much, each kernel takes the sequences
+    // that it is for: a prompt beside single tokens over 64 to 2000 entries, both / codes as they are / bf16 alone: 130
+    // tokens beside 255 199 / 355 / 388 us, 160 beside 127 119 / 200 / 213, 765 beside 255 229 / 612 / 401, 1500 beside 511
+    // 437 / 1205 / 722 (440 beside 63, 31 rows on average and so by bf16 alone: 127).  Two more launches cost 64 sequences
+    // of 3 tokens 8 us of 194.
+    const long long most = ((long long)a.batch.n_tokens - a.batch.n_seqs + 1) * a.group;
+    if (most <= kLong) return attn8_few_launch(a, sms, st);
+    AttnArgs part = a;
+    part.max_rows = kFew;
+    const cudaError_t e = attn8_few_launch(part, sms, st);
+    if (e != cudaSuccess) return e;
+    part.max_rows = a.max_rows;
+    part.min_rows = kFew + 1;
+    return launch<true>(part, most, sms, st);
 }
 
 }  // namespace pp

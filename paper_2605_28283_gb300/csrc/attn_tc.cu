@@ -3,6 +3,6 @@
 
 namespace pp {
 
-cudaError_t attn_tc_launch(const AttnArgs& a, int sms, cudaStream_t st) { return launch<false>(a, sms, st); }
+cudaError_t attn_tc_launch(const AttnArgs& a, int sms, cudaStream_t st) { return launch<false>(a, mean_rows(a), sms, st); }
 
 }  // namespace pp

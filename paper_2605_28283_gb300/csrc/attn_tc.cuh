@@ -1106,18 +1106,22 @@ cudaError_t go(AttnArgs a, bool join_later, int sms, cudaStream_t st) {
     return launch_overlapped(join_kernel<DP, MT>, dim3(grid, (unsigned)(MT * ((a.head_dim + 15) / 16))), dim3(128), 0, st, a);
 }
 
+// Rows a sequence brings to a key head on average (the host knows no lengths;
+// padding tokens and empty sequences count).
+long long mean_rows(const AttnArgs& a) {
+    return ((long long)a.batch.n_tokens * a.group + a.batch.n_seqs - 1) / a.batch.n_seqs;
+}
+
+// rows: about as many a sequence brings to a key head.
 template <bool Q8>
-cudaError_t launch(const AttnArgs& a, int sms, cudaStream_t st) {
-    // Rows a sequence brings to a key head on average (the host knows no
-    // lengths; padding tokens and empty sequences count): two row tiles share
-    // each key tile where one does not hold them.  One / two, 32 heads on 8 of
-    // 128: 8 trees of 32 tokens (128 rows) 35 / 40 us, of 36 (144 rows) 53 / 44,
-    // of 64 58 / 49; 4 prompts of 160 tokens, 40 heads, 31 / 26.  An average
-    // says little of mixed lengths: a prompt of 2048 tokens beside 7 single
-    // tokens over 64 to 8191 entries (1027) 111 / 98, beside 31 (259) 176 / 190,
-    // beside 63 (131) 252 / 301, beside 127 (67) 415 / 518: from 129 to about 300
-    // such a batch is up to a fifth slower than it could be.
-    const long long rows = ((long long)a.batch.n_tokens * a.group + a.batch.n_seqs - 1) / a.batch.n_seqs;
+cudaError_t launch(const AttnArgs& a, long long rows, int sms, cudaStream_t st) {
+    // Two row tiles share each key tile where one does not hold the rows.  One
+    // / two, 32 heads on 8 of 128: 8 trees of 32 tokens (128 rows) 35 / 40 us, of
+    // 36 (144 rows) 53 / 44, of 64 58 / 49; 4 prompts of 160 tokens, 40 heads, 31 /
+    // 26.  An average says little of mixed lengths: a prompt of 2048 tokens beside
+    // 7 single tokens over 64 to 8191 entries (1027) 111 / 98, beside 31 (259) 176
+    // / 190, beside 63 (131) 252 / 301, beside 127 (67) 415 / 518: from 129 to about
+    // 300 such a batch is up to a fifth slower than it could be.
     const bool two = rows > 128;
     // Split items of a few rows are joined by the CTA that finishes last, those of many by a second kernel (8 trees of
     // 8 tokens, 32 rows: 40 us against 41; of 9, 36 rows: 48 against 32; one of 12 over 4000 entries: 56 against 16).

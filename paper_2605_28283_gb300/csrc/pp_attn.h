@@ -130,6 +130,7 @@ struct AttnArgs {
     const uint32_t* mask;
     int mask_words;
     int n_kv_heads, group, head_dim;
+    unsigned min_rows, max_rows;  // query rows a key head of the sequences that this launch takes
     int head_shift;      // 1 << head_shift CTAs take as many key heads side by side (8-bit cache, few rows)
     int box;             // tokens of a TMA box of the cache, 0: copied row by row
     int q_box;           // whether the rows of q go by TMA

@@ -194,6 +194,7 @@ AttnArgs attn_args(const pp_cache& c, const BatchArgs& batch, const PageArgs& pa
     a.n_kv_heads = c.n_kv_heads;
     a.group = c.n_heads / c.n_kv_heads;
     a.head_dim = c.head_dim;
+    a.max_rows = 0xffffffffu;
     a.scale_log2 = (float)((double)scale * 1.4426950408889634);
     a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + L.part);
     a.tails = static_cast<char*>(ws) + L.tails;

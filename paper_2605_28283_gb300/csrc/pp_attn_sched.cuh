@@ -43,6 +43,14 @@ struct Sched {
     PP_DEVINL int shift() const { return GROUPED ? shift_ : 0; }
     PP_DEVINL int heads() const { return a->n_kv_heads >> shift(); }
 
+    // Sequence b, without its tokens where another launch takes it.
+    PP_DEVINL Seq sequence(int b) const {
+        Seq s = load_seq(a->batch, b);
+        const unsigned rows = (unsigned)s.n * (unsigned)a->group;
+        if (rows < a->min_rows || rows > a->max_rows) s.n = 0;
+        return s;
+    }
+
     PP_DEVINL int row_tiles(const Seq& s) const { return (int)(((unsigned)s.n * (unsigned)a->group + ROWS - 1) / ROWS); }
 
     // Entries that row tile j's rows may see (all of a masked tree's).
@@ -116,7 +124,7 @@ struct Walk {
     PP_DEVINL void enter(int b_, long long base_) {
         b = b_;
         base = base_;
-        seq = load_seq(sched.a->batch, b);
+        seq = sched.sequence(b);
         m = sched.row_tiles(seq);
         h = 0;
         j = 0;
@@ -177,7 +185,7 @@ PP_DEVINL Walk<ROWS, TOK, GROUPED> start_walk(const AttnArgs* a, int lane, bool 
     long long mine = 0, items = 0;
 #pragma unroll 2
     for (int b = b0; b < b1; b++) {
-        const Seq q = load_seq(a->batch, b);
+        const Seq q = w.sched.sequence(b);
         if (report && q.bad) record_status(a->status, PP_ERR_INVALID_ARG);
         mine += w.sched.head_tiles(q);
         if (GROUPED) items += w.sched.row_tiles(q);
@@ -209,7 +217,7 @@ PP_DEVINL Walk<ROWS, TOK, GROUPED> start_walk(const AttnArgs* a, int lane, bool 
     if (here) {
 #pragma unroll 1
         for (; b + 1 < b1; b++) {
-            const long long t = w.sched.head_tiles(load_seq(a->batch, b)) * w.sched.heads();
+            const long long t = w.sched.head_tiles(w.sched.sequence(b)) * w.sched.heads();
             if (base + t > w.at) break;
             base += t;
         }
