@@ -503,7 +503,10 @@ size_t pp_kvq_workspace_size(const pp_cache8 *cache);
    finite magnitude of its new entries; a block that holds cached ones keeps
    its scale unless 448 times it is less than that, and then gets the new
    entries' scale, its cached codes rounded again at it.  So the block that the
-   first new token falls into is rewritten: it belongs to one sequence. */
+   first new token falls into is rewritten: it belongs to one sequence.  Scales
+   do not shrink while entries stay: a drafted token that made its block's
+   scale grow leaves it so when it is rejected, and cached values below 2^-6 of
+   that scale are held in steps of 2^-9 of it. */
 pp_status pp_kvq_append(const pp_cache8 *cache, const pp_batch *batch, const pp_head_norm *norm, const pp_rotation *rot,
                         const int32_t *positions, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
                         const void *v, int64_t v_stride, void *q_out, int64_t q_out_stride, void *ws, size_t ws_bytes,
@@ -526,7 +529,9 @@ pp_status pp_kvq_read(const pp_cache8 *cache, const pp_batch *batch, void *k_out
    element exactly down to 2^-14 of its head's largest, and below to 2^-21 of
    the largest; and a weight, times its block's value scale, to 2^-8 of itself
    (as in bf16) or 2^-41 of the largest such product of its row.  With more
-   rows, the codes are made bf16 (exact for powers of two as scales). */
+   rows, the codes are made bf16 (exact for powers of two as scales), which
+   costs more than reading half the bytes saves: for drafted trees and prompts
+   pp_tree_attention over a bf16 cache is the faster call. */
 pp_status pp_kvq_tree_attention(const pp_cache8 *cache, const pp_batch *batch, const void *q, int64_t q_stride,
                              const uint32_t *mask, int mask_words, float scale, void *out, int64_t out_stride, void *ws,
                              size_t ws_bytes, void *stream);

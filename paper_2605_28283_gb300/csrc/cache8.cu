@@ -22,10 +22,11 @@ namespace {
 // registers: its largest magnitude is known before anything is written, and
 // every element is read once.  The strips of a longer block meet in shared
 // memory.  The other CTAs take a token's query heads, as in norm_kernel.  8192
-// tokens of 40 + 40 + 40 heads of 128, bf16, blocks of 64, normed (399 MB): 107 us,
-// 3.7 TB/s (0.55 of the copy rate), 95 of it for the keys and values, which 16
-// warps an SM do not keep on their way (blocks of 16: 68; without norms 57); 64
-// single tokens: 5.3 us, a chain of latencies.
+// tokens of 40 + 40 + 40 heads of 128, bf16, blocks of 64, normed (399 MB): 108 us,
+// 3.7 TB/s (0.55 of the copy rate); the keys and values are most of it, of which 16
+// warps an SM keep too little on its way.  Blocks of 16: 100 us, of 128: 176;
+// without norms 88; fp32 (719 MB) 256.  64 single tokens: 5.4 us, a chain of
+// latencies.
 constexpr int kMaxStrips = 16;  // warps of a CTA at most (8 where that does)
 constexpr int kAppend8Smem = 216 * 1024;
 
@@ -530,8 +531,8 @@ __global__ void __launch_bounds__(256) read8_kernel(const Read8Args a, const int
 // place and without a barrier between warps: path[j] >= j, so what is read lies
 // at or past what is written, and rows of one batch are read by the whole warp
 // before any is written.  32 sequences of 8 accepted tokens in 32 layers (34 MB):
-// 21 us, half of it instructions (codes apart and together again) and the rest
-// the chain path - places - codes - stores; one sequence: 5.0 us.
+// 20 to 21 us (paths in their place already 18), half of it instructions (codes apart and together again) and the rest
+// the chain path - places - codes - stores; one sequence: 4.9 us.
 constexpr int kMoveBatch = 4;
 constexpr int kMoveChunk = 128;  // entries of a destination block at most
 
