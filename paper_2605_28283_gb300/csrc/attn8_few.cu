@@ -49,9 +49,10 @@ namespace pp {
 namespace {
 
 constexpr int kFewRows = 8;         // rows of an item
-// Tiles that an item counts more than it has: 0 / 2 / 4 / 8, 64 ragged single tokens 112.5 / 104.7 / 106.3 / 107.9 us.
+// Tiles that an item counts more than it has: 0 / 2 / 4 / 8, 64 ragged single tokens 100.2 / 99.0 / 99.1 / 102.6 us.
 constexpr int kPad = 2;
-constexpr float kLazy8 = 2.0f;      // growth of the base (log2) that O absorbs unscaled
+// Growth of the base (log2) that O absorbs unscaled: 1 / 2 / 3, 100.5 / 99.0 / 98.2 us; 3 costs small weights a bit.
+constexpr float kLazy8 = 2.0f;
 // The largest weight at its base, in codes: 2^kLazy8 times that, times the fraction of a scale (below 2), stays below 448.
 constexpr float kTopWeight = 32.f;
 constexpr int kFacTiles = 8;        // tiles whose scales are held
