@@ -382,14 +382,6 @@ def _devices(what, device):
     raise PPError(PP_ERR_INVALID_ARG, what + (": tensors must be on a CUDA device" if device < 0 else ": tensors of several devices"))
 
 
-def _handle_off(device, *handles):
-    """Whether a handle (or None) has tensors on another device."""
-    for h in handles:
-        if h is not None and h.device != device and h.device is not None:
-            return True
-    return False
-
-
 def _stream_handle(stream) -> int:
     if stream is None:
         return _current_stream()
@@ -602,7 +594,8 @@ def pp_head_norm_rope(norm, rot, positions, q, k, q_out, k_out, stream=None):
     pos = _positions_of(rot, positions, T, what)
     d = q.get_device()
     if d < 0 or q_out.get_device() != d or (k is not None and (k.get_device() != d or k_out.get_device() != d)) or \
-            (rot is not None and (rot.device != d or positions.get_device() != d)) or _handle_off(d, norm):
+            (rot is not None and (rot.device != d or positions.get_device() != d)) or \
+            (norm.device != d and norm.device is not None):
         _devices(what, d)
     _check(load().pp_head_norm_rope(_torch_dtype(dt), norm.ref, None if rot is None else rot.ref,
                                     pos, T, H, Hkv, D, pq, sq, pk, sk, po, so, pko, sko, _stream_handle(stream)), what)
@@ -645,7 +638,7 @@ def pp_head_norm_rope_grad(norm, rot, positions, q, k, q_grad, k_grad, dq, dk, d
     pos = _positions_of(rot, positions, T, what)
     gamma_grads = _gamma_grad(dq_gamma, D, what + ": dq_gamma"), _gamma_grad(dk_gamma, D, what + ": dk_gamma")
     d = q.get_device()
-    if d < 0 or _handle_off(d, norm, rot) or any(
+    if d < 0 or (norm.device != d and norm.device is not None) or (rot is not None and rot.device != d) or any(
             t is not None and t.get_device() != d
             for t in (k, q_grad, dq, dq_gamma, dk_gamma, ws) + (() if k is None else (k_grad, dk)) + (() if rot is None else (positions,))):
         _devices(what, d)
@@ -746,7 +739,8 @@ def pp_kvq_append(cache, batch, norm, rot, positions, q, k, v, q_out, ws, stream
     d = cache.device
     if d < 0 or batch.device != d or k.get_device() != d or v.get_device() != d or ws.get_device() != d or \
             (q is not None and q.get_device() != d) or (q_out is not None and q_out.get_device() != d) or \
-            (positions is not None and positions.get_device() != d) or _handle_off(d, norm, rot):
+            (positions is not None and positions.get_device() != d) or (rot is not None and rot.device != d) or \
+            (norm is not None and norm.device != d and norm.device is not None):
         _devices("pp_kvq_append", d)
     _check(load().pp_kvq_append(cache.ref, batch.ref, None if norm is None else norm.ref, None if rot is None else rot.ref,
                                 pos, pq, sq, pk, sk, pv, sv, po, so, *w, _stream_handle(stream)),
